@@ -442,7 +442,9 @@ def _lin8_plain(s):
     for r in range(0, c["N"], rows):
         xr = x[r:r + rows].float()
         big = xr.abs().amax(1, keepdim=True)
-        q = torch.round(xr * torch.where(big > 0, 127.0 / big, torch.zeros_like(big)))
+        # (one division: torch forms 127.0 / big from a rounded reciprocal)
+        per = torch.div(torch.full_like(big, 127.0), big)
+        q = torch.round(xr * torch.where(big > 0, per, torch.zeros_like(big)))
         D = (q @ w) * ((big / 127.0) * s["sw"]) + s["b"]
         if c["gelu"]:
             D = _erf_gelu(D)
