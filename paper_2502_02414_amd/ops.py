@@ -1,0 +1,435 @@
+"""Thin Python binding of include/pa_ops.h, beside ``binding`` (same library,
+same manner): the operators around the block stack.
+
+  pa_residual_norm(_backward)  norm after a block, its gate and residual scale,
+                               the residual add, norm before the next block
+  pa_adamw                     one AdamW step over many tensors, moments in 32
+                               or in 8 bits; ``AdamW`` keeps a model's moments
+  pa_linear_i8                 a linear layer in 8-bit integers (pa_quant_rows,
+                               pa_quant_weight, pa_gemm_i8: its parts)
+
+Tensors are contiguous GPU tensors on the current device; outputs are passed
+in.  Each wrapper checks device, dtype, size and contiguity against the call,
+and raises ValueError, or PAError with the library's message.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import binding as B
+from .binding import PA_BF16, PA_F32, PAError  # noqa: F401
+
+SYMBOLS = (
+    "pa_ops_version", "pa_residual_norm", "pa_residual_norm_backward",
+    "pa_residual_norm_workspace", "pa_adamw", "pa_adamw_unpack", "pa_quant_rows",
+    "pa_quant_weight", "pa_gemm_i8", "pa_linear_i8", "pa_linear_i8_workspace",
+)
+
+NORMS = {None: 0, "none": 0, "layer": 1, "rms": 2}
+GATES = {"linear": 0, "sigmoid": 1}
+ACTS = {None: 0, "none": 0, "gelu": 1}
+BLOCK = 256  # elements that share a scale of the 8-bit moments
+
+_P = ctypes.c_void_p
+
+
+class pa_residual_norm_params(ctypes.Structure):
+    _fields_ = [("post", ctypes.c_int32), ("pre", ctypes.c_int32), ("gate", ctypes.c_int32),
+                ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float),
+                ("alpha", ctypes.c_float), ("post_g", _P), ("post_b", _P), ("scale", _P),
+                ("pre_g", _P), ("pre_b", _P)]
+
+
+class pa_residual_norm_grads(ctypes.Structure):
+    _fields_ = [(n, _P) for n in ("dpost_g", "dpost_b", "dscale", "dpre_g", "dpre_b")]
+
+
+class pa_adamw_item(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64)] + [(k, _P) for k in (
+        "p", "copy", "g", "m", "v", "m_scale", "v_scale")] + [
+            ("wd", ctypes.c_float), ("g_dtype", ctypes.c_int32)]
+
+
+class pa_adamw_args(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("gscale", _P), ("lr_dev", _P), ("step_dev", _P)]
+
+
+_lib = None
+
+
+def load():
+    """libpa.so with this header's calls declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = B.load()
+    I64, I32, S = ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+    Sp = ctypes.POINTER(S)
+    NP, NG = ctypes.POINTER(pa_residual_norm_params), ctypes.POINTER(pa_residual_norm_grads)
+    lib.pa_residual_norm.argtypes = [I64, I32, I32, NP, _P, _P, _P, _P, _P, _P, _P, _P]
+    lib.pa_residual_norm_backward.argtypes = [I64, I32, I32, NP] + [_P] * 8 + [NG, _P, S, _P]
+    lib.pa_residual_norm_workspace.argtypes = [I64, I32, I32, Sp]
+    lib.pa_adamw.argtypes = [I32, ctypes.POINTER(pa_adamw_item), ctypes.POINTER(pa_adamw_args), _P]
+    lib.pa_adamw_unpack.argtypes = [I64, _P, _P, I32, _P, _P]
+    lib.pa_quant_rows.argtypes = [I64, I32, I32, _P, _P, _P, _P]
+    lib.pa_quant_weight.argtypes = [I32, I32, I32, _P, _P, _P, _P]
+    lib.pa_gemm_i8.argtypes = [I64, I32, I32, _P, _P, _P, _P, _P, I32, _P, _P, I32, _P]
+    lib.pa_linear_i8.argtypes = [I64, I32, I32, _P, I32, _P, _P, _P, I32, _P, _P, I32, _P, S, _P]
+    lib.pa_linear_i8_workspace.argtypes = [I64, I32, I32, Sp]
+    for name in SYMBOLS:
+        getattr(lib, name).restype = ctypes.c_int
+    _lib = lib
+    return lib
+
+
+def _check(status: int):
+    if status != B.PA_OK:
+        raise PAError(status, load().pa_last_error().decode())
+
+
+def _code(dtype, name):
+    code = B._codes[dtype]
+    if code is None:
+        raise ValueError(f"{name}: dtype {dtype} is neither float32 nor bfloat16")
+    return code
+
+
+def _dev(t, name):
+    """Pointer of a contiguous tensor on the current device."""
+    p = B._ptr(t)
+    if t.is_cuda and t.get_device() != _current_device():
+        raise ValueError(f"{name}: on {t.device}, not on the current device")
+    return p
+
+
+_device = None
+
+
+def _current_device() -> int:
+    global _device
+    if _device is None:
+        import torch
+        torch.cuda.current_device()
+        _device = torch._C._cuda_getDevice
+    return _device()
+
+
+def _in(t, n, dtype, name, required=True):
+    """Pointer of t after checking it against n elements of a torch dtype."""
+    if t is None:
+        if required:
+            raise ValueError(f"{name} is required")
+        return None
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
+    if t.numel() != n:
+        raise ValueError(f"{name}: {t.numel()} elements, the call needs {n}")
+    return _dev(t, name)
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def pa_ops_version() -> int:
+    return load().pa_ops_version()
+
+
+# ---- the joint between two blocks ----
+class ResidualNormParams:
+    """The host struct of the joint's parameters and the tensors it points at."""
+
+    def __init__(self, st, C, tensors):
+        self.st, self.C, self.tensors = st, C, tensors
+        self.ref = ctypes.byref(st)
+        self.pre = st.pre
+        self.post = st.post
+
+
+def _vectors(named):
+    """Pointers of fp32 vectors of one length, and that length."""
+    f32, C, out = _torch().float32, None, {}
+    for k, t in named.items():
+        if t is not None:
+            C = t.numel() if C is None else C
+            out[k] = _in(t, C, f32, k)
+    return out, C
+
+
+def make_residual_norm_params(post=None, pre=None, alpha=1.0, scale=None, gate="sigmoid",
+                              post_g=None, post_b=None, pre_g=None, pre_b=None, post_eps=1e-5,
+                              pre_eps=1e-5) -> ResidualNormParams:
+    """post, pre: None, "layer" or "rms"; scale and the gains and biases: fp32
+    [C] or None; gate: "linear" or "sigmoid" (of the gate tensor t, where a
+    call has one)."""
+    for what, v, table in (("post", post, NORMS), ("pre", pre, NORMS), ("gate", gate, GATES)):
+        if v not in table:
+            raise ValueError(f"{what}: {v!r} is not one of {sorted(map(str, table))}")
+    named = dict(post_g=post_g, post_b=post_b, scale=scale, pre_g=pre_g, pre_b=pre_b)
+    ptr, C = _vectors(named)
+    st = pa_residual_norm_params(NORMS[post], NORMS[pre], GATES[gate], float(post_eps),
+                                 float(pre_eps), float(alpha), *(ptr.get(k) for k in named))
+    return ResidualNormParams(st, C, named)
+
+
+class ResidualNormGrads:
+    def __init__(self, st, C, tensors):
+        self.C, self.tensors, self.ref = C, tensors, ctypes.byref(st)
+
+
+def make_residual_norm_grads(dpost_g=None, dpost_b=None, dscale=None, dpre_g=None,
+                             dpre_b=None) -> ResidualNormGrads:
+    """fp32 [C] outputs of the backward, each optional."""
+    named = dict(dpost_g=dpost_g, dpost_b=dpost_b, dscale=dscale, dpre_g=dpre_g, dpre_b=dpre_b)
+    ptr, C = _vectors(named)
+    return ResidualNormGrads(pa_residual_norm_grads(*(ptr.get(k) for k in named)), C, named)
+
+
+def _joint(x, name, par, gr=None):
+    if x.dim() != 2:
+        raise ValueError(f"{name} must be [N, C]")
+    N, C = x.shape
+    for s in (par, gr):
+        if s is not None and s.C is not None and s.C != C:
+            raise ValueError(f"{name} has {C} channels, the parameters {s.C}")
+    return N, C, N * C, _code(x.dtype, name)
+
+
+def padded(K: int) -> int:
+    """Bytes between the rows of an int8 matrix of K columns."""
+    return (K + 15) // 16 * 16
+
+
+def pa_residual_norm(x, y, par, x1, h=None, t=None, hq=None, hs=None, stream=None):
+    """x1 = alpha x + scale gate(t) post(y); h = pre(x1), in x's dtype (h) and /
+    or as int8 rows hq [N, padded(C)] with scales hs [N]."""
+    N, C, n, code = _joint(x, "x", par)
+    dt = x.dtype
+    if hq is not None:
+        torch = _torch()
+        hqp = _in(hq, N * padded(C), torch.int8, "hq")
+        hsp = _in(hs, N, torch.float32, "hs")
+    else:
+        hqp, hsp = None, (None if hs is None else _dev(hs, "hs"))
+    _check(load().pa_residual_norm(
+        N, C, code, par.ref, _dev(x, "x"), _in(y, n, dt, "y"), _in(t, n, dt, "t", False),
+        _in(x1, n, dt, "x1"), _in(h, n, dt, "h", False), hqp, hsp, B._stream(stream)))
+
+
+def residual_norm_workspace(N, C, dtype, device="cuda"):
+    """A uint8 workspace for the backward of [N, C] tensors of a torch dtype."""
+    k = ctypes.c_size_t(0)
+    _check(load().pa_residual_norm_workspace(N, C, _code(dtype, "dtype"), ctypes.byref(k)))
+    return _torch().empty(k.value, dtype=_torch().uint8, device=device)
+
+
+def pa_residual_norm_backward(x1, y, par, dx1, dh, dx, dy, gr=None, ws=None, t=None, dt=None,
+                              stream=None):
+    """The chain rule: dx1 and dh (either may be None) to dx, dy, dt and the
+    parameters' gradients gr (make_residual_norm_grads)."""
+    N, C, n, code = _joint(x1, "x1", par, gr)
+    ty = x1.dtype
+    _check(load().pa_residual_norm_backward(
+        N, C, code, par.ref, _dev(x1, "x1"), _in(y, n, ty, "y"), _in(t, n, ty, "t", False),
+        _in(dx1, n, ty, "dx1", False), _in(dh, n, ty, "dh", False), _in(dx, n, ty, "dx"),
+        _in(dy, n, ty, "dy"), _in(dt, n, ty, "dt", False), gr.ref if gr is not None else None,
+        None if ws is None else _dev(ws, "ws"), B._nbytes(ws), B._stream(stream)))
+
+
+# ---- AdamW ----
+class AdamWItems:
+    """The host array of pa_adamw's tensors; ``set_grad`` exchanges a gradient."""
+
+    def __init__(self, n):
+        self.n = n
+        self.arr = (pa_adamw_item * max(n, 1))()
+        self.tensors = [None] * n
+
+    def set_grad(self, i, g):
+        it = self.arr[i]
+        if g.numel() != it.n:
+            raise ValueError(f"g of item {i}: {g.numel()} elements, the item has {it.n}")
+        code = _code(g.dtype, "g")
+        it.g = _dev(g, "g")
+        it.g_dtype = code
+        self.tensors[i]["g"] = g
+
+
+def make_adamw_items(items) -> AdamWItems:
+    """items: dicts with p (fp32), g (fp32 or bf16), m and v (fp32; or uint8
+    with m_scale and v_scale, fp32 [ceil(n / 256)]), optionally copy (bf16)
+    and wd."""
+    torch = _torch()
+    f32 = torch.float32
+    out = AdamWItems(len(items))
+    for i, d in enumerate(items):
+        extra = set(d) - {"p", "g", "m", "v", "m_scale", "v_scale", "copy", "wd"}
+        if extra:
+            raise ValueError(f"item {i}: unknown {sorted(extra)}")
+        n, it = d["p"].numel(), out.arr[i]
+        q8 = d.get("m_scale") is not None or d.get("v_scale") is not None
+        state, blocks = torch.uint8 if q8 else f32, -(-n // BLOCK)
+        it.n = n
+        it.p = _in(d["p"], n, f32, "p")
+        it.copy = _in(d.get("copy"), n, torch.bfloat16, "copy", False)
+        it.m, it.v = _in(d["m"], n, state, "m"), _in(d["v"], n, state, "v")
+        if q8:
+            it.m_scale = _in(d.get("m_scale"), blocks, f32, "m_scale")
+            it.v_scale = _in(d.get("v_scale"), blocks, f32, "v_scale")
+        it.wd = float(d.get("wd", 0.0))
+        out.tensors[i] = dict(d)
+        if d.get("g") is not None:
+            out.set_grad(i, d["g"])
+    return out
+
+
+def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale=None,
+             lr_dev=None, step_dev=None, stream=None):
+    """One step over the tensors of make_adamw_items; gscale: a device fp32
+    scalar that every gradient is multiplied by; lr_dev (fp32), step_dev
+    (int64): device scalars in place of lr and step, for captured graphs."""
+    torch = _torch()
+    a = pa_adamw_args(float(lr), float(beta1), float(beta2), float(eps), int(step),
+                      int(seed) & 0xFFFFFFFFFFFFFFFF,
+                      _in(gscale, 1, torch.float32, "gscale", False),
+                      _in(lr_dev, 1, torch.float32, "lr_dev", False),
+                      _in(step_dev, 1, torch.int64, "step_dev", False))
+    _check(load().pa_adamw(items.n, items.arr, ctypes.byref(a), B._stream(stream)))
+
+
+def pa_adamw_unpack(codes, scales, out, signed, stream=None):
+    """The values of 8-bit moments (signed: m's codes) as fp32."""
+    torch = _torch()
+    n = codes.numel()
+    _check(load().pa_adamw_unpack(
+        n, _in(codes, n, torch.uint8, "codes"), _in(scales, -(-n // BLOCK), torch.float32, "scales"),
+        int(bool(signed)), _in(out, n, torch.float32, "out"), B._stream(stream)))
+
+
+class AdamW:
+    """AdamW over named fp32 tensors, e.g. a block stack's parameters: the
+    moments (fp32, or 8 bits where a tensor has at least ``small`` elements)
+    and one pa_adamw call per step.
+
+    params: {name: fp32 tensor}; copies: {name: bf16 tensor} that receive the
+    parameters rounded (what the stack's products read); decay: names with
+    weight decay (default: tensors of more than one dimension)."""
+
+    def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, wd=0.01, bits=32, copies=None,
+                 decay=None, small=4096, seed=0):
+        torch = _torch()
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        self.lr, self.betas, self.eps, self.seed, self.t = lr, betas, eps, seed, 0
+        self.names = list(params)
+        copies = copies or {}
+        unknown = [k for k in list(copies) + list(decay or ()) if k not in params]
+        if unknown:
+            raise ValueError(f"not among the parameters: {unknown}")
+        items = []
+        for k, p in params.items():
+            d = {"p": p, "copy": copies.get(k)}
+            d["wd"] = wd if (k in decay if decay is not None else p.dim() > 1) else 0.0
+            if bits == 8 and p.numel() >= small:
+                nb = -(-p.numel() // BLOCK)
+                for s in "mv":
+                    d[s] = torch.zeros(p.numel(), dtype=torch.uint8, device=p.device)
+                    d[s + "_scale"] = torch.zeros(nb, dtype=torch.float32, device=p.device)
+            else:
+                d["m"], d["v"] = torch.zeros_like(p), torch.zeros_like(p)
+            items.append(d)
+        self.items = make_adamw_items(items)
+
+    def step(self, grads, gscale=None, lr=None, stream=None):
+        """grads: {name: tensor} for every parameter (fp32 or bf16)."""
+        for i, k in enumerate(self.names):
+            self.items.set_grad(i, grads[k])
+        pa_adamw(self.items, self.lr if lr is None else lr, self.t + 1, *self.betas, self.eps,
+                 self.seed, gscale, stream=stream)
+        self.t += 1
+
+    def moments(self, name):
+        """(m, v) of a parameter as fp32 tensors."""
+        torch = _torch()
+        d = self.items.tensors[self.names.index(name)]
+        if d.get("m_scale") is None:
+            return d["m"].clone(), d["v"].clone()
+        out = []
+        for s in "mv":
+            o = torch.empty(d["p"].shape, dtype=torch.float32, device=d["p"].device)
+            pa_adamw_unpack(d[s], d[s + "_scale"], o, signed=s == "m")
+            out.append(o)
+        return tuple(out)
+
+
+# ---- 8-bit integer products ----
+def pa_quant_rows(x, q, s, stream=None):
+    """x [N, K] to int8 rows q [N, padded(K)] with scales s [N]."""
+    torch = _torch()
+    N, K = x.shape
+    _check(load().pa_quant_rows(N, K, _code(x.dtype, "x"), _dev(x, "x"),
+                                _in(q, N * padded(K), torch.int8, "q"),
+                                _in(s, N, torch.float32, "s"), B._stream(stream)))
+
+
+def pa_quant_weight(W, Wq, sw, stream=None):
+    """W [K, F] to Wq [F, padded(K)] int8 with a scale per output channel."""
+    torch = _torch()
+    K, F = W.shape
+    _check(load().pa_quant_weight(K, F, _code(W.dtype, "W"), _dev(W, "W"),
+                                  _in(Wq, F * padded(K), torch.int8, "Wq"),
+                                  _in(sw, F, torch.float32, "sw"), B._stream(stream)))
+
+
+def quant_weight(W):
+    """(Wq, sw) of a weight [K, F], in new tensors."""
+    torch = _torch()
+    K, F = W.shape
+    Wq = torch.empty(F, padded(K), dtype=torch.int8, device=W.device)
+    sw = torch.empty(F, dtype=torch.float32, device=W.device)
+    pa_quant_weight(W, Wq, sw)
+    return Wq, sw
+
+
+def _product(K, wq, sw, D, bias, act, C):
+    torch = _torch()
+    if D.dim() != 2:
+        raise ValueError("D must be [N, F]")
+    if act not in ACTS:
+        raise ValueError(f"act: {act!r} is not one of {sorted(map(str, ACTS))}")
+    N, F = D.shape
+    f32 = torch.float32
+    return (N, F, (_in(wq, F * padded(K), torch.int8, "Wq"), _in(sw, F, f32, "sw"),
+                   _in(bias, F, f32, "bias", False), ACTS[act],
+                   _in(C, N * F, D.dtype, "C", False), _dev(D, "D"), _code(D.dtype, "D")))
+
+
+def pa_gemm_i8(q, s, wq, sw, D, K=None, bias=None, act=None, C=None, stream=None):
+    """D = act(s sw (q wq^T) + bias) + C from int8 rows q [N, padded(K)] (K:
+    q's width when not given) and weights wq [F, padded(K)]."""
+    torch = _torch()
+    K = q.shape[1] if K is None else K
+    N, F, rest = _product(K, wq, sw, D, bias, act, C)
+    _check(load().pa_gemm_i8(N, F, K, _in(q, N * padded(K), torch.int8, "q"),
+                             _in(s, N, torch.float32, "s"), *rest, B._stream(stream)))
+
+
+def linear_i8_workspace(N, K, F, device="cuda"):
+    """A uint8 workspace for pa_linear_i8 at these sizes."""
+    k = ctypes.c_size_t(0)
+    _check(load().pa_linear_i8_workspace(N, F, K, ctypes.byref(k)))
+    return _torch().empty(k.value, dtype=_torch().uint8, device=device)
+
+
+def pa_linear_i8(x, wq, sw, D, ws, bias=None, act=None, C=None, stream=None):
+    """D [N, F] = act(x W + bias) + C with x [N, K] quantised row by row and W
+    as pa_quant_weight left it."""
+    N, K = x.shape
+    Nd, F, rest = _product(K, wq, sw, D, bias, act, C)
+    if Nd != N:
+        raise ValueError(f"D has {Nd} rows, x {N}")
+    _check(load().pa_linear_i8(N, F, K, _dev(x, "x"), _code(x.dtype, "x"), *rest, _dev(ws, "ws"),
+                               B._nbytes(ws), B._stream(stream)))

@@ -1,0 +1,605 @@
+"""The operators of include/pa_ops.h on the GPU against 64 bits (ops_ref.py).
+
+A bound is half a step of the stored type, relative to the value, plus the
+magnitude of a 32-bit evaluation's error in units of 2^-24, which the reference
+carries along (the sums of absolute values of what is added and multiplied)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import ops_ref as R
+from paper_2502_02414_amd import ops
+from pa_cases import say
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+DT = {"f32": F32, "bf16": BF16}
+
+
+def draw(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def dev(t):
+    return None if t is None else t.cuda()
+
+
+def within(got, ref, err, dt, name, extra=0.0):
+    got, ref, err = got.cpu().double(), ref.expand(got.shape), err.expand(got.shape)
+    bound = R.half_step(dt) * ref.abs() * (1 + 2 ** -8) + R.U * err + extra + 1e-37
+    off = (got - ref).abs()
+    assert torch.isfinite(got).all(), name
+    worst = (off / bound).max().item()
+    assert worst <= 1, f"{name}: {worst:.3g} of the bound at {(off / bound).argmax().item()}"
+    return worst
+
+
+# ---- the joint between two blocks ----
+def joint_case(N, C, dt, post, pre, gated, alpha, full, seed=1):
+    g = draw(seed + N + C)
+    rnd = lambda *s: torch.randn(*s, generator=g)
+    p = {"post": post, "pre": pre, "alpha": alpha, "gate": gated or "sigmoid"}
+    if full:
+        p["scale"] = 0.5 + 0.3 * rnd(C)
+        if post:
+            p["post_g"], p["post_b"] = 1 + 0.2 * rnd(C), 0.2 * rnd(C)
+        if pre:
+            p["pre_g"], p["pre_b"] = 1 + 0.2 * rnd(C), 0.2 * rnd(C)
+    d = {"x": rnd(N, C) + 0.5 * rnd(C), "y": 2 * rnd(N, C) + rnd(C), "dx1": rnd(N, C),
+         "dh": rnd(N, C), "t": 2 * rnd(N, C) if gated else None}
+    return p, {k: None if v is None else v.to(dt) for k, v in d.items()}
+
+
+def params(p):
+    kw = {k: dev(v) if torch.is_tensor(v) else v for k, v in p.items()}
+    return ops.make_residual_norm_params(**kw)
+
+
+JOINTS = [
+    # N, C, post, pre, gate, alpha, gains and biases
+    (1, 16, "layer", "layer", None, 1.0, True),
+    (1, 256, "layer", "rms", "sigmoid", 1.0, True),
+    (3, 24, "rms", "layer", "linear", 0.75, True),
+    (257, 40, None, "layer", "sigmoid", 1.0, True),
+    (1000, 64, "layer", None, None, -1.5, True),
+    (4096, 64, "layer", "layer", None, 1.0, False),
+    (777, 96, "rms", "rms", "sigmoid", 1.0, True),
+    (5001, 256, "layer", "layer", None, 1.0, True),
+    (2048, 256, None, None, "linear", 2.0, False),
+    (1003, 264, "rms", "layer", "sigmoid", 1.0, True),
+    (513, 512, "layer", "rms", None, 1.0, True),
+    (300, 520, "layer", "layer", "sigmoid", 1.0, True),
+    (129, 1000, "rms", "rms", "linear", 0.5, True),
+    (65, 4096, "layer", "layer", "sigmoid", 1.0, True),
+]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C,post,pre,gated,alpha,full", JOINTS)
+def test_joint_forward(dt, N, C, post, pre, gated, alpha, full):
+    say(f"joint forward {dt} N={N} C={C} {post} {pre} {gated}")
+    ty = DT[dt]
+    p, d = joint_case(N, C, ty, post, pre, gated, alpha, full)
+    x, y, t = dev(d["x"]), dev(d["y"]), dev(d["t"])
+    x1 = torch.full((N, C), 7.0, dtype=ty, device="cuda")
+    h = torch.full_like(x1, 7.0) if pre else None
+    par = params(p)
+    ops.pa_residual_norm(x, y, par, x1, h, t=t)
+    ref, err = R.joint(p, d["x"], d["y"], d["t"])
+    within(x1, ref, err, ty, "x1")
+    if not pre:
+        return
+    ref, err = R.pre(p, x1.cpu())
+    within(h, ref, err, ty, "h")
+    # h as int8 rows: the same x1; integers and scales of an fp32 h, within one
+    # integer where its error decides a border
+    Kp = ops.padded(C)
+    x1b, hq = torch.empty_like(x1), torch.full((N, Kp), 5, dtype=torch.int8, device="cuda")
+    hs = torch.empty(N, device="cuda")
+    ops.pa_residual_norm(x, y, par, x1b, None, t=t, hq=hq, hs=hs)
+    assert torch.equal(x1, x1b)
+    big = ref.abs().amax(1)
+    top = err.amax(1)
+    assert ((hs.cpu().double() - big / 127).abs() <= (2 * big + top) * R.U / 127 + 1e-37).all()
+    q = hq.cpu().double()
+    assert (q[:, C:] == 0).all()
+    slack = 0.5 + 127 * R.U * ((err + top[:, None]) / big[:, None] + 4)
+    assert ((q[:, :C] - 127 * ref / big[:, None]).abs() <= slack).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,C,post,pre,gated,alpha,full", JOINTS)
+@pytest.mark.parametrize("use", ["both", "dx1", "dh"])
+def test_joint_backward(dt, N, C, post, pre, gated, alpha, full, use):
+    if use == "dh" and not pre:
+        return
+    say(f"joint backward {dt} N={N} C={C} {post} {pre} {gated} {use}")
+    ty = DT[dt]
+    p, d = joint_case(N, C, ty, post, pre, gated, alpha, full)
+    dx1 = d["dx1"] if use != "dh" else None
+    dh = d["dh"] if use != "dx1" and pre else None
+    e = lambda: torch.full((N, C), 7.0, dtype=ty, device="cuda")
+    dx, dy, dt_ = e(), e(), e() if gated else None
+    names = ("dpost_g", "dpost_b", "dscale", "dpre_g", "dpre_b")
+    gr = {k: torch.full((C,), 7.0, device="cuda") for k in names}
+    ws = ops.residual_norm_workspace(N, C, ty)
+    ops.pa_residual_norm_backward(dev(d["x"]), dev(d["y"]), params(p), dev(dx1), dev(dh), dx, dy,
+                                  ops.make_residual_norm_grads(**gr), ws, t=dev(d["t"]), dt=dt_)
+    rec = ws.numel() // (20 * C)  # partial records: at most one running sum each
+    ref = R.joint_backward(p, d["x"], d["y"], d["t"], dx1, dh, N // rec + 300)
+    out = {"dx": dx, "dy": dy, "dt": dt_, **gr}
+    for k, (v, err) in ref.items():
+        within(out[k], v, err, F32 if k in gr else ty, k)
+    for k in names:  # without the norm: left as they are; without dh: zeros
+        if k.startswith("dpost") and not post or k.startswith("dpre") and not pre:
+            assert (gr[k] == 7).all()
+        elif k.startswith("dpre") and dh is None:
+            assert (gr[k] == 0).all()
+
+
+def test_joint_gradient_against_differences():
+    """Directional differences of the 64-bit forward against the kernel's fp32
+    gradients: step 1e-5, so the quotient is good to about 1e-9 of the terms."""
+    N, C = 37, 72
+    p, d = joint_case(N, C, F32, "layer", "rms", "sigmoid", 0.75, True, seed=5)
+    names = ("dpost_g", "dpost_b", "dscale", "dpre_g", "dpre_b")
+    gr = {k: torch.empty(C, device="cuda") for k in names}
+    x1 = R.joint(p, d["x"], d["y"], d["t"])[0]
+    out = {k: torch.empty(N, C, device="cuda") for k in ("dx", "dy", "dt")}
+    ops.pa_residual_norm_backward(dev(x1.float()), dev(d["y"]), params(p), dev(d["dx1"]),
+                                  dev(d["dh"]), out["dx"], out["dy"],
+                                  ops.make_residual_norm_grads(**gr),
+                                  ops.residual_norm_workspace(N, C, F32), t=dev(d["t"]),
+                                  dt=out["dt"])
+    out.update(gr)
+
+    def loss(z):
+        q = {**p, **{k: z[k] for k in z if k in p}}
+        x1 = R.joint(q, z["x"], z["y"], z["t"])[0]
+        return (d["dx1"].double() * x1 + d["dh"].double() * R.pre(q, x1)[0]).sum().item()
+
+    at = {k: v.double() for k, v in {**p, **d}.items() if torch.is_tensor(v)}
+    g = draw(9)
+    for k, name in (("x", "dx"), ("y", "dy"), ("t", "dt"), ("post_g", "dpost_g"),
+                    ("post_b", "dpost_b"), ("scale", "dscale"), ("pre_g", "dpre_g"),
+                    ("pre_b", "dpre_b")):
+        v = torch.randn(at[k].shape, generator=g, dtype=torch.float64)
+        diff = (loss({**at, k: at[k] + 1e-5 * v}) - loss({**at, k: at[k] - 1e-5 * v})) / 2e-5
+        terms = out[name].cpu().double() * v
+        assert abs(terms.sum().item() - diff) <= 1e-5 * terms.abs().sum().item(), k
+
+
+def test_joint_constant_and_extreme_rows():
+    """A row of one value (no spread), of zeros, of huge values, and gates far out."""
+    C = 64
+    x = torch.zeros(5, C)
+    y = torch.zeros(5, C)
+    y[1] = 3.0
+    y[2] = torch.linspace(-1e15, 1e15, C)
+    y[3, 0] = 1.0
+    t = torch.zeros(5, C)
+    t[3], t[4] = 200.0, -200.0
+    par = ops.make_residual_norm_params(post="layer", pre="rms")
+    x1, h = (torch.empty(5, C, device="cuda") for _ in range(2))
+    ops.pa_residual_norm(dev(x), dev(y), par, x1, h, t=dev(t))
+    p = {"post": "layer", "pre": "rms"}
+    ref, err = R.joint(p, x, y, t)
+    within(x1, ref, err, F32, "x1")
+    within(h, *R.pre(p, x1.cpu()), F32, "h")
+    o = {k: torch.empty(5, C, device="cuda") for k in ("dx", "dy", "dt")}
+    one = torch.ones(5, C)
+    ops.pa_residual_norm_backward(x1, dev(y), par, dev(one), dev(one), o["dx"], o["dy"], t=dev(t),
+                                  dt=o["dt"])
+    for k, (v, e) in R.joint_backward(p, x1.cpu(), y, t, one, one, 1).items():
+        if k in o:
+            within(o[k], v, e, F32, k)
+
+
+def test_joint_rows_that_are_not_finite_stay_their_own():
+    C = 128
+    p, d = joint_case(9, C, F32, "layer", "layer", None, 1.0, True)
+    clean = dev(d["x"])
+    bad = clean.clone()
+    bad[4, 7], bad[6, 3] = math.nan, math.inf
+    par, out = params(p), []
+    for x in (clean, bad):
+        x1, h = torch.empty_like(x), torch.empty_like(x)
+        hq = torch.empty(9, C, dtype=torch.int8, device="cuda")
+        hs = torch.empty(9, device="cuda")
+        ops.pa_residual_norm(x, dev(d["y"]), par, x1, h, hq=hq, hs=hs)
+        out.append((x1, h, hq, hs))
+    keep = [i for i in range(9) if i not in (4, 6)]
+    for a, b in zip(*out):
+        assert torch.equal(a[keep], b[keep])
+    x1, h, hq, hs = out[1]
+    assert torch.isnan(h[4]).all() and torch.isnan(h[6]).all()
+    assert (hq[[4, 6]] == 0).all() and torch.isnan(hs[[4, 6]]).all()
+
+
+def test_joint_repeats_bit_for_bit_and_leaves_what_lies_behind():
+    N, C = 10007, 256
+    p, d = joint_case(N, C, BF16, "layer", "layer", "sigmoid", 1.0, True)
+    par = params(p)
+    runs = []
+    for _ in range(2):
+        big = [torch.full((N + 3, C), 7.0, dtype=BF16, device="cuda") for _ in range(5)]
+        x1, h, dx, dy, dt = (b[:N] for b in big)
+        gr = {k: torch.empty(C, device="cuda") for k in ("dpost_g", "dscale", "dpre_b")}
+        ops.pa_residual_norm(dev(d["x"]), dev(d["y"]), par, x1, h, t=dev(d["t"]))
+        ops.pa_residual_norm_backward(x1, dev(d["y"]), par, dev(d["dx1"]), dev(d["dh"]), dx, dy,
+                                      ops.make_residual_norm_grads(**gr),
+                                      ops.residual_norm_workspace(N, C, BF16), t=dev(d["t"]), dt=dt)
+        assert all((b[N:] == 7).all() for b in big)
+        runs.append(big + list(gr.values()))
+    for a, b in zip(*runs):
+        assert torch.equal(a, b)
+
+
+# ---- AdamW ----
+def adam_tensors(sizes, seed, g_dtypes, q8, copies):
+    g = draw(seed)
+    rnd = lambda n: torch.randn(n, generator=g)
+    out = []
+    for i, n in enumerate(sizes):
+        size = torch.exp(2 * rnd(n) - 6)
+        d = {"p": 0.1 * rnd(n), "g": (size * rnd(n)).to(g_dtypes[i % len(g_dtypes)]),
+             "wd": 0.01 * (i % 2)}
+        m, v = 0.4 * size * rnd(n), 0.01 * size * size * torch.rand(n, generator=g)
+        if q8(n):
+            h = torch.full((n,), 32768)
+            d["m"], d["m_scale"] = R.encode(m, h, True)
+            d["v"], d["v_scale"] = R.encode(v, h, False)
+        else:
+            d["m"], d["v"] = m, v
+        if copies and i % 3 != 1:
+            d["copy"] = d["p"].to(BF16)
+        out.append(d)
+    return out
+
+
+def on_gpu(ts):
+    return [{k: dev(v) if torch.is_tensor(v) else v for k, v in d.items()} for d in ts]
+
+
+def check_step(before, after, step, seed, gscale=None, lr=1e-3, b1=0.9, b2=0.999, eps=1e-8):
+    """Every tensor after one step: moments and codes equal, p and the copy
+    within their bounds."""
+    for i, (a, b) in enumerate(zip(before, after)):
+        q8 = "m_scale" in a
+        m = R.decode(a["m"], a["m_scale"], True) if q8 else a["m"]
+        v = R.decode(a["v"], a["v_scale"], False) if q8 else a["v"]
+        p, m, v, upd = R.adamw(a["p"], a["g"], m, v, lr, b1, b2, eps, a["wd"], step, gscale)
+        got = {k: x.cpu() for k, x in b.items() if torch.is_tensor(x)}
+        # p: its own rounding, the update's few (sqrt, quotient, constants in fp32)
+        err = 2 * p.abs() + 16 * (lr * upd).abs() + 4 * abs(lr * a["wd"]) * a["p"].double().abs()
+        off = (got["p"].double() - p).abs()
+        assert (off <= R.U * err + 1e-37).all(), (i, (off / (R.U * err + 1e-37)).max())
+        if "copy" in got:
+            assert torch.equal(got["copy"], got["p"].to(BF16)), i
+        if not q8:
+            assert torch.equal(got["m"], m) and torch.equal(got["v"], v), i
+            continue
+        h = R.random_bits(m.numel(), seed, step, i)
+        for k, x, part, sgn in (("m", m, h & 0xFFFF, True), ("v", v, h >> 16, False)):
+            c, S = R.encode(x, part, sgn)
+            assert torch.equal(got[k + "_scale"], S), (i, k)
+            assert torch.equal(got[k], c), (i, k)
+
+
+SIZES = [1, 2, 3, 4, 5, 255, 256, 257, 1023, 4095, 4096, 4097, 10000, 65536, 100003]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["f32", "bf16", "mixed"])
+def test_adamw_steps(bits, grad):
+    say(f"adamw {bits} bits, {grad} gradients")
+    gd = {"f32": [F32], "bf16": [BF16], "mixed": [F32, BF16]}[grad]
+    # mixed: small tensors keep moments in 32 bits beside others in 8
+    q8 = lambda n: bits == 8 and (grad != "mixed" or n > 1000)
+    before = adam_tensors(SIZES, 3, gd, q8, True)
+    gs = torch.tensor([0.7])
+    for step in (1, 2, 1000):
+        t = on_gpu(before)
+        ops.pa_adamw(ops.make_adamw_items(t), lr=1e-3, step=step, gscale=gs.cuda(), seed=11 + (5 << 40))
+        check_step(before, t, step, 11 + (5 << 40), gs)
+        before = [{k: v.cpu() if torch.is_tensor(v) else v for k, v in d.items()} for d in t]
+
+
+def test_adamw_more_tensors_than_a_launch_takes():
+    sizes = [1 + (37 * i) % 700 for i in range(131)]
+    sizes[5] = sizes[50] = 5000
+    before = adam_tensors(sizes, 4, [F32], lambda n: n % 2 == 0, False)
+    empty = {"p": torch.empty(0), "g": torch.empty(0), "m": torch.empty(0), "v": torch.empty(0)}
+    t = on_gpu(before)
+    items = ops.make_adamw_items(t)
+    ops.pa_adamw(items, lr=1e-2, step=3, seed=2, beta1=0.0, beta2=0.5, eps=1e-3)
+    check_step(before, t, 3, 2, lr=1e-2, b1=0.0, b2=0.5, eps=1e-3)
+    ops.pa_adamw(ops.make_adamw_items([]), lr=1e-2)
+    ops.pa_adamw(ops.make_adamw_items(on_gpu([empty])), lr=1e-2)
+
+
+def test_adamw_extreme_gradients():
+    """Zeros, the smallest and largest magnitudes, and a block with an infinity or
+    a NaN: its moments are NaN from then on, other blocks are untouched by it."""
+    n = 256 * 6
+    g = torch.zeros(n)
+    g[256:512] = torch.logspace(-30, 15, 256)
+    g[512:768] = 1e-30 * torch.randn(256, generator=draw(1))
+    g[768 + 5] = math.inf
+    g[1024 + 9] = math.nan
+    g[1280:] = torch.randn(256, generator=draw(2))
+    z = torch.zeros(n, dtype=torch.uint8)
+    sc = torch.zeros(6)
+    before = [{"p": torch.ones(n), "g": g, "m": z, "v": z.clone(), "m_scale": sc,
+               "v_scale": sc.clone(), "wd": 0.0}]
+    t = on_gpu(before)
+    ops.pa_adamw(ops.make_adamw_items(t), lr=1e-3, step=1, seed=3)
+    keep = torch.ones(n, dtype=torch.bool)
+    keep[768:1280] = False
+    ok = [0, 1, 2, 5]
+    cut = lambda d: [{k: (x.cpu()[keep] if torch.is_tensor(x) and x.numel() == n else
+                          x.cpu()[ok] if torch.is_tensor(x) else x) for k, x in d[0].items()}]
+    got, ref = cut(t), cut(before)
+    v = t[0]["v_scale"].cpu()
+    assert torch.isnan(v[3]) and torch.isnan(v[4])
+    assert torch.isfinite(got[0]["p"]).all()
+    # the kept blocks as if alone: their random bits are those of their places
+    m = torch.zeros(n)
+    p, m, vv, _ = R.adamw(before[0]["p"], g, m, m.clone(), 1e-3, 0.9, 0.999, 1e-8, 0.0, 1)
+    h = R.random_bits(n, 3, 1, 0)
+    for k, x, part, sgn in (("m", m, h & 0xFFFF, True), ("v", vv, h >> 16, False)):
+        c, S = R.encode(x, part, sgn)
+        assert torch.equal(got[0][k], c[keep]) and torch.equal(got[0][k + "_scale"], S[ok])
+        out = torch.empty(n, device="cuda")
+        ops.pa_adamw_unpack(t[0][k], t[0][k + "_scale"], out, signed=sgn)
+        val = R.decode(c, S, sgn)
+        assert torch.equal(out.cpu()[keep], val[keep])
+        assert torch.isnan(out.cpu()[768:1280]).all()
+
+
+def test_adamw_8_bits_do_not_stand_still():
+    """A constant gradient of 1: after 400 steps v's mean is 1 - 0.999^400 = 0.330
+    and m's 1.  A value wanders by at most a code (1/8) a step with the chance
+    of its distance to it: v's variance is at most 400 * 0.001 * 0.33 * 0.041 / 4
+    and the mean of 65,536 of them is within 5 standard deviations 0.0008; a v
+    rounded to nearest would have stopped at 16 steps' worth."""
+    n = 65536
+    ones = torch.ones(n, device="cuda")
+    w = ops.AdamW({"w": torch.zeros(n, device="cuda")}, lr=0.0, bits=8, seed=7)
+    for _ in range(400):
+        w.step({"w": ones})
+    m, v = w.moments("w")
+    assert abs(v.mean().item() - (1 - 0.999 ** 400)) < 0.004
+    assert abs(m.mean().item() - 1) < 0.004
+
+
+# ---- 8-bit integer products ----
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K", [(1, 1), (1, 4096), (3, 7), (5, 16), (64, 17), (100, 64), (33, 100),
+                                 (1000, 256), (257, 1000), (40, 1024), (7, 8192), (9, 8200),
+                                 (2, 131072)])
+def test_quant_rows(dt, N, K):
+    say(f"quant rows {dt} {N} x {K}")
+    g = draw(N + K)
+    x = (torch.randn(N, K, generator=g) * torch.exp(torch.randn(N, 1, generator=g))).to(DT[dt])
+    if N > 4:
+        x[1] = 0
+        x[2] = 1e-37
+        x[3, 0] = math.inf
+        x[4, K - 1] = math.nan
+    q = torch.full((N, ops.padded(K)), 5, dtype=torch.int8, device="cuda")
+    s = torch.empty(N, device="cuda")
+    ops.pa_quant_rows(dev(x), q, s)
+    rq, rs = R.quant(x)
+    assert torch.equal(q.cpu(), R.padded(rq))
+    assert torch.equal(torch.nan_to_num(s.cpu(), nan=-1), torch.nan_to_num(rs, nan=-1))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("K,F", [(1, 1), (7, 65), (64, 64), (100, 33), (256, 1024), (1000, 517)])
+def test_quant_weight(dt, K, F):
+    W = torch.randn(K, F, generator=draw(K + F)).to(DT[dt])
+    if F > 10:
+        W[:, 4] = 0
+    q, s = ops.quant_weight(dev(W))
+    rq, rs = R.quant(W.t().contiguous())
+    assert torch.equal(q.cpu(), R.padded(rq)) and torch.equal(s.cpu(), rs)
+
+
+PRODUCTS = [(1, 16, 16), (1, 256, 1024), (1, 4096, 4096), (2, 100, 33), (5, 1000, 517), (8, 7, 3),
+            (15, 64, 64), (16, 256, 256), (17, 128, 100), (31, 2048, 96), (64, 64, 1), (100, 1, 40),
+            (129, 1024, 256), (257, 256, 1024), (500, 1000, 517), (1000, 320, 136), (1025, 96, 264),
+            (3000, 256, 1024), (2111, 1024, 256), (4097, 72, 72)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,K,F", PRODUCTS)
+def test_products(dt, N, K, F):
+    say(f"products {dt} N={N} K={K} F={F}")
+    ty = DT[dt]
+    g = draw(N + K + F)
+    x = torch.randn(N, K, generator=g).to(ty)
+    W = torch.randn(K, F, generator=g) / math.sqrt(K)
+    bias, C = 0.5 * torch.randn(F, generator=g), torch.randn(N, F, generator=g).to(ty)
+    if N > 3:
+        x[1] = 0
+    wq, sw = R.quant(W.t().contiguous())
+    q, s = R.quant(x)
+    xg, wg, sg, bg, cg = dev(x), dev(R.padded(wq)), dev(sw), dev(bias), dev(C)
+    ws = ops.linear_i8_workspace(N, K, F)
+    for b, act, c in ((None, None, None), (bias, "gelu", None), (bias, None, C), (bias, "gelu", C)):
+        ref, err = R.linear(q, s, wq, sw, b, act, c)
+        # GELU itself in bf16 results: 1e-4 of its value or 2e-7
+        u = ref - c.double() if c is not None else ref
+        extra = 1e-4 * u.abs() + 2e-7 if act and ty == BF16 else 0.0
+        back = torch.full((N + 2, F), 7.0, dtype=ty, device="cuda")
+        D = back[:N]
+        kw = dict(bias=bg if b is not None else None, act=act, C=cg if c is not None else None)
+        ops.pa_linear_i8(xg, wg, sg, D, ws, **kw)
+        within(D, ref, err, ty, f"linear {act}", extra)
+        assert (back[N:] == 7).all()
+        D2 = torch.empty_like(D)
+        ops.pa_gemm_i8(dev(R.padded(q)), dev(s), wg, sg, D2, K=K, **kw)
+        within(D2, ref, err, ty, f"gemm {act}", extra)
+        if c is not None:  # the residual stream in place
+            D3 = cg.clone()
+            ops.pa_gemm_i8(dev(R.padded(q)), dev(s), wg, sg, D3, K=K, bias=bg, act=act, C=D3)
+            assert torch.equal(D3, D2)
+
+
+def test_products_of_the_largest_integers():
+    """All integers 127 at the longest row: the sum 131072 * 127^2 fits 32 bits."""
+    K = 131072
+    q = torch.full((17, K), 127, dtype=torch.int8, device="cuda")
+    w = torch.full((5, K), -127, dtype=torch.int8, device="cuda")
+    s, sw = torch.full((17,), 2.0 ** -20, device="cuda"), torch.full((5,), 2.0 ** -10, device="cuda")
+    D = torch.empty(17, 5, device="cuda")
+    ops.pa_gemm_i8(q, s, w, sw, D)
+    assert (D == -float(K * 127 * 127) * 2.0 ** -30).all()
+
+
+def test_a_row_that_is_not_finite_stays_its_own():
+    x = torch.randn(40, 64, generator=draw(1))
+    W = torch.randn(64, 48, generator=draw(2)) / 8
+    wq, sw = ops.quant_weight(dev(W))
+    D, E = (torch.empty(40, 48, device="cuda") for _ in range(2))
+    ws = ops.linear_i8_workspace(40, 64, 48)
+    ops.pa_linear_i8(dev(x), wq, sw, D, ws)
+    x[7, 3] = math.nan
+    ops.pa_linear_i8(dev(x), wq, sw, E, ws)
+    keep = [i for i in range(40) if i != 7]
+    assert torch.equal(D[keep], E[keep]) and torch.isnan(E[7]).all()
+
+
+# ---- streams, graphs, long offsets ----
+def test_on_another_stream():
+    N, C = 3000, 256
+    p, d = joint_case(N, C, BF16, "layer", "layer", None, 1.0, True)
+    par, x, y = params(p), dev(d["x"]), dev(d["y"])
+    x1, h = torch.empty_like(x), torch.empty_like(x)
+    ops.pa_residual_norm(x, y, par, x1, h)
+    wq, sw = ops.quant_weight(dev(torch.randn(C, 64, generator=draw(1)).to(BF16)))
+    D = torch.empty(N, 64, dtype=BF16, device="cuda")
+    ws = ops.linear_i8_workspace(N, C, 64)
+    ops.pa_linear_i8(h, wq, sw, D, ws)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    x1b, hb, Db, wsb = (torch.zeros_like(z) for z in (x1, h, D, ws))
+    s.wait_stream(torch.cuda.current_stream())
+    ops.pa_residual_norm(x, y, par, x1b, hb, stream=s)  # handed over
+    with torch.cuda.stream(s):                           # or the current one
+        ops.pa_linear_i8(hb, wq, sw, Db, wsb)
+    s.synchronize()
+    assert torch.equal(x1, x1b) and torch.equal(h, hb) and torch.equal(D, Db)
+
+
+def test_graph_of_a_training_step():
+    """Joint, its backward and the optimiser step in one graph, the step count and
+    the learning rate on the device; every replay against the eager step."""
+    N, C = 2001, 64
+    p, d = joint_case(N, C, F32, "layer", "layer", "sigmoid", 1.0, True)
+
+    def make():
+        w = {k: dev(p[k]).clone() for k in ("post_g", "post_b", "scale", "pre_g", "pre_b")}
+        par = ops.make_residual_norm_params(post="layer", pre="layer", **w)
+        gr = {"d" + k: torch.zeros(C, device="cuda") for k in w}
+        o = {k: torch.zeros(N, C, device="cuda") for k in ("x1", "h", "dx", "dy", "dt")}
+        items = []
+        for k in w:
+            st = {s: torch.zeros(C, dtype=torch.uint8, device="cuda") for s in "mv"}
+            st.update({s + "_scale": torch.zeros(1, device="cuda") for s in "mv"})
+            items.append({"p": w[k], "g": gr["d" + k], **st})
+        return w, par, ops.make_residual_norm_grads(**gr), o, ops.make_adamw_items(items), items
+
+    x, y, t, dx1, dh = (dev(d[k]) for k in ("x", "y", "t", "dx1", "dh"))
+    ws = [ops.residual_norm_workspace(N, C, F32) for _ in range(2)]
+
+    def step(s, ws, **kw):
+        w, par, gr, o, items, _ = s
+        ops.pa_residual_norm(x, y, par, o["x1"], o["h"], t=t)
+        ops.pa_residual_norm_backward(o["x1"], y, par, dx1, dh, o["dx"], o["dy"], gr, ws, t=t,
+                                      dt=o["dt"])
+        ops.pa_adamw(items, seed=5, **kw)
+
+    eager, graphed = make(), make()
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+    lr = torch.full((1,), 1e-2, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        count.add_(1)
+        step(graphed, ws[0], lr=0.0, lr_dev=lr, step_dev=count)
+    for rep in range(1, 5):
+        lr.fill_(1e-2 / rep)
+        step(eager, ws[1], lr=lr.item(), step=rep)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(eager[5], graphed[5]):
+            for k in a:
+                assert torch.equal(a[k], b[k]), (rep, k)
+        for k in eager[3]:
+            assert torch.equal(eager[3][k], graphed[3][k]), (rep, k)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements (and 2^32 bytes) per tensor: the last rows."""
+    say("joint, 2^31 + elements")
+    C = 256
+    N = (1 << 31) // C + 77
+    p, d = joint_case(64, C, BF16, "layer", "layer", None, 1.0, True)
+    par = params(p)
+    x, y = (torch.zeros(N, C, dtype=BF16, device="cuda") for _ in range(2))
+    x[-64:], y[-64:] = dev(d["x"]), dev(d["y"])
+    x1, h = torch.empty_like(x), torch.empty_like(x)
+    ops.pa_residual_norm(x, y, par, x1, h)
+    within(x1[-64:], *R.joint(p, d["x"], d["y"]), BF16, "x1")
+    within(h[-64:], *R.pre(p, x1[-64:].cpu()), BF16, "h")
+    dx, dy = x, torch.empty_like(x)
+    dh = torch.zeros_like(x)
+    dh[-64:] = dev(d["dh"])
+    ops.pa_residual_norm_backward(x1, y, par, None, dh, dx, dy)
+    ref = R.joint_backward(p, x1[-64:].cpu(), d["y"], None, None, d["dh"], 1)
+    within(dx[-64:], *ref["dx"], BF16, "dx")
+    within(dy[-64:], *ref["dy"], BF16, "dy")
+    del x, y, x1, dx, dy, dh
+    say("linear, 2^31 + elements")
+    F = 64
+    W = torch.randn(C, F, generator=draw(3)) / 16
+    wq, sw = R.quant(W.t().contiguous())
+    N = (1 << 31) // F + 33
+    ws = ops.linear_i8_workspace(N, C, F)
+    hq, hs = R.quant(d["x"].float())
+    D = torch.empty(N, F, dtype=BF16, device="cuda")
+    big = torch.zeros(N, C, dtype=BF16, device="cuda")
+    big[-64:] = dev(d["x"])
+    ops.pa_linear_i8(big, dev(R.padded(wq)), dev(sw), D, ws)
+    within(D[-64:], *R.linear(hq, hs, wq, sw), BF16, "D")
+    assert (D[:64] == 0).all()
+    del big, D, ws
+    say("adamw, 2^31 + elements")
+    n = (1 << 31) + 515
+    tail = adam_tensors([515], 6, [BF16], lambda n: True, False)[0]
+    t = {"p": torch.zeros(n, device="cuda"), "g": torch.zeros(n, dtype=BF16, device="cuda"),
+         "m": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "v": torch.zeros(n, dtype=torch.uint8, device="cuda"),
+         "m_scale": torch.zeros(n // 256 + 1, device="cuda"),
+         "v_scale": torch.zeros(n // 256 + 1, device="cuda"), "wd": 0.0}
+    for k in ("p", "g", "m", "v"):
+        t[k][-515:] = dev(tail[k])
+    for k in ("m_scale", "v_scale"):
+        t[k][-3:] = dev(tail[k])
+    ops.pa_adamw(ops.make_adamw_items([t]), lr=1e-3, step=5, seed=1)
+    m, v = R.decode(tail["m"], tail["m_scale"], True), R.decode(tail["v"], tail["v_scale"], False)
+    ref, m, v, upd = R.adamw(tail["p"], tail["g"], m, v, 1e-3, 0.9, 0.999, 1e-8, 0.0, 5)
+    off = (t["p"][-515:].cpu().double() - ref).abs()
+    assert (off <= R.U * (2 * ref.abs() + 16e-3 * upd.abs()) + 1e-37).all()
+    i = torch.arange(515) + (1 << 31)
+    key = R.mix(R.mix(R.mix(1, 0), 5), 0)
+    h = R.fmix((R.mix(torch.full_like(i, key), i // 256) + i % 256) & 0xFFFFFFFF)
+    assert torch.equal(t["m"][-515:].cpu(), R.encode(m, h & 0xFFFF, True)[0])
+    assert torch.equal(t["v"][-515:].cpu(), R.encode(v, h >> 16, False)[0])
+    assert (t["p"][:1000] == 0).all()
