@@ -4,74 +4,255 @@
 //
 // The weights are the MFMA's A operand and the points its B operand, so that a
 // lane of a 16 x 16 result tile holds four consecutive channels of one point.
-#include "pa_device.hpp"
-#include "pa_ops_internal.h"
+#include <cstdlib>
+#include <type_traits>
+
+#include "pa_i8.hpp"
 
 namespace pa {
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ float gelu_exact(float x) {
-  return 0.5f * x * (1.f + erff(x * 0.7071067811865476f));
+// Every access of a wave's LDS writes (also those that come from memory) is
+// done, for all waves of the block.
+__device__ __forceinline__ void tile_ready() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <typename T>
-__device__ __forceinline__ float finish(const I8Args& a, int64_t n, int f, int sum, float s) {
-  float u = (float)sum * (s * a.sw[f]);
-  if (a.bias) u += a.bias[f];
-  if (a.act == PA_ACT_GELU) u = gelu_exact(u);
-  if (a.C) u += to_f<T>(reinterpret_cast<const T*>(a.C)[n * a.F + f]);
-  return u;
-}
+// ---------------------------------------------------------------------------
+// Tiled product.  A block of WF x WN waves forms a tile of TF channels x TN
+// points, each wave MF x MN MFMA tiles of 16 x 16, over steps of 128 bytes of
+// K.  A step's rows come from memory straight into LDS (16 bytes per lane), one
+// step ahead, in two buffers.  A buffer load past the last row or past a row's
+// end (K is no multiple of 128) leaves zeros.
+//
+// LDS rows are 128 bytes, without padding (a wave's load fills 1 KB in order);
+// the 16-byte chunks of row j lie at c ^ key(j), so that the lanes of an operand
+// read (one chunk of 16 rows) meet different banks.
+//
+// Channels go to MFMA rows so that a lane's results are 16 bytes of a point's
+// row: bf16: tile pairs (2 j, 2 j + 1) hold channels 32 j + 8 g + 4 (i & 1) ..
+// of lane group g; fp32: tile i holds channels 16 i + 4 g ..
+// ---------------------------------------------------------------------------
+template <int WF, int WN, int MF, int MN>
+struct I8Geo {
+  static constexpr int W = WF * WN, TF = 16 * MF * WF, TN = 16 * MN * WN, BK = 128;
+  static constexpr int LF = TF / 8 / W, LN = TN / 8 / W;  // 1 KB loads per wave and step
+  static constexpr int BUF = (TF + TN) * BK;
+  static_assert(LF * W * 8 == TF && LN * W * 8 == TN, "whole loads");
+  static_assert(2 * BUF <= 160 * 1024, "two buffers fit");
+};
 
-// 16 points x 64 channels per wave, operands straight from memory; points past
-// N and channels past F read the last one and are not stored.
 template <typename T>
-__global__ void __launch_bounds__(256) k_gemm_i8(I8Args a) {
+__device__ __forceinline__ int key_f(int row) {  // of a row of weights
+  if constexpr (sizeof(T) == 2) return (row & 3) | ((row >> 3) & 1) << 2;
+  else return row & 7;
+}
+__device__ __forceinline__ int key_n(int row) { return row & 7; }
+
+template <typename T, int ACT, int WF, int WN, int MF, int MN>
+__global__ void __launch_bounds__(64 * WF * WN, WF * WN == 8 ? 2 : 2) k_gemm_i8(I8Args a) {
+  using G = I8Geo<WF, WN, MF, MN>;
+  constexpr int BK = G::BK;
+  __shared__ __attribute__((aligned(16))) char buf0[G::BUF];
+  __shared__ __attribute__((aligned(16))) char buf1[G::BUF];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const int f0 = ((int)blockIdx.y * 4 + (int)(threadIdx.x >> 6)) * 64;
-  if (f0 >= a.F) return;
-  const int64_t n = n0 + r < a.N ? n0 + r : a.N - 1;
-  i32x4 acc[4];
-  for (int t = 0; t < 4; ++t) acc[t] = i32x4{0, 0, 0, 0};
-  for (int k = 16 * g; k < (a.Kp + 63) / 64 * 64; k += 64) {
-    const i32x4 zero = {0, 0, 0, 0};
-    const bool in = k < a.Kp;
-    const i32x4 x = in ? *reinterpret_cast<const i32x4*>(a.q + n * a.Kp + k) : zero;
-    for (int t = 0; t < 4; ++t) {
-      const int f = f0 + 16 * t + r < a.F ? f0 + 16 * t + r : a.F - 1;
-      const i32x4 w = in ? *reinterpret_cast<const i32x4*>(a.w + (int64_t)f * a.Kp + k) : zero;
-      acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc[t], 0, 0, 0);
+  const int wf = wave % WF, wn = wave / WF;
+  const int ftiles = (a.F + G::TF - 1) / G::TF;
+  const int64_t tile = blockIdx.x;
+  const int64_t n0 = tile / ftiles * G::TN;
+  const int f0 = (int)(tile % ftiles) * G::TF;
+  const int rows_n = (int)(a.N - n0 < G::TN ? a.N - n0 : G::TN);
+  const int rows_f = a.F - f0 < G::TF ? a.F - f0 : G::TF;
+
+  const auto rw = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<int8_t*>(a.w) + (int64_t)f0 * a.Kp, 0, rows_f * a.Kp, 0x00027000);
+  const auto rq = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<int8_t*>(a.q) + n0 * a.Kp, 0, rows_n * a.Kp, 0x00027000);
+
+  // this lane's row and chunk in each of its wave's loads
+  int off[G::LF + G::LN], chunk[G::LF + G::LN];
+#pragma unroll
+  for (int j = 0; j < G::LF + G::LN; ++j) {
+    const bool isf = j < G::LF;
+    const int row = 8 * ((isf ? j : j - G::LF) * G::W + wave) + (lane >> 3);
+    chunk[j] = 16 * ((lane & 7) ^ (isf ? key_f<T>(row) : key_n(row)));
+    off[j] = row * a.Kp + chunk[j];
+  }
+  auto load = [&](char* buf, int k0) {
+#pragma unroll
+    for (int j = 0; j < G::LF + G::LN; ++j) {
+      const bool isf = j < G::LF;
+      char* dst = buf + (isf ? 0 : G::TF * BK) + 1024 * ((isf ? j : j - G::LF) * G::W + wave);
+      const int o = k0 + chunk[j] < a.Kp ? off[j] + k0 : 0x7fffff00;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          isf ? rw : rq, (__attribute__((address_space(3))) void*)dst, 16, o, 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (before the products of the step before, not behind them)
+  };
+
+  i32x4 acc[MF][MN];
+#pragma unroll
+  for (int i = 0; i < MF; ++i)
+#pragma unroll
+    for (int j = 0; j < MN; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+
+  // operand reads: row of MFMA row r of the wave's first tile, then constants
+  const int row_f = wf * 16 * MF + (sizeof(T) == 2 ? 8 * (r >> 2) + (r & 3) : r);
+  const int row_n = wn * 16 * MN + r;
+  const int kf = key_f<T>(row_f), kn = key_n(row_n);
+  auto step_f = [](int i) { return sizeof(T) == 2 ? 32 * (i / 2) + 4 * (i & 1) : 16 * i; };
+  auto compute = [&](const char* buf) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      i32x4 x[MN], w[MF];
+      const char* pf = buf + row_f * BK + 16 * ((4 * s + g) ^ kf);
+      const char* pn = buf + (G::TF + row_n) * BK + 16 * ((4 * s + g) ^ kn);
+#pragma unroll
+      for (int j = 0; j < MN; ++j) x[j] = *reinterpret_cast<const i32x4*>(pn + 16 * BK * j);
+#pragma unroll
+      for (int i = 0; i < MF; ++i) w[i] = *reinterpret_cast<const i32x4*>(pf + BK * step_f(i));
+#pragma unroll
+      for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int j = 0; j < MN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i], x[j], acc[i][j], 0, 0, 0);
+    }
+  };
+
+  // step k is computed while step k + 1 comes into the other buffer, which
+  // every wave has read before the barrier
+  const int steps = (a.Kp + BK - 1) / BK;
+  load(buf0, 0);
+  int s = 0;
+  for (; s + 1 < steps; s += 2) {
+    tile_ready();
+    load(buf1, (s + 1) * BK);
+    compute(buf0);
+    tile_ready();
+    if (s + 2 < steps) load(buf0, (s + 2) * BK);
+    compute(buf1);
+  }
+  if (s < steps) {
+    tile_ready();
+    compute(buf0);
+  }
+
+  // the results: runs of V channels of one point
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, RUN = V / 4;
+  T* D = reinterpret_cast<T*>(a.D);
+  const T* Cr = reinterpret_cast<const T*>(a.C);
+  float sn[MN];
+#pragma unroll
+  for (int j = 0; j < MN; ++j) {
+    const int64_t n = n0 + row_n + 16 * j;
+    sn[j] = a.s[n < a.N ? n : a.N - 1];
+  }
+  // whole: F is a multiple of V, so that every run is aligned and lies inside or
+  // outside of a row
+  auto finish = [&](auto whole) {
+#pragma unroll
+    for (int i = 0; i < MF; i += RUN) {
+      const int f = f0 + wf * 16 * MF + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
+      float sw[V], b[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int fe = f + e < a.F ? f + e : a.F - 1;
+        sw[e] = a.sw[fe];
+        b[e] = a.bias ? a.bias[fe] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < MN; ++j) {
+        const int64_t n = n0 + row_n + 16 * j, at = n * a.F + f;
+        float u[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          u[e] = fmaf((float)acc[i + e / 4][j][e % 4], sn[j] * sw[e], b[e]);
+          if constexpr (ACT == PA_ACT_GELU) u[e] = gelu_for<T>(u[e]);
+        }
+        if (n < a.N && f < a.F) {
+          if constexpr (decltype(whole)::value) {
+            typedef T TV __attribute__((ext_vector_type(V)));
+            if (Cr) {
+              const TV c = *reinterpret_cast<const TV*>(Cr + at);
+#pragma unroll
+              for (int e = 0; e < V; ++e) u[e] += (float)c[e];
+            }
+            TV o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = (T)u[e];
+            *reinterpret_cast<TV*>(D + at) = o;
+          } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+              if (f + e < a.F) D[at + e] = from_f<T>(Cr ? u[e] + to_f<T>(Cr[at + e]) : u[e]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
+      }
+    }
+  };
+  if (a.F % V == 0) finish(std::true_type{});
+  else finish(std::false_type{});
+}
+
+// ---------------------------------------------------------------------------
+// Rows quantised.  A lane holds chunks of 16 bytes of a row in registers (the
+// last one of a row may be cut short; rows need not be aligned), so that a row is
+// read once: rows of up to 64 chunks are shared by the smallest power of two of
+// lanes, U rows each in turn with all their loads first; longer ones take a wave
+// and NC chunks per lane.  Rows beyond 512 chunks take a block and are read twice.
+// ---------------------------------------------------------------------------
+template <typename T, int NC, int U>
+__global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, int L, const T* x,
+                                                    int8_t* q, float* s) {
+  constexpr int E = Row16<T>::E;
+  const int per = 256 / L, slot = threadIdx.x / L, c0 = threadIdx.x % L, CP = Kp / E;
+  const int64_t step = (int64_t)gridDim.x * per * U;
+  for (int64_t base = (int64_t)blockIdx.x * per * U; base < N; base += step) {
+    Row16<T> v[U][NC];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t n = base + u * per + slot;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+        v[u][j] = row_chunk<T>(x + (n < N ? n : N - 1) * K, K, c0 + j * L);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t n = base + u * per + slot;
+      uint32_t big = 0;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) big = max(big, largest(v[u][j]));
+      for (int o = 1; o < L; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
+      const QuantScale c = quant_scale(big);
+      if (n >= N) continue;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+        if (c0 + j * L < CP) put_chunk(q + n * Kp + E * (c0 + j * L), v[u][j], c.inv);
+      if (c0 == 0) s[n] = c.s;
     }
   }
-  if (n0 + r >= a.N) return;
-  const float s = a.s[n];
-  for (int t = 0; t < 4; ++t)
-    for (int i = 0; i < 4; ++i) {
-      const int f = f0 + 16 * t + 4 * g + i;
-      if (f < a.F) reinterpret_cast<T*>(a.D)[n * a.F + f] = from_f<T>(finish<T>(a, n, f, acc[t][i], s));
-    }
 }
 
-// A block per row.
 template <typename T>
-__global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, const T* x,
+__global__ void __launch_bounds__(512) k_quant_long(int64_t N, int K, int Kp, const T* x,
                                                     int8_t* q, float* s) {
-  __shared__ uint32_t red[4];
+  constexpr int E = Row16<T>::E;
+  __shared__ uint32_t red[8];
+  const int CP = Kp / E;
   for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
     uint32_t big = 0;
-    for (int k = threadIdx.x; k < K; k += blockDim.x)
-      big = max(big, __builtin_bit_cast(uint32_t, fabsf(to_f<T>(x[n * K + k]))));
+    for (int c = threadIdx.x; c < CP; c += 512) big = max(big, largest(row_chunk<T>(x + n * K, K, c)));
     for (int o = 1; o < 64; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
     __syncthreads();
-    const QuantScale c = quant_scale(max(max(red[0], red[1]), max(red[2], red[3])));
-    for (int k = threadIdx.x; k < Kp; k += blockDim.x)
-      q[n * Kp + k] = k < K ? (int8_t)quant1(to_f<T>(x[n * K + k]), c.inv) : (int8_t)0;
-    if (threadIdx.x == 0) s[n] = c.s;
+    for (int w = 0; w < 8; ++w) big = max(big, red[w]);
+    const QuantScale k = quant_scale(big);
+    for (int c = threadIdx.x; c < CP; c += 512)
+      put_chunk(q + n * Kp + E * c, row_chunk<T>(x + n * K, K, c), k.inv);
+    if (threadIdx.x == 0) s[n] = k.s;
   }
 }
 
@@ -101,26 +282,61 @@ __global__ void __launch_bounds__(256) k_quant_weight(int K, int Kp, int F, cons
 
 bool gemm_i8_fused_quant(int64_t N, int F, int K) { return false; }
 
-hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st) {
-  const int64_t gx = (a.N + 15) / 16, gy = (a.F + 255) / 256;
-  if (a.N < 1 || a.F < 1 || gx > 0x7fffffff || gy > 65535) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)gx, (unsigned)gy);
-  if (d_dtype == 1)
-    hipLaunchKernelGGL(k_gemm_i8<bf16>, grid, dim3(256), 0, st, a);
+namespace {
+template <typename T, int WF, int WN, int MF, int MN>
+hipError_t run_tiled(const I8Args& a, hipStream_t st) {
+  using G = I8Geo<WF, WN, MF, MN>;
+  const int64_t tiles = (a.N + G::TN - 1) / G::TN * ((a.F + G::TF - 1) / G::TF);
+  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)tiles), block(64 * G::W);
+  if (a.act == PA_ACT_GELU)
+    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_GELU, WF, WN, MF, MN>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL(k_gemm_i8<float>, grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_NONE, WF, WN, MF, MN>), grid, block, 0, st, a);
   return hipGetLastError();
 }
+template <typename T>
+hipError_t run_gemm(const I8Args& a, hipStream_t st) {
+  const auto tiles = [&](int t) { return (a.N + t - 1) / t * ((a.F + t - 1) / t); };
+  const char* v = getenv("I8V");
+  const int want = v ? atoi(v) : tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
+  if (want == 256) return run_tiled<T, 2, 4, 8, 4>(a, st);
+  if (want == 128) return run_tiled<T, 2, 2, 4, 4>(a, st);
+  return run_tiled<T, 2, 2, 2, 2>(a, st);
+}
+}  // namespace
+
+hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st) {
+  if (a.N < 1 || a.F < 1 || a.Kp < 16) return hipErrorInvalidValue;
+  return d_dtype == 1 ? run_gemm<bf16>(a, st) : run_gemm<float>(a, st);
+}
+
+namespace {
+template <typename T>
+hipError_t run_quant(int64_t N, int K, const T* x, int8_t* q, float* s, hipStream_t st) {
+  const int Kp = (K + 15) / 16 * 16, CP = Kp / Row16<T>::E;
+  int L = 1;
+  while (L < CP && L < 64) L <<= 1;
+  auto go = [&](auto* k, int U) {
+    const int64_t rows = 256 / L * U, need = (N + rows - 1) / rows;
+    hipLaunchKernelGGL(k, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, st, N, K, Kp, L,
+                       x, q, s);
+  };
+  if (CP <= 64) go(k_quant_rows<T, 1, 4>, 4);
+  else if (CP <= 128) go(k_quant_rows<T, 2, 2>, 2);
+  else if (CP <= 256) go(k_quant_rows<T, 4, 1>, 1);
+  else if (CP <= 512) go(k_quant_rows<T, 8, 1>, 1);
+  else
+    hipLaunchKernelGGL(k_quant_long<T>, dim3((unsigned)(N < 4096 ? N : 4096)), dim3(512), 0, st, N, K,
+                       Kp, x, q, s);
+  return hipGetLastError();
+}
+}  // namespace
 
 hipError_t launch_quant_rows(int64_t N, int K, int dtype, const void* x, int8_t* q, float* s,
                              hipStream_t st) {
-  const int Kp = (K + 15) / 16 * 16;
-  const dim3 grid((unsigned)(N < 65536 ? N : 65536));
-  if (dtype == 1)
-    hipLaunchKernelGGL(k_quant_rows<bf16>, grid, dim3(256), 0, st, N, K, Kp, (const bf16*)x, q, s);
-  else
-    hipLaunchKernelGGL(k_quant_rows<float>, grid, dim3(256), 0, st, N, K, Kp, (const float*)x, q, s);
-  return hipGetLastError();
+  return dtype == 1 ? run_quant(N, K, (const bf16*)x, q, s, st)
+                    : run_quant(N, K, (const float*)x, q, s, st);
 }
 
 hipError_t launch_quant_weight(int K, int F, int dtype, const void* W, int8_t* Wq, float* sw,

@@ -1,0 +1,74 @@
+// Device helpers of the 8-bit integer products (gfx950): the activation, and rows
+// of bf16 or fp32 turned into integers.
+#pragma once
+
+#include "pa_device.hpp"
+#include "pa_ops_internal.h"
+
+namespace pa {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float gelu_exact(float x) {
+  return 0.5f * x * (1.f + erff(x * 0.7071067811865476f));
+}
+// GELU for bf16 results: x Phi(x) = max(x, 0) - z Q(z), z = |x|, the upper tail
+// Q(z) = 1 - Phi(z) as exp2 of a polynomial of degree 7, fitted for this kernel
+// over [0, 9] (weighted minimax, linear programming over 4,001 points).  In
+// fp32 against 64 bits: relative 1.8e-5 for x > -3, 3.6e-5 down to -4, 1.1e-4 to
+// -6, 3.8e-4 to -9, below that 1e-18 absolute; half a bf16 step is 2e-3 to 3.9e-3.
+// (Half of the kernel's vector instructions: one exp2, the time of four others,
+// and ten more; erff takes three times as many.)
+__device__ __forceinline__ float gelu_tail(float x) {
+  const float z = __builtin_elementwise_minimum(fabsf(x), 9.f);
+  float p = -1.2643212130569736e-06f;
+  p = fmaf(p, z, 4.878497202298604e-05f);
+  p = fmaf(p, z, -0.0008188498904928565f);
+  p = fmaf(p, z, 0.008031141944229603f);
+  p = fmaf(p, z, -0.05292445048689842f);
+  p = fmaf(p, z, -0.45953628420829773f);
+  p = fmaf(p, z, -1.1508264541625977f);
+  p = fmaf(p, z, -1.0000252723693848f);
+  return fmaf(-z, fast_exp2(p), __builtin_elementwise_maximum(x, 0.f));
+}
+template <typename T> __device__ __forceinline__ float gelu_for(float x) {
+  if constexpr (sizeof(T) == 2) return gelu_tail(x);
+  else return gelu_exact(x);
+}
+
+template <typename T> struct Row16 {
+  static constexpr int E = 16 / (int)sizeof(T);
+  T v[E];
+};
+template <typename T>
+__device__ __forceinline__ Row16<T> row_chunk(const T* row, int K, int c) {
+  constexpr int E = Row16<T>::E;
+  Row16<T> o;
+  if (E * c + E <= K) {
+    __builtin_memcpy(&o, row + E * c, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) o.v[e] = E * c + e < K ? row[E * c + e] : from_f<T>(0.f);
+  }
+  return o;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t largest(const Row16<T>& c) {
+  uint32_t big = 0;
+#pragma unroll
+  for (int e = 0; e < Row16<T>::E; ++e)
+    big = max(big, __builtin_bit_cast(uint32_t, fabsf(to_f<T>(c.v[e]))));
+  return big;
+}
+template <typename T>
+__device__ __forceinline__ void put_chunk(int8_t* q, const Row16<T>& x, float inv) {
+  constexpr int E = Row16<T>::E;
+  uint32_t w[E / 4];
+#pragma unroll
+  for (int e = 0; e < E; e += 4)
+    w[e / 4] = quant4(to_f<T>(x.v[e]), to_f<T>(x.v[e + 1]), to_f<T>(x.v[e + 2]),
+                      to_f<T>(x.v[e + 3]), inv);
+  __builtin_memcpy(__builtin_assume_aligned(q, E), w, E);
+}
+
+}  // namespace pa

@@ -1,0 +1,192 @@
+// A linear layer in 8-bit integers on many rows of few channels, in one pass
+// (gfx950, bf16 rows in and out): the rows are quantised on the way into LDS, so
+// that neither their integers nor their scales go through memory.
+//
+// A block is persistent on its CU: each of its eight waves keeps the integer
+// weights of 16 NCT output channels in registers (the MFMA A operand, at most
+// 128 registers), and the block walks a range of the points in tiles of 32.  A
+// tile's rows come from memory a tile ahead, 16 lanes per row, which find the
+// row's largest magnitude among themselves, and go into a double-buffered LDS
+// tile as integers; all waves read it as the B operand: one barrier per tile.
+// Results leave from the registers, 64 bytes of a point's row per instruction.
+//
+// LDS rows hold 64 KS bytes without padding; the 16-byte chunks of row j lie at
+// c ^ key(j), so that the lanes of an operand read meet different banks.
+#include "pa_i8.hpp"
+#include "pa_stream.hpp"
+
+namespace pa {
+namespace {
+
+template <int KS, int NCT>
+struct FusedGeo {
+  static constexpr int FCB = 128 * NCT;               // channels of a block
+  static constexpr int PTS = 32, RB = 64 * KS;        // points of a tile, bytes of a row
+  static constexpr int TILE = PTS * RB;
+  static constexpr int NC = (8 * KS + 15) / 16;       // 16-byte chunks of a row per lane
+  static constexpr int RUNS = (NCT + 1) / 2;          // runs of 8 (NCT = 1: 4) channels
+};
+template <int KS> __device__ __forceinline__ int key_of(int row) {
+  return KS == 1 ? (row >> 1) & 3 : row & 7;
+}
+
+template <int ACT, int KS, int NCT>
+__global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
+  using G = FusedGeo<KS, NCT>;
+  constexpr int V = NCT == 1 ? 4 : 8;
+  __shared__ __attribute__((aligned(16))) char xs[2][G::TILE];
+  __shared__ float ss[2][G::PTS];
+  __shared__ __attribute__((aligned(16))) float sws[G::FCB], bs[G::FCB];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const int F = a.F, K = a.K, ncg = (F + G::FCB - 1) / G::FCB;
+  // blocks are dealt to the XCDs round robin: the column blocks of one range of
+  // points share an XCD's L2
+  const int nb = gridDim.x, bl = blockIdx.x;
+  const int l = nb % 8 == 0 ? (bl % 8) * (nb / 8) + bl / 8 : bl;
+  const int pg = l / ncg, f0 = (l - pg * ncg) * G::FCB;
+  const int64_t tiles = (a.N + G::PTS - 1) / G::PTS;
+  const int64_t t0 = tiles * pg / PG, t1 = tiles * (pg + 1) / PG;  // t0 < t1 (PG <= tiles)
+  const int fw = f0 + 16 * NCT * wave;  // the wave's first channel
+  const bool on = fw < F;
+
+  // the tile's row and chunks of this thread
+  const bf16* X = reinterpret_cast<const bf16*>(a.x);
+  const int row = threadIdx.x >> 4, c0 = threadIdx.x & 15;
+  Row16<bf16> xr[G::NC];
+  auto load = [&](int64_t t) {
+    const int64_t n = (t < t1 ? t : t1 - 1) * G::PTS + row;
+    const bf16* p = X + (n < a.N ? n : a.N - 1) * K;
+#pragma unroll
+    for (int j = 0; j < G::NC; ++j) {
+      const int c = 8 * (c0 + 16 * j);  // K is a multiple of 8
+      xr[j] = Row16<bf16>{};
+      if (c < K)
+        xr[j] = __builtin_bit_cast(Row16<bf16>, *reinterpret_cast<const uint4*>(p + c));
+    }
+  };
+  const int kr = key_of<KS>(row);
+  auto store = [&](int buf) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int j = 0; j < G::NC; ++j) big = max(big, largest(xr[j]));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
+    const QuantScale q = quant_scale(big);
+#pragma unroll
+    for (int j = 0; j < G::NC; ++j) {
+      const int c = c0 + 16 * j;  // 8 integers: half a 16-byte chunk
+      if (8 * c < G::RB)
+        put_chunk(reinterpret_cast<int8_t*>(xs[buf] + row * G::RB + 16 * ((c >> 1) ^ kr) + 8 * (c & 1)),
+                  xr[j], q.inv);
+    }
+    if (c0 == 0) ss[buf][row] = q.s;
+  };
+
+  // weights: MFMA row r of tile i is channel fw + step(i) + 8 (r / 4) + r % 4 (NCT
+  // = 1: r itself), so that a lane's results of a tile pair are 8 channels in order
+  auto step = [](int i) { return NCT == 1 ? 0 : 32 * (i / 2) + 4 * (i & 1); };
+  const int fr = NCT == 1 ? r : 8 * (r >> 2) + (r & 3);
+  i32x4 w[NCT][KS];
+#pragma unroll
+  for (int i = 0; i < NCT; ++i) {
+    const int f = fw + step(i) + fr;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int k = 64 * s + 16 * g;
+      w[i][s] = i32x4{0, 0, 0, 0};
+      if (f < F && k < a.Kp) w[i][s] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)f * a.Kp + k);
+    }
+  }
+  for (int f = threadIdx.x; f < G::FCB; f += 512) {
+    const bool in = f0 + f < F;
+    sws[f] = in ? a.sw[f0 + f] : 0.f;
+    bs[f] = in && a.bias ? a.bias[f0 + f] : 0.f;
+  }
+  load(t0);
+  store(0);
+  load(t0 + 1);
+
+  bf16* D = reinterpret_cast<bf16*>(a.D);
+  const bf16* Cr = reinterpret_cast<const bf16*>(a.C);
+  const int kb = key_of<KS>(r);  // (of rows r and 16 + r)
+  for (int64_t t = t0; t < t1; ++t) {
+    const int buf = (int)(t - t0) & 1;
+    block_sync();  // tile t is in LDS, tile t - 1 is read
+    if (t + 1 < t1) store(buf ^ 1);
+    load(t + 2);
+    if (!on) continue;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const char* xb = xs[buf] + (16 * u + r) * G::RB;
+      i32x4 acc[NCT];
+#pragma unroll
+      for (int i = 0; i < NCT; ++i) acc[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const i32x4 x = *reinterpret_cast<const i32x4*>(xb + 16 * ((4 * s + g) ^ kb));
+#pragma unroll
+        for (int i = 0; i < NCT; ++i)
+          acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][s], x, acc[i], 0, 0, 0);
+      }
+      const float sn = ss[buf][16 * u + r];
+      const int64_t n = t * G::PTS + 16 * u + r;
+#pragma unroll
+      for (int q = 0; q < G::RUNS; ++q) {
+        const int fl = 16 * NCT * wave + (NCT == 1 ? 4 * g : 32 * q + 8 * g), f = f0 + fl;
+        float y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          y[e] = fmaf((float)acc[2 * q + e / 4][e % 4], sn * sws[fl + e], bs[fl + e]);
+          if constexpr (ACT == PA_ACT_GELU) y[e] = gelu_tail(y[e]);
+        }
+        if (n < a.N && f < F) {  // F is a multiple of V
+          typedef bf16 BV __attribute__((ext_vector_type(V)));
+          const int64_t at = n * F + f;
+          if (Cr) {
+            const BV c = *reinterpret_cast<const BV*>(Cr + at);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] += (float)c[e];
+          }
+          BV o;
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] = (bf16)y[e];
+          *reinterpret_cast<BV*>(D + at) = o;
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
+      }
+    }
+  }
+}
+
+template <int KS, int NCT>
+hipError_t run(const I8Args& a, hipStream_t st) {
+  using G = FusedGeo<KS, NCT>;
+  const int ncg = (a.F + G::FCB - 1) / G::FCB;
+  const int64_t tiles = (a.N + G::PTS - 1) / G::PTS;
+  const int PG = (int)(tiles < 256 / ncg ? tiles : 256 / ncg);
+  const dim3 grid(PG * ncg), block(512);
+  if (a.act == PA_ACT_GELU)
+    hipLaunchKernelGGL((k_linear_i8<PA_ACT_GELU, KS, NCT>), grid, block, 0, st, a, PG);
+  else
+    hipLaunchKernelGGL((k_linear_i8<PA_ACT_NONE, KS, NCT>), grid, block, 0, st, a, PG);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool linear_i8_fused(int64_t N, int F, int K, int x_dtype, int d_dtype) {
+  if (x_dtype != 1 || d_dtype != 1 || K % 8 || F % 8 || K > 1024) return false;
+  const int most = K <= 64 ? 1024 : K <= 128 ? 1024 : K <= 256 ? 2048 : K <= 512 ? 1024 : 512;
+  return F <= most && N >= 16384;
+}
+
+hipError_t launch_linear_i8(const I8Args& a, hipStream_t st) {
+  if (a.K <= 64) return run<1, 4>(a, st);
+  if (a.K <= 128) return run<2, 4>(a, st);
+  if (a.K <= 256) return a.F <= 256 ? run<4, 2>(a, st) : run<4, 8>(a, st);
+  if (a.K <= 512) return a.F <= 128 ? run<8, 1>(a, st) : run<8, 4>(a, st);
+  return run<16, 2>(a, st);
+}
+
+}  // namespace pa

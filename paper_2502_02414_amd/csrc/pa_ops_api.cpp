@@ -350,10 +350,13 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   PO_TRY(product(who, a, N, F, K, Wq, sw, bias, act, C, D, d_dtype));
   PO_TRY(dtype_ok(who, x_dtype));
   PO_TRY(need(who, x, "x"));
-  if (pa::gemm_i8_fused_quant(N, F, K)) {
-    a.x = x;
-    a.x_dtype = x_dtype;
-  } else {
+  a.x = x;
+  a.x_dtype = x_dtype;
+  if (pa::linear_i8_fused(N, F, K, x_dtype, d_dtype)) {
+    PO_HIP(pa::launch_linear_i8(a, as_stream(stream)), who);
+    return PA_OK;
+  }
+  if (!pa::gemm_i8_fused_quant(N, F, K)) {
     const size_t rows = (size_t)N * a.Kp;
     if (!ws || ws_bytes < rows + (size_t)N * 4)
       return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, rows + (size_t)N * 4);
@@ -363,6 +366,7 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
     PO_HIP(pa::launch_quant_rows(N, K, x_dtype, x, q, s, as_stream(stream)), who);
     a.q = q;
     a.s = s;
+    a.x = nullptr;
   }
   PO_HIP(pa::launch_gemm_i8(a, d_dtype, as_stream(stream)), who);
   return PA_OK;
