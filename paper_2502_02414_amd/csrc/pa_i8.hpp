@@ -2,6 +2,8 @@
 // of bf16 or fp32 turned into integers.
 #pragma once
 
+#include <type_traits>
+
 #include "pa_device.hpp"
 #include "pa_ops_internal.h"
 
@@ -52,13 +54,33 @@ __device__ __forceinline__ Row16<T> row_chunk(const T* row, int K, int c) {
   }
   return o;
 }
-template <typename T>
-__device__ __forceinline__ uint32_t largest(const Row16<T>& c) {
+// The bits of a chunk's largest magnitude as an fp32 number.
+__device__ __forceinline__ uint32_t largest(const Row16<float>& c) {
   uint32_t big = 0;
 #pragma unroll
-  for (int e = 0; e < Row16<T>::E; ++e)
-    big = max(big, __builtin_bit_cast(uint32_t, fabsf(to_f<T>(c.v[e]))));
+  for (int e = 0; e < 4; ++e) big = max(big, __builtin_bit_cast(uint32_t, c.v[e]) & 0x7fffffffu);
   return big;
+}
+__device__ __forceinline__ uint32_t largest(const Row16<bf16>& c) {  // two at a time
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  uint32_t w[4];
+  __builtin_memcpy(w, &c, 16);
+  u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+  for (int i = 1; i < 4; ++i)
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  return (uint32_t)max(m[0], m[1]) << 16;
+}
+// ... over the 16 lanes of a row of lanes.
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+  const auto step = [&](auto ctrl) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  step(std::integral_constant<int, kQuadSwap1>{});
+  step(std::integral_constant<int, kQuadSwap2>{});
+  step(std::integral_constant<int, kHalfMirror>{});
+  step(std::integral_constant<int, kMirror>{});
+  return v;
 }
 template <typename T>
 __device__ __forceinline__ void put_chunk(int8_t* q, const Row16<T>& x, float inv) {

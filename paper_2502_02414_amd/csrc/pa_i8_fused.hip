@@ -12,6 +12,8 @@
 //
 // LDS rows hold 64 KS bytes without padding; the 16-byte chunks of row j lie at
 // c ^ key(j), so that the lanes of an operand read meet different banks.
+#include <type_traits>
+
 #include "pa_i8.hpp"
 #include "pa_stream.hpp"
 
@@ -50,35 +52,42 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   const int fw = f0 + 16 * NCT * wave;  // the wave's first channel
   const bool on = fw < F;
 
+  // Rows, results and residuals go by buffer instructions, which leave out (or read
+  // as zeros) what lies behind the rows of the tile, or at an offset behind them:
+  // with no branch around a load or a store, the wait for a tile's rows is neither
+  // where they are requested nor one for results that were stored after that.
+  auto tile_of = [&](const void* p, int64_t t, int width) {
+    const int64_t left = a.N - t * G::PTS;
+    return __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(reinterpret_cast<const char*>(p)) + t * G::PTS * width * 2, 0,
+        (int)(left < G::PTS ? left : G::PTS) * width * 2, 0x00027000);
+  };
+  constexpr int NOWHERE = 0x7fffff00;
   // the tile's row and chunks of this thread
-  const bf16* X = reinterpret_cast<const bf16*>(a.x);
   const int row = threadIdx.x >> 4, c0 = threadIdx.x & 15;
-  Row16<bf16> xr[G::NC];
-  auto load = [&](int64_t t) {
-    const int64_t n = (t < t1 ? t : t1 - 1) * G::PTS + row;
-    const bf16* p = X + (n < a.N ? n : a.N - 1) * K;
+  i32x4 xr[G::NC];
+  auto load = [&](int64_t t) __attribute__((always_inline)) {
+    const auto rx = tile_of(a.x, t < t1 ? t : t1 - 1, K);
 #pragma unroll
     for (int j = 0; j < G::NC; ++j) {
       const int c = 8 * (c0 + 16 * j);  // K is a multiple of 8
-      xr[j] = Row16<bf16>{};
-      if (c < K)
-        xr[j] = __builtin_bit_cast(Row16<bf16>, *reinterpret_cast<const uint4*>(p + c));
+      xr[j] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, c < K ? (row * K + c) * 2 : NOWHERE, 0, 0));
     }
   };
-  const int kr = key_of<KS>(row);
-  auto store = [&](int buf) {
+  const int put = row * G::RB + 16 * ((c0 >> 1) ^ key_of<KS>(row)) + 8 * (c0 & 1);
+  auto store = [&](int buf) __attribute__((always_inline)) {
     uint32_t big = 0;
 #pragma unroll
-    for (int j = 0; j < G::NC; ++j) big = max(big, largest(xr[j]));
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
-    const QuantScale q = quant_scale(big);
+    for (int j = 0; j < G::NC; ++j) big = max(big, largest(__builtin_bit_cast(Row16<bf16>, xr[j])));
+    const QuantScale q = quant_scale(row16_max(big));
 #pragma unroll
     for (int j = 0; j < G::NC; ++j) {
       const int c = c0 + 16 * j;  // 8 integers: half a 16-byte chunk
       if (8 * c < G::RB)
-        put_chunk(reinterpret_cast<int8_t*>(xs[buf] + row * G::RB + 16 * ((c >> 1) ^ kr) + 8 * (c & 1)),
-                  xr[j], q.inv);
+        put_chunk(reinterpret_cast<int8_t*>(xs[buf] + put + 128 * j),
+                  __builtin_bit_cast(Row16<bf16>, xr[j]), q.inv);
+      if (G::NC > 2) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
     }
     if (c0 == 0) ss[buf][row] = q.s;
   };
@@ -87,6 +96,9 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   // = 1: r itself), so that a lane's results of a tile pair are 8 channels in order
   auto step = [](int i) { return NCT == 1 ? 0 : 32 * (i / 2) + 4 * (i & 1); };
   const int fr = NCT == 1 ? r : 8 * (r >> 2) + (r & 3);
+  const auto rw = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<int8_t*>(a.w) + (int64_t)f0 * a.Kp, 0,
+      (F - f0 < G::FCB ? F - f0 : G::FCB) * a.Kp, 0x00027000);
   i32x4 w[NCT][KS];
 #pragma unroll
   for (int i = 0; i < NCT; ++i) {
@@ -94,8 +106,9 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       const int k = 64 * s + 16 * g;
-      w[i][s] = i32x4{0, 0, 0, 0};
-      if (f < F && k < a.Kp) w[i][s] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)f * a.Kp + k);
+      w[i][s] = __builtin_bit_cast(
+          i32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                     rw, f < F && k < a.Kp ? (f - f0) * a.Kp + k : NOWHERE, 0, 0));
     }
   }
   for (int f = threadIdx.x; f < G::FCB; f += 512) {
@@ -107,56 +120,86 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   store(0);
   load(t0 + 1);
 
-  bf16* D = reinterpret_cast<bf16*>(a.D);
-  const bf16* Cr = reinterpret_cast<const bf16*>(a.C);
-  const int kb = key_of<KS>(r);  // (of rows r and 16 + r)
-  for (int64_t t = t0; t < t1; ++t) {
-    const int buf = (int)(t - t0) & 1;
-    block_sync();  // tile t is in LDS, tile t - 1 is read
-    if (t + 1 < t1) store(buf ^ 1);
+  // operand chunk 4 s + g of rows r and 16 + r (the same key)
+  const int at[2] = {r * G::RB + 16 * (g ^ key_of<KS>(r)), r * G::RB + 16 * ((4 + g) ^ key_of<KS>(r))};
+  // A tile's results; residuals (RES) of up to two runs a half are requested
+  // before the rows of the tile after next, so that they do not wait for those.
+  typedef bf16 BV __attribute__((ext_vector_type(V)));
+  constexpr bool AHEAD = G::RUNS <= 2;
+  auto channel = [&](int q) { return 16 * NCT * wave + (NCT == 1 ? 4 * g : 32 * q + 8 * g); };
+  auto place = [&](int u, int q) {  // F is a multiple of V
+    const int f = f0 + channel(q);
+    return f < F ? ((16 * u + r) * F + f) * 2 : NOWHERE;
+  };
+  auto residual = [&](__amdgpu_buffer_rsrc_t rc, int u, int q) {
+    if constexpr (V == 8)
+      return __builtin_bit_cast(BV, __builtin_amdgcn_raw_buffer_load_b128(rc, place(u, q), 0, 0));
+    else
+      return __builtin_bit_cast(BV, __builtin_amdgcn_raw_buffer_load_b64(rc, place(u, q), 0, 0));
+  };
+  auto tile = [&](int64_t t, int buf, auto RES) __attribute__((always_inline)) {
+    constexpr bool res = decltype(RES)::value;
+    const auto rd = tile_of(a.D, t, F), rc = tile_of(res ? a.C : a.D, t, F);
+    BV c[2][AHEAD ? G::RUNS : 1];
+    if constexpr (res && AHEAD)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int q = 0; q < G::RUNS; ++q) c[u][q] = residual(rc, u, q);
     load(t + 2);
-    if (!on) continue;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const char* xb = xs[buf] + (16 * u + r) * G::RB;
+      const char* xb = xs[buf] + 16 * u * G::RB;
       i32x4 acc[NCT];
 #pragma unroll
       for (int i = 0; i < NCT; ++i) acc[i] = i32x4{0, 0, 0, 0};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const i32x4 x = *reinterpret_cast<const i32x4*>(xb + 16 * ((4 * s + g) ^ kb));
+        const i32x4 x = *reinterpret_cast<const i32x4*>(xb + at[s & 1] + 128 * (s / 2));
 #pragma unroll
         for (int i = 0; i < NCT; ++i)
           acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][s], x, acc[i], 0, 0, 0);
+        if (KS > 4 && s % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
       }
       const float sn = ss[buf][16 * u + r];
-      const int64_t n = t * G::PTS + 16 * u + r;
 #pragma unroll
       for (int q = 0; q < G::RUNS; ++q) {
-        const int fl = 16 * NCT * wave + (NCT == 1 ? 4 * g : 32 * q + 8 * g), f = f0 + fl;
-        float y[V];
+        const int fl = channel(q);
+        if constexpr (res && !AHEAD) c[u][0] = residual(rc, u, q);
+        BV o;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          y[e] = fmaf((float)acc[2 * q + e / 4][e % 4], sn * sws[fl + e], bs[fl + e]);
-          if constexpr (ACT == PA_ACT_GELU) y[e] = gelu_tail(y[e]);
+          float y = fmaf((float)acc[2 * q + e / 4][e % 4], sn * sws[fl + e], bs[fl + e]);
+          if constexpr (ACT == PA_ACT_GELU) y = gelu_tail(y);
+          if constexpr (res) y += (float)c[u][AHEAD ? q : 0][e];
+          o[e] = (bf16)y;
         }
-        if (n < a.N && f < F) {  // F is a multiple of V
-          typedef bf16 BV __attribute__((ext_vector_type(V)));
-          const int64_t at = n * F + f;
-          if (Cr) {
-            const BV c = *reinterpret_cast<const BV*>(Cr + at);
-#pragma unroll
-            for (int e = 0; e < V; ++e) y[e] += (float)c[e];
-          }
-          BV o;
-#pragma unroll
-          for (int e = 0; e < V; ++e) o[e] = (bf16)y[e];
-          *reinterpret_cast<BV*>(D + at) = o;
-        }
+        typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        if constexpr (V == 8)
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rd, place(u, q), 0, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, o), rd, place(u, q), 0, 0);
         __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
       }
     }
-  }
+  };
+  // One loop each for waves with channels, with and without residuals, and for
+  // those without, and nothing in flight before it: a wait in a loop has to suit
+  // every way into it.
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  auto walk = [&](auto body) __attribute__((always_inline)) {
+    for (int64_t t = t0; t < t1; ++t) {
+      const int buf = (int)(t - t0) & 1;
+      block_sync();    // tile t is in LDS, tile t - 1 is read
+      store(buf ^ 1);  // (behind the last tile: rows that nothing reads)
+      body(t, buf);
+    }
+  };
+  if (!on) walk([&](int64_t t, int) { load(t + 2); });
+  else if (a.C) walk([&](int64_t t, int buf) { tile(t, buf, std::true_type{}); });
+  else walk([&](int64_t t, int buf) { tile(t, buf, std::false_type{}); });
 }
 
 template <int KS, int NCT>

@@ -96,17 +96,27 @@ struct QuantScale {
 };
 __device__ __forceinline__ QuantScale quant_scale(uint32_t big) {
   const float m = __builtin_bit_cast(float, big);
-  if (big >= 0x7f800000u) return {0.f, __builtin_nanf("")};
-  if (m < 1e-36f) return {0.f, 0.f};
-  return {__fdiv_rn(127.f, m), __fdiv_rn(m, 127.f)};
+  const bool zero = m < 1e-36f, bad = big >= 0x7f800000u;
+  const float inv = __fdiv_rn(127.f, m), s = __fdiv_rn(m, 127.f);
+  return {zero || bad ? 0.f : inv, bad ? __builtin_nanf("") : zero ? 0.f : s};
 }
-// Four integers of a row in one word, |x inv| <= 127 (1 + 2^-23): rounded to
-// even they stay within +-127.  (inv = 0: zeros, also where x is not finite.)
-__device__ __forceinline__ uint32_t quant1(float x, float inv) {
-  return inv == 0.f ? 0u : (uint32_t)(int)rintf(x * inv) & 0xffu;
-}
+// Four integers of a row in one word.  |x inv| <= 127 (1 + 2^-23): rounded to
+// even they stay within +-127; 1.5 2^23 added leaves the integer in the lowest
+// bits.  inv = 0 (zeros, or a row that is not finite): zeros.
 __device__ __forceinline__ uint32_t quant4(float a, float b, float c, float d, float inv) {
-  return quant1(a, inv) | quant1(b, inv) << 8 | quant1(c, inv) << 16 | quant1(d, inv) << 24;
+  const float v[4] = {a, b, c, d};
+  uint32_t t[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma clang fp contract(off)
+    t[i] = __builtin_bit_cast(uint32_t, v[i] * inv + 12582912.f);
+  }
+  const uint32_t lo = __builtin_amdgcn_perm(t[1], t[0], 0x0c0c0400u);
+  const uint32_t hi = __builtin_amdgcn_perm(t[3], t[2], 0x04000c0cu);
+  return inv == 0.f ? 0u : lo | hi;
+}
+__device__ __forceinline__ uint32_t quant1(float x, float inv) {
+  return quant4(x, 0.f, 0.f, 0.f, inv) & 0xffu;
 }
 #endif
 
