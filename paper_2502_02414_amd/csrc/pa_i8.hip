@@ -280,8 +280,6 @@ __global__ void __launch_bounds__(256) k_quant_weight(int K, int Kp, int F, cons
 
 }  // namespace
 
-bool gemm_i8_fused_quant(int64_t N, int F, int K) { return false; }
-
 namespace {
 template <typename T, int WF, int WN, int MF, int MN>
 hipError_t run_tiled(const I8Args& a, hipStream_t st) {

@@ -352,22 +352,23 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   PO_TRY(need(who, x, "x"));
   a.x = x;
   a.x_dtype = x_dtype;
+  if (pa::linear_i8_few(N, K)) {
+    PO_HIP(pa::launch_linear_few(a, d_dtype, as_stream(stream)), who);
+    return PA_OK;
+  }
   if (pa::linear_i8_fused(N, F, K, x_dtype, d_dtype)) {
     PO_HIP(pa::launch_linear_i8(a, as_stream(stream)), who);
     return PA_OK;
   }
-  if (!pa::gemm_i8_fused_quant(N, F, K)) {
-    const size_t rows = (size_t)N * a.Kp;
-    if (!ws || ws_bytes < rows + (size_t)N * 4)
-      return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, rows + (size_t)N * 4);
-    PO_TRY(opt(who, ws, "ws"));
-    int8_t* q = reinterpret_cast<int8_t*>(ws);
-    float* s = reinterpret_cast<float*>(q + rows);
-    PO_HIP(pa::launch_quant_rows(N, K, x_dtype, x, q, s, as_stream(stream)), who);
-    a.q = q;
-    a.s = s;
-    a.x = nullptr;
-  }
+  const size_t rows = (size_t)N * a.Kp;
+  if (!ws || ws_bytes < rows + (size_t)N * 4)
+    return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, rows + (size_t)N * 4);
+  PO_TRY(opt(who, ws, "ws"));
+  int8_t* q = reinterpret_cast<int8_t*>(ws);
+  float* s = reinterpret_cast<float*>(q + rows);
+  PO_HIP(pa::launch_quant_rows(N, K, x_dtype, x, q, s, as_stream(stream)), who);
+  a.q = q;
+  a.s = s;
   PO_HIP(pa::launch_gemm_i8(a, d_dtype, as_stream(stream)), who);
   return PA_OK;
 }

@@ -76,12 +76,14 @@ struct I8Args {
   const void* C = nullptr;
   void* D = nullptr;
 };
-bool gemm_i8_fused_quant(int64_t N, int F, int K);  // such few rows that the product quantises them
 hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st);
 // Rows quantised on the way into a product that keeps its weights in registers
 // (pa_i8_fused.hip): served, and faster than the two launches.
 bool linear_i8_fused(int64_t N, int F, int K, int x_dtype, int d_dtype);
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st);
+// Few rows (pa_i8_few.hip): served.
+bool linear_i8_few(int64_t N, int K);
+hipError_t launch_linear_few(const I8Args& a, int d_dtype, hipStream_t st);
 hipError_t launch_quant_rows(int64_t N, int K, int dtype, const void* x, int8_t* q, float* s,
                              hipStream_t st);
 hipError_t launch_quant_weight(int K, int F, int dtype, const void* W, int8_t* Wq, float* sw,

@@ -415,6 +415,9 @@ PRODUCTS = [(1, 16, 16), (1, 256, 1024), (1, 4096, 4096), (2, 100, 33), (5, 1000
             (15, 64, 64), (16, 256, 256), (17, 128, 100), (31, 2048, 96), (64, 64, 1), (100, 1, 40),
             (129, 1024, 256), (257, 256, 1024), (500, 1000, 517), (1000, 320, 136), (1025, 96, 264),
             (3000, 256, 1024), (2111, 1024, 256), (4097, 72, 72),
+            # few rows: one launch
+            (1, 131072, 32), (2, 65536, 20), (3, 1001, 100), (9, 4104, 48), (16, 8192, 64),
+            (16, 9200, 17), (13, 576, 2000), (4, 128, 5),
             # rows quantised on the way into the product (bf16)
             (16384, 64, 256), (16385, 128, 512), (16411, 256, 1024), (16400, 1024, 256),
             (20000, 72, 72), (17000, 512, 128), (16390, 504, 512), (16999, 240, 2000),
