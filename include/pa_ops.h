@@ -128,7 +128,7 @@ typedef struct {
 } pa_adamw_item;
 
 typedef struct {
-  double lr, beta1, beta2, eps;  /* betas in [0, 1), eps > 0                   */
+  double lr, beta1, beta2, eps;  /* betas in [0, 1), eps a normal fp32 > 0      */
   int64_t step;                  /* of this update, from 1                     */
   uint64_t seed;                 /* of the 8-bit moments' rounding             */
   const float* gscale;           /* nullable device scalar (1): clipping       */

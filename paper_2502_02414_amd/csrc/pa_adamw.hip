@@ -5,6 +5,9 @@
 // works on 16 units of 256 consecutive elements of one tensor, a wave on four of
 // them, four elements per lane: a unit is a block of the 8-bit moments, whose
 // largest magnitude is a reduction within the wave.
+#include <cmath>
+#include <type_traits>
+
 #include "pa_device.hpp"
 #include "pa_ops_internal.h"
 
@@ -20,6 +23,25 @@ __host__ __device__ static inline uint32_t mix32(uint32_t a, uint32_t b) {
   return fmix32(a ^ (b * 0x9E3779B9u));
 }
 uint32_t adam_mix(uint32_t a, uint32_t b) { return mix32(a, b); }
+
+// lr / (1 - b1^step) and 1 / sqrt(1 - b2^step): the same operations of 64 bits on
+// the host and on the device, so that both give the same step.
+__host__ __device__ static inline double whole_power(double b, int64_t n) {
+#pragma clang fp contract(off)
+  double r = 1.0;
+  for (; n > 0; n >>= 1, b = b * b)
+    if (n & 1) r = r * b;
+  return r;
+}
+__host__ __device__ static inline void adam_step_consts(double lr, double b1, double b2,
+                                                        int64_t step, float& ss, float& rs) {
+#pragma clang fp contract(off)
+  ss = (float)(lr / (1.0 - whole_power(b1, step)));
+  rs = (float)(1.0 / sqrt(1.0 - whole_power(b2, step)));
+}
+void adam_consts(double lr, double b1, double b2, int64_t step, float* ss, float* rs) {
+  adam_step_consts(lr, b1, b2, step, *ss, *rs);
+}
 
 namespace {
 
@@ -47,6 +69,12 @@ __device__ __forceinline__ float block_scale(uint32_t big) {
   up = up < 0x00800000u ? 0x00800000u : up > 0x7F000000u ? 0x7F000000u : up;
   return __builtin_bit_cast(float, up);
 }
+// 1 / S of a power of two from 2^-126 to 2^127 (its exponent mirrored; 2^-127 is
+// subnormal); a NaN stays one.
+__device__ __forceinline__ float fast_rcp_pow2(float S) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, S);
+  return S != S ? S : __builtin_bit_cast(float, b == 0x7F000000u ? 0x00400000u : 0x7F000000u - b);
+}
 __device__ __forceinline__ int code_of(float mag, float inv, uint32_t h, uint32_t lo) {
   return (int)((__builtin_bit_cast(uint32_t, mag * inv) + 16 * h + 8) >> 20) - (int)lo;
 }
@@ -56,7 +84,9 @@ struct Consts {
 };
 
 // p, m, v of one element after the step (the moments without fused
-// multiply-adds, as documented).
+// multiply-adds, as documented).  The root and the reciprocal are the
+// hardware's, good to one step of fp32 each; it takes a subnormal v for zero, so
+// such ones are scaled.
 __device__ __forceinline__ void update(const Consts& k, float g, float& p, float& m, float& v) {
   {
 #pragma clang fp contract(off)
@@ -64,8 +94,200 @@ __device__ __forceinline__ void update(const Consts& k, float g, float& p, float
     m = m * k.b1 + g * k.c1;
     v = v * k.b2 + (g * g) * k.c2;
   }
-  const float den = fmaf(sqrtf(v), k.rs, k.eps);
-  p -= fmaf(k.lrwd, p, k.ss * (m / den));
+  const bool tiny = v < 0x1p-96f;
+  const float root = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v) * (tiny ? 0x1p-32f : 1.f);
+  const float den = fmaf(root, k.rs, k.eps);
+  p -= fmaf(k.lrwd, p, k.ss * (m * fast_rcp(den)));
+}
+
+// The tensors of an item.
+struct Item {
+  float* p;
+  bf16* copy;
+  const void* g;
+  void *m, *v;
+  float *ms, *vs;
+  int64_t n;
+};
+
+// Four elements of one unit, this lane's.
+struct Four {
+  float p[4], g[4], m[4], v[4];
+};
+
+template <typename V> __device__ __forceinline__ V get(const void* base, int64_t i) {
+  return reinterpret_cast<const V*>(base)[i];
+}
+
+// WHOLE: units that lie inside of the tensor, with 16-byte accesses; otherwise
+// element by element up to its end.
+template <bool Q8, bool GB, bool WHOLE>
+__device__ __forceinline__ void load_unit(const Item& t, int64_t i0, int live, Four& x, uint32_t& mc,
+                                          uint32_t& vc) {
+  if constexpr (WHOLE) {
+    const f32x4 p = get<f32x4>(t.p, i0 / 4);
+    f32x4 m, v;
+    if constexpr (Q8) {
+      mc = get<uint32_t>(t.m, i0 / 4);
+      vc = get<uint32_t>(t.v, i0 / 4);
+    } else {
+      m = get<f32x4>(t.m, i0 / 4);
+      v = get<f32x4>(t.v, i0 / 4);
+    }
+    if constexpr (GB) {
+      const bf16x4 g = get<bf16x4>(t.g, i0 / 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.g[e] = (float)g[e];
+    } else {
+      const f32x4 g = get<f32x4>(t.g, i0 / 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.g[e] = g[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x.p[e] = p[e];
+      if constexpr (!Q8) {
+        x.m[e] = m[e];
+        x.v[e] = v[e];
+      }
+    }
+  } else {
+    mc = vc = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t i = i0 + e;
+      const bool in = e < live;
+      x.p[e] = in ? t.p[i] : 0.f;
+      x.g[e] = !in ? 0.f : GB ? (float)get<bf16>(t.g, i) : get<float>(t.g, i);
+      if constexpr (Q8) {
+        if (in) {
+          mc |= (uint32_t)get<uint8_t>(t.m, i) << 8 * e;
+          vc |= (uint32_t)get<uint8_t>(t.v, i) << 8 * e;
+        }
+      } else {
+        x.m[e] = in ? get<float>(t.m, i) : 0.f;
+        x.v[e] = in ? get<float>(t.v, i) : 0.f;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  const auto step = [&](auto ctrl) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, 0xF, 0xF, false));
+  };
+  step(std::integral_constant<int, kQuadSwap1>{});
+  step(std::integral_constant<int, kQuadSwap2>{});
+  step(std::integral_constant<int, kHalfMirror>{});
+  step(std::integral_constant<int, kMirror>{});
+  // (the four rows of 16 lanes)
+  return max(max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+             max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
+// Codes of a unit's new moments (lanes behind the end: zeros).
+__device__ __forceinline__ void encode(const Four& x, uint32_t kb, int lane, float& sm, float& sv,
+                                       uint32_t& mc, uint32_t& vc) {
+  uint32_t bm = 0, bv = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    bm = max(bm, __builtin_bit_cast(uint32_t, x.m[e]) & 0x7fffffffu);
+    bv = max(bv, __builtin_bit_cast(uint32_t, x.v[e]));
+  }
+  sm = block_scale(wave_max(bm));
+  sv = block_scale(wave_max(bv));
+  // (powers of two: exact; a NaN stays one)
+  const float im = sm == 0.f ? 0.f : fast_rcp_pow2(sm), iv = sv == 0.f ? 0.f : fast_rcp_pow2(sv);
+  mc = vc = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t h = fmix32(kb + (uint32_t)(4 * lane + e));
+    int c = code_of(fabsf(x.m[e]), im, h & 0xffffu, kLoM);
+    c = min(max(c, 0), 127);
+    c |= c && x.m[e] < 0.f ? 128 : 0;
+    int d = code_of(x.v[e], iv, h >> 16, kLoV);
+    d = x.v[e] == 0.f ? 0 : min(max(d, 1), 255);
+    mc |= (uint32_t)c << 8 * e;
+    vc |= (uint32_t)d << 8 * e;
+  }
+}
+
+template <bool Q8, bool GB, bool WHOLE, int U>
+__device__ __forceinline__ void units(const Item& t, int64_t unit0, const Consts& k, uint32_t key) {
+  const int lane = lane_id();
+  Four x[U];
+  uint32_t mc[U], vc[U];
+  float sm[U], sv[U];
+  int live[U];
+#pragma unroll
+  for (int w = 0; w < U; ++w) {
+    const int64_t i0 = (unit0 + w) * kUnit + 4 * lane, left = t.n - i0;
+    live[w] = WHOLE ? 4 : left >= 4 ? 4 : left > 0 ? (int)left : 0;
+    load_unit<Q8, GB, WHOLE>(t, i0, live[w], x[w], mc[w], vc[w]);
+    if constexpr (Q8) {
+      sm[w] = t.ms[unit0 + w];
+      sv[w] = t.vs[unit0 + w];
+    }
+  }
+#pragma unroll
+  for (int w = 0; w < U; ++w) {
+    const int64_t unit = unit0 + w, i0 = unit * kUnit + 4 * lane;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (Q8) {
+        const uint32_t c = mc[w] >> 8 * e & 0xffu;
+        const float mag = level(c & 127u, kLoM) * sm[w];
+        x[w].m[e] = c & 128u ? -mag : mag;
+        x[w].v[e] = level(vc[w] >> 8 * e & 0xffu, kLoV) * sv[w];
+      }
+      update(k, x[w].g[e], x[w].p[e], x[w].m[e], x[w].v[e]);
+      if (!WHOLE && e >= live[w]) x[w].m[e] = x[w].v[e] = 0.f;
+    }
+    if constexpr (Q8) encode(x[w], mix32(key, (uint32_t)unit), lane, sm[w], sv[w], mc[w], vc[w]);
+    if constexpr (WHOLE) {
+      reinterpret_cast<f32x4*>(t.p)[i0 / 4] = f32x4{x[w].p[0], x[w].p[1], x[w].p[2], x[w].p[3]};
+      if (t.copy)
+        reinterpret_cast<bf16x4*>(t.copy)[i0 / 4] =
+            bf16x4{(bf16)x[w].p[0], (bf16)x[w].p[1], (bf16)x[w].p[2], (bf16)x[w].p[3]};
+      if constexpr (Q8) {
+        reinterpret_cast<uint32_t*>(t.m)[i0 / 4] = mc[w];
+        reinterpret_cast<uint32_t*>(t.v)[i0 / 4] = vc[w];
+      } else {
+        reinterpret_cast<f32x4*>(t.m)[i0 / 4] = f32x4{x[w].m[0], x[w].m[1], x[w].m[2], x[w].m[3]};
+        reinterpret_cast<f32x4*>(t.v)[i0 / 4] = f32x4{x[w].v[0], x[w].v[1], x[w].v[2], x[w].v[3]};
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e < live[w]) {
+          t.p[i0 + e] = x[w].p[e];
+          if (t.copy) t.copy[i0 + e] = (bf16)x[w].p[e];
+          if constexpr (Q8) {
+            reinterpret_cast<uint8_t*>(t.m)[i0 + e] = (uint8_t)(mc[w] >> 8 * e);
+            reinterpret_cast<uint8_t*>(t.v)[i0 + e] = (uint8_t)(vc[w] >> 8 * e);
+          } else {
+            reinterpret_cast<float*>(t.m)[i0 + e] = x[w].m[e];
+            reinterpret_cast<float*>(t.v)[i0 + e] = x[w].v[e];
+          }
+        }
+    }
+    if constexpr (Q8)
+      if (lane == 0) {
+        t.ms[unit] = sm[w];
+        t.vs[unit] = sv[w];
+      }
+  }
+}
+
+template <bool Q8, bool GB>
+__device__ __forceinline__ void wave_units(const Item& t, int64_t unit0, const Consts& k,
+                                           uint32_t key) {
+  if ((unit0 + kWaveUnits) * kUnit <= t.n) {
+    units<Q8, GB, true, kWaveUnits>(t, unit0, k, key);
+  } else {
+    for (int w = 0; w < kWaveUnits && (unit0 + w) * kUnit < t.n; ++w)
+      units<Q8, GB, false, 1>(t, unit0 + w, k, key);
+  }
 }
 
 __global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
@@ -78,108 +300,65 @@ __global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
     if (A->first[mid] <= b) lo = mid;
     else hi = mid;
   }
-  const int k = lo;
-  const int64_t n = A->it[k].n;
-  float* P = A->it[k].p;
-  bf16* CP = reinterpret_cast<bf16*>(A->it[k].copy);
-  const void* G = A->it[k].g;
-  void* M = A->it[k].m;
-  void* V = A->it[k].v;
-  float* MS = A->it[k].ms;
-  float* VS = A->it[k].vs;
-  const uint32_t bits = A->it[k].bits;
+  const int i = lo;
+  const Item t = {A->it[i].p, reinterpret_cast<bf16*>(A->it[i].copy), A->it[i].g, A->it[i].m,
+                  A->it[i].v, A->it[i].ms, A->it[i].vs, A->it[i].n};
+  const uint32_t bits = A->it[i].bits;
 
-  Consts c;
-  c.b1 = A->b1; c.b2 = A->b2; c.c1 = A->c1; c.c2 = A->c2;
-  c.gs = A->gscale ? *A->gscale : 1.f;
-  const double lr = A->lr_dev ? (double)*A->lr_dev : A->lr;
-  const int64_t step = A->step_dev ? *A->step_dev : A->step;
-  c.ss = (float)(lr / (1.0 - exp2((double)step * A->log2b1)));
-  c.rs = (float)(1.0 / sqrt(1.0 - exp2((double)step * A->log2b2)));
-  c.eps = (float)A->eps;
-  c.lrwd = (float)(lr * (double)A->it[k].wd);
-  const uint32_t key = mix32(mix32(A->seed_key, (uint32_t)step), (uint32_t)(A->base + k));
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int w = 0; w < kWaveUnits; ++w) {
-    const int64_t unit = ((int64_t)(b - A->first[k]) * 4 + wave) * kWaveUnits + w;
-    const int64_t i0 = unit * kUnit + 4 * lane;
-    if (unit * kUnit >= n) break;
-    const int live = n - i0 >= 4 ? 4 : n > i0 ? (int)(n - i0) : 0;  // of this lane's four
-    float p[4], g[4], m[4], v[4];
-    uint32_t mc = 0, vc = 0;
-    float sm = 0.f, sv = 0.f;
-    if (bits & 2) {
-      sm = MS[unit];
-      sv = VS[unit];
-    }
-    for (int e = 0; e < 4; ++e) {
-      p[e] = g[e] = m[e] = v[e] = 0.f;
-      if (e < live) {
-        p[e] = P[i0 + e];
-        g[e] = bits & 1 ? (float)reinterpret_cast<const bf16*>(G)[i0 + e]
-                        : reinterpret_cast<const float*>(G)[i0 + e];
-        if (bits & 2) {
-          const uint32_t x = reinterpret_cast<const uint8_t*>(M)[i0 + e];
-          const float mag = level(x & 127, kLoM) * sm;
-          m[e] = x & 128 ? -mag : mag;
-          v[e] = level(reinterpret_cast<const uint8_t*>(V)[i0 + e], kLoV) * sv;
-        } else {
-          m[e] = reinterpret_cast<const float*>(M)[i0 + e];
-          v[e] = reinterpret_cast<const float*>(V)[i0 + e];
-        }
-      }
-    }
-    for (int e = 0; e < 4; ++e) update(c, g[e], p[e], m[e], v[e]);
-    for (int e = 0; e < live; ++e) {
-      P[i0 + e] = p[e];
-      if (CP) CP[i0 + e] = (bf16)p[e];
-    }
-    if (!(bits & 2)) {
-      for (int e = 0; e < live; ++e) {
-        reinterpret_cast<float*>(M)[i0 + e] = m[e];
-        reinterpret_cast<float*>(V)[i0 + e] = v[e];
-      }
-      continue;
-    }
-    uint32_t bm = 0, bv = 0;
-    for (int e = 0; e < 4; ++e)
-      if (e < live) {
-        bm = max(bm, __builtin_bit_cast(uint32_t, fabsf(m[e])));
-        bv = max(bv, __builtin_bit_cast(uint32_t, v[e]));
-      }
-    for (int o = 1; o < 64; o <<= 1) {
-      bm = max(bm, (uint32_t)__shfl_xor((int)bm, o));
-      bv = max(bv, (uint32_t)__shfl_xor((int)bv, o));
-    }
-    sm = block_scale(bm);
-    sv = block_scale(bv);
-    const float im = sm == 0.f ? 0.f : __fdiv_rn(1.f, sm), iv = sv == 0.f ? 0.f : __fdiv_rn(1.f, sv);
-    const uint32_t kb = mix32(key, (uint32_t)unit);
-    for (int e = 0; e < live; ++e) {
-      const uint32_t h = fmix32(kb + (uint32_t)(4 * lane + e));
-      int x = code_of(fabsf(m[e]), im, h & 0xffffu, kLoM);
-      x = x < 0 ? 0 : x > 127 ? 127 : x;
-      if (x && m[e] < 0.f) x |= 128;
-      int y = code_of(v[e], iv, h >> 16, kLoV);
-      y = v[e] == 0.f ? 0 : y < 1 ? 1 : y > 255 ? 255 : y;
-      reinterpret_cast<uint8_t*>(M)[i0 + e] = (uint8_t)x;
-      reinterpret_cast<uint8_t*>(V)[i0 + e] = (uint8_t)y;
-    }
-    if (lane == 0) {
-      MS[unit] = sm;
-      VS[unit] = sv;
-    }
+  Consts k;
+  k.b1 = A->b1; k.b2 = A->b2; k.c1 = A->c1; k.c2 = A->c2;
+  k.gs = A->gscale ? *A->gscale : 1.f;
+  k.eps = A->eps;
+  double lr = A->lr;
+  uint32_t step_key = A->step_key;
+  k.ss = A->ss;
+  k.rs = A->rs;
+  if (A->lr_dev || A->step_dev) {  // a captured graph's: as the host forms them
+    if (A->lr_dev) lr = (double)*A->lr_dev;
+    const int64_t step = A->step_dev ? *A->step_dev : A->step;
+    adam_step_consts(lr, A->beta1, A->beta2, step, k.ss, k.rs);
+    step_key = mix32(A->seed_key, (uint32_t)step);
+  }
+  k.lrwd = (float)(lr * (double)A->it[i].wd);
+  const uint32_t key = mix32(step_key, (uint32_t)(A->base + i));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit0 = ((int64_t)(b - A->first[i]) * 4 + wave) * kWaveUnits;
+  if (bits & 2) {
+    if (bits & 1) wave_units<true, true>(t, unit0, k, key);
+    else wave_units<true, false>(t, unit0, k, key);
+  } else {
+    if (bits & 1) wave_units<false, true>(t, unit0, k, key);
+    else wave_units<false, false>(t, unit0, k, key);
   }
 }
 
+// Four codes per thread (the last ones one by one).
 __global__ void __launch_bounds__(256) k_adam_unpack(int64_t n, const uint8_t* codes,
                                                      const float* scales, int sgn, float* out) {
   const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
-    const uint32_t x = codes[i], c = sgn ? x & 127 : x;
-    const float mag = level(c, sgn ? kLoM : kLoV) * scales[i / kUnit];
-    out[i] = sgn && (x & 128) ? -mag : mag;
+  for (int64_t q = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; 4 * q < n; q += stride) {
+    const bool whole = 4 * q + 4 <= n;
+    uint32_t w = 0;
+    if (whole) {
+      w = reinterpret_cast<const uint32_t*>(codes)[q];
+    } else {
+      for (int e = 0; 4 * q + e < n; ++e) w |= (uint32_t)codes[4 * q + e] << 8 * e;
+    }
+    const float s = scales[q / (kUnit / 4)];
+    f32x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t x = w >> 8 * e & 0xffu, c = sgn ? x & 127u : x;
+      const float mag = level(c, sgn ? kLoM : kLoV) * s;
+      o[e] = sgn && (x & 128u) ? -mag : mag;
+    }
+    if (whole) {
+      reinterpret_cast<f32x4*>(out)[q] = o;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (4 * q + e < n) out[4 * q + e] = o[e];
+    }
   }
 }
 
@@ -195,7 +374,7 @@ hipError_t launch_adamw(const AdamBatch& b, hipStream_t st) {
 
 hipError_t launch_adam_unpack(int64_t n, const uint8_t* codes, const float* scales, bool sgn,
                               float* out, hipStream_t st) {
-  const int64_t need = (n + 255) / 256;
+  const int64_t need = (n + 1023) / 1024;
   hipLaunchKernelGGL(k_adam_unpack, dim3((unsigned)(need < 8192 ? need : 8192)), dim3(256), 0, st,
                      n, codes, scales, sgn ? 1 : 0, out);
   return hipGetLastError();

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -218,8 +219,8 @@ pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args*
     return err(PA_ERR_INVALID, "%s: items and args are required", who);
   const auto unit = [](double b) { return b >= 0.0 && b < 1.0; };
   if (!std::isfinite(args->lr) || !unit(args->beta1) || !unit(args->beta2) ||
-      !std::isfinite(args->eps) || !((float)args->eps > 0.f))
-    return err(PA_ERR_INVALID, "%s: lr finite, betas in [0, 1), eps > 0", who);
+      !std::isfinite(args->eps) || !((float)args->eps >= FLT_MIN))
+    return err(PA_ERR_INVALID, "%s: lr finite, betas in [0, 1), eps at least %g", who, FLT_MIN);
   if (!args->step_dev && args->step < 1) return err(PA_ERR_INVALID, "%s: step must be >= 1", who);
   PO_TRY(opt(who, args->gscale, "gscale", 4));
   PO_TRY(opt(who, args->lr_dev, "lr_dev", 4));
@@ -243,12 +244,14 @@ pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args*
   }
   PO_TRY(adamw_overlap(who, n_items, items));
   pa::AdamBatch b{};
-  b.log2b1 = std::log2(args->beta1);
-  b.log2b2 = std::log2(args->beta2);
-  b.lr = args->lr; b.eps = args->eps;
+  b.lr = args->lr; b.beta1 = args->beta1; b.beta2 = args->beta2;
+  b.eps = (float)args->eps;
   b.gscale = args->gscale; b.lr_dev = args->lr_dev; b.step_dev = args->step_dev;
   b.step = args->step;
   b.seed_key = pa::adam_mix((uint32_t)args->seed, (uint32_t)(args->seed >> 32));
+  b.step_key = pa::adam_mix(b.seed_key, (uint32_t)args->step);
+  if (!args->step_dev)
+    pa::adam_consts(args->lr, args->beta1, args->beta2, args->step, &b.ss, &b.rs);
   b.b1 = (float)args->beta1; b.c1 = (float)(1.0 - args->beta1);
   b.b2 = (float)args->beta2; b.c2 = (float)(1.0 - args->beta2);
   for (int i = 0; i < n_items;) {

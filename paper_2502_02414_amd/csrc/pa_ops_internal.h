@@ -32,7 +32,7 @@ hipError_t launch_resnorm(const ResNormArgs& a, int dtype, bool bwd, hipStream_t
 // ---- AdamW (pa_adamw.hip) ----
 // One launch's items, at most kAdamMax; first[i]: the launch's first block that
 // works on item i.
-constexpr int kAdamMax = 40;
+constexpr int kAdamMax = 52;
 struct AdamItem {
   float* p;
   void* copy;
@@ -44,17 +44,20 @@ struct AdamItem {
   uint32_t bits;  // 1: bf16 gradient, 2: 8-bit moments
 };
 struct AdamBatch {
-  double log2b1, log2b2, lr, eps;
+  double lr, beta1, beta2;
   const float* gscale;
   const float* lr_dev;
   const int64_t* step_dev;
   int64_t step;
-  uint32_t seed_key;          // mix(seed, seed >> 32)
-  float b1, b2, c1, c2;       // c = 1 - b
+  float ss, rs;               // adam_consts of lr and step
+  uint32_t seed_key, step_key;  // mix(seed, seed >> 32), mix(that, step)
+  float b1, b2, c1, c2, eps;  // c = 1 - b
   int n, base;                // items; the index of item 0 in the call
   uint32_t first[kAdamMax + 1];
   AdamItem it[kAdamMax];
 };
+static_assert(sizeof(AdamBatch) <= 4096, "a launch's arguments");
+void adam_consts(double lr, double b1, double b2, int64_t step, float* ss, float* rs);
 uint32_t adam_mix(uint32_t a, uint32_t b);
 uint32_t adam_blocks(int64_t n);  // blocks that an item of n elements takes
 hipError_t launch_adamw(const AdamBatch& b, hipStream_t st);
