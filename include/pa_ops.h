@@ -143,6 +143,19 @@ typedef struct {
 pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args* args,
                    void* stream);
 
+/* The same step over a table that a program keeps where its tensors stay where
+ * they are: one launch however many tensors there are, and nothing to check or
+ * copy per step.  pa_adamw_table_size: the table's bytes and its blocks;
+ * pa_adamw_table fills `host` (host memory, 8-byte aligned) with it, which the
+ * caller copies to the device, `table` of pa_adamw_run, and fills anew when a
+ * tensor (a gradient, too) moves.  Both make pa_adamw's checks of the items;
+ * pa_adamw_run takes the table on trust.  Same results, bit for bit. */
+pa_status pa_adamw_table_size(int n_items, const pa_adamw_item* items, size_t* bytes,
+                              int64_t* blocks);
+pa_status pa_adamw_table(int n_items, const pa_adamw_item* items, void* host, size_t bytes);
+pa_status pa_adamw_run(int n_items, int64_t blocks, const void* table, const pa_adamw_args* args,
+                       void* stream);
+
 /* The values that n codes stand for: out [n] fp32 (is_signed = 1: m's codes,
  * 0: v's). */
 pa_status pa_adamw_unpack(int64_t n, const void* codes, const float* scales, int is_signed,

@@ -1,7 +1,8 @@
 // One AdamW step over many tensors (gfx950), moments in fp32 or in 8 bits; the
 // formulas and the 8-bit code are in include/pa_ops.h.
 //
-// A launch takes up to kAdamMax tensors, described in its arguments.  A block
+// A launch takes the tensors of a table in device memory, or up to kAdamMax of
+// them that are described in its arguments.  A block
 // works on 16 units of 256 consecutive elements of one tensor, a wave on four of
 // them, four elements per lane: a unit is a block of the 8-bit moments, whose
 // largest magnitude is a reduction within the wave.
@@ -290,21 +291,11 @@ __device__ __forceinline__ void wave_units(const Item& t, int64_t unit0, const C
   }
 }
 
-__global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
-  const ArgPtr A = kernel_args();
-  // the item of this block: the last one that starts at or before it
-  const uint32_t b = blockIdx.x;
-  int lo = 0, hi = A->n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (A->first[mid] <= b) lo = mid;
-    else hi = mid;
-  }
-  const int i = lo;
-  const Item t = {A->it[i].p, reinterpret_cast<bf16*>(A->it[i].copy), A->it[i].g, A->it[i].m,
-                  A->it[i].v, A->it[i].ms, A->it[i].vs, A->it[i].n};
-  const uint32_t bits = A->it[i].bits;
-
+// Block `b` of an item whose first block is `first`; A: where the step's constants
+// are (the launch's arguments).
+template <typename Step>
+__device__ __forceinline__ void item_block(Step A, const Item& t, float wd, uint32_t bits,
+                                           uint32_t index, uint32_t b) {
   Consts k;
   k.b1 = A->b1; k.b2 = A->b2; k.c1 = A->c1; k.c2 = A->c2;
   k.gs = A->gscale ? *A->gscale : 1.f;
@@ -319,10 +310,10 @@ __global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
     adam_step_consts(lr, A->beta1, A->beta2, step, k.ss, k.rs);
     step_key = mix32(A->seed_key, (uint32_t)step);
   }
-  k.lrwd = (float)(lr * (double)A->it[i].wd);
-  const uint32_t key = mix32(step_key, (uint32_t)(A->base + i));
+  k.lrwd = (float)(lr * (double)wd);
+  const uint32_t key = mix32(step_key, index);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t unit0 = ((int64_t)(b - A->first[i]) * 4 + wave) * kWaveUnits;
+  const int64_t unit0 = ((int64_t)b * 4 + wave) * kWaveUnits;
   if (bits & 2) {
     if (bits & 1) wave_units<true, true>(t, unit0, k, key);
     else wave_units<true, false>(t, unit0, k, key);
@@ -330,6 +321,30 @@ __global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
     if (bits & 1) wave_units<false, true>(t, unit0, k, key);
     else wave_units<false, false>(t, unit0, k, key);
   }
+}
+
+template <typename I> __device__ __forceinline__ Item tensors(const I& i) {
+  return {i.p, reinterpret_cast<bf16*>(i.copy), i.g, i.m, i.v, i.ms, i.vs, i.n};
+}
+
+__global__ void __launch_bounds__(256) k_adamw(AdamBatch by_value) {
+  const ArgPtr A = kernel_args();
+  // the item of this block: the last one that starts at or before it
+  const uint32_t b = blockIdx.x;
+  int lo = 0, hi = A->n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (A->first[mid] <= b) lo = mid;
+    else hi = mid;
+  }
+  item_block(&A->s, tensors(A->it[lo]), A->it[lo].wd, A->it[lo].bits, (uint32_t)(A->base + lo),
+             b - A->first[lo]);
+}
+
+__global__ void __launch_bounds__(256) k_adamw_table(AdamStep s, const AdamEntry* entries,
+                                                     const uint32_t* map) {
+  const AdamEntry* e = entries + map[blockIdx.x];
+  item_block(&s, tensors(e->it), e->it.wd, e->it.bits, e->index, blockIdx.x - e->first);
 }
 
 // Four codes per thread (the last ones one by one).
@@ -369,6 +384,12 @@ uint32_t adam_blocks(int64_t n) { return (uint32_t)((n + kBlockElems - 1) / kBlo
 hipError_t launch_adamw(const AdamBatch& b, hipStream_t st) {
   if (b.n < 1 || b.n > kAdamMax || b.first[b.n] < 1) return hipErrorInvalidValue;
   hipLaunchKernelGGL(k_adamw, dim3(b.first[b.n]), dim3(256), 0, st, b);
+  return hipGetLastError();
+}
+
+hipError_t launch_adamw_table(const AdamStep& s, const AdamEntry* entries, const uint32_t* map,
+                              uint32_t blocks, hipStream_t st) {
+  hipLaunchKernelGGL(k_adamw_table, dim3(blocks), dim3(256), 0, st, s, entries, map);
   return hipGetLastError();
 }
 

@@ -212,19 +212,8 @@ static pa_status adamw_overlap(const char* who, int n, const pa_adamw_item* item
   return PA_OK;
 }
 
-pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args* args,
-                   void* stream) {
-  const char* who = "pa_adamw";
-  if (n_items < 0 || (n_items && !items) || !args)
-    return err(PA_ERR_INVALID, "%s: items and args are required", who);
-  const auto unit = [](double b) { return b >= 0.0 && b < 1.0; };
-  if (!std::isfinite(args->lr) || !unit(args->beta1) || !unit(args->beta2) ||
-      !std::isfinite(args->eps) || !((float)args->eps >= FLT_MIN))
-    return err(PA_ERR_INVALID, "%s: lr finite, betas in [0, 1), eps at least %g", who, FLT_MIN);
-  if (!args->step_dev && args->step < 1) return err(PA_ERR_INVALID, "%s: step must be >= 1", who);
-  PO_TRY(opt(who, args->gscale, "gscale", 4));
-  PO_TRY(opt(who, args->lr_dev, "lr_dev", 4));
-  PO_TRY(opt(who, args->step_dev, "step_dev", 8));
+static pa_status adamw_items(const char* who, int n_items, const pa_adamw_item* items) {
+  if (n_items < 0 || (n_items && !items)) return err(PA_ERR_INVALID, "%s: items are required", who);
   for (int i = 0; i < n_items; ++i) {
     const pa_adamw_item& t = items[i];
     if (t.n < 0 || t.n > ((int64_t)1 << 36))
@@ -242,31 +231,107 @@ pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args*
     PO_TRY(opt(who, t.v_scale, "v_scale", 4));
     if (!std::isfinite(t.wd)) return err(PA_ERR_INVALID, "%s: wd must be finite", who);
   }
-  PO_TRY(adamw_overlap(who, n_items, items));
-  pa::AdamBatch b{};
-  b.lr = args->lr; b.beta1 = args->beta1; b.beta2 = args->beta2;
-  b.eps = (float)args->eps;
-  b.gscale = args->gscale; b.lr_dev = args->lr_dev; b.step_dev = args->step_dev;
-  b.step = args->step;
-  b.seed_key = pa::adam_mix((uint32_t)args->seed, (uint32_t)(args->seed >> 32));
-  b.step_key = pa::adam_mix(b.seed_key, (uint32_t)args->step);
+  return adamw_overlap(who, n_items, items);
+}
+
+static pa::AdamItem adamw_item(const pa_adamw_item& t) {
+  return {t.p, t.copy, t.g, t.m, t.v, t.m_scale, t.v_scale, t.n, t.wd,
+          (t.g_dtype == PA_BF16 ? 1u : 0u) | (t.m_scale ? 2u : 0u)};
+}
+
+static pa_status adamw_step(const char* who, const pa_adamw_args* args, pa::AdamStep* s) {
+  if (!args) return err(PA_ERR_INVALID, "%s: args is NULL", who);
+  const auto unit = [](double b) { return b >= 0.0 && b < 1.0; };
+  if (!std::isfinite(args->lr) || !unit(args->beta1) || !unit(args->beta2) ||
+      !std::isfinite(args->eps) || !((float)args->eps >= FLT_MIN))
+    return err(PA_ERR_INVALID, "%s: lr finite, betas in [0, 1), eps at least %g", who, FLT_MIN);
+  if (!args->step_dev && args->step < 1) return err(PA_ERR_INVALID, "%s: step must be >= 1", who);
+  PO_TRY(opt(who, args->gscale, "gscale", 4));
+  PO_TRY(opt(who, args->lr_dev, "lr_dev", 4));
+  PO_TRY(opt(who, args->step_dev, "step_dev", 8));
+  s->lr = args->lr; s->beta1 = args->beta1; s->beta2 = args->beta2;
+  s->eps = (float)args->eps;
+  s->gscale = args->gscale; s->lr_dev = args->lr_dev; s->step_dev = args->step_dev;
+  s->step = args->step;
+  s->seed_key = pa::adam_mix((uint32_t)args->seed, (uint32_t)(args->seed >> 32));
+  s->step_key = pa::adam_mix(s->seed_key, (uint32_t)args->step);
   if (!args->step_dev)
-    pa::adam_consts(args->lr, args->beta1, args->beta2, args->step, &b.ss, &b.rs);
-  b.b1 = (float)args->beta1; b.c1 = (float)(1.0 - args->beta1);
-  b.b2 = (float)args->beta2; b.c2 = (float)(1.0 - args->beta2);
+    pa::adam_consts(args->lr, args->beta1, args->beta2, args->step, &s->ss, &s->rs);
+  s->b1 = (float)args->beta1; s->c1 = (float)(1.0 - args->beta1);
+  s->b2 = (float)args->beta2; s->c2 = (float)(1.0 - args->beta2);
+  return PA_OK;
+}
+
+pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args* args,
+                   void* stream) {
+  const char* who = "pa_adamw";
+  pa::AdamBatch b{};
+  PO_TRY(adamw_step(who, args, &b.s));
+  PO_TRY(adamw_items(who, n_items, items));
   for (int i = 0; i < n_items;) {
     // the next items, up to kAdamMax (one without elements takes no block)
     b.n = 0;
     b.base = i;
     b.first[0] = 0;
     for (; i < n_items && b.n < pa::kAdamMax; ++i, ++b.n) {
-      const pa_adamw_item& t = items[i];
-      b.it[b.n] = {t.p, t.copy, t.g, t.m, t.v, t.m_scale, t.v_scale, t.n, t.wd,
-                   (t.g_dtype == PA_BF16 ? 1u : 0u) | (t.m_scale ? 2u : 0u)};
-      b.first[b.n + 1] = b.first[b.n] + pa::adam_blocks(t.n);
+      b.it[b.n] = adamw_item(items[i]);
+      b.first[b.n + 1] = b.first[b.n] + pa::adam_blocks(items[i].n);
     }
     if (b.first[b.n]) PO_HIP(pa::launch_adamw(b, as_stream(stream)), who);
   }
+  return PA_OK;
+}
+
+// A table's blocks, or -1: more than a launch takes.
+static int64_t adamw_blocks(int n_items, const pa_adamw_item* items) {
+  int64_t blocks = 0;
+  for (int i = 0; i < n_items; ++i) blocks += pa::adam_blocks(items[i].n);
+  return blocks <= 0x7fffffff ? blocks : -1;
+}
+
+pa_status pa_adamw_table_size(int n_items, const pa_adamw_item* items, size_t* bytes,
+                              int64_t* blocks) {
+  const char* who = "pa_adamw_table_size";
+  if (!bytes || !blocks) return err(PA_ERR_INVALID, "%s: bytes and blocks are required", who);
+  PO_TRY(adamw_items(who, n_items, items));
+  *blocks = adamw_blocks(n_items, items);
+  if (*blocks < 0) return err(PA_ERR_UNSUPPORTED, "%s: too many elements for one table", who);
+  *bytes = sizeof(pa::AdamEntry) * (size_t)n_items + sizeof(uint32_t) * (size_t)*blocks;
+  return PA_OK;
+}
+
+pa_status pa_adamw_table(int n_items, const pa_adamw_item* items, void* host, size_t bytes) {
+  const char* who = "pa_adamw_table";
+  size_t size = 0;
+  int64_t blocks = 0;
+  PO_TRY(pa_adamw_table_size(n_items, items, &size, &blocks));
+  if (size && (!host || bytes < size))
+    return err(PA_ERR_WORKSPACE, "%s: the table needs %zu bytes", who, size);
+  PO_TRY(opt(who, host, "host", 8));
+  pa::AdamEntry* e = reinterpret_cast<pa::AdamEntry*>(host);
+  uint32_t* map = reinterpret_cast<uint32_t*>(e + n_items);
+  uint32_t first = 0;
+  for (int i = 0; i < n_items; ++i) {
+    const uint32_t k = pa::adam_blocks(items[i].n);
+    e[i] = {adamw_item(items[i]), first, (uint32_t)i};
+    for (uint32_t j = 0; j < k; ++j) map[first + j] = (uint32_t)i;
+    first += k;
+  }
+  return PA_OK;
+}
+
+pa_status pa_adamw_run(int n_items, int64_t blocks, const void* table, const pa_adamw_args* args,
+                       void* stream) {
+  const char* who = "pa_adamw_run";
+  pa::AdamStep s{};
+  PO_TRY(adamw_step(who, args, &s));
+  if (n_items < 0 || blocks < 0 || blocks > 0x7fffffff)
+    return err(PA_ERR_INVALID, "%s: n_items and blocks as pa_adamw_table_size gave them", who);
+  if (!blocks) return PA_OK;
+  PO_TRY(need(who, table, "table"));
+  const pa::AdamEntry* e = reinterpret_cast<const pa::AdamEntry*>(table);
+  PO_HIP(pa::launch_adamw_table(s, e, reinterpret_cast<const uint32_t*>(e + n_items),
+                                (uint32_t)blocks, as_stream(stream)), who);
   return PA_OK;
 }
 

@@ -30,9 +30,6 @@ int resnorm_blocks(int64_t N, int C, int dtype, bool bwd);
 hipError_t launch_resnorm(const ResNormArgs& a, int dtype, bool bwd, hipStream_t st);
 
 // ---- AdamW (pa_adamw.hip) ----
-// One launch's items, at most kAdamMax; first[i]: the launch's first block that
-// works on item i.
-constexpr int kAdamMax = 52;
 struct AdamItem {
   float* p;
   void* copy;
@@ -43,7 +40,8 @@ struct AdamItem {
   float wd;
   uint32_t bits;  // 1: bf16 gradient, 2: 8-bit moments
 };
-struct AdamBatch {
+// What all tensors of a step have in common.
+struct AdamStep {
   double lr, beta1, beta2;
   const float* gscale;
   const float* lr_dev;
@@ -52,11 +50,25 @@ struct AdamBatch {
   float ss, rs;               // adam_consts of lr and step
   uint32_t seed_key, step_key;  // mix(seed, seed >> 32), mix(that, step)
   float b1, b2, c1, c2, eps;  // c = 1 - b
-  int n, base;                // items; the index of item 0 in the call
+};
+// Tensors in a launch's arguments, at most kAdamMax; first[i]: the launch's first
+// block that works on item i.
+constexpr int kAdamMax = 52;
+struct AdamBatch {
+  AdamStep s;
+  int n, base;  // items; the index of item 0 in the call
   uint32_t first[kAdamMax + 1];
   AdamItem it[kAdamMax];
 };
 static_assert(sizeof(AdamBatch) <= 4096, "a launch's arguments");
+// Tensors in a table in device memory: the entries, then the entry of each block.
+struct AdamEntry {
+  AdamItem it;
+  uint32_t first;  // the first block that works on it
+  uint32_t index;  // in the call's list
+};
+hipError_t launch_adamw_table(const AdamStep& s, const AdamEntry* entries, const uint32_t* map,
+                              uint32_t blocks, hipStream_t st);
 void adam_consts(double lr, double b1, double b2, int64_t step, float* ss, float* rs);
 uint32_t adam_mix(uint32_t a, uint32_t b);
 uint32_t adam_blocks(int64_t n);  // blocks that an item of n elements takes

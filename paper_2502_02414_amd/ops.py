@@ -21,7 +21,8 @@ from .binding import PA_BF16, PA_F32, PAError  # noqa: F401
 
 SYMBOLS = (
     "pa_ops_version", "pa_residual_norm", "pa_residual_norm_backward",
-    "pa_residual_norm_workspace", "pa_adamw", "pa_adamw_unpack", "pa_quant_rows",
+    "pa_residual_norm_workspace", "pa_adamw", "pa_adamw_table_size", "pa_adamw_table",
+    "pa_adamw_run", "pa_adamw_unpack", "pa_quant_rows",
     "pa_quant_weight", "pa_gemm_i8", "pa_linear_i8", "pa_linear_i8_workspace",
 )
 
@@ -72,6 +73,10 @@ def load():
     lib.pa_residual_norm_backward.argtypes = [I64, I32, I32, NP] + [_P] * 8 + [NG, _P, S, _P]
     lib.pa_residual_norm_workspace.argtypes = [I64, I32, I32, Sp]
     lib.pa_adamw.argtypes = [I32, ctypes.POINTER(pa_adamw_item), ctypes.POINTER(pa_adamw_args), _P]
+    lib.pa_adamw_table_size.argtypes = [I32, ctypes.POINTER(pa_adamw_item), Sp,
+                                        ctypes.POINTER(I64)]
+    lib.pa_adamw_table.argtypes = [I32, ctypes.POINTER(pa_adamw_item), _P, S]
+    lib.pa_adamw_run.argtypes = [I32, I64, _P, ctypes.POINTER(pa_adamw_args), _P]
     lib.pa_adamw_unpack.argtypes = [I64, _P, _P, I32, _P, _P]
     lib.pa_quant_rows.argtypes = [I64, I32, I32, _P, _P, _P, _P]
     lib.pa_quant_weight.argtypes = [I32, I32, I32, _P, _P, _P, _P]
@@ -241,27 +246,53 @@ def pa_residual_norm_backward(x1, y, par, dx1, dh, dx, dy, gr=None, ws=None, t=N
 
 # ---- AdamW ----
 class AdamWItems:
-    """The host array of pa_adamw's tensors; ``set_grad`` exchanges a gradient."""
+    """The host array of pa_adamw's tensors.  ``set_grad`` exchanges a gradient;
+    ``table`` lays the tensors out on the device for one launch per step, until
+    one of them moves."""
 
     def __init__(self, n):
         self.n = n
         self.arr = (pa_adamw_item * max(n, 1))()
         self.tensors = [None] * n
+        self.dev, self.blocks, self.moved = None, 0, 0
 
     def set_grad(self, i, g):
         it = self.arr[i]
         if g.numel() != it.n:
             raise ValueError(f"g of item {i}: {g.numel()} elements, the item has {it.n}")
-        code = _code(g.dtype, "g")
-        it.g = _dev(g, "g")
-        it.g_dtype = code
+        code, ptr = _code(g.dtype, "g"), _dev(g, "g")
+        if ptr != it.g or code != it.g_dtype:
+            it.g, it.g_dtype = ptr, code
+            self.dev = None
+            self.moved += 1
         self.tensors[i]["g"] = g
 
+    def table(self):
+        """Makes the device table (a copy from host memory that has arrived when
+        this returns, so that every stream may read it)."""
+        torch = _torch()
+        size, blocks = ctypes.c_size_t(0), ctypes.c_int64(0)
+        _check(load().pa_adamw_table_size(self.n, self.arr, ctypes.byref(size),
+                                          ctypes.byref(blocks)))
+        host = torch.empty(-(-max(size.value, 8) // 8), dtype=torch.int64)
+        _check(load().pa_adamw_table(self.n, self.arr, host.data_ptr(), 8 * host.numel()))
+        dev = host.to("cuda")
+        torch.cuda.current_stream().synchronize()
+        self.dev, self.blocks, self.stream = dev, blocks.value, B._stream()
 
-def make_adamw_items(items) -> AdamWItems:
+    def on(self, stream, handle):
+        """The table's pointer for a launch on a stream (its handle given); a
+        stream other than the table's keeps its memory from being handed out."""
+        if handle != self.stream:
+            self.dev.record_stream(stream or _torch().cuda.current_stream())
+        return _dev(self.dev, "table")
+
+
+def make_adamw_items(items, table=True) -> AdamWItems:
     """items: dicts with p (fp32), g (fp32 or bf16), m and v (fp32; or uint8
     with m_scale and v_scale, fp32 [ceil(n / 256)]), optionally copy (bf16)
-    and wd."""
+    and wd.  table: with all gradients given, as a table on the device
+    (AdamWItems.table; waits for the current stream)."""
     torch = _torch()
     f32 = torch.float32
     out = AdamWItems(len(items))
@@ -283,6 +314,8 @@ def make_adamw_items(items) -> AdamWItems:
         out.tensors[i] = dict(d)
         if d.get("g") is not None:
             out.set_grad(i, d["g"])
+    if table and items and all(d.get("g") is not None and d["p"].is_cuda for d in items):
+        out.table()
     return out
 
 
@@ -297,7 +330,12 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
                       _in(gscale, 1, torch.float32, "gscale", False),
                       _in(lr_dev, 1, torch.float32, "lr_dev", False),
                       _in(step_dev, 1, torch.int64, "step_dev", False))
-    _check(load().pa_adamw(items.n, items.arr, ctypes.byref(a), B._stream(stream)))
+    handle = B._stream(stream)
+    if items.dev is not None:
+        _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle),
+                                   ctypes.byref(a), handle))
+    else:
+        _check(load().pa_adamw(items.n, items.arr, ctypes.byref(a), handle))
 
 
 def pa_adamw_unpack(codes, scales, out, signed, stream=None):
@@ -345,8 +383,12 @@ class AdamW:
 
     def step(self, grads, gscale=None, lr=None, stream=None):
         """grads: {name: tensor} for every parameter (fp32 or bf16)."""
+        it = self.items
+        before = it.moved
         for i, k in enumerate(self.names):
-            self.items.set_grad(i, grads[k])
+            it.set_grad(i, grads[k])
+        if it.dev is None and it.moved == before and not _torch().cuda.is_current_stream_capturing():
+            it.table()  # the gradients stay where they are
         pa_adamw(self.items, self.lr if lr is None else lr, self.t + 1, *self.betas, self.eps,
                  self.seed, gscale, stream=stream)
         self.t += 1

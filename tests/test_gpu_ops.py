@@ -305,7 +305,8 @@ def test_adamw_steps(bits, grad):
     gs = torch.tensor([0.7])
     for step in (1, 2, 1000):
         t = on_gpu(before)
-        ops.pa_adamw(ops.make_adamw_items(t), lr=1e-3, step=step, gscale=gs.cuda(), seed=11 + (5 << 40))
+        items = ops.make_adamw_items(t, table=step != 2)
+        ops.pa_adamw(items, lr=1e-3, step=step, gscale=gs.cuda(), seed=11 + (5 << 40))
         check_step(before, t, step, 11 + (5 << 40), gs)
         before = [{k: v.cpu() if torch.is_tensor(v) else v for k, v in d.items()} for d in t]
 
@@ -315,12 +316,50 @@ def test_adamw_more_tensors_than_a_launch_takes():
     sizes[5] = sizes[50] = 5000
     before = adam_tensors(sizes, 4, [F32], lambda n: n % 2 == 0, False)
     empty = {"p": torch.empty(0), "g": torch.empty(0), "m": torch.empty(0), "v": torch.empty(0)}
-    t = on_gpu(before)
-    items = ops.make_adamw_items(t)
-    ops.pa_adamw(items, lr=1e-2, step=3, seed=2, beta1=0.0, beta2=0.5, eps=1e-3)
-    check_step(before, t, 3, 2, lr=1e-2, b1=0.0, b2=0.5, eps=1e-3)
+    for table in (False, True):
+        t = on_gpu(before)
+        items = ops.make_adamw_items(t, table=table)
+        assert (items.dev is not None) == table
+        ops.pa_adamw(items, lr=1e-2, step=3, seed=2, beta1=0.0, beta2=0.5, eps=1e-3)
+        check_step(before, t, 3, 2, lr=1e-2, b1=0.0, b2=0.5, eps=1e-3)
     ops.pa_adamw(ops.make_adamw_items([]), lr=1e-2)
     ops.pa_adamw(ops.make_adamw_items(on_gpu([empty])), lr=1e-2)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_of_named_parameters(bits):
+    """Gradients that move, then stay (a table from then on), then move again, on
+    two streams: every step as from fresh tensors."""
+    sizes = {"a": 5000, "b": 300, "c": 70000}
+    g = draw(8)
+    p0 = {k: torch.randn(n, generator=g) for k, n in sizes.items()}
+    params = {k: dev(v).clone() for k, v in p0.items()}
+    copies = {"c": params["c"].to(BF16)}
+    opt = ops.AdamW(params, lr=1e-2, bits=bits, copies=copies, decay=["a"], wd=0.1, seed=3)
+    state = [{"p": p0[k], "wd": 0.1 * (k == "a")} for k in sizes]
+    for d, n in zip(state, sizes.values()):
+        q8 = bits == 8 and n >= 4096
+        for s in "mv":
+            d[s] = torch.zeros(n, dtype=torch.uint8 if q8 else F32)
+            if q8:
+                d[s + "_scale"] = torch.zeros(-(-n // 256))
+    stay = {k: torch.randn(n, generator=g) for k, n in sizes.items()}
+    kept = {k: dev(v) for k, v in stay.items()}
+    side = torch.cuda.Stream()
+    for step in range(1, 7):
+        move = step in (1, 5)
+        grads = {k: torch.randn(n, generator=g) for k, n in sizes.items()} if move else stay
+        on = {k: dev(v) for k, v in grads.items()} if move else kept
+        side.wait_stream(torch.cuda.current_stream())
+        opt.step(on, stream=side if step == 4 else None)
+        side.synchronize()
+        assert (opt.items.dev is not None) == (step in (3, 4))
+        now = [{k: v.cpu() if torch.is_tensor(v) else v for k, v in d.items()}
+               for d in opt.items.tensors]
+        check_step([{**d, "g": grads[k]} for d, k in zip(state, sizes)], now, step, 3, lr=1e-2)
+        state = [{k: v for k, v in d.items() if k not in ("g", "copy") and v is not None}
+                 for d in now]
+    assert torch.equal(copies["c"].cpu(), params["c"].cpu().to(BF16))
 
 
 def test_adamw_extreme_gradients():

@@ -189,6 +189,42 @@ def test_adamw_tensors_that_share_memory_are_refused(lib):
     assert adamw(lib, [item(n=0, p=None)], adam_args()) == B.PA_OK
 
 
+def test_adamw_table(lib):
+    """The table holds every block's item; its sizes and refusals (host memory
+    only)."""
+    far = 1 << 26
+    ns = [1000, 0, 4096, 4097, 100000]
+    items = [item(n=n, p=FAKE + (i + 1) * far, m=FAKE + (i + 1) * far + (2 << 20),
+                  v=FAKE + (i + 1) * far + (3 << 20)) for i, n in enumerate(ns)]
+    arr = (ops.pa_adamw_item * len(ns))(*items)
+    size, blocks = ctypes.c_size_t(0), ctypes.c_int64(0)
+    assert lib.pa_adamw_table_size(5, arr, ctypes.byref(size), ctypes.byref(blocks)) == B.PA_OK
+    per = [-(-n // 4096) for n in ns]
+    assert blocks.value == sum(per)
+    host = torch.zeros(size.value // 4 + 2, dtype=torch.int32)
+    assert lib.pa_adamw_table(5, arr, host.data_ptr(), size.value) == B.PA_OK
+    want = [i for i, k in enumerate(per) for _ in range(k)]
+    assert host[size.value // 4 - sum(per):size.value // 4].tolist() == want
+    assert host[size.value // 4:].tolist() == [0, 0]
+    refused(lib, lib.pa_adamw_table(5, arr, host.data_ptr(), size.value - 1), WS, "table")
+    refused(lib, lib.pa_adamw_table(5, arr, None, size.value), WS, "table")
+    refused(lib, lib.pa_adamw_table(5, arr, host.data_ptr() + 4, size.value), INV, "host")
+    refused(lib, lib.pa_adamw_table_size(5, arr, None, ctypes.byref(blocks)), INV, "bytes")
+    arr[4].m = arr[3].p
+    refused(lib, lib.pa_adamw_table_size(5, arr, ctypes.byref(size), ctypes.byref(blocks)), INV,
+            "overlap")
+    huge = [item(n=1 << 36, p=FAKE + (3 * i + 1) * (1 << 39), m=FAKE + (3 * i + 2) * (1 << 39),
+                 v=FAKE + (3 * i + 3) * (1 << 39)) for i in range(130)]
+    arr = (ops.pa_adamw_item * 130)(*huge)
+    refused(lib, lib.pa_adamw_table_size(130, arr, ctypes.byref(size), ctypes.byref(blocks)), UNS,
+            "table")
+    a = adam_args()
+    assert lib.pa_adamw_run(0, 0, None, ctypes.byref(a), None) == B.PA_OK
+    refused(lib, lib.pa_adamw_run(3, -1, None, ctypes.byref(a), None), INV, "blocks")
+    refused(lib, lib.pa_adamw_run(3, 5, None, ctypes.byref(a), None), INV, "table")
+    refused(lib, lib.pa_adamw_run(3, 5, None, ctypes.byref(adam_args(step=0)), None), INV, "step")
+
+
 @fake_addresses
 def test_unpack_refusals(lib):
     refused(lib, lib.pa_adamw_unpack(0, FAKE, FAKE, 1, FAKE, None), INV, "n")
