@@ -17,24 +17,28 @@
 // row's end read its first chunk and count as zeros.
 #include <type_traits>
 
-#include "pa_device.hpp"
 #include "pa_ops_internal.h"
+#include "pa_stream.hpp"
 
 namespace pa {
 namespace {
 
-template <typename T> struct Chunk16 { static constexpr int E = 16 / (int)sizeof(T); };
-
+template <typename T> struct Chunk16 {
+  static constexpr int E = 16 / (int)sizeof(T);
+  uint4 q;
+};
 template <typename T>
-__device__ __forceinline__ void load_chunk(const void* base, int64_t at,
-                                           float (&v)[Chunk16<T>::E]) {
-  const T* p = reinterpret_cast<const T*>(base) + at;
+__device__ __forceinline__ Chunk16<T> fetch(const void* base, int64_t at) {
+  return {ld_global16<true>(reinterpret_cast<const T*>(base) + at)};
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Chunk16<T>& c, float (&v)[Chunk16<T>::E]) {
   if constexpr (sizeof(T) == 2) {
-    const bf16x8 b = *reinterpret_cast<const bf16x8*>(p);
+    const bf16x8 b = __builtin_bit_cast(bf16x8, c.q);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = (float)b[e];
   } else {
-    const f32x4 f = *reinterpret_cast<const f32x4*>(p);
+    const f32x4 f = __builtin_bit_cast(f32x4, c.q);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = f[e];
   }
@@ -42,101 +46,146 @@ __device__ __forceinline__ void load_chunk(const void* base, int64_t at,
 template <typename T>
 __device__ __forceinline__ void store_chunk(void* base, int64_t at,
                                             const float (&v)[Chunk16<T>::E]) {
-  T* p = reinterpret_cast<T*>(base) + at;
+  uint4 q;
   if constexpr (sizeof(T) == 2) {
     bf16x8 b;
 #pragma unroll
     for (int e = 0; e < 8; ++e) b[e] = (bf16)v[e];
-    *reinterpret_cast<bf16x8*>(p) = b;
+    q = __builtin_bit_cast(uint4, b);
   } else {
     f32x4 f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) f[e] = v[e];
-    *reinterpret_cast<f32x4*>(p) = f;
+    q = __builtin_bit_cast(uint4, f);
   }
+  st_global16(reinterpret_cast<T*>(base) + at, q);
 }
 
-// The lanes that share a row: L lanes of a wave (narrow), or the block.
-template <bool WIDE>
+// Sums and maxima over the lanes that share a row: L lanes of a wave (narrow), by
+// lane exchanges without LDS, or the block's waves (wide), which meet in LDS, in
+// two places in turn, so that a sum takes one barrier.
+template <int WIDE>
 struct RowGroup {
   int L;
-  float* red;  // [waves] (wide)
-  __device__ __forceinline__ float sum(float v) const {
-    if constexpr (!WIDE) {
-      for (int o = 1; o < L; o <<= 1) v += __shfl_xor(v, o);
-      return v;
-    } else {
-      for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-      __syncthreads();  // the sums before have been read
-      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  float2* red;  // [2][16] (wide)
+  int turn = 0;
+
+  __device__ __forceinline__ float lanes_sum(float v) const {
+    if (WIDE || L > 1) v += dpp<kQuadSwap1>(v);
+    if (WIDE || L > 2) v += dpp<kQuadSwap2>(v);
+    if (WIDE || L > 4) v += dpp<kHalfMirror>(v);
+    if (WIDE || L > 8) v += dpp<kMirror>(v);
+    if (WIDE || L > 16) {
+      float a = v, b = v;
+      lane_swap16(a, b);
+      v = a + b;
+    }
+    if (WIDE || L > 32) {
+      float a = v, b = v;
+      lane_swap32(a, b);
+      v = a + b;
+    }
+    return v;
+  }
+  // a and b summed, together
+  __device__ __forceinline__ void sum2(float& a, float& b) {
+    a = lanes_sum(a);
+    b = lanes_sum(b);
+    if constexpr (WIDE) {
+      float2* r = red + 16 * turn;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = {a, b};
       __syncthreads();
-      float s = 0.f;
-      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += red[w];
-      return s;
+      a = b = 0.f;
+      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+        a += r[w].x;
+        b += r[w].y;
+      }
     }
   }
-  __device__ __forceinline__ uint32_t max(uint32_t v) const {
-    if constexpr (!WIDE) {
-      for (int o = 1; o < L; o <<= 1) v = ::max(v, (uint32_t)__shfl_xor((int)v, o));
-      return v;
-    } else {
-      for (int o = 1; o < 64; o <<= 1) v = ::max(v, (uint32_t)__shfl_xor((int)v, o));
-      uint32_t* r = reinterpret_cast<uint32_t*>(red);
+  __device__ __forceinline__ uint32_t max(uint32_t v) {
+    for (int o = 1; o < (WIDE ? 64 : L); o <<= 1) v = ::max(v, (uint32_t)__shfl_xor((int)v, o));
+    if constexpr (WIDE) {
+      float2* r = red + 16 * turn;
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6].x = __builtin_bit_cast(float, v);
       __syncthreads();
-      if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = v;
-      __syncthreads();
-      uint32_t s = 0;
-      for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s = ::max(s, r[w]);
-      return s;
+      v = 0;
+      for (int w = 0; w < (int)(blockDim.x >> 6); ++w)
+        v = ::max(v, __builtin_bit_cast(uint32_t, r[w].x));
     }
+    return v;
   }
 };
 
-// v <- the row normalised (lanes off the row: zeros); returns 1 / its size.
-template <int E, bool WIDE>
-__device__ __forceinline__ float normalise(float (&v)[E], bool on, int kind, float eps, float invC,
-                                           const RowGroup<WIDE>& grp) {
-  if (kind == PA_NORM_LAYER) {
-    float s = 0.f;
+template <int E> __device__ __forceinline__ float total(const float (&v)[E]) {
+  float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += v[e];
-    const float mean = grp.sum(on ? s : 0.f) * invC;
+  for (int e = 0; e < E; ++e) s += v[e];
+  return s;
+}
+template <int E>
+__device__ __forceinline__ float dot(const float (&v)[E], const float (&w)[E]) {
+  float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = v[e] - mean;
+  for (int e = 0; e < E; ++e) s = fmaf(v[e], w[e], s);
+  return s;
+}
+
+// Two rows normalised together (their sums share the exchanges): a <- its
+// deviation from the mean (LayerNorm) over its size, on the lanes of the row,
+// zeros on the others; ra = 1 / size.  NONE leaves a row as it is, r = 1.
+template <int E, int WIDE>
+__device__ __forceinline__ void normalise2(float (&a)[E], int ka, float ea, float& ra, float (&b)[E],
+                                           int kb, float eb, float& rb, bool on, float invC,
+                                           RowGroup<WIDE>& grp) {
+  if (ka == PA_NORM_LAYER || kb == PA_NORM_LAYER) {
+    float sa = on ? total(a) : 0.f, sb = on ? total(b) : 0.f;
+    grp.sum2(sa, sb);
+    const float ma = ka == PA_NORM_LAYER ? sa * invC : 0.f, mb = kb == PA_NORM_LAYER ? sb * invC : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      a[e] -= ma;
+      b[e] -= mb;
+    }
   }
-  float q = 0.f;
+  ra = rb = 1.f;
+  if (ka != PA_NORM_NONE || kb != PA_NORM_NONE) {
+    float qa = on ? dot(a, a) : 0.f, qb = on ? dot(b, b) : 0.f;
+    grp.sum2(qa, qb);
+    if (ka != PA_NORM_NONE) ra = 1.0f / sqrtf(fmaf(qa, invC, ea));
+    if (kb != PA_NORM_NONE) rb = 1.0f / sqrtf(fmaf(qb, invC, eb));
+  }
+  const float fa = on ? ra : 0.f, fb = on ? rb : 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) q += v[e] * v[e];
-  const float r = 1.0f / sqrtf(grp.sum(on ? q : 0.f) * invC + eps);
-#pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = on ? v[e] * r : 0.f;
-  return r;
+  for (int e = 0; e < E; ++e) {
+    a[e] *= fa;
+    b[e] *= fb;
+  }
 }
 
 // z's gradient from that of its normalised form: d <- r (d - [mean d] - zhat
-// mean(d zhat)).
-template <int E, bool WIDE>
+// mean(d zhat)).  (zhat and d are finite or the row's are not.)
+template <int E, int WIDE>
 __device__ __forceinline__ void pull_back(float (&d)[E], const float (&zh)[E], float r, bool on,
-                                          int kind, float invC, const RowGroup<WIDE>& grp) {
-  float sd = 0.f, sz = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    sd += d[e];
-    sz += d[e] * zh[e];
-  }
-  const float md = kind == PA_NORM_LAYER ? grp.sum(on ? sd : 0.f) * invC : 0.f;
-  const float mz = grp.sum(on ? sz : 0.f) * invC;
+                                          int kind, float invC, RowGroup<WIDE>& grp) {
+  float sd = on ? total(d) : 0.f, sz = on ? dot(d, zh) : 0.f;
+  grp.sum2(sd, sz);
+  const float md = kind == PA_NORM_LAYER ? sd * invC : 0.f, mz = sz * invC;
 #pragma unroll
   for (int e = 0; e < E; ++e) d[e] = r * (d[e] - md - zh[e] * mz);
 }
 
 // The gate and its slope; exp of -|t| alone, so that nothing overflows.
+// (bf16: the hardware's exp2 and reciprocal, good to a few steps of fp32.)
+template <typename T>
 __device__ __forceinline__ float gate_of(float t, int kind, float& slope) {
   if (kind == PA_GATE_LINEAR) {
     slope = 1.f;
     return t;
   }
-  const float q = expf(-fabsf(t)), s = 1.f / (1.f + q);
+  const float q = sizeof(T) == 2 ? fast_exp2(-kLog2e * fabsf(t)) : expf(-fabsf(t));
+  const float s = sizeof(T) == 2 ? fast_rcp(1.f + q) : 1.f / (1.f + q);
   slope = q * s * s;
   return t >= 0.f ? s : q * s;
 }
@@ -148,13 +197,13 @@ __device__ __forceinline__ void gains(const float* p, int c0, float none, float 
   for (int e = 0; e < E; ++e) v[e] = p ? p[c0 + e] : none;
 }
 
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) k_resnorm(ResNormArgs a) {
-  constexpr int E = Chunk16<T>::E;
-  __shared__ float red[16];
+template <typename T, int WIDE, bool GATE>
+__global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
+  constexpr int E = Chunk16<T>::E, U = WIDE ? 1 : 2;  // rows in turn per group
+  __shared__ float2 red[32];
   const int L = WIDE ? blockDim.x : a.L;
-  const RowGroup<WIDE> grp{L, red};
-  const int rows = WIDE ? 1 : blockDim.x / L;  // rows per block and turn
+  RowGroup<WIDE> grp{L, red};
+  const int rows = WIDE ? 1 : blockDim.x / L;  // groups per block
   const int c = (threadIdx.x % L) * E;
   const bool on = c < a.C;
   const int c0 = on ? c : 0;
@@ -165,60 +214,84 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) k_resnorm(ResNormArgs a) {
   gains(a.scale, c0, 1.f, sc);
   gains(a.pre_g, c0, 1.f, qg);
   gains(a.pre_b, c0, 0.f, qb);
-  const int64_t step = (int64_t)gridDim.x * rows;
-  for (int64_t base = (int64_t)blockIdx.x * rows; base < a.N; base += step) {
-    const int64_t row = base + (WIDE ? 0 : threadIdx.x / L);
-    const bool ok = row < a.N;
-    const int64_t at = (ok ? row : a.N - 1) * a.C + c0;
-    float u[E], v[E];
-    load_chunk<T>(a.y, at, u);
-    load_chunk<T>(a.x, at, v);
+  const int64_t step = (int64_t)gridDim.x * rows * U;
+  for (int64_t base = (int64_t)blockIdx.x * rows * U; base < a.N; base += step) {
+    Chunk16<T> x[U], y[U], t[U];
+    int64_t row[U], at[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      row[k] = base + k * rows + (WIDE ? 0 : threadIdx.x / L);
+      at[k] = (row[k] < a.N ? row[k] : a.N - 1) * a.C + c0;  // (rows past N: the last one)
+      y[k] = fetch<T>(a.y, at[k]);
+      x[k] = fetch<T>(a.x, at[k]);
+      if constexpr (GATE) t[k] = fetch<T>(a.t, at[k]);
+    }
+    float u[U][E], v[U][E], r0, r1;
+#pragma unroll
+    for (int k = 0; k < U; ++k) unpack<T>(y[k], u[k]);
     if (a.post != PA_NORM_NONE) {
-      normalise(u, on, a.post, a.post_eps, invC, grp);
-#pragma unroll
-      for (int e = 0; e < E; ++e) u[e] = u[e] * pg[e] + pb[e];
-    }
-    if (a.t) {
-      float t[E], slope;
-      load_chunk<T>(a.t, at, t);
-#pragma unroll
-      for (int e = 0; e < E; ++e) u[e] *= gate_of(t[e], a.gate, slope);
+      if constexpr (U == 2) {
+        normalise2(u[0], a.post, a.post_eps, r0, u[1], a.post, a.post_eps, r1, on, invC, grp);
+      } else {
+        float none[E] = {};
+        normalise2(u[0], a.post, a.post_eps, r0, none, PA_NORM_NONE, 0.f, r1, on, invC, grp);
+      }
     }
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = to_f<T>(from_f<T>(fmaf(a.alpha, v[e], sc[e] * u[e])));
-    if (ok && on) store_chunk<T>(a.x1, at, v);
+    for (int k = 0; k < U; ++k) {
+      float g[E];
+      unpack<T>(x[k], v[k]);
+      if constexpr (GATE) unpack<T>(t[k], g);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (a.post != PA_NORM_NONE) u[k][e] = fmaf(u[k][e], pg[e], pb[e]);
+        if constexpr (GATE) {
+          float slope;
+          u[k][e] *= gate_of<T>(g[e], a.gate, slope);
+        }
+        v[k][e] = to_f<T>(from_f<T>(fmaf(a.alpha, v[k][e], sc[e] * u[k][e])));
+      }
+      if (row[k] < a.N && on) store_chunk<T>(a.x1, at[k], v[k]);
+    }
     if (a.pre == PA_NORM_NONE) continue;
-    normalise(v, on, a.pre, a.pre_eps, invC, grp);
+    if constexpr (U == 2) {
+      normalise2(v[0], a.pre, a.pre_eps, r0, v[1], a.pre, a.pre_eps, r1, on, invC, grp);
+    } else {
+      float none[E] = {};
+      normalise2(v[0], a.pre, a.pre_eps, r0, none, PA_NORM_NONE, 0.f, r1, on, invC, grp);
+    }
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = v[e] * qg[e] + qb[e];
-    if (a.h && ok && on) store_chunk<T>(a.h, at, v);
-    if (a.hq) {
-      uint32_t big = 0;
+    for (int k = 0; k < U; ++k) {
+      const bool ok = row[k] < a.N;
 #pragma unroll
-      for (int e = 0; e < E; ++e) big = ::max(big, __builtin_bit_cast(uint32_t, fabsf(v[e])));
-      const QuantScale q = quant_scale(grp.max(on ? big : 0u));
-      uint32_t w[E / 4];
+      for (int e = 0; e < E; ++e) v[k][e] = fmaf(v[k][e], qg[e], qb[e]);
+      if (a.h && ok && on) store_chunk<T>(a.h, at[k], v[k]);
+      if (a.hq) {
+        uint32_t big = 0;
 #pragma unroll
-      for (int e = 0; e < E; e += 4)
-        w[e / 4] = on ? quant4(v[e], v[e + 1], v[e + 2], v[e + 3], q.inv) : 0u;
-      const int Kp = (a.C + 15) / 16 * 16;
-      if (ok && c < Kp) {
-        uint32_t* o = reinterpret_cast<uint32_t*>(a.hq + row * Kp + c);
+        for (int e = 0; e < E; ++e)
+          big = ::max(big, __builtin_bit_cast(uint32_t, v[k][e]) & 0x7fffffffu);
+        const QuantScale q = quant_scale(grp.max(on ? big : 0u));
+        const int Kp = (a.C + 15) / 16 * 16;
+        if (ok && c < Kp) {
+          uint32_t* o = reinterpret_cast<uint32_t*>(a.hq + row[k] * Kp + c);
 #pragma unroll
-        for (int e = 0; e < E / 4; ++e) o[e] = w[e];
-        if (c == 0) a.hs[row] = q.s;
+          for (int e = 0; e < E; e += 4)
+            o[e / 4] = on ? quant4(v[k][e], v[k][e + 1], v[k][e + 2], v[k][e + 3], q.inv) : 0u;
+          if (c == 0) a.hs[row[k]] = q.s;
+        }
       }
     }
   }
 }
 
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 1024 : 256) k_resnorm_bwd(ResNormArgs a) {
+template <typename T, int WIDE, bool GATE>
+__global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd(ResNormArgs a) {
   constexpr int E = Chunk16<T>::E;
-  __shared__ float red[16];
-  extern __shared__ float fold[];  // [rows][C] (narrow)
+  __shared__ float2 red[32];
+  extern __shared__ float fold[];  // [rows][5][C] (narrow)
   const int L = WIDE ? blockDim.x : a.L;
-  const RowGroup<WIDE> grp{L, red};
+  RowGroup<WIDE> grp{L, red};
   const int rows = WIDE ? 1 : blockDim.x / L;
   const int c = (threadIdx.x % L) * E;
   const bool on = c < a.C;
@@ -234,99 +307,96 @@ __global__ void __launch_bounds__(WIDE ? 1024 : 256) k_resnorm_bwd(ResNormArgs a
   for (int k = 0; k < 5; ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[k][e] = 0.f;
+  // (a gradient that is not given: y's rows, which are read anyway, as zeros)
+  const void* DX1 = a.dx1 ? a.dx1 : a.y;
+  const void* DH = a.dh ? a.dh : a.y;
+  const int pre = a.dh ? a.pre : PA_NORM_NONE;
   const int64_t step = (int64_t)gridDim.x * rows;
   for (int64_t base = (int64_t)blockIdx.x * rows; base < a.N; base += step) {
     const int64_t row = base + (WIDE ? 0 : threadIdx.x / L);
     const bool ok = row < a.N;
     const int64_t at = (ok ? row : a.N - 1) * a.C + c0;
-    float d[E];
-    if (a.dx1) {
-      load_chunk<T>(a.dx1, at, d);
-    } else {
+    const Chunk16<T> y_ = fetch<T>(a.y, at), x_ = fetch<T>(a.x1, at), dh_ = fetch<T>(DH, at),
+                     dx_ = fetch<T>(DX1, at);
+    Chunk16<T> t_;
+    if constexpr (GATE) t_ = fetch<T>(a.t, at);
+    float yh[E], xh[E], gh[E], d[E], ry, rx;
+    unpack<T>(y_, yh);
+    unpack<T>(x_, xh);
+    normalise2(yh, a.post, a.post_eps, ry, xh, pre, a.pre_eps, rx, on, invC, grp);
+    unpack<T>(dx_, d);
+    if (!a.dx1) {
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] = 0.f;
     }
     if (a.dh) {
-      float xh[E], gh[E];
-      load_chunk<T>(a.x1, at, xh);
-      load_chunk<T>(a.dh, at, gh);
-      const float rx = normalise(xh, on, a.pre, a.pre_eps, invC, grp);
+      unpack<T>(dh_, gh);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (ok) {
-          acc[3][e] += gh[e] * xh[e];
+          acc[3][e] = fmaf(gh[e], xh[e], acc[3][e]);
           acc[4][e] += gh[e];
         }
         gh[e] *= qg[e];
       }
-      pull_back(gh, xh, rx, on, a.pre, invC, grp);
+      pull_back(gh, xh, rx, on, pre, invC, grp);
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] += gh[e];
     }
-    // d: e of the header.  u: post(y); yh its normalised row
-    float yh[E], u[E], o[E];
-    load_chunk<T>(a.y, at, yh);
-    float ry = 1.f;
-    if (a.post != PA_NORM_NONE) ry = normalise(yh, on, a.post, a.post_eps, invC, grp);
+    // d: e of the header; u: post(y)
+    float u[E], o[E], m[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      u[e] = a.post != PA_NORM_NONE ? yh[e] * pg[e] + pb[e] : yh[e];
+      u[e] = a.post != PA_NORM_NONE ? fmaf(yh[e], pg[e], pb[e]) : yh[e];
       o[e] = a.alpha * d[e];
+      m[e] = 1.f;
     }
     if (ok && on) store_chunk<T>(a.dx, at, o);
-    float m[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) m[e] = 1.f;
-    if (a.t) {
+    if constexpr (GATE) {
       float t[E];
-      load_chunk<T>(a.t, at, t);
+      unpack<T>(t_, t);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         float slope;
-        m[e] = gate_of(t[e], a.gate, slope);
+        m[e] = gate_of<T>(t[e], a.gate, slope);
         t[e] = sc[e] * d[e] * u[e] * slope;
       }
       if (ok && on) store_chunk<T>(a.dt, at, t);
     }
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      const float du = d[e] * sc[e] * m[e];
+      const float em = d[e] * m[e], du = em * sc[e];
       if (ok) {
-        acc[2][e] += d[e] * m[e] * u[e];
-        acc[0][e] += du * yh[e];
+        acc[2][e] = fmaf(em, u[e], acc[2][e]);
+        acc[0][e] = fmaf(du, yh[e], acc[0][e]);
         acc[1][e] += du;
       }
-      u[e] = du * pg[e];
+      u[e] = a.post != PA_NORM_NONE ? du * pg[e] : du;
     }
-    if (a.post != PA_NORM_NONE) {
-      pull_back(u, yh, ry, on, a.post, invC, grp);
-      if (ok && on) store_chunk<T>(a.dy, at, u);
-    } else if (ok && on) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] = d[e] * sc[e] * m[e];
-      store_chunk<T>(a.dy, at, o);
-    }
+    if (a.post != PA_NORM_NONE) pull_back(u, yh, ry, on, a.post, invC, grp);
+    if (ok && on) store_chunk<T>(a.dy, at, u);
   }
   if (!a.partials) return;
   // the block's record [5][C]: its rows added in order
   float* rec = a.partials + (int64_t)blockIdx.x * 5 * a.C;
+  if constexpr (WIDE) {
+    if (on)
 #pragma unroll
-  for (int k = 0; k < 5; ++k) {
-    if constexpr (WIDE) {
-      if (on)
+      for (int k = 0; k < 5; ++k)
 #pragma unroll
         for (int e = 0; e < E; ++e) rec[k * a.C + c + e] = acc[k][e];
-    } else {
-      __syncthreads();
-      if (on)
+  } else {
+    const int C5 = 5 * a.C;
+    if (on)
 #pragma unroll
-        for (int e = 0; e < E; ++e) fold[(threadIdx.x / L) * a.C + c + e] = acc[k][e];
-      __syncthreads();
-      for (int i = threadIdx.x; i < a.C; i += blockDim.x) {
-        float s = 0.f;
-        for (int r = 0; r < rows; ++r) s += fold[r * a.C + i];
-        rec[k * a.C + i] = s;
-      }
+      for (int k = 0; k < 5; ++k)
+#pragma unroll
+        for (int e = 0; e < E; ++e) fold[(threadIdx.x / L) * C5 + k * a.C + c + e] = acc[k][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < C5; i += blockDim.x) {
+      float s = 0.f;
+      for (int r = 0; r < rows; ++r) s += fold[r * C5 + i];
+      rec[i] = s;
     }
   }
 }
@@ -351,8 +421,11 @@ ResNormGeo geo(int C, int dtype) {
 
 int resnorm_blocks(int64_t N, int C, int dtype, bool bwd) {
   const ResNormGeo g = geo(C, dtype);
-  const int64_t need = (N + g.rows - 1) / g.rows;
-  const int64_t cap = g.wide ? 512 : bwd ? 1024 : 2048;
+  const int turn = g.rows * (bwd || g.wide ? 1 : 2);
+  const int64_t need = (N + turn - 1) / turn;
+  // (backward: three blocks per CU, what its registers allow, in one round; 1024
+  // blocks took 934 us where these take 793, at N = 1,000,000, C = 256)
+  const int64_t cap = g.wide ? 512 : bwd ? 768 : 2048;
   return (int)(need < cap ? need : cap);
 }
 
@@ -363,15 +436,21 @@ hipError_t launch_resnorm(const ResNormArgs& a0, int dtype, bool bwd, hipStream_
   const ResNormGeo g = geo(a.C, dtype);
   a.L = g.L;
   const dim3 grid(resnorm_blocks(a.N, a.C, dtype, bwd)), block(g.threads);
-  const size_t lds = bwd && !g.wide ? (size_t)g.rows * a.C * sizeof(float) : 0;
+  const size_t lds = bwd && !g.wide ? (size_t)g.rows * 5 * a.C * sizeof(float) : 0;
   auto go = [&](auto* k) { hipLaunchKernelGGL(k, grid, block, lds, st, a); };
-  if (dtype == 1) {
-    if (g.wide) bwd ? go(k_resnorm_bwd<bf16, true>) : go(k_resnorm<bf16, true>);
-    else bwd ? go(k_resnorm_bwd<bf16, false>) : go(k_resnorm<bf16, false>);
-  } else {
-    if (g.wide) bwd ? go(k_resnorm_bwd<float, true>) : go(k_resnorm<float, true>);
-    else bwd ? go(k_resnorm_bwd<float, false>) : go(k_resnorm<float, false>);
-  }
+  auto pick = [&](auto type, auto wide) {
+    using T = decltype(type);
+    constexpr int W = decltype(wide)::value;
+    if (a.t) bwd ? go(k_resnorm_bwd<T, W, true>) : go(k_resnorm<T, W, true>);
+    else bwd ? go(k_resnorm_bwd<T, W, false>) : go(k_resnorm<T, W, false>);
+  };
+  auto width = [&](auto type) {
+    if (!g.wide) pick(type, std::integral_constant<int, 0>{});
+    else if (g.threads <= 512) pick(type, std::integral_constant<int, 512>{});
+    else pick(type, std::integral_constant<int, 1024>{});
+  };
+  if (dtype == 1) width(bf16{});
+  else width(float{});
   return hipGetLastError();
 }
 

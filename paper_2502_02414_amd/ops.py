@@ -101,14 +101,6 @@ def _code(dtype, name):
     return code
 
 
-def _dev(t, name):
-    """Pointer of a contiguous tensor on the current device."""
-    p = B._ptr(t)
-    if t.is_cuda and t.get_device() != _current_device():
-        raise ValueError(f"{name}: on {t.device}, not on the current device")
-    return p
-
-
 _device = None
 
 
@@ -121,7 +113,18 @@ def _current_device() -> int:
     return _device()
 
 
-def _in(t, n, dtype, name, required=True):
+# The checks below run for every tensor of every call: one that holds takes a few
+# comparisons, and only one that fails goes on to find out what to say.
+def _dev(t, name, cur=None):
+    """Pointer of a contiguous tensor on the current device (its index, where a
+    call has asked before)."""
+    if t.get_device() != (_current_device() if cur is None else cur) or not t.is_contiguous():
+        B._ptr(t)
+        raise ValueError(f"{name}: on {t.device}, not on the current device")
+    return t.data_ptr()
+
+
+def _in(t, n, dtype, name, required=True, cur=None):
     """Pointer of t after checking it against n elements of a torch dtype."""
     if t is None:
         if required:
@@ -131,12 +134,18 @@ def _in(t, n, dtype, name, required=True):
         raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
     if t.numel() != n:
         raise ValueError(f"{name}: {t.numel()} elements, the call needs {n}")
-    return _dev(t, name)
+    return _dev(t, name, cur)
+
+
+_torch_module = None
 
 
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def pa_ops_version() -> int:
@@ -219,9 +228,11 @@ def pa_residual_norm(x, y, par, x1, h=None, t=None, hq=None, hs=None, stream=Non
         hsp = _in(hs, N, torch.float32, "hs")
     else:
         hqp, hsp = None, (None if hs is None else _dev(hs, "hs"))
+    cur = _current_device()
     _check(load().pa_residual_norm(
-        N, C, code, par.ref, _dev(x, "x"), _in(y, n, dt, "y"), _in(t, n, dt, "t", False),
-        _in(x1, n, dt, "x1"), _in(h, n, dt, "h", False), hqp, hsp, B._stream(stream)))
+        N, C, code, par.ref, _dev(x, "x", cur), _in(y, n, dt, "y", True, cur),
+        _in(t, n, dt, "t", False, cur), _in(x1, n, dt, "x1", True, cur),
+        _in(h, n, dt, "h", False, cur), hqp, hsp, B._stream(stream)))
 
 
 def residual_norm_workspace(N, C, dtype, device="cuda"):
@@ -237,11 +248,14 @@ def pa_residual_norm_backward(x1, y, par, dx1, dh, dx, dy, gr=None, ws=None, t=N
     parameters' gradients gr (make_residual_norm_grads)."""
     N, C, n, code = _joint(x1, "x1", par, gr)
     ty = x1.dtype
+    cur = _current_device()
     _check(load().pa_residual_norm_backward(
-        N, C, code, par.ref, _dev(x1, "x1"), _in(y, n, ty, "y"), _in(t, n, ty, "t", False),
-        _in(dx1, n, ty, "dx1", False), _in(dh, n, ty, "dh", False), _in(dx, n, ty, "dx"),
-        _in(dy, n, ty, "dy"), _in(dt, n, ty, "dt", False), gr.ref if gr is not None else None,
-        None if ws is None else _dev(ws, "ws"), B._nbytes(ws), B._stream(stream)))
+        N, C, code, par.ref, _dev(x1, "x1", cur), _in(y, n, ty, "y", True, cur),
+        _in(t, n, ty, "t", False, cur), _in(dx1, n, ty, "dx1", False, cur),
+        _in(dh, n, ty, "dh", False, cur), _in(dx, n, ty, "dx", True, cur),
+        _in(dy, n, ty, "dy", True, cur), _in(dt, n, ty, "dt", False, cur),
+        gr.ref if gr is not None else None, None if ws is None else _dev(ws, "ws", cur),
+        B._nbytes(ws), B._stream(stream)))
 
 
 # ---- AdamW ----
@@ -443,10 +457,11 @@ def _product(K, wq, sw, D, bias, act, C):
     if act not in ACTS:
         raise ValueError(f"act: {act!r} is not one of {sorted(map(str, ACTS))}")
     N, F = D.shape
-    f32 = torch.float32
-    return (N, F, (_in(wq, F * padded(K), torch.int8, "Wq"), _in(sw, F, f32, "sw"),
-                   _in(bias, F, f32, "bias", False), ACTS[act],
-                   _in(C, N * F, D.dtype, "C", False), _dev(D, "D"), _code(D.dtype, "D")))
+    f32, cur = torch.float32, _current_device()
+    return (N, F, cur, (_in(wq, F * padded(K), torch.int8, "Wq", True, cur),
+                        _in(sw, F, f32, "sw", True, cur), _in(bias, F, f32, "bias", False, cur),
+                        ACTS[act], _in(C, N * F, D.dtype, "C", False, cur), _dev(D, "D", cur),
+                        _code(D.dtype, "D")))
 
 
 def pa_gemm_i8(q, s, wq, sw, D, K=None, bias=None, act=None, C=None, stream=None):
@@ -454,9 +469,9 @@ def pa_gemm_i8(q, s, wq, sw, D, K=None, bias=None, act=None, C=None, stream=None
     q's width when not given) and weights wq [F, padded(K)]."""
     torch = _torch()
     K = q.shape[1] if K is None else K
-    N, F, rest = _product(K, wq, sw, D, bias, act, C)
-    _check(load().pa_gemm_i8(N, F, K, _in(q, N * padded(K), torch.int8, "q"),
-                             _in(s, N, torch.float32, "s"), *rest, B._stream(stream)))
+    N, F, cur, rest = _product(K, wq, sw, D, bias, act, C)
+    _check(load().pa_gemm_i8(N, F, K, _in(q, N * padded(K), torch.int8, "q", True, cur),
+                             _in(s, N, torch.float32, "s", True, cur), *rest, B._stream(stream)))
 
 
 def linear_i8_workspace(N, K, F, device="cuda"):
@@ -470,8 +485,8 @@ def pa_linear_i8(x, wq, sw, D, ws, bias=None, act=None, C=None, stream=None):
     """D [N, F] = act(x W + bias) + C with x [N, K] quantised row by row and W
     as pa_quant_weight left it."""
     N, K = x.shape
-    Nd, F, rest = _product(K, wq, sw, D, bias, act, C)
+    Nd, F, cur, rest = _product(K, wq, sw, D, bias, act, C)
     if Nd != N:
         raise ValueError(f"D has {Nd} rows, x {N}")
-    _check(load().pa_linear_i8(N, F, K, _dev(x, "x"), _code(x.dtype, "x"), *rest, _dev(ws, "ws"),
-                               B._nbytes(ws), B._stream(stream)))
+    _check(load().pa_linear_i8(N, F, K, _dev(x, "x", cur), _code(x.dtype, "x"), *rest,
+                               _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))

@@ -281,7 +281,8 @@ class _Recorder:
 def fake(monkeypatch):
     rec = _Recorder()
     monkeypatch.setattr(ops, "load", lambda: rec)
-    monkeypatch.setattr(B, "_ptr", lambda t: None if t is None else 4096)
+    monkeypatch.setattr(ops, "_dev", lambda t, name, cur=None: 4096)
+    monkeypatch.setattr(ops, "_current_device", lambda: 0)
     monkeypatch.setattr(B, "_stream", lambda s=None: None)
     return rec
 
@@ -371,6 +372,7 @@ def test_binding_refuses_before_the_call(fake):
 
 
 def test_tensors_on_the_cpu_or_not_contiguous_are_refused():
-    par = ops.make_residual_norm_params()
     with pytest.raises(ValueError, match="GPU"):
-        ops.pa_residual_norm(z(4, 32), z(4, 32), par, z(4, 32))
+        ops._dev(z(4, 32), "x", 0)
+    with pytest.raises(ValueError, match="GPU"):
+        ops._in(z(4, 32), 128, torch.float32, "x", True, 0)
