@@ -4,7 +4,6 @@
 //
 // The weights are the MFMA's A operand and the points its B operand, so that a
 // lane of a 16 x 16 result tile holds four consecutive channels of one point.
-#include <cstdlib>
 #include <type_traits>
 
 #include "pa_i8.hpp"
@@ -12,17 +11,17 @@
 namespace pa {
 namespace {
 
-// Every access of a wave's LDS writes (also those that come from memory) is
-// done, for all waves of the block.
-__device__ __forceinline__ void tile_ready() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+// All but the wave's last LATER loads are done, and all its LDS reads, for all
+// waves of the block.
+template <int LATER> __device__ __forceinline__ void tile_ready() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"i"(LATER) : "memory");
 }
 
 // ---------------------------------------------------------------------------
 // Tiled product.  A block of WF x WN waves forms a tile of TF channels x TN
 // points, each wave MF x MN MFMA tiles of 16 x 16, over steps of 128 bytes of
-// K.  A step's rows come from memory straight into LDS (16 bytes per lane), one
-// step ahead, in two buffers.  A buffer load past the last row or past a row's
+// K.  A step's rows come from memory straight into LDS (16 bytes per lane), NB - 1
+// steps ahead, in NB buffers.  A buffer load past the last row or past a row's
 // end (K is no multiple of 128) leaves zeros.
 //
 // LDS rows are 128 bytes, without padding (a wave's load fills 1 KB in order);
@@ -33,13 +32,13 @@ __device__ __forceinline__ void tile_ready() {
 // row: bf16: tile pairs (2 j, 2 j + 1) hold channels 32 j + 8 g + 4 (i & 1) ..
 // of lane group g; fp32: tile i holds channels 16 i + 4 g ..
 // ---------------------------------------------------------------------------
-template <int WF, int WN, int MF, int MN>
+template <int WF, int WN, int MF, int MN, int NB>
 struct I8Geo {
   static constexpr int W = WF * WN, TF = 16 * MF * WF, TN = 16 * MN * WN, BK = 128;
   static constexpr int LF = TF / 8 / W, LN = TN / 8 / W;  // 1 KB loads per wave and step
   static constexpr int BUF = (TF + TN) * BK;
   static_assert(LF * W * 8 == TF && LN * W * 8 == TN, "whole loads");
-  static_assert(2 * BUF <= 160 * 1024, "two buffers fit");
+  static_assert(NB * BUF <= 160 * 1024, "the buffers fit");
 };
 
 template <typename T>
@@ -49,12 +48,14 @@ __device__ __forceinline__ int key_f(int row) {  // of a row of weights
 }
 __device__ __forceinline__ int key_n(int row) { return row & 7; }
 
-template <typename T, int ACT, int WF, int WN, int MF, int MN>
-__global__ void __launch_bounds__(64 * WF * WN, WF * WN == 8 ? 2 : 2) k_gemm_i8(I8Args a) {
-  using G = I8Geo<WF, WN, MF, MN>;
+template <typename T, int ACT, int WF, int WN, int MF, int MN, int NB>
+__global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
+  using G = I8Geo<WF, WN, MF, MN, NB>;
   constexpr int BK = G::BK;
   __shared__ __attribute__((aligned(16))) char buf0[G::BUF];
   __shared__ __attribute__((aligned(16))) char buf1[G::BUF];
+  __shared__ __attribute__((aligned(16))) char buf2[NB > 2 ? G::BUF : 16];
+  __shared__ __attribute__((aligned(16))) char buf3[NB > 3 ? G::BUF : 16];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const int wf = wave % WF, wn = wave / WF;
@@ -120,22 +121,46 @@ __global__ void __launch_bounds__(64 * WF * WN, WF * WN == 8 ? 2 : 2) k_gemm_i8(
     }
   };
 
-  // step k is computed while step k + 1 comes into the other buffer, which
-  // every wave has read before the barrier
+  // step k is computed while the NB - 1 next ones come into the other buffers, the
+  // last of which every wave has read before the barrier.  (Separate arrays, not
+  // one: the compiler waits for the loads into the array that it reads.  Loads
+  // behind the last step put zeros where nothing is read.)
+  constexpr int PER = G::LF + G::LN;
   const int steps = (a.Kp + BK - 1) / BK;
-  load(buf0, 0);
-  int s = 0;
-  for (; s + 1 < steps; s += 2) {
-    tile_ready();
-    load(buf1, (s + 1) * BK);
-    compute(buf0);
-    tile_ready();
-    if (s + 2 < steps) load(buf0, (s + 2) * BK);
-    compute(buf1);
-  }
-  if (s < steps) {
-    tile_ready();
-    compute(buf0);
+  if constexpr (NB == 2) {
+    load(buf0, 0);
+    int s = 0;
+    for (; s + 1 < steps; s += 2) {
+      tile_ready<0>();
+      load(buf1, (s + 1) * BK);
+      compute(buf0);
+      tile_ready<0>();
+      if (s + 2 < steps) load(buf0, (s + 2) * BK);
+      compute(buf1);
+    }
+    if (s < steps) {
+      tile_ready<0>();
+      compute(buf0);
+    }
+  } else {
+    static_assert(NB == 4, "two or four buffers");
+    load(buf0, 0);
+    load(buf1, BK);
+    load(buf2, 2 * BK);
+    auto step = [&](int s, char* next, const char* now) __attribute__((always_inline)) {
+      if (s < steps) {
+        tile_ready<2 * PER>();
+        load(next, (s + 3) * BK);
+        compute(now);
+      }
+    };
+    for (int s = 0; s < steps; s += 4) {
+      step(s, buf3, buf0);
+      step(s + 1, buf0, buf1);
+      step(s + 2, buf1, buf2);
+      step(s + 3, buf2, buf3);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing comes into LDS once it is given back
   }
 
   // the results: runs of V channels of one point
@@ -281,26 +306,34 @@ __global__ void __launch_bounds__(256) k_quant_weight(int K, int Kp, int F, cons
 }  // namespace
 
 namespace {
-template <typename T, int WF, int WN, int MF, int MN>
+template <typename T, int WF, int WN, int MF, int MN, int NB>
 hipError_t run_tiled(const I8Args& a, hipStream_t st) {
-  using G = I8Geo<WF, WN, MF, MN>;
+  using G = I8Geo<WF, WN, MF, MN, NB>;
   const int64_t tiles = (a.N + G::TN - 1) / G::TN * ((a.F + G::TF - 1) / G::TF);
   if (tiles > 0x7fffffff) return hipErrorInvalidValue;
   const dim3 grid((unsigned)tiles), block(64 * G::W);
   if (a.act == PA_ACT_GELU)
-    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_GELU, WF, WN, MF, MN>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_GELU, WF, WN, MF, MN, NB>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_NONE, WF, WN, MF, MN>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_NONE, WF, WN, MF, MN, NB>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t run_gemm(const I8Args& a, hipStream_t st) {
-  const auto tiles = [&](int t) { return (a.N + t - 1) / t * ((a.F + t - 1) / t); };
-  const char* v = getenv("I8V");
-  const int want = v ? atoi(v) : tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
-  if (want == 256) return run_tiled<T, 2, 4, 8, 4>(a, st);
-  if (want == 128) return run_tiled<T, 2, 2, 4, 4>(a, st);
-  return run_tiled<T, 2, 2, 2, 2>(a, st);
+  // The tile that takes the least time: rounds of the blocks that fit the chip at
+  // once (one of 256 x 256 per CU, two of the others) times a round's time, which at
+  // 4096 x 4096 x 4096 was 64, 38 and 14 us.  (256 against 128: 4096^3 64 and 76
+  // us, 5000 x 4096 x 4096 111 and 101; 128 against 64: 16384 x 512 x 1536 30 and
+  // 42, 2048 x 1024 x 1024 9.3 and 6.6.)
+  const auto cost = [&](int t, int at_once, double round) {
+    const int64_t n = (a.N + t - 1) / t * ((a.F + t - 1) / t);
+    return (double)((n + at_once - 1) / at_once) * round;
+  };
+  const double c256 = cost(256, 256, 64), c128 = cost(128, 512, 38), c64 = cost(64, 512, 14);
+  const int want = c256 <= c128 && c256 <= c64 ? 256 : c128 <= c64 ? 128 : 64;
+  if (want == 256) return run_tiled<T, 2, 4, 8, 4, 2>(a, st);
+  if (want == 128) return run_tiled<T, 2, 2, 4, 4, 2>(a, st);
+  return run_tiled<T, 2, 2, 2, 2, 4>(a, st);
 }
 }  // namespace
 

@@ -218,10 +218,15 @@ hipError_t run(const I8Args& a, hipStream_t st) {
 
 }  // namespace
 
+// Every block first fetches its weights: above 128 KiB of them that takes about as
+// long as all of the two launches on few rows.  (Two launches against this, us:
+// 256 to 1024 with GELU 14.3 and 16.2 at 4,096 rows, 18.4 and 17.5 at 8,192, 118
+// and 79 at 100,000; 1024 to 256 10.8 and 12.9 at 2,048, 19.1 and 14.0 at 8,192; 256
+// to 256 7.9 and 5.4 at 512, 41 and 22 at 100,000; 128 to 1024 7.5 and 5.9 at 512.)
 bool linear_i8_fused(int64_t N, int F, int K, int x_dtype, int d_dtype) {
   if (x_dtype != 1 || d_dtype != 1 || K % 8 || F % 8 || K > 1024) return false;
-  const int most = K <= 64 ? 1024 : K <= 128 ? 1024 : K <= 256 ? 2048 : K <= 512 ? 1024 : 512;
-  return F <= most && N >= 16384;
+  const int most = K <= 128 ? 1024 : K <= 256 ? 2048 : K <= 512 ? 1024 : 512;
+  return F <= most && (K * F <= 131072 || N >= 6144);
 }
 
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st) {
