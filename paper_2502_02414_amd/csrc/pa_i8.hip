@@ -165,60 +165,52 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
 
   // the results: runs of V channels of one point
   constexpr int V = sizeof(T) == 2 ? 8 : 4, RUN = V / 4;
+  typedef T TV __attribute__((ext_vector_type(V)));
   T* D = reinterpret_cast<T*>(a.D);
   const T* Cr = reinterpret_cast<const T*>(a.C);
+  const int64_t nr = n0 + row_n;
   float sn[MN];
 #pragma unroll
-  for (int j = 0; j < MN; ++j) {
-    const int64_t n = n0 + row_n + 16 * j;
-    sn[j] = a.s[n < a.N ? n : a.N - 1];
-  }
-  // whole: F is a multiple of V, so that every run is aligned and lies inside or
-  // outside of a row
-  auto finish = [&](auto whole) {
+  for (int j = 0; j < MN; ++j) sn[j] = a.s[nr + 16 * j < a.N ? nr + 16 * j : a.N - 1];
 #pragma unroll
-    for (int i = 0; i < MF; i += RUN) {
-      const int f = f0 + wf * 16 * MF + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
-      float sw[V], b[V];
+  for (int i = 0; i < MF; i += RUN) {
+    const int f = f0 + wf * 16 * MF + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
+    float sw[V], b[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int fe = f + e < a.F ? f + e : a.F - 1;
+      sw[e] = a.sw[fe];
+      b[e] = a.bias ? a.bias[fe] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < MN; ++j) {
+      const int64_t n = nr + 16 * j, at = n * a.F + f;
+      float u[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const int fe = f + e < a.F ? f + e : a.F - 1;
-        sw[e] = a.sw[fe];
-        b[e] = a.bias ? a.bias[fe] : 0.f;
+        u[e] = fmaf((float)acc[i + e / 4][j][e % 4], sn[j] * sw[e], b[e]);
+        if constexpr (ACT == PA_ACT_GELU) u[e] = gelu_for<T>(u[e]);
       }
+      if (n < a.N && f + V <= a.F) {
+        // (a row's start, and so a run, need not be aligned: F is any number)
+        if (Cr) {
+          TV c;
+          __builtin_memcpy(&c, Cr + at, 16);
 #pragma unroll
-      for (int j = 0; j < MN; ++j) {
-        const int64_t n = n0 + row_n + 16 * j, at = n * a.F + f;
-        float u[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          u[e] = fmaf((float)acc[i + e / 4][j][e % 4], sn[j] * sw[e], b[e]);
-          if constexpr (ACT == PA_ACT_GELU) u[e] = gelu_for<T>(u[e]);
+          for (int e = 0; e < V; ++e) u[e] += (float)c[e];
         }
-        if (n < a.N && f < a.F) {
-          if constexpr (decltype(whole)::value) {
-            typedef T TV __attribute__((ext_vector_type(V)));
-            if (Cr) {
-              const TV c = *reinterpret_cast<const TV*>(Cr + at);
+        TV o;
 #pragma unroll
-              for (int e = 0; e < V; ++e) u[e] += (float)c[e];
-            }
-            TV o;
+        for (int e = 0; e < V; ++e) o[e] = (T)u[e];
+        __builtin_memcpy(D + at, &o, 16);
+      } else if (n < a.N) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = (T)u[e];
-            *reinterpret_cast<TV*>(D + at) = o;
-          } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-              if (f + e < a.F) D[at + e] = from_f<T>(Cr ? u[e] + to_f<T>(Cr[at + e]) : u[e]);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
+        for (int e = 0; e < V; ++e)
+          if (f + e < a.F) D[at + e] = from_f<T>(Cr ? u[e] + to_f<T>(Cr[at + e]) : u[e]);
       }
+      __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
     }
-  };
-  if (a.F % V == 0) finish(std::true_type{});
-  else finish(std::false_type{});
+  }
 }
 
 // ---------------------------------------------------------------------------

@@ -15,6 +15,7 @@
 // them, several rows per wave, the sums over a row by lane exchanges; wider rows
 // take a block of one wave per 64 chunks and sums through LDS.  Lanes behind a
 // row's end read its first chunk and count as zeros.
+#include <algorithm>
 #include <type_traits>
 
 #include "pa_ops_internal.h"
@@ -95,7 +96,7 @@ struct RowGroup {
       float2* r = red + 16 * turn;
       turn ^= 1;
       if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = {a, b};
-      __syncthreads();
+      block_sync();
       a = b = 0.f;
       for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
         a += r[w].x;
@@ -109,7 +110,7 @@ struct RowGroup {
       float2* r = red + 16 * turn;
       turn ^= 1;
       if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6].x = __builtin_bit_cast(float, v);
-      __syncthreads();
+      block_sync();
       v = 0;
       for (int w = 0; w < (int)(blockDim.x >> 6); ++w)
         v = ::max(v, __builtin_bit_cast(uint32_t, r[w].x));
@@ -197,7 +198,7 @@ __device__ __forceinline__ void gains(const float* p, int c0, float none, float 
   for (int e = 0; e < E; ++e) v[e] = p ? p[c0 + e] : none;
 }
 
-template <typename T, int WIDE, bool GATE>
+template <typename T, int WIDE, bool AHEAD, bool GATE>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
   constexpr int E = Chunk16<T>::E, U = WIDE ? 1 : 2;  // rows in turn per group
   __shared__ float2 red[32];
@@ -214,21 +215,31 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
   gains(a.scale, c0, 1.f, sc);
   gains(a.pre_g, c0, 1.f, qg);
   gains(a.pre_b, c0, 0.f, qb);
-  const int64_t step = (int64_t)gridDim.x * rows * U;
-  for (int64_t base = (int64_t)blockIdx.x * rows * U; base < a.N; base += step) {
+  struct Rows {
     Chunk16<T> x[U], y[U], t[U];
+  };
+  const int64_t step = (int64_t)gridDim.x * rows * U;
+  // (rows past N: the last one)
+  auto place = [&](int64_t row) { return (row < a.N ? row : a.N - 1) * a.C + c0; };
+  auto load = [&](int64_t base, Rows& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const int64_t at = place(base + k * rows + (WIDE ? 0 : threadIdx.x / L));
+      w.y[k] = fetch<T>(a.y, at);
+      w.x[k] = fetch<T>(a.x, at);
+      if constexpr (GATE) w.t[k] = fetch<T>(a.t, at);
+    }
+  };
+  auto work = [&](int64_t base, const Rows& w) __attribute__((always_inline)) {
     int64_t row[U], at[U];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       row[k] = base + k * rows + (WIDE ? 0 : threadIdx.x / L);
-      at[k] = (row[k] < a.N ? row[k] : a.N - 1) * a.C + c0;  // (rows past N: the last one)
-      y[k] = fetch<T>(a.y, at[k]);
-      x[k] = fetch<T>(a.x, at[k]);
-      if constexpr (GATE) t[k] = fetch<T>(a.t, at[k]);
+      at[k] = place(row[k]);
     }
     float u[U][E], v[U][E], r0, r1;
 #pragma unroll
-    for (int k = 0; k < U; ++k) unpack<T>(y[k], u[k]);
+    for (int k = 0; k < U; ++k) unpack<T>(w.y[k], u[k]);
     if (a.post != PA_NORM_NONE) {
       if constexpr (U == 2) {
         normalise2(u[0], a.post, a.post_eps, r0, u[1], a.post, a.post_eps, r1, on, invC, grp);
@@ -240,8 +251,8 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       float g[E];
-      unpack<T>(x[k], v[k]);
-      if constexpr (GATE) unpack<T>(t[k], g);
+      unpack<T>(w.x[k], v[k]);
+      if constexpr (GATE) unpack<T>(w.t[k], g);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (a.post != PA_NORM_NONE) u[k][e] = fmaf(u[k][e], pg[e], pb[e]);
@@ -253,7 +264,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
       }
       if (row[k] < a.N && on) store_chunk<T>(a.x1, at[k], v[k]);
     }
-    if (a.pre == PA_NORM_NONE) continue;
+    if (a.pre == PA_NORM_NONE) return;
     if constexpr (U == 2) {
       normalise2(v[0], a.pre, a.pre_eps, r0, v[1], a.pre, a.pre_eps, r1, on, invC, grp);
     } else {
@@ -282,10 +293,29 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256) k_resnorm(ResNormArgs a) {
         }
       }
     }
+  };
+  int64_t base = (int64_t)blockIdx.x * rows * U;  // < N
+  if constexpr (AHEAD) {  // the next rows on their way while these are worked on
+    Rows r0, r1;
+    load(base, r0);
+    for (;;) {
+      load(base + step, r1);
+      work(base, r0);
+      if ((base += step) >= a.N) break;
+      load(base + step, r0);
+      work(base, r1);
+      if ((base += step) >= a.N) break;
+    }
+  } else {
+    for (; base < a.N; base += step) {
+      Rows r;
+      load(base, r);
+      work(base, r);
+    }
   }
 }
 
-template <typename T, int WIDE, bool GATE>
+template <typename T, int WIDE, bool AHEAD, bool GATE>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd(ResNormArgs a) {
   constexpr int E = Chunk16<T>::E;
   __shared__ float2 red[32];
@@ -311,26 +341,34 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
   const void* DX1 = a.dx1 ? a.dx1 : a.y;
   const void* DH = a.dh ? a.dh : a.y;
   const int pre = a.dh ? a.pre : PA_NORM_NONE;
+  struct Rows {
+    Chunk16<T> y, x, dh, dx, t;
+  };
   const int64_t step = (int64_t)gridDim.x * rows;
-  for (int64_t base = (int64_t)blockIdx.x * rows; base < a.N; base += step) {
+  auto place = [&](int64_t row) { return (row < a.N ? row : a.N - 1) * a.C + c0; };
+  auto load = [&](int64_t base, Rows& r) __attribute__((always_inline)) {
+    const int64_t at = place(base + (WIDE ? 0 : threadIdx.x / L));
+    r.y = fetch<T>(a.y, at);
+    r.x = fetch<T>(a.x1, at);
+    r.dh = fetch<T>(DH, at);
+    r.dx = fetch<T>(DX1, at);
+    if constexpr (GATE) r.t = fetch<T>(a.t, at);
+  };
+  auto work = [&](int64_t base, const Rows& r) __attribute__((always_inline)) {
     const int64_t row = base + (WIDE ? 0 : threadIdx.x / L);
     const bool ok = row < a.N;
-    const int64_t at = (ok ? row : a.N - 1) * a.C + c0;
-    const Chunk16<T> y_ = fetch<T>(a.y, at), x_ = fetch<T>(a.x1, at), dh_ = fetch<T>(DH, at),
-                     dx_ = fetch<T>(DX1, at);
-    Chunk16<T> t_;
-    if constexpr (GATE) t_ = fetch<T>(a.t, at);
+    const int64_t at = place(row);
     float yh[E], xh[E], gh[E], d[E], ry, rx;
-    unpack<T>(y_, yh);
-    unpack<T>(x_, xh);
+    unpack<T>(r.y, yh);
+    unpack<T>(r.x, xh);
     normalise2(yh, a.post, a.post_eps, ry, xh, pre, a.pre_eps, rx, on, invC, grp);
-    unpack<T>(dx_, d);
+    unpack<T>(r.dx, d);
     if (!a.dx1) {
 #pragma unroll
       for (int e = 0; e < E; ++e) d[e] = 0.f;
     }
     if (a.dh) {
-      unpack<T>(dh_, gh);
+      unpack<T>(r.dh, gh);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (ok) {
@@ -354,7 +392,7 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
     if (ok && on) store_chunk<T>(a.dx, at, o);
     if constexpr (GATE) {
       float t[E];
-      unpack<T>(t_, t);
+      unpack<T>(r.t, t);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         float slope;
@@ -375,6 +413,25 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
     }
     if (a.post != PA_NORM_NONE) pull_back(u, yh, ry, on, a.post, invC, grp);
     if (ok && on) store_chunk<T>(a.dy, at, u);
+  };
+  int64_t base = (int64_t)blockIdx.x * rows;  // < N
+  if constexpr (AHEAD) {
+    Rows r0, r1;
+    load(base, r0);
+    for (;;) {
+      load(base + step, r1);
+      work(base, r0);
+      if ((base += step) >= a.N) break;
+      load(base + step, r0);
+      work(base, r1);
+      if ((base += step) >= a.N) break;
+    }
+  } else {
+    for (; base < a.N; base += step) {
+      Rows r;
+      load(base, r);
+      work(base, r);
+    }
   }
   if (!a.partials) return;
   // the block's record [5][C]: its rows added in order
@@ -425,7 +482,10 @@ int resnorm_blocks(int64_t N, int C, int dtype, bool bwd) {
   const int64_t need = (N + turn - 1) / turn;
   // (backward: three blocks per CU, what its registers allow, in one round; 1024
   // blocks took 934 us where these take 793, at N = 1,000,000, C = 256)
-  const int64_t cap = g.wide ? 512 : bwd ? 768 : 2048;
+  const int waves = g.threads / 64;
+  const int64_t cap = g.wide ? (bwd ? std::min(1024, std::max(1, 12 / waves) * 256)
+                                    : std::min(2048, std::max(1, 20 / waves) * 256))
+                             : bwd ? 768 : 2048;
   return (int)(need < cap ? need : cap);
 }
 
@@ -438,16 +498,24 @@ hipError_t launch_resnorm(const ResNormArgs& a0, int dtype, bool bwd, hipStream_
   const dim3 grid(resnorm_blocks(a.N, a.C, dtype, bwd)), block(g.threads);
   const size_t lds = bwd && !g.wide ? (size_t)g.rows * 5 * a.C * sizeof(float) : 0;
   auto go = [&](auto* k) { hipLaunchKernelGGL(k, grid, block, lds, st, a); };
-  auto pick = [&](auto type, auto wide) {
+  auto pick = [&](auto type, auto wide, auto ahead) {
     using T = decltype(type);
     constexpr int W = decltype(wide)::value;
-    if (a.t) bwd ? go(k_resnorm_bwd<T, W, true>) : go(k_resnorm<T, W, true>);
-    else bwd ? go(k_resnorm_bwd<T, W, false>) : go(k_resnorm<T, W, false>);
+    constexpr bool A = decltype(ahead)::value, AB = A && !(W == 1024 && sizeof(T) == 2);
+    if (a.t) bwd ? go(k_resnorm_bwd<T, W, AB, true>) : go(k_resnorm<T, W, A, true>);
+    else bwd ? go(k_resnorm_bwd<T, W, AB, false>) : go(k_resnorm<T, W, A, false>);
   };
+  // The next rows are requested ahead where a block meets at barriers for every row
+  // (but for the backward of 1024 threads of bf16, which has no registers for it),
+  // and where a fifth or more of the lanes have no part of a row and there is less in
+  // flight (backward, us: 500,000 rows of 264 with a gate 686 -> 590, 1,000,000 of 96
+  // 341 -> 320; rows that fill their lanes lose 5%: of 256 788 and 834).
+  const int chunks = (a.C + (dtype == 1 ? 7 : 3)) / (dtype == 1 ? 8 : 4);
   auto width = [&](auto type) {
-    if (!g.wide) pick(type, std::integral_constant<int, 0>{});
-    else if (g.threads <= 512) pick(type, std::integral_constant<int, 512>{});
-    else pick(type, std::integral_constant<int, 1024>{});
+    if (!g.wide && 5 * chunks > 4 * g.L) pick(type, std::integral_constant<int, 0>{}, std::false_type{});
+    else if (!g.wide) pick(type, std::integral_constant<int, 0>{}, std::true_type{});
+    else if (g.threads <= 512) pick(type, std::integral_constant<int, 512>{}, std::true_type{});
+    else pick(type, std::integral_constant<int, 1024>{}, std::true_type{});
   };
   if (dtype == 1) width(bf16{});
   else width(float{});
