@@ -218,9 +218,9 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
 // last one of a row may be cut short; rows need not be aligned), so that a row is
 // read once: rows of up to 64 chunks are shared by the smallest power of two of
 // lanes, U rows each in turn with all their loads first; longer ones take a wave
-// and NC chunks per lane.  Rows beyond 512 chunks take a block and are read twice.
+// and NC chunks per lane.  Rows beyond 1024 chunks take a block and are read twice.
 // ---------------------------------------------------------------------------
-template <typename T, int NC, int U>
+template <typename T, bool ODD, int NC, int U>
 __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, int L, const T* x,
                                                     int8_t* q, float* s) {
   constexpr int E = Row16<T>::E;
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, in
       const int64_t n = base + u * per + slot;
 #pragma unroll
       for (int j = 0; j < NC; ++j)
-        v[u][j] = row_chunk<T>(x + (n < N ? n : N - 1) * K, K, c0 + j * L);
+        v[u][j] = row_chunk<ODD>(x + (n < N ? n : N - 1) * K, K, c0 + j * L);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, in
   }
 }
 
-template <typename T>
+template <typename T, bool ODD>
 __global__ void __launch_bounds__(512) k_quant_long(int64_t N, int K, int Kp, const T* x,
                                                     int8_t* q, float* s) {
   constexpr int E = Row16<T>::E;
@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(512) k_quant_long(int64_t N, int K, int Kp, co
   const int CP = Kp / E;
   for (int64_t n = blockIdx.x; n < N; n += gridDim.x) {
     uint32_t big = 0;
-    for (int c = threadIdx.x; c < CP; c += 512) big = max(big, largest(row_chunk<T>(x + n * K, K, c)));
+    for (int c = threadIdx.x; c < CP; c += 512) big = max(big, largest(row_chunk<ODD>(x + n * K, K, c)));
     for (int o = 1; o < 64; o <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, o));
     __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = big;
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(512) k_quant_long(int64_t N, int K, int Kp, co
     for (int w = 0; w < 8; ++w) big = max(big, red[w]);
     const QuantScale k = quant_scale(big);
     for (int c = threadIdx.x; c < CP; c += 512)
-      put_chunk(q + n * Kp + E * c, row_chunk<T>(x + n * K, K, c), k.inv);
+      put_chunk(q + n * Kp + E * c, row_chunk<ODD>(x + n * K, K, c), k.inv);
     if (threadIdx.x == 0) s[n] = k.s;
   }
 }
@@ -335,7 +335,7 @@ hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st) {
 }
 
 namespace {
-template <typename T>
+template <typename T, bool ODD>
 hipError_t run_quant(int64_t N, int K, const T* x, int8_t* q, float* s, hipStream_t st) {
   const int Kp = (K + 15) / 16 * 16, CP = Kp / Row16<T>::E;
   int L = 1;
@@ -345,21 +345,26 @@ hipError_t run_quant(int64_t N, int K, const T* x, int8_t* q, float* s, hipStrea
     hipLaunchKernelGGL(k, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, st, N, K, Kp, L,
                        x, q, s);
   };
-  if (CP <= 64) go(k_quant_rows<T, 1, 4>, 4);
-  else if (CP <= 128) go(k_quant_rows<T, 2, 2>, 2);
-  else if (CP <= 256) go(k_quant_rows<T, 4, 1>, 1);
-  else if (CP <= 512) go(k_quant_rows<T, 8, 1>, 1);
+  if (CP <= 64) go(k_quant_rows<T, ODD, 1, 4>, 4);
+  else if (CP <= 128) go(k_quant_rows<T, ODD, 2, 2>, 2);
+  else if (CP <= 256) go(k_quant_rows<T, ODD, 4, 1>, 1);
+  else if (CP <= 512) go(k_quant_rows<T, ODD, 8, 1>, 1);
+  else if (CP <= 1024) go(k_quant_rows<T, ODD, 16, 1>, 1);
   else
-    hipLaunchKernelGGL(k_quant_long<T>, dim3((unsigned)(N < 4096 ? N : 4096)), dim3(512), 0, st, N, K,
-                       Kp, x, q, s);
+    hipLaunchKernelGGL((k_quant_long<T, ODD>), dim3((unsigned)(N < 4096 ? N : 4096)), dim3(512), 0, st,
+                       N, K, Kp, x, q, s);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t run_quant(int64_t N, int K, const void* x, int8_t* q, float* s, hipStream_t st) {
+  const T* p = reinterpret_cast<const T*>(x);
+  return K % Row16<T>::E ? run_quant<T, true>(N, K, p, q, s, st) : run_quant<T, false>(N, K, p, q, s, st);
 }
 }  // namespace
 
 hipError_t launch_quant_rows(int64_t N, int K, int dtype, const void* x, int8_t* q, float* s,
                              hipStream_t st) {
-  return dtype == 1 ? run_quant(N, K, (const bf16*)x, q, s, st)
-                    : run_quant(N, K, (const float*)x, q, s, st);
+  return dtype == 1 ? run_quant<bf16>(N, K, x, q, s, st) : run_quant<float>(N, K, x, q, s, st);
 }
 
 hipError_t launch_quant_weight(int K, int F, int dtype, const void* W, int8_t* Wq, float* sw,

@@ -42,17 +42,35 @@ template <typename T> struct Row16 {
   static constexpr int E = 16 / (int)sizeof(T);
   T v[E];
 };
-template <typename T>
+// Chunk c of a row of K elements, zeros behind its end, without a branch around
+// the load (which would be waited for at once).  ODD: K is no multiple of E and
+// rows start anywhere; the chunk that is cut short is the row's last E elements
+// shifted down.  K < E: element by element.
+template <bool ODD, typename T>
 __device__ __forceinline__ Row16<T> row_chunk(const T* row, int K, int c) {
   constexpr int E = Row16<T>::E;
   Row16<T> o;
-  if (E * c + E <= K) {
-    __builtin_memcpy(&o, row + E * c, 16);
+  if constexpr (!ODD) {
+    const bool in = E * c < K;
+    const uint4 q = *reinterpret_cast<const uint4*>(row + (in ? E * c : 0));
+    return __builtin_bit_cast(Row16<T>, in ? q : uint4{0, 0, 0, 0});
   } else {
+    if (K < E) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) o.v[e] = E * c + e < K ? row[E * c + e] : from_f<T>(0.f);
+      for (int e = 0; e < E; ++e) o.v[e] = E * c + e < K ? row[E * c + e] : from_f<T>(0.f);
+      return o;
+    }
+    const int start = E * c + E <= K ? E * c : K - E;
+    uint64_t w[2];
+    __builtin_memcpy(w, row + start, 16);
+    const int s = (E * c - start) * 8 * (int)sizeof(T);  // bits behind the end, 0 .. 128 and more
+    const uint64_t lo = s >= 128 ? 0 : s >= 64 ? w[1] >> (s - 64) : s ? w[0] >> s | w[1] << (64 - s) : w[0];
+    const uint64_t hi = s >= 64 ? 0 : w[1] >> s;
+    w[0] = lo;
+    w[1] = hi;
+    __builtin_memcpy(&o, w, 16);
+    return o;
   }
-  return o;
 }
 // The bits of a chunk's largest magnitude as an fp32 number.
 __device__ __forceinline__ uint32_t largest(const Row16<float>& c) {

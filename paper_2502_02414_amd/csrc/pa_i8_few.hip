@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kFewRows = 16, kFewLds = 144 * 1024;
 
-template <typename TX, typename TD>
+template <typename TX, typename TD, bool ODD>
 __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
   constexpr int E = Row16<TX>::E, U = 8, NOWHERE = 0x7fffff00;
   extern __shared__ __attribute__((aligned(16))) char xs[];  // [N][Kp + 16]
@@ -45,29 +45,17 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
   // them in registers
   constexpr int H = 4;
   const int n = tid / G, tg = tid % G, CP = Kp / E;
-  const bool mine = n < N, whole = K % E == 0;
+  const bool mine = n < N;
   const TX* X = reinterpret_cast<const TX*>(a.x) + (int64_t)(mine ? n : 0) * K;
   if (tid < kFewRows) big[tid] = 0;
   Row16<TX> v[H];
-  if (whole) {
-    const auto rx = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(a.x), 0,
-                                                      N * K * (int)sizeof(TX), 0x00027000);
 #pragma unroll
-    for (int j = 0; j < H; ++j) {
-      const int c = tg + j * G;
-      v[j] = __builtin_bit_cast(
-          Row16<TX>, __builtin_amdgcn_raw_buffer_load_b128(
-                         rx, mine && c * E < K ? (n * K + c * E) * (int)sizeof(TX) : NOWHERE, 0, 0));
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < H; ++j) v[j] = row_chunk<TX>(X, K, tg + j * G);
-  }
+  for (int j = 0; j < H; ++j) v[j] = row_chunk<ODD>(X, K, tg + j * G);
   __syncthreads();
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < H; ++j) m = max(m, largest(v[j]));
-  for (int c = tg + H * G; c < CP; c += G) m = max(m, largest(row_chunk<TX>(X, K, c)));
+  for (int c = tg + H * G; c < CP; c += G) m = max(m, largest(row_chunk<ODD>(X, K, c)));
   if (mine) atomicMax(&big[n], m);
   __syncthreads();
   if (mine) {
@@ -76,7 +64,7 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
 #pragma unroll
     for (int j = 0; j < H; ++j)
       if (tg + j * G < CP) put_chunk(row + E * (tg + j * G), v[j], q.inv);
-    for (int c = tg + H * G; c < CP; c += G) put_chunk(row + E * c, row_chunk<TX>(X, K, c), q.inv);
+    for (int c = tg + H * G; c < CP; c += G) put_chunk(row + E * c, row_chunk<ODD>(X, K, c), q.inv);
     if (tg == 0) ss[n] = q.s;
   }
   __syncthreads();
@@ -119,8 +107,11 @@ hipError_t run(const I8Args& a, hipStream_t st) {
   while (NP < a.N) NP *= 2;
   const int FB = 16 * (8 / KW);
   const size_t lds = (size_t)a.N * (a.Kp + 16);
-  hipLaunchKernelGGL((k_linear_few<TX, TD>), dim3((a.F + FB - 1) / FB), dim3(512), lds, st, a, KW,
-                     512 / NP);
+  const dim3 grid((a.F + FB - 1) / FB), block(512);
+  if (a.K % Row16<TX>::E)
+    hipLaunchKernelGGL((k_linear_few<TX, TD, true>), grid, block, lds, st, a, KW, 512 / NP);
+  else
+    hipLaunchKernelGGL((k_linear_few<TX, TD, false>), grid, block, lds, st, a, KW, 512 / NP);
   return hipGetLastError();
 }
 
