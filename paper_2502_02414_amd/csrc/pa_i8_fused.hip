@@ -1,6 +1,7 @@
 // A linear layer in 8-bit integers on many rows of few channels, in one pass
 // (gfx950, bf16 rows in and out): the rows are quantised on the way into LDS, so
-// that neither their integers nor their scales go through memory.
+// that neither their integers nor their scales go through memory (XQ: rows that
+// are integers already).
 //
 // A block is persistent on its CU: each of its eight waves keeps the integer
 // weights of 16 NCT output channels in registers (the MFMA A operand, at most
@@ -20,21 +21,22 @@
 namespace pa {
 namespace {
 
-template <int KS, int NCT>
+template <bool XQ, int KS, int NCT>
 struct FusedGeo {
   static constexpr int FCB = 128 * NCT;               // channels of a block
   static constexpr int PTS = 32, RB = 64 * KS;        // points of a tile, bytes of a row
   static constexpr int TILE = PTS * RB;
-  static constexpr int NC = (8 * KS + 15) / 16;       // 16-byte chunks of a row per lane
+  // 16-byte chunks of a row per lane (XQ: of integers)
+  static constexpr int NC = XQ ? (4 * KS + 15) / 16 : (8 * KS + 15) / 16;
   static constexpr int RUNS = (NCT + 1) / 2;          // runs of 8 (NCT = 1: 4) channels
 };
 template <int KS> __device__ __forceinline__ int key_of(int row) {
   return KS == 1 ? (row >> 1) & 3 : row & 7;
 }
 
-template <int ACT, int KS, int NCT>
+template <bool XQ, int ACT, int KS, int NCT>
 __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
-  using G = FusedGeo<KS, NCT>;
+  using G = FusedGeo<XQ, KS, NCT>;
   constexpr int V = NCT == 1 ? 4 : 8;
   __shared__ __attribute__((aligned(16))) char xs[2][G::TILE];
   __shared__ float ss[2][G::PTS];
@@ -56,40 +58,64 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   // as zeros) what lies behind the rows of the tile, or at an offset behind them:
   // with no branch around a load or a store, the wait for a tile's rows is neither
   // where they are requested nor one for results that were stored after that.
-  auto tile_of = [&](const void* p, int64_t t, int width) {
+  auto tile_of = [&](const void* p, int64_t t, int width) {  // rows of `width` bytes
     const int64_t left = a.N - t * G::PTS;
     return __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<char*>(reinterpret_cast<const char*>(p)) + t * G::PTS * width * 2, 0,
-        (int)(left < G::PTS ? left : G::PTS) * width * 2, 0x00027000);
+        const_cast<char*>(reinterpret_cast<const char*>(p)) + t * G::PTS * width, 0,
+        (int)(left < G::PTS ? left : G::PTS) * width, 0x00027000);
   };
   constexpr int NOWHERE = 0x7fffff00;
   // the tile's row and chunks of this thread
   const int row = threadIdx.x >> 4, c0 = threadIdx.x & 15;
   i32x4 xr[G::NC];
+  float xscale = 0.f;
   auto load = [&](int64_t t) __attribute__((always_inline)) {
-    const auto rx = tile_of(a.x, t < t1 ? t : t1 - 1, K);
+    const int64_t tc = t < t1 ? t : t1 - 1;
+    if constexpr (XQ) {
+      const auto rx = tile_of(a.q, tc, a.Kp), rs = tile_of(a.s, tc, 4);
 #pragma unroll
-    for (int j = 0; j < G::NC; ++j) {
-      const int c = 8 * (c0 + 16 * j);  // K is a multiple of 8
-      xr[j] = __builtin_bit_cast(
-          i32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, c < K ? (row * K + c) * 2 : NOWHERE, 0, 0));
+      for (int j = 0; j < G::NC; ++j) {
+        const int c = 16 * (c0 + 16 * j);
+        xr[j] = __builtin_bit_cast(
+            i32x4,
+            __builtin_amdgcn_raw_buffer_load_b128(rx, c < a.Kp ? row * a.Kp + c : NOWHERE, 0, 0));
+      }
+      xscale = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rs, row * 4, 0, 0));
+    } else {
+      const auto rx = tile_of(a.x, tc, K * 2);
+#pragma unroll
+      for (int j = 0; j < G::NC; ++j) {
+        const int c = 8 * (c0 + 16 * j);  // K is a multiple of 8
+        xr[j] = __builtin_bit_cast(
+            i32x4,
+            __builtin_amdgcn_raw_buffer_load_b128(rx, c < K ? (row * K + c) * 2 : NOWHERE, 0, 0));
+      }
     }
   };
-  const int put = row * G::RB + 16 * ((c0 >> 1) ^ key_of<KS>(row)) + 8 * (c0 & 1);
+  // a lane's chunk j: 8 integers, half a 16-byte chunk (XQ: 16, a whole one)
+  const int put = row * G::RB + (XQ ? 16 * (c0 ^ key_of<KS>(row))
+                                    : 16 * ((c0 >> 1) ^ key_of<KS>(row)) + 8 * (c0 & 1));
   auto store = [&](int buf) __attribute__((always_inline)) {
-    uint32_t big = 0;
+    if constexpr (XQ) {
 #pragma unroll
-    for (int j = 0; j < G::NC; ++j) big = max(big, largest(__builtin_bit_cast(Row16<bf16>, xr[j])));
-    const QuantScale q = quant_scale(row16_max(big));
+      for (int j = 0; j < G::NC; ++j)
+        if (16 * (c0 + 16 * j) < G::RB)
+          *reinterpret_cast<i32x4*>(xs[buf] + put + 256 * j) = xr[j];
+      if (c0 == 0) ss[buf][row] = xscale;
+    } else {
+      uint32_t big = 0;
 #pragma unroll
-    for (int j = 0; j < G::NC; ++j) {
-      const int c = c0 + 16 * j;  // 8 integers: half a 16-byte chunk
-      if (8 * c < G::RB)
-        put_chunk(reinterpret_cast<int8_t*>(xs[buf] + put + 128 * j),
-                  __builtin_bit_cast(Row16<bf16>, xr[j]), q.inv);
-      if (G::NC > 2) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
+      for (int j = 0; j < G::NC; ++j) big = max(big, largest(__builtin_bit_cast(Row16<bf16>, xr[j])));
+      const QuantScale q = quant_scale(row16_max(big));
+#pragma unroll
+      for (int j = 0; j < G::NC; ++j) {
+        if (8 * (c0 + 16 * j) < G::RB)
+          put_chunk(reinterpret_cast<int8_t*>(xs[buf] + put + 128 * j),
+                    __builtin_bit_cast(Row16<bf16>, xr[j]), q.inv);
+        if (G::NC > 2) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
+      }
+      if (c0 == 0) ss[buf][row] = q.s;
     }
-    if (c0 == 0) ss[buf][row] = q.s;
   };
 
   // weights: MFMA row r of tile i is channel fw + step(i) + 8 (r / 4) + r % 4 (NCT
@@ -139,7 +165,7 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   };
   auto tile = [&](int64_t t, int buf, auto RES) __attribute__((always_inline)) {
     constexpr bool res = decltype(RES)::value;
-    const auto rd = tile_of(a.D, t, F), rc = tile_of(res ? a.C : a.D, t, F);
+    const auto rd = tile_of(a.D, t, F * 2), rc = tile_of(res ? a.C : a.D, t, F * 2);
     BV c[2][AHEAD ? G::RUNS : 1];
     if constexpr (res && AHEAD)
 #pragma unroll
@@ -202,18 +228,26 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   else walk([&](int64_t t, int buf) { tile(t, buf, std::false_type{}); });
 }
 
-template <int KS, int NCT>
+template <bool XQ, int KS, int NCT>
 hipError_t run(const I8Args& a, hipStream_t st) {
-  using G = FusedGeo<KS, NCT>;
+  using G = FusedGeo<XQ, KS, NCT>;
   const int ncg = (a.F + G::FCB - 1) / G::FCB;
   const int64_t tiles = (a.N + G::PTS - 1) / G::PTS;
   const int PG = (int)(tiles < 256 / ncg ? tiles : 256 / ncg);
   const dim3 grid(PG * ncg), block(512);
   if (a.act == PA_ACT_GELU)
-    hipLaunchKernelGGL((k_linear_i8<PA_ACT_GELU, KS, NCT>), grid, block, 0, st, a, PG);
+    hipLaunchKernelGGL((k_linear_i8<XQ, PA_ACT_GELU, KS, NCT>), grid, block, 0, st, a, PG);
   else
-    hipLaunchKernelGGL((k_linear_i8<PA_ACT_NONE, KS, NCT>), grid, block, 0, st, a, PG);
+    hipLaunchKernelGGL((k_linear_i8<XQ, PA_ACT_NONE, KS, NCT>), grid, block, 0, st, a, PG);
   return hipGetLastError();
+}
+template <bool XQ>
+hipError_t by_size(const I8Args& a, hipStream_t st) {
+  if (a.K <= 64) return run<XQ, 1, 4>(a, st);
+  if (a.K <= 128) return run<XQ, 2, 4>(a, st);
+  if (a.K <= 256) return a.F <= 256 ? run<XQ, 4, 2>(a, st) : run<XQ, 4, 8>(a, st);
+  if (a.K <= 512) return a.F <= 128 ? run<XQ, 8, 1>(a, st) : run<XQ, 8, 4>(a, st);
+  return run<XQ, 16, 2>(a, st);
 }
 
 }  // namespace
@@ -223,18 +257,14 @@ hipError_t run(const I8Args& a, hipStream_t st) {
 // 256 to 1024 with GELU 14.3 and 16.2 at 4,096 rows, 18.4 and 17.5 at 8,192, 118
 // and 79 at 100,000; 1024 to 256 10.8 and 12.9 at 2,048, 19.1 and 14.0 at 8,192; 256
 // to 256 7.9 and 5.4 at 512, 41 and 22 at 100,000; 128 to 1024 7.5 and 5.9 at 512.)
-bool linear_i8_fused(int64_t N, int F, int K, int x_dtype, int d_dtype) {
-  if (x_dtype != 1 || d_dtype != 1 || K % 8 || F % 8 || K > 1024) return false;
+bool linear_i8_fused(int64_t N, int F, int K) {
+  if (F % 8 || K > 1024) return false;
   const int most = K <= 128 ? 1024 : K <= 256 ? 2048 : K <= 512 ? 1024 : 512;
   return F <= most && (K * F <= 131072 || N >= 6144);
 }
 
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st) {
-  if (a.K <= 64) return run<1, 4>(a, st);
-  if (a.K <= 128) return run<2, 4>(a, st);
-  if (a.K <= 256) return a.F <= 256 ? run<4, 2>(a, st) : run<4, 8>(a, st);
-  if (a.K <= 512) return a.F <= 128 ? run<8, 1>(a, st) : run<8, 4>(a, st);
-  return run<16, 2>(a, st);
+  return a.q ? by_size<true>(a, st) : by_size<false>(a, st);
 }
 
 }  // namespace pa

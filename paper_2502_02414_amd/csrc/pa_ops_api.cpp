@@ -388,6 +388,12 @@ static pa_status product(const char* who, pa::I8Args& a, int64_t N, int F, int K
   return PA_OK;
 }
 
+// The product of rows that are integers.
+static hipError_t integers(const pa::I8Args& a, int d_dtype, hipStream_t st) {
+  return d_dtype == PA_BF16 && pa::linear_i8_fused(a.N, a.F, a.K) ? pa::launch_linear_i8(a, st)
+                                                                  : pa::launch_gemm_i8(a, d_dtype, st);
+}
+
 pa_status pa_gemm_i8(int64_t N, int F, int K, const int8_t* q, const float* s, const int8_t* Wq,
                      const float* sw, const float* bias, pa_act act, const void* C, void* D,
                      pa_dtype d_dtype, void* stream) {
@@ -397,7 +403,7 @@ pa_status pa_gemm_i8(int64_t N, int F, int K, const int8_t* q, const float* s, c
   PO_TRY(need(who, q, "q"));
   PO_TRY(need(who, s, "s", 4));
   a.q = q; a.s = s;
-  PO_HIP(pa::launch_gemm_i8(a, d_dtype, as_stream(stream)), who);
+  PO_HIP(integers(a, d_dtype, as_stream(stream)), who);
   return PA_OK;
 }
 
@@ -424,7 +430,7 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
     PO_HIP(pa::launch_linear_few(a, d_dtype, as_stream(stream)), who);
     return PA_OK;
   }
-  if (pa::linear_i8_fused(N, F, K, x_dtype, d_dtype)) {
+  if (x_dtype == PA_BF16 && d_dtype == PA_BF16 && K % 8 == 0 && pa::linear_i8_fused(N, F, K)) {
     PO_HIP(pa::launch_linear_i8(a, as_stream(stream)), who);
     return PA_OK;
   }
@@ -437,7 +443,7 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   PO_HIP(pa::launch_quant_rows(N, K, x_dtype, x, q, s, as_stream(stream)), who);
   a.q = q;
   a.s = s;
-  PO_HIP(pa::launch_gemm_i8(a, d_dtype, as_stream(stream)), who);
+  PO_HIP(integers(a, d_dtype, as_stream(stream)), who);
   return PA_OK;
 }
 

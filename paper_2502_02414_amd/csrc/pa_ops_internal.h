@@ -92,9 +92,10 @@ struct I8Args {
   void* D = nullptr;
 };
 hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st);
-// Rows quantised on the way into a product that keeps its weights in registers
-// (pa_i8_fused.hip): served, and faster than the two launches.
-bool linear_i8_fused(int64_t N, int F, int K, int x_dtype, int d_dtype);
+// Products of many rows that keep their weights in registers (pa_i8_fused.hip; bf16
+// results), of integers, or of bf16 rows that they quantise: served, and faster
+// than the tiles.
+bool linear_i8_fused(int64_t N, int F, int K);
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st);
 // Few rows (pa_i8_few.hip): served.
 bool linear_i8_few(int64_t N, int K);
