@@ -1,0 +1,154 @@
+"""The operators of include/pa_ops.h together, as the block stack uses them: a
+training step (SandwichStack forward and backward, AdamW), and inference with
+the MLP in 8-bit integers."""
+import numpy as np
+import pytest
+import torch
+
+import ops_ref as R
+from paper_2502_02414_amd import ops
+from paper_2502_02414_amd.stack import BlockStack, SandwichStack
+from pa_cases import say
+from test_gpu_ops import check_step
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def make(N, C, M, L, dt, kind=BlockStack, seed=0, **kw):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    rnd = lambda *s, scale=1.0: scale * torch.randn(*s, generator=g)
+    ps = []
+    for _ in range(L):
+        p = {"Wp": rnd(C, C, scale=C ** -0.5), "bp": rnd(C, scale=0.1), "A": rnd(C, M, scale=C ** -0.5),
+             "b": rnd(M, scale=0.1), "a": rnd(C, scale=0.02 * C ** -0.5),
+             "ln1_g": 1 + rnd(C, scale=0.1), "ln1_b": rnd(C, scale=0.1),
+             "ln2_g": 1 + rnd(C, scale=0.1), "ln2_b": rnd(C, scale=0.1),
+             "b1": rnd(4 * C, scale=0.1), "b2": rnd(C, scale=0.1),
+             "W1": rnd(C, 4 * C, scale=C ** -0.5).to(dt), "W2": rnd(4 * C, C, scale=0.5 * C ** -0.5).to(dt)}
+        for n in "qkvo":
+            p["W" + n], p["b" + n] = rnd(C, C, scale=C ** -0.5), rnd(C, scale=0.1)
+        if kind is SandwichStack:
+            for k in "12":
+                p["rs" + k] = 0.5 + rnd(C, scale=0.1)
+                p[f"post{k}_g"] = 1 + rnd(C, scale=0.1)
+                if kw.get("post") == "layer":
+                    p[f"post{k}_b"] = rnd(C, scale=0.1)
+        p = {k: v.cuda() for k, v in p.items()}
+        p["b_t"] = 0.5
+        ps.append(p)
+    x = rnd(N, C).to(dt).cuda()
+    Gs = [-torch.log(-torch.log(torch.rand(N, M, generator=g).clamp(1e-6, 1 - 1e-6))).to(dt).cuda()
+          for _ in range(L)]
+    return kind(N, C, 4, M, ps, dt, **kw), x, Gs, rnd(N, C).to(dt).cuda()
+
+
+@pytest.mark.parametrize("post", ["rms", "layer"])
+def test_sandwich_joins_as_its_parts(post):
+    """Forward: each joint against 64 bits on the tensors that the stack kept."""
+    s, x, Gs, _ = make(777, 64, 16, 2, F32, SandwichStack, post=post)
+    out = s.forward(x, Gs)
+    cpu = lambda t: None if t is None else t.cpu()
+    for l, c in enumerate(s.caches):
+        p = {k: cpu(v) for k, v in s.params[l].items() if torch.is_tensor(v)}
+        before = x if l == 0 else s.caches[l - 1]["x2"]
+        for k, (xi, y, x1) in enumerate(((before, c["y"], c["x1"]), (c["x1"], c["z"], c["x2"])), 1):
+            q = {"post": post, "post_g": p[f"post{k}_g"], "post_b": p.get(f"post{k}_b"),
+                 "scale": p[f"rs{k}"]}
+            ref, err = R.joint(q, cpu(xi), cpu(y))
+            off = (cpu(x1).double() - ref).abs()
+            assert (off <= R.U * (err + ref.abs())).all(), (l, k)
+        q = {"pre": "layer", "pre_g": p["ln2_g"], "pre_b": p["ln2_b"]}
+        ref, err = R.pre(q, cpu(c["x1"]))
+        assert ((cpu(c["h2"]).double() - ref).abs() <= R.U * (err + ref.abs())).all(), l
+    assert torch.equal(out, s.caches[-1]["x2"])
+    assert torch.equal(s.infer(x, Gs), out)
+
+
+@pytest.mark.parametrize("post", ["rms", "layer"])
+def test_sandwich_gradients_against_differences(post):
+    """Directional differences of <w, forward> for the input and every parameter.
+    Two step widths tell the truncation (the quotient's error goes with the
+    square of the step: the wider one has four times as much); the outputs' fp32
+    rounding, at most 2^-18 of their size each after some 30 operations on a path,
+    divided by the step 2^-6, is below 1e-3 of the terms' root sum of squares."""
+    s, x, Gs, w = make(300, 64, 16, 2, F32, SandwichStack, post=post, seed=3)
+    w = 1 + 0.5 * w
+    out = s.forward(x, Gs)
+    dx, grads = s.backward(w.clone())
+    noise = 2.0 ** -18 * (w.double() * out.double()).norm().item() / 2.0 ** -6
+
+    def loss():
+        return (w.double() * s.forward(x, Gs).double()).sum().item()
+
+    named = {**s.named_parameters(), "x": x}
+    got = {**s.named_grads(grads), "x": dx}
+    assert set(named) - set(got) == set()
+    g = torch.Generator()
+    g.manual_seed(5)
+    for k, t in named.items():
+        v = torch.randn(t.shape, generator=g).cuda()
+        v = v / v.norm() * t.norm() if t.norm() > 0 else v
+        keep, quot = t.clone(), {}
+        for h in (2.0 ** -6, 2.0 ** -5):
+            side = []
+            for sign in (1, -1):
+                t.copy_(keep + sign * h * v)
+                side.append(loss())
+            quot[h] = (side[0] - side[1]) / (2 * h)
+        t.copy_(keep)
+        want = (got[k].double() * v.double()).sum().item()
+        tol = 2 * abs(quot[2.0 ** -5] - quot[2.0 ** -6]) + noise + 1e-3 * abs(want)
+        say(f"  {k:12s} {want:12.5g} differences {quot[2.0 ** -6]:12.5g} tolerance {tol:.3g}")
+        assert abs(want - quot[2.0 ** -6]) <= tol, k
+
+
+@pytest.mark.parametrize("kind,dt,bits", [(BlockStack, F32, 32), (SandwichStack, F32, 8),
+                                          (SandwichStack, BF16, 8), (BlockStack, BF16, 32)])
+def test_training_steps(kind, dt, bits):
+    """Three steps: after each, every parameter, moment and rounded copy is the
+    reference's step from the gradients that the backward returned."""
+    say(f"{kind.__name__} {dt} {bits} bits")
+    s, x, Gs, w = make(1001, 64, 16, 2, dt, kind)
+    opt = s.adamw(lr=1e-2, bits=bits, wd=0.1, seed=4)
+    clip = torch.tensor([0.25], device="cuda")
+    names = list(s.named_parameters())
+    cpu = lambda t: t.cpu().clone() if torch.is_tensor(t) else t
+    for step in (1, 2, 3):
+        s.forward(x, Gs)
+        _, grads = s.backward(w)
+        grads = s.named_grads(grads)
+        before = [{k: cpu(v) for k, v in d.items() if v is not None} for d in opt.items.tensors]
+        for d, k in zip(before, names):
+            d["g"] = grads[k].cpu()
+            d["shape"] = d["p"].shape
+        opt.step(grads, gscale=clip)
+        after = [{k: v for k, v in d.items() if v is not None} for d in opt.items.tensors]
+        flat = lambda ds: [{k: v.reshape(-1) if torch.is_tensor(v) else v for k, v in d.items()}
+                           for d in ds]
+        check_step(flat(before), flat(after), step, 4, clip.cpu(), lr=1e-2)
+    for k, t in s.named_parameters().items():  # the stack computes with them
+        p = opt.items.tensors[names.index(k)]["p"]
+        assert torch.equal(t, p.to(t.dtype)), k
+    assert torch.isfinite(s.forward(x, Gs).float()).all()
+
+
+@pytest.mark.parametrize("kind,dt", [(BlockStack, F32), (BlockStack, BF16), (SandwichStack, F32),
+                                     (SandwichStack, BF16)])
+@pytest.mark.parametrize("N,C", [(1001, 64), (8192, 128)])
+def test_inference_in_8_bits(kind, dt, N, C):
+    """infer is forward bit for bit; with the MLP's products in integers it is
+    within 3%: an element is off by at most half of max / 127, about 0.3 / 127
+    max ~ 0.8% of a row's size, for the rows and the weights of two products
+    (together 1.6% of the MLP's part), and the next block carries that on."""
+    s, x, Gs, _ = make(N, C, 16, 2, dt, kind)
+    want = s.forward(x, Gs)
+    assert torch.equal(s.infer(x, Gs), want)
+    s.quantize()
+    got = s.infer(x, Gs)
+    rel = ((got.double() - want.double()).norm() / want.double().norm()).item()
+    say(f"  {kind.__name__} {dt} N={N} C={C}: {rel:.4f}")
+    assert 1e-5 < rel <= 0.03
+    assert torch.equal(s.infer(x, Gs), got)
