@@ -139,7 +139,8 @@ typedef struct {
 } pa_adamw_args;
 
 /* items is a host array, read before the call returns.  The tensors of one
- * call must not overlap: p, m and v ranges of different items are checked. */
+ * call must not overlap: whatever is written (p, copy, m, v and the scales) is
+ * checked; gradients may be shared. */
 pa_status pa_adamw(int n_items, const pa_adamw_item* items, const pa_adamw_args* args,
                    void* stream);
 

@@ -4,6 +4,19 @@
 //
 // The weights are the MFMA's A operand and the points its B operand, so that a
 // lane of a 16 x 16 result tile holds four consecutive channels of one point.
+//
+// Large products are bound by what the card's matrix cores sustain on integers:
+// 8192^3 474 us (2.32 PFLOP/s' worth of operations; a library product of plain
+// integers 2.07), 4096^3 64 to 74 us by the card, on a first form whose
+// operands came straight from memory, without LDS, 640 us.  Counters at 4096^3: no
+// LDS bank conflicts, the matrix cores busy 42% of the time.  Also built, exact and
+// within 3% (not kept): two groups of four waves that take turns between the
+// products and the operand reads, with raised wave priority and four buffers of 64
+// bytes of K (4096^3 75 us where this form takes 74 on the same card; 8192^3 463
+// and 474).  Small products are bound by latency: 333 x 1000 x 517 5.0 us with
+// four buffers under the tiles of 64 x 64, 9.8 us with two.  Four groups of waves
+// that share K gained 0 to 15% there (128 x 4096 x 4096 10.8 -> 9.2 us) and lost
+// as much below K = 1024: not kept.
 #include <type_traits>
 
 #include "pa_i8.hpp"
@@ -47,6 +60,59 @@ __device__ __forceinline__ int key_f(int row) {  // of a row of weights
   else return row & 7;
 }
 __device__ __forceinline__ int key_n(int row) { return row & 7; }
+
+// A wave's results: acc[i][j] is MFMA tile i of its channels, from f1 on, and j of
+// its points, n1 + 16 j; in runs of V channels of one point.  (A row's start, and
+// so a run, need not be aligned: F is any number.)
+template <typename T, int ACT, int MF, int MN>
+__device__ __forceinline__ void results(const I8Args& a, const i32x4 (&acc)[MF][MN], int64_t n1,
+                                        int f1, int g) {
+  constexpr int V = sizeof(T) == 2 ? 8 : 4, RUN = V / 4;
+  typedef T TV __attribute__((ext_vector_type(V)));
+  T* D = reinterpret_cast<T*>(a.D);
+  const T* Cr = reinterpret_cast<const T*>(a.C);
+  float sn[MN];
+#pragma unroll
+  for (int j = 0; j < MN; ++j) sn[j] = a.s[n1 + 16 * j < a.N ? n1 + 16 * j : a.N - 1];
+#pragma unroll
+  for (int i = 0; i < MF; i += RUN) {
+    const int f = f1 + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
+    float sw[V], b[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int fe = f + e < a.F ? f + e : a.F - 1;
+      sw[e] = a.sw[fe];
+      b[e] = a.bias ? a.bias[fe] : 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < MN; ++j) {
+      const int64_t n = n1 + 16 * j, at = n * a.F + f;
+      float u[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        u[e] = fmaf((float)acc[i + e / 4][j][e % 4], sn[j] * sw[e], b[e]);
+        if constexpr (ACT == PA_ACT_GELU) u[e] = gelu_for<T>(u[e]);
+      }
+      if (n < a.N && f + V <= a.F) {
+        if (Cr) {
+          TV c;
+          __builtin_memcpy(&c, Cr + at, 16);
+#pragma unroll
+          for (int e = 0; e < V; ++e) u[e] += (float)c[e];
+        }
+        TV o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = (T)u[e];
+        __builtin_memcpy(D + at, &o, 16);
+      } else if (n < a.N) {
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+          if (f + e < a.F) D[at + e] = from_f<T>(Cr ? u[e] + to_f<T>(Cr[at + e]) : u[e]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
+    }
+  }
+}
 
 template <typename T, int ACT, int WF, int WN, int MF, int MN, int NB>
 __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
@@ -163,54 +229,7 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing comes into LDS once it is given back
   }
 
-  // the results: runs of V channels of one point
-  constexpr int V = sizeof(T) == 2 ? 8 : 4, RUN = V / 4;
-  typedef T TV __attribute__((ext_vector_type(V)));
-  T* D = reinterpret_cast<T*>(a.D);
-  const T* Cr = reinterpret_cast<const T*>(a.C);
-  const int64_t nr = n0 + row_n;
-  float sn[MN];
-#pragma unroll
-  for (int j = 0; j < MN; ++j) sn[j] = a.s[nr + 16 * j < a.N ? nr + 16 * j : a.N - 1];
-#pragma unroll
-  for (int i = 0; i < MF; i += RUN) {
-    const int f = f0 + wf * 16 * MF + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
-    float sw[V], b[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int fe = f + e < a.F ? f + e : a.F - 1;
-      sw[e] = a.sw[fe];
-      b[e] = a.bias ? a.bias[fe] : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < MN; ++j) {
-      const int64_t n = nr + 16 * j, at = n * a.F + f;
-      float u[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        u[e] = fmaf((float)acc[i + e / 4][j][e % 4], sn[j] * sw[e], b[e]);
-        if constexpr (ACT == PA_ACT_GELU) u[e] = gelu_for<T>(u[e]);
-      }
-      if (n < a.N && f + V <= a.F) {
-        // (a row's start, and so a run, need not be aligned: F is any number)
-        if (Cr) {
-          TV c;
-          __builtin_memcpy(&c, Cr + at, 16);
-#pragma unroll
-          for (int e = 0; e < V; ++e) u[e] += (float)c[e];
-        }
-        TV o;
-#pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = (T)u[e];
-        __builtin_memcpy(D + at, &o, 16);
-      } else if (n < a.N) {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-          if (f + e < a.F) D[at + e] = from_f<T>(Cr ? u[e] + to_f<T>(Cr[at + e]) : u[e]);
-      }
-      __builtin_amdgcn_sched_barrier(0);  // (more runs at once would spill)
-    }
-  }
+  results<T, ACT, MF, MN>(a, acc, n0 + row_n, f0 + wf * 16 * MF, g);
 }
 
 // ---------------------------------------------------------------------------
@@ -218,7 +237,9 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
 // last one of a row may be cut short; rows need not be aligned), so that a row is
 // read once: rows of up to 64 chunks are shared by the smallest power of two of
 // lanes, U rows each in turn with all their loads first; longer ones take a wave
-// and NC chunks per lane.  Rows beyond 1024 chunks take a block and are read twice.
+// and NC chunks per lane.  Bound by memory: 4096 rows of 4096 bf16 9.7 us (5.2
+// TB/s), a million of 256 147 us (5.2 TB/s); rows of odd lengths at 2.3 to 3 TB/s
+// (unaligned loads touch more lines, and the shifts of a cut chunk).  Rows beyond 1024 chunks take a block and are read twice.
 // ---------------------------------------------------------------------------
 template <typename T, bool ODD, int NC, int U>
 __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, int L, const T* x,

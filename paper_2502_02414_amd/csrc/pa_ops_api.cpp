@@ -194,7 +194,7 @@ static pa_status adamw_overlap(const char* who, int n, const pa_adamw_item* item
   struct Range { uintptr_t lo, hi; };
   try {
     std::vector<Range> r;
-    r.reserve(3 * (size_t)n);
+    r.reserve(6 * (size_t)n);
     for (int i = 0; i < n; ++i) {
       const pa_adamw_item& t = items[i];
       if (!t.n) continue;
@@ -202,6 +202,10 @@ static pa_status adamw_overlap(const char* who, int n, const pa_adamw_item* item
       r.push_back({(uintptr_t)t.p, (uintptr_t)t.p + 4 * (uintptr_t)t.n});
       r.push_back({(uintptr_t)t.m, (uintptr_t)t.m + st * (uintptr_t)t.n});
       r.push_back({(uintptr_t)t.v, (uintptr_t)t.v + st * (uintptr_t)t.n});
+      if (t.copy) r.push_back({(uintptr_t)t.copy, (uintptr_t)t.copy + 2 * (uintptr_t)t.n});
+      const uintptr_t sb = 4 * (((uintptr_t)t.n + 255) / 256);
+      if (t.m_scale) r.push_back({(uintptr_t)t.m_scale, (uintptr_t)t.m_scale + sb});
+      if (t.v_scale) r.push_back({(uintptr_t)t.v_scale, (uintptr_t)t.v_scale + sb});
     }
     std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
     for (size_t i = 1; i < r.size(); ++i)

@@ -458,7 +458,8 @@ PRODUCTS = [(1, 16, 16), (1, 256, 1024), (1, 4096, 4096), (2, 100, 33), (5, 1000
             (1, 131072, 32), (2, 65536, 20), (3, 1001, 100), (9, 4104, 48), (16, 8192, 64),
             (16, 9200, 17), (13, 576, 2000), (4, 128, 5),
             # rows quantised on the way into the product (bf16)
-            (16384, 64, 256), (16385, 128, 512), (16411, 256, 1024), (16400, 1024, 256),
+            (17, 128, 104), (33, 64, 8), (45, 1024, 64), (100, 512, 128), (64, 256, 256),
+            (6144, 520, 896), (16384, 64, 256), (16385, 128, 512), (16411, 256, 1024), (16400, 1024, 256),
             (20000, 72, 72), (17000, 512, 128), (16390, 504, 512), (16999, 240, 2000),
             (16391, 8, 8), (16401, 1024, 64), (16385, 250, 256), (16389, 256, 100)]
 

@@ -156,6 +156,9 @@ def adamw(lib, items, args):
     (dict(wd=float("nan")), {}, "wd"),
     (dict(m=FAKE + 16), {}, "overlap"),
     (dict(v=FAKE + (2 << 20) + 16), {}, "overlap"),
+    (dict(copy=FAKE + 3984), {}, "overlap"),
+    (dict(m_scale=FAKE + (2 << 20) + 996, v_scale=FAKE + (4 << 20)), {}, "overlap"),
+    (dict(m_scale=FAKE + (4 << 20), v_scale=FAKE + (4 << 20) + 12), {}, "overlap"),
     ({}, dict(lr=float("nan")), "lr"),
     ({}, dict(beta1=1.0), "betas"),
     ({}, dict(beta2=-0.1), "betas"),
