@@ -297,12 +297,10 @@ class SandwichStack(BlockStack):
             raise ValueError("post must be \"layer\" or \"rms\"")
         self.post, self.post_eps = post, post_eps
         self.ws_joint = ops.residual_norm_workspace(self.N, self.C, self.dt, self.dev)
-        L = len(self.params)
-        # joint 2 l: after layer l's attention, before its MLP; 2 l + 1: after its MLP,
-        # before the next layer (the last one: nothing after it)
-        self.joints = [self._joint(l, k) for l in range(L) for k in (1, 2)]
 
     def _joint(self, l, k):
+        """Joint 1 of layer l: after its attention, before its MLP; joint 2: after its
+        MLP, before the next layer (the last one: nothing after it)."""
         p = self.params[l]
         pre = (p, "ln2") if k == 1 else (self.params[l + 1], "ln1") if l + 1 < len(self.params) \
             else None
@@ -329,11 +327,11 @@ class SandwichStack(BlockStack):
             c = {}
             y = self._attention(p, c, h, G)
             x1, h2 = self._e(N, C), self._e(N, C)
-            ops.pa_residual_norm(x, y, self.joints[2 * l], x1, h2)
+            ops.pa_residual_norm(x, y, self._joint(l, 1), x1, h2)
             z = self._mlp(p, c, h2)
             last = l + 1 == len(self.params)
             x, h = self._e(N, C), None if last else self._e(N, C)
-            ops.pa_residual_norm(x1, z, self.joints[2 * l + 1], x, h)
+            ops.pa_residual_norm(x1, z, self._joint(l, 2), x, h)
             c.update({"y": y, "x1": x1, "z": z, "x2": x})
             self.caches.append(c)
         return x
@@ -353,7 +351,7 @@ class SandwichStack(BlockStack):
             to, ln = (grads[l], "ln2") if k == 1 else (grads[l + 1], "ln1")
             kw["dpre_g"] = to[f"d{ln}_g"] = self._f(C)
             kw["dpre_b"] = to[f"d{ln}_b"] = self._f(C)
-        ops.pa_residual_norm_backward(x1, y, self.joints[2 * l + k - 1], dx1, dh, dx, dy,
+        ops.pa_residual_norm_backward(x1, y, self._joint(l, k), dx1, dh, dx, dy,
                                       ops.make_residual_norm_grads(**kw), self.ws_joint)
         return dx, dy
 
@@ -381,17 +379,17 @@ class SandwichStack(BlockStack):
             y = self._attention(p, {}, h, G)
             x1, h2 = self._e(N, C), h
             if self.int8 is None:
-                ops.pa_residual_norm(x, y, self.joints[2 * l], x1, h2)
+                ops.pa_residual_norm(x, y, self._joint(l, 1), x1, h2)
                 z = self._mlp(p, {}, h2)
             else:  # the norm writes the MLP's input as integers
                 hq = self.torch.empty(N, ops.padded(C), dtype=self.torch.int8, device=self.dev)
                 hs = self._f(N)
-                ops.pa_residual_norm(x, y, self.joints[2 * l], x1, None, hq=hq, hs=hs)
+                ops.pa_residual_norm(x, y, self._joint(l, 1), x1, None, hq=hq, hs=hs)
                 w1, s1, w2, s2 = self.int8[l]
                 gu, z = self._e(N, 4 * C), y
                 ops.pa_gemm_i8(hq, hs, w1, s1, gu, K=C, bias=p["b1"], act="gelu")
                 ops.pa_linear_i8(gu, w2, s2, z, self.ws_int8, bias=p["b2"])
             last = l + 1 == len(self.params)
             x = self._e(N, C)
-            ops.pa_residual_norm(x1, z, self.joints[2 * l + 1], x, None if last else h)
+            ops.pa_residual_norm(x1, z, self._joint(l, 2), x, None if last else h)
         return x

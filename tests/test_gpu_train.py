@@ -67,6 +67,24 @@ def test_sandwich_joins_as_its_parts(post):
     assert torch.equal(s.infer(x, Gs), out)
 
 
+def test_sandwich_reads_the_parameters_of_the_moment():
+    """A tensor put in a parameter's place after the stack was made."""
+    s, x, Gs, dy = make(500, 64, 16, 2, F32, SandwichStack)
+    fresh, *_ = make(500, 64, 16, 2, F32, SandwichStack, seed=1)
+    for kind in ("rs1", "rs2", "post1_g", "post2_g", "ln1_g", "ln2_b"):
+        for p, q in zip(s.params, fresh.params):
+            p[kind] = q[kind].clone()
+    t = SandwichStack(500, 64, 4, 16, s.params, F32)
+    t.tuned = s.tuned  # (each would choose the products' algorithms by its own timing)
+    assert torch.equal(s.infer(x, Gs), t.infer(x, Gs))
+    assert torch.equal(s.forward(x, Gs), t.forward(x, Gs))
+    for a, b in zip(s.backward(dy), t.backward(dy)):
+        if torch.is_tensor(a):
+            assert torch.equal(a, b)
+        else:
+            assert all(torch.equal(u[k], v[k]) for u, v in zip(a, b) for k in u)
+
+
 @pytest.mark.parametrize("post", ["rms", "layer"])
 def test_sandwich_gradients_against_differences(post):
     """Directional differences of <w, forward> for the input and every parameter.
