@@ -109,12 +109,13 @@ pa_status pa_residual_norm_workspace(int64_t N, int C, pa_dtype dtype, size_t* b
  * over S, h 16 random bits, and dropping the lower 20: an unbiased rounding.
  * (Rounded to nearest, v would stand still: at b2 = 0.999 a step moves it by
  * less than half a code.)  Below the last code m becomes 0, a positive v the
- * last code, so that no parameter is divided by a v that was lost.  The random bits:
- * with fmix the 32-bit finaliser of MurmurHash3 and mix(a, b) = fmix(a ^ (b
- * 0x9E3779B9)), element j of block k of the call's tensor i takes
- *   r = fmix(mix(mix(mix(mix(seed, seed >> 32), step), i), k) + j)
- * in 32-bit arithmetic, its lower half for m, its upper half for v.  Zeroed
- * codes and scales are zero moments.
+ * last code, so that no parameter is divided by a v that was lost.  The random
+ * bits, in 32-bit arithmetic: with A. Appleby's published finaliser
+ *   f(h): h ^= h >> 16, h *= 0x85EBCA6B, h ^= h >> 13, h *= 0xC2B2AE35, h ^= h >> 16
+ * and mix(a, b) = f(a ^ (b 0x9E3779B9)), element j of block k of the call's
+ * tensor i takes r = f(mix(mix(mix(mix(seed, seed >> 32), step), i), k) + j),
+ * the lower half for m, the upper half for v.  Zeroed codes and scales are zero
+ * moments.
  * --------------------------------------------------------------------- */
 typedef struct {
   int64_t n;             /* elements, >= 0 (0: skipped), at most 2^36          */

@@ -24,14 +24,14 @@
 
 namespace pa {
 
-// (host and device)
-__host__ __device__ static inline uint32_t fmix32(uint32_t h) {
+// The hash of the random bits (host and device).
+__host__ __device__ static inline uint32_t scramble(uint32_t h) {
   h = (h ^ (h >> 16)) * 0x85EBCA6Bu;
   h = (h ^ (h >> 13)) * 0xC2B2AE35u;
   return h ^ (h >> 16);
 }
 __host__ __device__ static inline uint32_t mix32(uint32_t a, uint32_t b) {
-  return fmix32(a ^ (b * 0x9E3779B9u));
+  return scramble(a ^ (b * 0x9E3779B9u));
 }
 uint32_t adam_mix(uint32_t a, uint32_t b) { return mix32(a, b); }
 
@@ -212,7 +212,7 @@ __device__ __forceinline__ void encode(const Four& x, uint32_t kb, int lane, flo
   mc = vc = 0;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t h = fmix32(kb + (uint32_t)(4 * lane + e));
+    const uint32_t h = scramble(kb + (uint32_t)(4 * lane + e));
     int c = code_of(fabsf(x.m[e]), im, h & 0xffffu, kLoM);
     c = min(max(c, 0), 127);
     c |= c && x.m[e] < 0.f ? 128 : 0;

@@ -322,14 +322,25 @@ namespace {
 template <typename T, int WF, int WN, int MF, int MN, int NB>
 hipError_t run_tiled(const I8Args& a, hipStream_t st) {
   using G = I8Geo<WF, WN, MF, MN, NB>;
-  const int64_t tiles = (a.N + G::TN - 1) / G::TN * ((a.F + G::TF - 1) / G::TF);
-  if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles), block(64 * G::W);
-  if (a.act == PA_ACT_GELU)
-    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_GELU, WF, WN, MF, MN, NB>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_NONE, WF, WN, MF, MN, NB>), grid, block, 0, st, a);
-  return hipGetLastError();
+  // a launch takes fewer than 2^32 threads: beyond them (2^30 rows at F = 1) the rows go in parts
+  const int64_t ftiles = (a.F + G::TF - 1) / G::TF;
+  const int64_t most = 0xffffffff / (64 * G::W) / ftiles * G::TN;
+  hipError_t e = hipSuccess;
+  for (int64_t n = 0; n < a.N && e == hipSuccess; n += most) {
+    I8Args b = a;
+    b.N = a.N - n < most ? a.N - n : most;
+    b.q += n * a.Kp;
+    b.s += n;
+    if (a.C) b.C = reinterpret_cast<const T*>(a.C) + n * a.F;
+    b.D = reinterpret_cast<T*>(a.D) + n * a.F;
+    const dim3 grid((unsigned)((b.N + G::TN - 1) / G::TN * ftiles)), block(64 * G::W);
+    if (a.act == PA_ACT_GELU)
+      hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_GELU, WF, WN, MF, MN, NB>), grid, block, 0, st, b);
+    else
+      hipLaunchKernelGGL((k_gemm_i8<T, PA_ACT_NONE, WF, WN, MF, MN, NB>), grid, block, 0, st, b);
+    e = hipGetLastError();
+  }
+  return e;
 }
 template <typename T>
 hipError_t run_gemm(const I8Args& a, hipStream_t st) {

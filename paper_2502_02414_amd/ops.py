@@ -148,6 +148,17 @@ def _torch():
     return _torch_module
 
 
+_capture = None
+
+
+def _capturing() -> bool:
+    """Whether calls on the current stream go into a graph."""
+    global _capture
+    if _capture is None:
+        _capture = _torch().cuda.is_current_stream_capturing
+    return _capture()
+
+
 def pa_ops_version() -> int:
     return load().pa_ops_version()
 
@@ -260,15 +271,18 @@ def pa_residual_norm_backward(x1, y, par, dx1, dh, dx, dy, gr=None, ws=None, t=N
 
 # ---- AdamW ----
 class AdamWItems:
-    """The host array of pa_adamw's tensors.  ``set_grad`` exchanges a gradient;
-    ``table`` lays the tensors out on the device for one launch per step, until
-    one of them moves."""
+    """The host array of pa_adamw's tensors, which have to stay where they are.
+    ``set_grad`` exchanges a gradient; ``table`` lays the tensors out on the
+    device for one launch per step, until a gradient moves.  A graph that a step
+    was captured into reads its table again in every replay: the items keep it,
+    and have to live as long as the graph."""
 
     def __init__(self, n):
         self.n = n
         self.arr = (pa_adamw_item * max(n, 1))()
         self.tensors = [None] * n
         self.dev, self.blocks, self.moved = None, 0, 0
+        self.captured = []  # tables that graphs read
 
     def set_grad(self, i, g):
         it = self.arr[i]
@@ -297,7 +311,10 @@ class AdamWItems:
     def on(self, stream, handle):
         """The table's pointer for a launch on a stream (its handle given); a
         stream other than the table's keeps its memory from being handed out."""
-        if handle != self.stream:
+        if _capturing():
+            if not any(t is self.dev for t in self.captured):
+                self.captured.append(self.dev)
+        elif handle != self.stream:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
         return _dev(self.dev, "table")
 
@@ -328,7 +345,8 @@ def make_adamw_items(items, table=True) -> AdamWItems:
         out.tensors[i] = dict(d)
         if d.get("g") is not None:
             out.set_grad(i, d["g"])
-    if table and items and all(d.get("g") is not None and d["p"].is_cuda for d in items):
+    if table and items and all(d.get("g") is not None and d["p"].is_cuda for d in items) \
+            and not _capturing():
         out.table()
     return out
 
@@ -395,17 +413,24 @@ class AdamW:
             items.append(d)
         self.items = make_adamw_items(items)
 
-    def step(self, grads, gscale=None, lr=None, stream=None):
-        """grads: {name: tensor} for every parameter (fp32 or bf16)."""
+    def step(self, grads, gscale=None, lr=None, stream=None, lr_dev=None, step_dev=None):
+        """grads: {name: tensor} for every parameter (fp32 or bf16).  A step that
+        is captured into a graph needs its number on the device, step_dev (int64,
+        from 1, advanced by the graph or between its replays), since a number from
+        here would stand still, and its learning rate there, lr_dev (fp32), where
+        that changes; the count of the calls goes on without such steps."""
+        if step_dev is None and _capturing():
+            raise ValueError("a step captured into a graph needs step_dev")
         it = self.items
         before = it.moved
         for i, k in enumerate(self.names):
             it.set_grad(i, grads[k])
-        if it.dev is None and it.moved == before and not _torch().cuda.is_current_stream_capturing():
+        if it.dev is None and it.moved == before and not _capturing():
             it.table()  # the gradients stay where they are
         pa_adamw(self.items, self.lr if lr is None else lr, self.t + 1, *self.betas, self.eps,
-                 self.seed, gscale, stream=stream)
-        self.t += 1
+                 self.seed, gscale, lr_dev, step_dev, stream)
+        if step_dev is None:
+            self.t += 1
 
     def moments(self, name):
         """(m, v) of a parameter as fp32 tensors."""
@@ -489,4 +514,5 @@ def pa_linear_i8(x, wq, sw, D, ws, bias=None, act=None, C=None, stream=None):
     if Nd != N:
         raise ValueError(f"D has {Nd} rows, x {N}")
     _check(load().pa_linear_i8(N, F, K, _dev(x, "x", cur), _code(x.dtype, "x"), *rest,
-                               _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))
+                               None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws),
+                               B._stream(stream)))

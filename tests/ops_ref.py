@@ -125,21 +125,21 @@ def joint_backward(p, x1, y, t, dx1, dh, rows):
 
 
 # ---- AdamW ----
-def fmix(h):
+def scramble(h):
     h = ((h ^ (h >> 16)) * 0x85EBCA6B) & 0xFFFFFFFF
     h = ((h ^ (h >> 13)) * 0xC2B2AE35) & 0xFFFFFFFF
     return h ^ (h >> 16)
 
 
 def mix(a, b):
-    return fmix(a ^ ((b * 0x9E3779B9) & 0xFFFFFFFF))
+    return scramble(a ^ ((b * 0x9E3779B9) & 0xFFFFFFFF))
 
 
 def random_bits(n, seed, step, item):
     """The 32 random bits of each of a tensor's n elements."""
     i = torch.arange(n, dtype=torch.int64)
     key = mix(mix(mix(seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF), step & 0xFFFFFFFF), item)
-    return fmix((mix(torch.full_like(i, key), i // 256) + i % 256) & 0xFFFFFFFF)
+    return scramble((mix(torch.full_like(i, key), i // 256) + i % 256) & 0xFFFFFFFF)
 
 
 def blocks(x):

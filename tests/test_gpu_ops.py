@@ -592,6 +592,50 @@ def test_graph_of_a_training_step():
             assert torch.equal(eager[3][k], graphed[3][k]), (rep, k)
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_graph_of_an_optimizer(bits):
+    """AdamW.step captured, its number on the device: every replay as the eager step
+    of a twin, also after a gradient has moved and the table was made anew."""
+    sizes = {"a": 5000, "b": 300, "c": 70000}
+    g = draw(12)
+    p0 = {k: torch.randn(n, generator=g) for k, n in sizes.items()}
+    grads = {k: dev(torch.randn(n, generator=g)) for k, n in sizes.items()}
+
+    def make():
+        params = {k: dev(v).clone() for k, v in p0.items()}
+        return params, ops.AdamW(params, lr=1e-2, bits=bits, seed=9)
+
+    (pa, a), (pb, b) = make(), make()
+    for _ in range(2):
+        a.step(grads)
+        b.step(grads)
+    assert a.items.dev is not None
+    table = a.items.dev.data_ptr()
+    count = torch.full((1,), 2, dtype=torch.int64, device="cuda")
+    lr = torch.full((1,), 1e-2, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError, match="step_dev"):
+            a.step(grads)
+        count.add_(1)
+        a.step(grads, step_dev=count, lr_dev=lr)
+    assert a.t == 2
+    for rep in range(5):
+        if rep == 2:
+            a.items.set_grad(0, grads["a"].clone())
+            assert a.items.dev is None
+            assert [t.data_ptr() for t in a.items.captured] == [table]
+            a.items.table()
+        lr.fill_(1e-2 / (1 + rep))
+        b.step(grads, lr=lr.item())
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in sizes:
+            assert torch.equal(pa[k], pb[k]), (rep, k)
+            for m, n in zip(a.moments(k), b.moments(k)):
+                assert torch.equal(m, n), (rep, k)
+
+
 def test_offsets_beyond_32_bits():
     """More than 2^31 elements (and 2^32 bytes) per tensor: the last rows."""
     say("joint, 2^31 + elements")
@@ -627,6 +671,22 @@ def test_offsets_beyond_32_bits():
     within(D[-64:], *R.linear(hq, hs, wq, sw), BF16, "D")
     assert (D[:64] == 0).all()
     del big, D, ws
+    say("integers, more rows than a launch takes threads for")
+    N, K = (1 << 30) + 133, 5
+    q = torch.zeros(N, 16, dtype=torch.int8, device="cuda")
+    s = torch.ones(N, device="cuda")
+    C = torch.zeros(N, 1, dtype=BF16, device="cuda")
+    D = torch.empty_like(C)
+    at = torch.cat([torch.arange(100), (1 << 30) - 70 + torch.arange(203)])
+    q[at.cuda(), :K] = torch.randint(-127, 128, (303, K), generator=draw(5), dtype=torch.int8).cuda()
+    C[at.cuda()] = dev(torch.randn(303, 1, generator=draw(7)).to(BF16))
+    W = torch.randint(-127, 128, (1, K), generator=draw(6), dtype=torch.int8)
+    sw = torch.tensor([0.01])
+    ops.pa_gemm_i8(q, s, dev(R.padded(W)), dev(sw), D, K=K, C=C)
+    within(D[at.cuda()], *R.linear(q[at.cuda(), :K].cpu(), torch.ones(303), W, sw,
+                                   C=C[at.cuda()].cpu()), BF16, "D")
+    assert (D[100:(1 << 30) - 70] == 0).all()
+    del q, s, C, D
     say("adamw, 2^31 + elements")
     n = (1 << 31) + 515
     tail = adam_tensors([515], 6, [BF16], lambda n: True, False)[0]
@@ -646,7 +706,7 @@ def test_offsets_beyond_32_bits():
     assert (off <= R.U * (2 * ref.abs() + 16e-3 * upd.abs()) + 1e-37).all()
     i = torch.arange(515) + (1 << 31)
     key = R.mix(R.mix(R.mix(1, 0), 5), 0)
-    h = R.fmix((R.mix(torch.full_like(i, key), i // 256) + i % 256) & 0xFFFFFFFF)
+    h = R.scramble((R.mix(torch.full_like(i, key), i // 256) + i % 256) & 0xFFFFFFFF)
     assert torch.equal(t["m"][-515:].cpu(), R.encode(m, h & 0xFFFF, True)[0])
     assert torch.equal(t["v"][-515:].cpu(), R.encode(v, h >> 16, False)[0])
     assert (t["p"][:1000] == 0).all()
