@@ -192,8 +192,9 @@ pa_status pa_gemm_i8(int64_t N, int F, int K, const int8_t* q, const float* s, c
                      const float* sw, const float* bias, pa_act act, const void* C, void* D,
                      pa_dtype d_dtype, void* stream);
 
-/* pa_quant_rows into the workspace and pa_gemm_i8: x [N,K] x_dtype.  Few rows
- * are quantised inside the product, in one launch. */
+/* pa_quant_rows and pa_gemm_i8, the rows quantised into the workspace or, where
+ * that is faster, inside of the product, in one launch: x [N,K] x_dtype; ws at
+ * least pa_linear_i8_workspace bytes. */
 pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
                        const int8_t* Wq, const float* sw, const float* bias, pa_act act,
                        const void* C, void* D, pa_dtype d_dtype, void* ws, size_t ws_bytes,

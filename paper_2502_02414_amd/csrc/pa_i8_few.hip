@@ -1,30 +1,51 @@
-// A linear layer in 8-bit integers on up to 16 rows (gfx950): one launch, bound by
-// the weights' way from memory.
+// A linear layer in 8-bit integers on few rows, or where one round of blocks does it
+// (gfx950): one launch, bound by latency and the weights' way from memory.
 //
-// A block of eight waves takes 16 output channels per KW waves, which share the
-// contraction; every wave requests its weights (MFMA operands straight from
-// memory, up to eight steps of 64 in flight) before anything else.  Meanwhile
-// the block quantises all the rows into LDS, each by 512 / (N's next power of
-// two) threads, which find its largest magnitude together.  The waves' integer
-// sums (exact, so their order does not matter) meet in LDS.
+// A block of eight waves takes up to 16 or 32 rows and 16 output channels per KW
+// waves, which share the contraction; every wave requests its weights (MFMA
+// operands straight from memory, up to eight steps of 64 in flight) before anything
+// else.  Meanwhile the block quantises its rows into LDS, each by 512 / (the rows'
+// next power of two) threads, which find its largest magnitude together.  The
+// waves' integer sums (exact, so their order does not matter) meet in LDS.
+//
+// With more rows than 16 every block of channels quantises them again, which costs
+// less than a second launch while all the blocks run at once.  Measured, us, as two
+// launches (quantiser, tiles) and as one: 333 rows of 1000 to 517 fp32 8.3 and
+// 7.6; bf16 32 rows of 1024 to 4096 7.9 and 5.8, 333 of 256 to 517 7.8 and 5.5, 1024
+// of 1024 to 256 8.8 and 6.6, 512 of 4096 to 256 15.4 and 13.2.  One row of 4096 to
+// 4096 5.5 us (16.8 MB of weights, from the last cache in these figures), 16 of 4096
+// to 4096 9.3.
 #include "pa_i8.hpp"
 
 namespace pa {
 namespace {
 
-constexpr int kFewRows = 16, kFewLds = 144 * 1024;
+constexpr int kFewRows = 16;
 
-template <typename TX, typename TD, bool ODD>
-__global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
+// Bytes between rows in LDS: an odd number of 16-byte chunks, so that the 16 rows
+// of an operand read lie in different banks.
+__host__ __device__ constexpr int row_bytes(int Kp) { return Kp % 32 ? Kp : Kp + 16; }
+
+// RT: tiles of 16 rows that a block takes; H: a thread's chunks of a row in flight.
+template <int RT> struct FewGeo {
+  static constexpr int ROWS = kFewRows * RT, H = RT == 1 ? 4 : 8;
+  static constexpr int OWN = 8 * ROWS * 64 + 8 * ROWS + 1024 + 256;  // LDS beside the rows
+};
+
+template <typename TX, typename TD, bool ODD, int RT>
+__global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G, int rows_first) {
   constexpr int E = Row16<TX>::E, U = 8, NOWHERE = 0x7fffff00;
-  extern __shared__ __attribute__((aligned(16))) char xs[];  // [N][Kp + 16]
-  __shared__ int red[8][16][16];
-  __shared__ uint32_t big[kFewRows];
-  __shared__ float ss[kFewRows];
+  constexpr int ROWS = FewGeo<RT>::ROWS, H = FewGeo<RT>::H;
+  extern __shared__ __attribute__((aligned(16))) char xs[];  // [N][RB]
+  __shared__ __attribute__((aligned(16))) int red[8][ROWS][16];
+  __shared__ uint32_t big[ROWS];
+  __shared__ float ss[ROWS], sws[128], bs[128];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
-  const int N = (int)a.N, F = a.F, K = a.K, Kp = a.Kp, RB = Kp + 16;
-  const int FB = 16 * (8 / KW), f0 = blockIdx.x * FB;
+  const int64_t n0 = (int64_t)(rows_first ? blockIdx.x : blockIdx.y) * ROWS;
+  const int N = (int)(a.N - n0 < ROWS ? a.N - n0 : ROWS);  // the block's rows
+  const int F = a.F, K = a.K, Kp = a.Kp, RB = row_bytes(Kp);
+  const int FB = 16 * (8 / KW), f0 = (rows_first ? blockIdx.y : blockIdx.x) * FB;
 
   // the wave's weights: channel f0 + 16 (wave / KW) + r, steps [s0, s1)
   const int steps = (Kp + 63) / 64, per = (steps + KW - 1) / KW;
@@ -42,39 +63,69 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
   for (int j = 0; j < U; ++j) w[j] = weight(s0 + j);
 
   // the rows: G threads each, chunk c of E channels by thread c % G, the first H of
-  // them in registers
-  constexpr int H = 4;
+  // them kept in registers, the others in turns of H
   const int n = tid / G, tg = tid % G, CP = Kp / E;
   const bool mine = n < N;
-  const TX* X = reinterpret_cast<const TX*>(a.x) + (int64_t)(mine ? n : 0) * K;
-  if (tid < kFewRows) big[tid] = 0;
-  Row16<TX> v[H];
+  const TX* X = reinterpret_cast<const TX*>(a.x) + (n0 + (mine ? n : 0)) * K;
+  if (tid < ROWS) big[tid] = 0;
+  if (tid < FB) {
+    const int f = f0 + tid < F ? f0 + tid : F - 1;
+    sws[tid] = a.sw[f];
+    bs[tid] = a.bias ? a.bias[f] : 0.f;
+  }
+  auto fetch = [&](int c0, Row16<TX>(&v)[H]) __attribute__((always_inline)) {
 #pragma unroll
-  for (int j = 0; j < H; ++j) v[j] = row_chunk<ODD>(X, K, tg + j * G);
+    for (int j = 0; j < H; ++j) v[j] = row_chunk<ODD>(X, K, c0 + tg + j * G);
+  };
+  Row16<TX> v[H];
+  fetch(0, v);
   __syncthreads();
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < H; ++j) m = max(m, largest(v[j]));
-  for (int c = tg + H * G; c < CP; c += G) m = max(m, largest(row_chunk<ODD>(X, K, c)));
+  for (int c = H * G; c < CP; c += H * G) {
+    Row16<TX> u[H];
+    fetch(c, u);
+#pragma unroll
+    for (int j = 0; j < H; ++j) m = max(m, largest(u[j]));
+  }
   if (mine) atomicMax(&big[n], m);
   __syncthreads();
   if (mine) {
     const QuantScale q = quant_scale(big[n]);
     int8_t* row = reinterpret_cast<int8_t*>(xs) + n * RB;
+    auto put = [&](int c0, const Row16<TX>(&v)[H]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < H; ++j)
-      if (tg + j * G < CP) put_chunk(row + E * (tg + j * G), v[j], q.inv);
-    for (int c = tg + H * G; c < CP; c += G) put_chunk(row + E * c, row_chunk<ODD>(X, K, c), q.inv);
+      for (int j = 0; j < H; ++j) {
+        const int c = c0 + tg + j * G;
+        if (c < CP) put_chunk(row + E * c, v[j], q.inv);
+      }
+    };
+    put(0, v);
+    for (int c = H * G; c < CP; c += H * G) {
+      Row16<TX> u[H];
+      fetch(c, u);
+      put(c, u);
+    }
     if (tg == 0) ss[n] = q.s;
   }
   __syncthreads();
 
-  i32x4 acc = {0, 0, 0, 0};
-  const char* xr = xs + (r < N ? r : N - 1) * RB;  // (columns past N are not used)
+  i32x4 acc[RT];
+  const char* xr[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    acc[t] = i32x4{0, 0, 0, 0};
+    const int p = 16 * t + r;  // (columns past N are not used)
+    xr[t] = xs + (p < N ? p : N - 1) * RB;
+  }
   auto product = [&](int s, i32x4 ws) {
-    const int k = 64 * s + 16 * g;  // (behind a row's end the weights are zeros)
-    const i32x4 x = *reinterpret_cast<const i32x4*>(xr + (k < Kp ? k : Kp - 16));
-    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(ws, x, acc, 0, 0, 0);
+    const int k = 64 * s + 16 * g, at = k < Kp ? k : Kp - 16;  // (behind a row's end the weights are zeros)
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const i32x4 x = *reinterpret_cast<const i32x4*>(xr[t] + at);
+      acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(ws, x, acc[t], 0, 0, 0);
+    }
   };
 #pragma unroll
   for (int j = 0; j < U; ++j) product(s0 + j, w[j]);
@@ -84,46 +135,78 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G) {
 #pragma unroll
     for (int j = 0; j < U; ++j) product(s + j, w[j]);
   }
-  *reinterpret_cast<i32x4*>(&red[wave][r][4 * g]) = acc;
+#pragma unroll
+  for (int t = 0; t < RT; ++t) *reinterpret_cast<i32x4*>(&red[wave][16 * t + r][4 * g]) = acc[t];
   __syncthreads();
   for (int t = tid; t < N * FB; t += 512) {
     const int p = t / FB, fl = t % FB, f = f0 + fl;
     if (f >= F) continue;
     int sum = 0;
     for (int k = 0; k < KW; ++k) sum += red[fl / 16 * KW + k][p][fl % 16];
-    float u = fmaf((float)sum, ss[p] * a.sw[f], a.bias ? a.bias[f] : 0.f);
+    float u = fmaf((float)sum, ss[p] * sws[fl], bs[fl]);
     if (a.act == PA_ACT_GELU) u = gelu_for<TD>(u);
-    const int64_t at = (int64_t)p * F + f;
+    const int64_t at = (n0 + p) * F + f;
     if (a.C) u += to_f<TD>(reinterpret_cast<const TD*>(a.C)[at]);
     reinterpret_cast<TD*>(a.D)[at] = from_f<TD>(u);
   }
 }
 
-template <typename TX, typename TD>
+// The waves that share a contraction; 0: not served.  Beyond 16 rows: as many as let
+// all the blocks run at once (a block takes a CU), if each wave's weights fit its
+// registers; and rows short enough to be read again by every block of channels (us,
+// two launches and one: bf16 32 rows of 4096 to 1024 13.7 and 12.2; fp32 of 2048 to
+// 1024 9.4 and 10.0, of 4096 13.9 and 15.8), longer than 2 KB only where few
+// channels to a block make up for it (fp32 512 rows of 1024 to 1024 8.2 and, at KW =
+// 2, 8.6).
+template <int RT> int few_split(int64_t N, int F, int K, int x_dtype) {
+  constexpr int ROWS = FewGeo<RT>::ROWS;
+  const int Kp = (K + 15) / 16 * 16, steps = (Kp + 63) / 64;
+  const int64_t rows = N < ROWS ? N : ROWS, nb = (N + ROWS - 1) / ROWS;
+  if (rows * row_bytes(Kp) + FewGeo<RT>::OWN > 160 * 1024) return 0;
+  int KW = 8;
+  // (waves without a step cost nothing while there are CUs for the blocks)
+  while (KW && nb * ((F + 128 / KW - 1) / (128 / KW)) > 256 && (RT == 2 || KW > steps)) KW /= 2;
+  if (RT == 1) return KW;
+  const int bytes = x_dtype == 1 ? 2 * K : 4 * K;
+  return 8 * KW < steps || bytes > (x_dtype == 1 ? 8192 : 4096) || (bytes > 2048 && KW < 4) ? 0 : KW;
+}
+
+template <typename TX, typename TD, int RT>
 hipError_t run(const I8Args& a, hipStream_t st) {
-  const int steps = (a.Kp + 63) / 64;
-  int KW = 1, NP = 1;
-  while (KW < 8 && 2 * KW <= steps) KW *= 2;
-  while (NP < a.N) NP *= 2;
-  const int FB = 16 * (8 / KW);
-  const size_t lds = (size_t)a.N * (a.Kp + 16);
-  const dim3 grid((a.F + FB - 1) / FB), block(512);
+  constexpr int ROWS = FewGeo<RT>::ROWS;
+  const int rows = a.N < ROWS ? (int)a.N : ROWS, KW = few_split<RT>(a.N, a.F, a.K, a.x_dtype);
+  if (!KW) return hipErrorInvalidValue;
+  int NP = 1;
+  while (NP < rows) NP *= 2;
+  const int FB = 128 / KW;
+  const size_t lds = (size_t)rows * row_bytes(a.Kp);
+  // Blocks are dealt to the XCDs round robin: those with the larger operand in common
+  // a multiple of the other count apart, in one L2.
+  const unsigned nf = (a.F + FB - 1) / FB, nb = (unsigned)((a.N + ROWS - 1) / ROWS);
+  const int rows_first = a.N * (int64_t)sizeof(TX) > a.F && nf <= 65535;
+  const dim3 grid(rows_first ? nb : nf, rows_first ? nf : nb), block(512);
   if (a.K % Row16<TX>::E)
-    hipLaunchKernelGGL((k_linear_few<TX, TD, true>), grid, block, lds, st, a, KW, 512 / NP);
+    hipLaunchKernelGGL((k_linear_few<TX, TD, true, RT>), grid, block, lds, st, a, KW, 512 / NP,
+                       rows_first);
   else
-    hipLaunchKernelGGL((k_linear_few<TX, TD, false>), grid, block, lds, st, a, KW, 512 / NP);
+    hipLaunchKernelGGL((k_linear_few<TX, TD, false, RT>), grid, block, lds, st, a, KW, 512 / NP,
+                       rows_first);
   return hipGetLastError();
+}
+template <typename TX, typename TD>
+hipError_t by_rows(const I8Args& a, hipStream_t st) {
+  return a.N <= kFewRows ? run<TX, TD, 1>(a, st) : run<TX, TD, 2>(a, st);
 }
 
 }  // namespace
 
-bool linear_i8_few(int64_t N, int K) {
-  return N <= kFewRows && N * ((K + 15) / 16 * 16 + 16) <= kFewLds;
+bool linear_i8_few(int64_t N, int F, int K, int x_dtype) {
+  return (N <= kFewRows ? few_split<1>(N, F, K, x_dtype) : few_split<2>(N, F, K, x_dtype)) > 0;
 }
 
 hipError_t launch_linear_few(const I8Args& a, int d_dtype, hipStream_t st) {
-  if (a.x_dtype == 1) return d_dtype == 1 ? run<bf16, bf16>(a, st) : run<bf16, float>(a, st);
-  return d_dtype == 1 ? run<float, bf16>(a, st) : run<float, float>(a, st);
+  if (a.x_dtype == 1) return d_dtype == 1 ? by_rows<bf16, bf16>(a, st) : by_rows<bf16, float>(a, st);
+  return d_dtype == 1 ? by_rows<float, bf16>(a, st) : by_rows<float, float>(a, st);
 }
 
 }  // namespace pa

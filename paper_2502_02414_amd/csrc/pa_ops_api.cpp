@@ -430,18 +430,23 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   PO_TRY(need(who, x, "x"));
   a.x = x;
   a.x_dtype = x_dtype;
-  if (pa::linear_i8_few(N, K)) {
-    PO_HIP(pa::launch_linear_few(a, d_dtype, as_stream(stream)), who);
-    return PA_OK;
-  }
-  if (x_dtype == PA_BF16 && d_dtype == PA_BF16 && K % 8 == 0 && pa::linear_i8_fused(N, F, K)) {
-    PO_HIP(pa::launch_linear_i8(a, as_stream(stream)), who);
-    return PA_OK;
-  }
+  // (asked for whether the kernel of these sizes uses it or not)
   const size_t rows = (size_t)N * a.Kp;
   if (!ws || ws_bytes < rows + (size_t)N * 4)
     return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, rows + (size_t)N * 4);
   PO_TRY(opt(who, ws, "ws"));
+  const bool fused =
+      x_dtype == PA_BF16 && d_dtype == PA_BF16 && K % 8 == 0 && pa::linear_i8_fused(N, F, K);
+  // (of both, for weights of at most 64 KiB and 512 inputs the one-pass product is as
+  // fast or faster: us at 333 rows, 256 to 128 4.3 and 5.2, 512 to 128 5.9 and 5.0)
+  if (pa::linear_i8_few(N, F, K, x_dtype) && (N <= 16 || !fused || K > 512 || K * F > 65536)) {
+    PO_HIP(pa::launch_linear_few(a, d_dtype, as_stream(stream)), who);
+    return PA_OK;
+  }
+  if (fused) {
+    PO_HIP(pa::launch_linear_i8(a, as_stream(stream)), who);
+    return PA_OK;
+  }
   int8_t* q = reinterpret_cast<int8_t*>(ws);
   float* s = reinterpret_cast<float*>(q + rows);
   PO_HIP(pa::launch_quant_rows(N, K, x_dtype, x, q, s, as_stream(stream)), who);

@@ -97,8 +97,8 @@ hipError_t launch_gemm_i8(const I8Args& a, int d_dtype, hipStream_t st);
 // than the tiles.
 bool linear_i8_fused(int64_t N, int F, int K);
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st);
-// Few rows (pa_i8_few.hip): served.
-bool linear_i8_few(int64_t N, int K);
+// Few rows, or few blocks (pa_i8_few.hip): served.
+bool linear_i8_few(int64_t N, int F, int K, int x_dtype);
 hipError_t launch_linear_few(const I8Args& a, int d_dtype, hipStream_t st);
 hipError_t launch_quant_rows(int64_t N, int K, int dtype, const void* x, int8_t* q, float* s,
                              hipStream_t st);
