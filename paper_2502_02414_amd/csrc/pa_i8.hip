@@ -238,8 +238,11 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
 // read once: rows of up to 64 chunks are shared by the smallest power of two of
 // lanes, U rows each in turn with all their loads first; longer ones take a wave
 // and NC chunks per lane.  Bound by memory: 4096 rows of 4096 bf16 9.7 us (5.2
-// TB/s), a million of 256 147 us (5.2 TB/s); rows of odd lengths at 2.3 to 3 TB/s
-// (unaligned loads touch more lines, and the shifts of a cut chunk).  Rows beyond 1024 chunks take a block and are read twice.
+// TB/s), a million of 256 147 us (5.2 TB/s); unaligned rows touch more lines:
+// 100,000 of 257 23 us where 256 take 17, 50,000 of 1001 fp32 38 us.  (With the shift
+// of a cut chunk on the row's elements, for every chunk, in place of one on its
+// integers those took 20 to 60% longer.)  Rows beyond 1024 chunks take a block and
+// are read twice.
 // ---------------------------------------------------------------------------
 template <typename T, bool ODD, int NC, int U>
 __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, int L, const T* x,
@@ -267,9 +270,30 @@ __global__ void __launch_bounds__(256) k_quant_rows(int64_t N, int K, int Kp, in
       if (n >= N) continue;
 #pragma unroll
       for (int j = 0; j < NC; ++j)
-        if (c0 + j * L < CP) put_chunk(q + n * Kp + E * (c0 + j * L), v[u][j], c.inv);
+        if (c0 + j * L < CP)
+          put_chunk<ODD>(q + n * Kp + E * (c0 + j * L), v[u][j], c.inv, K, c0 + j * L);
       if (c0 == 0) s[n] = c.s;
     }
+  }
+}
+
+// Rows shorter than a chunk: a row per thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_quant_short(int64_t N, int K, const T* x, int8_t* q,
+                                                     float* s) {
+  const int64_t step = (int64_t)gridDim.x * 256;
+  for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < N; n += step) {
+    float v[8];
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = e < K ? to_f<T>(x[n * K + e]) : 0.f;
+      big = max(big, __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu);
+    }
+    const QuantScale c = quant_scale(big);
+    *reinterpret_cast<uint4*>(q + n * 16) = {quant4(v[0], v[1], v[2], v[3], c.inv),
+                                             quant4(v[4], v[5], v[6], v[7], c.inv), 0u, 0u};
+    s[n] = c.s;
   }
 }
 
@@ -289,7 +313,7 @@ __global__ void __launch_bounds__(512) k_quant_long(int64_t N, int K, int Kp, co
     for (int w = 0; w < 8; ++w) big = max(big, red[w]);
     const QuantScale k = quant_scale(big);
     for (int c = threadIdx.x; c < CP; c += 512)
-      put_chunk(q + n * Kp + E * c, row_chunk<ODD>(x + n * K, K, c), k.inv);
+      put_chunk<ODD>(q + n * Kp + E * c, row_chunk<ODD>(x + n * K, K, c), k.inv, K, c);
     if (threadIdx.x == 0) s[n] = k.s;
   }
 }
@@ -390,6 +414,12 @@ hipError_t run_quant(int64_t N, int K, const T* x, int8_t* q, float* s, hipStrea
 template <typename T>
 hipError_t run_quant(int64_t N, int K, const void* x, int8_t* q, float* s, hipStream_t st) {
   const T* p = reinterpret_cast<const T*>(x);
+  if (K < Row16<T>::E) {
+    const int64_t need = (N + 255) / 256;
+    hipLaunchKernelGGL(k_quant_short<T>, dim3((unsigned)(need < 4096 ? need : 4096)), dim3(256), 0, st,
+                       N, K, p, q, s);
+    return hipGetLastError();
+  }
   return K % Row16<T>::E ? run_quant<T, true>(N, K, p, q, s, st) : run_quant<T, false>(N, K, p, q, s, st);
 }
 }  // namespace

@@ -42,10 +42,10 @@ template <typename T> struct Row16 {
   static constexpr int E = 16 / (int)sizeof(T);
   T v[E];
 };
-// Chunk c of a row of K elements, zeros behind its end, without a branch around
-// the load (which would be waited for at once).  ODD: K is no multiple of E and
-// rows start anywhere; the chunk that is cut short is the row's last E elements
-// shifted down.  K < E: element by element.
+// Chunk c of a row of K elements, without a branch around the load (which would be
+// waited for at once).  ODD: K, at least E, is no multiple of E and rows start
+// anywhere; of a chunk that is cut short, or lies behind the row's end, the row's
+// last E elements (put_chunk moves them).  Otherwise zeros behind the end.
 template <bool ODD, typename T>
 __device__ __forceinline__ Row16<T> row_chunk(const T* row, int K, int c) {
   constexpr int E = Row16<T>::E;
@@ -55,20 +55,7 @@ __device__ __forceinline__ Row16<T> row_chunk(const T* row, int K, int c) {
     const uint4 q = *reinterpret_cast<const uint4*>(row + (in ? E * c : 0));
     return __builtin_bit_cast(Row16<T>, in ? q : uint4{0, 0, 0, 0});
   } else {
-    if (K < E) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) o.v[e] = E * c + e < K ? row[E * c + e] : from_f<T>(0.f);
-      return o;
-    }
-    const int start = E * c + E <= K ? E * c : K - E;
-    uint64_t w[2];
-    __builtin_memcpy(w, row + start, 16);
-    const int s = (E * c - start) * 8 * (int)sizeof(T);  // bits behind the end, 0 .. 128 and more
-    const uint64_t lo = s >= 128 ? 0 : s >= 64 ? w[1] >> (s - 64) : s ? w[0] >> s | w[1] << (64 - s) : w[0];
-    const uint64_t hi = s >= 64 ? 0 : w[1] >> s;
-    w[0] = lo;
-    w[1] = hi;
-    __builtin_memcpy(&o, w, 16);
+    __builtin_memcpy(&o, row + (E * c + E <= K ? E * c : K - E), 16);
     return o;
   }
 }
@@ -100,15 +87,20 @@ __device__ __forceinline__ uint32_t row16_max(uint32_t v) {
   step(std::integral_constant<int, kMirror>{});
   return v;
 }
-template <typename T>
-__device__ __forceinline__ void put_chunk(int8_t* q, const Row16<T>& x, float inv) {
+// Chunk c in integers, at q.  ODD: of the row's last E elements those that belong
+// there, in place, and zeros.
+template <bool ODD, typename T>
+__device__ __forceinline__ void put_chunk(int8_t* q, const Row16<T>& x, float inv, int K, int c) {
   constexpr int E = Row16<T>::E;
-  uint32_t w[E / 4];
-#pragma unroll
-  for (int e = 0; e < E; e += 4)
-    w[e / 4] = quant4(to_f<T>(x.v[e]), to_f<T>(x.v[e + 1]), to_f<T>(x.v[e + 2]),
-                      to_f<T>(x.v[e + 3]), inv);
-  __builtin_memcpy(__builtin_assume_aligned(q, E), w, E);
+  typedef typename std::conditional<E == 8, uint64_t, uint32_t>::type W;
+  W w = quant4(to_f<T>(x.v[0]), to_f<T>(x.v[1]), to_f<T>(x.v[2]), to_f<T>(x.v[3]), inv);
+  if constexpr (E == 8)
+    w |= (W)quant4(to_f<T>(x.v[4]), to_f<T>(x.v[5]), to_f<T>(x.v[6]), to_f<T>(x.v[7]), inv) << 32;
+  if constexpr (ODD) {
+    const int over = E * c + E - K;  // elements behind the end
+    w = over >= E ? 0 : over > 0 ? w >> 8 * over : w;
+  }
+  *reinterpret_cast<W*>(q) = w;
 }
 
 }  // namespace pa

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G, int
 #pragma unroll
       for (int j = 0; j < H; ++j) {
         const int c = c0 + tg + j * G;
-        if (c < CP) put_chunk(row + E * c, v[j], q.inv);
+        if (c < CP) put_chunk<ODD>(row + E * c, v[j], q.inv, K, c);
       }
     };
     put(0, v);
@@ -155,20 +155,21 @@ __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G, int
 // all the blocks run at once (a block takes a CU), if each wave's weights fit its
 // registers; and rows short enough to be read again by every block of channels (us,
 // two launches and one: bf16 32 rows of 4096 to 1024 13.7 and 12.2; fp32 of 2048 to
-// 1024 9.4 and 10.0, of 4096 13.9 and 15.8), longer than 2 KB only where few
+// 1024 9.4 and 10.0, of 4096 13.9 and 15.8; bf16 128 of 3695, whose rows are not aligned, to
+// 1500 14.8 and 16.5), longer than 2 KB only where few
 // channels to a block make up for it (fp32 512 rows of 1024 to 1024 8.2 and, at KW =
 // 2, 8.6).
 template <int RT> int few_split(int64_t N, int F, int K, int x_dtype) {
   constexpr int ROWS = FewGeo<RT>::ROWS;
-  const int Kp = (K + 15) / 16 * 16, steps = (Kp + 63) / 64;
+  const int Kp = (K + 15) / 16 * 16, steps = (Kp + 63) / 64, E = x_dtype == 1 ? 8 : 4;
   const int64_t rows = N < ROWS ? N : ROWS, nb = (N + ROWS - 1) / ROWS;
-  if (rows * row_bytes(Kp) + FewGeo<RT>::OWN > 160 * 1024) return 0;
+  if (K < E || rows * row_bytes(Kp) + FewGeo<RT>::OWN > 160 * 1024) return 0;
   int KW = 8;
   // (waves without a step cost nothing while there are CUs for the blocks)
   while (KW && nb * ((F + 128 / KW - 1) / (128 / KW)) > 256 && (RT == 2 || KW > steps)) KW /= 2;
   if (RT == 1) return KW;
   const int bytes = x_dtype == 1 ? 2 * K : 4 * K;
-  return 8 * KW < steps || bytes > (x_dtype == 1 ? 8192 : 4096) || (bytes > 2048 && KW < 4) ? 0 : KW;
+  return 8 * KW < steps || bytes > (x_dtype == 1 && K % 8 == 0 ? 8192 : 4096) || (bytes > 2048 && KW < 4) ? 0 : KW;
 }
 
 template <typename TX, typename TD, int RT>

@@ -121,8 +121,8 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
 #pragma unroll
       for (int j = 0; j < G::NC; ++j) {
         if (8 * (c0 + 16 * j) < G::RB)
-          put_chunk(reinterpret_cast<int8_t*>(xs[buf] + put + 128 * j),
-                    __builtin_bit_cast(Row16<bf16>, xr[j]), q.inv);
+          put_chunk<false>(reinterpret_cast<int8_t*>(xs[buf] + put + 128 * j),
+                           __builtin_bit_cast(Row16<bf16>, xr[j]), q.inv, 0, 0);
         if (G::NC > 2) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
       }
       if (c0 == 0) ss[buf][row] = q.s;
