@@ -184,8 +184,11 @@ pa_status pa_residual_norm_backward(int64_t N, int C, pa_dtype dtype,
   a.y = y; a.t = t; a.x1 = const_cast<void*>(x1);
   a.dx1 = dx1; a.dh = dh; a.dx = dx; a.dy = dy; a.dt = dt;
   a.partials = sums ? reinterpret_cast<float*>(ws) : nullptr;
+  if (sums && P == 1) {  // (nothing to add to the only block's sums)
+    a.g0 = seg.dst[0]; a.g1 = seg.dst[1]; a.g2 = seg.dst[2]; a.g3 = seg.dst[3]; a.g4 = seg.dst[4];
+  }
   PO_HIP(pa::launch_resnorm(a, dtype, true, as_stream(stream)), who);
-  if (sums) PO_HIP(pa::launch_reduce(a.partials, P, 5 * C, seg, as_stream(stream)), who);
+  if (sums && P > 1) PO_HIP(pa::launch_reduce(a.partials, P, 5 * C, seg, as_stream(stream)), who);
   return PA_OK;
 }
 

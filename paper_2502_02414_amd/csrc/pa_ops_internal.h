@@ -25,6 +25,8 @@ struct ResNormArgs {
   const void *dx1 = nullptr, *dh = nullptr;
   void *dx = nullptr, *dy = nullptr, *dt = nullptr;
   float* partials = nullptr;  // resnorm_blocks records [5][C], nullable
+  // one block: the gradients that the record is for, in its place, each nullable
+  float *g0 = nullptr, *g1 = nullptr, *g2 = nullptr, *g3 = nullptr, *g4 = nullptr;
 };
 int resnorm_blocks(int64_t N, int C, int dtype, bool bwd);
 hipError_t launch_resnorm(const ResNormArgs& a, int dtype, bool bwd, hipStream_t st);

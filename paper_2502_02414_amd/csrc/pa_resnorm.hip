@@ -443,14 +443,22 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
     }
   }
   if (!a.partials) return;
-  // the block's record [5][C]: its rows added in order
+  // the block's record [5][C]: its rows added in order; of the only block, the gradients
   float* rec = a.partials + (int64_t)blockIdx.x * 5 * a.C;
+  const bool only = gridDim.x == 1;
+  auto place_of = [&](int k) {
+    if (!only) return rec + k * a.C;
+    return k == 0 ? a.g0 : k == 1 ? a.g1 : k == 2 ? a.g2 : k == 3 ? a.g3 : a.g4;
+  };
   if constexpr (WIDE) {
     if (on)
 #pragma unroll
-      for (int k = 0; k < 5; ++k)
+      for (int k = 0; k < 5; ++k) {
+        float* to = place_of(k);
+        if (to)
 #pragma unroll
-        for (int e = 0; e < E; ++e) rec[k * a.C + c + e] = acc[k][e];
+          for (int e = 0; e < E; ++e) to[c + e] = acc[k][e];
+      }
   } else {
     const int C5 = 5 * a.C;
     if (on)
@@ -462,7 +470,9 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
     for (int i = threadIdx.x; i < C5; i += blockDim.x) {
       float s = 0.f;
       for (int r = 0; r < rows; ++r) s += fold[r * C5 + i];
-      rec[i] = s;
+      const int k = i / a.C;
+      float* to = place_of(k);
+      if (to) to[i - k * a.C] = s;
     }
   }
 }
@@ -489,6 +499,11 @@ int resnorm_blocks(int64_t N, int C, int dtype, bool bwd) {
   const ResNormGeo g = geo(C, dtype);
   const int turn = g.rows * (bwd || g.wide ? 1 : 2);
   const int64_t need = (N + turn - 1) / turn;
+  // (backward: up to two turns in one block, which writes the parameters' gradients
+  // itself; us, two turns in one block and in two with the sum of their records: 64
+  // rows of 64 bf16 9.1 and 10.0, 16 of 256 9.8 and 10.5, 8 of 256 fp32 8.9 and 9.8;
+  // four turns 14.5 and 10.6)
+  if (bwd && need <= 2) return 1;
   // (backward: three blocks per CU, what its registers allow, in one round; 1024
   // blocks took 934 us where these take 793, at N = 1,000,000, C = 256)
   const int waves = g.threads / 64;

@@ -76,6 +76,11 @@ JOINTS = [
     (300, 520, "layer", "layer", "sigmoid", 1.0, True),
     (129, 1000, "rms", "rms", "linear", 0.5, True),
     (65, 4096, "layer", "layer", "sigmoid", 1.0, True),
+    # one block in the backward, of one or two turns
+    (13, 256, "layer", "layer", "sigmoid", 1.0, True),
+    (61, 64, "rms", "layer", None, 0.5, True),
+    (2, 2048, "layer", "rms", "linear", 1.0, True),
+    (200, 16, "layer", "layer", "sigmoid", 1.0, True),
 ]
 
 
@@ -140,6 +145,31 @@ def test_joint_backward(dt, N, C, post, pre, gated, alpha, full, use):
             assert (gr[k] == 7).all()
         elif k.startswith("dpre") and dh is None:
             assert (gr[k] == 0).all()
+
+
+@pytest.mark.parametrize("N,C", [(5, 64), (1, 1032), (600, 64)])
+def test_joint_backward_gives_only_the_gradients_asked_for(N, C):
+    """Each of the parameters' gradients alone is the one that all of them give."""
+    p, d = joint_case(N, C, BF16, "layer", "layer", "sigmoid", 1.0, True)
+    a = [dev(d[k]) for k in ("x", "y")]
+    kw = {"t": dev(d["t"]), "ws": ops.residual_norm_workspace(N, C, BF16)}
+    names = ("dpost_g", "dpost_b", "dscale", "dpre_g", "dpre_b")
+
+    def run(gr):
+        o = [torch.empty_like(a[0]) for _ in range(3)]
+        ops.pa_residual_norm_backward(*a, params(p), dev(d["dx1"]), dev(d["dh"]), o[0], o[1],
+                                      ops.make_residual_norm_grads(**gr) if gr is not None else None,
+                                      dt=o[2], **kw)
+        return o
+
+    every = {k: torch.empty(C, device="cuda") for k in names}
+    outs = run(every)
+    for k in names:
+        one = {k: torch.empty(C, device="cuda")}
+        assert all(torch.equal(x, y) for x, y in zip(run(one), outs))
+        assert torch.equal(one[k], every[k]), k
+    kw["ws"] = None
+    assert all(torch.equal(x, y) for x, y in zip(run(None), outs))
 
 
 def test_joint_gradient_against_differences():
