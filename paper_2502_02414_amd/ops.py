@@ -130,6 +130,8 @@ def _in(t, n, dtype, name, required=True, cur=None):
         if required:
             raise ValueError(f"{name} is required")
         return None
+    if t.get_device() == cur and t.dtype == dtype and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
     if t.numel() != n:
@@ -217,9 +219,10 @@ def _joint(x, name, par, gr=None):
     if x.dim() != 2:
         raise ValueError(f"{name} must be [N, C]")
     N, C = x.shape
-    for s in (par, gr):
-        if s is not None and s.C is not None and s.C != C:
-            raise ValueError(f"{name} has {C} channels, the parameters {s.C}")
+    if par.C is not None and par.C != C:
+        raise ValueError(f"{name} has {C} channels, the parameters {par.C}")
+    if gr is not None and gr.C is not None and gr.C != C:
+        raise ValueError(f"{name} has {C} channels, the gradients {gr.C}")
     return N, C, N * C, _code(x.dtype, name)
 
 
@@ -242,8 +245,8 @@ def pa_residual_norm(x, y, par, x1, h=None, t=None, hq=None, hs=None, stream=Non
     cur = _current_device()
     _check(load().pa_residual_norm(
         N, C, code, par.ref, _dev(x, "x", cur), _in(y, n, dt, "y", True, cur),
-        _in(t, n, dt, "t", False, cur), _in(x1, n, dt, "x1", True, cur),
-        _in(h, n, dt, "h", False, cur), hqp, hsp, B._stream(stream)))
+        None if t is None else _in(t, n, dt, "t", True, cur), _in(x1, n, dt, "x1", True, cur),
+        None if h is None else _in(h, n, dt, "h", True, cur), hqp, hsp, B._stream(stream)))
 
 
 def residual_norm_workspace(N, C, dtype, device="cuda"):
@@ -307,16 +310,19 @@ class AdamWItems:
         dev = host.to("cuda")
         torch.cuda.current_stream().synchronize()
         self.dev, self.blocks, self.stream = dev, blocks.value, B._stream()
+        self.ptr, self.device = dev.data_ptr(), dev.get_device()
 
     def on(self, stream, handle):
         """The table's pointer for a launch on a stream (its handle given); a
         stream other than the table's keeps its memory from being handed out."""
-        if _capturing():
+        if _current_device() != self.device:
+            raise ValueError(f"items: on device {self.device}, not on the current one")
+        if handle and _capturing():  # (the default stream cannot be captured)
             if not any(t is self.dev for t in self.captured):
                 self.captured.append(self.dev)
         elif handle != self.stream:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
-        return _dev(self.dev, "table")
+        return self.ptr
 
 
 def make_adamw_items(items, table=True) -> AdamWItems:
@@ -476,17 +482,19 @@ def quant_weight(W):
 
 
 def _product(K, wq, sw, D, bias, act, C):
-    torch = _torch()
+    torch = _torch_module or _torch()
     if D.dim() != 2:
         raise ValueError("D must be [N, F]")
-    if act not in ACTS:
+    a = ACTS.get(act)
+    if a is None:
         raise ValueError(f"act: {act!r} is not one of {sorted(map(str, ACTS))}")
     N, F = D.shape
-    f32, cur = torch.float32, _current_device()
-    return (N, F, cur, (_in(wq, F * padded(K), torch.int8, "Wq", True, cur),
-                        _in(sw, F, f32, "sw", True, cur), _in(bias, F, f32, "bias", False, cur),
-                        ACTS[act], _in(C, N * F, D.dtype, "C", False, cur), _dev(D, "D", cur),
-                        _code(D.dtype, "D")))
+    f32, cur, dt = torch.float32, _current_device(), D.dtype
+    return (N, F, cur, (_in(wq, F * ((K + 15) // 16 * 16), torch.int8, "Wq", True, cur),
+                        _in(sw, F, f32, "sw", True, cur),
+                        None if bias is None else _in(bias, F, f32, "bias", True, cur), a,
+                        None if C is None else _in(C, N * F, dt, "C", True, cur),
+                        _dev(D, "D", cur), _code(dt, "D")))
 
 
 def pa_gemm_i8(q, s, wq, sw, D, K=None, bias=None, act=None, C=None, stream=None):
