@@ -71,6 +71,19 @@ __device__ __forceinline__ void results(const I8Args& a, const i32x4 (&acc)[MF][
   typedef T TV __attribute__((ext_vector_type(V)));
   T* D = reinterpret_cast<T*>(a.D);
   const T* Cr = reinterpret_cast<const T*>(a.C);
+  // Residuals of MN runs are requested together, the next ones before these are worked
+  // on.  (From the start of C where there is no whole run.)
+  const bool some = Cr && a.N * a.F >= V;
+  auto residuals = [&](int i, TV(&c)[MN]) __attribute__((always_inline)) {
+    const int f = f1 + (sizeof(T) == 2 ? 16 * i + 8 * g : 16 * i + 4 * g);
+#pragma unroll
+    for (int j = 0; j < MN; ++j) {
+      const int64_t n = n1 + 16 * j;
+      __builtin_memcpy(&c[j], Cr + (n < a.N && f + V <= a.F ? n * a.F + f : 0), 16);
+    }
+  };
+  TV c[2][MN];
+  if (some) residuals(0, c[0]);
   float sn[MN];
 #pragma unroll
   for (int j = 0; j < MN; ++j) sn[j] = a.s[n1 + 16 * j < a.N ? n1 + 16 * j : a.N - 1];
@@ -84,6 +97,7 @@ __device__ __forceinline__ void results(const I8Args& a, const i32x4 (&acc)[MF][
       sw[e] = a.sw[fe];
       b[e] = a.bias ? a.bias[fe] : 0.f;
     }
+    if (some && i + RUN < MF) residuals(i + RUN, c[(i / RUN + 1) & 1]);
 #pragma unroll
     for (int j = 0; j < MN; ++j) {
       const int64_t n = n1 + 16 * j, at = n * a.F + f;
@@ -95,10 +109,8 @@ __device__ __forceinline__ void results(const I8Args& a, const i32x4 (&acc)[MF][
       }
       if (n < a.N && f + V <= a.F) {
         if (Cr) {
-          TV c;
-          __builtin_memcpy(&c, Cr + at, 16);
 #pragma unroll
-          for (int e = 0; e < V; ++e) u[e] += (float)c[e];
+          for (int e = 0; e < V; ++e) u[e] += (float)c[(i / RUN) & 1][j][e];
         }
         TV o;
 #pragma unroll
@@ -125,10 +137,18 @@ __global__ void __launch_bounds__(64 * WF * WN, 2) k_gemm_i8(I8Args a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const int wf = wave % WF, wn = wave / WF;
-  const int ftiles = (a.F + G::TF - 1) / G::TF;
-  const int64_t tile = blockIdx.x;
-  const int64_t n0 = tile / ftiles * G::TN;
-  const int f0 = (int)(tile % ftiles) * G::TF;
+  // Blocks are dealt to the XCDs round robin: each gets a run of tiles in an order that
+  // goes over all channels for GROUP tiles of points at a time, so that both operands'
+  // rows are found in its L2 (in order of blockIdx: 13,426 x 4096 to 223 56 us in place
+  // of 28, 100,000 x 1040 to 300 84 in place of 65; squares of 4096 and 8192 the same).
+  constexpr unsigned GROUP = 8;
+  const unsigned ftiles = (unsigned)(a.F + G::TF - 1) / G::TF, ntiles = gridDim.x / ftiles;
+  const unsigned xcd = blockIdx.x % 8, per = gridDim.x / 8, more = gridDim.x % 8;
+  const unsigned l = xcd * per + (xcd < more ? xcd : more) + blockIdx.x / 8;
+  const unsigned grp = l / (GROUP * ftiles), in = l - grp * GROUP * ftiles;
+  const unsigned wide = ntiles - grp * GROUP < GROUP ? ntiles - grp * GROUP : GROUP;
+  const int64_t n0 = (int64_t)(grp * GROUP + in % wide) * G::TN;
+  const int f0 = (int)(in / wide) * G::TF;
   const int rows_n = (int)(a.N - n0 < G::TN ? a.N - n0 : G::TN);
   const int rows_f = a.F - f0 < G::TF ? a.F - f0 : G::TF;
 
@@ -368,16 +388,19 @@ hipError_t run_tiled(const I8Args& a, hipStream_t st) {
 }
 template <typename T>
 hipError_t run_gemm(const I8Args& a, hipStream_t st) {
-  // The tile that takes the least time: rounds of the blocks that fit the chip at
-  // once (one of 256 x 256 per CU, two of the others) times a round's time, which at
-  // 4096 x 4096 x 4096 was 64, 38 and 14 us.  (256 against 128: 4096^3 64 and 76
-  // us, 5000 x 4096 x 4096 111 and 101; 128 against 64: 16384 x 512 x 1536 30 and
-  // 42, 2048 x 1024 x 1024 9.3 and 6.6.)
-  const auto cost = [&](int t, int at_once, double round) {
+  // The tile that takes the least time, by a model of its measured ones (us): a block to
+  // each CU takes `first` and, for a step of 128 of K, `step`; each further block of a CU
+  // `more` and `more_step`.  (Within 10% of the best tile over N from 333 to 100,000, F
+  // from 76 to 8188, K from 64 to 4096: 4096^3 65, 70 and 106 us with tiles of 256,
+  // 128 and 64; 4096 x 256 to 4092 18, 14 and 24; 2000 x 1040 to 2001 27, 13 and 15;
+  // 2000 x 4096 to 2001 60, 32 and 29.)
+  const int steps = (a.Kp + 127) / 128;
+  const auto cost = [&](int t, double first, double step, double more, double more_step) {
     const int64_t n = (a.N + t - 1) / t * ((a.F + t - 1) / t);
-    return (double)((n + at_once - 1) / at_once) * round;
+    return first + step * steps + (double)((n + 255) / 256 - 1) * (more + more_step * steps);
   };
-  const double c256 = cost(256, 256, 64), c128 = cost(128, 512, 38), c64 = cost(64, 512, 14);
+  const double c256 = cost(256, 12.0, 1.45, 8.5, 1.6), c128 = cost(128, 5.5, 0.8, 1.4, 0.46),
+               c64 = cost(64, 3.9, 0.27, 1.2, 0.14);
   const int want = c256 <= c128 && c256 <= c64 ? 256 : c128 <= c64 ? 128 : 64;
   if (want == 256) return run_tiled<T, 2, 4, 8, 4, 2>(a, st);
   if (want == 128) return run_tiled<T, 2, 2, 4, 4, 2>(a, st);

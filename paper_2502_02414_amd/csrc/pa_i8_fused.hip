@@ -159,10 +159,9 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
 
   // operand chunk 4 s + g of rows r and 16 + r (the same key)
   const int at[2] = {r * G::RB + 16 * (g ^ key_of<KS>(r)), r * G::RB + 16 * ((4 + g) ^ key_of<KS>(r))};
-  // A tile's results; residuals (RES) of up to two runs a half are requested
-  // before the rows of the tile after next, so that they do not wait for those.
+  // A tile's results; residuals (RES; up to two runs a half) are requested before the
+  // rows of the tile after next, so that they do not wait for those.
   typedef bf16 BV __attribute__((ext_vector_type(V)));
-  constexpr bool AHEAD = G::RUNS <= 2;
   auto channel = [&](int q) { return 16 * NCT * wave + (NCT == 1 ? 4 * g : 32 * q + 8 * g); };
   auto place = [&](int u, int q) {  // F is a multiple of V
     const int f = f0 + channel(q);
@@ -177,8 +176,8 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
   auto tile = [&](int64_t t, int buf, auto RES) __attribute__((always_inline)) {
     constexpr bool res = decltype(RES)::value;
     const auto rd = tile_of(a.D, t, F * 2), rc = tile_of(res ? a.C : a.D, t, F * 2);
-    BV c[2][AHEAD ? G::RUNS : 1];
-    if constexpr (res && AHEAD)
+    BV c[2][G::RUNS];
+    if constexpr (res)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -202,13 +201,12 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
 #pragma unroll
       for (int q = 0; q < G::RUNS; ++q) {
         const int fl = channel(q);
-        if constexpr (res && !AHEAD) c[u][0] = residual(rc, u, q);
         BV o;
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float y = fmaf((float)acc[2 * q + e / 4][e % 4], sn * sws[fl + e], bs[fl + e]);
           if constexpr (ACT == PA_ACT_GELU) y = gelu_tail(y);
-          if constexpr (res) y += (float)c[u][AHEAD ? q : 0][e];
+          if constexpr (res) y += (float)c[u][q][e];
           o[e] = (bf16)y;
         }
         typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -235,13 +233,15 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
     }
   };
   if (!on) walk([&](int64_t t, int) { load(t + 2); });
-  else if (a.C) walk([&](int64_t t, int buf) { tile(t, buf, std::true_type{}); });
-  else walk([&](int64_t t, int buf) { tile(t, buf, std::false_type{}); });
+  else if (G::RUNS > 2 || !a.C) walk([&](int64_t t, int buf) { tile(t, buf, std::false_type{}); });
+  else if constexpr (G::RUNS <= 2)
+    walk([&](int64_t t, int buf) { tile(t, buf, std::true_type{}); });
 }
 
 template <bool XQ, int KS, int NCT>
 hipError_t run(const I8Args& a, hipStream_t st) {
   using G = FusedGeo<XQ, KS, NCT>;
+  if (a.C && G::RUNS > 2) return hipErrorInvalidValue;
   const int ncg = (a.F + G::FCB - 1) / G::FCB;
   const int64_t tiles = (a.N + G::PTS - 1) / G::PTS;
   const int PG = (int)(tiles < 256 / ncg ? tiles : 256 / ncg);
@@ -256,22 +256,29 @@ template <bool XQ>
 hipError_t by_size(const I8Args& a, hipStream_t st) {
   if (a.K <= 64) return run<XQ, 1, 4>(a, st);
   if (a.K <= 128) return run<XQ, 2, 4>(a, st);
-  if (a.K <= 256) return a.F <= 256 ? run<XQ, 4, 2>(a, st) : run<XQ, 4, 8>(a, st);
+  if (a.K <= 256) {
+    if (a.F <= 256) return run<XQ, 4, 2>(a, st);
+    // (128 channels to a wave, so that 1024 share their rows, leave no registers for
+    // residuals, which then wait for each other, and fewer, longer turns: 256 to 1024,
+    // us, with 64 and 128: a million rows 607 and 519, with residuals 827 and 971;
+    // 100,000 65 and 56; 50,000 30 and 32; 10,000 13 and 18)
+    return a.F <= 512 || a.C || a.N < 65536 ? run<XQ, 4, 4>(a, st) : run<XQ, 4, 8>(a, st);
+  }
   if (a.K <= 512) return a.F <= 128 ? run<XQ, 8, 1>(a, st) : run<XQ, 8, 4>(a, st);
   return run<XQ, 16, 2>(a, st);
 }
 
 }  // namespace
 
-// Every block first fetches its weights: above 128 KiB of them that takes about as
-// long as all of the two launches on few rows.  (Two launches against this, us:
-// 256 to 1024 with GELU 14.3 and 16.2 at 4,096 rows, 18.4 and 17.5 at 8,192, 118
-// and 79 at 100,000; 1024 to 256 10.8 and 12.9 at 2,048, 19.1 and 14.0 at 8,192; 256
-// to 256 7.9 and 5.4 at 512, 41 and 22 at 100,000; 128 to 1024 7.5 and 5.9 at 512.)
+// Every block first fetches its weights: above 128 KiB of more than 256 inputs that
+// takes about as long as all of the two launches on few rows.  (Two launches against
+// this, us: 256 to 1024 9.5 and 8.3 at 2,048 rows, 13.2 and 8.9 at 4,096; 512 to 1024
+// 10.7 and 12.3, 15.4 and 13.1; 1024 to 256 11.3 and 13.1 at 4,096, 16.4 and 13.4
+// at 6,144; 256 to 256 7.9 and 5.4 at 512; 128 to 1024 7.5 and 5.9 at 512.)
 bool linear_i8_fused(int64_t N, int F, int K) {
   if (F % 8 || K > 1024) return false;
   const int most = K <= 128 ? 1024 : K <= 256 ? 2048 : K <= 512 ? 1024 : 512;
-  return F <= most && (K * F <= 131072 || N >= 6144);
+  return F <= most && (K <= 256 || K * F <= 131072 || N >= (K <= 512 ? 4096 : 6144));
 }
 
 hipError_t launch_linear_i8(const I8Args& a, hipStream_t st) {
