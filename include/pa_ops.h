@@ -185,9 +185,9 @@ pa_status pa_quant_weight(int K, int F, pa_dtype dtype, const void* W, int8_t* W
 typedef enum { PA_ACT_NONE = 0, PA_ACT_GELU = 1 } pa_act;
 
 /* D [N,F] (d_dtype) = act(s_i sw_f sum_k q_ik Wq_fk + bias_f) + C_if; bias
- * [F] fp32 and C [N,F] d_dtype nullable; GELU(u) = u Phi(u) on the fp32 value
- * (bf16 results: to within 1e-4 of it, or 2e-7).  D may be C (the residual
- * stream updated in place). */
+ * [F] fp32 and C [N,F] d_dtype nullable; GELU(u) = u Phi(u) on the fp32 value,
+ * to within 2e-6 of it, or 2e-10 (bf16 results: 1e-4, or 2e-7, before rounding).
+ * D may be C (the residual stream updated in place). */
 pa_status pa_gemm_i8(int64_t N, int F, int K, const int8_t* q, const float* s, const int8_t* Wq,
                      const float* sw, const float* bias, pa_act act, const void* C, void* D,
                      pa_dtype d_dtype, void* stream);

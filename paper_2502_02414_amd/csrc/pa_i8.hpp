@@ -11,31 +11,46 @@ namespace pa {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ float gelu_exact(float x) {
-  return 0.5f * x * (1.f + erff(x * 0.7071067811865476f));
-}
-// GELU for bf16 results: x Phi(x) = max(x, 0) - z Q(z), z = |x|, the upper tail
-// Q(z) = 1 - Phi(z) as exp2 of a polynomial of degree 6, fitted for this kernel
-// over [0, 9] (weighted minimax, linear programming over 4,001 points).  In
-// fp32 against 64 bits: relative 2.1e-5 for x > -4, 1.5e-4 down to -5, 3.8e-4 to
-// -6, below that 1e-12 absolute; half a bf16 step is 2e-3 to 3.9e-3.
-// (Half of the kernel's vector instructions: one exp2, the time of four others,
-// and nine more; erff takes three times as many.  A million rows, 256 to 1024, on
-// one card: degree 7 674 us, 6 650, 5 640 but 0.5% off at -4.5.)
-__device__ __forceinline__ float gelu_tail(float x) {
-  const float z = __builtin_elementwise_minimum(fabsf(x), 9.f);
-  float p = 2.65611924987752e-05f;
-  p = fmaf(p, z, -0.000669357308652252f);
-  p = fmaf(p, z, 0.0075453296303749084f);
-  p = fmaf(p, z, -0.05213657766580582f);
-  p = fmaf(p, z, -0.46012184023857117f);
-  p = fmaf(p, z, -1.15067458152771f);
-  p = fmaf(p, z, -1.0000303983688354f);
+// GELU: x Phi(x) = max(x, 0) - z Q(z), z = |x|, the upper tail Q(z) = 1 - Phi(z) as exp2
+// of a polynomial, fitted for these kernels (weighted minimax, linear programming
+// over 4,001 points).  Half of the kernels' vector instructions: one exp2, the time of
+// four others, and a few more than the polynomial's.
+//
+// bf16 results: degree 6 over [0, 9].  In fp32 against 64 bits: relative 2.1e-5 for
+// x > -4, 1.5e-4 down to -5, 3.8e-4 to -6, below that 1e-12 absolute; half a bf16
+// step is 2e-3 to 3.9e-3.  (A million rows, 256 to 1024, on one card: degree 7 674 us,
+// 6 650, 5 640 but 0.5% off at -4.5.)
+//
+// fp32 results: degree 10 over [0, 8].  Relative 6e-7 for x > -2, 1.1e-6 down to -4,
+// 6e-6 to -5, 1.2e-4 to -6, below that 1e-10 absolute (0.5 x (1 + erf) in fp32, which
+// cancels there, is 5e-4 off at -4 and takes longer: 29,205 rows, 64 to 2496, 128 us and 92).
+__device__ __forceinline__ float tail_of(float x, float z, float p) {
   return fmaf(-z, fast_exp2(p), __builtin_elementwise_maximum(x, 0.f));
 }
 template <typename T> __device__ __forceinline__ float gelu_for(float x) {
-  if constexpr (sizeof(T) == 2) return gelu_tail(x);
-  else return gelu_exact(x);
+  if constexpr (sizeof(T) == 2) {
+    const float z = __builtin_elementwise_minimum(fabsf(x), 9.f);
+    float p = 2.65611924987752e-05f;
+    p = fmaf(p, z, -0.000669357308652252f);
+    p = fmaf(p, z, 0.0075453296303749084f);
+    p = fmaf(p, z, -0.05213657766580582f);
+    p = fmaf(p, z, -0.46012184023857117f);
+    p = fmaf(p, z, -1.15067458152771f);
+    return tail_of(x, z, fmaf(p, z, -1.0000303983688354f));
+  } else {
+    const float z = __builtin_elementwise_minimum(fabsf(x), 8.f);
+    float p = -2.5640650491709494e-08f;
+    p = fmaf(p, z, 7.68178097132477e-07f);
+    p = fmaf(p, z, -9.893834430840798e-06f);
+    p = fmaf(p, z, 6.959781603654847e-05f);
+    p = fmaf(p, z, -0.00025399887817911804f);
+    p = fmaf(p, z, -5.7297507737530395e-05f);
+    p = fmaf(p, z, 0.007021773606538773f);
+    p = fmaf(p, z, -0.05249564349651337f);
+    p = fmaf(p, z, -0.4592008888721466f);
+    p = fmaf(p, z, -1.1511073112487793f);
+    return tail_of(x, z, fmaf(p, z, -0.9999998807907104f));
+  }
 }
 
 template <typename T> struct Row16 {

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float y = fmaf((float)acc[2 * q + e / 4][e % 4], sn * sws[fl + e], bs[fl + e]);
-          if constexpr (ACT == PA_ACT_GELU) y = gelu_tail(y);
+          if constexpr (ACT == PA_ACT_GELU) y = gelu_for<bf16>(y);
           if constexpr (res) y += (float)c[u][q][e];
           o[e] = (bf16)y;
         }

@@ -533,6 +533,31 @@ def test_products(dt, N, K, F):
             assert torch.equal(D3, D2)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("F", [1, 8])
+def test_gelu_over_its_range(dt, F):
+    """u from -20 to 20 in one product of 1 and -1 with a scale: 2e-6 of GELU or 2e-10
+    (bf16 1e-4 or 2e-7, then its rounding); infinities and NaN as in u Phi(u)."""
+    ty = DT[dt]
+    u = torch.cat([torch.linspace(-20, 20, 8001), torch.tensor([0.0, 1e-30, -1e-30])])
+    n, extra = u.numel(), torch.tensor([math.inf, math.nan])
+    q = torch.zeros(n + 2, 16, dtype=torch.int8)
+    q[:, 0] = torch.cat([torch.where(u < 0, -1, 1), torch.ones(2)]).to(torch.int8)
+    s = torch.cat([u.abs(), extra])
+    w = torch.zeros(F, 16, dtype=torch.int8)
+    w[:, 0] = 1
+    D = torch.empty(n + 2, F, dtype=ty, device="cuda")
+    ops.pa_gemm_i8(dev(q), dev(s), dev(w), torch.ones(F, device="cuda"), D, K=1, act="gelu")
+    v = u.double()
+    ref = (0.5 * v * torch.erfc(-v / math.sqrt(2.0)))[:, None].expand(n, F)
+    rel, least, half = (2e-6, 2e-10, 0.0) if dt == "f32" else (1e-4, 2e-7, 2.0 ** -8)
+    got = D.cpu().double()
+    off = (got[:n] - ref).abs()
+    bound = torch.maximum(rel * ref.abs(), torch.full_like(ref, least))
+    assert (off <= bound + half * (ref.abs() + bound)).all(), (off - bound).max()
+    assert (got[n] == math.inf).all() and torch.isnan(got[n + 1]).all()
+
+
 def test_products_of_the_largest_integers():
     """All integers 127 at the longest row: the sum 131072 * 127^2 fits 32 bits."""
     K = 131072
