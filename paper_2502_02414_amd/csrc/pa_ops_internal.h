@@ -135,9 +135,6 @@ __device__ __forceinline__ uint32_t quant4(float a, float b, float c, float d, f
   const uint32_t hi = __builtin_amdgcn_perm(t[3], t[2], 0x04000c0cu);
   return inv == 0.f ? 0u : lo | hi;
 }
-__device__ __forceinline__ uint32_t quant1(float x, float inv) {
-  return quant4(x, 0.f, 0.f, 0.f, inv) & 0xffu;
-}
 #endif
 
 }  // namespace pa

@@ -470,14 +470,31 @@ def test_quant_rows(dt, N, K):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("K,F", [(1, 1), (7, 65), (64, 64), (100, 33), (256, 1024), (1000, 517)])
+@pytest.mark.parametrize("K,F", [(1, 1), (7, 65), (64, 64), (100, 33), (256, 1024), (1000, 517),
+                                 (513, 72), (1025, 200), (2600, 100), (17, 4), (4100, 68)])
 def test_quant_weight(dt, K, F):
     W = torch.randn(K, F, generator=draw(K + F)).to(DT[dt])
     if F > 10:
         W[:, 4] = 0
+        W[K // 2, 7], W[K - 1, 9] = math.inf, math.nan
     q, s = ops.quant_weight(dev(W))
     rq, rs = R.quant(W.t().contiguous())
-    assert torch.equal(q.cpu(), R.padded(rq)) and torch.equal(s.cpu(), rs)
+    assert torch.equal(q.cpu(), R.padded(rq))
+    assert torch.equal(torch.nan_to_num(s.cpu(), nan=-1), torch.nan_to_num(rs, nan=-1))
+
+
+@pytest.mark.parametrize("N,K,F", [(5, 72, 40), (100, 256, 64), (300, 100, 517), (3000, 264, 128),
+                                   (17000, 256, 256)])
+@pytest.mark.parametrize("kinds", [("f32", "bf16"), ("bf16", "f32")])
+def test_products_of_one_type_into_the_other(kinds, N, K, F):
+    tx, td = DT[kinds[0]], DT[kinds[1]]
+    g = draw(N + F)
+    x, W = torch.randn(N, K, generator=g).to(tx), torch.randn(K, F, generator=g) / math.sqrt(K)
+    C = torch.randn(N, F, generator=g).to(td)
+    (wq, sw), (q, s) = R.quant(W.t().contiguous()), R.quant(x)
+    D = torch.empty(N, F, dtype=td, device="cuda")
+    ops.pa_linear_i8(dev(x), dev(R.padded(wq)), dev(sw), D, ops.linear_i8_workspace(N, K, F), C=dev(C))
+    within(D, *R.linear(q, s, wq, sw, C=C), td, "D")
 
 
 PRODUCTS = [(1, 16, 16), (1, 256, 1024), (1, 4096, 4096), (2, 100, 33), (5, 1000, 517), (8, 7, 3),
