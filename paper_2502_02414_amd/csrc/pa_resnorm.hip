@@ -328,7 +328,11 @@ template <typename T, int WIDE, bool AHEAD, bool GATE>
 __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd(ResNormArgs a) {
   constexpr int E = Chunk16<T>::E;
   __shared__ float2 red[32];
-  extern __shared__ float fold[];  // [rows][5][C] (narrow)
+  extern __shared__ __attribute__((aligned(16))) float fold[];  // [rows][5][C] (narrow)
+  // Blocks of 1024 threads on bf16 keep the parameters in LDS, [4][C], for want of
+  // registers (16,384 rows of 8192 with a gate: 638 us with them in registers, and
+  // 35 of those spilled, 554 so; narrower rows lose 5 to 20% by it).
+  constexpr bool LP = WIDE == 1024 && sizeof(T) == 2;
   const int L = WIDE ? blockDim.x : a.L;
   RowGroup<WIDE> grp{L, red};
   const int rows = WIDE ? 1 : blockDim.x / L;
@@ -336,11 +340,25 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
   const bool on = c < a.C;
   const int c0 = on ? c : 0;
   const float invC = 1.f / (float)a.C;
-  float pg[E], pb[E], sc[E], qg[E];
-  gains(a.post_g, c0, 1.f, pg);
-  gains(a.post_b, c0, 0.f, pb);
-  gains(a.scale, c0, 1.f, sc);
-  gains(a.pre_g, c0, 1.f, qg);
+  float kept[LP ? 1 : 4][E];
+  if constexpr (LP) {
+    for (int i = threadIdx.x; i < a.C; i += blockDim.x) {
+      fold[i] = a.post_g ? a.post_g[i] : 1.f;
+      fold[a.C + i] = a.post_b ? a.post_b[i] : 0.f;
+      fold[2 * a.C + i] = a.scale ? a.scale[i] : 1.f;
+      fold[3 * a.C + i] = a.pre_g ? a.pre_g[i] : 1.f;
+    }
+    __syncthreads();
+  } else {
+    gains(a.post_g, c0, 1.f, kept[0]);
+    gains(a.post_b, c0, 0.f, kept[1]);
+    gains(a.scale, c0, 1.f, kept[2]);
+    gains(a.pre_g, c0, 1.f, kept[3]);
+  }
+  auto param = [&](int k, float(&v)[E]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = LP ? fold[k * a.C + c0 + e] : kept[LP ? 0 : k][e];
+  };
   float acc[5][E];
 #pragma unroll
   for (int k = 0; k < 5; ++k)
@@ -378,6 +396,8 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
     }
     if (a.dh) {
       unpack<T>(r.dh, gh);
+      float qg[E];
+      param(3, qg);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         if (ok) {
@@ -391,7 +411,10 @@ __global__ void __launch_bounds__(WIDE ? WIDE : 256, WIDE ? 1 : 3) k_resnorm_bwd
       for (int e = 0; e < E; ++e) d[e] += gh[e];
     }
     // d: e of the header; u: post(y)
-    float u[E], o[E], m[E];
+    float u[E], o[E], m[E], pg[E], pb[E], sc[E];
+    param(0, pg);
+    param(1, pb);
+    param(2, sc);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       u[e] = a.post != PA_NORM_NONE ? fmaf(yh[e], pg[e], pb[e]) : yh[e];
@@ -520,7 +543,8 @@ hipError_t launch_resnorm(const ResNormArgs& a0, int dtype, bool bwd, hipStream_
   const ResNormGeo g = geo(a.C, dtype);
   a.L = g.L;
   const dim3 grid(resnorm_blocks(a.N, a.C, dtype, bwd)), block(g.threads);
-  const size_t lds = bwd && !g.wide ? (size_t)g.rows * 5 * a.C * sizeof(float) : 0;
+  const size_t lds = !bwd ? 0 : !g.wide ? (size_t)g.rows * 5 * a.C * sizeof(float)
+                                        : dtype == 1 && g.threads > 512 ? (size_t)4 * a.C * sizeof(float) : 0;
   auto go = [&](auto* k) { hipLaunchKernelGGL(k, grid, block, lds, st, a); };
   auto pick = [&](auto type, auto wide, auto ahead) {
     using T = decltype(type);

@@ -76,6 +76,10 @@ JOINTS = [
     (300, 520, "layer", "layer", "sigmoid", 1.0, True),
     (129, 1000, "rms", "rms", "linear", 0.5, True),
     (65, 4096, "layer", "layer", "sigmoid", 1.0, True),
+    # bf16 only
+    (33, 5000, "layer", "rms", "sigmoid", 1.0, True),
+    (1100, 4104, "rms", "layer", "linear", 0.5, True),
+    (9, 8192, "layer", "layer", None, 1.0, True),
     # one block in the backward, of one or two turns
     (13, 256, "layer", "layer", "sigmoid", 1.0, True),
     (61, 64, "rms", "layer", None, 0.5, True),
@@ -87,6 +91,8 @@ JOINTS = [
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("N,C,post,pre,gated,alpha,full", JOINTS)
 def test_joint_forward(dt, N, C, post, pre, gated, alpha, full):
+    if dt == "f32" and C > 4096:
+        return
     say(f"joint forward {dt} N={N} C={C} {post} {pre} {gated}")
     ty = DT[dt]
     p, d = joint_case(N, C, ty, post, pre, gated, alpha, full)
@@ -121,7 +127,7 @@ def test_joint_forward(dt, N, C, post, pre, gated, alpha, full):
 @pytest.mark.parametrize("N,C,post,pre,gated,alpha,full", JOINTS)
 @pytest.mark.parametrize("use", ["both", "dx1", "dh"])
 def test_joint_backward(dt, N, C, post, pre, gated, alpha, full, use):
-    if use == "dh" and not pre:
+    if use == "dh" and not pre or dt == "f32" and C > 4096:
         return
     say(f"joint backward {dt} N={N} C={C} {post} {pre} {gated} {use}")
     ty = DT[dt]
