@@ -153,6 +153,39 @@ def test_training_steps(kind, dt, bits):
     assert torch.isfinite(s.forward(x, Gs).float()).all()
 
 
+@pytest.mark.parametrize("kind,dt,bits", [(SandwichStack, F32, 8), (BlockStack, BF16, 32)])
+def test_training_steps_in_a_graph(kind, dt, bits):
+    """Forward, backward and the optimiser's step in one graph, replayed beside a twin
+    that runs them eagerly: the same parameters after every step."""
+    s, x, Gs, w = make(1001, 64, 16, 2, dt, kind)
+    t, *_ = make(1001, 64, 16, 2, dt, kind)
+    t.tuned = s.tuned
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+    lr = torch.full((1,), 1e-2, device="cuda")
+    a, b = (k.adamw(lr=1e-2, bits=bits, wd=0.1, seed=4) for k in (s, t))
+
+    def step(k, opt, **kw):
+        k.forward(x, Gs)
+        opt.step(k.named_grads(k.backward(w)[1]), **kw)
+
+    for _ in range(2):  # (the first chooses the library products' algorithms)
+        step(s, a)
+        step(t, b)
+        count.add_(1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        count.add_(1)
+        step(s, a, step_dev=count, lr_dev=lr)
+    for rep in range(4):
+        step(t, b, lr=lr.item())  # (the fp32 number that the graph reads)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in s.named_parameters().items():
+            assert torch.equal(v, t.named_parameters()[k]), (rep, k)
+    assert count.item() == 6 and a.t == 2 and b.t == 6
+
+
 @pytest.mark.parametrize("kind,dt", [(BlockStack, F32), (BlockStack, BF16), (SandwichStack, F32),
                                      (SandwichStack, BF16)])
 @pytest.mark.parametrize("N,C", [(1001, 64), (8192, 128)])
