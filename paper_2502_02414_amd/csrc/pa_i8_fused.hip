@@ -12,7 +12,7 @@
 // Results leave from the registers, 64 bytes of a point's row per instruction.
 //
 // Measured, a million rows of bf16: 256 to 1024 channels 518 us (4.9 TB/s, what a
-// copy reaches), with GELU 640 to 690 us by the card; 1024 to 256 with a residual
+// copy reaches), with GELU 630 to 690 us by the card; 1024 to 256 with a residual
 // 677 us (4.5 TB/s); 256 to 256 214 us, 64 to 256 with GELU 206 us, 256 to 64
 // 174 us.  As two launches, quantised rows through memory and tiles: 1064, 1200,
 // 1217, 377, 272 and 334 us.  With GELU the vector units bound it: 16 issue slots an
@@ -20,7 +20,8 @@
 // beside 0.25M of the matrix cores.  Before the loads and stores lost their
 // branches the compiler waited for each at once: 1024 to 256 838 us.  Issuing the
 // products among the activation's instructions, run by run, changed nothing; with
-// two halves' sums in registers it spilled (970 us).
+// two halves' sums in registers it spilled (970 us).  Waves in their products come
+// first: 1 to 3% (128 to 512 with GELU 314 -> 305 us).
 //
 // LDS rows hold 64 KS bytes without padding; the 16-byte chunks of row j lie at
 // c ^ key(j), so that the lanes of an operand read meet different banks.
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
       i32x4 acc[NCT];
 #pragma unroll
       for (int i = 0; i < NCT; ++i) acc[i] = i32x4{0, 0, 0, 0};
+      __builtin_amdgcn_s_setprio(1);  // (products first: they run beside another wave's activation)
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const i32x4 x = *reinterpret_cast<const i32x4*>(xb + at[s & 1] + 128 * (s / 2));
@@ -197,6 +199,7 @@ __global__ void __launch_bounds__(512) k_linear_i8(I8Args a, int PG) {
           acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[i][s], x, acc[i], 0, 0, 0);
         if (KS > 4 && s % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (all at once would spill)
       }
+      __builtin_amdgcn_s_setprio(0);
       const float sn = ss[buf][16 * u + r];
 #pragma unroll
       for (int q = 0; q < G::RUNS; ++q) {

@@ -286,6 +286,7 @@ class AdamWItems:
         self.tensors = [None] * n
         self.dev, self.blocks, self.moved = None, 0, 0
         self.captured = []  # tables that graphs read
+        self.grads = [None] * n  # (pointer, elements, dtype) of each gradient
 
     def set_grad(self, i, g):
         it = self.arr[i]
@@ -297,6 +298,18 @@ class AdamWItems:
             self.dev = None
             self.moved += 1
         self.tensors[i]["g"] = g
+        self.grads[i] = (ptr, it.n, g.dtype)
+
+    def set_grads(self, gs):
+        """All gradients, in the items' order."""
+        cur = _current_device()
+        for i, (g, had, d) in enumerate(zip(gs, self.grads, self.tensors)):
+            # (one that stayed where it was takes its checks alone)
+            if had and (g.data_ptr(), g.numel(), g.dtype) == had and g.get_device() == cur \
+                    and g.is_contiguous():
+                d["g"] = g
+            else:
+                self.set_grad(i, g)
 
     def table(self):
         """Makes the device table (a copy from host memory that has arrived when
@@ -429,8 +442,7 @@ class AdamW:
             raise ValueError("a step captured into a graph needs step_dev")
         it = self.items
         before = it.moved
-        for i, k in enumerate(self.names):
-            it.set_grad(i, grads[k])
+        it.set_grads([grads[k] for k in self.names])
         if it.dev is None and it.moved == before and not _capturing():
             it.table()  # the gradients stay where they are
         pa_adamw(self.items, self.lr if lr is None else lr, self.t + 1, *self.betas, self.eps,
