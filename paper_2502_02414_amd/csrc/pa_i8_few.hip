@@ -11,7 +11,7 @@
 // With more rows than 16 every block of channels quantises them again, which costs
 // less than a second launch while all the blocks run at once.  Measured, us, as two
 // launches (quantiser, tiles) and as one: 333 rows of 1000 to 517 fp32 8.3 and
-// 7.6; bf16 32 rows of 1024 to 4096 7.9 and 5.8, 333 of 256 to 517 7.8 and 5.5, 1024
+// 6.7; bf16 32 rows of 1024 to 4096 7.9 and 5.8, 333 of 256 to 517 7.8 and 5.5, 1024
 // of 1024 to 256 8.8 and 6.6, 512 of 4096 to 256 15.4 and 13.2.  One row of 4096 to
 // 4096 5.5 us (16.8 MB of weights, from the last cache in these figures), 16 of 4096
 // to 4096 9.3.
@@ -26,16 +26,17 @@ constexpr int kFewRows = 16;
 // of an operand read lie in different banks.
 __host__ __device__ constexpr int row_bytes(int Kp) { return Kp % 32 ? Kp : Kp + 16; }
 
-// RT: tiles of 16 rows that a block takes; H: a thread's chunks of a row in flight.
+// RT: tiles of 16 rows that a block takes.
 template <int RT> struct FewGeo {
-  static constexpr int ROWS = kFewRows * RT, H = RT == 1 ? 4 : 8;
+  static constexpr int ROWS = kFewRows * RT;
   static constexpr int OWN = 8 * ROWS * 64 + 8 * ROWS + 1024 + 256;  // LDS beside the rows
 };
 
-template <typename TX, typename TD, bool ODD, int RT>
+// H: a thread's chunks of a row in flight.
+template <typename TX, typename TD, bool ODD, int RT, int H>
 __global__ void __launch_bounds__(512) k_linear_few(I8Args a, int KW, int G, int rows_first) {
   constexpr int E = Row16<TX>::E, U = 8, NOWHERE = 0x7fffff00;
-  constexpr int ROWS = FewGeo<RT>::ROWS, H = FewGeo<RT>::H;
+  constexpr int ROWS = FewGeo<RT>::ROWS;
   extern __shared__ __attribute__((aligned(16))) char xs[];  // [N][RB]
   __shared__ __attribute__((aligned(16))) int red[8][ROWS][16];
   __shared__ uint32_t big[ROWS];
@@ -172,7 +173,7 @@ template <int RT> int few_split(int64_t N, int F, int K, int x_dtype) {
   return 8 * KW < steps || bytes > (x_dtype == 1 && K % 8 == 0 ? 8192 : 4096) || (bytes > 2048 && KW < 4) ? 0 : KW;
 }
 
-template <typename TX, typename TD, int RT>
+template <typename TX, typename TD, int RT, int H>
 hipError_t run(const I8Args& a, hipStream_t st) {
   constexpr int ROWS = FewGeo<RT>::ROWS;
   const int rows = a.N < ROWS ? (int)a.N : ROWS, KW = few_split<RT>(a.N, a.F, a.K, a.x_dtype);
@@ -187,16 +188,21 @@ hipError_t run(const I8Args& a, hipStream_t st) {
   const int rows_first = a.N * (int64_t)sizeof(TX) > a.F && nf <= 65535;
   const dim3 grid(rows_first ? nb : nf, rows_first ? nf : nb), block(512);
   if (a.K % Row16<TX>::E)
-    hipLaunchKernelGGL((k_linear_few<TX, TD, true, RT>), grid, block, lds, st, a, KW, 512 / NP,
+    hipLaunchKernelGGL((k_linear_few<TX, TD, true, RT, H>), grid, block, lds, st, a, KW, 512 / NP,
                        rows_first);
   else
-    hipLaunchKernelGGL((k_linear_few<TX, TD, false, RT>), grid, block, lds, st, a, KW, 512 / NP,
+    hipLaunchKernelGGL((k_linear_few<TX, TD, false, RT, H>), grid, block, lds, st, a, KW, 512 / NP,
                        rows_first);
   return hipGetLastError();
 }
 template <typename TX, typename TD>
 hipError_t by_rows(const I8Args& a, hipStream_t st) {
-  return a.N <= kFewRows ? run<TX, TD, 1>(a, st) : run<TX, TD, 2>(a, st);
+  if (a.N <= kFewRows) return run<TX, TD, 1, 4>(a, st);
+  // (32 rows have 16 threads each, to which 8 chunks are 2 KB of a row and 16 are 4; us, 333
+  // rows to 517 with 8 and 16: 1000 fp32 7.5 and 6.7, 1542 bf16 9.0 and 7.9; to 64, 3000
+  // bf16 9.7 and 11.0)
+  const int bytes = a.K * (int)sizeof(TX);
+  return bytes > 2048 && bytes <= 4096 ? run<TX, TD, 2, 16>(a, st) : run<TX, TD, 2, 8>(a, st);
 }
 
 }  // namespace

@@ -514,6 +514,7 @@ PRODUCTS = [(1, 16, 16), (1, 256, 1024), (1, 4096, 4096), (2, 100, 33), (5, 1000
             (17, 1, 1), (31, 4096, 24), (32, 4000, 40), (33, 1024, 40), (128, 2048, 136),
             (32, 1024, 4096), (63, 333, 1500), (513, 250, 515), (1000, 60, 64), (333, 1000, 517),
             (4096, 1000, 16), (8192, 33, 16), (4097, 1024, 16), (260, 777, 8), (96, 640, 1030),
+            (40, 1542, 70), (100, 2047, 33),
             # rows quantised on the way into the product (bf16)
             (17, 128, 104), (33, 64, 8), (45, 1024, 64), (100, 512, 128), (64, 256, 256),
             (6144, 520, 896), (16384, 64, 256), (16385, 128, 512), (16411, 256, 1024), (16400, 1024, 256),
