@@ -483,12 +483,17 @@ def pa_quant_weight(W, Wq, sw, stream=None):
                                   _in(sw, F, torch.float32, "sw"), B._stream(stream)))
 
 
-def quant_weight(W):
-    """(Wq, sw) of a weight [K, F], in new tensors."""
+def empty_weight(W):
+    """(Wq, sw): tensors for the integers and scales of a weight [K, F]."""
     torch = _torch()
     K, F = W.shape
-    Wq = torch.empty(F, padded(K), dtype=torch.int8, device=W.device)
-    sw = torch.empty(F, dtype=torch.float32, device=W.device)
+    return (torch.empty(F, padded(K), dtype=torch.int8, device=W.device),
+            torch.empty(F, dtype=torch.float32, device=W.device))
+
+
+def quant_weight(W):
+    """(Wq, sw) of a weight [K, F], in new tensors."""
+    Wq, sw = empty_weight(W)
     pa_quant_weight(W, Wq, sw)
     return Wq, sw
 

@@ -249,8 +249,15 @@ class BlockStack:
     # -- inference ------------------------------------------------------------
     def quantize(self):
         """The MLP's weights in 8-bit integers with a scale per output channel, for
-        ``infer``; again after the weights have changed."""
-        self.int8 = [(*ops.quant_weight(p["W1"]), *ops.quant_weight(p["W2"])) for p in self.params]
+        ``infer``; again after the weights have changed.  Every call writes the same
+        tensors, so that an ``infer`` in a graph replays with the integers of the
+        moment."""
+        if self.int8 is None:
+            self.int8 = [(*ops.empty_weight(p["W1"]), *ops.empty_weight(p["W2"]))
+                         for p in self.params]
+        for p, (w1, s1, w2, s2) in zip(self.params, self.int8):
+            ops.pa_quant_weight(p["W1"], w1, s1)
+            ops.pa_quant_weight(p["W2"], w2, s2)
         if self.ws_int8 is None:
             self.ws_int8 = ops.linear_i8_workspace(self.N, 4 * self.C, self.C, self.dev)
 

@@ -203,3 +203,34 @@ def test_inference_in_8_bits(kind, dt, N, C):
     say(f"  {kind.__name__} {dt} N={N} C={C}: {rel:.4f}")
     assert 1e-5 < rel <= 0.03
     assert torch.equal(s.infer(x, Gs), got)
+
+
+@pytest.mark.parametrize("kind,dt", [(BlockStack, BF16), (SandwichStack, BF16), (SandwichStack, F32)])
+def test_quantised_inference_in_a_graph(kind, dt):
+    """infer captured after quantize and replayed: as the eager one, also after the
+    weights have changed and been quantised again, with new tensors in the place of
+    whatever the stack let go of."""
+    say(f"quantised infer in a graph, {kind.__name__} {dt}")
+    s, x, Gs, _ = make(1001, 64, 16, 2, dt, kind)
+    s.quantize()
+    s.infer(x, Gs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = s.infer(x, Gs)
+    seen, hold = [], []
+    for rep in range(4):
+        if rep:
+            for p in s.params:
+                for k in ("W1", "W2"):
+                    p[k].mul_(1 + 0.25 * rep)
+            s.quantize()
+            hold += [torch.full_like(t, 77) for layer in s.int8 for t in layer]
+        want = s.infer(x, Gs)
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want), rep
+        seen.append(want)
+    assert all(not torch.equal(a, b) for a, b in zip(seen, seen[1:]))

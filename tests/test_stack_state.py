@@ -1,0 +1,77 @@
+"""What the block stack and its optimiser keep from call to call, on the CPU (the
+library's launches replaced by a recorder)."""
+import gc
+
+import pytest
+import torch
+
+from paper_2502_02414_amd import binding as B
+from paper_2502_02414_amd import ops
+from paper_2502_02414_amd.stack import BlockStack, SandwichStack
+
+
+class Recorder:
+    """libpa.so's calls by name and arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, args))
+            return B.PA_OK
+        return call
+
+    def names(self):
+        return [n for n, _ in self.calls]
+
+
+@pytest.fixture
+def fake(monkeypatch):
+    rec = Recorder()
+    monkeypatch.setattr(ops, "load", lambda: rec)
+    monkeypatch.setattr(ops, "_dev", lambda t, name, cur=None: t.data_ptr())
+    monkeypatch.setattr(ops, "_current_device", lambda: -1)  # (a CPU tensor's index)
+    monkeypatch.setattr(ops, "_capturing", lambda *a: False)
+    monkeypatch.setattr(B, "_stream", lambda s=None: 0)
+    return rec
+
+
+def params(C=64, M=16, dt=torch.bfloat16, kind=BlockStack):
+    r = lambda *s: torch.randn(*s)
+    p = {"Wp": r(C, C), "bp": r(C), "A": r(C, M), "b": r(M), "a": r(C), "b1": r(4 * C), "b2": r(C),
+         "W1": r(C, 4 * C).to(dt), "W2": r(4 * C, C).to(dt), "b_t": 0.5}
+    for n in ("ln1", "ln2"):
+        p[n + "_g"], p[n + "_b"] = r(C), r(C)
+    for n in "qkv":
+        p["W" + n], p["b" + n] = r(C, C), r(C)
+    if kind is SandwichStack:
+        for k in "12":
+            p["rs" + k], p[f"post{k}_g"] = r(C), r(C)
+    return p
+
+
+def stack(kind=BlockStack, L=2, N=100, C=64, M=16, dt=torch.bfloat16):
+    return kind(N, C, 4, M, [params(C, M, dt, kind) for _ in range(L)], dt, device="cpu")
+
+
+@pytest.mark.parametrize("kind", [BlockStack, SandwichStack])
+def test_quantize_writes_the_same_tensors_every_time(fake, monkeypatch, kind):
+    """A captured infer reads the integers and scales by their addresses: quantising
+    again has to write those, and may not let go of them."""
+    if kind is SandwichStack:
+        monkeypatch.setattr(ops, "residual_norm_workspace", lambda *a: torch.empty(8))
+    s = stack(kind)
+    s.quantize()
+    first = [[t.data_ptr() for t in layer] for layer in s.int8]
+    sizes = [[tuple(t.shape) for t in layer] for layer in s.int8]
+    assert sizes == [[(256, 64), (256,), (64, 256), (64,)]] * 2
+    hold = list(fake.calls)
+    fake.calls.clear()
+    for p in s.params:
+        p["W1"] = p["W1"] + 1
+    s.quantize()
+    gc.collect()
+    assert [[t.data_ptr() for t in layer] for layer in s.int8] == first
+    out = lambda calls: [a[4:6] for n, a in calls if n == "pa_quant_weight"]
+    assert out(fake.calls) == out(hold) and len(out(hold)) == 4
