@@ -277,8 +277,8 @@ class AdamWItems:
     """The host array of pa_adamw's tensors, which have to stay where they are.
     ``set_grad`` exchanges a gradient; ``table`` lays the tensors out on the
     device for one launch per step, until a gradient moves.  A graph that a step
-    was captured into reads its table again in every replay: the items keep it,
-    and have to live as long as the graph."""
+    was captured into reads its table and its gradients again in every replay: the
+    items keep both, and have to live as long as the graph."""
 
     def __init__(self, n):
         self.n = n
@@ -286,6 +286,7 @@ class AdamWItems:
         self.tensors = [None] * n
         self.dev, self.blocks, self.moved = None, 0, 0
         self.captured = []  # tables that graphs read
+        self.captured_grads = []  # and gradients, a list for every set of them
         self.grads = [None] * n  # (pointer, elements, dtype) of each gradient
 
     def set_grad(self, i, g):
@@ -337,6 +338,13 @@ class AdamWItems:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
         return self.ptr
 
+    def hold(self, handle):
+        """Keeps the gradients of a step that is captured on a stream."""
+        if handle and _capturing():
+            now = [d.get("g") for d in self.tensors]
+            if not any(all(a is b for a, b in zip(now, had)) for had in self.captured_grads):
+                self.captured_grads.append(now)
+
 
 def make_adamw_items(items, table=True) -> AdamWItems:
     """items: dicts with p (fp32), g (fp32 or bf16), m and v (fp32; or uint8
@@ -382,6 +390,7 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
                       _in(lr_dev, 1, torch.float32, "lr_dev", False),
                       _in(step_dev, 1, torch.int64, "step_dev", False))
     handle = B._stream(stream)
+    items.hold(handle)
     if items.dev is not None:
         _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle),
                                    ctypes.byref(a), handle))

@@ -793,3 +793,49 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(t["m"][-515:].cpu(), R.encode(m, h & 0xFFFF, True)[0])
     assert torch.equal(t["v"][-515:].cpu(), R.encode(v, h >> 16, False)[0])
     assert (t["p"][:1000] == 0).all()
+
+
+@pytest.mark.parametrize("table", [True, False])
+def test_graph_of_an_optimizer_whose_gradients_were_let_go_of(table):
+    """The program drops the gradients that a captured step reads, steps eagerly with
+    others and fills new tensors: every replay as a twin's eager step with the first
+    gradients."""
+    sizes = {"a": 5000, "b": 300, "c": 70000}
+    g = draw(13)
+    p0 = {k: torch.randn(n, generator=g) for k, n in sizes.items()}
+    first = {k: torch.randn(n, generator=g) for k, n in sizes.items()}
+    other = {k: dev(torch.randn(n, generator=g)) for k, n in sizes.items()}
+
+    def make():
+        params = {k: dev(v).clone() for k, v in p0.items()}
+        return params, ops.AdamW(params, lr=1e-2, bits=8, seed=9)
+
+    (pa, a), (pb, b) = make(), make()
+    kept = {k: dev(v) for k, v in first.items()}  # the twin's own
+    mine = {k: dev(v) for k, v in first.items()}
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+    for _ in range(2 if table else 1):
+        a.step(mine)
+        b.step(kept)
+        count.add_(1)
+    assert (a.items.dev is not None) == table
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        count.add_(1)
+        a.step(mine, step_dev=count)
+    del mine
+    over = []
+    for rep in range(4):
+        step = count.item() + 1
+        b.t = step - 1
+        b.step(kept)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in sizes:
+            assert torch.equal(pa[k], pb[k]), (rep, k)
+        a.t = b.t = step
+        a.step(other)
+        b.step(other)
+        count.add_(1)
+        over += [torch.full((n,), 1e3, device="cuda") for n in sizes.values()]

@@ -1,6 +1,7 @@
 """What the block stack and its optimiser keep from call to call, on the CPU (the
 library's launches replaced by a recorder)."""
 import gc
+import weakref
 
 import pytest
 import torch
@@ -75,3 +76,33 @@ def test_quantize_writes_the_same_tensors_every_time(fake, monkeypatch, kind):
     assert [[t.data_ptr() for t in layer] for layer in s.int8] == first
     out = lambda calls: [a[4:6] for n, a in calls if n == "pa_quant_weight"]
     assert out(fake.calls) == out(hold) and len(out(hold)) == 4
+
+
+def items_of(*sizes):
+    z = torch.zeros
+    return ops.make_adamw_items([{"p": z(n), "g": z(n), "m": z(n), "v": z(n)} for n in sizes])
+
+
+@pytest.mark.parametrize("table", [False, True])
+def test_gradients_that_a_graph_reads_are_kept(fake, monkeypatch, table):
+    """A step captured into a graph, then a step with other gradients: the first ones'
+    memory stays as long as the items."""
+    monkeypatch.setattr(ops, "_capturing", lambda *a: True)
+    monkeypatch.setattr(B, "_stream", lambda s=None: 1)
+    it = items_of(300, 400)
+    if table:
+        it.dev, it.blocks, it.stream, it.ptr, it.device = torch.zeros(8), 2, 1, 4096, -1
+    alive = [weakref.ref(d["g"]) for d in it.tensors]
+    for _ in range(3):  # (several graphs of the same gradients keep them once)
+        ops.pa_adamw(it, lr=1e-3, step_dev=torch.ones(1, dtype=torch.int64))
+    assert len(it.captured_grads) == 1 and len(it.captured) == table
+    monkeypatch.setattr(ops, "_capturing", lambda *a: False)
+    monkeypatch.setattr(B, "_stream", lambda s=None: 0)
+    it.set_grads([torch.ones(300), torch.ones(400)])
+    ops.pa_adamw(it, lr=1e-3)
+    gc.collect()
+    assert all(r() is not None for r in alive)
+    loose = [weakref.ref(d["g"]) for d in it.tensors]
+    it.set_grads([torch.ones(300), torch.ones(400)])
+    gc.collect()
+    assert all(r() is None for r in loose)  # (those of an eager step are let go of)
