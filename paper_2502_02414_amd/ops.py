@@ -153,12 +153,15 @@ def _torch():
 _capture = None
 
 
-def _capturing() -> bool:
-    """Whether calls on the current stream go into a graph."""
+def _capturing(stream=None) -> bool:
+    """Whether calls on a stream (the current one, if none is given) go into a graph."""
     global _capture
     if _capture is None:
         _capture = _torch().cuda.is_current_stream_capturing
-    return _capture()
+    if stream is None:
+        return _capture()
+    with _torch().cuda.stream(stream):
+        return _capture()
 
 
 def pa_ops_version() -> int:
@@ -331,16 +334,17 @@ class AdamWItems:
         stream other than the table's keeps its memory from being handed out."""
         if _current_device() != self.device:
             raise ValueError(f"items: on device {self.device}, not on the current one")
-        if handle and _capturing():  # (the default stream cannot be captured)
+        if handle and _capturing(stream):  # (the default stream cannot be captured)
             if not any(t is self.dev for t in self.captured):
                 self.captured.append(self.dev)
         elif handle != self.stream:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
         return self.ptr
 
-    def hold(self, handle):
-        """Keeps the gradients of a step that is captured on a stream."""
-        if handle and _capturing():
+    def hold(self, stream, handle):
+        """Keeps the gradients of a step that is captured on a stream (its handle
+        given)."""
+        if handle and _capturing(stream):
             now = [d.get("g") for d in self.tensors]
             if not any(all(a is b for a, b in zip(now, had)) for had in self.captured_grads):
                 self.captured_grads.append(now)
@@ -390,7 +394,7 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
                       _in(lr_dev, 1, torch.float32, "lr_dev", False),
                       _in(step_dev, 1, torch.int64, "step_dev", False))
     handle = B._stream(stream)
-    items.hold(handle)
+    items.hold(stream, handle)
     if items.dev is not None:
         _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle),
                                    ctypes.byref(a), handle))
@@ -447,12 +451,13 @@ class AdamW:
         from 1, advanced by the graph or between its replays), since a number from
         here would stand still, and its learning rate there, lr_dev (fp32), where
         that changes; the count of the calls goes on without such steps."""
-        if step_dev is None and _capturing():
+        capturing = _capturing(stream)
+        if step_dev is None and capturing:
             raise ValueError("a step captured into a graph needs step_dev")
         it = self.items
         before = it.moved
         it.set_grads([grads[k] for k in self.names])
-        if it.dev is None and it.moved == before and not _capturing():
+        if it.dev is None and it.moved == before and not capturing:
             it.table()  # the gradients stay where they are
         pa_adamw(self.items, self.lr if lr is None else lr, self.t + 1, *self.betas, self.eps,
                  self.seed, gscale, lr_dev, step_dev, stream)

@@ -839,3 +839,38 @@ def test_graph_of_an_optimizer_whose_gradients_were_let_go_of(table):
         b.step(other)
         count.add_(1)
         over += [torch.full((n,), 1e3, device="cuda") for n in sizes.values()]
+
+
+def test_optimizer_captured_on_a_stream_that_is_handed_over():
+    """A capture that goes on on another stream than the current one: refused without a
+    number on the device, otherwise every replay as a twin's eager step."""
+    n = 9000
+    g = draw(14)
+    p0, gr = torch.randn(n, generator=g), dev(torch.randn(n, generator=g))
+    make = lambda: (lambda p: (p, ops.AdamW({"w": p}, lr=1e-2, bits=8, seed=2)))(dev(p0).clone())
+    (pa, a), (pb, b) = make(), make()
+    for _ in range(2):
+        a.step({"w": gr})
+        b.step({"w": gr})
+    count = torch.full((1,), 2, dtype=torch.int64, device="cuda")
+    side, main = torch.cuda.Stream(), torch.cuda.current_stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        with torch.cuda.stream(main):  # (the capture goes on on `side`)
+            with pytest.raises(ValueError, match="step_dev"):
+                a.step({"w": gr}, stream=side)
+        count.add_(1)
+        with torch.cuda.stream(main):
+            a.step({"w": gr}, stream=side, step_dev=count)
+        graph.capture_end()
+    assert len(a.items.captured) == 1 and a.t == 2
+    a.items.set_grad(0, gr.clone())
+    hold = [torch.full((64,), 77, dtype=torch.int64, device="cuda") for _ in range(50)]
+    for rep in range(4):
+        b.step({"w": gr})
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(pa, pb), rep
+    assert len(hold) == 50

@@ -106,3 +106,29 @@ def test_gradients_that_a_graph_reads_are_kept(fake, monkeypatch, table):
     it.set_grads([torch.ones(300), torch.ones(400)])
     gc.collect()
     assert all(r() is None for r in loose)  # (those of an eager step are let go of)
+
+
+def test_a_capture_is_looked_for_on_the_stream_of_the_call(fake, monkeypatch):
+    """A stream handed over that is being captured, while the current one is not: the
+    step needs its number on the device, makes no table (a copy and a wait, which end
+    a capture), and what it reads is kept."""
+    side = object()
+    monkeypatch.setattr(ops, "_capturing", lambda stream=None: stream is side)
+    monkeypatch.setattr(B, "_stream", lambda s=None: 7 if s is side else 0)
+    w, g = {"w": torch.zeros(300)}, {"w": torch.ones(300)}
+    opt = ops.AdamW(w, lr=1e-3)
+    made = []
+    monkeypatch.setattr(opt.items, "table", lambda: made.append(1))
+    opt.step(g)
+    with pytest.raises(ValueError, match="step_dev"):
+        opt.step(g, stream=side)
+    one = torch.ones(1, dtype=torch.int64)
+    opt.step(g, stream=side, step_dev=one)  # (its gradients have stayed)
+    assert not made and len(opt.items.captured_grads) == 1
+    it = opt.items
+    it.dev, it.blocks, it.stream, it.ptr, it.device = torch.zeros(8), 1, 0, 4096, -1
+    opt.step(g, stream=side, step_dev=one)
+    assert len(it.captured) == 1 and it.captured[0] is it.dev
+    it.dev = None
+    opt.step(g)
+    assert made and fake.names() == ["pa_adamw", "pa_adamw", "pa_adamw_run", "pa_adamw"]
