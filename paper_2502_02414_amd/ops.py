@@ -341,13 +341,19 @@ class AdamWItems:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
         return self.ptr
 
-    def hold(self, stream, handle):
-        """Keeps the gradients of a step that is captured on a stream (its handle
-        given)."""
+    def hold(self, stream, handle, scalars):
+        """Before a step on a stream (its handle given): of one that is captured, the
+        gradients are kept.  On a stream other than the current one the memory of the
+        gradients, which the next step lets go of, and of the device scalars is not
+        handed out before the step has run."""
         if handle and _capturing(stream):
             now = [d.get("g") for d in self.tensors]
             if not any(all(a is b for a, b in zip(now, had)) for had in self.captured_grads):
                 self.captured_grads.append(now)
+        elif stream is not None and handle != B._stream():
+            for t in (*(d.get("g") for d in self.tensors), *scalars):
+                if t is not None:
+                    t.record_stream(stream)
 
 
 def make_adamw_items(items, table=True) -> AdamWItems:
@@ -394,7 +400,7 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
                       _in(lr_dev, 1, torch.float32, "lr_dev", False),
                       _in(step_dev, 1, torch.int64, "step_dev", False))
     handle = B._stream(stream)
-    items.hold(stream, handle)
+    items.hold(stream, handle, (gscale, lr_dev, step_dev))
     if items.dev is not None:
         _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle),
                                    ctypes.byref(a), handle))

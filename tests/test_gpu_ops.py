@@ -874,3 +874,30 @@ def test_optimizer_captured_on_a_stream_that_is_handed_over():
         torch.cuda.synchronize()
         assert torch.equal(pa, pb), rep
     assert len(hold) == 50
+
+
+def test_gradients_dropped_while_another_stream_has_yet_to_read_them():
+    """Steps on a stream that is kept busy for some milliseconds, each with its own
+    gradients, which the program drops and overwrites at once."""
+    n = 1 << 18
+    g = draw(15)
+    p0 = torch.randn(n, generator=g)
+    pa, pb = dev(p0).clone(), dev(p0).clone()
+    a, b = (ops.AdamW({"w": p}, lr=1e-2, bits=32) for p in (pa, pb))
+    host = [torch.randn(n, generator=g) for _ in range(4)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for h in host:
+        one = dev(h)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(5_000_000)
+        a.step({"w": one}, stream=side)
+        del one
+        a.items.set_grad(0, pb)  # (let go of)
+        for _ in range(3):
+            torch.full((n,), 1e3, device="cuda")
+    side.synchronize()
+    for h in host:
+        b.step({"w": dev(h)})
+    assert torch.equal(pa, pb)

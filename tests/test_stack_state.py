@@ -132,3 +132,20 @@ def test_a_capture_is_looked_for_on_the_stream_of_the_call(fake, monkeypatch):
     it.dev = None
     opt.step(g)
     assert made and fake.names() == ["pa_adamw", "pa_adamw", "pa_adamw_run", "pa_adamw"]
+
+
+def test_gradients_of_a_step_on_another_stream(fake, monkeypatch):
+    """The allocator hears of the stream that reads the gradients and device scalars:
+    the next step lets go of the gradients while that one may not have run."""
+    side = object()
+    monkeypatch.setattr(B, "_stream", lambda s=None: 7 if s is side else 3)
+    seen = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: seen.append((id(t), s)))
+    opt = ops.AdamW({"a": torch.zeros(300), "b": torch.zeros(20)}, lr=1e-3)
+    g = {"a": torch.ones(300), "b": torch.ones(20)}
+    scale = torch.ones(1)
+    monkeypatch.setattr(opt.items, "table", lambda: None)
+    opt.step(g)
+    assert seen == []
+    opt.step(g, gscale=scale, stream=side)
+    assert sorted(seen) == sorted((id(t), side) for t in (g["a"], g["b"], scale))
