@@ -7,9 +7,10 @@
  * synchronised, so every call may be captured into a HIP graph; the host
  * validates the arguments before anything is launched (PA_ERR_INVALID,
  * PA_ERR_UNSUPPORTED, PA_ERR_WORKSPACE, pa_last_error()); results are
- * deterministic; outputs must not alias inputs unless said otherwise; a
- * workspace belongs to one call at a time (calls on two streams, or in two
- * graphs that may run together, need one each).
+ * deterministic; outputs and workspaces must not overlap inputs or each other
+ * unless said otherwise (PA_ERR_INVALID); a workspace belongs to one call at a
+ * time (calls on two streams, or in two graphs that may run together, need one
+ * each).
  *
  *   pa_residual_norm   the joint between a block and the next one: a norm
  *                      after the block, its gate and residual scale, the

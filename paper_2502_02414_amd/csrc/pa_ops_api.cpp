@@ -53,6 +53,31 @@ pa_status dtype_ok(const char* who, int dt) {
              : err(PA_ERR_INVALID, "%s: dtype must be PA_F32 or PA_BF16", who);
 }
 
+// Memory of one tensor of a call (without a pointer or bytes: none).
+struct Span {
+  const char* name;
+  const void* p;
+  uint64_t bytes;
+};
+// Every output apart from the inputs and from the other outputs: kernels read rows
+// ahead of those that they write, and again (a row past the end is the last one).
+template <size_t NO, size_t NI>
+pa_status apart(const char* who, const Span (&out)[NO], const Span (&in)[NI]) {
+  const auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+  };
+  for (size_t i = 0; i < NO; ++i) {
+    for (size_t j = i + 1; j < NO; ++j)
+      if (meet(out[i], out[j]))
+        return err(PA_ERR_INVALID, "%s: %s and %s overlap", who, out[i].name, out[j].name);
+    for (const Span& s : in)
+      if (meet(out[i], s)) return err(PA_ERR_INVALID, "%s: %s and %s overlap", who, out[i].name, s.name);
+  }
+  return PA_OK;
+}
+uint64_t dtype_bytes(int dt) { return dt == PA_BF16 ? 2 : 4; }
+
 // Sizes and parameters of the joint.
 pa_status joint_sizes(const char* who, int64_t N, int C, int dtype) {
   PO_TRY(dtype_ok(who, dtype));
@@ -125,6 +150,10 @@ pa_status pa_residual_norm(int64_t N, int C, pa_dtype dtype, const pa_residual_n
   if (!hq != !hs) return err(PA_ERR_INVALID, "%s: hq and hs go together", who);
   if (p->pre == PA_NORM_NONE && (h || hq))
     return err(PA_ERR_INVALID, "%s: h, hq and hs need a pre norm", who);
+  const uint64_t n = (uint64_t)N * C * dtype_bytes(dtype), v = (uint64_t)C * 4;
+  PO_TRY(apart(who, {{"x1", x1, n}, {"h", h, n}, {"hq", hq, (uint64_t)N * pad16(C)}, {"hs", hs, (uint64_t)N * 4}},
+               {{"x", x, n}, {"y", y, n}, {"t", t, n}, {"post_g", p->post_g, v}, {"post_b", p->post_b, v},
+                {"scale", p->scale, v}, {"pre_g", p->pre_g, v}, {"pre_b", p->pre_b, v}}));
   pa::ResNormArgs a = joint_args(N, C, p);
   a.x = x; a.y = y; a.t = t; a.x1 = x1; a.h = h; a.hq = hq; a.hs = hs;
   if (!h && !hq) a.pre = PA_NORM_NONE;
@@ -180,6 +209,14 @@ pa_status pa_residual_norm_backward(int64_t N, int C, pa_dtype dtype,
   if (sums && (!ws || ws_bytes < bytes))
     return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, bytes);
   if (sums) PO_TRY(opt(who, ws, "ws"));
+  const uint64_t n = (uint64_t)N * C * dtype_bytes(dtype), v = (uint64_t)C * 4;
+  PO_TRY(apart(who,
+               {{"dx", dx, n}, {"dy", dy, n}, {"dt", dt, n}, {"dpost_g", seg.dst[0], v},
+                {"dpost_b", seg.dst[1], v}, {"dscale", seg.dst[2], v}, {"dpre_g", seg.dst[3], v},
+                {"dpre_b", seg.dst[4], v}, {"ws", sums ? ws : nullptr, bytes}},
+               {{"x1", x1, n}, {"y", y, n}, {"t", t, n}, {"dx1", dx1, n}, {"dh", dh, n},
+                {"post_g", p->post_g, v}, {"post_b", p->post_b, v}, {"scale", p->scale, v},
+                {"pre_g", p->pre_g, v}}));
   pa::ResNormArgs a = joint_args(N, C, p);
   a.y = y; a.t = t; a.x1 = const_cast<void*>(x1);
   a.dx1 = dx1; a.dh = dh; a.dx = dx; a.dy = dy; a.dt = dt;
@@ -349,6 +386,8 @@ pa_status pa_adamw_unpack(int64_t n, const void* codes, const float* scales, int
   PO_TRY(need(who, codes, "codes"));
   PO_TRY(need(who, scales, "scales", 4));
   PO_TRY(need(who, out, "out"));
+  PO_TRY(apart(who, {{"out", out, (uint64_t)n * 4}},
+               {{"codes", codes, (uint64_t)n}, {"scales", scales, ((uint64_t)n + 255) / 256 * 4}}));
   PO_HIP(pa::launch_adam_unpack(n, (const uint8_t*)codes, scales, is_signed != 0, out,
                                 as_stream(stream)), who);
   return PA_OK;
@@ -362,6 +401,8 @@ pa_status pa_quant_rows(int64_t N, int K, pa_dtype dtype, const void* x, int8_t*
   PO_TRY(need(who, x, "x"));
   PO_TRY(need(who, q, "q"));
   PO_TRY(need(who, s, "s", 4));
+  PO_TRY(apart(who, {{"q", q, (uint64_t)N * pad16(K)}, {"s", s, (uint64_t)N * 4}},
+               {{"x", x, (uint64_t)N * K * dtype_bytes(dtype)}}));
   PO_HIP(pa::launch_quant_rows(N, K, dtype, x, q, s, as_stream(stream)), who);
   return PA_OK;
 }
@@ -374,6 +415,8 @@ pa_status pa_quant_weight(int K, int F, pa_dtype dtype, const void* W, int8_t* W
   PO_TRY(need(who, W, "W"));
   PO_TRY(need(who, Wq, "Wq"));
   PO_TRY(need(who, sw, "sw", 4));
+  PO_TRY(apart(who, {{"Wq", Wq, (uint64_t)F * pad16(K)}, {"sw", sw, (uint64_t)F * 4}},
+               {{"W", W, (uint64_t)K * F * dtype_bytes(dtype)}}));
   PO_HIP(pa::launch_quant_weight(K, F, dtype, W, Wq, sw, as_stream(stream)), who);
   return PA_OK;
 }
@@ -395,6 +438,18 @@ static pa_status product(const char* who, pa::I8Args& a, int64_t N, int F, int K
   return PA_OK;
 }
 
+// D apart from what the product reads: its rows (of a width in bytes) and their
+// scales, the weights, the bias, and C where D is not C itself; and the workspace,
+// where there is one, from all of them.
+static pa_status product_apart(const char* who, const pa::I8Args& a, pa_dtype d_dtype,
+                               const void* rows, uint64_t width, const float* s, const void* ws,
+                               uint64_t ws_bytes) {
+  const uint64_t N = (uint64_t)a.N, F = (uint64_t)a.F, d = N * F * dtype_bytes(d_dtype);
+  return apart(who, {{"D", a.D, d}, {"ws", ws, ws_bytes}},
+               {{a.x ? "x" : "q", rows, N * width}, {"s", s, N * 4}, {"Wq", a.w, F * (uint64_t)a.Kp},
+                {"sw", a.sw, F * 4}, {"bias", a.bias, F * 4}, {"C", a.C == a.D ? nullptr : a.C, d}});
+}
+
 // The product of rows that are integers.
 static hipError_t integers(const pa::I8Args& a, int d_dtype, hipStream_t st) {
   return d_dtype == PA_BF16 && pa::linear_i8_fused(a.N, a.F, a.K) ? pa::launch_linear_i8(a, st)
@@ -410,6 +465,7 @@ pa_status pa_gemm_i8(int64_t N, int F, int K, const int8_t* q, const float* s, c
   PO_TRY(need(who, q, "q"));
   PO_TRY(need(who, s, "s", 4));
   a.q = q; a.s = s;
+  PO_TRY(product_apart(who, a, d_dtype, q, (uint64_t)a.Kp, s, nullptr, 0));
   PO_HIP(integers(a, d_dtype, as_stream(stream)), who);
   return PA_OK;
 }
@@ -438,6 +494,8 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   if (!ws || ws_bytes < rows + (size_t)N * 4)
     return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, rows + (size_t)N * 4);
   PO_TRY(opt(who, ws, "ws"));
+  PO_TRY(product_apart(who, a, d_dtype, x, (uint64_t)K * dtype_bytes(x_dtype), nullptr, ws,
+                       rows + (uint64_t)N * 4));
   const bool fused =
       x_dtype == PA_BF16 && d_dtype == PA_BF16 && K % 8 == 0 && pa::linear_i8_fused(N, F, K);
   // (of both, for weights of at most 64 KiB and 512 inputs the one-pass product is as

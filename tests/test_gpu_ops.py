@@ -901,3 +901,44 @@ def test_gradients_dropped_while_another_stream_has_yet_to_read_them():
     for h in host:
         b.step({"w": dev(h)})
     assert torch.equal(pa, pb)
+
+
+def test_tensors_side_by_side():
+    """Every tensor of a call cut from one buffer, one right behind the other: neither
+    refused nor written over."""
+    N, C, F = 333, 64, 48
+    p, d = joint_case(N, C, BF16, "layer", "layer", "sigmoid", 1.0, True)
+    buf = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    end = [0]
+
+    def cut(*shape, dt=BF16):
+        n = math.prod(shape) * torch.empty(0, dtype=dt).element_size()
+        t = buf[end[0]:end[0] + n].view(dt).view(shape)
+        end[0] += n + -n % 16
+        return t
+
+    def joint(new):
+        x, y, t = new(N, C), new(N, C), new(N, C)
+        x1, h, hq, hs = new(N, C), new(N, C), new(N, C, dt=torch.int8), new(N, dt=F32)
+        for a, k in ((x, "x"), (y, "y"), (t, "t")):
+            a.copy_(d[k])
+        w = {k: new(C, dt=F32) for k in ("post_g", "post_b", "scale", "pre_g", "pre_b")}
+        for k in w:
+            w[k].copy_(p[k])
+        ops.pa_residual_norm(x, y, ops.make_residual_norm_params(post="layer", pre="layer", **w), x1,
+                             h, t=t, hq=hq, hs=hs)
+        wq, sw, D = new(F, C, dt=torch.int8), new(F, dt=F32), new(N, F)
+        W = new(C, F, dt=F32)
+        W.copy_(torch.randn(C, F, generator=draw(2)) / 8)
+        ops.pa_quant_weight(W, wq, sw)
+        ws = new(N * (C + 4), dt=torch.uint8)
+        ops.pa_linear_i8(h, wq, sw, D, ws)
+        E = new(N, F)
+        ops.pa_gemm_i8(hq, hs, wq, sw, E)
+        return x1, h, hq, hs, wq, sw, D, E, x, y, t
+
+    one = joint(cut)
+    two = joint(lambda *shape, dt=BF16: torch.zeros(*shape, dtype=dt, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(one, two))
+    with pytest.raises(ops.PAError, match="overlap"):
+        ops.pa_linear_i8(one[8], one[4], one[5], one[6], buf[:N * (C + 4)])  # (x lies there)

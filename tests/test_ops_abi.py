@@ -379,3 +379,77 @@ def test_tensors_on_the_cpu_or_not_contiguous_are_refused():
         ops._dev(z(4, 32), "x", 0)
     with pytest.raises(ValueError, match="GPU"):
         ops._in(z(4, 32), 128, torch.float32, "x", True, 0)
+
+
+# ---- tensors of one call that share memory ----
+MB = 1 << 20
+
+
+def apart(names):
+    """Fake addresses a megabyte apart."""
+    return {k: FAKE + (i + 1) * MB for i, k in enumerate(names)}
+
+
+@fake_addresses
+@pytest.mark.parametrize("out,inp", [
+    (o, i) for o in ("x1", "h", "hq", "hs") for i in ("x", "y", "t", "scale", "post_g", "pre_b")])
+@pytest.mark.parametrize("by", ["same", "last bytes"])
+def test_joint_outputs_over_inputs_are_refused(lib, out, inp, by):
+    """100 rows of 64 bf16: 12,800 bytes, int8 rows 6,400, scales 400, vectors 256."""
+    a = apart(("x", "y", "t", "x1", "h", "hq", "hs", "scale", "post_g", "pre_b"))
+    size = {"x1": 12800, "h": 12800, "hq": 6400, "hs": 400}[out]
+    a[inp] = a[out] + (0 if by == "same" else size - 16)
+    p = joint(**{k: a[k] for k in ("scale", "post_g", "pre_b")})
+    refused(lib, lib.pa_residual_norm(100, 64, 1, ctypes.byref(p), a["x"], a["y"], a["t"], a["x1"],
+                                      a["h"], a["hq"], a["hs"], None), INV, f"{out} and {inp} overlap")
+
+
+@fake_addresses
+def test_joint_backward_outputs_over_inputs_are_refused(lib):
+    outs, ins = ("dx", "dy", "dt", "dscale", "ws"), ("x1", "y", "t", "dx1", "dh", "pre_g")
+    size = ctypes.c_size_t(0)
+    assert lib.pa_residual_norm_workspace(5000, 64, 1, ctypes.byref(size)) == B.PA_OK
+
+    def call(a):
+        p, gr = joint(pre_g=a["pre_g"]), ops.pa_residual_norm_grads(None, None, a["dscale"], None, None)
+        return lib.pa_residual_norm_backward(5000, 64, 1, ctypes.byref(p), a["x1"], a["y"], a["t"],
+                                             a["dx1"], a["dh"], a["dx"], a["dy"], a["dt"],
+                                             ctypes.byref(gr), a["ws"], size.value, None)
+
+    for o in outs:
+        for i in ins:
+            a = apart(outs + ins)
+            a[i] = a[o]
+            refused(lib, call(a), INV, f"{o} and {i} overlap")
+    for o, q in (("dx", "dy"), ("dy", "dt"), ("dt", "ws"), ("dscale", "ws")):
+        a = apart(outs + ins)
+        a[q] = a[o]
+        refused(lib, call(a), INV, f"{o} and {q} overlap")
+
+
+@fake_addresses
+def test_product_outputs_over_inputs_are_refused(lib):
+    """1000 rows of 60 (int8: 64) to 64 outputs, bf16."""
+    names = ("q", "s", "w", "sw", "bias", "C", "D", "x", "ws")
+    size = ctypes.c_size_t(0)
+    assert lib.pa_linear_i8_workspace(1000, 64, 60, ctypes.byref(size)) == B.PA_OK
+    gemm = lambda a: lib.pa_gemm_i8(1000, 64, 60, a["q"], a["s"], a["w"], a["sw"], a["bias"], 0,
+                                    a["C"], a["D"], 1, None)
+    linear = lambda a: lib.pa_linear_i8(1000, 64, 60, a["x"], 1, a["w"], a["sw"], a["bias"], 0,
+                                        a["C"], a["D"], 1, a["ws"], size.value, None)
+    for call, o, i, by in ([(gemm, "D", i, 0) for i in ("q", "s", "w", "sw", "bias")] +
+                           [(linear, "D", i, 0) for i in ("x", "w", "sw", "bias", "ws")] +
+                           [(linear, "ws", i, 0) for i in ("x", "w", "sw", "bias", "C")] +
+                           # (C may be D itself, and not a part of it)
+                           [(gemm, "D", "C", 16), (linear, "D", "C", 127984), (gemm, "D", "C", -16)]):
+        a = apart(names)
+        a[i] = a[o] + by
+        name = {"w": "Wq"}.get(i, i)
+        refused(lib, call(a), INV, f"{o} and {name} overlap")
+    refused(lib, lib.pa_quant_rows(10, 8, 1, FAKE, FAKE + 144, FAKE + MB, None), INV, "q and x")
+    refused(lib, lib.pa_quant_rows(10, 8, 1, FAKE, FAKE + MB, FAKE + MB + 156, None), INV, "q and s")
+    refused(lib, lib.pa_quant_weight(8, 8, 1, FAKE, FAKE + 112, FAKE + MB, None), INV, "Wq and W")
+    refused(lib, lib.pa_quant_weight(8, 8, 1, FAKE, FAKE + MB, FAKE + 124, None), INV, "sw and W")
+    refused(lib, lib.pa_adamw_unpack(300, FAKE, FAKE + MB, 1, FAKE + 288, None), INV, "out and codes")
+    refused(lib, lib.pa_adamw_unpack(300, FAKE, FAKE + MB + 1196, 1, FAKE + MB, None), INV,
+            "out and scales")
