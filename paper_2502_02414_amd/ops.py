@@ -306,6 +306,8 @@ class AdamWItems:
 
     def set_grads(self, gs):
         """All gradients, in the items' order."""
+        if len(gs) != self.n:
+            raise ValueError(f"{len(gs)} gradients for {self.n} items")
         cur = _current_device()
         for i, (g, had, d) in enumerate(zip(gs, self.grads, self.tensors)):
             # (one that stayed where it was takes its checks alone)

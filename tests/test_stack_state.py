@@ -149,3 +149,13 @@ def test_gradients_of_a_step_on_another_stream(fake, monkeypatch):
     assert seen == []
     opt.step(g, gscale=scale, stream=side)
     assert sorted(seen) == sorted((id(t), side) for t in (g["a"], g["b"], scale))
+
+
+@pytest.mark.parametrize("n", [0, 1, 3])
+def test_a_gradient_for_every_item(fake, n):
+    """Too few gradients left the others at the last step's, too many were passed over."""
+    it = items_of(300, 400)
+    had = [d["g"] for d in it.tensors]
+    with pytest.raises(ValueError, match="2 items"):
+        it.set_grads([torch.ones(300), torch.ones(400), torch.ones(5)][:n])
+    assert all(d["g"] is g for d, g in zip(it.tensors, had))
