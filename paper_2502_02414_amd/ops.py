@@ -170,10 +170,12 @@ def pa_ops_version() -> int:
 
 # ---- the joint between two blocks ----
 class ResidualNormParams:
-    """The host struct of the joint's parameters and the tensors it points at."""
+    """The host struct of the joint's parameters and the tensors it points at, on
+    one device (None: no tensors)."""
 
     def __init__(self, st, C, tensors):
         self.st, self.C, self.tensors = st, C, tensors
+        self.device = None if C is None else _current_device()
         self.ref = ctypes.byref(st)
         self.pre = st.pre
         self.post = st.post
@@ -208,6 +210,7 @@ def make_residual_norm_params(post=None, pre=None, alpha=1.0, scale=None, gate="
 class ResidualNormGrads:
     def __init__(self, st, C, tensors):
         self.C, self.tensors, self.ref = C, tensors, ctypes.byref(st)
+        self.device = None if C is None else _current_device()
 
 
 def make_residual_norm_grads(dpost_g=None, dpost_b=None, dscale=None, dpre_g=None,
@@ -218,7 +221,16 @@ def make_residual_norm_grads(dpost_g=None, dpost_b=None, dscale=None, dpre_g=Non
     return ResidualNormGrads(pa_residual_norm_grads(*(ptr.get(k) for k in named)), C, named)
 
 
-def _joint(x, name, par, gr=None):
+def _here(had, name, cur):
+    """Refuses a struct whose pointers are another device's than the current one."""
+    if had is not None and had != cur:
+        raise ValueError(f"{name}: on device {had}, not on the current one")
+
+
+def _joint(x, name, par, cur, gr=None):
+    _here(par.device, "the parameters", cur)
+    if gr is not None:
+        _here(gr.device, "the gradients", cur)
     if x.dim() != 2:
         raise ValueError(f"{name} must be [N, C]")
     N, C = x.shape
@@ -237,7 +249,8 @@ def padded(K: int) -> int:
 def pa_residual_norm(x, y, par, x1, h=None, t=None, hq=None, hs=None, stream=None):
     """x1 = alpha x + scale gate(t) post(y); h = pre(x1), in x's dtype (h) and /
     or as int8 rows hq [N, padded(C)] with scales hs [N]."""
-    N, C, n, code = _joint(x, "x", par)
+    cur = _current_device()
+    N, C, n, code = _joint(x, "x", par, cur)
     dt = x.dtype
     if hq is not None:
         torch = _torch()
@@ -245,7 +258,6 @@ def pa_residual_norm(x, y, par, x1, h=None, t=None, hq=None, hs=None, stream=Non
         hsp = _in(hs, N, torch.float32, "hs")
     else:
         hqp, hsp = None, (None if hs is None else _dev(hs, "hs"))
-    cur = _current_device()
     _check(load().pa_residual_norm(
         N, C, code, par.ref, _dev(x, "x", cur), _in(y, n, dt, "y", True, cur),
         None if t is None else _in(t, n, dt, "t", True, cur), _in(x1, n, dt, "x1", True, cur),
@@ -263,9 +275,9 @@ def pa_residual_norm_backward(x1, y, par, dx1, dh, dx, dy, gr=None, ws=None, t=N
                               stream=None):
     """The chain rule: dx1 and dh (either may be None) to dx, dy, dt and the
     parameters' gradients gr (make_residual_norm_grads)."""
-    N, C, n, code = _joint(x1, "x1", par, gr)
-    ty = x1.dtype
     cur = _current_device()
+    N, C, n, code = _joint(x1, "x1", par, cur, gr)
+    ty = x1.dtype
     _check(load().pa_residual_norm_backward(
         N, C, code, par.ref, _dev(x1, "x1", cur), _in(y, n, ty, "y", True, cur),
         _in(t, n, ty, "t", False, cur), _in(dx1, n, ty, "dx1", False, cur),
@@ -285,6 +297,7 @@ class AdamWItems:
 
     def __init__(self, n):
         self.n = n
+        self.home = None  # the tensors' device (None: no tensors yet)
         self.arr = (pa_adamw_item * max(n, 1))()
         self.tensors = [None] * n
         self.dev, self.blocks, self.moved = None, 0, 0
@@ -321,6 +334,7 @@ class AdamWItems:
         """Makes the device table (a copy from host memory that has arrived when
         this returns, so that every stream may read it)."""
         torch = _torch()
+        _here(self.home, "items", _current_device())
         size, blocks = ctypes.c_size_t(0), ctypes.c_int64(0)
         _check(load().pa_adamw_table_size(self.n, self.arr, ctypes.byref(size),
                                           ctypes.byref(blocks)))
@@ -329,13 +343,11 @@ class AdamWItems:
         dev = host.to("cuda")
         torch.cuda.current_stream().synchronize()
         self.dev, self.blocks, self.stream = dev, blocks.value, B._stream()
-        self.ptr, self.device = dev.data_ptr(), dev.get_device()
+        self.ptr = dev.data_ptr()
 
     def on(self, stream, handle):
         """The table's pointer for a launch on a stream (its handle given); a
         stream other than the table's keeps its memory from being handed out."""
-        if _current_device() != self.device:
-            raise ValueError(f"items: on device {self.device}, not on the current one")
         if handle and _capturing(stream):  # (the default stream cannot be captured)
             if not any(t is self.dev for t in self.captured):
                 self.captured.append(self.dev)
@@ -366,6 +378,8 @@ def make_adamw_items(items, table=True) -> AdamWItems:
     torch = _torch()
     f32 = torch.float32
     out = AdamWItems(len(items))
+    if items:
+        out.home = _current_device()
     for i, d in enumerate(items):
         extra = set(d) - {"p", "g", "m", "v", "m_scale", "v_scale", "copy", "wd"}
         if extra:
@@ -396,6 +410,7 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
     scalar that every gradient is multiplied by; lr_dev (fp32), step_dev
     (int64): device scalars in place of lr and step, for captured graphs."""
     torch = _torch()
+    _here(items.home, "items", _current_device())
     a = pa_adamw_args(float(lr), float(beta1), float(beta2), float(eps), int(step),
                       int(seed) & 0xFFFFFFFFFFFFFFFF,
                       _in(gscale, 1, torch.float32, "gscale", False),

@@ -159,3 +159,30 @@ def test_a_gradient_for_every_item(fake, n):
     with pytest.raises(ValueError, match="2 items"):
         it.set_grads([torch.ones(300), torch.ones(400), torch.ones(5)][:n])
     assert all(d["g"] is g for d, g in zip(it.tensors, had))
+
+
+def test_structs_of_another_device_are_refused(fake, monkeypatch):
+    """Parameters, gradients and items are pointers that were checked where they were
+    made: with another current device a call refuses them, with a table or without."""
+    x, w = torch.zeros(10, 32), torch.ones(32)
+    par, none = ops.make_residual_norm_params(pre="rms", pre_g=w), ops.make_residual_norm_params(pre="rms")
+    gr = ops.make_residual_norm_grads(dpre_g=w)
+    it = items_of(300)
+    at = [0]
+    monkeypatch.setattr(ops, "_current_device", lambda: at[0])
+    monkeypatch.setattr(ops, "_in", lambda t, *a: None if t is None else t.data_ptr())
+    for bad in (lambda: ops.pa_residual_norm(x, x, par, x, x),
+                lambda: ops.pa_residual_norm_backward(x, x, par, x, x, x, x),
+                lambda: ops.pa_residual_norm_backward(x, x, none, x, x, x, x, gr),
+                lambda: ops.pa_adamw(it, lr=1e-3), it.table):
+        with pytest.raises(ValueError, match="current one"):
+            bad()
+    it.dev, it.blocks, it.stream, it.ptr = torch.zeros(8), 1, 0, 4096
+    with pytest.raises(ValueError, match="current one"):
+        ops.pa_adamw(it, lr=1e-3)
+    assert fake.calls == []
+    ops.pa_residual_norm(x, x, none, x, x)  # (nothing that could be elsewhere)
+    at[0] = -1
+    ops.pa_residual_norm(x, x, par, x, x)
+    ops.pa_adamw(it, lr=1e-3)
+    assert fake.names() == ["pa_residual_norm"] * 2 + ["pa_adamw_run"]
