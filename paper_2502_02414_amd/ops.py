@@ -434,6 +434,11 @@ def pa_adamw_unpack(codes, scales, out, signed, stream=None):
         int(bool(signed)), _in(out, n, torch.float32, "out"), B._stream(stream)))
 
 
+def _version(t):
+    """How often torch has written a tensor (this library's calls do not count)."""
+    return None if t.is_inference() else t._version
+
+
 class AdamW:
     """AdamW over named fp32 tensors, e.g. a block stack's parameters: the
     moments (fp32, or 8 bits where a tensor has at least ``small`` elements)
@@ -441,17 +446,22 @@ class AdamW:
 
     params: {name: fp32 tensor}; copies: {name: bf16 tensor} that receive the
     parameters rounded (what the stack's products read); decay: names with
-    weight decay (default: tensors of more than one dimension)."""
+    weight decay (default: tensors of more than one dimension); where: {name:
+    (dict, key)}, the places that the program reads a parameter, or its copy, from.
+
+    A step refuses what would be lost in it: a copy that torch has written since the
+    last one (``refresh`` takes the parameter from it), and another tensor in a
+    place of ``where``."""
 
     def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, wd=0.01, bits=32, copies=None,
-                 decay=None, small=4096, seed=0):
+                 decay=None, small=4096, seed=0, where=None):
         torch = _torch()
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
         self.lr, self.betas, self.eps, self.seed, self.t = lr, betas, eps, seed, 0
         self.names = list(params)
-        copies = copies or {}
-        unknown = [k for k in list(copies) + list(decay or ()) if k not in params]
+        copies, where = dict(copies or {}), where or {}
+        unknown = [k for k in [*copies, *(decay or ()), *where] if k not in params]
         if unknown:
             raise ValueError(f"not among the parameters: {unknown}")
         items = []
@@ -467,6 +477,26 @@ class AdamW:
                 d["m"], d["v"] = torch.zeros_like(p), torch.zeros_like(p)
             items.append(d)
         self.items = make_adamw_items(items)
+        self.copies = copies
+        self.versions = {k: _version(c) for k, c in copies.items()}
+        self.where = [(k, *at, copies.get(k, params[k])) for k, at in where.items()]
+
+    def refresh(self):
+        """The parameters from their copies, after the program has written those (a
+        checkpoint's weights, say); the moments stay."""
+        for k, c in self.copies.items():
+            self.items.tensors[self.names.index(k)]["p"].copy_(c)
+            self.versions[k] = _version(c)
+
+    def _unchanged(self):
+        for k, d, key, t in self.where:
+            if d.get(key) is not t:
+                raise ValueError(f"{k}: another tensor has taken its place, and this optimizer "
+                                 "holds the one before; it needs an optimizer of its own")
+        for k, c in self.copies.items():
+            if _version(c) != self.versions[k]:
+                raise ValueError(f"{k}: its copy was written since the last step, which this one "
+                                 "would undo; refresh() takes the parameter from it")
 
     def step(self, grads, gscale=None, lr=None, stream=None, lr_dev=None, step_dev=None):
         """grads: {name: tensor} for every parameter (fp32 or bf16).  A step that
@@ -477,6 +507,7 @@ class AdamW:
         capturing = _capturing(stream)
         if step_dev is None and capturing:
             raise ValueError("a step captured into a graph needs step_dev")
+        self._unchanged()
         it = self.items
         before = it.moved
         it.set_grads([grads[k] for k in self.names])

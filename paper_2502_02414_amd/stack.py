@@ -98,12 +98,15 @@ class BlockStack:
 
     def adamw(self, lr, **kw):
         """ops.AdamW over the stack's parameters: those in bf16 (W1, W2) as fp32
-        ones whose rounded copies are the stack's.  step(named_grads(grads))."""
+        ones whose rounded copies are the stack's.  step(named_grads(grads)), which
+        refuses to go on where a parameter of the stack is another tensor by then, or
+        W1 or W2 have been written (then ``refresh`` of the optimizer first)."""
         named = self.named_parameters()
         f32 = self.torch.float32
         copies = {k: v for k, v in named.items() if v.dtype != f32}
+        where = {f"{l}.{k}": (p, k) for l, p in enumerate(self.params) for k in p}
         return ops.AdamW({k: v.float() if k in copies else v for k, v in named.items()}, lr,
-                         copies=copies, **kw)
+                         copies=copies, where={k: where[k] for k in named}, **kw)
 
     @staticmethod
     def named_grads(grads):

@@ -234,3 +234,34 @@ def test_quantised_inference_in_a_graph(kind, dt):
             assert torch.equal(out, want), rep
         seen.append(want)
     assert all(not torch.equal(a, b) for a, b in zip(seen, seen[1:]))
+
+
+def test_training_goes_on_from_weights_that_were_loaded():
+    """bf16 weights loaded in place between two steps: refused, then, refreshed, a step
+    from the loaded weights."""
+    s, x, Gs, w = make(1001, 64, 16, 2, BF16, SandwichStack)
+    t, *_ = make(1001, 64, 16, 2, BF16, SandwichStack, seed=1)
+    opt = s.adamw(lr=1e-2, wd=0.1, seed=4)
+
+    def grads():
+        s.forward(x, Gs)
+        return s.named_grads(s.backward(w)[1])
+
+    opt.step(grads())
+    for p, q in zip(s.params, t.params):
+        for k in ("W1", "W2"):
+            p[k].copy_(q[k])
+    g = grads()
+    with pytest.raises(ValueError, match="refresh"):
+        opt.step(g)
+    opt.refresh()
+    flat = lambda: [{k: v.cpu().reshape(-1) if torch.is_tensor(v) else v for k, v in d.items()
+                     if v is not None} for d in opt.items.tensors]
+    before = flat()
+    for d, k in zip(before, opt.names):
+        d["g"] = g[k].cpu().reshape(-1)
+        if k.endswith(("W1", "W2")):
+            l, name = k.split(".")
+            assert torch.equal(d["p"], t.params[int(l)][name].float().cpu().reshape(-1))
+    opt.step(g)
+    check_step(before, flat(), 2, 4, lr=1e-2)

@@ -186,3 +186,50 @@ def test_structs_of_another_device_are_refused(fake, monkeypatch):
     ops.pa_residual_norm(x, x, par, x, x)
     ops.pa_adamw(it, lr=1e-3)
     assert fake.names() == ["pa_residual_norm"] * 2 + ["pa_adamw_run"]
+
+
+def grads_of(s):
+    return {k: torch.ones_like(v, dtype=torch.float32) for k, v in s.named_parameters().items()}
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+def test_a_step_for_tensors_that_the_stack_has_no_more(fake, dt):
+    """A tensor put in a parameter's place: the optimizer would go on with the one
+    before and the stack would never see a step."""
+    s = stack(dt=dt)
+    opt = s.adamw(lr=1e-3)
+    g = grads_of(s)
+    opt.step(g)
+    for name in ("W1", "bp", "ln2_g"):
+        p = s.params[1]
+        had, p[name] = p[name], p[name].clone()
+        with pytest.raises(ValueError, match="1." + name):
+            opt.step(g)
+        p[name] = had
+    del s.params[0]["b"]
+    with pytest.raises(ValueError, match="0.b"):
+        opt.step(g)
+    assert fake.names() == ["pa_adamw"] and opt.t == 1
+
+
+def test_a_bf16_weight_that_was_written(fake):
+    """A checkpoint loaded in place: the step would write the old fp32 parameter's
+    rounding over it.  Refused until refresh() has taken it over."""
+    s = stack()
+    opt = s.adamw(lr=1e-3)
+    g = grads_of(s)
+    opt.items.table = lambda: None
+    opt.step(g)
+    w = s.params[0]["W1"]
+    master = opt.items.tensors[opt.names.index("0.W1")]["p"]
+    w.copy_(torch.full_like(w, 3.0))
+    with pytest.raises(ValueError, match="0.W1.*refresh"):
+        opt.step(g)
+    assert fake.names() == ["pa_adamw"] and not (master == 3).all()
+    opt.refresh()
+    assert (master == 3).all()
+    s.params[0]["Wp"].add_(1)  # (fp32: the optimizer's own)
+    opt.step(g)
+    assert fake.names() == ["pa_adamw"] * 2 and opt.t == 2
+    with torch.inference_mode():  # (their writes are not counted)
+        ops.AdamW({"w": torch.zeros(20)}, lr=1e-3, copies={"w": torch.zeros(20, dtype=torch.bfloat16)})
