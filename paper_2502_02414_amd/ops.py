@@ -488,6 +488,42 @@ class AdamW:
             self.items.tensors[self.names.index(k)]["p"].copy_(c)
             self.versions[k] = _version(c)
 
+    def state(self):
+        """What the next steps depend on beside the parameters that the program holds
+        itself, in new tensors: the count of the steps, the seed, the moments as they
+        are kept (codes and scales of 8 bits) and the parameters that have copies."""
+        return {"t": self.t, "seed": self.seed,
+                "tensors": {k: {s: t.detach().clone() for s, t in d.items()}
+                            for k, d in self._kept().items()}}
+
+    def _kept(self):
+        return {k: {s: d[s] for s in ("p", "m", "v", "m_scale", "v_scale")
+                    if d.get(s) is not None and (s != "p" or k in self.copies)}
+                for k, d in zip(self.names, self.items.tensors)}
+
+    def load_state(self, state):
+        """``state`` of an optimizer over the same names and sizes, with moments of
+        the same bits, put into this one's tensors (also where graphs read them);
+        copies are rounded from their parameters."""
+        mine, tensors = self._kept(), state["tensors"]
+        if set(tensors) != set(mine):
+            raise ValueError(f"names that differ: {sorted(set(tensors) ^ set(mine))}")
+        for k, d in mine.items():
+            if set(d) != set(tensors[k]):
+                raise ValueError(f"{k}: has {sorted(d)}, the state {sorted(tensors[k])}")
+            for s, t in d.items():
+                o = tensors[k][s]
+                if o.shape != t.shape or o.dtype != t.dtype:
+                    raise ValueError(f"{k}: {s} is {list(t.shape)} {t.dtype}, the state's "
+                                     f"{list(o.shape)} {o.dtype}")
+        for k, d in mine.items():
+            for s, t in d.items():
+                t.copy_(tensors[k][s])
+            if k in self.copies:
+                self.copies[k].copy_(d["p"])
+                self.versions[k] = _version(self.copies[k])
+        self.t, self.seed = int(state["t"]), int(state["seed"])
+
     def _unchanged(self):
         for k, d, key, t in self.where:
             if d.get(key) is not t:

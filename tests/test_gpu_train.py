@@ -265,3 +265,34 @@ def test_training_goes_on_from_weights_that_were_loaded():
             assert torch.equal(d["p"], t.params[int(l)][name].float().cpu().reshape(-1))
     opt.step(g)
     check_step(before, flat(), 2, 4, lr=1e-2)
+
+
+@pytest.mark.parametrize("kind,dt,bits", [(SandwichStack, BF16, 8), (BlockStack, BF16, 32),
+                                          (BlockStack, F32, 8)])
+def test_training_goes_on_from_a_state(kind, dt, bits, tmp_path):
+    """Parameters and the optimizer's state saved after two steps and loaded into a stack
+    of its own: the next two steps bit for bit."""
+    s, x, Gs, w = make(1001, 64, 16, 2, dt, kind)
+    t, *_ = make(1001, 64, 16, 2, dt, kind, seed=1)
+    t.tuned = s.tuned
+    a, b = s.adamw(lr=1e-2, bits=bits, seed=4), t.adamw(lr=1e-2, bits=bits)
+
+    def step(k, opt):
+        k.forward(x, Gs)
+        opt.step(k.named_grads(k.backward(w)[1]))
+
+    for _ in range(2):
+        step(s, a)
+    torch.save({"params": s.named_parameters(), "state": a.state()}, tmp_path / "c.pt")
+    got = torch.load(tmp_path / "c.pt", weights_only=True)
+    for k, v in t.named_parameters().items():
+        v.copy_(got["params"][k])
+    b.load_state(got["state"])
+    for rep in range(2):
+        step(s, a)
+        step(t, b)
+        for k, v in s.named_parameters().items():
+            assert torch.equal(v, t.named_parameters()[k]), (rep, k)
+        for k in a.names:
+            assert all(torch.equal(m, n) for m, n in zip(a.moments(k), b.moments(k))), (rep, k)
+    assert a.t == b.t == 4

@@ -233,3 +233,33 @@ def test_a_bf16_weight_that_was_written(fake):
     assert fake.names() == ["pa_adamw"] * 2 and opt.t == 2
     with torch.inference_mode():  # (their writes are not counted)
         ops.AdamW({"w": torch.zeros(20)}, lr=1e-3, copies={"w": torch.zeros(20, dtype=torch.bfloat16)})
+
+
+def test_state_of_an_optimizer(fake):
+    s = stack()
+    a = s.adamw(lr=1e-3, bits=8, seed=5)
+    for d in a.items.tensors:  # (as if after some steps)
+        for k in ("m", "v", "m_scale", "v_scale"):
+            if d.get(k) is not None:
+                d[k].copy_(torch.randint(0, 100, d[k].shape))
+    a.items.tensors[a.names.index("0.W1")]["p"].fill_(1 + 2 ** -12)
+    a.t = 7
+    st = a.state()
+    assert "p" in st["tensors"]["0.W1"] and "p" not in st["tensors"]["0.Wp"]
+    a.items.tensors[0]["m"].zero_()  # (new tensors)
+    b = stack().adamw(lr=1e-3, bits=8)
+    b.load_state(st)
+    assert b.t == 7 and b.seed == 5
+    for k, d in zip(b.names, b.items.tensors):
+        for key, v in st["tensors"][k].items():
+            assert torch.equal(d[key], v), (k, key)
+    copy = b.items.tensors[b.names.index("0.W1")]["copy"]
+    assert torch.equal(copy, torch.ones_like(copy))
+    b.step({k: torch.ones_like(d["p"]) for k, d in zip(b.names, b.items.tensors)})
+    had = b.state()
+    for other in (stack().adamw(lr=1e-3), stack(L=1).adamw(lr=1e-3, bits=8),
+                  stack(C=32).adamw(lr=1e-3, bits=8), stack(dt=torch.float32).adamw(lr=1e-3, bits=8)):
+        with pytest.raises(ValueError):
+            b.load_state(other.state())
+    for k, d in b.state()["tensors"].items():
+        assert all(torch.equal(v, had["tensors"][k][key]) for key, v in d.items())
