@@ -434,7 +434,7 @@ def pa_adamw_unpack(codes, scales, out, signed, stream=None):
         int(bool(signed)), _in(out, n, torch.float32, "out"), B._stream(stream)))
 
 
-def _version(t):
+def version(t):
     """How often torch has written a tensor (this library's calls do not count)."""
     return None if t.is_inference() else t._version
 
@@ -447,14 +447,15 @@ class AdamW:
     params: {name: fp32 tensor}; copies: {name: bf16 tensor} that receive the
     parameters rounded (what the stack's products read); decay: names with
     weight decay (default: tensors of more than one dimension); where: {name:
-    (dict, key)}, the places that the program reads a parameter, or its copy, from.
+    (dict, key)}, the places that the program reads a parameter, or its copy, from;
+    after: called after every step.
 
     A step refuses what would be lost in it: a copy that torch has written since the
     last one (``refresh`` takes the parameter from it), and another tensor in a
     place of ``where``."""
 
     def __init__(self, params, lr, betas=(0.9, 0.999), eps=1e-8, wd=0.01, bits=32, copies=None,
-                 decay=None, small=4096, seed=0, where=None):
+                 decay=None, small=4096, seed=0, where=None, after=None):
         torch = _torch()
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
@@ -477,8 +478,8 @@ class AdamW:
                 d["m"], d["v"] = torch.zeros_like(p), torch.zeros_like(p)
             items.append(d)
         self.items = make_adamw_items(items)
-        self.copies = copies
-        self.versions = {k: _version(c) for k, c in copies.items()}
+        self.copies, self.after = copies, after
+        self.versions = {k: version(c) for k, c in copies.items()}
         self.where = [(k, *at, copies.get(k, params[k])) for k, at in where.items()]
 
     def refresh(self):
@@ -486,7 +487,7 @@ class AdamW:
         checkpoint's weights, say); the moments stay."""
         for k, c in self.copies.items():
             self.items.tensors[self.names.index(k)]["p"].copy_(c)
-            self.versions[k] = _version(c)
+            self.versions[k] = version(c)
 
     def state(self):
         """What the next steps depend on beside the parameters that the program holds
@@ -521,7 +522,7 @@ class AdamW:
                 t.copy_(tensors[k][s])
             if k in self.copies:
                 self.copies[k].copy_(d["p"])
-                self.versions[k] = _version(self.copies[k])
+                self.versions[k] = version(self.copies[k])
         self.t, self.seed = int(state["t"]), int(state["seed"])
 
     def _unchanged(self):
@@ -530,7 +531,7 @@ class AdamW:
                 raise ValueError(f"{k}: another tensor has taken its place, and this optimizer "
                                  "holds the one before; it needs an optimizer of its own")
         for k, c in self.copies.items():
-            if _version(c) != self.versions[k]:
+            if version(c) != self.versions[k]:
                 raise ValueError(f"{k}: its copy was written since the last step, which this one "
                                  "would undo; refresh() takes the parameter from it")
 
@@ -553,6 +554,8 @@ class AdamW:
                  self.seed, gscale, lr_dev, step_dev, stream)
         if step_dev is None:
             self.t += 1
+        if self.after is not None:
+            self.after()
 
     def moments(self, name):
         """(m, v) of a parameter as fp32 tensors."""

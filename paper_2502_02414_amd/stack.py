@@ -35,6 +35,8 @@ plus the float b_t.
 """
 from __future__ import annotations
 
+import weakref
+
 from . import binding as B
 from . import ops
 
@@ -62,6 +64,8 @@ class BlockStack:
         self.dev = device
         self.ws_int8 = None
         self.int8 = None  # per layer: W1 and W2 as integers with scales (quantize)
+        self.int8_of = None  # what they were made from
+        self.steps = 0  # of the optimizers that adamw has made
 
     # -- helpers ------------------------------------------------------------
     def _e(self, *shape, dt=None):
@@ -105,8 +109,12 @@ class BlockStack:
         f32 = self.torch.float32
         copies = {k: v for k, v in named.items() if v.dtype != f32}
         where = {f"{l}.{k}": (p, k) for l, p in enumerate(self.params) for k in p}
+
+        def after():
+            self.steps += 1
+
         return ops.AdamW({k: v.float() if k in copies else v for k, v in named.items()}, lr,
-                         copies=copies, where={k: where[k] for k in named}, **kw)
+                         copies=copies, where={k: where[k] for k in named}, after=after, **kw)
 
     @staticmethod
     def named_grads(grads):
@@ -250,19 +258,35 @@ class BlockStack:
         return dy, grads
 
     # -- inference ------------------------------------------------------------
+    def _weights(self):
+        return [p[k] for p in self.params for k in ("W1", "W2")]
+
     def quantize(self):
         """The MLP's weights in 8-bit integers with a scale per output channel, for
-        ``infer``; again after the weights have changed.  Every call writes the same
-        tensors, so that an ``infer`` in a graph replays with the integers of the
-        moment."""
+        ``infer``; again after the weights have changed: ``infer`` refuses integers of
+        weights that were written since (by torch, or a step of ``adamw``'s optimizer; of
+        a replayed graph's it cannot know) or of tensors that are others by then.  Every
+        call writes the same tensors, so that an ``infer`` in a graph replays with the
+        integers of the moment."""
         if self.int8 is None:
             self.int8 = [(*ops.empty_weight(p["W1"]), *ops.empty_weight(p["W2"]))
                          for p in self.params]
+        self.int8_of = None
         for p, (w1, s1, w2, s2) in zip(self.params, self.int8):
             ops.pa_quant_weight(p["W1"], w1, s1)
             ops.pa_quant_weight(p["W2"], w2, s2)
+        # (how often they were written: by adamw's optimizers, and by torch)
+        self.int8_of = self.steps, [(weakref.ref(t), ops.version(t)) for t in self._weights()]
         if self.ws_int8 is None:
             self.ws_int8 = ops.linear_i8_workspace(self.N, 4 * self.C, self.C, self.dev)
+
+    def _ready(self):
+        if self.int8 is None:
+            return
+        steps, of = self.int8_of or (None, ())  # (None: a quantize that did not end)
+        if steps != self.steps or any(ref() is not t or n != ops.version(t)
+                                      for (ref, n), t in zip(of, self._weights())):
+            raise ValueError("the weights have changed since quantize: call it again")
 
     def _mlp_infer(self, l, h2, x1=None):
         p, N, C = self.params[l], self.N, self.C
@@ -277,6 +301,7 @@ class BlockStack:
     def infer(self, x, Gs):
         """``forward`` with nothing kept for a backward and, after ``quantize``, the
         MLP in 8-bit integers."""
+        self._ready()
         N, C = self.N, self.C
         m, r = self._f(N), self._f(N)
         for l, (p, G) in enumerate(zip(self.params, Gs)):
@@ -383,6 +408,7 @@ class SandwichStack(BlockStack):
         return out, grads
 
     def infer(self, x, Gs):
+        self._ready()
         N, C = self.N, self.C
         h = self._first_norm(x, self._f(N), self._f(N))
         for l, (p, G) in enumerate(zip(self.params, Gs)):

@@ -296,3 +296,22 @@ def test_training_goes_on_from_a_state(kind, dt, bits, tmp_path):
         for k in a.names:
             assert all(torch.equal(m, n) for m, n in zip(a.moments(k), b.moments(k))), (rep, k)
     assert a.t == b.t == 4
+
+
+@pytest.mark.parametrize("kind,dt", [(BlockStack, BF16), (SandwichStack, F32)])
+def test_quantised_inference_after_a_step(kind, dt):
+    """Refused with the integers of the weights before the step; quantised again, as a
+    stack that never had other weights."""
+    s, x, Gs, w = make(1001, 64, 16, 2, dt, kind)
+    opt = s.adamw(lr=1e-2)
+    s.quantize()
+    s.infer(x, Gs)
+    s.forward(x, Gs)
+    opt.step(s.named_grads(s.backward(w)[1]))
+    with pytest.raises(ValueError, match="quantize"):
+        s.infer(x, Gs)
+    s.quantize()
+    got = s.infer(x, Gs)
+    t = kind(1001, 64, 4, 16, s.params, dt)
+    t.quantize()
+    assert torch.equal(got, t.infer(x, Gs))

@@ -263,3 +263,36 @@ def test_state_of_an_optimizer(fake):
             b.load_state(other.state())
     for k, d in b.state()["tensors"].items():
         assert all(torch.equal(v, had["tensors"][k][key]) for key, v in d.items())
+
+
+@pytest.mark.parametrize("kind", [BlockStack, SandwichStack])
+def test_infer_with_integers_of_other_weights(fake, monkeypatch, kind):
+    """After an optimizer's step, a write or another tensor infer answered with the last
+    quantize's integers."""
+    monkeypatch.setattr(ops, "residual_norm_workspace", lambda *a: torch.empty(8))
+    for name in ("pa_layernorm", "pa_mlp_up", "pa_gemm"):
+        monkeypatch.setattr(B, name, lambda *a, **kw: None)
+    monkeypatch.setattr(kind, "_attention", lambda self, p, c, h, G: torch.empty_like(h))
+    s = stack(kind)
+    x, Gs = torch.zeros(100, 64, dtype=torch.bfloat16), [None, None]
+    opt = s.adamw(lr=1e-3)
+    opt.items.table = lambda: None
+
+    def put(l, k):
+        s.params[l][k] = s.params[l][k].clone()
+
+    s.infer(x, Gs)  # (no integers: the weights themselves)
+    opt.step(grads_of(s))
+    s.quantize()
+    s.infer(x, Gs)
+    s.params[0]["bp"].add_(1)  # (not quantised)
+    s.infer(x, Gs)
+    for change in (lambda: opt.step(grads_of(s)), lambda: s.params[1]["W2"].mul_(2),
+                   lambda: put(0, "W1")):
+        change()
+        for _ in range(2):
+            with pytest.raises(ValueError, match="quantize"):
+                s.infer(x, Gs)
+        s.quantize()
+        s.infer(x, Gs)
+        opt.refresh()
