@@ -16,10 +16,9 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 // over 4,001 points).  Half of the kernels' vector instructions: one exp2, the time of
 // four others, and a few more than the polynomial's.
 //
-// bf16 results: degree 6 over [0, 9].  In fp32 against 64 bits: relative 2.1e-5 for
-// x > -4, 1.5e-4 down to -5, 3.8e-4 to -6, below that 1e-12 absolute; half a bf16
-// step is 2e-3 to 3.9e-3.  (A million rows, 256 to 1024, on one card: degree 7 674 us,
-// 6 650, 5 640 but 0.5% off at -4.5.)
+// bf16 results: degree 7 over [0, 9].  In fp32 against 64 bits: relative 1.8e-5 for
+// x > -3, 3.6e-5 down to -4, 1.1e-4 to -6, 3.8e-4 to -9, below that 1.1e-18 absolute;
+// half a bf16 step is 2e-3 to 3.9e-3.  (Degree 6 is 1% off at -7, 32% at -9.)
 //
 // fp32 results: degree 10 over [0, 8].  Relative 6e-7 for x > -2, 1.1e-6 down to -4,
 // 6e-6 to -5, 1.2e-4 to -6, below that 1e-10 absolute (0.5 x (1 + erf) in fp32, which
@@ -30,13 +29,14 @@ __device__ __forceinline__ float tail_of(float x, float z, float p) {
 template <typename T> __device__ __forceinline__ float gelu_for(float x) {
   if constexpr (sizeof(T) == 2) {
     const float z = __builtin_elementwise_minimum(fabsf(x), 9.f);
-    float p = 2.65611924987752e-05f;
-    p = fmaf(p, z, -0.000669357308652252f);
-    p = fmaf(p, z, 0.0075453296303749084f);
-    p = fmaf(p, z, -0.05213657766580582f);
-    p = fmaf(p, z, -0.46012184023857117f);
-    p = fmaf(p, z, -1.15067458152771f);
-    return tail_of(x, z, fmaf(p, z, -1.0000303983688354f));
+    float p = -1.2643212130569736e-06f;
+    p = fmaf(p, z, 4.878497202298604e-05f);
+    p = fmaf(p, z, -0.0008188498904928565f);
+    p = fmaf(p, z, 0.008031141944229603f);
+    p = fmaf(p, z, -0.05292445048689842f);
+    p = fmaf(p, z, -0.45953628420829773f);
+    p = fmaf(p, z, -1.1508264541625977f);
+    return tail_of(x, z, fmaf(p, z, -1.0000252723693848f));
   } else {
     const float z = __builtin_elementwise_minimum(fabsf(x), 8.f);
     float p = -2.5640650491709494e-08f;

@@ -12,11 +12,11 @@
 // Results leave from the registers, 64 bytes of a point's row per instruction.
 //
 // Measured, a million rows of bf16: 256 to 1024 channels 518 us (4.9 TB/s, what a
-// copy reaches), with GELU 630 to 690 us by the card; 1024 to 256 with a residual
+// copy reaches), with GELU 659 to 672 us on that card; 1024 to 256 with a residual
 // 677 us (4.5 TB/s); 256 to 256 214 us, 64 to 256 with GELU 206 us, 256 to 64
 // 174 us.  As two launches, quantised rows through memory and tiles: 1064, 1200,
-// 1217, 377, 272 and 334 us.  With GELU the vector units bound it: 16 issue slots an
-// output (the exp2 takes four), 1.2M cycles of four per CU at a million rows,
+// 1217, 377, 272 and 334 us.  With GELU the vector units bound it: 17 issue slots an
+// output (the exp2 takes four), 1.3M cycles of four per CU at a million rows,
 // beside 0.25M of the matrix cores.  Before the loads and stores lost their
 // branches the compiler waited for each at once: 1024 to 256 838 us.  Issuing the
 // products among the activation's instructions, run by run, changed nothing; with

@@ -942,3 +942,26 @@ def test_tensors_side_by_side():
     assert all(torch.equal(a, b) for a, b in zip(one, two))
     with pytest.raises(ops.PAError, match="overlap"):
         ops.pa_linear_i8(one[8], one[4], one[5], one[6], buf[:N * (C + 4)])  # (x lies there)
+
+
+@pytest.mark.parametrize("N,F", [(7, 8), (900, 8), (4000, 64), (4000, 33)])
+def test_gelu_keeps_its_digits_in_the_lower_tail(N, F):
+    """bf16 results from -9 to -2, of every kernel that has a GELU: half a step, and
+    4e-4 of the value beside what the sum's and the scale's roundings move it by (three
+    of 2^-24, with GELU's slope of at most x^2 + 1 of the value per relative step)."""
+    u = torch.linspace(-9, -2, N)
+    x = u[:, None].clone()
+    D = [torch.empty(N, F, dtype=BF16, device="cuda") for _ in range(2)]
+    w = torch.zeros(F, 16, dtype=torch.int8)
+    w[:, 0] = 127
+    sw = torch.full((F,), 1 / 127.0)
+    wg, sg = dev(w), dev(sw)
+    ops.pa_linear_i8(dev(x), wg, sg, D[0], ops.linear_i8_workspace(N, 1, F), act="gelu")
+    q, s = R.quant(x)
+    ops.pa_gemm_i8(dev(R.padded(q)), dev(s), wg, sg, D[1], K=1, act="gelu")
+    v = q[:, :1].double() * s.double()[:, None] * 127 * sw.double()[None, :]
+    ref = 0.5 * v * torch.erfc(-v / math.sqrt(2.0))
+    bound = ref.abs() * (2.0 ** -8 * (1 + 2.0 ** -8) + 4e-4 + 3 * R.U * (v * v + 1))
+    for d in D:
+        off = (d.cpu().double() - ref).abs()
+        assert (off <= bound).all(), (off / bound).max()
