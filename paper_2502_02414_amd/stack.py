@@ -31,7 +31,7 @@ training step is ``forward``, ``backward`` and a step of ``adamw``'s optimizer.
 Parameters per layer (dict of device tensors): fp32 ln1_g, ln1_b, Wp [C,C],
 bp [C], A [C,M], b [M], a [C], Wq, bq, Wk, bk, Wv, bv (optional Wo, bo),
 ln2_g, ln2_b, b1 [4C], b2 [C]; W1 [C,4C] and W2 [4C,C] in the storage dtype;
-plus the float b_t.
+plus b_t: a float, which training leaves as it is, or an fp32 tensor [1].
 """
 from __future__ import annotations
 
@@ -88,15 +88,21 @@ class BlockStack:
         """The folded slice parameters of a layer (pa_project_fold)."""
         C, M = self.C, self.M
         A_f, a_f = self._e(C, M), self._e(C)
-        b_f, bt_f = self._f(M), self._f(1)
+        b_f, bt_f, b_t = self._f(M), self._f(1), p.get("b_t", 0.0)
         B.pa_project_fold(self.dims, p["Wp"], p["bp"], p["A"], p.get("b"), p.get("a"), A_f, b_f,
                           a_f, bt_f)
-        sp = B.make_slice_params(A_f, b_f, a_f, p.get("b_t", 0.0), b_t_dev=bt_f)
+        if self.torch.is_tensor(b_t):  # (added on the device: nothing waits for it)
+            both, b_t = (bt_f, b_t), 0.0
+            pair, bt_f = self._f(2), self._f(1)
+            for i, t in enumerate(both):
+                B.pa_heads_expand(t, pair[i:i + 1], 1, False)
+            B.pa_heads_sum(pair, bt_f, 2, False)
+        sp = B.make_slice_params(A_f, b_f, a_f, b_t, b_t_dev=bt_f)
         return {"A": A_f, "b": b_f, "a": a_f, "bt": bt_f, "sp": sp}
 
     def named_parameters(self):
-        """{"<layer>.<name>": tensor} of every trained tensor (b_t, a float of
-        the layer's dict, is not one)."""
+        """{"<layer>.<name>": tensor} of every trained tensor (b_t among them where it
+        is one)."""
         return {f"{l}.{k}": v for l, p in enumerate(self.params) for k, v in p.items()
                 if self.torch.is_tensor(v)}
 

@@ -315,3 +315,74 @@ def test_quantised_inference_after_a_step(kind, dt):
     t = kind(1001, 64, 4, 16, s.params, dt)
     t.quantize()
     assert torch.equal(got, t.infer(x, Gs))
+
+
+def with_b_t(s, value=0.375):
+    for p in s.params:
+        p["b_t"] = torch.tensor([value], device="cuda")
+
+
+@pytest.mark.parametrize("kind", [BlockStack, SandwichStack])
+def test_b_t_as_a_tensor(kind):
+    """The same outputs as with a float (0.375 and bp.a add to one fp32 rounding, 2^-24
+    of a temperature of about 1; a weight's logarithm goes with logit / tau, here up to
+    about 20: 1e-5), and its gradient against differences: a step of 2^-6, so that the
+    fp32 outputs' roundings, 2^-18 of each at most, stay below the tolerance."""
+    s, x, Gs, w = make(300, 64, 16, 2, F32, kind, seed=3)
+    for p in s.params:
+        p["b_t"] = 0.375
+    want = s.forward(x, Gs)
+    with_b_t(s)
+    out = s.forward(x, Gs)
+    assert ((out - want).double().norm() / want.double().norm()).item() <= 1e-5
+    _, grads = s.backward(w)
+    noise = 2.0 ** -18 * (w.double() * out.double()).norm().item() / 2.0 ** -6
+    for l, p in enumerate(s.params):
+        quot = {}
+        for h in (2.0 ** -6, 2.0 ** -5):
+            side = []
+            for sign in (1, -1):
+                p["b_t"].fill_(0.375 + sign * h)
+                side.append((w.double() * s.forward(x, Gs).double()).sum().item())
+            quot[h] = (side[0] - side[1]) / (2 * h)
+        p["b_t"].fill_(0.375)
+        got = grads[l]["db_t"].item()
+        tol = 2 * abs(quot[2.0 ** -5] - quot[2.0 ** -6]) + noise + 1e-3 * abs(got)
+        say(f"  {l}: {got:.5g} differences {quot[2.0 ** -6]:.5g} tolerance {tol:.3g}")
+        assert abs(got - quot[2.0 ** -6]) <= tol
+
+
+@pytest.mark.parametrize("kind,dt", [(SandwichStack, F32), (BlockStack, BF16)])
+def test_b_t_is_trained(kind, dt):
+    """Steps with b_t among the parameters, eagerly and in a graph: it moves, by the
+    optimizer's first step lr from where it was, and both ways alike."""
+    s, x, Gs, w = make(1001, 64, 16, 2, dt, kind)
+    t, *_ = make(1001, 64, 16, 2, dt, kind)
+    t.tuned = s.tuned
+    for k in (s, t):
+        with_b_t(k)
+    a, b = s.adamw(lr=1e-2), t.adamw(lr=1e-2)
+    count = torch.zeros(1, dtype=torch.int64, device="cuda")
+
+    def step(k, opt, **kw):
+        k.forward(x, Gs)
+        opt.step(k.named_grads(k.backward(w)[1]), **kw)
+
+    for _ in range(2):
+        step(s, a)
+        step(t, b)
+        count.add_(1)
+        if count.item() == 1:
+            for p in s.params:
+                assert abs(abs(p["b_t"].item() - 0.375) - 1e-2) <= 1e-5
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        count.add_(1)
+        step(s, a, step_dev=count)
+    for rep in range(3):
+        step(t, b)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in s.named_parameters().items():
+            assert torch.equal(v, t.named_parameters()[k]), (rep, k)

@@ -296,3 +296,26 @@ def test_infer_with_integers_of_other_weights(fake, monkeypatch, kind):
         s.quantize()
         s.infer(x, Gs)
         opt.refresh()
+
+
+def test_b_t_as_a_tensor_stays_on_the_device(fake, monkeypatch):
+    """The folded parameters take a device b_t without reading it on the host (a wait,
+    and an error in a capture); a float as before."""
+    def read(t):
+        raise AssertionError("b_t was read on the host")
+
+    monkeypatch.setattr(torch.Tensor, "__float__", read)
+    calls = []
+    for name in ("pa_project_fold", "pa_heads_expand", "pa_heads_sum"):
+        monkeypatch.setattr(B, name, lambda *a, name=name: calls.append((name, a)))
+    monkeypatch.setattr(B, "make_slice_params",
+                        lambda A, b, a, b_t, b_t_dev: (float(b_t), b_t_dev))
+    s = stack()
+    assert s._folded(s.params[0])["sp"][0] == 0.5 and [n for n, _ in calls] == ["pa_project_fold"]
+    bt = s.params[1]["b_t"] = torch.tensor([0.25])
+    calls.clear()
+    host, on_device = s._folded(s.params[1])["sp"]
+    names = [n for n, _ in calls]
+    assert names == ["pa_project_fold", "pa_heads_expand", "pa_heads_expand", "pa_heads_sum"]
+    assert host == 0.0 and calls[2][1][0] is bt and calls[3][1][1] is on_device
+    assert set(s.named_parameters()) - set(stack().named_parameters()) == {"1.b_t"}
