@@ -386,3 +386,64 @@ def test_b_t_is_trained(kind, dt):
         torch.cuda.synchronize()
         for k, v in s.named_parameters().items():
             assert torch.equal(v, t.named_parameters()[k]), (rep, k)
+
+
+@pytest.mark.parametrize("post", ["rms", "layer"])
+def test_sandwich_backward_joins_as_its_parts_in_bf16(post, monkeypatch):
+    """Every joint's backward that the stack runs, against 64 bits on what it was given;
+    each from the forward's tensors of its place and with its place's parameters, the
+    residual stream's gradient handed on from joint to joint, and the parameters'
+    gradients under their names."""
+    s, x, Gs, w = make(777, 64, 16, 2, BF16, SandwichStack, post=post)
+    s.forward(x, Gs)
+    calls, real = [], ops.pa_residual_norm_backward
+
+    def record(x1, y, par, dx1, dh, dx, dy, gr, ws):
+        real(x1, y, par, dx1, dh, dx, dy, gr, ws)
+        calls.append(({"x1": x1, "y": y, "dx1": dx1, "dh": dh},
+                      {"dx": dx.clone(), "dy": dy.clone()}, gr.tensors, ws.numel() // (20 * 64)))
+
+    monkeypatch.setattr(ops, "pa_residual_norm_backward", record)
+    import test_gpu_ops as check
+    _, grads = s.backward(w)
+    assert len(calls) == 4
+    cpu = lambda t: None if t is None else t.cpu()
+    dx = w
+    for (l, k), (i, o, gr, rec) in zip(((1, 2), (1, 1), (0, 2), (0, 1)), calls):
+        c, p = s.caches[l], {n: cpu(v) for n, v in s.params[l].items() if torch.is_tensor(v)}
+        assert i["x1"] is c["x2" if k == 2 else "x1"] and i["y"] is c["z" if k == 2 else "y"]
+        assert torch.equal(i["dx1"], dx)
+        dx = o["dx"]
+        q = {"post": post, "post_g": p[f"post{k}_g"], "post_b": p.get(f"post{k}_b"),
+             "scale": p[f"rs{k}"], "pre": None}
+        at, ln = (l, "ln2") if k == 1 else (l + 1, "ln1")
+        assert (i["dh"] is None) == (at == len(s.params))
+        names = {"dscale": grads[l][f"drs{k}"], "dpost_g": grads[l][f"dpost{k}_g"]}
+        if post == "layer":
+            names["dpost_b"] = grads[l][f"dpost{k}_b"]
+        if i["dh"] is not None:
+            n = s.params[at]
+            q.update(pre="layer", pre_g=cpu(n[ln + "_g"]), pre_b=cpu(n[ln + "_b"]))
+            names.update(dpre_g=grads[at][f"d{ln}_g"], dpre_b=grads[at][f"d{ln}_b"])
+        for name, t in names.items():
+            assert gr[name] is t, (l, k, name)
+        ref = R.joint_backward(q, *(cpu(i[n]) for n in ("x1", "y")), None, cpu(i["dx1"]),
+                               cpu(i["dh"]), 777 // rec + 300)
+        for name, (v, err) in ref.items():
+            if name in o or name in names:
+                check.within(o.get(name, names.get(name)), v, err, BF16 if name in o else F32,
+                       f"{l}.{k} {name}")
+
+
+@pytest.mark.parametrize("kind", [BlockStack, SandwichStack])
+def test_inference_in_8_bits_at_256_channels(kind):
+    """As test_inference_in_8_bits, to its bound, at the widest stack's channels, whose
+    products keep their weights in registers."""
+    s, x, Gs, _ = make(5003, 256, 32, 2, BF16, kind)
+    want = s.infer(x, Gs)
+    s.quantize()
+    got = s.infer(x, Gs)
+    rel = ((got.double() - want.double()).norm() / want.double().norm()).item()
+    say(f"  {kind.__name__}: {rel:.4f}")
+    assert 1e-5 < rel <= 0.03
+    assert torch.equal(s.infer(x, Gs), got)
