@@ -345,22 +345,22 @@ class AdamWItems:
         self.dev, self.blocks, self.stream = dev, blocks.value, B._stream()
         self.ptr = dev.data_ptr()
 
-    def on(self, stream, handle):
+    def on(self, stream, handle, capturing):
         """The table's pointer for a launch on a stream (its handle given); a
         stream other than the table's keeps its memory from being handed out."""
-        if handle and _capturing(stream):  # (the default stream cannot be captured)
+        if capturing:
             if not any(t is self.dev for t in self.captured):
                 self.captured.append(self.dev)
         elif handle != self.stream:
             self.dev.record_stream(stream or _torch().cuda.current_stream())
         return self.ptr
 
-    def hold(self, stream, handle, scalars):
+    def hold(self, stream, handle, capturing, scalars):
         """Before a step on a stream (its handle given): of one that is captured, the
         gradients are kept.  On a stream other than the current one the memory of the
         gradients, which the next step lets go of, and of the device scalars is not
         handed out before the step has run."""
-        if handle and _capturing(stream):
+        if capturing:
             now = [d.get("g") for d in self.tensors]
             if not any(all(a is b for a, b in zip(now, had)) for had in self.captured_grads):
                 self.captured_grads.append(now)
@@ -417,9 +417,10 @@ def pa_adamw(items, lr, step=1, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, gscale
                       _in(lr_dev, 1, torch.float32, "lr_dev", False),
                       _in(step_dev, 1, torch.int64, "step_dev", False))
     handle = B._stream(stream)
-    items.hold(stream, handle, (gscale, lr_dev, step_dev))
+    capturing = bool(handle) and _capturing(stream)  # (the default stream never is)
+    items.hold(stream, handle, capturing, (gscale, lr_dev, step_dev))
     if items.dev is not None:
-        _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle),
+        _check(load().pa_adamw_run(items.n, items.blocks, items.on(stream, handle, capturing),
                                    ctypes.byref(a), handle))
     else:
         _check(load().pa_adamw(items.n, items.arr, ctypes.byref(a), handle))
