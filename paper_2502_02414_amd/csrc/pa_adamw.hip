@@ -10,9 +10,9 @@
 // Bound by memory: per element 28 bytes with fp32 gradients and moments, 16 with
 // 8-bit moments, 2 more for a bf16 copy.  110 million parameters in 168 tensors
 // with bf16 gradients and copies 576 us (3.07 GB, 5.3 TB/s; a copy reaches 4.85);
-// 7 million in 168 with 8-bit moments and copies 25 us (5.0 TB/s).  A first form
-// with one element at a time took 1008 us, one with the tensors in the arguments of
-// four launches 50 us.  The 8-bit code takes about 60 vector instructions an
+// 7 million in 168 with 8-bit moments and copies 25 us (5.0 TB/s) through a table, 50
+// with the tensors in the arguments of four launches (where gradients are new tensors
+// every step).  A first form with one element at a time took 1008 us.  The 8-bit code takes about 60 vector instructions an
 // element: the rounding is an integer addition and a shift, since a code is the top
 // of a float's bits, and the scale a power of two, so that dividing by it is exact
 // and cheap.

@@ -5,11 +5,13 @@
 // The weights are the MFMA's A operand and the points its B operand, so that a
 // lane of a 16 x 16 result tile holds four consecutive channels of one point.
 //
-// Large products are bound by what the card's matrix cores sustain on integers:
-// 8192^3 474 us (2.32 PFLOP/s' worth of operations; a library product of plain
-// integers 2.07), 4096^3 64 to 74 us by the card, on a first form whose
-// operands came straight from memory, without LDS, 640 us.  Counters at 4096^3: no
-// LDS bank conflicts, the matrix cores busy 42% of the time.  Also built, exact and
+// Large products: 8192^3 456 to 474 us (2.3 to 2.4 PFLOP/s' worth of operations; a
+// library product of plain integers 2.07), 4096^3 64 to 74 us by the card, on a first
+// form whose operands came straight from memory, without LDS, 640 us.  Bound by waits,
+// not by a unit: counters at 4096^3 (72.5 us at 2.27 GHz) have the matrix cores busy 40%
+// of the cycles and LDS 15%, without bank conflicts, and the waves waiting 42% of
+// theirs (for loads one step ahead, at a barrier per step; before the first products
+// and behind the last, 12 us by the constants of the tiles' model).  Also built, exact and
 // within 3% (not kept): two groups of four waves that take turns between the
 // products and the operand reads, with raised wave priority and four buffers of 64
 // bytes of K (4096^3 75 us where this form takes 74 on the same card; 8192^3 463

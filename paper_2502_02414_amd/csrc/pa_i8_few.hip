@@ -9,12 +9,13 @@
 // waves' integer sums (exact, so their order does not matter) meet in LDS.
 //
 // With more rows than 16 every block of channels quantises them again, which costs
-// less than a second launch while all the blocks run at once.  Measured, us, as two
-// launches (quantiser, tiles) and as one: 333 rows of 1000 to 517 fp32 8.3 and
+// less than a second launch while all the blocks run at once.  Measured, the least of
+// some, us, as two launches (quantiser, tiles) and as one: 333 rows of 1000 to 517 fp32 8.3 and
 // 6.7; bf16 32 rows of 1024 to 4096 7.9 and 5.8, 333 of 256 to 517 7.8 and 5.5, 1024
-// of 1024 to 256 8.8 and 6.6, 512 of 4096 to 256 15.4 and 13.2.  One row of 4096 to
-// 4096 5.5 us (16.8 MB of weights, from the last cache in these figures), 16 of 4096
-// to 4096 9.3.
+// of 1024 to 256 8.8 and 6.6, 512 of 4096 to 256 15.4 and 13.2.  Medians of 60 in a row:
+// these 7.3, 6.4, 5.8, 7.1 and 14.5; one row of 4096 to 4096 5.9 us (16.8 MB of
+// weights, from the last cache in these figures), 2 of them 6.3, 16 10.1, 16 of 1024 to
+// 4096 5.4.
 #include "pa_i8.hpp"
 
 namespace pa {

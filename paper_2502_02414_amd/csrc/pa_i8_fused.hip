@@ -11,12 +11,13 @@
 // tile as integers; all waves read it as the B operand: one barrier per tile.
 // Results leave from the registers, 64 bytes of a point's row per instruction.
 //
-// Measured, a million rows of bf16: 256 to 1024 channels 518 us (4.9 TB/s, what a
-// copy reaches), with GELU 659 to 672 us on that card; 1024 to 256 with a residual
-// 677 us (4.5 TB/s); 256 to 256 214 us, 64 to 256 with GELU 206 us, 256 to 64
-// 174 us.  As two launches, quantised rows through memory and tiles: 1064, 1200,
-// 1217, 377, 272 and 334 us.  With GELU the vector units bound it: 17 issue slots an
-// output (the exp2 takes four), 1.3M cycles of four per CU at a million rows,
+// Measured, a million rows of bf16: 256 to 1024 channels 514 us (5.0 TB/s, what a
+// copy reaches), with GELU 665 to 690 us (once the card's clock has settled: 650 to
+// 990 in the first thirty passes after a pause); 1024 to 256 with a residual 635 to
+// 677 us by the card (4.5 to 4.8 TB/s); 256 to 256 214 us, 64 to 256 with GELU 209 us,
+// 256 to 64 174 us.  As two launches, quantised rows through memory and tiles: 1064,
+// 1200, 1217, 377, 272 and 334 us.  With GELU the vector units bound it: 17 issue slots
+// an output (the exp2 takes four), 1.3M cycles of four per CU at a million rows,
 // beside 0.25M of the matrix cores.  Before the loads and stores lost their
 // branches the compiler waited for each at once: 1024 to 256 838 us.  Issuing the
 // products among the activation's instructions, run by run, changed nothing; with

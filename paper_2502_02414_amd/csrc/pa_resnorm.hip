@@ -18,7 +18,8 @@
 //
 // Bound by memory (4 to 8 rows of C elements read or written per row, some 20 and
 // 45 operations an element).  A million rows of 256 in bf16: forward 373 us (5.5
-// TB/s), backward with a gate 790 us (5.2 TB/s); a copy reaches 4.85.  A first form
+// TB/s), to int8 rows 358 (5.0), backward with a gate 782 to 794 us (5.2 TB/s); in fp32
+// 801, 683 and, without a gate, 1173 us (4.9 to 5.2 TB/s); a copy reaches 4.85.  A first form
 // with one row at a time, its tensors loaded where they were needed, and sums by
 // ds_bpermute took 415 and 1371 us.  Sums share their exchanges two at a time:
 // four rounds for a backward row.  Rows that do not fill their lanes or cache
