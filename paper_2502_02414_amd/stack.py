@@ -92,6 +92,8 @@ class BlockStack:
         B.pa_project_fold(self.dims, p["Wp"], p["bp"], p["A"], p.get("b"), p.get("a"), A_f, b_f,
                           a_f, bt_f)
         if self.torch.is_tensor(b_t):  # (added on the device: nothing waits for it)
+            if b_t.numel() != 1 or b_t.dtype != self.torch.float32:
+                raise ValueError(f"b_t: {b_t.numel()} elements of {b_t.dtype}, it is one of fp32")
             both, b_t = (bt_f, b_t), 0.0
             pair, bt_f = self._f(2), self._f(1)
             for i, t in enumerate(both):

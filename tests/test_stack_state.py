@@ -319,3 +319,18 @@ def test_b_t_as_a_tensor_stays_on_the_device(fake, monkeypatch):
     assert names == ["pa_project_fold", "pa_heads_expand", "pa_heads_expand", "pa_heads_sum"]
     assert host == 0.0 and calls[2][1][0] is bt and calls[3][1][1] is on_device
     assert set(s.named_parameters()) - set(stack().named_parameters()) == {"1.b_t"}
+
+
+@pytest.mark.parametrize("b_t", [torch.zeros(2), torch.zeros(16), torch.zeros(0),
+                                 torch.zeros(1, dtype=torch.bfloat16),
+                                 torch.zeros(1, dtype=torch.float64)])
+def test_b_t_of_another_size_or_type_is_refused(fake, monkeypatch, b_t):
+    """(More than one element would be written behind the pair that is added.)"""
+    calls = []
+    for name in ("pa_project_fold", "pa_heads_expand", "pa_heads_sum"):
+        monkeypatch.setattr(B, name, lambda *a, name=name: calls.append(name))
+    s = stack()
+    s.params[0]["b_t"] = b_t
+    with pytest.raises(ValueError, match="b_t"):
+        s._folded(s.params[0])
+    assert "pa_heads_expand" not in calls
