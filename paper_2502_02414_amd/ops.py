@@ -319,6 +319,7 @@ class AdamWItems:
 
     def set_grads(self, gs):
         """All gradients, in the items' order."""
+        gs = list(gs)
         if len(gs) != self.n:
             raise ValueError(f"{len(gs)} gradients for {self.n} items")
         cur = _current_device()

@@ -334,3 +334,10 @@ def test_b_t_of_another_size_or_type_is_refused(fake, monkeypatch, b_t):
     with pytest.raises(ValueError, match="b_t"):
         s._folded(s.params[0])
     assert "pa_heads_expand" not in calls
+
+
+def test_gradients_from_any_iterable(fake):
+    it = items_of(300, 400)
+    new = [torch.ones(300), torch.ones(400)]
+    it.set_grads(g for g in new)
+    assert all(d["g"] is g for d, g in zip(it.tensors, new))
