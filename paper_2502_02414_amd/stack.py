@@ -31,7 +31,7 @@ training step is ``forward``, ``backward`` and a step of ``adamw``'s optimizer.
 Parameters per layer (dict of device tensors): fp32 ln1_g, ln1_b, Wp [C,C],
 bp [C], A [C,M], b [M], a [C], Wq, bq, Wk, bk, Wv, bv (optional Wo, bo),
 ln2_g, ln2_b, b1 [4C], b2 [C]; W1 [C,4C] and W2 [4C,C] in the storage dtype;
-plus b_t: a float, which training leaves as it is, or an fp32 tensor [1].
+plus b_t: a float, which training leaves as it is, or an fp32 device tensor [1].
 """
 from __future__ import annotations
 
@@ -91,9 +91,11 @@ class BlockStack:
         b_f, bt_f, b_t = self._f(M), self._f(1), p.get("b_t", 0.0)
         B.pa_project_fold(self.dims, p["Wp"], p["bp"], p["A"], p.get("b"), p.get("a"), A_f, b_f,
                           a_f, bt_f)
-        if self.torch.is_tensor(b_t):  # (added on the device: nothing waits for it)
-            if b_t.numel() != 1 or b_t.dtype != self.torch.float32:
-                raise ValueError(f"b_t: {b_t.numel()} elements of {b_t.dtype}, it is one of fp32")
+        tensor = self.torch.is_tensor(b_t)
+        if tensor and b_t.numel() != 1:
+            raise ValueError(f"b_t: {b_t.numel()} elements, it is one")
+        if tensor and b_t.dtype == self.torch.float32 and b_t.device.type in str(self.dev):
+            # (added on the device, so that nothing waits for it; others are read as floats)
             both, b_t = (bt_f, b_t), 0.0
             pair, bt_f = self._f(2), self._f(1)
             for i, t in enumerate(both):

@@ -321,10 +321,26 @@ def test_b_t_as_a_tensor_stays_on_the_device(fake, monkeypatch):
     assert set(s.named_parameters()) - set(stack().named_parameters()) == {"1.b_t"}
 
 
+@pytest.mark.parametrize("b_t", [torch.tensor(0.5), torch.tensor([0.5], dtype=torch.float64),
+                                 torch.tensor([0.5], dtype=torch.bfloat16)])
+def test_b_t_that_is_read_on_the_host(fake, monkeypatch, b_t):
+    """Of another type, or (as a stack on the GPU finds them) on the CPU: as the float."""
+    calls = []
+    for name in ("pa_project_fold", "pa_heads_expand", "pa_heads_sum"):
+        monkeypatch.setattr(B, name, lambda *a, name=name: calls.append(name))
+    monkeypatch.setattr(B, "make_slice_params",
+                        lambda A, b, a, b_t, b_t_dev: (float(b_t), b_t_dev))
+    s = stack()
+    if b_t.dtype == torch.float32:
+        s._e = s._f = lambda *shape, **kw: torch.empty(*shape)
+        s.dev = "cuda"
+    s.params[0]["b_t"] = b_t
+    assert s._folded(s.params[0])["sp"][0] == 0.5 and calls == ["pa_project_fold"]
+
+
 @pytest.mark.parametrize("b_t", [torch.zeros(2), torch.zeros(16), torch.zeros(0),
-                                 torch.zeros(1, dtype=torch.bfloat16),
-                                 torch.zeros(1, dtype=torch.float64)])
-def test_b_t_of_another_size_or_type_is_refused(fake, monkeypatch, b_t):
+                                 torch.zeros(2, dtype=torch.bfloat16)])
+def test_b_t_of_another_size_is_refused(fake, monkeypatch, b_t):
     """(More than one element would be written behind the pair that is added.)"""
     calls = []
     for name in ("pa_project_fold", "pa_heads_expand", "pa_heads_sum"):
