@@ -20,6 +20,10 @@
  *                      bits
  *   pa_linear_i8       a linear layer in 8-bit integers with scales per row
  *                      (token) and per output channel
+ *   pa_cross_attention attention of query points over an encoder's states, many
+ *                      requests at once, and its backward
+ *   pa_dropout         dropout from a counter-based generator with the residual
+ *                      add; its own backward
  */
 #ifndef PA_OPS_H
 #define PA_OPS_H
@@ -201,6 +205,77 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
                        const void* C, void* D, pa_dtype d_dtype, void* ws, size_t ws_bytes,
                        void* stream);
 pa_status pa_linear_i8_workspace(int64_t N, int F, int K, size_t* bytes);
+
+/* ---------------------------------------------------------------------
+ * Attention of query points over the states of their request.  Requests are
+ * packed: rows q_off[r] .. q_off[r+1] of q [Nq, Hq, D] attend to rows
+ * k_off[r] .. k_off[r+1] of k and v [Nk, Hkv, D]; query heads h of a group of
+ * G = Hq / Hkv share head h / G of k and v.  Over the states j of i's request
+ * whose mask is not 0,
+ *   s_ij = scale q_i.k_j,  lse_i = log sum_j exp(s_ij),
+ *   o_i = sum_j exp(s_ij - lse_i) v_j,
+ * o [Nq, Hq, D], lse [Hq, Nq] fp32.  A row without a state (or whose scores are
+ * all -infinity) has o = 0 and lse = -infinity, and passes no gradient.  What k
+ * and v hold where the mask is 0 is of no account, be it infinities or NaN.
+ * Rows outside of the requests, in front of the first or behind the last, are
+ * not read and their outputs left as they were.
+ *
+ * D a multiple of 8 in [8, 128]; Hkv divides Hq, Hq at most 4096; requests,
+ * their rows and Nk from 0; Nq G and Nk below 2^31 - 1024.  ld*: elements
+ * between the rows of a tensor, a multiple of 16 bytes and at least its heads
+ * times D (with fewer than two rows: not looked at); k and v may lie side by side
+ * in the rows of one product, and dk and dv so too.  Scores, softmax statistics and
+ * sums are fp32; for bf16 the weights, and in the backward ds, are rounded to bf16
+ * for the products over the states and over the queries.
+ * --------------------------------------------------------------------- */
+typedef struct {
+  int32_t R;               /* requests, >= 1                                     */
+  int32_t Hq, Hkv, D;
+  float scale;             /* > 0, finite                                        */
+  const int64_t* q_off;    /* [R + 1] on the device, not decreasing (values      */
+  const int64_t* k_off;    /* outside of the tensor count as its ends); both, or */
+                           /* both NULL with R = 1: all rows                     */
+  const uint8_t* mask;     /* [Nk] on the device, nullable: 0 leaves a state out */
+  int64_t max_k;           /* states of the longest request, 0: not known.  It   */
+                           /* steers the choice of a kernel, not the result      */
+} pa_cross_attention_params;
+
+/* lse nullable.  Workspace: pa_cross_attention_workspace bytes (may be 0). */
+pa_status pa_cross_attention(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                             const pa_cross_attention_params* p, const void* q, int64_t ldq,
+                             const void* k, int64_t ldk, const void* v, int64_t ldv, void* o,
+                             int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* From the forward's o and lse and the gradient d_o of o: dq, and dk and dv (both
+ * NULL: not computed), summed over the heads and queries that share a state. */
+pa_status pa_cross_attention_backward(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                                      const pa_cross_attention_params* p, const void* q,
+                                      int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                      int64_t ldv, const void* o, int64_t ldo, const float* lse,
+                                      const void* d_o, int64_t lddo, void* dq, int64_t lddq,
+                                      void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
+                                      size_t ws_bytes, void* stream);
+pa_status pa_cross_attention_workspace(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                                       const pa_cross_attention_params* p, int backward,
+                                       size_t* bytes);
+
+/* ---------------------------------------------------------------------
+ * Dropout with the residual add, over n elements of dtype:
+ *   out = r + y / (1 - P) where an element is kept, r where it is not,
+ * r nullable (0), P = T / 65536 with T = round(65536 p), p in [0, 1) with T at most
+ * 65535.  Element e is kept if its 16 bits are at least T: the (e % 2)-th half,
+ * lower first, of word (e % 8) / 2 of Philox-4x32-10 (J. Salmon, M. Moraes, R.
+ * Dror, D. Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011) of the
+ * counter (e / 8, offset), 64 bits each, lower words first, under the key seed.  An
+ * offset per use (a step's number times the dropouts of a step, say) makes every
+ * use's numbers its own.  offset_dev: nullable device scalar, added to offset when
+ * the call runs, for a captured graph, whose host values stand still.
+ * Its backward is the call on the gradient without r, with the same p, seed and
+ * offset.  What is dropped is not read into the result (it may be NaN).  out may be
+ * y or r.
+ * --------------------------------------------------------------------- */
+pa_status pa_dropout(int64_t n, pa_dtype dtype, const void* y, const void* r, void* out, double p,
+                     uint64_t seed, uint64_t offset, const int64_t* offset_dev, void* stream);
 
 #ifdef __cplusplus
 }

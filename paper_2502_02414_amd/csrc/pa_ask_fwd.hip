@@ -1,0 +1,239 @@
+// Attention of query points over the states of their request, forward (gfx950):
+//   s_ij = scale q_i.k_j,  lse_i = log sum_j exp(s_ij),  o_i = sum_j exp(s_ij - lse_i) v_j
+// over the states j of i's request that the mask leaves.  One pass over the states in
+// tiles of 64 with the running maximum m and sum l of a softmax; scores, maxima and
+// sums are fp32, and exp(s - m) is rounded to the operands' type for the product with
+// v (bf16: 2^-9 of each weight, below the rounding of o, since the errors of several
+// weights do not line up; l adds up the unrounded ones).
+#include "pa_ask.hpp"
+
+namespace pa {
+namespace {
+using namespace ask;
+
+template <typename T, int DP, int QT>
+__global__ void __launch_bounds__(256) k_ask(AskArgs a) {
+  using Gm = AskGeo<T, DP>;
+  constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
+  __shared__ float live[2][kTile];                             // 0, or -inf where left out
+  const int G = a.Hq / a.Hkv;
+  const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
+  const int64_t slot = blockIdx.x / a.Hkv;
+  const int rq = request_of(a.q_off, a.R, a.Nq, G, SHIFT, slot);
+  if (rq < 0) return;
+  const Range qr = range_of(a.q_off, rq, a.Nq);
+  const int n = (int)(qr.e - qr.b) * G;
+  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - (a.q_off ? rq : 0);
+  if (tile < 0 || tile * TQ >= n) return;
+  const int v0 = (int)tile * TQ;
+  const Range kr = piece(range_of(a.k_off, rq, a.Nk), s, a.S);
+
+  const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
+  const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
+  const T* K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
+  const T* V = reinterpret_cast<const T*>(a.v) + (int64_t)h * a.D;
+  // this lane's queries: column r of the wave's QT tiles of 16
+  int vq[QT];
+  int64_t row[QT];
+  int head[QT];
+  K32<T> qf[QT][Gm::NK];
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    vq[c] = v0 + (w * QT + c) * 16 + r;
+    const uint32_t v = vq[c] < n ? vq[c] : n - 1;
+    const uint32_t i = G == 1 ? v : v / (uint32_t)G;
+    row[c] = qr.b + i;
+    head[c] = v - i * G;
+    row_frags<T, DP>(qf[c], Q + row[c] * a.ldq + (int64_t)head[c] * a.D, a.D, vq[c] < n);
+  }
+  const bool busy = v0 + w * QT * 16 < n;  // (of the wave; all load)
+  const float sc = a.scale * kLog2e;
+  f32x4 o[QT][Gm::ND];
+  float m[QT], l[QT];
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    m[c] = -INFINITY;
+    l[c] = 0.f;
+#pragma unroll
+    for (int d = 0; d < Gm::ND; ++d) o[c][d] = zero4();
+  }
+
+  TileLoad<T, DP> tk, tv;
+  float alive;
+  auto load = [&](int64_t p0) __attribute__((always_inline)) {
+    tk.states(K, a.ldk, p0, kr.e, a.D, a.mask);
+    tv.states(V, a.ldv, p0, kr.e, a.D, a.mask);
+    if (threadIdx.x < kTile) {
+      const int64_t p = p0 + threadIdx.x;
+      alive = p < kr.e && (!a.mask || a.mask[p]) ? 0.f : -INFINITY;
+    }
+  };
+  auto put = [&](int buf) __attribute__((always_inline)) {
+    tk.put(smem + buf * 2 * Gm::TB);
+    tv.put(smem + buf * 2 * Gm::TB + Gm::TB);
+    if (threadIdx.x < kTile) live[buf][threadIdx.x] = alive;
+  };
+  const RowBase<T> rb = row_base<T>(r, Gm::RB);
+  const int tb = tr_base<T>(Gm::RB);
+  if (kr.b < kr.e) {
+    load(kr.b);
+    put(0);
+  }
+  int buf = 0;
+  for (int64_t p0 = kr.b; p0 < kr.e; p0 += kTile, buf ^= 1) {
+    block_sync();
+    const bool more = p0 + kTile < kr.e;
+    if (more) load(p0 + kTile);
+    if (busy) {
+      const char* kt = smem + buf * 2 * Gm::TB;
+      const char* vt = kt + Gm::TB;
+      f32x4 x[QT][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int c = 0; c < QT; ++c) x[c][t] = zero4();
+#pragma unroll
+        for (int k = 0; k < Gm::NK; ++k) {
+          K32<T> kf;
+          ld_row<T>(kf, kt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
+#pragma unroll
+          for (int c = 0; c < QT; ++c) x[c][t] = mma32(kf, qf[c][k], x[c][t]);
+        }
+        if (a.mask || p0 + kTile > kr.e) {
+          const f32x4 dead = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+#pragma unroll
+          for (int c = 0; c < QT; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[c][t][i] = dead[i] == 0.f ? x[c][t][i] : -INFINITY;
+        }
+      }
+      K16<T> pf[QT][4];
+#pragma unroll
+      for (int c = 0; c < QT; ++c) {
+        float mx = x[c][0][0];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[c][t][i]);
+        mx = fmaxf(m[c], groups_max(mx) * sc);
+        const float base = mx == -INFINITY ? 0.f : mx;  // (nothing yet: weights of 0)
+        const float down = fast_exp2(m[c] - base);
+        m[c] = mx;
+        l[c] *= down;
+#pragma unroll
+        for (int d = 0; d < Gm::ND; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[c][d][i] *= down;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] = fast_exp2(fmaf(x[c][t][i], sc, -base));
+            l[c] += p[i];
+          }
+          set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) {
+#pragma unroll
+        for (int t = 0; t < 4; t += 2) {
+          K16<T> v0f, v1f;
+          ld_tr<T>(v0f, vt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
+          ld_tr<T>(v1f, vt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
+#pragma unroll
+          for (int c = 0; c < QT; ++c)
+            o[c][d] = mma16x2(v0f, pf[c][t], v1f, pf[c][t + 1], o[c][d]);
+        }
+      }
+    }
+    if (more) put(buf ^ 1);
+  }
+#pragma unroll
+  for (int c = 0; c < QT; ++c) {
+    const float sum = groups_sum(l[c]);
+    if (vq[c] >= n) continue;
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+    const float lse2 = sum == 0.f ? -INFINITY : m[c] + log2f(sum);
+    const int hq = h * G + head[c];
+    if (a.S == 1) {
+      T* O = reinterpret_cast<T*>(a.o) + row[c] * a.ldo + (int64_t)hq * a.D;
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d)
+        if (16 * d + 4 * g < a.D) store4<T>(O + 16 * d + 4 * g, o[c][d] * inv);
+      if (a.lse && g == 0) a.lse[(int64_t)hq * a.Nq + row[c]] = lse2 * kLn2;
+    } else {
+      const int64_t at = ((int64_t)s * a.Nq + row[c]) * a.Hq + hq;
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d)
+        if (16 * d + 4 * g < a.D) store4<float>(a.part + at * a.D + 16 * d + 4 * g, o[c][d] * inv);
+      if (g == 0) a.part_lse[at] = lse2;
+    }
+  }
+}
+
+// The pieces of the states joined: a thread has four elements of a head of a row.
+template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs a) {
+  const int per = a.D / 4;
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.Nq * a.Hq;
+  const int64_t at = t / per;
+  const int c = (int)(t - at * per) * 4;
+  if (at >= rows) return;
+  const int64_t row = at / a.Hq;
+  const int hq = (int)(at - row * a.Hq);
+  if (a.q_off && (row < a.q_off[0] || row >= a.q_off[a.R])) return;
+  float m = -INFINITY;
+  for (int s = 0; s < a.S; ++s) m = fmaxf(m, a.part_lse[s * rows + at]);
+  const float base = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4 o = zero4();
+  for (int s = 0; s < a.S; ++s) {
+    const float w = fast_exp2(a.part_lse[s * rows + at] - base);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
+    sum += w;
+    o += x * w;
+  }
+  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+  store4<T>(reinterpret_cast<T*>(a.o) + row * a.ldo + (int64_t)hq * a.D + c, o * inv);
+  if (a.lse && c == 0)
+    a.lse[(int64_t)hq * a.Nq + row] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
+}
+
+template <typename T, int DP, int QT> hipError_t launch(const AskArgs& a, hipStream_t st) {
+  using Gm = AskGeo<T, DP>;
+  const int64_t G = a.Hq / a.Hkv, slots = (a.Nq * G >> (QT == 1 ? 6 : 7)) + a.R;
+  hipLaunchKernelGGL((k_ask<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256),
+                     4 * Gm::TB, st, a);
+  return hipGetLastError();
+}
+template <typename T> hipError_t width(const AskArgs& a, hipStream_t st) {
+  if (a.D <= 32) return launch<T, 32, 1>(a, st);
+  if (a.D <= 64) return launch<T, 64, 1>(a, st);
+  if (a.D <= 96) return launch<T, 96, 1>(a, st);
+  return launch<T, 128, 1>(a, st);
+}
+
+}  // namespace
+
+// Pieces of the states: with fewer blocks of whole ones than the chip holds.
+int ask_pieces(const AskArgs& a) {
+  const int64_t G = a.Hq / a.Hkv, blocks = ((a.Nq * G >> 6) + a.R) * a.Hkv;
+  const int64_t tiles = (a.Nk / a.R + kTile - 1) / kTile;
+  int64_t S = (1024 + blocks - 1) / blocks;
+  if (S > tiles / 2) S = tiles / 2;
+  return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
+}
+
+hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
+  hipError_t e = dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  if (e != hipSuccess || a.S == 1) return e;
+  const int64_t threads = a.Nq * a.Hq * (a.D / 4);
+  const dim3 grid((uint32_t)((threads + 255) / 256));
+  if (dtype == 1) hipLaunchKernelGGL(k_ask_join<bf16>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_ask_join<float>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace pa

@@ -78,6 +78,35 @@ pa_status apart(const char* who, const Span (&out)[NO], const Span (&in)[NI]) {
 }
 uint64_t dtype_bytes(int dt) { return dt == PA_BF16 ? 2 : 4; }
 
+// Rows of one tensor of a call: `width` bytes, `pitch` from one to the next.
+struct Rows {
+  const char* name;
+  const void* p;
+  uint64_t rows, width, pitch;
+};
+bool rows_meet(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p || !a.rows || !b.rows) return false;
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  if (x >= y + (b.rows - 1) * b.pitch + b.width || y >= x + (a.rows - 1) * a.pitch + a.width)
+    return false;
+  // side by side in rows of one pitch: b's columns from a's, in the row they begin in
+  if (a.pitch != b.pitch) return true;
+  const uint64_t off = y >= x ? (y - x) % a.pitch : (a.pitch - (x - y) % a.pitch) % a.pitch;
+  return off < a.width || off + b.width > a.pitch;
+}
+template <size_t NO, size_t NI>
+pa_status rows_apart(const char* who, const Rows (&out)[NO], const Rows (&in)[NI]) {
+  for (size_t i = 0; i < NO; ++i) {
+    for (size_t j = i + 1; j < NO; ++j)
+      if (rows_meet(out[i], out[j]))
+        return err(PA_ERR_INVALID, "%s: %s and %s overlap", who, out[i].name, out[j].name);
+    for (const Rows& s : in)
+      if (rows_meet(out[i], s))
+        return err(PA_ERR_INVALID, "%s: %s and %s overlap", who, out[i].name, s.name);
+  }
+  return PA_OK;
+}
+
 // Sizes and parameters of the joint.
 pa_status joint_sizes(const char* who, int64_t N, int C, int dtype) {
   PO_TRY(dtype_ok(who, dtype));
@@ -514,6 +543,184 @@ pa_status pa_linear_i8(int64_t N, int F, int K, const void* x, pa_dtype x_dtype,
   a.q = q;
   a.s = s;
   PO_HIP(integers(a, d_dtype, as_stream(stream)), who);
+  return PA_OK;
+}
+
+// ---- attention of query points over states ----
+static pa_status ask_params(const char* who, int64_t Nq, int64_t Nk, int dtype,
+                            const pa_cross_attention_params* p, pa::AskArgs* a) {
+  PO_TRY(dtype_ok(who, dtype));
+  if (!p) return err(PA_ERR_INVALID, "%s: params is NULL", who);
+  if (Nq < 0 || Nk < 0) return err(PA_ERR_INVALID, "%s: Nq and Nk must be >= 0", who);
+  if (p->R < 1) return err(PA_ERR_INVALID, "%s: R must be >= 1", who);
+  if (p->Hq < 1 || p->Hkv < 1 || p->Hq % p->Hkv)
+    return err(PA_ERR_INVALID, "%s: Hkv must divide Hq", who);
+  if (p->D < 8 || p->D % 8 || p->D > 128)
+    return err(PA_ERR_UNSUPPORTED, "%s: D must be a multiple of 8 in [8, 128]", who);
+  const int64_t most = 0x7fffffff - 1024;
+  if (p->Hq > 4096 || p->R > (1 << 24) || Nk > most || Nq > most / (p->Hq / p->Hkv))
+    return err(PA_ERR_UNSUPPORTED, "%s: Hq at most 4096, R 2^24, Nk and Nq Hq / Hkv below 2^31 - 1024",
+               who);
+  if (((Nq * (p->Hq / p->Hkv) >> 6) + p->R) * p->Hkv > most || ((Nk >> 6) + p->R) * p->Hkv > most)
+    return err(PA_ERR_UNSUPPORTED, "%s: too many rows times heads for one launch", who);
+  if (!(p->scale > 0.f) || !std::isfinite(p->scale))
+    return err(PA_ERR_INVALID, "%s: scale must be > 0 and finite", who);
+  if (!p->q_off != !p->k_off) return err(PA_ERR_INVALID, "%s: q_off and k_off go together", who);
+  if (!p->q_off && p->R != 1) return err(PA_ERR_INVALID, "%s: R > 1 needs q_off and k_off", who);
+  if (p->max_k < 0) return err(PA_ERR_INVALID, "%s: max_k must be >= 0", who);
+  PO_TRY(opt(who, p->q_off, "q_off", 8));
+  PO_TRY(opt(who, p->k_off, "k_off", 8));
+  a->Nq = Nq; a->Nk = Nk; a->R = p->R; a->Hq = p->Hq; a->Hkv = p->Hkv; a->D = p->D;
+  a->scale = p->scale; a->q_off = p->q_off; a->k_off = p->k_off; a->mask = p->mask;
+  a->max_k = p->max_k && p->max_k < Nk ? p->max_k : Nk;
+  return PA_OK;
+}
+// A tensor of N rows of H heads, given with the elements between its rows; without
+// rows it may be NULL.
+static pa_status ask_rows(const char* who, const char* name, const void* ptr, int64_t N, int H,
+                          int D, int64_t* ld, int dtype, Rows* out) {
+  const int64_t b = (int64_t)dtype_bytes(dtype), width = (int64_t)H * D;
+  if (N < 2) *ld = width;
+  if (*ld < width || *ld > ((int64_t)1 << 32) || *ld * b % 16)
+    return err(PA_ERR_INVALID, "%s: ld of %s must be a multiple of 16 bytes in [%lld, 2^32]", who,
+               name, (long long)width);
+  if (N) PO_TRY(need(who, ptr, name));
+  *out = {name, ptr, (uint64_t)N, (uint64_t)(width * b), (uint64_t)(*ld * b)};
+  return PA_OK;
+}
+static Rows flat(const char* name, const void* p, uint64_t bytes) { return {name, p, 1, bytes, bytes}; }
+
+// The workspace's parts, of which the forward has the first two; returns the bytes.
+static size_t ask_layout(pa::AskArgs* a, bool backward, void* ws) {
+  char* base = reinterpret_cast<char*>(ws);
+  size_t at = 0;
+  const auto take = [&](uint64_t floats) {
+    float* p = base ? reinterpret_cast<float*>(base + at) : nullptr;
+    at += (floats * 4 + 255) / 256 * 256;
+    return p;
+  };
+  const uint64_t rows = (uint64_t)a->Nq * a->Hq;
+  a->S = pa::ask_pieces(*a);
+  if (a->S > 1) {
+    a->part = take((uint64_t)a->S * rows * a->D);
+    a->part_lse = take((uint64_t)a->S * rows);
+  }
+  if (!backward) return at;
+  a->delta = take(rows);
+  if (a->S > 1) a->part_b = take((uint64_t)a->S * rows * a->D);
+  a->SQ = pa::ask_pieces_q(*a);
+  if (a->SQ > 1) {
+    const uint64_t n = (uint64_t)a->SQ * a->Nk * a->Hkv * a->D;
+    a->part_k = take(n);
+    a->part_v = take(n);
+  }
+  return at;
+}
+
+pa_status pa_cross_attention_workspace(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                                       const pa_cross_attention_params* p, int backward,
+                                       size_t* bytes) {
+  const char* who = "pa_cross_attention_workspace";
+  pa::AskArgs a;
+  PO_TRY(ask_params(who, Nq, Nk, dtype, p, &a));
+  if (!bytes) return err(PA_ERR_INVALID, "%s: bytes is NULL", who);
+  *bytes = ask_layout(&a, backward != 0, nullptr);
+  return PA_OK;
+}
+
+pa_status pa_cross_attention(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                             const pa_cross_attention_params* p, const void* q, int64_t ldq,
+                             const void* k, int64_t ldk, const void* v, int64_t ldv, void* o,
+                             int64_t ldo, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* who = "pa_cross_attention";
+  pa::AskArgs a;
+  Rows rq, rk, rv, ro;
+  PO_TRY(ask_params(who, Nq, Nk, dtype, p, &a));
+  PO_TRY(ask_rows(who, "q", q, Nq, a.Hq, a.D, &ldq, dtype, &rq));
+  PO_TRY(ask_rows(who, "k", k, Nk, a.Hkv, a.D, &ldk, dtype, &rk));
+  PO_TRY(ask_rows(who, "v", v, Nk, a.Hkv, a.D, &ldv, dtype, &rv));
+  PO_TRY(ask_rows(who, "o", o, Nq, a.Hq, a.D, &ldo, dtype, &ro));
+  PO_TRY(opt(who, lse, "lse", 4));
+  const size_t bytes = ask_layout(&a, false, nullptr);
+  if (bytes && (!ws || ws_bytes < bytes))
+    return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, bytes);
+  if (bytes) PO_TRY(opt(who, ws, "ws"));
+  const uint64_t offs = ((uint64_t)a.R + 1) * 8;
+  PO_TRY(rows_apart(who, {ro, flat("lse", lse, (uint64_t)Nq * a.Hq * 4), flat("ws", bytes ? ws : nullptr, bytes)},
+                    {rq, rk, rv, flat("mask", a.mask, (uint64_t)Nk), flat("q_off", a.q_off, offs),
+                     flat("k_off", a.k_off, offs)}));
+  if (!Nq) return PA_OK;
+  ask_layout(&a, false, ws);
+  a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
+  a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
+  PO_HIP(pa::launch_ask(a, dtype, as_stream(stream)), who);
+  return PA_OK;
+}
+
+pa_status pa_cross_attention_backward(int64_t Nq, int64_t Nk, pa_dtype dtype,
+                                      const pa_cross_attention_params* p, const void* q,
+                                      int64_t ldq, const void* k, int64_t ldk, const void* v,
+                                      int64_t ldv, const void* o, int64_t ldo, const float* lse,
+                                      const void* d_o, int64_t lddo, void* dq, int64_t lddq,
+                                      void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
+                                      size_t ws_bytes, void* stream) {
+  const char* who = "pa_cross_attention_backward";
+  pa::AskArgs a;
+  Rows rq, rk, rv, ro, rd, rdq, rdk, rdv;
+  PO_TRY(ask_params(who, Nq, Nk, dtype, p, &a));
+  PO_TRY(ask_rows(who, "q", q, Nq, a.Hq, a.D, &ldq, dtype, &rq));
+  PO_TRY(ask_rows(who, "k", k, Nk, a.Hkv, a.D, &ldk, dtype, &rk));
+  PO_TRY(ask_rows(who, "v", v, Nk, a.Hkv, a.D, &ldv, dtype, &rv));
+  PO_TRY(ask_rows(who, "o", o, Nq, a.Hq, a.D, &ldo, dtype, &ro));
+  PO_TRY(ask_rows(who, "d_o", d_o, Nq, a.Hq, a.D, &lddo, dtype, &rd));
+  PO_TRY(ask_rows(who, "dq", dq, Nq, a.Hq, a.D, &lddq, dtype, &rdq));
+  if (Nk && !dk != !dv) return err(PA_ERR_INVALID, "%s: dk and dv go together", who);
+  const bool states = dk && dv;
+  PO_TRY(ask_rows(who, "dk", dk, states ? Nk : 0, a.Hkv, a.D, &lddk, dtype, &rdk));
+  PO_TRY(ask_rows(who, "dv", dv, states ? Nk : 0, a.Hkv, a.D, &lddv, dtype, &rdv));
+  if (Nq) PO_TRY(need(who, lse, "lse", 4));
+  const size_t bytes = ask_layout(&a, true, nullptr);
+  if (bytes && (!ws || ws_bytes < bytes))
+    return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, bytes);
+  if (bytes) PO_TRY(opt(who, ws, "ws"));
+  const uint64_t offs = ((uint64_t)a.R + 1) * 8;
+  PO_TRY(rows_apart(who, {rdq, rdk, rdv, flat("ws", bytes ? ws : nullptr, bytes)},
+                    {rq, rk, rv, ro, rd, flat("lse", lse, (uint64_t)Nq * a.Hq * 4),
+                     flat("mask", a.mask, (uint64_t)Nk), flat("q_off", a.q_off, offs),
+                     flat("k_off", a.k_off, offs)}));
+  if (!Nq && !Nk) return PA_OK;
+  ask_layout(&a, true, ws);
+  a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse);
+  a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
+  a.d_o = d_o; a.dq = dq; a.lddo = lddo; a.lddq = lddq;
+  a.dk = states ? dk : nullptr; a.dv = states ? dv : nullptr;
+  a.lddk = lddk; a.lddv = lddv;
+  PO_HIP(pa::launch_ask_backward(a, dtype, as_stream(stream)), who);
+  return PA_OK;
+}
+
+pa_status pa_dropout(int64_t n, pa_dtype dtype, const void* y, const void* r, void* out, double p,
+                     uint64_t seed, uint64_t offset, const int64_t* offset_dev, void* stream) {
+  const char* who = "pa_dropout";
+  PO_TRY(dtype_ok(who, dtype));
+  if (n < 0 || n > ((int64_t)1 << 40)) return err(PA_ERR_INVALID, "%s: n must be in [0, 2^40]", who);
+  if (!(p >= 0.0) || !(65536.0 * p < 65535.5))
+    return err(PA_ERR_INVALID, "%s: p must be in [0, 1 - 2^-17)", who);
+  PO_TRY(opt(who, offset_dev, "offset_dev", 8));
+  if (!n) return PA_OK;
+  PO_TRY(need(who, y, "y"));
+  PO_TRY(opt(who, r, "r"));
+  PO_TRY(need(who, out, "out"));
+  const uint64_t bytes = (uint64_t)n * dtype_bytes(dtype);
+  PO_TRY(apart(who, {{"out", out, bytes}},
+               {{"y", y == out ? nullptr : y, bytes}, {"r", r == out ? nullptr : r, bytes},
+                {"offset_dev", offset_dev, 8}}));
+  pa::DropArgs a;
+  a.n = n; a.y = y; a.r = r; a.out = out;
+  a.threshold = (uint32_t)std::llround(65536.0 * p);
+  a.scale = (float)(65536.0 / (65536.0 - a.threshold));
+  a.seed = seed; a.offset = offset; a.offset_dev = offset_dev;
+  PO_HIP(pa::launch_dropout(a, dtype, as_stream(stream)), who);
   return PA_OK;
 }
 

@@ -1,5 +1,6 @@
 // Internal launch interface of the operators of include/pa_ops.h, between
-// pa_ops_api.cpp and the kernels (pa_resnorm.hip, pa_adamw.hip, pa_i8.hip).
+// pa_ops_api.cpp and the kernels (pa_resnorm.hip, pa_adamw.hip, pa_i8*.hip, pa_ask_*.hip,
+// pa_dropout.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -106,6 +107,48 @@ hipError_t launch_quant_rows(int64_t N, int K, int dtype, const void* x, int8_t*
                              hipStream_t st);
 hipError_t launch_quant_weight(int K, int F, int dtype, const void* W, int8_t* Wq, float* sw,
                                hipStream_t st);
+
+// ---- attention of query points over states (pa_ask_fwd.hip, pa_ask_bwd.hip) ----
+struct AskArgs {
+  int64_t Nq = 0, Nk = 0;
+  int R = 1, Hq = 1, Hkv = 1, D = 0;
+  float scale = 1.f;
+  const int64_t *q_off = nullptr, *k_off = nullptr;  // [R + 1], both or none (R = 1)
+  const uint8_t* mask = nullptr;                     // [Nk]
+  int64_t max_k = 0;  // states of the longest request, or more; steers choices only
+  int64_t ldq = 0, ldk = 0, ldv = 0, ldo = 0;        // elements between rows
+  const void *q = nullptr, *k = nullptr, *v = nullptr;
+  void* o = nullptr;     // (read by the backward)
+  float* lse = nullptr;  // [Hq,Nq] (read by the backward)
+  // pieces of the states that are worked on apart and joined
+  int S = 1;
+  float* part = nullptr;      // [S,Nq,Hq,D]
+  float* part_lse = nullptr;  // [S,Nq,Hq], base 2
+  // backward
+  int64_t lddo = 0, lddq = 0, lddk = 0, lddv = 0;
+  const void* d_o = nullptr;
+  void *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  float* delta = nullptr;   // [Hq,Nq]
+  float* part_b = nullptr;  // [S,Nq,Hq,D]
+  int SQ = 1;               // pieces of the queries
+  float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D]
+};
+int ask_pieces(const AskArgs& a);    // S
+int ask_pieces_q(const AskArgs& a);  // SQ
+hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
+hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st);
+
+// ---- dropout with the residual add (pa_dropout.hip) ----
+struct DropArgs {
+  int64_t n = 0;
+  const void *y = nullptr, *r = nullptr;
+  void* out = nullptr;
+  uint32_t threshold = 0;  // of 16 bits; below: dropped
+  float scale = 1.f;       // 65536 / (65536 - threshold)
+  uint64_t seed = 0, offset = 0;
+  const int64_t* offset_dev = nullptr;  // added to offset
+};
+hipError_t launch_dropout(const DropArgs& a, int dtype, hipStream_t st);
 
 #ifdef __HIPCC__
 // A row's scale from the bits of its largest magnitude (as integers, so that

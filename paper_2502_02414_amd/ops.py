@@ -7,9 +7,13 @@ same manner): the operators around the block stack.
                                or in 8 bits; ``AdamW`` keeps a model's moments
   pa_linear_i8                 a linear layer in 8-bit integers (pa_quant_rows,
                                pa_quant_weight, pa_gemm_i8: its parts)
+  pa_cross_attention(_backward)  query points that attend to the states of their
+                               request, many requests at once
+  pa_dropout                   dropout from a counter-based generator with the
+                               residual add
 
-Tensors are contiguous GPU tensors on the current device; outputs are passed
-in.  Each wrapper checks device, dtype, size and contiguity against the call,
+Tensors are contiguous GPU tensors on the current device (of pa_cross_attention's
+the rows may lie further apart); outputs are passed in.  Each wrapper checks device, dtype, size and contiguity against the call,
 and raises ValueError, or PAError with the library's message.
 """
 from __future__ import annotations
@@ -24,6 +28,8 @@ SYMBOLS = (
     "pa_residual_norm_workspace", "pa_adamw", "pa_adamw_table_size", "pa_adamw_table",
     "pa_adamw_run", "pa_adamw_unpack", "pa_quant_rows",
     "pa_quant_weight", "pa_gemm_i8", "pa_linear_i8", "pa_linear_i8_workspace",
+    "pa_cross_attention", "pa_cross_attention_backward", "pa_cross_attention_workspace",
+    "pa_dropout",
 )
 
 NORMS = {None: 0, "none": 0, "layer": 1, "rms": 2}
@@ -57,6 +63,12 @@ class pa_adamw_args(ctypes.Structure):
                 ("gscale", _P), ("lr_dev", _P), ("step_dev", _P)]
 
 
+class pa_cross_attention_params(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("R", "Hq", "Hkv", "D")] + [
+        ("scale", ctypes.c_float), ("q_off", _P), ("k_off", _P), ("mask", _P),
+        ("max_k", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -83,6 +95,12 @@ def load():
     lib.pa_gemm_i8.argtypes = [I64, I32, I32, _P, _P, _P, _P, _P, I32, _P, _P, I32, _P]
     lib.pa_linear_i8.argtypes = [I64, I32, I32, _P, I32, _P, _P, _P, I32, _P, _P, I32, _P, S, _P]
     lib.pa_linear_i8_workspace.argtypes = [I64, I32, I32, Sp]
+    CP, F64, U64 = ctypes.POINTER(pa_cross_attention_params), ctypes.c_double, ctypes.c_uint64
+    row = [_P, I64]  # a tensor and the elements between its rows
+    lib.pa_cross_attention.argtypes = [I64, I64, I32, CP, *row * 4, _P, _P, S, _P]
+    lib.pa_cross_attention_backward.argtypes = [I64, I64, I32, CP, *row * 4, _P, *row * 4, _P, S, _P]
+    lib.pa_cross_attention_workspace.argtypes = [I64, I64, I32, CP, I32, Sp]
+    lib.pa_dropout.argtypes = [I64, I32, _P, _P, _P, F64, U64, U64, _P, _P]
     for name in SYMBOLS:
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -650,3 +668,133 @@ def pa_linear_i8(x, wq, sw, D, ws, bias=None, act=None, C=None, stream=None):
     _check(load().pa_linear_i8(N, F, K, _dev(x, "x", cur), _code(x.dtype, "x"), *rest,
                                None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws),
                                B._stream(stream)))
+
+
+# ---- attention of query points over states ----
+class CrossAttention:
+    """The host struct of pa_cross_attention's parameters and the tensors it points
+    at, on one device (None: no tensors)."""
+
+    def __init__(self, st, tensors):
+        self.st, self.tensors = st, tensors
+        self.ref = ctypes.byref(st)
+        self.Hq, self.Hkv, self.D = st.Hq, st.Hkv, st.D
+        self.mask = tensors["mask"]
+        self.device = None if all(t is None for t in tensors.values()) else _current_device()
+
+
+def make_cross_attention(Hq, Hkv, D, scale=None, q_off=None, k_off=None, mask=None,
+                         max_k=0) -> CrossAttention:
+    """Hq query heads over Hkv heads of states, D wide; scale: 1 / sqrt(D) where none
+    is given; q_off, k_off: int64 [requests + 1], where the rows of each request begin
+    and end (None: one request of all rows); mask: bool or uint8 [Nk], false for the
+    states that are left out; max_k: the states of the longest request, if known."""
+    torch = _torch()
+    Hq, Hkv, D, R, ptr = int(Hq), int(Hkv), int(D), 1, {}
+    if (q_off is None) != (k_off is None):
+        raise ValueError("q_off and k_off go together")
+    if q_off is not None:
+        R = q_off.numel() - 1
+        for name, t in (("q_off", q_off), ("k_off", k_off)):
+            ptr[name] = _in(t, R + 1, torch.int64, name)
+    if mask is not None:
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise ValueError(f"mask: dtype {mask.dtype}, the call needs bool or uint8")
+        ptr["mask"] = _dev(mask, "mask")
+    if scale is None:
+        scale = D ** -0.5 if D > 0 else 1.0
+    st = pa_cross_attention_params(R, Hq, Hkv, D, float(scale), ptr.get("q_off"),
+                                   ptr.get("k_off"), ptr.get("mask"), int(max_k))
+    return CrossAttention(st, {"q_off": q_off, "k_off": k_off, "mask": mask})
+
+
+def _rows(t, N, H, D, dtype, name, cur):
+    """(pointer, elements between rows) of a tensor of N rows of H heads of D, [N, H, D]
+    or [N, H D], whose rows may be further apart than they are long."""
+    if t.get_device() != cur:
+        B._ptr(t)
+        raise ValueError(f"{name}: on {t.device}, not on the current device")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
+    shape = t.shape
+    if len(shape) == 3:
+        ok = shape[0] == N and shape[1] == H and shape[2] == D
+        s0, s1, s2 = t.stride()
+        whole = (s2 == 1 or D == 1) and (s1 == D or H == 1)
+    elif len(shape) == 2:
+        ok = shape[0] == N and shape[1] == H * D
+        s0, s2 = t.stride()
+        whole = s2 == 1
+    else:
+        ok = False
+    if not ok:
+        raise ValueError(f"{name}: {list(shape)}, the call needs {[N, H, D]}")
+    if N and not whole:
+        raise ValueError(f"{name}: the elements of a row have to lie one behind the other")
+    return t.data_ptr(), s0
+
+
+def _asked(q, k, par, cur):
+    """The sizes of a call."""
+    _here(par.device, "the parameters", cur)
+    if q.dim() not in (2, 3) or k.dim() not in (2, 3):
+        raise ValueError("q must be [Nq, Hq, D] and k [Nk, Hkv, D]")
+    Nq, Nk = q.shape[0], k.shape[0]
+    if par.mask is not None and par.mask.numel() != Nk:
+        raise ValueError(f"mask: {par.mask.numel()} elements, the call needs {Nk}")
+    return Nq, Nk, q.dtype, _code(q.dtype, "q")
+
+
+def cross_attention_workspace(par, Nq, Nk, dtype, backward=False, device="cuda"):
+    """A uint8 workspace for calls with these parameters and sizes."""
+    n = ctypes.c_size_t(0)
+    _check(load().pa_cross_attention_workspace(Nq, Nk, _code(dtype, "dtype"), par.ref,
+                                               int(bool(backward)), ctypes.byref(n)))
+    return _torch().empty(n.value, dtype=_torch().uint8, device=device)
+
+
+def pa_cross_attention(q, k, v, par, o, lse=None, ws=None, stream=None):
+    """o [Nq, Hq, D] (and lse [Hq, Nq] fp32): every row of q over the rows of k and v of
+    its request (make_cross_attention); ws as cross_attention_workspace gives it."""
+    cur = _current_device()
+    Nq, Nk, dt, code = _asked(q, k, par, cur)
+    Hq, Hkv, D = par.Hq, par.Hkv, par.D
+    _check(load().pa_cross_attention(
+        Nq, Nk, code, par.ref, *_rows(q, Nq, Hq, D, dt, "q", cur),
+        *_rows(k, Nk, Hkv, D, dt, "k", cur), *_rows(v, Nk, Hkv, D, dt, "v", cur),
+        *_rows(o, Nq, Hq, D, dt, "o", cur),
+        _in(lse, Nq * Hq, _torch().float32, "lse", False, cur),
+        None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))
+
+
+def pa_cross_attention_backward(q, k, v, o, lse, par, d_o, dq, dk=None, dv=None, ws=None,
+                                stream=None):
+    """dq and, where given, dk and dv from the forward's o and lse and the gradient d_o
+    of o; ws as cross_attention_workspace(..., backward=True) gives it."""
+    cur = _current_device()
+    Nq, Nk, dt, code = _asked(q, k, par, cur)
+    Hq, Hkv, D = par.Hq, par.Hkv, par.D
+    if (dk is None) != (dv is None):
+        raise ValueError("dk and dv go together")
+    none = (None, 0)
+    _check(load().pa_cross_attention_backward(
+        Nq, Nk, code, par.ref, *_rows(q, Nq, Hq, D, dt, "q", cur),
+        *_rows(k, Nk, Hkv, D, dt, "k", cur), *_rows(v, Nk, Hkv, D, dt, "v", cur),
+        *_rows(o, Nq, Hq, D, dt, "o", cur), _in(lse, Nq * Hq, _torch().float32, "lse", True, cur),
+        *_rows(d_o, Nq, Hq, D, dt, "d_o", cur), *_rows(dq, Nq, Hq, D, dt, "dq", cur),
+        *(none if dk is None else _rows(dk, Nk, Hkv, D, dt, "dk", cur)),
+        *(none if dv is None else _rows(dv, Nk, Hkv, D, dt, "dv", cur)),
+        None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))
+
+
+# ---- dropout ----
+def pa_dropout(y, out, p, seed, offset=0, r=None, offset_dev=None, stream=None):
+    """out = r + y / (1 - p) where an element is kept, r (None: 0) where it is not; seed
+    and offset (and offset_dev, a device int64 that is added to it) name the numbers.  The
+    backward is the same call on the gradient without r.  out may be y or r."""
+    cur, n, dt = _current_device(), y.numel(), y.dtype
+    _check(load().pa_dropout(
+        n, _code(dt, "y"), _dev(y, "y", cur), _in(r, n, dt, "r", False, cur),
+        _in(out, n, dt, "out", True, cur), float(p), int(seed) & 0xFFFFFFFFFFFFFFFF,
+        int(offset) & 0xFFFFFFFFFFFFFFFF, _in(offset_dev, 1, _torch().int64, "offset_dev", False,
+                                              cur), B._stream(stream)))

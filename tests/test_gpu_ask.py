@@ -1,0 +1,394 @@
+"""pa_cross_attention and its backward on the GPU against 64 bits (ask_ref.py)."""
+import math
+
+import pytest
+import torch
+
+import ask_ref as R
+from paper_2502_02414_amd import ops
+from pa_cases import say
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+DT = {"f32": F32, "bf16": BF16}
+INF, NAN = float("inf"), float("nan")
+
+
+def offsets(lengths, first=0):
+    out = [first]
+    for n in lengths:
+        out.append(out[-1] + n)
+    return out
+
+
+class Case:
+    """Requests of ql[r] queries and kl[r] states, `first` rows in front of them and
+    `tail` behind; masks: None, "some", "most", "rows" (of request 0 all left out)."""
+
+    def __init__(self, ql, kl, Hq, Hkv, D, dt, mask=None, layout="plain", first=0, tail=0, seed=1,
+                 packed=None):
+        g = torch.Generator()
+        g.manual_seed(seed + 1000 * Hq + D + sum(ql) + 7 * sum(kl))
+        rnd = lambda *s: torch.randn(*s, generator=g)
+        self.packed = len(ql) > 1 or first or tail if packed is None else packed
+        self.q_off = offsets(ql, first) if self.packed else None
+        self.k_off = offsets(kl, first) if self.packed else None
+        Nq, Nk = sum(ql) + first + tail, sum(kl) + first + tail
+        self.Nq, self.Nk, self.Hq, self.Hkv, self.D, self.dt = Nq, Nk, Hq, Hkv, D, dt
+        self.scale = D ** -0.5
+        self.q = (1.5 * rnd(Nq, Hq, D)).to(dt)
+        self.do = (rnd(Nq, Hq, D) + 0.5 * rnd(Hq, D)).to(dt)
+        self.k = (rnd(Nk, Hkv, D) + 0.3 * rnd(Hkv, D)).to(dt)
+        self.v = (rnd(Nk, Hkv, D) + 0.5 * rnd(Hkv, D)).to(dt)
+        self.mask = None
+        if mask is not None:
+            self.mask = torch.rand(Nk, generator=g) < {"some": 0.8, "most": 0.03, "rows": 0.7}[mask]
+            if mask == "rows":
+                a, b = (self.k_off[0], self.k_off[1]) if self.packed else (0, Nk)
+                self.mask[a:b] = False
+            # what is left out may hold anything
+            junk = torch.tensor([NAN, INF, -INF, 3e38])
+            off = ~self.mask
+            self.k[off] = junk[torch.randint(4, (int(off.sum()), Hkv, D), generator=g)].to(dt)
+            self.v[off] = junk[torch.randint(4, (int(off.sum()), Hkv, D), generator=g)].to(dt)
+        # rows of no request: nothing that may reach a result
+        for t, off in ((self.q, self.q_off), (self.do, self.q_off), (self.k, self.k_off),
+                       (self.v, self.k_off)):
+            if off is not None:
+                t[:off[0]] = NAN
+                t[off[-1]:] = NAN
+        dev = lambda t: t.cuda()
+        self.par = ops.make_cross_attention(
+            Hq, Hkv, D, q_off=dev(torch.tensor(self.q_off)) if self.packed else None,
+            k_off=dev(torch.tensor(self.k_off)) if self.packed else None,
+            mask=None if self.mask is None else dev(self.mask), max_k=max(kl))
+        self.layout = layout
+        self.gq, self.gdo = self.place(self.q, 3), self.place(self.do, 0)
+        if layout == "fused":
+            kv = torch.stack((self.k, self.v), 1).cuda()
+            self.gk, self.gv = kv[:, 0], kv[:, 1]
+        else:
+            self.gk, self.gv = self.place(self.k, 1), self.place(self.v, 2)
+
+    def place(self, t, pad):
+        """On the GPU; "apart": in rows that are longer by 8 `pad` elements."""
+        if self.layout != "apart" or not pad:
+            return t.cuda()
+        wide = torch.full((t.shape[0], t[0].numel() + 8 * pad), NAN, dtype=t.dtype)
+        wide[:, :t[0].numel()] = t.flatten(1)
+        return wide.cuda()[:, :t[0].numel()].unflatten(1, t.shape[1:])
+
+    def out(self, like, fill=7.0):
+        if self.layout != "apart":
+            return torch.full(like.shape, fill, dtype=self.dt, device="cuda")
+        wide = torch.full((like.shape[0], like[0].numel() + 16), fill, dtype=self.dt, device="cuda")
+        return wide[:, :like[0].numel()].unflatten(1, like.shape[1:])
+
+    def ws(self, backward=False):
+        return ops.cross_attention_workspace(self.par, self.Nq, self.Nk, self.dt, backward)
+
+    def forward(self):
+        o = self.out(self.q)
+        lse = torch.full((self.Hq, self.Nq), 7.0, device="cuda")
+        ops.pa_cross_attention(self.gq, self.gk, self.gv, self.par, o, lse, self.ws())
+        return o, lse
+
+    def refs(self):
+        return (self.q, self.k, self.v), dict(scale=self.scale, q_off=self.q_off, k_off=self.k_off,
+                                              mask=self.mask)
+
+    def check_forward(self):
+        o, lse = self.forward()
+        a, kw = self.refs()
+        ro, rl, touched = R.forward(*a, **kw)
+        seven = torch.full((), 7.0)
+        R.check(o, ro, self.dt, "o", touched, seven.to(self.dt).expand(o.shape))
+        R.check(lse.t(), rl, F32, "lse", touched, seven.expand(lse.t().shape))
+        return ro, rl
+
+    def check_backward(self):
+        a, kw = self.refs()
+        ro, rl, _ = R.forward(*a, **kw)
+        o, lse = ro.v.to(self.dt), rl.v.t().contiguous().float()
+        ref, tq, tk = R.backward(*a, o, self.do, **kw)
+        dq, dk, dv = self.backward(o, lse)
+        for name, got, t in (("dq", dq, tq), ("dk", dk, tk), ("dv", dv, tk)):
+            R.check(got, ref[name], self.dt, name, t,
+                    torch.full((), 7.0, dtype=self.dt).expand(got.shape))
+        return dq
+
+    def backward(self, o, lse, states=True):
+        dq = self.out(self.q)
+        if self.layout == "fused":
+            z = torch.full((self.Nk, 2, self.Hkv, self.D), 7.0, dtype=self.dt, device="cuda")
+            dk, dv = z[:, 0], z[:, 1]
+        else:
+            dk, dv = self.out(self.k), self.out(self.v)
+        ops.pa_cross_attention_backward(self.gq, self.gk, self.gv, o.cuda(), lse.cuda(), self.par,
+                                        self.gdo, dq, dk if states else None,
+                                        dv if states else None, self.ws(True))
+        return dq, dk, dv
+
+
+CASES = [
+    # ql, kl, Hq, Hkv, D, mask, layout, first, tail
+    ((1,), (1,), 1, 1, 8, None, "plain", 0, 0),
+    ((1,), (64,), 8, 8, 32, None, "fused", 0, 0),
+    ((3,), (5,), 2, 1, 16, None, "plain", 0, 0),
+    ((65,), (63,), 2, 2, 24, None, "apart", 0, 0),
+    ((64,), (64,), 4, 4, 32, "some", "fused", 0, 0),
+    ((200,), (65,), 3, 1, 40, None, "plain", 0, 0),
+    ((129,), (257,), 4, 2, 64, "some", "apart", 0, 0),
+    ((77,), (130,), 2, 2, 72, None, "plain", 0, 0),
+    ((130,), (191,), 6, 2, 96, "some", "plain", 0, 0),
+    ((33,), (300,), 4, 1, 104, None, "fused", 0, 0),
+    ((100,), (129,), 2, 1, 128, "some", "fused", 0, 0),
+    ((700,), (40,), 8, 8, 32, None, "plain", 0, 0),
+    ((900,), (33,), 2, 2, 64, "some", "fused", 0, 0),
+    ((300,), (90,), 4, 4, 16, "most", "plain", 0, 0),
+    # few queries over many states: pieces that are joined
+    ((1,), (5000,), 2, 2, 32, None, "fused", 0, 0),
+    ((2,), (3001,), 8, 2, 64, "some", "plain", 0, 0),
+    ((1,), (2777,), 16, 1, 128, "most", "apart", 0, 0),
+    ((17,), (2048,), 1, 1, 80, None, "plain", 0, 0),
+    # requests: of nothing, of one row, of many; rows in front of them and behind
+    ((0, 5, 1, 70, 0, 64), (3, 0, 1, 65, 9, 64), 2, 2, 32, None, "plain", 0, 5),
+    ((0, 5, 1, 70, 0, 64), (3, 0, 1, 65, 9, 64), 4, 2, 40, "some", "fused", 3, 2),
+    ((10, 20, 30), (40, 50, 60), 4, 1, 64, "rows", "apart", 1, 1),
+    ((128, 1, 200), (1, 128, 0), 2, 1, 128, None, "plain", 0, 0),
+    ((1,) * 70, (33,) * 70, 4, 2, 32, "some", "plain", 0, 1),
+    ((1, 1, 2, 1), (700, 0, 1500, 64), 8, 4, 64, None, "fused", 0, 0),
+    ((5,), (9,), 2, 2, 32, "rows", "plain", 0, 0),
+    ((40,), (100,), 1, 1, 16, None, "plain", 4, 4),
+]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, (sum(c[0]), sum(c[1]), *c[2:]))))
+def test_forward(dt, case):
+    ql, kl, Hq, Hkv, D, mask, layout, first, tail = case
+    say(f"cross attention {dt} {case}")
+    Case(ql, kl, Hq, Hkv, D, DT[dt], mask, layout, first, tail).check_forward()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, (sum(c[0]), sum(c[1]), *c[2:]))))
+def test_backward(dt, case):
+    ql, kl, Hq, Hkv, D, mask, layout, first, tail = case
+    say(f"cross attention backward {dt} {case}")
+    Case(ql, kl, Hq, Hkv, D, DT[dt], mask, layout, first, tail).check_backward()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_gradient_against_differences(dt):
+    """Directional differences of the 64-bit forward against the kernel's gradients,
+    within what ask_ref allows these (the difference itself, step 1e-5, is good to 1e-8
+    of its terms)."""
+    c = Case((9, 14), (21, 30), 4, 2, 24, DT[dt], "some", "plain", 0, 0, seed=5)
+    (q, k, v), kw = c.refs()
+    ro, rl, _ = R.forward(q, k, v, **kw)
+    got = dict(zip(("q", "k", "v"), c.backward(ro.v.to(c.dt), rl.v.t().contiguous().float())))
+    ref = R.backward(q, k, v, ro.v.to(c.dt), c.do, **kw)[0]
+    live = c.mask
+    clean = lambda t: torch.where(live[:, None, None], t.double(), 0.0)
+    at = {"q": q.double(), "k": clean(k), "v": clean(v)}
+
+    def loss(z):
+        w = {n: z[n] for n in at}
+        return (c.do.double() * R.forward(w["q"], w["k"], w["v"], **kw)[0].v).sum().item()
+
+    g = torch.Generator()
+    g.manual_seed(3)
+    for n in at:
+        d = torch.randn(at[n].shape, generator=g, dtype=torch.float64)
+        if n != "q":
+            d = clean(d)
+        h = 1e-5
+        num = (loss({**at, n: at[n] + h * d}) - loss({**at, n: at[n] - h * d})) / (2 * h)
+        mine = (got[n].cpu().double() * d).sum().item()
+        r = ref["d" + n]
+        bound = ((R.half_step(c.dt) * r.v.abs() + 2 * r.worst) * d.abs()).sum().item()
+        size = (r.v * d).abs().sum().item()
+        assert abs(num - mine) <= bound + 1e-7 * size, n
+
+
+def test_only_the_queries_gradient():
+    """Without dk and dv: the same dq, and none of theirs written."""
+    c = Case((70, 3), (100, 40), 4, 2, 32, BF16)
+    (q, k, v), kw = c.refs()
+    ro, rl, _ = R.forward(q, k, v, **kw)
+    o, lse = ro.v.to(BF16), rl.v.t().contiguous().float()
+    dq, _, _ = c.backward(o, lse)
+    alone, dk, dv = c.backward(o, lse, states=False)
+    assert torch.equal(dq, alone) and (dk == 7).all() and (dv == 7).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_no_states_and_no_queries(dt):
+    """Tensors without rows: answers of zeros, gradients of zeros."""
+    par = ops.make_cross_attention(2, 2, 32)
+    e = lambda n: torch.full((n, 2, 32), 7.0, dtype=DT[dt], device="cuda")
+    lse = torch.full((2, 5), 7.0, device="cuda")
+    o, dq, dk, dv = e(5), e(5), e(4), e(4)
+    ops.pa_cross_attention(e(5), e(0), e(0), par, o, lse)
+    assert (o == 0).all() and (lse == -INF).all()
+    ws = lambda a, b: ops.cross_attention_workspace(par, a, b, DT[dt], True)
+    ops.pa_cross_attention_backward(e(5), e(0), e(0), o, lse, par, e(5), dq, e(0), e(0), ws(5, 0))
+    assert (dq == 0).all()
+    ops.pa_cross_attention_backward(e(0), e(4), e(4), e(0), lse[:, :0], par, e(0), e(0), dk, dv,
+                                    ws(0, 4))
+    assert (dk == 0).all() and (dv == 0).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_infinities_and_nan_that_count_stay_in_their_rows(dt):
+    """A NaN query makes its own row NaN; a NaN state every row of its request, and no
+    other request's."""
+    c = Case((6, 5), (40, 70), 2, 2, 32, DT[dt])
+    c.gq[2, 0] = NAN
+    o, lse = c.forward()
+    assert torch.isnan(o[2, 0]).all() and torch.isnan(lse[0, 2])
+    ok = torch.ones(11, 2, dtype=torch.bool)
+    ok[2, 0] = False
+    assert torch.isfinite(o[ok.cuda()]).all()
+    c.gv[45, 1, 3] = NAN
+    o, _ = c.forward()
+    assert torch.isnan(o[6:, 1, 3]).all()
+    bad = torch.isnan(o)
+    bad[6:, 1, 3] = False
+    bad[2, 0] = False
+    assert not bad.any()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_scores_far_apart(dt):
+    """Scores from -3e4 to 3e4: one state takes all the weight, nothing overflows."""
+    c = Case((50,), (200,), 2, 1, 32, DT[dt])
+    c.q *= 400
+    c.gq *= 400
+    c.check_forward()
+    c.check_backward()
+
+
+def test_offsets_beyond_32_bits():
+    """Rows so far apart that their elements lie beyond 2^32: the same as close by."""
+    c = Case((3, 40), (900, 1200), 4, 2, 64, BF16, "some")
+    o, lse = c.forward()
+    g = c.backward(o, lse)
+    pitch = 1 << 22
+    wide = torch.empty(c.Nk, pitch, dtype=BF16, device="cuda")  # 17.6 GB
+    assert wide.numel() > 1 << 32
+    kv = wide[:, :256].unflatten(1, (2, 2, 64))
+    kv[:, 0], kv[:, 1] = c.gk, c.gv
+    c.gk, c.gv = kv[:, 0], kv[:, 1]
+    o2, lse2 = c.forward()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+    far = wide[:, 1024:1280].unflatten(1, (2, 2, 64))
+    far.fill_(7.0)
+    dq = c.out(c.q)
+    ops.pa_cross_attention_backward(c.gq, c.gk, c.gv, o, lse, c.par, c.gdo, dq, far[:, 0], far[:, 1],
+                                    c.ws(True))
+    for a, b in zip(g, (dq, far[:, 0], far[:, 1])):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("case", [((1,), (6000,), 8, 2, 64), ((700, 900), (64, 50), 8, 8, 32),
+                                  ((500,), (700,), 4, 1, 128)])
+def test_the_same_bits_every_time(dt, case):
+    c = Case(*case, DT[dt], "some")
+    o, lse = c.forward()
+    g = c.backward(o, lse)
+    for _ in range(4):
+        o2, lse2 = c.forward()
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+        assert all(torch.equal(a, b) for a, b in zip(g, c.backward(o, lse)))
+
+
+def test_a_padded_batch():
+    """[B, L] rows with lengths: requests of L rows whose padding the mask leaves out."""
+    B, L, Lk, H, D = 5, 37, 90, 4, 32
+    g = torch.Generator()
+    g.manual_seed(8)
+    q, k, v = (torch.randn(B * n, H, D, generator=g).to(BF16) for n in (L, Lk, Lk))
+    kl = torch.tensor([90, 1, 0, 64, 33])
+    mask = (torch.arange(Lk) < kl[:, None]).view(-1)
+    qo, ko = torch.arange(B + 1) * L, torch.arange(B + 1) * Lk
+    par = ops.make_cross_attention(H, H, D, q_off=qo.cuda(), k_off=ko.cuda(), mask=mask.cuda(),
+                                   max_k=Lk)
+    o = torch.empty_like(q, device="cuda")
+    ops.pa_cross_attention(q.cuda(), k.cuda(), v.cuda(), par, o,
+                           ws=ops.cross_attention_workspace(par, B * L, B * Lk, BF16))
+    ref, _, touched = R.forward(q, k, v, D ** -0.5, qo.tolist(), ko.tolist(), mask)
+    R.check(o, ref, BF16, "o", touched, o.cpu())
+    assert (o[2 * L:3 * L] == 0).all()
+
+
+def test_max_k_steers_the_choice_alone():
+    """Too small a max_k, none and the right one: results within the bounds."""
+    for max_k in (0, 1, 64, 1000):
+        c = Case((300, 200), (64, 200), 8, 8, 32, BF16)
+        c.par.st.max_k = max_k
+        c.check_forward()
+        c.check_backward()
+
+
+def test_offsets_outside_of_the_tensors():
+    """Offsets that leave the tensors count as their ends."""
+    c = Case((30, 50), (40, 20), 2, 2, 32, BF16)
+    want, _ = c.forward()
+    c.par = ops.make_cross_attention(2, 2, 32, q_off=torch.tensor([-5, 30, 1 << 40]).cuda(),
+                                     k_off=torch.tensor([-(1 << 50), 40, 61]).cuda())
+    got, _ = c.forward()
+    assert torch.equal(want, got)
+
+
+def test_on_other_streams_and_two_at_once():
+    """A stream that is handed over, and two calls at once with a workspace each."""
+    c = Case((2,), (9000,), 4, 2, 64, BF16)
+    o, lse = c.forward()
+    dq, dk, dv = c.backward(o, lse)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for s in streams:
+        o2, l2 = c.out(c.q), torch.zeros_like(lse)
+        g2 = [c.out(t) for t in (c.q, c.k, c.v)]
+        outs.append((o2, l2, g2, c.ws(), c.ws(True)))
+    torch.cuda.synchronize()
+    for s, (o2, l2, g2, w, wb) in zip(streams, outs):
+        ops.pa_cross_attention(c.gq, c.gk, c.gv, c.par, o2, l2, w, stream=s)
+        ops.pa_cross_attention_backward(c.gq, c.gk, c.gv, o, lse, c.par, c.gdo, *g2, wb, stream=s)
+    torch.cuda.synchronize()
+    for o2, l2, g2, *_ in outs:
+        assert torch.equal(o, o2) and torch.equal(lse, l2)
+        assert all(torch.equal(a, b) for a, b in zip((dq, dk, dv), g2))
+
+
+@pytest.mark.parametrize("case", [((2,), (5000,), 4, 2, 64), ((300, 9), (64, 40), 8, 8, 32)])
+def test_in_a_graph(case):
+    """Forward and backward captured; replays on new inputs, eager calls between them."""
+    c = Case(*case, BF16)
+    o, lse = c.out(c.q), torch.zeros(c.Hq, c.Nq, device="cuda")
+    g = [c.out(t) for t in (c.q, c.k, c.v)]
+    ws, wb = c.ws(), c.ws(True)
+
+    def both(o, lse, g, ws, wb):
+        ops.pa_cross_attention(c.gq, c.gk, c.gv, c.par, o, lse, ws)
+        ops.pa_cross_attention_backward(c.gq, c.gk, c.gv, o, lse, c.par, c.gdo, *g, wb)
+
+    both(o, lse, g, ws, wb)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(o, lse, g, ws, wb)
+    for rep in range(5):
+        c.gq.copy_(torch.randn(c.gq.shape, device="cuda"))
+        c.gk.copy_(torch.randn(c.gk.shape, device="cuda"))
+        eo, el, eg = c.out(c.q), torch.zeros_like(lse), [c.out(t) for t in (c.q, c.k, c.v)]
+        both(eo, el, eg, c.ws(), c.ws(True))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, eo) and torch.equal(lse, el), rep
+        assert all(torch.equal(a, b) for a, b in zip(g, eg)), rep
