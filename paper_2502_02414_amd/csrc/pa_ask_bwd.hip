@@ -35,7 +35,8 @@ __global__ void __launch_bounds__(256) k_ask_dq(AskArgs a) {
   const int64_t tile = slot - ((qr.b * G) >> SHIFT) - rq;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  const Range kr = piece(range_of(a.k_off, rq, a.Nk), s, a.S);
+  const Range all = range_of(a.k_off, rq, a.Nk), kr = piece(all, s, a.S);
+  if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const T* K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
@@ -203,7 +204,7 @@ __global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
   if (rq < 0) return;
   const Range kr = range_of(a.k_off, rq, a.Nk);
   const int64_t tile = slot - (kr.b >> 6) - rq;
-  if (tile < 0 || tile * kTile >= kr.e - kr.b) return;
+  if (tile < 0 || tile * kTile >= kr.e - kr.b || kr.e - kr.b <= a.few) return;
   const Range qr = range_of(a.q_off, rq, a.Nq);
   const Range vr = piece(Range{0, (qr.e - qr.b) * G}, s, a.SQ);  // virtual rows
   const int n = (int)vr.e;
@@ -381,7 +382,14 @@ int ask_pieces_q(const AskArgs& a) {
 }
 
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st) {
-  return dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  if (!ask_few_backward_served(a, dtype)) return dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  const hipError_t e = launch_ask_few_backward(a, st);
+  if (e != hipSuccess || a.R == 1 || a.Nk <= ask_few_most(a)) return e;
+  // (a request that is longer than max_k says)
+  AskArgs rest = a;
+  rest.few = ask_few_most(a);
+  rest.S = rest.SQ = 1;
+  return width<bf16>(rest, st);
 }
 
 }  // namespace pa

@@ -1,0 +1,499 @@
+// Attention of many query points over few states, as a block stack's 16 to 64 are
+// (gfx950, bf16): a wave keeps its head's rows of k and v in registers and streams the
+// queries past them, forward and backward in one pass each.
+//
+// Forward: scores as k q^T (states are rows, queries columns), left out states as
+// -infinity in the accumulators' first value, and o^T = v^T p^T with the weights as
+// they leave the first product.  v's columns are permuted so that a lane has eight
+// consecutive elements of its query's row of o.
+// Backward: the same for p and dp = v do^T; delta = sum_j p dp is formed here (all
+// states are at hand), so that o is not read and a lone state's ds is 0; dq^T = k^T
+// ds^T.  The sums over the queries, dv += p^T do and dk += ds^T q, need p and ds with
+// queries along the product: they go through the wave's part of LDS, as do q and do.
+// A block's dk and dv are a record in the workspace, added in order.
+#include "pa_ask.hpp"
+
+namespace pa {
+namespace {
+using namespace ask;
+
+// Row 4 g + i of product tile d stands for element 32 (d / 2) + 8 g + 4 (d % 2) + i.
+__device__ __forceinline__ int column_of(int d, int r) {
+  return 32 * (d >> 1) + 8 * (r >> 2) + 4 * (d & 1) + (r & 3);
+}
+
+// The states of one head as operands.
+template <int DP, int NT> struct States {
+  static constexpr int NK = DP / 32, ND = DP / 16;
+  // rows: lane (r, g) elements 32 k + 8 g .. of state 16 t + r
+  static __device__ __forceinline__ void rows(K32<bf16> (&f)[NT][NK], const bf16* base, int64_t ld,
+                                              Range k, const uint8_t* mask, int D) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int64_t p = k.b + 16 * t + (lane_id() & 15);
+      bool counts = p < k.e;
+      if (k.b < k.e) {
+        const int64_t pc = counts ? p : k.e - 1;
+        if (mask) counts = counts && mask[pc];
+        row_frags<bf16, DP>(f[t], base + pc * ld, D, counts);
+      } else {
+#pragma unroll
+        for (int c = 0; c < NK; ++c) f[t][c].v = __builtin_bit_cast(bf16x8, zero16());
+      }
+    }
+  }
+  // columns: lane (r, g) element column_of(d, r) of states 16 t + 4 g .. + 3, from rows
+  // by way of the wave's part of LDS (kBytes of it)
+  static constexpr int RB = 2 * DP + 32, kBytes = 16 * NT * RB;
+  static __device__ __forceinline__ void columns(K16<bf16> (&f)[ND][NT],
+                                                 const K32<bf16> (&rows)[NT][NK], char* mine) {
+    const int r = lane_id() & 15, g = lane_id() >> 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+        *reinterpret_cast<bf16x8*>(mine + lds_off(16 * t + r, 64 * k + 16 * g, RB)) = rows[t][k].v;
+    wave_sync();
+    const int at = lds_off(4 * g + (r >> 2), 16 * (r & 3), RB);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+        ld_tr<bf16>(f[d][t], mine, at, 16 * t * RB + 64 * (d >> 1) + 8 * (d & 1), RB);
+    wave_sync();
+  }
+  // 0, or -infinity where a state is left out
+  static __device__ __forceinline__ void alive(f32x4 (&f)[NT], Range k, const uint8_t* mask) {
+    const int g = lane_id() >> 4;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t p = k.b + 16 * t + 4 * g + i;
+        bool counts = p < k.e;
+        if (mask && k.b < k.e) counts = counts && mask[counts ? p : k.e - 1];
+        f[t][i] = counts ? 0.f : -INFINITY;
+      }
+  }
+};
+
+// A wave's LDS in the backward: 32 rows of q and of do, 32 of p (or ds).
+template <int DP, int NT> constexpr int few_bwd_bytes() {
+  return States<DP, NT>::kBytes > 64 * (2 * DP + 32) + 32 * (32 * NT + 32)
+             ? States<DP, NT>::kBytes
+             : 64 * (2 * DP + 32) + 32 * (32 * NT + 32);
+}
+
+// A virtual row of a request.
+struct Place {
+  int v, n;         // of n rows
+  uint32_t i, g;    // its query and head of the group (of row n - 1 past the end)
+  __device__ __forceinline__ void at(int v_, int n_, int G) {
+    v = v_;
+    n = n_;
+    const uint32_t c = v < n ? v : n - 1;
+    i = G == 1 ? c : c / (uint32_t)G;
+    g = c - i * G;
+  }
+  __device__ __forceinline__ bool in() const { return v < n; }
+};
+
+// Which of the block's waves works on what: `heads` of them a head each, the others on
+// other tiles of the same heads.
+struct Role {
+  int h, sub, subs;
+};
+__device__ __forceinline__ Role role_of(int Hkv) {
+  const int w = threadIdx.x >> 6, W = blockDim.x >> 6, heads = Hkv < W ? Hkv : W;
+  return {(int)blockIdx.y * heads + w % heads, w / heads, W / heads};
+}
+
+template <int DP, int NT>
+__global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs a, int P) {
+  constexpr int NK = DP / 32, ND = DP / 16, C = 2;  // C: tiles of 16 queries at once
+  using S_ = States<DP, NT>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int G = a.Hq / a.Hkv;
+  const Role me = role_of(a.Hkv);
+  const int rq = blockIdx.x / P;
+  const Range qr = range_of(a.q_off, rq, a.Nq), kr = range_of(a.k_off, rq, a.Nk);
+  const Range vr = piece(Range{0, (qr.e - qr.b) * G}, blockIdx.x % P, P);
+  if (me.h >= a.Hkv || me.sub >= me.subs || vr.b >= vr.e) return;
+  const int n = (int)vr.e;
+  const int lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const bf16* Q = reinterpret_cast<const bf16*>(a.q) + (int64_t)me.h * G * a.D + qr.b * a.ldq;
+  const bf16* K = reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D;
+  const bf16* V = reinterpret_cast<const bf16*>(a.v) + (int64_t)me.h * a.D;
+  bf16* O = reinterpret_cast<bf16*>(a.o) + (int64_t)me.h * G * a.D + qr.b * a.ldo;
+  const float sc = a.scale * kLog2e;
+
+  // (longer ones are the other kernel's, none has no states to read)
+  if (kr.e - kr.b > 16 * NT) return;
+  K32<bf16> kf[NT][NK];
+  K16<bf16> vf[ND][NT];
+  f32x4 none[NT];
+  {
+    K32<bf16> vr_[NT][NK];
+    S_::rows(kf, K, a.ldk, kr, a.mask, a.D);
+    S_::rows(vr_, V, a.ldv, kr, a.mask, a.D);
+    S_::alive(none, kr, a.mask);
+    S_::columns(vf, vr_, smem + (threadIdx.x >> 6) * S_::kBytes);
+  }
+
+  struct Tile {
+    Place at[C];
+    K32<bf16> q[C][NK];
+  };
+  const int step = 16 * C * me.subs;
+  auto load = [&](int v, Tile& t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      t.at[c].at(v + 16 * c + r, n, G);
+      const bf16* row = Q + t.at[c].i * a.ldq + t.at[c].g * a.D;
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const int col = 32 * k + 8 * g;
+        const uint4 x = ld_global16<true>(row + (col < a.D ? col : 0));
+        t.q[c][k].v = __builtin_bit_cast(bf16x8, col < a.D ? x : zero16());
+      }
+    }
+  };
+  auto work = [&](const Tile& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      f32x4 x[NT], o[ND];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        x[t] = none[t];
+#pragma unroll
+        for (int k = 0; k < NK; ++k) x[t] = mma32(kf[t][k], q.q[c][k], x[t]);
+      }
+      float mx = x[0][0];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[t][i]);
+      mx = groups_max(mx) * sc;
+      const float base = mx == -INFINITY ? 0.f : mx;
+      float sum = 0.f;
+      K16<bf16> pf[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          p[i] = fast_exp2(fmaf(x[t][i], sc, -base));
+          sum += p[i];
+        }
+        set_k16(pf[t], p[0], p[1], p[2], p[3]);
+      }
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        o[d] = zero4();
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) o[d] = mma16x2(vf[d][t], pf[t], vf[d][t + 1], pf[t + 1], o[d]);
+      }
+      sum = groups_sum(sum);
+      const float inv = sum > 0.f ? fast_rcp(sum) : sum == 0.f ? 0.f : sum;
+      const float lse2 = sum == 0.f ? -INFINITY : base + __builtin_amdgcn_logf(sum);
+      if (!q.at[c].in()) continue;
+      bf16* to = O + q.at[c].i * a.ldo + q.at[c].g * a.D + 8 * g;
+#pragma unroll
+      for (int d = 0; d < ND; d += 2) {
+        bf16x8 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[i] = (bf16)(o[d][i] * inv);
+          y[i + 4] = (bf16)(o[d + 1][i] * inv);
+        }
+        if (16 * d + 8 * g < a.D) st_global16(to + 16 * d, __builtin_bit_cast(uint4, y));
+      }
+      if (a.lse && g == 0)
+        a.lse[(int64_t)(me.h * G + q.at[c].g) * a.Nq + qr.b + q.at[c].i] = lse2 * kLn2;
+    }
+  };
+  int v = (int)vr.b + 16 * C * me.sub;
+  if (v >= n) return;
+  Tile t0, t1;
+  load(v, t0);
+  for (;;) {  // the next tiles on their way while these are worked on
+    load(v + step, t1);
+    work(t0);
+    if ((v += step) >= n) break;
+    load(v + step, t0);
+    work(t1);
+    if ((v += step) >= n) break;
+  }
+}
+
+// The same states' gradients and the queries', 32 queries of a wave's head at a time.
+template <int DP, int NT, int TH>
+__global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) {
+  constexpr int NK = DP / 32, ND = DP / 16;
+  constexpr int RB = 2 * DP + 32, PB = 32 * NT + 32;  // bytes of LDS rows: q and do; p and ds
+  constexpr int CPR = DP / 8, NCH = CPR / 2;          // 16-byte chunks of a row; per lane of 32 rows
+  using S_ = States<DP, NT>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int G = a.Hq / a.Hkv;
+  const Role me = role_of(a.Hkv);
+  const int rq = blockIdx.x / P;
+  const Range qr = range_of(a.q_off, rq, a.Nq), kr = range_of(a.k_off, rq, a.Nk);
+  const Range vr = piece(Range{0, (qr.e - qr.b) * G}, blockIdx.x % P, P);
+  // (requests that are longer are the other kernels')
+  if (me.h >= a.Hkv || me.sub >= me.subs || kr.e - kr.b > 16 * NT) return;
+  const int n = (int)vr.e;
+  const int lane = lane_id(), r = lane & 15, g = lane >> 4;
+  const int64_t head = (int64_t)me.h * G * a.D;
+  const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head + qr.b * a.ldq;
+  const bf16* DO = reinterpret_cast<const bf16*>(a.d_o) + head + qr.b * a.lddo;
+  bf16* DQ = reinterpret_cast<bf16*>(a.dq) + head + qr.b * a.lddq;
+  const float sc = a.scale * kLog2e;
+  char* qt = smem + (threadIdx.x >> 6) * few_bwd_bytes<DP, NT>();
+  char* dt = qt + 32 * RB;
+  char* pt = qt + 64 * RB;
+
+  K32<bf16> kf[NT][NK], vf[NT][NK];
+  K16<bf16> kc[ND][NT];
+  f32x4 none[NT], dk[NT][ND], dv[NT][ND];
+  S_::rows(kf, reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D, a.ldk, kr, a.mask, a.D);
+  S_::rows(vf, reinterpret_cast<const bf16*>(a.v) + (int64_t)me.h * a.D, a.ldv, kr, a.mask, a.D);
+  S_::alive(none, kr, a.mask);
+  S_::columns(kc, kf, qt);
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) dk[t][d] = dv[t][d] = zero4();
+
+  struct Tile {
+    uint4 q[NCH], d[NCH];
+    Place at[2];
+    float lse[2];
+  } tl;
+  auto load = [&](int v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = lane + 64 * j, col = (c % CPR) * 8;
+      Place at;
+      at.at(v + c / CPR, n, G);
+      const int64_t in = at.g * a.D + (col < a.D ? col : 0);
+      const uint4 x = ld_global16<true>(Q + at.i * a.ldq + in);
+      const uint4 y = ld_global16<true>(DO + at.i * a.lddo + in);
+      const bool ok = at.in() && col < a.D;
+      tl.q[j] = ok ? x : zero16();
+      tl.d[j] = ok ? y : zero16();
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      Place& at = tl.at[c];
+      at.at(v + 16 * c + r, n, G);
+      const float l = a.lse[(int64_t)(me.h * G + at.g) * a.Nq + qr.b + at.i] * kLog2e;
+      tl.lse[c] = !at.in() || l == -INFINITY ? INFINITY : l;  // (weights of 0)
+    }
+  };
+  const RowBase<bf16> rb = row_base<bf16>(r, RB);
+  const int tr = tr_base<bf16>(RB), tp = tr_base<bf16>(PB), sp = r * PB + 8 * g;
+  const int step = 32 * me.subs;
+  int v = (int)vr.b + 32 * me.sub;
+  if (v < n) load(v);
+  for (; v < n; v += step) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = lane + 64 * j;
+      *reinterpret_cast<uint4*>(qt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.q[j];
+      *reinterpret_cast<uint4*>(dt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.d[j];
+    }
+    const Place at[2] = {tl.at[0], tl.at[1]};
+    const float lse[2] = {tl.lse[0], tl.lse[1]};
+    wave_sync();
+    if (v + step < n) load(v + step);
+    K16<bf16> sf[2][NT];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      K32<bf16> qf[NK], of[NK];
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        ld_row<bf16>(qf[k], qt, rb, 16 * c * RB + 64 * k);
+        ld_row<bf16>(of[k], dt, rb, 16 * c * RB + 64 * k);
+      }
+      f32x4 x[NT], dp[NT];
+      float delta = 0.f;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        x[t] = none[t];
+        dp[t] = zero4();
+#pragma unroll
+        for (int k = 0; k < NK; ++k) {
+          x[t] = mma32(kf[t][k], qf[k], x[t]);
+          dp[t] = mma32(vf[t][k], of[k], dp[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[t][i] = fast_exp2(fmaf(x[t][i], sc, -lse[c]));
+          delta = fmaf(x[t][i], dp[t][i], delta);
+        }
+        K16<bf16> pf;
+        set_k16(pf, x[t][0], x[t][1], x[t][2], x[t][3]);
+        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = pf.v;
+      }
+      delta = groups_sum(delta);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float ds[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ds[i] = x[t][i] * (dp[t][i] - delta);
+        set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
+      }
+      f32x4 dq[ND];
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        dq[d] = zero4();
+#pragma unroll
+        for (int t = 0; t < NT; t += 2)
+          dq[d] = mma16x2(kc[d][t], sf[c][t], kc[d][t + 1], sf[c][t + 1], dq[d]);
+      }
+      if (at[c].in()) {
+        bf16* to = DQ + at[c].i * a.lddq + at[c].g * a.D + 8 * g;
+#pragma unroll
+        for (int d = 0; d < ND; d += 2) {
+          bf16x8 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            y[i] = (bf16)(dq[d][i] * a.scale);
+            y[i + 4] = (bf16)(dq[d + 1][i] * a.scale);
+          }
+          if (16 * d + 8 * g < a.D) st_global16(to + 16 * d, __builtin_bit_cast(uint4, y));
+        }
+      }
+    }
+    // acc += (p or ds, in LDS)^T (rows, in LDS)
+    auto add = [&](const char* rows, f32x4(&acc)[NT][ND]) __attribute__((always_inline)) {
+      wave_sync();
+      K16<bf16> b0[ND], b1[ND];
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        ld_tr<bf16>(b0[d], rows, tr, 32 * d, RB);
+        ld_tr<bf16>(b1[d], rows, tr, 16 * RB + 32 * d, RB);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        K16<bf16> a0, a1;
+        ld_tr<bf16>(a0, pt, tp, 32 * t, PB);
+        ld_tr<bf16>(a1, pt, tp, 16 * PB + 32 * t, PB);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[t][d] = mma16x2(a0, b0[d], a1, b1[d], acc[t][d]);
+      }
+      wave_sync();
+    };
+    add(dt, dv);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = sf[c][t].v;
+    add(qt, dk);
+  }
+  if (!a.dk) return;
+  const int64_t rec = (int64_t)16 * NT * a.Hkv * a.D;
+  const int64_t at = ((int64_t)blockIdx.x * me.subs + me.sub) * rec + (int64_t)me.h * a.D;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+      if (16 * d + r >= a.D) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t to = at + (int64_t)(16 * t + 4 * g + i) * a.Hkv * a.D + 16 * d + r;
+        a.part_k[to] = dk[t][d][i] * a.scale;
+        a.part_v[to] = dv[t][d][i];
+      }
+    }
+}
+
+// A request's records added, each of 8 threads every eighth and those in order: four
+// elements of its states' rows.
+__global__ void __launch_bounds__(256) k_ask_few_sum(AskArgs a, int per, int64_t rec, int blocks) {
+  __shared__ f32x4 part[8][32];
+  const int rq = blockIdx.x / blocks, u = threadIdx.x >> 5, c = threadIdx.x & 31;
+  const int64_t e = ((int64_t)(blockIdx.x % blocks) * 32 + c) * 4, width = (int64_t)a.Hkv * a.D;
+  const Range kr = range_of(a.k_off, rq, a.Nk);
+  const int64_t n = (kr.e - kr.b) * width;
+  if (n > rec) return;  // (not this kernel's)
+  const float* p = (blockIdx.y ? a.part_v : a.part_k) + (int64_t)rq * per * rec;
+  f32x4 s = zero4();
+  if (e < n)
+    for (int i = u; i < per; i += 8) s += *reinterpret_cast<const f32x4*>(p + i * rec + e);
+  part[u][c] = s;
+  __syncthreads();
+  if (u || e >= n) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) s += part[i][c];
+  const int64_t row = e / width, col = e - row * width;
+  bf16* to = reinterpret_cast<bf16*>(blockIdx.y ? a.dv : a.dk);
+  store4<bf16>(to + (kr.b + row) * (blockIdx.y ? a.lddv : a.lddk) + col, s);
+}
+
+// Blocks of a request, and how many waves of a block share a head.
+struct Split {
+  int P, groups, subs, waves;
+};
+Split split_of(const AskArgs& a, bool bwd) {
+  Split s;
+  s.waves = bwd && a.D > 32 && a.max_k > 32 ? 4 : 8;
+  const int heads = a.Hkv < s.waves ? a.Hkv : s.waves;
+  s.groups = (a.Hkv + heads - 1) / heads;
+  s.subs = s.waves / heads;
+  // some 2048 blocks forward, one per CU backward; at least two tiles a wave
+  const int64_t n = a.Nq * (a.Hq / a.Hkv) / a.R, least = 64 * s.subs;
+  int64_t P = (bwd ? 256 : 2048) / ((int64_t)a.R * s.groups);
+  if (P > n / least) P = n / least;
+  s.P = P < 1 ? 1 : (int)P;
+  return s;
+}
+int tiles_of(const AskArgs& a) { return a.max_k <= 32 ? 2 : 4; }
+
+template <int DP, int NT> hipError_t launch(const AskArgs& a, bool bwd, hipStream_t st) {
+  const Split s = split_of(a, bwd);
+  const dim3 grid((uint32_t)(a.R * s.P), s.groups), block(64 * s.waves);
+  constexpr int TH = DP * NT > 128 ? 256 : 512, lds = States<DP, NT>::kBytes;
+  constexpr int lds_bwd = few_bwd_bytes<DP, NT>();
+  if (!bwd) hipLaunchKernelGGL((k_ask_few<DP, NT>), grid, block, s.waves * lds, st, a, s.P);
+  else hipLaunchKernelGGL((k_ask_few_bwd<DP, NT, TH>), grid, block, s.waves * lds_bwd, st, a, s.P);
+  return hipGetLastError();
+}
+hipError_t sizes(const AskArgs& a, bool bwd, hipStream_t st) {
+  const bool two = tiles_of(a) == 2;
+  if (a.D <= 32) return two ? launch<32, 2>(a, bwd, st) : launch<32, 4>(a, bwd, st);
+  return two ? launch<64, 2>(a, bwd, st) : launch<64, 4>(a, bwd, st);
+}
+
+}  // namespace
+
+bool ask_few_served(const AskArgs& a, int dtype) {
+  return dtype == 1 && a.D <= 64 && a.max_k <= 64 && a.R <= (1 << 20);
+}
+int ask_few_most(const AskArgs& a) { return 16 * tiles_of(a); }
+
+// Floats of the backward's records of dk, or of dv.
+int64_t ask_few_records(const AskArgs& a) {
+  const Split s = split_of(a, true);
+  return (int64_t)a.R * s.P * s.subs * 16 * tiles_of(a) * a.Hkv * a.D;
+}
+// (records of up to 256 MB: for more requests than that the other kernels need none)
+bool ask_few_backward_served(const AskArgs& a, int dtype) {
+  return ask_few_served(a, dtype) && ask_few_records(a) <= (1 << 25);
+}
+
+hipError_t launch_ask_few(const AskArgs& a, hipStream_t st) { return sizes(a, false, st); }
+
+hipError_t launch_ask_few_backward(const AskArgs& a, hipStream_t st) {
+  hipError_t e = sizes(a, true, st);
+  if (e != hipSuccess || !a.dk) return e;
+  const Split s = split_of(a, true);
+  const int64_t rec = (int64_t)16 * tiles_of(a) * a.Hkv * a.D;
+  const int blocks = (int)((rec / 4 + 31) / 32);
+  hipLaunchKernelGGL(k_ask_few_sum, dim3((uint32_t)(a.R * blocks), 2), dim3(256), 0, st, a,
+                     s.P * s.subs, rec, blocks);
+  return hipGetLastError();
+}
+
+}  // namespace pa

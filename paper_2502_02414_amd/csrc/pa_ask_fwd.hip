@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
   const int64_t tile = slot - ((qr.b * G) >> SHIFT) - (a.q_off ? rq : 0);
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  const Range kr = piece(range_of(a.k_off, rq, a.Nk), s, a.S);
+  const Range all = range_of(a.k_off, rq, a.Nk), kr = piece(all, s, a.S);
+  if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
@@ -227,7 +228,17 @@ int ask_pieces(const AskArgs& a) {
 }
 
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
-  hipError_t e = dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  hipError_t e;
+  if (ask_few_served(a, dtype)) {
+    e = launch_ask_few(a, st);
+    if (e != hipSuccess || a.R == 1 || a.Nk <= ask_few_most(a)) return e;
+    // (a request that is longer than max_k says)
+    AskArgs rest = a;
+    rest.few = ask_few_most(a);
+    rest.S = 1;
+    return width<bf16>(rest, st);
+  }
+  e = dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t threads = a.Nq * a.Hq * (a.D / 4);
   const dim3 grid((uint32_t)((threads + 255) / 256));

@@ -591,7 +591,7 @@ static pa_status ask_rows(const char* who, const char* name, const void* ptr, in
 static Rows flat(const char* name, const void* p, uint64_t bytes) { return {name, p, 1, bytes, bytes}; }
 
 // The workspace's parts, of which the forward has the first two; returns the bytes.
-static size_t ask_layout(pa::AskArgs* a, bool backward, void* ws) {
+static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
   char* base = reinterpret_cast<char*>(ws);
   size_t at = 0;
   const auto take = [&](uint64_t floats) {
@@ -600,6 +600,14 @@ static size_t ask_layout(pa::AskArgs* a, bool backward, void* ws) {
     return p;
   };
   const uint64_t rows = (uint64_t)a->Nq * a->Hq;
+  if (backward ? pa::ask_few_backward_served(*a, dtype) : pa::ask_few_served(*a, dtype)) {
+    if (!backward) return at;
+    const uint64_t n = (uint64_t)pa::ask_few_records(*a);
+    a->part_k = take(n);
+    a->part_v = take(n);
+    a->delta = take(rows);  // (for requests that are longer than max_k says)
+    return at;
+  }
   a->S = pa::ask_pieces(*a);
   if (a->S > 1) {
     a->part = take((uint64_t)a->S * rows * a->D);
@@ -624,7 +632,7 @@ pa_status pa_cross_attention_workspace(int64_t Nq, int64_t Nk, pa_dtype dtype,
   pa::AskArgs a;
   PO_TRY(ask_params(who, Nq, Nk, dtype, p, &a));
   if (!bytes) return err(PA_ERR_INVALID, "%s: bytes is NULL", who);
-  *bytes = ask_layout(&a, backward != 0, nullptr);
+  *bytes = ask_layout(&a, dtype, backward != 0, nullptr);
   return PA_OK;
 }
 
@@ -641,7 +649,7 @@ pa_status pa_cross_attention(int64_t Nq, int64_t Nk, pa_dtype dtype,
   PO_TRY(ask_rows(who, "v", v, Nk, a.Hkv, a.D, &ldv, dtype, &rv));
   PO_TRY(ask_rows(who, "o", o, Nq, a.Hq, a.D, &ldo, dtype, &ro));
   PO_TRY(opt(who, lse, "lse", 4));
-  const size_t bytes = ask_layout(&a, false, nullptr);
+  const size_t bytes = ask_layout(&a, dtype, false, nullptr);
   if (bytes && (!ws || ws_bytes < bytes))
     return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, bytes);
   if (bytes) PO_TRY(opt(who, ws, "ws"));
@@ -650,7 +658,7 @@ pa_status pa_cross_attention(int64_t Nq, int64_t Nk, pa_dtype dtype,
                     {rq, rk, rv, flat("mask", a.mask, (uint64_t)Nk), flat("q_off", a.q_off, offs),
                      flat("k_off", a.k_off, offs)}));
   if (!Nq) return PA_OK;
-  ask_layout(&a, false, ws);
+  ask_layout(&a, dtype, false, ws);
   a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse;
   a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
   PO_HIP(pa::launch_ask(a, dtype, as_stream(stream)), who);
@@ -679,7 +687,8 @@ pa_status pa_cross_attention_backward(int64_t Nq, int64_t Nk, pa_dtype dtype,
   PO_TRY(ask_rows(who, "dk", dk, states ? Nk : 0, a.Hkv, a.D, &lddk, dtype, &rdk));
   PO_TRY(ask_rows(who, "dv", dv, states ? Nk : 0, a.Hkv, a.D, &lddv, dtype, &rdv));
   if (Nq) PO_TRY(need(who, lse, "lse", 4));
-  const size_t bytes = ask_layout(&a, true, nullptr);
+  if (!Nq && !Nk) return PA_OK;
+  const size_t bytes = ask_layout(&a, dtype, true, nullptr);
   if (bytes && (!ws || ws_bytes < bytes))
     return err(PA_ERR_WORKSPACE, "%s: workspace needs %zu bytes", who, bytes);
   if (bytes) PO_TRY(opt(who, ws, "ws"));
@@ -688,8 +697,7 @@ pa_status pa_cross_attention_backward(int64_t Nq, int64_t Nk, pa_dtype dtype,
                     {rq, rk, rv, ro, rd, flat("lse", lse, (uint64_t)Nq * a.Hq * 4),
                      flat("mask", a.mask, (uint64_t)Nk), flat("q_off", a.q_off, offs),
                      flat("k_off", a.k_off, offs)}));
-  if (!Nq && !Nk) return PA_OK;
-  ask_layout(&a, true, ws);
+  ask_layout(&a, dtype, true, ws);
   a.q = q; a.k = k; a.v = v; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse);
   a.ldq = ldq; a.ldk = ldk; a.ldv = ldv; a.ldo = ldo;
   a.d_o = d_o; a.dq = dq; a.lddo = lddo; a.lddq = lddq;

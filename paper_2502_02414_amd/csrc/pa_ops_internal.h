@@ -115,7 +115,8 @@ struct AskArgs {
   float scale = 1.f;
   const int64_t *q_off = nullptr, *k_off = nullptr;  // [R + 1], both or none (R = 1)
   const uint8_t* mask = nullptr;                     // [Nk]
-  int64_t max_k = 0;  // states of the longest request, or more; steers choices only
+  int64_t max_k = 0;  // states of the longest request, as the caller knows it
+  int few = -1;       // requests of at most so many states are another kernel's
   int64_t ldq = 0, ldk = 0, ldv = 0, ldo = 0;        // elements between rows
   const void *q = nullptr, *k = nullptr, *v = nullptr;
   void* o = nullptr;     // (read by the backward)
@@ -131,11 +132,18 @@ struct AskArgs {
   float* delta = nullptr;   // [Hq,Nq]
   float* part_b = nullptr;  // [S,Nq,Hq,D]
   int SQ = 1;               // pieces of the queries
-  float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D]
+  float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
 int ask_pieces(const AskArgs& a);    // S
 int ask_pieces_q(const AskArgs& a);  // SQ
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
+// Few states (pa_ask_few.hip): served, and faster.
+bool ask_few_served(const AskArgs& a, int dtype);
+int ask_few_most(const AskArgs& a);  // the most states of a request that it serves
+hipError_t launch_ask_few(const AskArgs& a, hipStream_t st);
+bool ask_few_backward_served(const AskArgs& a, int dtype);
+int64_t ask_few_records(const AskArgs& a);  // floats of its records in part_k, and in part_v
+hipError_t launch_ask_few_backward(const AskArgs& a, hipStream_t st);
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st);
 
 // ---- dropout with the residual add (pa_dropout.hip) ----
