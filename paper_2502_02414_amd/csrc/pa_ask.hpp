@@ -15,6 +15,8 @@
 // of the product over the states (and with the two exchanged, over the queries).
 #pragma once
 
+#include <type_traits>
+
 #include "pa_ops_internal.h"
 #include "pa_stream.hpp"
 
@@ -23,12 +25,41 @@ namespace ask {
 
 constexpr int kTile = 64;  // rows of a tile in LDS
 
+// Operands over the width: K32 of 32 elements for bf16; for fp32, whose products take 16
+// times as long, K16 of 16, so that less of a width is padding.
+template <typename T> struct Wide;
+template <> struct Wide<bf16> {
+  typedef K32<bf16> F;
+  static constexpr int W = 32, L = 8;  // elements of a step, and of a lane
+};
+template <> struct Wide<float> {
+  typedef K16<float> F;
+  static constexpr int W = 16, L = 4;
+};
+template <typename T> using WideF = typename Wide<T>::F;
+__device__ __forceinline__ f32x4 mma(const K32<bf16>& a, const K32<bf16>& b, f32x4 c) {
+  return mma32(a, b, c);
+}
+__device__ __forceinline__ f32x4 mma(const K16<float>& a, const K16<float>& b, f32x4 c) {
+  return mma16(a, b, c);
+}
+__device__ __forceinline__ void set_wide(K32<bf16>& f, const uint4& x) {
+  f.v = __builtin_bit_cast(bf16x8, x);
+}
+__device__ __forceinline__ void set_wide(K16<float>& f, const uint4& x) {
+  f.v = __builtin_bit_cast(f32x4, x);
+}
+__device__ __forceinline__ float wide_elem(const K32<bf16>& f, int e) { return (float)f.v[e]; }
+__device__ __forceinline__ float wide_elem(const K16<float>& f, int e) { return f.v[e]; }
+
+// DP: the width, rounded up to a multiple of 16.
 template <typename T, int DP> struct AskGeo {
   static constexpr int SZ = (int)sizeof(T), E = 16 / SZ;  // E: elements of 16 bytes
-  static constexpr int RB = DP * SZ + 32;                 // bytes of a row in LDS (lds_off)
-  static constexpr int CPR = DP * SZ / 16;                // 16-byte chunks of a row
+  static constexpr int NK = (DP + Wide<T>::W - 1) / Wide<T>::W, ND = DP / 16;  // steps; tiles
+  static constexpr int ROW = NK * Wide<T>::W * SZ;        // bytes of a row
+  static constexpr int RB = ROW + 32;                     // in LDS (lds_off)
+  static constexpr int CPR = ROW / 16;                    // 16-byte chunks of a row
   static constexpr int NCH = kTile * CPR / 256;           // chunks of a tile per thread
-  static constexpr int NK = DP / 32, ND = DP / 16;        // steps over the width; tiles of it
   static constexpr int TB = kTile * RB;                   // bytes of a tile
 };
 
@@ -78,74 +109,120 @@ __device__ __forceinline__ Range piece(Range k, int s, int S) {
 
 __device__ __forceinline__ uint4 zero16() { return uint4{0, 0, 0, 0}; }
 
-// A tile of up to 64 rows on its way to LDS: 256 threads, 16 bytes each.  Loads have
-// no branch around them: rows past the end read the last one, columns past D the
-// first chunk, and both become zeros, as do the rows of states that are left out
-// (which may hold anything).
+// Memory that loads are checked against: an offset past its end reads zeros, so that
+// no load stands behind a branch.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000);
+}
+__device__ __forceinline__ uint4 load16(Buffer b, int at) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
+}
+constexpr int kNowhere = 0x7fffff00;
+
+// A tile of up to 64 rows on its way to LDS: 256 threads, 16 bytes each, zeros where
+// rows or columns end.  Offsets within a tile stay below 2^31: rows are at most 2^25
+// bytes apart.
 template <typename T, int DP> struct TileLoad {
   using G_ = AskGeo<T, DP>;
   uint4 c[G_::NCH];
+  int off[G_::NCH];
 
-  // states [p0, p0 + 64) below e
-  __device__ __forceinline__ void states(const T* base, int64_t ld, int64_t p0, int64_t e, int D,
-                                         const uint8_t* mask) {
+  static __device__ __forceinline__ int row(int j) { return (threadIdx.x + 256 * j) / G_::CPR; }
+  static __device__ __forceinline__ int col(int j) {
+    return (threadIdx.x + 256 * j) % G_::CPR * G_::E;
+  }
+  // rows of states, ld elements apart
+  __device__ __forceinline__ void states(int64_t ld, int D) {
+#pragma unroll
+    for (int j = 0; j < G_::NCH; ++j)
+      off[j] = col(j) < D ? (row(j) * (int)ld + col(j)) * G_::SZ : kNowhere;
+  }
+  // virtual rows of a request from row `rem` of a query's group on
+  __device__ __forceinline__ void queries(int64_t ld, int G, int rem, int D) {
 #pragma unroll
     for (int j = 0; j < G_::NCH; ++j) {
-      const int q = threadIdx.x + 256 * j, row = q / G_::CPR, col = (q % G_::CPR) * G_::E;
-      const int64_t p = p0 + row < e ? p0 + row : e - 1;
-      uint8_t counts = 1;
-      if (mask) counts = mask[p];
-      const bool in = p0 + row < e && col < D && counts;
-      const uint4 x = ld_global16<false>(base + p * ld + (col < D ? col : 0));
-      c[j] = in ? x : zero16();
+      const uint32_t v = rem + row(j), i = G == 1 ? v : v / (uint32_t)G, g = v - i * G;
+      off[j] = col(j) < D ? (int)(i * (uint32_t)ld + g * D + col(j)) * G_::SZ : kNowhere;
     }
   }
-  // virtual rows [v0, v0 + 64) below n of a request that begins at query b
-  __device__ __forceinline__ void queries(const T* base, int64_t ld, int64_t b, int G, int v0, int n,
-                                          int D) {
+  __device__ __forceinline__ void load(Buffer b, int rows) {
 #pragma unroll
-    for (int j = 0; j < G_::NCH; ++j) {
-      const int q = threadIdx.x + 256 * j, row = q / G_::CPR, col = (q % G_::CPR) * G_::E;
-      const uint32_t v = v0 + row < n ? v0 + row : n - 1;
-      const uint32_t i = G == 1 ? v : v / (uint32_t)G, g = v - i * G;
-      const uint4 x = ld_global16<false>(base + (b + i) * ld + g * D + (col < D ? col : 0));
-      c[j] = v0 + row < n && col < D ? x : zero16();
-    }
+    for (int j = 0; j < G_::NCH; ++j) c[j] = load16(b, row(j) < rows ? off[j] : kNowhere);
   }
   __device__ __forceinline__ void put(char* tile) const {
 #pragma unroll
-    for (int j = 0; j < G_::NCH; ++j) {
-      const int q = threadIdx.x + 256 * j;
-      *reinterpret_cast<uint4*>(tile + lds_off(q / G_::CPR, (q % G_::CPR) * 16, G_::RB)) = c[j];
-    }
+    for (int j = 0; j < G_::NCH; ++j)
+      *reinterpret_cast<uint4*>(tile + lds_off(row(j), col(j) * G_::SZ, G_::RB)) = c[j];
   }
 };
 
-// A row's K32 fragments straight from memory: lane (r, g) elements 32 k + 8 g .. + 8
-// of its row, zeros past D or where the row is none.
-template <typename T, int DP>
-__device__ __forceinline__ void row_frags(K32<T> (&f)[DP / 32], const T* row, int D, bool on) {
-  const int g = lane_id() >> 4;
+// Tiles of a request's states: k and v, and which of them count, two of each in LDS.
+template <typename T, int DP> struct StateTiles {
+  using Gm = AskGeo<T, DP>;
+  TileLoad<T, DP> k, v;
+  const T *K, *V;
+  const uint8_t* mask;
+  int64_t ldk, ldv, e;
+  int D;
+  uint8_t keep[Gm::NCH];
+  uint8_t counts;
+  __device__ __forceinline__ void init(const AskArgs& a, int h, Range r) {
+    K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
+    V = reinterpret_cast<const T*>(a.v) + (int64_t)h * a.D;
+    mask = a.mask; ldk = a.ldk; ldv = a.ldv; e = r.e; D = a.D;
+    k.states(ldk, D);
+    v.states(ldv, D);
+  }
+  __device__ __forceinline__ void load(int64_t p0) {
+    const int rows = e - p0 < kTile ? (int)(e - p0) : kTile;
+    k.load(buffer_of(K + p0 * ldk, ((rows - 1) * ldk + D) * Gm::SZ), rows);
+    v.load(buffer_of(V + p0 * ldv, ((rows - 1) * ldv + D) * Gm::SZ), rows);
+    counts = (int)threadIdx.x < rows;
+    if (mask) {
+      const Buffer m = buffer_of(mask + p0, rows);
+      counts = __builtin_amdgcn_raw_buffer_load_b8(m, threadIdx.x & 63, 0, 0);
 #pragma unroll
-  for (int k = 0; k < DP / 32; ++k) {
-    const int c = 32 * k + 8 * g;
-    const bool in = on && c < D;
-    const T* p = row + (c < D ? c : 0);
-    if constexpr (sizeof(T) == 2) {
-      const uint4 x = ld_global16<false>(p);
-      f[k].v = __builtin_bit_cast(bf16x8, in ? x : zero16());
-    } else {
-      const uint4 x = ld_global16<false>(p), y = ld_global16<false>(p + 4);
-      f[k].lo = __builtin_bit_cast(f32x4, in ? x : zero16());
-      f[k].hi = __builtin_bit_cast(f32x4, in ? y : zero16());
+      for (int j = 0; j < Gm::NCH; ++j)
+        keep[j] = __builtin_amdgcn_raw_buffer_load_b8(m, k.row(j), 0, 0);
     }
   }
-}
+  // into LDS: k's tile, v's behind it; live: 0, or -infinity where a state is left out
+  __device__ __forceinline__ void put(char* tiles, float* live) {
+    if (mask) {  // (zeros for what may hold anything)
+#pragma unroll
+      for (int j = 0; j < Gm::NCH; ++j) {
+        k.c[j] = keep[j] ? k.c[j] : zero16();
+        v.c[j] = keep[j] ? v.c[j] : zero16();
+      }
+    }
+    k.put(tiles);
+    v.put(tiles + Gm::TB);
+    if (threadIdx.x < kTile) live[threadIdx.x] = counts ? 0.f : -INFINITY;
+  }
+};
 
-template <typename T> __device__ __forceinline__ float k32_elem(const K32<T>& f, int e) {
-  if constexpr (sizeof(T) == 2) return (float)f.v[e];
-  else return e < 4 ? f.lo[e & 3] : f.hi[e & 3];
+// Operand of lane (r, g)'s row straight from memory, zeros past D or where the row is
+// none (its address has to be one that may be read all the same).
+template <typename T, int DP>
+__device__ __forceinline__ void row_frags(WideF<T>* f, const T* row, int D, bool on) {
+  const int g = lane_id() >> 4;
+#pragma unroll
+  for (int k = 0; k < AskGeo<T, DP>::NK; ++k) {
+    const int c = Wide<T>::W * k + Wide<T>::L * g;
+    const uint4 x = ld_global16<false>(row + (c < D ? c : 0));
+    set_wide(f[k], on && c < D ? x : zero16());
+  }
 }
+// The same from LDS: row r of the 16 that begin at byte `at`, step k.
+template <typename T>
+__device__ __forceinline__ void ld_wide(WideF<T>& f, const char* tile, int base, int at) {
+  set_wide(f, *reinterpret_cast<const uint4*>(tile + base + at));
+}
+template <typename T, int DP> __device__ __forceinline__ int wide_base() {
+  return lds_off(lane_id() & 15, 16 * (lane_id() >> 4), AskGeo<T, DP>::RB);
+}
+constexpr int kStep = 64;  // bytes from one step over the width to the next
 
 // Four consecutive elements of a row.
 template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& v) {
@@ -156,6 +233,23 @@ template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& 
   } else {
     *reinterpret_cast<f32x4*>(p) = v;
   }
+}
+
+// f(type, std::integral_constant of the width rounded up): fp32 is padded to multiples
+// of 16, bf16, whose steps are 32 wide, too (the tiles of its results are 16 wide).
+template <typename F> hipError_t by_width(int D, int dtype, F f) {
+  const auto go = [&](auto type) {
+    using std::integral_constant;
+    if constexpr (sizeof(type) == 4)
+      if (D <= 16) return f(type, integral_constant<int, 16>{});
+    if (D <= 32) return f(type, integral_constant<int, 32>{});
+    if (D <= 48) return f(type, integral_constant<int, 48>{});
+    if (D <= 64) return f(type, integral_constant<int, 64>{});
+    if (D <= 80) return f(type, integral_constant<int, 80>{});
+    if (D <= 96) return f(type, integral_constant<int, 96>{});
+    return f(type, integral_constant<int, 128>{});
+  };
+  return dtype == 1 ? go(bf16{}) : go(float{});
 }
 
 }  // namespace ask

@@ -18,13 +18,13 @@ namespace pa {
 namespace {
 using namespace ask;
 
-template <typename T, int DP>
+template <typename T, int DP, int QT>
 __global__ void __launch_bounds__(256) k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr bool FIX = sizeof(T) == 2;
-  constexpr int TQ = 64, SHIFT = 6;
+  constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
-  __shared__ float live[2][kTile];                             // 0, or -inf where left out
+  __shared__ __attribute__((aligned(16))) float live[2][kTile];
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
@@ -39,93 +39,89 @@ __global__ void __launch_bounds__(256) k_ask_dq(AskArgs a) {
   if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  const T* K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
-  const T* V = reinterpret_cast<const T*>(a.v) + (int64_t)h * a.D;
-  const int vq = v0 + w * 16 + r;  // this lane's query: column r of the wave's tile
-  const bool on = vq < n;
-  const uint32_t v = on ? vq : n - 1, i = G == 1 ? v : v / (uint32_t)G;
-  const int64_t row = qr.b + i;
-  const int hq = h * G + (int)(v - i * G);
-  K32<T> qf[Gm::NK], of[Gm::NK];
-  row_frags<T, DP>(of, reinterpret_cast<const T*>(a.o) + row * a.ldo + (int64_t)hq * a.D, a.D, on);
-  row_frags<T, DP>(qf, reinterpret_cast<const T*>(a.d_o) + row * a.lddo + (int64_t)hq * a.D, a.D, on);
-  float d0 = 0.f;
+  StateTiles<T, DP> st;
+  st.init(a, h, kr);
+  if (kr.b < kr.e) st.load(kr.b);
+  // this lane's queries: column r of the wave's QT tiles of 16
+  int64_t row[QT];
+  int hq[QT];
+  bool on[QT];
+  float d0[QT], lse2[QT], e0[QT];
+  WideF<T> qf[QT][Gm::NK], of[QT][Gm::NK];
+  f32x4 A[QT][Gm::ND], Bk[FIX ? QT : 1][FIX ? Gm::ND : 1];
 #pragma unroll
-  for (int k = 0; k < Gm::NK; ++k)
+  for (int c = 0; c < QT; ++c) {
+    const int vq = v0 + (w * QT + c) * 16 + r;
+    on[c] = vq < n;
+    const uint32_t v = on[c] ? vq : n - 1, i = G == 1 ? v : v / (uint32_t)G;
+    row[c] = qr.b + i;
+    hq[c] = h * G + (int)(v - i * G);
+    const int64_t at = (int64_t)hq[c] * a.D;
+    row_frags<T, DP>(qf[c], reinterpret_cast<const T*>(a.o) + row[c] * a.ldo + at, a.D, on[c]);
+    row_frags<T, DP>(of[c], reinterpret_cast<const T*>(a.d_o) + row[c] * a.lddo + at, a.D, on[c]);
+    d0[c] = e0[c] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) d0 = fmaf(k32_elem(of[k], e), k32_elem(qf[k], e), d0);
-  d0 = groups_sum(d0);
+    for (int k = 0; k < Gm::NK; ++k)
 #pragma unroll
-  for (int k = 0; k < Gm::NK; ++k) of[k] = qf[k];  // do from here on
-  row_frags<T, DP>(qf, reinterpret_cast<const T*>(a.q) + row * a.ldq + (int64_t)hq * a.D, a.D, on);
-  const bool busy = v0 + w * 16 < n;
-  const float sc = a.scale * kLog2e;
-  // (a row without states: lse = -inf, weights of 0)
-  float lse2 = a.lse[(int64_t)hq * a.Nq + row] * kLog2e;
-  if (lse2 == -INFINITY) lse2 = INFINITY;
-  f32x4 A[Gm::ND], Bk[FIX ? Gm::ND : 1];
-  float e0 = 0.f;
+      for (int e = 0; e < Wide<T>::L; ++e)
+        d0[c] = fmaf(wide_elem(of[c][k], e), wide_elem(qf[c][k], e), d0[c]);
+    d0[c] = groups_sum(d0[c]);
+    row_frags<T, DP>(qf[c], reinterpret_cast<const T*>(a.q) + row[c] * a.ldq + at, a.D, on[c]);
+    // (a row without states: lse = -inf, weights of 0)
+    lse2[c] = a.lse[(int64_t)hq[c] * a.Nq + row[c]] * kLog2e;
+    if (lse2[c] == -INFINITY) lse2[c] = INFINITY;
 #pragma unroll
-  for (int d = 0; d < Gm::ND; ++d) {
-    A[d] = zero4();
-    if constexpr (FIX) Bk[d] = zero4();
-  }
-
-  TileLoad<T, DP> tk, tv;
-  float alive;
-  auto load = [&](int64_t p0) __attribute__((always_inline)) {
-    tk.states(K, a.ldk, p0, kr.e, a.D, a.mask);
-    tv.states(V, a.ldv, p0, kr.e, a.D, a.mask);
-    if (threadIdx.x < kTile) {
-      const int64_t p = p0 + threadIdx.x;
-      alive = p < kr.e && (!a.mask || a.mask[p]) ? 0.f : -INFINITY;
+    for (int d = 0; d < Gm::ND; ++d) {
+      A[c][d] = zero4();
+      if constexpr (FIX) Bk[c][d] = zero4();
     }
-  };
-  auto put = [&](int buf) __attribute__((always_inline)) {
-    tk.put(smem + buf * 2 * Gm::TB);
-    tv.put(smem + buf * 2 * Gm::TB + Gm::TB);
-    if (threadIdx.x < kTile) live[buf][threadIdx.x] = alive;
-  };
-  const RowBase<T> rb = row_base<T>(r, Gm::RB);
-  const int tb = tr_base<T>(Gm::RB);
-  if (kr.b < kr.e) {
-    load(kr.b);
-    put(0);
   }
+  const bool busy = v0 + w * QT * 16 < n;
+  const float sc = a.scale * kLog2e;
+  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
+  if (kr.b < kr.e) st.put(smem, live[0]);
   int buf = 0;
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += kTile, buf ^= 1) {
     block_sync();
     const bool more = p0 + kTile < kr.e;
-    if (more) load(p0 + kTile);
+    if (more) st.load(p0 + kTile);
     if (busy) {
       const char* kt = smem + buf * 2 * Gm::TB;
       const char* vt = kt + Gm::TB;
-      K16<T> pf[4], sf[4];
+      const bool part = a.mask || p0 + kTile > kr.e;
+      K16<T> pf[FIX ? QT : 1][4], sf[QT][4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        f32x4 x = zero4(), dp = zero4();
+        f32x4 x[QT], dp[QT];
+#pragma unroll
+        for (int c = 0; c < QT; ++c) x[c] = dp[c] = zero4();
+        if (part) {
+#pragma unroll
+          for (int c = 0; c < QT; ++c) x[c] = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+        }
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
-          K32<T> kf, vf;
-          ld_row<T>(kf, kt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
-          ld_row<T>(vf, vt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
-          x = mma32(kf, qf[k], x);
-          dp = mma32(vf, of[k], dp);
-        }
-        if (a.mask || p0 + kTile > kr.e) {
-          const f32x4 dead = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+          WideF<T> kf, vf;
+          ld_wide<T>(kf, kt, wb, t * 16 * Gm::RB + kStep * k);
+          ld_wide<T>(vf, vt, wb, t * 16 * Gm::RB + kStep * k);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = dead[i] == 0.f ? x[i] : -INFINITY;
+          for (int c = 0; c < QT; ++c) {
+            x[c] = mma(kf, qf[c][k], x[c]);
+            dp[c] = mma(vf, of[c][k], dp[c]);
+          }
         }
-        float p[4], ds[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = fast_exp2(fmaf(x[i], sc, -lse2));
-          ds[i] = p[i] * (dp[i] - d0);
-          if constexpr (FIX) e0 += ds[i];
+        for (int c = 0; c < QT; ++c) {
+          float p[4], ds[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] = fast_exp2(fmaf(x[c][i], sc, -lse2[c]));
+            ds[i] = p[i] * (dp[c][i] - d0[c]);
+            if constexpr (FIX) e0[c] += ds[i];
+          }
+          if constexpr (FIX) set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
+          set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
         }
-        if constexpr (FIX) set_k16(pf[t], p[0], p[1], p[2], p[3]);
-        set_k16(sf[t], ds[0], ds[1], ds[2], ds[3]);
       }
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
@@ -134,35 +130,41 @@ __global__ void __launch_bounds__(256) k_ask_dq(AskArgs a) {
           K16<T> k0, k1;
           ld_tr<T>(k0, kt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
           ld_tr<T>(k1, kt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          A[d] = mma16x2(k0, sf[t], k1, sf[t + 1], A[d]);
-          if constexpr (FIX) Bk[d] = mma16x2(k0, pf[t], k1, pf[t + 1], Bk[d]);
+#pragma unroll
+          for (int c = 0; c < QT; ++c) {
+            A[c][d] = mma16x2(k0, sf[c][t], k1, sf[c][t + 1], A[c][d]);
+            if constexpr (FIX) Bk[c][d] = mma16x2(k0, pf[c][t], k1, pf[c][t + 1], Bk[c][d]);
+          }
         }
       }
     }
-    if (more) put(buf ^ 1);
+    if (more) st.put(smem + (buf ^ 1) * 2 * Gm::TB, live[buf ^ 1]);
   }
-  if constexpr (FIX) e0 = groups_sum(e0);
-  if (!on) return;
-  if (a.S == 1) {
-    T* DQ = reinterpret_cast<T*>(a.dq) + row * a.lddq + (int64_t)hq * a.D;
 #pragma unroll
-    for (int d = 0; d < Gm::ND; ++d) {
-      f32x4 x = A[d];
-      if constexpr (FIX) x -= Bk[d] * e0;
-      if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, x * a.scale);
-    }
-    if (g == 0) a.delta[(int64_t)hq * a.Nq + row] = d0 + e0;
-  } else {
-    const int64_t at = ((int64_t)s * a.Nq + row) * a.Hq + hq;
+  for (int c = 0; c < QT; ++c) {
+    if constexpr (FIX) e0[c] = groups_sum(e0[c]);
+    if (!on[c]) continue;
+    if (a.S == 1) {
+      T* DQ = reinterpret_cast<T*>(a.dq) + row[c] * a.lddq + (int64_t)hq[c] * a.D;
 #pragma unroll
-    for (int d = 0; d < Gm::ND; ++d) {
-      if (16 * d + 4 * g >= a.D) continue;
-      store4<float>(a.part + at * a.D + 16 * d + 4 * g, A[d]);
-      if constexpr (FIX) store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, Bk[d]);
-    }
-    if (g == 0) {
-      a.part_lse[at] = e0;
-      if (s == 0) a.delta[(int64_t)hq * a.Nq + row] = d0;
+      for (int d = 0; d < Gm::ND; ++d) {
+        f32x4 x = A[c][d];
+        if constexpr (FIX) x -= Bk[c][d] * e0[c];
+        if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, x * a.scale);
+      }
+      if (g == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c] + e0[c];
+    } else {
+      const int64_t at = ((int64_t)s * a.Nq + row[c]) * a.Hq + hq[c];
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) {
+        if (16 * d + 4 * g >= a.D) continue;
+        store4<float>(a.part + at * a.D + 16 * d + 4 * g, A[c][d]);
+        if constexpr (FIX) store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, Bk[c][d]);
+      }
+      if (g == 0) {
+        a.part_lse[at] = e0[c];
+        if (s == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c];
+      }
     }
   }
 }
@@ -190,51 +192,48 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
 }
 
-// dk and dv of a tile of 64 states: a wave has 16 of them as columns, and their rows
-// of k and v in registers; the queries come through LDS.
-template <typename T, int DP>
+// dk and dv of a tile of 64 KT states: a wave has KT times 16 of them as columns, and
+// their rows of k and v in registers; the queries come through LDS.
+template <typename T, int DP, int KT>
 __global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
   using Gm = AskGeo<T, DP>;
+  constexpr int TK = 64 * KT, SHIFT = KT == 1 ? 6 : 7;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] q and do tiles
-  __shared__ float stat[2][2][kTile];                          // lse (base 2), delta
+  __shared__ __attribute__((aligned(16))) float stat[2][2][kTile];  // lse (base 2), delta
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
-  const int rq = request_of(a.k_off, a.R, a.Nk, 1, 6, slot);
+  const int rq = request_of(a.k_off, a.R, a.Nk, 1, SHIFT, slot);
   if (rq < 0) return;
   const Range kr = range_of(a.k_off, rq, a.Nk);
-  const int64_t tile = slot - (kr.b >> 6) - rq;
-  if (tile < 0 || tile * kTile >= kr.e - kr.b || kr.e - kr.b <= a.few) return;
+  const int64_t tile = slot - (kr.b >> SHIFT) - rq;
+  if (tile < 0 || tile * TK >= kr.e - kr.b || kr.e - kr.b <= a.few) return;
   const Range qr = range_of(a.q_off, rq, a.Nq);
   const Range vr = piece(Range{0, (qr.e - qr.b) * G}, s, a.SQ);  // virtual rows
   const int n = (int)vr.e;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
-  const T* DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * a.D;
-  const int64_t p = kr.b + tile * kTile + w * 16 + r;
-  const bool in = p < kr.e;
-  const int64_t pc = in ? p : kr.e - 1;
-  const bool on = in && (!a.mask || a.mask[pc]);
-  const bool busy = kr.b + tile * kTile + w * 16 < kr.e;
-  K32<T> kf[Gm::NK], vf[Gm::NK];
-  row_frags<T, DP>(kf, reinterpret_cast<const T*>(a.k) + pc * a.ldk + (int64_t)h * a.D, a.D, on);
-  row_frags<T, DP>(vf, reinterpret_cast<const T*>(a.v) + pc * a.ldv + (int64_t)h * a.D, a.D, on);
-  const float sc = a.scale * kLog2e;
-  f32x4 dk[Gm::ND], dv[Gm::ND];
-#pragma unroll
-  for (int d = 0; d < Gm::ND; ++d) dk[d] = dv[d] = zero4();
-
+  const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D + qr.b * a.ldq;
+  const T* DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * a.D + qr.b * a.lddo;
   TileLoad<T, DP> tq, td;
   float ls, de;
+  auto places = [&](int rem) __attribute__((always_inline)) {
+    tq.queries(a.ldq, G, rem, a.D);
+    td.queries(a.lddo, G, rem, a.D);
+  };
+  const bool even = 64 % G == 0;  // (tiles begin at a query)
+  if (even) places(0);
   auto load = [&](int v0) __attribute__((always_inline)) {
-    tq.queries(Q, a.ldq, qr.b, G, v0, n, a.D);
-    td.queries(DO, a.lddo, qr.b, G, v0, n, a.D);
+    const int rows = n - v0 < kTile ? n - v0 : kTile;
+    const int i0 = G == 1 ? v0 : v0 / G, i1 = G == 1 ? v0 + rows - 1 : (v0 + rows - 1) / G;
+    if (!even) places(v0 - i0 * G);
+    tq.load(buffer_of(Q + i0 * a.ldq, ((i1 - i0) * a.ldq + G * a.D) * Gm::SZ), rows);
+    td.load(buffer_of(DO + i0 * a.lddo, ((i1 - i0) * a.lddo + G * a.D) * Gm::SZ), rows);
     if (threadIdx.x < kTile) {
-      const uint32_t v = v0 + (int)threadIdx.x < n ? v0 + threadIdx.x : n - 1;
+      const bool ok = (int)threadIdx.x < rows;
+      const uint32_t v = ok ? v0 + threadIdx.x : v0 + rows - 1;
       const uint32_t i = G == 1 ? v : v / (uint32_t)G;
       const int64_t at = (int64_t)(h * G + (int)(v - i * G)) * a.Nq + qr.b + i;
-      const bool ok = v0 + (int)threadIdx.x < n;
       ls = a.lse[at] * kLog2e;
       de = a.delta[at];
       if (!ok || ls == -INFINITY) ls = INFINITY;  // (weights of 0)
@@ -249,13 +248,28 @@ __global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
       stat[buf][1][threadIdx.x] = de;
     }
   };
-  const RowBase<T> rb = row_base<T>(r, Gm::RB);
-  const int tb = tr_base<T>(Gm::RB);
   const int first = (int)vr.b;
-  if (first < n) {
-    load(first);
-    put(0);
+  if (first < n) load(first);
+  const int64_t p0 = kr.b + tile * TK + w * KT * 16 + r;
+  const bool busy = kr.b + tile * TK + w * KT * 16 < kr.e;
+  bool in[KT];
+  float none[KT];  // 0, or -infinity where the state is left out
+  WideF<T> kf[KT][Gm::NK], vf[KT][Gm::NK];
+  f32x4 dk[KT][Gm::ND], dv[KT][Gm::ND];
+#pragma unroll
+  for (int c = 0; c < KT; ++c) {
+    in[c] = p0 + 16 * c < kr.e;
+    const int64_t p = in[c] ? p0 + 16 * c : kr.e - 1;
+    const bool on = in[c] && (!a.mask || a.mask[p]);
+    none[c] = on ? 0.f : -INFINITY;
+    row_frags<T, DP>(kf[c], reinterpret_cast<const T*>(a.k) + p * a.ldk + (int64_t)h * a.D, a.D, on);
+    row_frags<T, DP>(vf[c], reinterpret_cast<const T*>(a.v) + p * a.ldv + (int64_t)h * a.D, a.D, on);
+#pragma unroll
+    for (int d = 0; d < Gm::ND; ++d) dk[c][d] = dv[c][d] = zero4();
   }
+  const float sc = a.scale * kLog2e;
+  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
+  if (first < n) put(0);
   int buf = 0;
   for (int v0 = first; v0 < n; v0 += kTile, buf ^= 1) {
     block_sync();
@@ -264,28 +278,39 @@ __global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
     if (busy) {
       const char* qt = smem + buf * 2 * Gm::TB;
       const char* dt = qt + Gm::TB;
-      K16<T> pf[4], sf[4];
+      K16<T> pf[KT][4], sf[KT][4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        f32x4 x = zero4(), dp = zero4();
+        f32x4 x[KT], dp[KT];
+#pragma unroll
+        for (int c = 0; c < KT; ++c) {
+          x[c] = f32x4{none[c], none[c], none[c], none[c]};
+          dp[c] = zero4();
+        }
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
-          K32<T> qf, of;
-          ld_row<T>(qf, qt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
-          ld_row<T>(of, dt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
-          x = mma32(qf, kf[k], x);
-          dp = mma32(of, vf[k], dp);
+          WideF<T> qf, of;
+          ld_wide<T>(qf, qt, wb, t * 16 * Gm::RB + kStep * k);
+          ld_wide<T>(of, dt, wb, t * 16 * Gm::RB + kStep * k);
+#pragma unroll
+          for (int c = 0; c < KT; ++c) {
+            x[c] = mma(qf, kf[c][k], x[c]);
+            dp[c] = mma(of, vf[c][k], dp[c]);
+          }
         }
         const f32x4 l = *reinterpret_cast<const f32x4*>(&stat[buf][0][16 * t + 4 * g]);
         const f32x4 de4 = *reinterpret_cast<const f32x4*>(&stat[buf][1][16 * t + 4 * g]);
-        float pr[4], ds[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          pr[i] = on ? fast_exp2(fmaf(x[i], sc, -l[i])) : 0.f;
-          ds[i] = pr[i] * (dp[i] - de4[i]);
+        for (int c = 0; c < KT; ++c) {
+          float pr[4], ds[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pr[i] = fast_exp2(fmaf(x[c][i], sc, -l[i]));
+            ds[i] = pr[i] * (dp[c][i] - de4[i]);
+          }
+          set_k16(pf[c][t], pr[0], pr[1], pr[2], pr[3]);
+          set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
         }
-        set_k16(pf[t], pr[0], pr[1], pr[2], pr[3]);
-        set_k16(sf[t], ds[0], ds[1], ds[2], ds[3]);
       }
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
@@ -294,32 +319,38 @@ __global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
           K16<T> a0, a1;
           ld_tr<T>(a0, dt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
           ld_tr<T>(a1, dt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          dv[d] = mma16x2(a0, pf[t], a1, pf[t + 1], dv[d]);
+#pragma unroll
+          for (int c = 0; c < KT; ++c) dv[c][d] = mma16x2(a0, pf[c][t], a1, pf[c][t + 1], dv[c][d]);
           ld_tr<T>(a0, qt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
           ld_tr<T>(a1, qt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          dk[d] = mma16x2(a0, sf[t], a1, sf[t + 1], dk[d]);
+#pragma unroll
+          for (int c = 0; c < KT; ++c) dk[c][d] = mma16x2(a0, sf[c][t], a1, sf[c][t + 1], dk[c][d]);
         }
       }
     }
     if (more) put(buf ^ 1);
   }
-  if (!in) return;
-  if (a.SQ == 1) {
-    T* DK = reinterpret_cast<T*>(a.dk) + p * a.lddk + (int64_t)h * a.D;
-    T* DV = reinterpret_cast<T*>(a.dv) + p * a.lddv + (int64_t)h * a.D;
 #pragma unroll
-    for (int d = 0; d < Gm::ND; ++d) {
-      if (16 * d + 4 * g >= a.D) continue;
-      store4<T>(DK + 16 * d + 4 * g, dk[d] * a.scale);
-      store4<T>(DV + 16 * d + 4 * g, dv[d]);
-    }
-  } else {
-    const int64_t at = (((int64_t)s * a.Nk + p) * a.Hkv + h) * a.D;
+  for (int c = 0; c < KT; ++c) {
+    if (!in[c]) continue;
+    const int64_t p = p0 + 16 * c;
+    if (a.SQ == 1) {
+      T* DK = reinterpret_cast<T*>(a.dk) + p * a.lddk + (int64_t)h * a.D;
+      T* DV = reinterpret_cast<T*>(a.dv) + p * a.lddv + (int64_t)h * a.D;
 #pragma unroll
-    for (int d = 0; d < Gm::ND; ++d) {
-      if (16 * d + 4 * g >= a.D) continue;
-      store4<float>(a.part_k + at + 16 * d + 4 * g, dk[d] * a.scale);
-      store4<float>(a.part_v + at + 16 * d + 4 * g, dv[d]);
+      for (int d = 0; d < Gm::ND; ++d) {
+        if (16 * d + 4 * g >= a.D) continue;
+        store4<T>(DK + 16 * d + 4 * g, dk[c][d] * a.scale);
+        store4<T>(DV + 16 * d + 4 * g, dv[c][d]);
+      }
+    } else {
+      const int64_t at = (((int64_t)s * a.Nk + p) * a.Hkv + h) * a.D;
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) {
+        if (16 * d + 4 * g >= a.D) continue;
+        store4<float>(a.part_k + at + 16 * d + 4 * g, dk[c][d] * a.scale);
+        store4<float>(a.part_v + at + 16 * d + 4 * g, dv[c][d]);
+      }
     }
   }
 }
@@ -339,57 +370,83 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskAr
   store4<T>(to, sum);
 }
 
-template <typename T, int DP> hipError_t launch(const AskArgs& a, hipStream_t st) {
-  using Gm = AskGeo<T, DP>;
-  const int64_t G = a.Hq / a.Hkv;
-  const int64_t qs = (a.Nq * G >> 6) + a.R, ks = (a.Nk >> 6) + a.R;
-  hipError_t e = hipSuccess;
-  if (a.Nq) {
-    hipLaunchKernelGGL((k_ask_dq<T, DP>), dim3((uint32_t)(qs * a.Hkv), a.S), dim3(256), 4 * Gm::TB,
-                       st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.Nq && a.S > 1) {
-    const int64_t threads = a.Nq * a.Hq * (a.D / 4);
-    hipLaunchKernelGGL(k_ask_dq_join<T>, dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, st, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (!a.dk || !a.Nk) return hipSuccess;
-  hipLaunchKernelGGL((k_ask_dkv<T, DP>), dim3((uint32_t)(ks * a.Hkv), a.SQ), dim3(256), 4 * Gm::TB,
-                     st, a);
-  if ((e = hipGetLastError()) != hipSuccess || a.SQ == 1) return e;
-  const int64_t threads = a.Nk * a.Hkv * a.D / 4;
-  hipLaunchKernelGGL(k_ask_dkv_sum<T>, dim3((uint32_t)((threads + 255) / 256), 2), dim3(256), 0, st,
-                     a);
+template <typename T, int DP, int QT> hipError_t launch_dq(const AskArgs& a, hipStream_t st) {
+  constexpr int lds = 4 * AskGeo<T, DP>::TB;
+  const int64_t slots = (a.Nq * (a.Hq / a.Hkv) >> (QT == 1 ? 6 : 7)) + a.R;
+  hipLaunchKernelGGL((k_ask_dq<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256),
+                     lds, st, a);
   return hipGetLastError();
 }
-template <typename T> hipError_t width(const AskArgs& a, hipStream_t st) {
-  if (a.D <= 32) return launch<T, 32>(a, st);
-  if (a.D <= 64) return launch<T, 64>(a, st);
-  if (a.D <= 96) return launch<T, 96>(a, st);
-  return launch<T, 128>(a, st);
+template <typename T, int DP, int KT> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
+  constexpr int lds = 4 * AskGeo<T, DP>::TB;
+  const int64_t slots = (a.Nk >> (KT == 1 ? 6 : 7)) + a.R;
+  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT>), dim3((uint32_t)(slots * a.Hkv), a.SQ), dim3(256),
+                     lds, st, a);
+  return hipGetLastError();
+}
+// Tiles of 16 states per wave in dk and dv's pass, as ask_tiles.
+int state_tiles(const AskArgs& a, int dtype) {
+  return dtype == 1 && a.Nk / a.R >= 128 && a.Nq * (a.Hq / a.Hkv) / a.R >= 128 ? 2 : 1;
+}
+
+hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
+  hipError_t e = hipSuccess;
+  if (a.Nq) {
+    const bool two = ask_tiles(a, dtype) == 2;
+    e = by_width(a.D, dtype, [&](auto type, auto dp) {
+      using T = decltype(type);
+      constexpr int DP = decltype(dp)::value;
+      if constexpr (sizeof(T) == 2)
+        if (two) return launch_dq<T, DP, 2>(a, st);
+      return launch_dq<T, DP, 1>(a, st);
+    });
+    if (e != hipSuccess) return e;
+    if (a.S > 1) {
+      const int64_t threads = a.Nq * a.Hq * (a.D / 4);
+      const dim3 grid((uint32_t)((threads + 255) / 256));
+      if (dtype == 1) hipLaunchKernelGGL(k_ask_dq_join<bf16>, grid, dim3(256), 0, st, a);
+      else hipLaunchKernelGGL(k_ask_dq_join<float>, grid, dim3(256), 0, st, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (!a.dk || !a.Nk) return hipSuccess;
+  const bool two = state_tiles(a, dtype) == 2;
+  e = by_width(a.D, dtype, [&](auto type, auto dp) {
+    using T = decltype(type);
+    constexpr int DP = decltype(dp)::value;
+    if constexpr (sizeof(T) == 2)
+      if (two) return launch_dkv<T, DP, 2>(a, st);
+    return launch_dkv<T, DP, 1>(a, st);
+  });
+  if (e != hipSuccess || a.SQ == 1) return e;
+  const int64_t threads = a.Nk * a.Hkv * a.D / 4;
+  const dim3 grid((uint32_t)((threads + 255) / 256), 2);
+  if (dtype == 1) hipLaunchKernelGGL(k_ask_dkv_sum<bf16>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(k_ask_dkv_sum<float>, grid, dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 }  // namespace
 
 // Pieces of the queries: with fewer blocks of all of them than the chip holds.
-int ask_pieces_q(const AskArgs& a) {
-  const int64_t G = a.Hq / a.Hkv, blocks = ((a.Nk >> 6) + a.R) * a.Hkv;
-  const int64_t tiles = (a.Nq * G / a.R + kTile - 1) / kTile;
-  int64_t S = (1024 + blocks - 1) / blocks;
+int ask_pieces_q(const AskArgs& a, int dtype) {
+  const int k = state_tiles(a, dtype);
+  const int64_t blocks = (a.Nk / (64 * k) + a.R) * a.Hkv;
+  const int64_t tiles = (a.Nq * (a.Hq / a.Hkv) / a.R + kTile - 1) / kTile;
+  int64_t S = ((k == 2 ? 512 : 1024) + blocks / 2) / blocks;
   if (S > tiles / 2) S = tiles / 2;
   return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
 }
 
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st) {
-  if (!ask_few_backward_served(a, dtype)) return dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  if (!ask_few_backward_served(a, dtype)) return passes(a, dtype, st);
   const hipError_t e = launch_ask_few_backward(a, st);
   if (e != hipSuccess || a.R == 1 || a.Nk <= ask_few_most(a)) return e;
   // (a request that is longer than max_k says)
   AskArgs rest = a;
   rest.few = ask_few_most(a);
   rest.S = rest.SQ = 1;
-  return width<bf16>(rest, st);
+  return passes(rest, dtype, st);
 }
 
 }  // namespace pa

@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
-  __shared__ float live[2][kTile];                             // 0, or -inf where left out
+  __shared__ __attribute__((aligned(16))) float live[2][kTile];
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
   if (rq < 0) return;
   const Range qr = range_of(a.q_off, rq, a.Nq);
   const int n = (int)(qr.e - qr.b) * G;
-  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - (a.q_off ? rq : 0);
+  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - rq;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
   const Range all = range_of(a.k_off, rq, a.Nk), kr = piece(all, s, a.S);
@@ -32,13 +32,14 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
-  const T* K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
-  const T* V = reinterpret_cast<const T*>(a.v) + (int64_t)h * a.D;
+  StateTiles<T, DP> st;
+  st.init(a, h, kr);
+  if (kr.b < kr.e) st.load(kr.b);
   // this lane's queries: column r of the wave's QT tiles of 16
   int vq[QT];
   int64_t row[QT];
   int head[QT];
-  K32<T> qf[QT][Gm::NK];
+  WideF<T> qf[QT][Gm::NK];
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     vq[c] = v0 + (w * QT + c) * 16 + r;
@@ -59,56 +60,38 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
 #pragma unroll
     for (int d = 0; d < Gm::ND; ++d) o[c][d] = zero4();
   }
-
-  TileLoad<T, DP> tk, tv;
-  float alive;
-  auto load = [&](int64_t p0) __attribute__((always_inline)) {
-    tk.states(K, a.ldk, p0, kr.e, a.D, a.mask);
-    tv.states(V, a.ldv, p0, kr.e, a.D, a.mask);
-    if (threadIdx.x < kTile) {
-      const int64_t p = p0 + threadIdx.x;
-      alive = p < kr.e && (!a.mask || a.mask[p]) ? 0.f : -INFINITY;
-    }
-  };
-  auto put = [&](int buf) __attribute__((always_inline)) {
-    tk.put(smem + buf * 2 * Gm::TB);
-    tv.put(smem + buf * 2 * Gm::TB + Gm::TB);
-    if (threadIdx.x < kTile) live[buf][threadIdx.x] = alive;
-  };
-  const RowBase<T> rb = row_base<T>(r, Gm::RB);
-  const int tb = tr_base<T>(Gm::RB);
-  if (kr.b < kr.e) {
-    load(kr.b);
-    put(0);
-  }
+  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
+  if (kr.b < kr.e) st.put(smem, live[0]);
   int buf = 0;
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += kTile, buf ^= 1) {
     block_sync();
     const bool more = p0 + kTile < kr.e;
-    if (more) load(p0 + kTile);
+    if (more) st.load(p0 + kTile);
     if (busy) {
       const char* kt = smem + buf * 2 * Gm::TB;
       const char* vt = kt + Gm::TB;
       f32x4 x[QT][4];
+      // (states that are left out begin at -infinity; their rows are zeros)
+      if (a.mask || p0 + kTile > kr.e) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int c = 0; c < QT; ++c) x[c][t] = zero4();
+          for (int c = 0; c < QT; ++c) x[c][t] = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int c = 0; c < QT; ++c) x[c][t] = zero4();
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
-          K32<T> kf;
-          ld_row<T>(kf, kt, rb, t * 16 * Gm::RB + 32 * k * Gm::SZ);
+          WideF<T> kf;
+          ld_wide<T>(kf, kt, wb, t * 16 * Gm::RB + kStep * k);
 #pragma unroll
-          for (int c = 0; c < QT; ++c) x[c][t] = mma32(kf, qf[c][k], x[c][t]);
+          for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], x[c][t]);
         }
-        if (a.mask || p0 + kTile > kr.e) {
-          const f32x4 dead = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
-#pragma unroll
-          for (int c = 0; c < QT; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[c][t][i] = dead[i] == 0.f ? x[c][t][i] : -INFINITY;
-        }
-      }
       K16<T> pf[QT][4];
 #pragma unroll
       for (int c = 0; c < QT; ++c) {
@@ -117,15 +100,17 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[c][t][i]);
-        mx = fmaxf(m[c], groups_max(mx) * sc);
-        const float base = mx == -INFINITY ? 0.f : mx;  // (nothing yet: weights of 0)
-        const float down = fast_exp2(m[c] - base);
-        m[c] = mx;
-        l[c] *= down;
+        mx = groups_max(mx) * sc;
+        // The maximum moves only where a score is 2^8 above it: weights up to 2^8 are as
+        // exact, and most tiles leave o and l as they are.
+        if (__any(mx > m[c] + 8.f)) {
+          const float to = fmaxf(m[c], mx), down = fast_exp2(m[c] - (to == -INFINITY ? 0.f : to));
+          m[c] = to;
+          l[c] *= down;
 #pragma unroll
-        for (int d = 0; d < Gm::ND; ++d)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[c][d][i] *= down;
+          for (int d = 0; d < Gm::ND; ++d) o[c][d] *= down;
+        }
+        const float base = m[c] == -INFINITY ? 0.f : m[c];  // (nothing yet: weights of 0)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           float p[4];
@@ -150,7 +135,7 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
         }
       }
     }
-    if (more) put(buf ^ 1);
+    if (more) st.put(smem + (buf ^ 1) * 2 * Gm::TB, live[buf ^ 1]);
   }
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
@@ -209,20 +194,31 @@ template <typename T, int DP, int QT> hipError_t launch(const AskArgs& a, hipStr
                      4 * Gm::TB, st, a);
   return hipGetLastError();
 }
-template <typename T> hipError_t width(const AskArgs& a, hipStream_t st) {
-  if (a.D <= 32) return launch<T, 32, 1>(a, st);
-  if (a.D <= 64) return launch<T, 64, 1>(a, st);
-  if (a.D <= 96) return launch<T, 96, 1>(a, st);
-  return launch<T, 128, 1>(a, st);
+hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
+  const bool two = dtype == 1 && ask_tiles(a, dtype) == 2;
+  return by_width(a.D, dtype, [&](auto type, auto dp) {
+    using T = decltype(type);
+    constexpr int DP = decltype(dp)::value;
+    if constexpr (sizeof(T) == 2)
+      if (two) return launch<T, DP, 2>(a, st);
+    return launch<T, DP, 1>(a, st);
+  });
 }
 
 }  // namespace
 
+// Tiles of 16 queries per wave: two (bf16), which halves what is read from LDS for a
+// product, where requests are long enough to fill them and the chip.
+int ask_tiles(const AskArgs& a, int dtype) {
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
+  return dtype == 1 && rows / a.R >= 128 && rows / 128 * a.Hkv >= 256 ? 2 : 1;
+}
 // Pieces of the states: with fewer blocks of whole ones than the chip holds.
-int ask_pieces(const AskArgs& a) {
-  const int64_t G = a.Hq / a.Hkv, blocks = ((a.Nq * G >> 6) + a.R) * a.Hkv;
+int ask_pieces(const AskArgs& a, int dtype) {
+  const int q = ask_tiles(a, dtype);
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), blocks = (rows / (64 * q) + a.R) * a.Hkv;
   const int64_t tiles = (a.Nk / a.R + kTile - 1) / kTile;
-  int64_t S = (1024 + blocks - 1) / blocks;
+  int64_t S = ((q == 2 ? 512 : 1024) + blocks / 2) / blocks;
   if (S > tiles / 2) S = tiles / 2;
   return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
 }
@@ -236,9 +232,9 @@ hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
     AskArgs rest = a;
     rest.few = ask_few_most(a);
     rest.S = 1;
-    return width<bf16>(rest, st);
+    return width(rest, dtype, st);
   }
-  e = dtype == 1 ? width<bf16>(a, st) : width<float>(a, st);
+  e = width(a, dtype, st);
   if (e != hipSuccess || a.S == 1) return e;
   const int64_t threads = a.Nq * a.Hq * (a.D / 4);
   const dim3 grid((uint32_t)((threads + 255) / 256));

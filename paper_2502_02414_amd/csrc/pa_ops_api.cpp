@@ -581,9 +581,11 @@ static pa_status ask_rows(const char* who, const char* name, const void* ptr, in
                           int D, int64_t* ld, int dtype, Rows* out) {
   const int64_t b = (int64_t)dtype_bytes(dtype), width = (int64_t)H * D;
   if (N < 2) *ld = width;
-  if (*ld < width || *ld > ((int64_t)1 << 32) || *ld * b % 16)
-    return err(PA_ERR_INVALID, "%s: ld of %s must be a multiple of 16 bytes in [%lld, 2^32]", who,
+  if (*ld < width || *ld * b % 16)
+    return err(PA_ERR_INVALID, "%s: ld of %s must be a multiple of 16 bytes and at least %lld", who,
                name, (long long)width);
+  if (*ld >= (1 << 25) / b)  // (offsets in a tile of 64 rows are 31 bits)
+    return err(PA_ERR_UNSUPPORTED, "%s: rows of %s must be less than 2^25 bytes apart", who, name);
   if (N) PO_TRY(need(who, ptr, name));
   *out = {name, ptr, (uint64_t)N, (uint64_t)(width * b), (uint64_t)(*ld * b)};
   return PA_OK;
@@ -608,7 +610,7 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
     a->delta = take(rows);  // (for requests that are longer than max_k says)
     return at;
   }
-  a->S = pa::ask_pieces(*a);
+  a->S = pa::ask_pieces(*a, dtype);
   if (a->S > 1) {
     a->part = take((uint64_t)a->S * rows * a->D);
     a->part_lse = take((uint64_t)a->S * rows);
@@ -616,7 +618,7 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
   if (!backward) return at;
   a->delta = take(rows);
   if (a->S > 1) a->part_b = take((uint64_t)a->S * rows * a->D);
-  a->SQ = pa::ask_pieces_q(*a);
+  a->SQ = pa::ask_pieces_q(*a, dtype);
   if (a->SQ > 1) {
     const uint64_t n = (uint64_t)a->SQ * a->Nk * a->Hkv * a->D;
     a->part_k = take(n);

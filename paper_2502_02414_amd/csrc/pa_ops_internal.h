@@ -134,8 +134,9 @@ struct AskArgs {
   int SQ = 1;               // pieces of the queries
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
-int ask_pieces(const AskArgs& a);    // S
-int ask_pieces_q(const AskArgs& a);  // SQ
+int ask_tiles(const AskArgs& a, int dtype);  // of 16 queries, per wave
+int ask_pieces(const AskArgs& a, int dtype);    // S
+int ask_pieces_q(const AskArgs& a, int dtype);  // SQ
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
 // Few states (pa_ask_few.hip): served, and faster.
 bool ask_few_served(const AskArgs& a, int dtype);
