@@ -224,6 +224,16 @@ template <typename T, int DP> __device__ __forceinline__ int wide_base() {
 }
 constexpr int kStep = 64;  // bytes from one step over the width to the next
 
+// The larger one, NaN where either is (one instruction of three operands; the score of
+// a NaN makes its row NaN in any case).
+__device__ __forceinline__ float largest(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+// Of an accumulator's four.
+__device__ __forceinline__ float largest(float a, const f32x4& x) {
+  return largest(largest(a, largest(x[0], x[1])), largest(x[2], x[3]));
+}
+
 // Four consecutive elements of a row.
 template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& v) {
   if constexpr (sizeof(T) == 2) {

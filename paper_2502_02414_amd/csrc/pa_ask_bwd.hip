@@ -19,7 +19,8 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256) k_ask_dq(AskArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && QT * DP <= 128 || DP <= 96 && sizeof(T) == 4 ? 2 : 1)
+k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr bool FIX = sizeof(T) == 2;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
@@ -195,7 +196,8 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
 // dk and dv of a tile of 64 KT states: a wave has KT times 16 of them as columns, and
 // their rows of k and v in registers; the queries come through LDS.
 template <typename T, int DP, int KT>
-__global__ void __launch_bounds__(256) k_ask_dkv(AskArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && KT * DP <= 128 || DP <= 64 && sizeof(T) == 4 ? 2 : 1)
+k_ask_dkv(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TK = 64 * KT, SHIFT = KT == 1 ? 6 : 7;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] q and do tiles

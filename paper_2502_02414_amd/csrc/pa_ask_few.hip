@@ -168,11 +168,9 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
 #pragma unroll
         for (int k = 0; k < NK; ++k) x[t] = mma32(kf[t][k], q.q[c][k], x[t]);
       }
-      float mx = x[0][0];
+      float mx = -INFINITY;
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[t][i]);
+      for (int t = 0; t < NT; ++t) mx = largest(mx, x[t]);
       mx = groups_max(mx) * sc;
       const float base = mx == -INFINITY ? 0.f : mx;
       float sum = 0.f;

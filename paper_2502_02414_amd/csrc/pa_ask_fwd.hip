@@ -12,7 +12,7 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256) k_ask(AskArgs a) {
+__global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
@@ -95,11 +95,9 @@ __global__ void __launch_bounds__(256) k_ask(AskArgs a) {
       K16<T> pf[QT][4];
 #pragma unroll
       for (int c = 0; c < QT; ++c) {
-        float mx = x[c][0][0];
+        float mx = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[c][t][i]);
+        for (int t = 0; t < 4; ++t) mx = largest(mx, x[c][t]);
         mx = groups_max(mx) * sc;
         // The maximum moves only where a score is 2^8 above it: weights up to 2^8 are as
         // exact, and most tiles leave o and l as they are.
