@@ -52,15 +52,22 @@ __device__ __forceinline__ void set_wide(K16<float>& f, const uint4& x) {
 __device__ __forceinline__ float wide_elem(const K32<bf16>& f, int e) { return (float)f.v[e]; }
 __device__ __forceinline__ float wide_elem(const K16<float>& f, int e) { return f.v[e]; }
 
-// DP: the width, rounded up to a multiple of 16.
+// DP: the width, rounded up to a multiple of 16.  A tile in LDS has rows of a power of
+// two of 16-byte chunks, the chunk c of row i in place c ^ key(i): a product's reads of
+// a chunk of 16 rows, and of the columns of 4 rows, then meet every bank once.
 template <typename T, int DP> struct AskGeo {
   static constexpr int SZ = (int)sizeof(T), E = 16 / SZ;  // E: elements of 16 bytes
   static constexpr int NK = (DP + Wide<T>::W - 1) / Wide<T>::W, ND = DP / 16;  // steps; tiles
-  static constexpr int ROW = NK * Wide<T>::W * SZ;        // bytes of a row
-  static constexpr int RB = ROW + 32;                     // in LDS (lds_off)
-  static constexpr int CPR = ROW / 16;                    // 16-byte chunks of a row
-  static constexpr int NCH = kTile * CPR / 256;           // chunks of a tile per thread
-  static constexpr int TB = kTile * RB;                   // bytes of a tile
+  static constexpr int CP = NK <= 1 ? 4 : NK <= 2 ? 8 : NK <= 4 ? 16 : 32;     // chunks of a row
+  static constexpr int RB = 16 * CP, TB = kTile * RB;     // bytes of a row, of a tile
+  static constexpr int NP = TB / 4096;                    // loads of a tile per wave (of 4)
+  static __device__ __forceinline__ int key(int row) {
+    if constexpr (CP == 4) return row >> 2 & 3;
+    const int j = row >> 1 & 7, k = row & 7;
+    if constexpr (SZ == 4) return CP == 8 ? j : row & 15;
+    if constexpr (CP == 8) return (2 * j & 7) + (j >> 2);
+    return 2 * k + (row >> 3 & 1);
+  }
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) {
@@ -118,46 +125,48 @@ __device__ __forceinline__ Buffer buffer_of(const void* p, int64_t bytes) {
 __device__ __forceinline__ uint4 load16(Buffer b, int at) {
   return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
 }
+// 16 bytes a lane to LDS, one behind the other from dst on (the same in all lanes).
+__device__ __forceinline__ void load_lds16(Buffer b, char* dst, int at) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(b, (__attribute__((address_space(3))) void*)dst, 16, at,
+                                           0, 0, 0);
+}
 constexpr int kNowhere = 0x7fffff00;
 
-// A tile of up to 64 rows on its way to LDS: 256 threads, 16 bytes each, zeros where
-// rows or columns end.  Offsets within a tile stay below 2^31: rows are at most 2^25
-// bytes apart.
+// Loads of a tile of up to 64 rows into LDS by 4 waves, 16 bytes a lane, without a
+// register between, zeros where rows or columns end.  Offsets within a tile stay below
+// 2^31: rows are at most 2^25 bytes apart.
 template <typename T, int DP> struct TileLoad {
-  using G_ = AskGeo<T, DP>;
-  uint4 c[G_::NCH];
-  int off[G_::NCH];
+  using Gm = AskGeo<T, DP>;
+  int off[Gm::NP];
 
-  static __device__ __forceinline__ int row(int j) { return (threadIdx.x + 256 * j) / G_::CPR; }
+  // this lane's row and column in load j of its wave
+  static __device__ __forceinline__ int row(int j) { return (256 * j + (int)threadIdx.x) / Gm::CP; }
   static __device__ __forceinline__ int col(int j) {
-    return (threadIdx.x + 256 * j) % G_::CPR * G_::E;
+    return ((256 * j + (int)threadIdx.x) % Gm::CP ^ Gm::key(row(j))) * Gm::E;
   }
   // rows of states, ld elements apart
   __device__ __forceinline__ void states(int64_t ld, int D) {
 #pragma unroll
-    for (int j = 0; j < G_::NCH; ++j)
-      off[j] = col(j) < D ? (row(j) * (int)ld + col(j)) * G_::SZ : kNowhere;
+    for (int j = 0; j < Gm::NP; ++j)
+      off[j] = col(j) < D ? (row(j) * (int)ld + col(j)) * Gm::SZ : kNowhere;
   }
   // virtual rows of a request from row `rem` of a query's group on
   __device__ __forceinline__ void queries(int64_t ld, int G, int rem, int D) {
 #pragma unroll
-    for (int j = 0; j < G_::NCH; ++j) {
+    for (int j = 0; j < Gm::NP; ++j) {
       const uint32_t v = rem + row(j), i = G == 1 ? v : v / (uint32_t)G, g = v - i * G;
-      off[j] = col(j) < D ? (int)(i * (uint32_t)ld + g * D + col(j)) * G_::SZ : kNowhere;
+      off[j] = col(j) < D ? (int)(i * (uint32_t)ld + g * D + col(j)) * Gm::SZ : kNowhere;
     }
   }
-  __device__ __forceinline__ void load(Buffer b, int rows) {
-#pragma unroll
-    for (int j = 0; j < G_::NCH; ++j) c[j] = load16(b, row(j) < rows ? off[j] : kNowhere);
-  }
-  __device__ __forceinline__ void put(char* tile) const {
-#pragma unroll
-    for (int j = 0; j < G_::NCH; ++j)
-      *reinterpret_cast<uint4*>(tile + lds_off(row(j), col(j) * G_::SZ, G_::RB)) = c[j];
+  __device__ __forceinline__ void load(Buffer b, int j, bool in, char* tile) const {
+    char* dst = tile + 4096 * j + 1024 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    load_lds16(b, dst, in ? off[j] : kNowhere);
   }
 };
 
-// Tiles of a request's states: k and v, and which of them count, two of each in LDS.
+// Tiles of a request's states in LDS: k's, v's behind it, and which of them count (0, or
+// -infinity where one is left out, whose rows are zeros: they may hold anything).  Which
+// rows are left out is asked for a tile ahead, before its loads are.
 template <typename T, int DP> struct StateTiles {
   using Gm = AskGeo<T, DP>;
   TileLoad<T, DP> k, v;
@@ -165,40 +174,133 @@ template <typename T, int DP> struct StateTiles {
   const uint8_t* mask;
   int64_t ldk, ldv, e;
   int D;
-  uint8_t keep[Gm::NCH];
-  uint8_t counts;
+  uint8_t keep[Gm::NP], counts;
+  float alive;
   __device__ __forceinline__ void init(const AskArgs& a, int h, Range r) {
     K = reinterpret_cast<const T*>(a.k) + (int64_t)h * a.D;
     V = reinterpret_cast<const T*>(a.v) + (int64_t)h * a.D;
     mask = a.mask; ldk = a.ldk; ldv = a.ldv; e = r.e; D = a.D;
     k.states(ldk, D);
     v.states(ldv, D);
+    if (mask && r.b < r.e) ask(r.b);
   }
-  __device__ __forceinline__ void load(int64_t p0) {
+  __device__ __forceinline__ void ask(int64_t p0) {
+    const Buffer m = buffer_of(mask + p0, e - p0 < kTile ? e - p0 : kTile);
+    counts = __builtin_amdgcn_raw_buffer_load_b8(m, threadIdx.x & 63, 0, 0);
+#pragma unroll
+    for (int j = 0; j < Gm::NP; ++j) keep[j] = __builtin_amdgcn_raw_buffer_load_b8(m, k.row(j), 0, 0);
+  }
+  __device__ __forceinline__ void load(int64_t p0, char* tiles) {
     const int rows = e - p0 < kTile ? (int)(e - p0) : kTile;
-    k.load(buffer_of(K + p0 * ldk, ((rows - 1) * ldk + D) * Gm::SZ), rows);
-    v.load(buffer_of(V + p0 * ldv, ((rows - 1) * ldv + D) * Gm::SZ), rows);
-    counts = (int)threadIdx.x < rows;
-    if (mask) {
-      const Buffer m = buffer_of(mask + p0, rows);
-      counts = __builtin_amdgcn_raw_buffer_load_b8(m, threadIdx.x & 63, 0, 0);
+    const Buffer bk = buffer_of(K + p0 * ldk, ((rows - 1) * ldk + D) * Gm::SZ);
+    const Buffer bv = buffer_of(V + p0 * ldv, ((rows - 1) * ldv + D) * Gm::SZ);
+    alive = (mask ? counts != 0 : (int)threadIdx.x < rows) ? 0.f : -INFINITY;
+    bool in[Gm::NP];
 #pragma unroll
-      for (int j = 0; j < Gm::NCH; ++j)
-        keep[j] = __builtin_amdgcn_raw_buffer_load_b8(m, k.row(j), 0, 0);
+    for (int j = 0; j < Gm::NP; ++j) in[j] = !mask || keep[j];
+    if (mask && p0 + kTile < e) ask(p0 + kTile);
+#pragma unroll
+    for (int j = 0; j < Gm::NP; ++j) {
+      k.load(bk, j, in[j], tiles);
+      v.load(bv, j, in[j], tiles + Gm::TB);
     }
   }
-  // into LDS: k's tile, v's behind it; live: 0, or -infinity where a state is left out
-  __device__ __forceinline__ void put(char* tiles, float* live) {
-    if (mask) {  // (zeros for what may hold anything)
+  __device__ __forceinline__ void put(float* live) {
+    if (threadIdx.x < kTile) live[threadIdx.x] = alive;
+  }
+};
+
+// Tiles of a request's virtual rows: q's, do's behind it, and their lse (base 2) and
+// delta, [2][64] floats, with which rows past the end have weights of 0.
+template <typename T, int DP> struct QueryTiles {
+  using Gm = AskGeo<T, DP>;
+  TileLoad<T, DP> q, d;
+  const T *Q, *DO;
+  const float *lse, *delta;
+  int64_t ldq, lddo, Nq;
+  int G, D, n;
+  float l, de;
+  // up to virtual row n of a request that begins at query b
+  __device__ __forceinline__ void init(const AskArgs& a, int h, int64_t b, int n_) {
+    G = a.Hq / a.Hkv; D = a.D; n = n_; Nq = a.Nq; ldq = a.ldq; lddo = a.lddo;
+    Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * D + b * ldq;
+    DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * D + b * lddo;
+    lse = a.lse + (int64_t)h * G * Nq + b;
+    delta = a.delta + (int64_t)h * G * Nq + b;
+    if (64 % G == 0) places(0);
+  }
+  __device__ __forceinline__ void places(int rem) {
+    q.queries(ldq, G, rem, D);
+    d.queries(lddo, G, rem, D);
+  }
+  __device__ __forceinline__ void load(int v0, char* tiles) {
+    const int rows = n - v0 < kTile ? n - v0 : kTile;
+    const int i0 = G == 1 ? v0 : v0 / G, i1 = G == 1 ? v0 + rows - 1 : (v0 + rows - 1) / G;
+    if (64 % G) places(v0 - i0 * G);  // (tiles do not begin at a query)
+    const Buffer bq = buffer_of(Q + i0 * ldq, ((i1 - i0) * ldq + G * D) * Gm::SZ);
+    const Buffer bd = buffer_of(DO + i0 * lddo, ((i1 - i0) * lddo + G * D) * Gm::SZ);
 #pragma unroll
-      for (int j = 0; j < Gm::NCH; ++j) {
-        k.c[j] = keep[j] ? k.c[j] : zero16();
-        v.c[j] = keep[j] ? v.c[j] : zero16();
-      }
+    for (int j = 0; j < Gm::NP; ++j) {
+      q.load(bq, j, q.row(j) < rows, tiles);
+      d.load(bd, j, q.row(j) < rows, tiles + Gm::TB);
     }
-    k.put(tiles);
-    v.put(tiles + Gm::TB);
-    if (threadIdx.x < kTile) live[threadIdx.x] = counts ? 0.f : -INFINITY;
+    if (threadIdx.x < kTile) {
+      const bool ok = (int)threadIdx.x < rows;
+      const uint32_t v = ok ? v0 + threadIdx.x : v0 + rows - 1;
+      const uint32_t i = G == 1 ? v : v / (uint32_t)G;
+      const int64_t at = (v - i * G) * Nq + i;
+      l = lse[at] * kLog2e;
+      de = delta[at];
+      if (!ok || l == -INFINITY) l = INFINITY;
+      if (!ok) de = 0.f;
+    }
+  }
+  __device__ __forceinline__ void put(float* stat) {
+    if (threadIdx.x < kTile) {
+      stat[threadIdx.x] = l;
+      stat[kTile + threadIdx.x] = de;
+    }
+  }
+};
+
+// Every wave's loads into LDS and writes to it have arrived.
+__device__ __forceinline__ void tiles_ready() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Reads of a tile's operands: a wide one, lane (r, g) elements of row 16 t + r; and
+// columns, lane (r, g) element 16 d + r of rows 16 t + 4 g .. + 3.
+template <typename T, int DP> struct TileRead {
+  using Gm = AskGeo<T, DP>;
+  int wide[Gm::NK], cols[Gm::ND], more[sizeof(T) == 2 ? 1 : 4];
+  __device__ __forceinline__ TileRead() {
+    const int r = lane_id() & 15, g = lane_id() >> 4;
+#pragma unroll
+    for (int k = 0; k < Gm::NK; ++k) wide[k] = r * Gm::RB + ((4 * k + g) ^ Gm::key(r)) * 16;
+    if constexpr (sizeof(T) == 2) {
+      const int row = 4 * g + (r >> 2);
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d)
+        cols[d] = row * Gm::RB + ((2 * d + (r >> 1 & 1)) ^ Gm::key(row)) * 16 + 8 * (r & 1);
+    } else {  // (a key's upper part is the same for the four rows)
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) cols[d] = ((d ^ (Gm::key(4 * g) >> 2)) * 4) * 16 + 4 * (r & 3);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        more[i] = (4 * g + i) * Gm::RB + (((r >> 2) ^ Gm::key(4 * g + i)) & 3) * 16;
+    }
+  }
+  __device__ __forceinline__ void rows(WideF<T>& f, const char* tile, int t, int k) const {
+    set_wide(f, *reinterpret_cast<const uint4*>(tile + wide[k] + t * 16 * Gm::RB));
+  }
+  __device__ __forceinline__ void columns(K16<T>& f, const char* tile, int t, int d) const {
+    if constexpr (sizeof(T) == 2) {
+      ld_tr<T>(f, tile, cols[d], t * 16 * Gm::RB, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        f.v[i] = *reinterpret_cast<const float*>(tile + cols[d] + more[i] + t * 16 * Gm::RB);
+    }
   }
 };
 
@@ -214,16 +316,6 @@ __device__ __forceinline__ void row_frags(WideF<T>* f, const T* row, int D, bool
     set_wide(f[k], on && c < D ? x : zero16());
   }
 }
-// The same from LDS: row r of the 16 that begin at byte `at`, step k.
-template <typename T>
-__device__ __forceinline__ void ld_wide(WideF<T>& f, const char* tile, int base, int at) {
-  set_wide(f, *reinterpret_cast<const uint4*>(tile + base + at));
-}
-template <typename T, int DP> __device__ __forceinline__ int wide_base() {
-  return lds_off(lane_id() & 15, 16 * (lane_id() >> 4), AskGeo<T, DP>::RB);
-}
-constexpr int kStep = 64;  // bytes from one step over the width to the next
-
 // The larger one, NaN where either is (one instruction of three operands; the score of
 // a NaN makes its row NaN in any case).
 __device__ __forceinline__ float largest(float a, float b) {

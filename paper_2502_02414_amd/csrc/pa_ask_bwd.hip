@@ -19,13 +19,13 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && QT * DP <= 128 || DP <= 96 && sizeof(T) == 4 ? 2 : 1)
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && QT * DP <= 192 || DP <= 64 && sizeof(T) == 4 ? 2 : 1)
 k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr bool FIX = sizeof(T) == 2;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
-  __shared__ __attribute__((aligned(16))) float live[2][kTile];
+  __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
+  __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
@@ -42,7 +42,7 @@ k_ask_dq(AskArgs a) {
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   StateTiles<T, DP> st;
   st.init(a, h, kr);
-  if (kr.b < kr.e) st.load(kr.b);
+  if (kr.b < kr.e) st.load(kr.b, tiles0);
   // this lane's queries: column r of the wave's QT tiles of 16
   int64_t row[QT];
   int hq[QT];
@@ -79,32 +79,29 @@ k_ask_dq(AskArgs a) {
   }
   const bool busy = v0 + w * QT * 16 < n;
   const float sc = a.scale * kLog2e;
-  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
-  if (kr.b < kr.e) st.put(smem, live[0]);
-  int buf = 0;
-  for (int64_t p0 = kr.b; p0 < kr.e; p0 += kTile, buf ^= 1) {
-    block_sync();
-    const bool more = p0 + kTile < kr.e;
-    if (more) st.load(p0 + kTile);
-    if (busy) {
-      const char* kt = smem + buf * 2 * Gm::TB;
-      const char* vt = kt + Gm::TB;
-      const bool part = a.mask || p0 + kTile > kr.e;
-      K16<T> pf[FIX ? QT : 1][4], sf[QT][4];
+  const TileRead<T, DP> at;
+  if (kr.b < kr.e) st.put(live0);
+  auto work = [&](int64_t p0, const char* kt, const float* live) __attribute__((always_inline)) {
+    const char* vt = kt + Gm::TB;
+    const bool part = a.mask || p0 + kTile > kr.e;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+    for (int t0 = 0; t0 < 4; t0 += 2) {
+      K16<T> pf[FIX ? QT : 1][2], sf[QT][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = t0 + u;
         f32x4 x[QT], dp[QT];
 #pragma unroll
         for (int c = 0; c < QT; ++c) x[c] = dp[c] = zero4();
         if (part) {
 #pragma unroll
-          for (int c = 0; c < QT; ++c) x[c] = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+          for (int c = 0; c < QT; ++c) x[c] = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
         }
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
           WideF<T> kf, vf;
-          ld_wide<T>(kf, kt, wb, t * 16 * Gm::RB + kStep * k);
-          ld_wide<T>(vf, vt, wb, t * 16 * Gm::RB + kStep * k);
+          at.rows(kf, kt, t, k);
+          at.rows(vf, vt, t, k);
 #pragma unroll
           for (int c = 0; c < QT; ++c) {
             x[c] = mma(kf, qf[c][k], x[c]);
@@ -120,26 +117,34 @@ k_ask_dq(AskArgs a) {
             ds[i] = p[i] * (dp[c][i] - d0[c]);
             if constexpr (FIX) e0[c] += ds[i];
           }
-          if constexpr (FIX) set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
-          set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
+          if constexpr (FIX) set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
+          set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       }
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
+        K16<T> k0, k1;
+        at.columns(k0, kt, t0, d);
+        at.columns(k1, kt, t0 + 1, d);
 #pragma unroll
-        for (int t = 0; t < 4; t += 2) {
-          K16<T> k0, k1;
-          ld_tr<T>(k0, kt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          ld_tr<T>(k1, kt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-#pragma unroll
-          for (int c = 0; c < QT; ++c) {
-            A[c][d] = mma16x2(k0, sf[c][t], k1, sf[c][t + 1], A[c][d]);
-            if constexpr (FIX) Bk[c][d] = mma16x2(k0, pf[c][t], k1, pf[c][t + 1], Bk[c][d]);
-          }
+        for (int c = 0; c < QT; ++c) {
+          A[c][d] = mma16x2(k0, sf[c][0], k1, sf[c][1], A[c][d]);
+          if constexpr (FIX) Bk[c][d] = mma16x2(k0, pf[c][0], k1, pf[c][1], Bk[c][d]);
         }
       }
     }
-    if (more) st.put(smem + (buf ^ 1) * 2 * Gm::TB, live[buf ^ 1]);
+  };
+  auto turn = [&](int64_t p0, const char* now, const float* live, char* next, float* live_next)
+                  __attribute__((always_inline)) {
+    tiles_ready();
+    const bool more = p0 + kTile < kr.e;
+    if (more) st.load(p0 + kTile, next);
+    if (busy) work(p0, now, live);
+    if (more) st.put(live_next);
+  };
+  for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
+    turn(p0, tiles0, live0, tiles1, live1);
+    if (p0 + kTile < kr.e) turn(p0 + kTile, tiles1, live1, tiles0, live0);
   }
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
@@ -200,8 +205,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && KT * DP <= 128 || DP <=
 k_ask_dkv(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TK = 64 * KT, SHIFT = KT == 1 ? 6 : 7;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] q and do tiles
-  __shared__ __attribute__((aligned(16))) float stat[2][2][kTile];  // lse (base 2), delta
+  __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
+  __shared__ __attribute__((aligned(16))) float stat0[2 * kTile], stat1[2 * kTile];  // lse (base 2), delta
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
@@ -215,43 +220,10 @@ k_ask_dkv(AskArgs a) {
   const int n = (int)vr.e;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D + qr.b * a.ldq;
-  const T* DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * a.D + qr.b * a.lddo;
-  TileLoad<T, DP> tq, td;
-  float ls, de;
-  auto places = [&](int rem) __attribute__((always_inline)) {
-    tq.queries(a.ldq, G, rem, a.D);
-    td.queries(a.lddo, G, rem, a.D);
-  };
-  const bool even = 64 % G == 0;  // (tiles begin at a query)
-  if (even) places(0);
-  auto load = [&](int v0) __attribute__((always_inline)) {
-    const int rows = n - v0 < kTile ? n - v0 : kTile;
-    const int i0 = G == 1 ? v0 : v0 / G, i1 = G == 1 ? v0 + rows - 1 : (v0 + rows - 1) / G;
-    if (!even) places(v0 - i0 * G);
-    tq.load(buffer_of(Q + i0 * a.ldq, ((i1 - i0) * a.ldq + G * a.D) * Gm::SZ), rows);
-    td.load(buffer_of(DO + i0 * a.lddo, ((i1 - i0) * a.lddo + G * a.D) * Gm::SZ), rows);
-    if (threadIdx.x < kTile) {
-      const bool ok = (int)threadIdx.x < rows;
-      const uint32_t v = ok ? v0 + threadIdx.x : v0 + rows - 1;
-      const uint32_t i = G == 1 ? v : v / (uint32_t)G;
-      const int64_t at = (int64_t)(h * G + (int)(v - i * G)) * a.Nq + qr.b + i;
-      ls = a.lse[at] * kLog2e;
-      de = a.delta[at];
-      if (!ok || ls == -INFINITY) ls = INFINITY;  // (weights of 0)
-      if (!ok) de = 0.f;
-    }
-  };
-  auto put = [&](int buf) __attribute__((always_inline)) {
-    tq.put(smem + buf * 2 * Gm::TB);
-    td.put(smem + buf * 2 * Gm::TB + Gm::TB);
-    if (threadIdx.x < kTile) {
-      stat[buf][0][threadIdx.x] = ls;
-      stat[buf][1][threadIdx.x] = de;
-    }
-  };
+  QueryTiles<T, DP> st;
+  st.init(a, h, qr.b, n);
   const int first = (int)vr.b;
-  if (first < n) load(first);
+  if (first < n) st.load(first, tiles0);
   const int64_t p0 = kr.b + tile * TK + w * KT * 16 + r;
   const bool busy = kr.b + tile * TK + w * KT * 16 < kr.e;
   bool in[KT];
@@ -270,19 +242,16 @@ k_ask_dkv(AskArgs a) {
     for (int d = 0; d < Gm::ND; ++d) dk[c][d] = dv[c][d] = zero4();
   }
   const float sc = a.scale * kLog2e;
-  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
-  if (first < n) put(0);
-  int buf = 0;
-  for (int v0 = first; v0 < n; v0 += kTile, buf ^= 1) {
-    block_sync();
-    const bool more = v0 + kTile < n;
-    if (more) load(v0 + kTile);
-    if (busy) {
-      const char* qt = smem + buf * 2 * Gm::TB;
-      const char* dt = qt + Gm::TB;
-      K16<T> pf[KT][4], sf[KT][4];
+  const TileRead<T, DP> at;
+  if (first < n) st.put(stat0);
+  auto work = [&](const char* qt, const float* stat) __attribute__((always_inline)) {
+    const char* dt = qt + Gm::TB;
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+    for (int t0 = 0; t0 < 4; t0 += 2) {
+      K16<T> pf[KT][2], sf[KT][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int t = t0 + u;
         f32x4 x[KT], dp[KT];
 #pragma unroll
         for (int c = 0; c < KT; ++c) {
@@ -292,16 +261,16 @@ k_ask_dkv(AskArgs a) {
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
           WideF<T> qf, of;
-          ld_wide<T>(qf, qt, wb, t * 16 * Gm::RB + kStep * k);
-          ld_wide<T>(of, dt, wb, t * 16 * Gm::RB + kStep * k);
+          at.rows(qf, qt, t, k);
+          at.rows(of, dt, t, k);
 #pragma unroll
           for (int c = 0; c < KT; ++c) {
             x[c] = mma(qf, kf[c][k], x[c]);
             dp[c] = mma(of, vf[c][k], dp[c]);
           }
         }
-        const f32x4 l = *reinterpret_cast<const f32x4*>(&stat[buf][0][16 * t + 4 * g]);
-        const f32x4 de4 = *reinterpret_cast<const f32x4*>(&stat[buf][1][16 * t + 4 * g]);
+        const f32x4 l = *reinterpret_cast<const f32x4*>(&stat[16 * t + 4 * g]);
+        const f32x4 de4 = *reinterpret_cast<const f32x4*>(&stat[kTile + 16 * t + 4 * g]);
 #pragma unroll
         for (int c = 0; c < KT; ++c) {
           float pr[4], ds[4];
@@ -310,27 +279,35 @@ k_ask_dkv(AskArgs a) {
             pr[i] = fast_exp2(fmaf(x[c][i], sc, -l[i]));
             ds[i] = pr[i] * (dp[c][i] - de4[i]);
           }
-          set_k16(pf[c][t], pr[0], pr[1], pr[2], pr[3]);
-          set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
+          set_k16(pf[c][u], pr[0], pr[1], pr[2], pr[3]);
+          set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       }
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
+        K16<T> a0, a1;
+        at.columns(a0, dt, t0, d);
+        at.columns(a1, dt, t0 + 1, d);
 #pragma unroll
-        for (int t = 0; t < 4; t += 2) {
-          K16<T> a0, a1;
-          ld_tr<T>(a0, dt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          ld_tr<T>(a1, dt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
+        for (int c = 0; c < KT; ++c) dv[c][d] = mma16x2(a0, pf[c][0], a1, pf[c][1], dv[c][d]);
+        at.columns(a0, qt, t0, d);
+        at.columns(a1, qt, t0 + 1, d);
 #pragma unroll
-          for (int c = 0; c < KT; ++c) dv[c][d] = mma16x2(a0, pf[c][t], a1, pf[c][t + 1], dv[c][d]);
-          ld_tr<T>(a0, qt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          ld_tr<T>(a1, qt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-#pragma unroll
-          for (int c = 0; c < KT; ++c) dk[c][d] = mma16x2(a0, sf[c][t], a1, sf[c][t + 1], dk[c][d]);
-        }
+        for (int c = 0; c < KT; ++c) dk[c][d] = mma16x2(a0, sf[c][0], a1, sf[c][1], dk[c][d]);
       }
     }
-    if (more) put(buf ^ 1);
+  };
+  auto turn = [&](int v0, const char* now, const float* stat, char* next, float* stat_next)
+                  __attribute__((always_inline)) {
+    tiles_ready();
+    const bool more = v0 + kTile < n;
+    if (more) st.load(v0 + kTile, next);
+    if (busy) work(now, stat);
+    if (more) st.put(stat_next);
+  };
+  for (int v0 = first; v0 < n; v0 += 2 * kTile) {
+    turn(v0, tiles0, stat0, tiles1, stat1);
+    if (v0 + kTile < n) turn(v0 + kTile, tiles1, stat1, tiles0, stat0);
   }
 #pragma unroll
   for (int c = 0; c < KT; ++c) {
@@ -373,17 +350,15 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskAr
 }
 
 template <typename T, int DP, int QT> hipError_t launch_dq(const AskArgs& a, hipStream_t st) {
-  constexpr int lds = 4 * AskGeo<T, DP>::TB;
   const int64_t slots = (a.Nq * (a.Hq / a.Hkv) >> (QT == 1 ? 6 : 7)) + a.R;
   hipLaunchKernelGGL((k_ask_dq<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256),
-                     lds, st, a);
+                     0, st, a);
   return hipGetLastError();
 }
 template <typename T, int DP, int KT> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
-  constexpr int lds = 4 * AskGeo<T, DP>::TB;
   const int64_t slots = (a.Nk >> (KT == 1 ? 6 : 7)) + a.R;
   hipLaunchKernelGGL((k_ask_dkv<T, DP, KT>), dim3((uint32_t)(slots * a.Hkv), a.SQ), dim3(256),
-                     lds, st, a);
+                     0, st, a);
   return hipGetLastError();
 }
 // Tiles of 16 states per wave in dk and dv's pass, as ask_tiles.

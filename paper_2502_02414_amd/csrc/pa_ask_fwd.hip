@@ -12,11 +12,12 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
+__global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // [2] k and v tiles
-  __shared__ __attribute__((aligned(16))) float live[2][kTile];
+  // (arrays of their own: the compiler waits for the loads into the one that it reads)
+  __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
+  __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
   const int G = a.Hq / a.Hkv;
   const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
   const int64_t slot = blockIdx.x / a.Hkv;
@@ -34,7 +35,7 @@ __global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
   const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
   StateTiles<T, DP> st;
   st.init(a, h, kr);
-  if (kr.b < kr.e) st.load(kr.b);
+  if (kr.b < kr.e) st.load(kr.b, tiles0);
   // this lane's queries: column r of the wave's QT tiles of 16
   int vq[QT];
   int64_t row[QT];
@@ -60,23 +61,17 @@ __global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
 #pragma unroll
     for (int d = 0; d < Gm::ND; ++d) o[c][d] = zero4();
   }
-  const int wb = wide_base<T, DP>(), tb = tr_base<T>(Gm::RB);
-  if (kr.b < kr.e) st.put(smem, live[0]);
-  int buf = 0;
-  for (int64_t p0 = kr.b; p0 < kr.e; p0 += kTile, buf ^= 1) {
-    block_sync();
-    const bool more = p0 + kTile < kr.e;
-    if (more) st.load(p0 + kTile);
-    if (busy) {
-      const char* kt = smem + buf * 2 * Gm::TB;
-      const char* vt = kt + Gm::TB;
+  const TileRead<T, DP> at;
+  if (kr.b < kr.e) st.put(live0);
+  auto work = [&](int64_t p0, const char* kt, const float* live) __attribute__((always_inline)) {
+    const char* vt = kt + Gm::TB;
       f32x4 x[QT][4];
       // (states that are left out begin at -infinity; their rows are zeros)
       if (a.mask || p0 + kTile > kr.e) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int c = 0; c < QT; ++c) x[c][t] = *reinterpret_cast<const f32x4*>(&live[buf][16 * t + 4 * g]);
+          for (int c = 0; c < QT; ++c) x[c][t] = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
       } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -88,7 +83,7 @@ __global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
           WideF<T> kf;
-          ld_wide<T>(kf, kt, wb, t * 16 * Gm::RB + kStep * k);
+          at.rows(kf, kt, t, k);
 #pragma unroll
           for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], x[c][t]);
         }
@@ -125,15 +120,26 @@ __global__ void __launch_bounds__(256, 2) k_ask(AskArgs a) {
 #pragma unroll
         for (int t = 0; t < 4; t += 2) {
           K16<T> v0f, v1f;
-          ld_tr<T>(v0f, vt, tb, t * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
-          ld_tr<T>(v1f, vt, tb, (t + 1) * 16 * Gm::RB + d * 16 * Gm::SZ, Gm::RB);
+          at.columns(v0f, vt, t, d);
+          at.columns(v1f, vt, t + 1, d);
 #pragma unroll
           for (int c = 0; c < QT; ++c)
             o[c][d] = mma16x2(v0f, pf[c][t], v1f, pf[c][t + 1], o[c][d]);
         }
       }
-    }
-    if (more) st.put(smem + (buf ^ 1) * 2 * Gm::TB, live[buf ^ 1]);
+  };
+  // a tile is worked on while the next one comes into the other array
+  auto turn = [&](int64_t p0, const char* now, const float* live, char* next, float* live_next)
+                  __attribute__((always_inline)) {
+    tiles_ready();
+    const bool more = p0 + kTile < kr.e;
+    if (more) st.load(p0 + kTile, next);
+    if (busy) work(p0, now, live);
+    if (more) st.put(live_next);
+  };
+  for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
+    turn(p0, tiles0, live0, tiles1, live1);
+    if (p0 + kTile < kr.e) turn(p0 + kTile, tiles1, live1, tiles0, live0);
   }
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
@@ -186,10 +192,9 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs 
 }
 
 template <typename T, int DP, int QT> hipError_t launch(const AskArgs& a, hipStream_t st) {
-  using Gm = AskGeo<T, DP>;
   const int64_t G = a.Hq / a.Hkv, slots = (a.Nq * G >> (QT == 1 ? 6 : 7)) + a.R;
-  hipLaunchKernelGGL((k_ask<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256),
-                     4 * Gm::TB, st, a);
+  hipLaunchKernelGGL((k_ask<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256), 0, st,
+                     a);
   return hipGetLastError();
 }
 hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
