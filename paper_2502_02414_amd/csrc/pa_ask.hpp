@@ -194,11 +194,20 @@ template <typename T, int DP> struct StateTiles {
     const int rows = e - p0 < kTile ? (int)(e - p0) : kTile;
     const Buffer bk = buffer_of(K + p0 * ldk, ((rows - 1) * ldk + D) * Gm::SZ);
     const Buffer bv = buffer_of(V + p0 * ldv, ((rows - 1) * ldv + D) * Gm::SZ);
-    alive = (mask ? counts != 0 : (int)threadIdx.x < rows) ? 0.f : -INFINITY;
+    if (!mask) {  // (rows past the end lie past the buffers')
+      alive = (int)threadIdx.x < rows ? 0.f : -INFINITY;
+#pragma unroll
+      for (int j = 0; j < Gm::NP; ++j) {
+        k.load(bk, j, true, tiles);
+        v.load(bv, j, true, tiles + Gm::TB);
+      }
+      return;
+    }
+    alive = counts ? 0.f : -INFINITY;
     bool in[Gm::NP];
 #pragma unroll
-    for (int j = 0; j < Gm::NP; ++j) in[j] = !mask || keep[j];
-    if (mask && p0 + kTile < e) ask(p0 + kTile);
+    for (int j = 0; j < Gm::NP; ++j) in[j] = keep[j];
+    if (p0 + kTile < e) ask(p0 + kTile);
 #pragma unroll
     for (int j = 0; j < Gm::NP; ++j) {
       k.load(bk, j, in[j], tiles);

@@ -81,9 +81,8 @@ k_ask_dq(AskArgs a) {
   const float sc = a.scale * kLog2e;
   const TileRead<T, DP> at;
   if (kr.b < kr.e) st.put(live0);
-  auto work = [&](int64_t p0, const char* kt, const float* live) __attribute__((always_inline)) {
+  auto work = [&](const char* kt, const float* live) __attribute__((always_inline)) {
     const char* vt = kt + Gm::TB;
-    const bool part = a.mask || p0 + kTile > kr.e;
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
       K16<T> pf[FIX ? QT : 1][2], sf[QT][2];
@@ -91,12 +90,7 @@ k_ask_dq(AskArgs a) {
       for (int u = 0; u < 2; ++u) {
         const int t = t0 + u;
         f32x4 x[QT], dp[QT];
-#pragma unroll
-        for (int c = 0; c < QT; ++c) x[c] = dp[c] = zero4();
-        if (part) {
-#pragma unroll
-          for (int c = 0; c < QT; ++c) x[c] = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
-        }
+        const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
 #pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
           WideF<T> kf, vf;
@@ -104,8 +98,8 @@ k_ask_dq(AskArgs a) {
           at.rows(vf, vt, t, k);
 #pragma unroll
           for (int c = 0; c < QT; ++c) {
-            x[c] = mma(kf, qf[c][k], x[c]);
-            dp[c] = mma(vf, of[c][k], dp[c]);
+            x[c] = mma(kf, qf[c][k], k ? x[c] : from);
+            dp[c] = mma(vf, of[c][k], k ? dp[c] : zero4());
           }
         }
 #pragma unroll
@@ -139,7 +133,7 @@ k_ask_dq(AskArgs a) {
     tiles_ready();
     const bool more = p0 + kTile < kr.e;
     if (more) st.load(p0 + kTile, next);
-    if (busy) work(p0, now, live);
+    if (busy) work(now, live);
     if (more) st.put(live_next);
   };
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
@@ -227,7 +221,7 @@ k_ask_dkv(AskArgs a) {
   const int64_t p0 = kr.b + tile * TK + w * KT * 16 + r;
   const bool busy = kr.b + tile * TK + w * KT * 16 < kr.e;
   bool in[KT];
-  float none[KT];  // 0, or -infinity where the state is left out
+  bool counts[KT];
   WideF<T> kf[KT][Gm::NK], vf[KT][Gm::NK];
   f32x4 dk[KT][Gm::ND], dv[KT][Gm::ND];
 #pragma unroll
@@ -235,7 +229,7 @@ k_ask_dkv(AskArgs a) {
     in[c] = p0 + 16 * c < kr.e;
     const int64_t p = in[c] ? p0 + 16 * c : kr.e - 1;
     const bool on = in[c] && (!a.mask || a.mask[p]);
-    none[c] = on ? 0.f : -INFINITY;
+    counts[c] = on;
     row_frags<T, DP>(kf[c], reinterpret_cast<const T*>(a.k) + p * a.ldk + (int64_t)h * a.D, a.D, on);
     row_frags<T, DP>(vf[c], reinterpret_cast<const T*>(a.v) + p * a.ldv + (int64_t)h * a.D, a.D, on);
 #pragma unroll
@@ -254,19 +248,14 @@ k_ask_dkv(AskArgs a) {
         const int t = t0 + u;
         f32x4 x[KT], dp[KT];
 #pragma unroll
-        for (int c = 0; c < KT; ++c) {
-          x[c] = f32x4{none[c], none[c], none[c], none[c]};
-          dp[c] = zero4();
-        }
-#pragma unroll
         for (int k = 0; k < Gm::NK; ++k) {
           WideF<T> qf, of;
           at.rows(qf, qt, t, k);
           at.rows(of, dt, t, k);
 #pragma unroll
           for (int c = 0; c < KT; ++c) {
-            x[c] = mma(qf, kf[c][k], x[c]);
-            dp[c] = mma(of, vf[c][k], dp[c]);
+            x[c] = mma(qf, kf[c][k], k ? x[c] : zero4());
+            dp[c] = mma(of, vf[c][k], k ? dp[c] : zero4());
           }
         }
         const f32x4 l = *reinterpret_cast<const f32x4*>(&stat[16 * t + 4 * g]);
@@ -313,6 +302,10 @@ k_ask_dkv(AskArgs a) {
   for (int c = 0; c < KT; ++c) {
     if (!in[c]) continue;
     const int64_t p = p0 + 16 * c;
+    if (!counts[c]) {  // (weights of a row of zeros: no gradient of a state that is left out)
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) dk[c][d] = dv[c][d] = zero4();
+    }
     if (a.SQ == 1) {
       T* DK = reinterpret_cast<T*>(a.dk) + p * a.lddk + (int64_t)h * a.D;
       T* DV = reinterpret_cast<T*>(a.dv) + p * a.lddv + (int64_t)h * a.D;
@@ -363,7 +356,7 @@ template <typename T, int DP, int KT> hipError_t launch_dkv(const AskArgs& a, hi
 }
 // Tiles of 16 states per wave in dk and dv's pass, as ask_tiles.
 int state_tiles(const AskArgs& a, int dtype) {
-  return dtype == 1 && a.Nk / a.R >= 128 && a.Nq * (a.Hq / a.Hkv) / a.R >= 128 ? 2 : 1;
+  return dtype == 1 && a.D <= 64 && a.Nk / a.R >= 128 && a.Nq * (a.Hq / a.Hkv) / a.R >= 128 ? 2 : 1;
 }
 
 hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {

@@ -12,7 +12,7 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
   // (arrays of their own: the compiler waits for the loads into the one that it reads)
@@ -63,70 +63,61 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskA
   }
   const TileRead<T, DP> at;
   if (kr.b < kr.e) st.put(live0);
-  auto work = [&](int64_t p0, const char* kt, const float* live) __attribute__((always_inline)) {
+  auto work = [&](const char* kt, const float* live) __attribute__((always_inline)) {
     const char* vt = kt + Gm::TB;
-      f32x4 x[QT][4];
+    f32x4 x[QT][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
       // (states that are left out begin at -infinity; their rows are zeros)
-      if (a.mask || p0 + kTile > kr.e) {
+      const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+      for (int k = 0; k < Gm::NK; ++k) {
+        WideF<T> kf;
+        at.rows(kf, kt, t, k);
 #pragma unroll
-          for (int c = 0; c < QT; ++c) x[c][t] = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
-      } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int c = 0; c < QT; ++c) x[c][t] = zero4();
+        for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], k ? x[c][t] : from);
       }
+    }
+    K16<T> pf[QT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+    for (int c = 0; c < QT; ++c) {
+      float mx = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < Gm::NK; ++k) {
-          WideF<T> kf;
-          at.rows(kf, kt, t, k);
+      for (int t = 0; t < 4; ++t) mx = largest(mx, x[c][t]);
+      mx = groups_max(mx) * sc;
+      // The maximum moves only where a score is 2^8 above it: weights up to 2^8 are as
+      // exact, and most tiles leave o and l as they are.
+      if (__any(mx > m[c] + 8.f)) {
+        const float to = fmaxf(m[c], mx), down = fast_exp2(m[c] - (to == -INFINITY ? 0.f : to));
+        m[c] = to;
+        l[c] *= down;
 #pragma unroll
-          for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], x[c][t]);
-        }
-      K16<T> pf[QT][4];
-#pragma unroll
-      for (int c = 0; c < QT; ++c) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) mx = largest(mx, x[c][t]);
-        mx = groups_max(mx) * sc;
-        // The maximum moves only where a score is 2^8 above it: weights up to 2^8 are as
-        // exact, and most tiles leave o and l as they are.
-        if (__any(mx > m[c] + 8.f)) {
-          const float to = fmaxf(m[c], mx), down = fast_exp2(m[c] - (to == -INFINITY ? 0.f : to));
-          m[c] = to;
-          l[c] *= down;
-#pragma unroll
-          for (int d = 0; d < Gm::ND; ++d) o[c][d] *= down;
-        }
-        const float base = m[c] == -INFINITY ? 0.f : m[c];  // (nothing yet: weights of 0)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          float p[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[i] = fast_exp2(fmaf(x[c][t][i], sc, -base));
-            l[c] += p[i];
-          }
-          set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
-        }
+        for (int d = 0; d < Gm::ND; ++d) o[c][d] *= down;
       }
+      const float base = m[c] == -INFINITY ? 0.f : m[c];  // (nothing yet: weights of 0)
 #pragma unroll
-      for (int d = 0; d < Gm::ND; ++d) {
+      for (int t = 0; t < 4; ++t) {
+        float p[4];
 #pragma unroll
-        for (int t = 0; t < 4; t += 2) {
-          K16<T> v0f, v1f;
-          at.columns(v0f, vt, t, d);
-          at.columns(v1f, vt, t + 1, d);
-#pragma unroll
-          for (int c = 0; c < QT; ++c)
-            o[c][d] = mma16x2(v0f, pf[c][t], v1f, pf[c][t + 1], o[c][d]);
+        for (int i = 0; i < 4; ++i) {
+          p[i] = fast_exp2(fmaf(x[c][t][i], sc, -base));
+          l[c] += p[i];
         }
+        set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
       }
+    }
+#pragma unroll
+    for (int d = 0; d < Gm::ND; ++d) {
+#pragma unroll
+      for (int t = 0; t < 4; t += 2) {
+        K16<T> v0f, v1f;
+        at.columns(v0f, vt, t, d);
+        at.columns(v1f, vt, t + 1, d);
+#pragma unroll
+        for (int c = 0; c < QT; ++c)
+          o[c][d] = mma16x2(v0f, pf[c][t], v1f, pf[c][t + 1], o[c][d]);
+      }
+    }
   };
   // a tile is worked on while the next one comes into the other array
   auto turn = [&](int64_t p0, const char* now, const float* live, char* next, float* live_next)
@@ -134,7 +125,7 @@ __global__ void __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskA
     tiles_ready();
     const bool more = p0 + kTile < kr.e;
     if (more) st.load(p0 + kTile, next);
-    if (busy) work(p0, now, live);
+    if (busy) work(now, live);
     if (more) st.put(live_next);
   };
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
