@@ -12,6 +12,8 @@
 // dq_i does.  So dq's pass corrects it: with d0 = do.o,
 //   A = sum p (dp - d0) k,  B = sum p k,  e = sum p (dp - d0):
 //   dq = scale (A - e B),  delta = d0 + e.
+#include <algorithm>
+
 #include "pa_ask.hpp"
 
 namespace pa {
@@ -83,38 +85,44 @@ k_ask_dq(AskArgs a) {
   if (kr.b < kr.e) st.put(live0);
   auto work = [&](const char* kt, const float* live) __attribute__((always_inline)) {
     const char* vt = kt + Gm::TB;
+    // (all scores first: they are on their way while the first weights are formed, and a
+    // half's products while the other's are)
+    f32x4 x[4][QT], dp[4][QT];
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
+#pragma unroll
+      for (int k = 0; k < Gm::NK; ++k) {
+        WideF<T> kf, vf;
+        at.rows(kf, kt, t, k);
+        at.rows(vf, vt, t, k);
+#pragma unroll
+        for (int c = 0; c < QT; ++c) {
+          x[t][c] = mma(kf, qf[c][k], k ? x[t][c] : from);
+          dp[t][c] = mma(vf, of[c][k], k ? dp[t][c] : zero4());
+        }
+      }
+    }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
       K16<T> pf[FIX ? QT : 1][2], sf[QT][2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int t = t0 + u;
-        f32x4 x[QT], dp[QT];
-        const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
-#pragma unroll
-        for (int k = 0; k < Gm::NK; ++k) {
-          WideF<T> kf, vf;
-          at.rows(kf, kt, t, k);
-          at.rows(vf, vt, t, k);
-#pragma unroll
-          for (int c = 0; c < QT; ++c) {
-            x[c] = mma(kf, qf[c][k], k ? x[c] : from);
-            dp[c] = mma(vf, of[c][k], k ? dp[c] : zero4());
-          }
-        }
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int c = 0; c < QT; ++c) {
           float p[4], ds[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            p[i] = fast_exp2(fmaf(x[c][i], sc, -lse2[c]));
-            ds[i] = p[i] * (dp[c][i] - d0[c]);
+            p[i] = fast_exp2(fmaf(x[t0 + u][c][i], sc, -lse2[c]));
+            ds[i] = p[i] * (dp[t0 + u][c][i] - d0[c]);
             if constexpr (FIX) e0[c] += ds[i];
           }
           if constexpr (FIX) set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
           set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
-      }
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
         K16<T> k0, k1;
@@ -126,6 +134,7 @@ k_ask_dq(AskArgs a) {
           if constexpr (FIX) Bk[c][d] = mma16x2(k0, pf[c][0], k1, pf[c][1], Bk[c][d]);
         }
       }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   auto turn = [&](int64_t p0, const char* now, const float* live, char* next, float* live_next)
@@ -240,24 +249,28 @@ k_ask_dkv(AskArgs a) {
   if (first < n) st.put(stat0);
   auto work = [&](const char* qt, const float* stat) __attribute__((always_inline)) {
     const char* dt = qt + Gm::TB;
+    f32x4 x[4][KT], dp[4][KT];
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < Gm::NK; ++k) {
+        WideF<T> qf, of;
+        at.rows(qf, qt, t, k);
+        at.rows(of, dt, t, k);
+#pragma unroll
+        for (int c = 0; c < KT; ++c) {
+          x[t][c] = mma(qf, kf[c][k], k ? x[t][c] : zero4());
+          dp[t][c] = mma(of, vf[c][k], k ? dp[t][c] : zero4());
+        }
+      }
+    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
       K16<T> pf[KT][2], sf[KT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int t = t0 + u;
-        f32x4 x[KT], dp[KT];
-#pragma unroll
-        for (int k = 0; k < Gm::NK; ++k) {
-          WideF<T> qf, of;
-          at.rows(qf, qt, t, k);
-          at.rows(of, dt, t, k);
-#pragma unroll
-          for (int c = 0; c < KT; ++c) {
-            x[c] = mma(qf, kf[c][k], k ? x[c] : zero4());
-            dp[c] = mma(of, vf[c][k], k ? dp[c] : zero4());
-          }
-        }
         const f32x4 l = *reinterpret_cast<const f32x4*>(&stat[16 * t + 4 * g]);
         const f32x4 de4 = *reinterpret_cast<const f32x4*>(&stat[kTile + 16 * t + 4 * g]);
 #pragma unroll
@@ -265,13 +278,14 @@ k_ask_dkv(AskArgs a) {
           float pr[4], ds[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            pr[i] = fast_exp2(fmaf(x[c][i], sc, -l[i]));
-            ds[i] = pr[i] * (dp[c][i] - de4[i]);
+            pr[i] = fast_exp2(fmaf(x[t][c][i], sc, -l[i]));
+            ds[i] = pr[i] * (dp[t][c][i] - de4[i]);
           }
           set_k16(pf[c][u], pr[0], pr[1], pr[2], pr[3]);
           set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       }
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
         K16<T> a0, a1;
@@ -284,6 +298,7 @@ k_ask_dkv(AskArgs a) {
 #pragma unroll
         for (int c = 0; c < KT; ++c) dk[c][d] = mma16x2(a0, sf[c][0], a1, sf[c][1], dk[c][d]);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   auto turn = [&](int v0, const char* now, const float* stat, char* next, float* stat_next)
@@ -354,7 +369,8 @@ template <typename T, int DP, int KT> hipError_t launch_dkv(const AskArgs& a, hi
                      0, st, a);
   return hipGetLastError();
 }
-// Tiles of 16 states per wave in dk and dv's pass, as ask_tiles.
+// Tiles of 16 queries per wave in dq's pass, as ask_tiles, and of states in dk and dv's.
+int query_tiles(const AskArgs& a, int dtype) { return a.D <= 64 ? ask_tiles(a, dtype) : 1; }
 int state_tiles(const AskArgs& a, int dtype) {
   return dtype == 1 && a.D <= 64 && a.Nk / a.R >= 128 && a.Nq * (a.Hq / a.Hkv) / a.R >= 128 ? 2 : 1;
 }
@@ -362,7 +378,7 @@ int state_tiles(const AskArgs& a, int dtype) {
 hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (a.Nq) {
-    const bool two = ask_tiles(a, dtype) == 2;
+    const bool two = query_tiles(a, dtype) == 2;
     e = by_width(a.D, dtype, [&](auto type, auto dp) {
       using T = decltype(type);
       constexpr int DP = decltype(dp)::value;
@@ -398,14 +414,19 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
 
 }  // namespace
 
-// Pieces of the queries: with fewer blocks of all of them than the chip holds.
+// Pieces of the states in dq's pass, and of the queries in dk and dv's: with fewer blocks
+// of all of them than the chip holds.
+int ask_pieces_dq(const AskArgs& a, int dtype) {
+  const int q = query_tiles(a, dtype);
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
+  return ask_pieces_of((rows / (64 * q) + a.R) * a.Hkv,
+                       std::min(q == 2 ? 2 : 4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
+}
 int ask_pieces_q(const AskArgs& a, int dtype) {
   const int k = state_tiles(a, dtype);
-  const int64_t blocks = (a.Nk / (64 * k) + a.R) * a.Hkv;
-  const int64_t tiles = (a.Nq * (a.Hq / a.Hkv) / a.R + kTile - 1) / kTile;
-  int64_t S = ((k == 2 ? 512 : 1024) + blocks / 2) / blocks;
-  if (S > tiles / 2) S = tiles / 2;
-  return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
+  return ask_pieces_of((a.Nk / (64 * k) + a.R) * a.Hkv,
+                       std::min(k == 2 ? 2 : 4, ask_lds_blocks(a, dtype)),
+                       a.Nq * (a.Hq / a.Hkv) / a.R);
 }
 
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st) {

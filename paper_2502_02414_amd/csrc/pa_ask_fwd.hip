@@ -5,6 +5,8 @@
 // sums are fp32, and exp(s - m) is rounded to the operands' type for the product with
 // v (bf16: 2^-9 of each weight, below the rounding of o, since the errors of several
 // weights do not line up; l adds up the unrounded ones).
+#include <algorithm>
+
 #include "pa_ask.hpp"
 
 namespace pa {
@@ -12,7 +14,7 @@ namespace {
 using namespace ask;
 
 template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 3 : DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 4 : DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP>;
   constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
   // (arrays of their own: the compiler waits for the loads into the one that it reads)
@@ -66,6 +68,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 3 : DP * siz
   auto work = [&](const char* kt, const float* live) __attribute__((always_inline)) {
     const char* vt = kt + Gm::TB;
     f32x4 x[QT][4];
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       // (states that are left out begin at -infinity; their rows are zeros)
@@ -78,7 +81,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 3 : DP * siz
         for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], k ? x[c][t] : from);
       }
     }
-    K16<T> pf[QT][4];
+    __builtin_amdgcn_s_setprio(0);
+    float base[QT];
 #pragma unroll
     for (int c = 0; c < QT; ++c) {
       float mx = -INFINITY;
@@ -94,29 +98,35 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 3 : DP * siz
 #pragma unroll
         for (int d = 0; d < Gm::ND; ++d) o[c][d] *= down;
       }
-      const float base = m[c] == -INFINITY ? 0.f : m[c];  // (nothing yet: weights of 0)
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          p[i] = fast_exp2(fmaf(x[c][t][i], sc, -base));
-          l[c] += p[i];
-        }
-        set_k16(pf[c][t], p[0], p[1], p[2], p[3]);
-      }
+      base[c] = m[c] == -INFINITY ? 0.f : m[c];  // (nothing yet: weights of 0)
     }
+    // (half of the states at a time: a half's products run while the next one's weights
+    // are formed)
 #pragma unroll
-    for (int d = 0; d < Gm::ND; ++d) {
+    for (int t0 = 0; t0 < 4; t0 += 2) {
+      K16<T> pf[QT][2];
 #pragma unroll
-      for (int t = 0; t < 4; t += 2) {
+      for (int c = 0; c < QT; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[i] = fast_exp2(fmaf(x[c][t0 + u][i], sc, -base[c]));
+            l[c] += p[i];
+          }
+          set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
+        }
+      __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int d = 0; d < Gm::ND; ++d) {
         K16<T> v0f, v1f;
-        at.columns(v0f, vt, t, d);
-        at.columns(v1f, vt, t + 1, d);
+        at.columns(v0f, vt, t0, d);
+        at.columns(v1f, vt, t0 + 1, d);
 #pragma unroll
-        for (int c = 0; c < QT; ++c)
-          o[c][d] = mma16x2(v0f, pf[c][t], v1f, pf[c][t + 1], o[c][d]);
+        for (int c = 0; c < QT; ++c) o[c][d] = mma16x2(v0f, pf[c][0], v1f, pf[c][1], o[c][d]);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
   };
   // a tile is worked on while the next one comes into the other array
@@ -207,14 +217,24 @@ int ask_tiles(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv);
   return dtype == 1 && rows / a.R >= 128 && rows / 128 * a.Hkv >= 256 ? 2 : 1;
 }
-// Pieces of the states: with fewer blocks of whole ones than the chip holds.
-int ask_pieces(const AskArgs& a, int dtype) {
-  const int q = ask_tiles(a, dtype);
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv), blocks = (rows / (64 * q) + a.R) * a.Hkv;
-  const int64_t tiles = (a.Nk / a.R + kTile - 1) / kTile;
-  int64_t S = ((q == 2 ? 512 : 1024) + blocks / 2) / blocks;
+// Blocks of whole requests, and of how many of them a CU has room for, to the pieces that
+// fill the chip: at least two tiles each.
+int ask_pieces_of(int64_t blocks, int resident, int64_t rows) {
+  const int64_t tiles = (rows + kTile - 1) / kTile;
+  int64_t S = (256 * resident + blocks / 2) / blocks;
   if (S > tiles / 2) S = tiles / 2;
   return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
+}
+// Blocks of the kernels that LDS has room for in a CU: two tiles of two tensors each.
+int ask_lds_blocks(const AskArgs& a, int dtype) {
+  const int bytes = a.D * (dtype == 1 ? 2 : 4);
+  return bytes <= 64 ? 9 : bytes <= 128 ? 4 : bytes <= 256 ? 2 : 1;
+}
+// Pieces of the states: with fewer blocks of whole ones than the chip holds.
+int ask_pieces(const AskArgs& a, int dtype) {
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
+  return ask_pieces_of((rows / (64 * ask_tiles(a, dtype)) + a.R) * a.Hkv,
+                       std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
 }
 
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {

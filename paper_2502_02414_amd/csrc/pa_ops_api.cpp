@@ -610,7 +610,7 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
     a->delta = take(rows);  // (for requests that are longer than max_k says)
     return at;
   }
-  a->S = pa::ask_pieces(*a, dtype);
+  a->S = backward ? pa::ask_pieces_dq(*a, dtype) : pa::ask_pieces(*a, dtype);
   if (a->S > 1) {
     a->part = take((uint64_t)a->S * rows * a->D);
     a->part_lse = take((uint64_t)a->S * rows);

@@ -135,8 +135,11 @@ struct AskArgs {
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
 int ask_tiles(const AskArgs& a, int dtype);  // of 16 queries, per wave
-int ask_pieces(const AskArgs& a, int dtype);    // S
-int ask_pieces_q(const AskArgs& a, int dtype);  // SQ
+int ask_pieces_of(int64_t blocks, int resident, int64_t rows);
+int ask_lds_blocks(const AskArgs& a, int dtype);
+int ask_pieces(const AskArgs& a, int dtype);     // S, forward
+int ask_pieces_dq(const AskArgs& a, int dtype);  // S, backward
+int ask_pieces_q(const AskArgs& a, int dtype);   // SQ
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
 // Few states (pa_ask_few.hip): served, and faster.
 bool ask_few_served(const AskArgs& a, int dtype);
