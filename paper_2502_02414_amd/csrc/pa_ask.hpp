@@ -58,12 +58,13 @@ __device__ __forceinline__ float wide_elem(const K16<float>& f, int e) { return 
 // neighbour) and, bf16, columns (ds_read_b64_tr_b16: in one cycle two chunks of rows 0-7
 // or of 8-15); with these keys both meet every bank once: 4.2 and 2.2 cycles for 1 KB and
 // 512 B, with keys that make the 16 rows' places differ 4.2 and 4.1, or 8.1 and 2.2.
-template <typename T, int DP> struct AskGeo {
+// W: waves of a block.
+template <typename T, int DP, int W = 4> struct AskGeo {
   static constexpr int SZ = (int)sizeof(T), E = 16 / SZ;  // E: elements of 16 bytes
   static constexpr int NK = (DP + Wide<T>::W - 1) / Wide<T>::W, ND = DP / 16;  // steps; tiles
   static constexpr int CP = NK <= 1 ? 4 : NK <= 2 ? 8 : NK <= 4 ? 16 : 32;     // chunks of a row
   static constexpr int RB = 16 * CP, TB = kTile * RB;     // bytes of a row, of a tile
-  static constexpr int NP = TB / 4096;                    // loads of a tile per wave (of 4)
+  static constexpr int NP = (TB + 1024 * W - 1) / (1024 * W);  // loads of a tile per wave
   static __device__ __forceinline__ int key(int row) {
     if constexpr (SZ == 4) return CP == 4 ? row >> 2 & 3 : CP == 8 ? row >> 1 & 7 : row & 15;
     return CP == 4 ? 2 * (row >> 2 & 1) : CP == 8 ? 2 * (row >> 1 & 3) : 2 * (row & 7);
@@ -132,17 +133,17 @@ __device__ __forceinline__ void load_lds16(Buffer b, char* dst, int at) {
 }
 constexpr int kNowhere = 0x7fffff00;
 
-// Loads of a tile of up to 64 rows into LDS by 4 waves, 16 bytes a lane, without a
+// Loads of a tile of up to 64 rows into LDS by W waves, 16 bytes a lane, without a
 // register between, zeros where rows or columns end.  Offsets within a tile stay below
 // 2^31: rows are at most 2^25 bytes apart.
-template <typename T, int DP> struct TileLoad {
-  using Gm = AskGeo<T, DP>;
+template <typename T, int DP, int W> struct TileLoad {
+  using Gm = AskGeo<T, DP, W>;
   int off[Gm::NP];
 
   // this lane's row and column in load j of its wave
-  static __device__ __forceinline__ int row(int j) { return (256 * j + (int)threadIdx.x) / Gm::CP; }
+  static __device__ __forceinline__ int row(int j) { return (64 * W * j + (int)threadIdx.x) / Gm::CP; }
   static __device__ __forceinline__ int col(int j) {
-    return ((256 * j + (int)threadIdx.x) % Gm::CP ^ Gm::key(row(j))) * Gm::E;
+    return ((64 * W * j + (int)threadIdx.x) % Gm::CP ^ Gm::key(row(j))) * Gm::E;
   }
   // rows of states, ld elements apart
   __device__ __forceinline__ void states(int64_t ld, int D) {
@@ -159,17 +160,17 @@ template <typename T, int DP> struct TileLoad {
     }
   }
   __device__ __forceinline__ void load(Buffer b, int j, bool in, char* tile) const {
-    char* dst = tile + 4096 * j + 1024 * __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    load_lds16(b, dst, in ? off[j] : kNowhere);
+    const int at = 1024 * (W * j + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    if (Gm::TB % (1024 * W) == 0 || at < Gm::TB) load_lds16(b, tile + at, in ? off[j] : kNowhere);
   }
 };
 
 // Tiles of a request's states in LDS: k's, v's behind it, and which of them count (0, or
 // -infinity where one is left out, whose rows are zeros: they may hold anything).  Which
 // rows are left out is asked for a tile ahead, before its loads are.
-template <typename T, int DP> struct StateTiles {
-  using Gm = AskGeo<T, DP>;
-  TileLoad<T, DP> k, v;
+template <typename T, int DP, int W> struct StateTiles {
+  using Gm = AskGeo<T, DP, W>;
+  TileLoad<T, DP, W> k, v;
   const T *K, *V;
   const uint8_t* mask;
   int64_t ldk, ldv, e;
@@ -221,9 +222,9 @@ template <typename T, int DP> struct StateTiles {
 
 // Tiles of a request's virtual rows: q's, do's behind it, and their lse (base 2) and
 // delta, [2][64] floats, with which rows past the end have weights of 0.
-template <typename T, int DP> struct QueryTiles {
-  using Gm = AskGeo<T, DP>;
-  TileLoad<T, DP> q, d;
+template <typename T, int DP, int W> struct QueryTiles {
+  using Gm = AskGeo<T, DP, W>;
+  TileLoad<T, DP, W> q, d;
   const T *Q, *DO;
   const float *lse, *delta;
   int64_t ldq, lddo, Nq;

@@ -20,12 +20,11 @@ namespace pa {
 namespace {
 using namespace ask;
 
-template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && QT * DP <= 192 || DP <= 64 && sizeof(T) == 4 ? 2 : 1)
-k_ask_dq(AskArgs a) {
-  using Gm = AskGeo<T, DP>;
+template <typename T, int DP, int QT, int W>
+__global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dq(AskArgs a) {
+  using Gm = AskGeo<T, DP, W>;
   constexpr bool FIX = sizeof(T) == 2;
-  constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
+  constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
   const int G = a.Hq / a.Hkv;
@@ -42,7 +41,7 @@ k_ask_dq(AskArgs a) {
   if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  StateTiles<T, DP> st;
+  StateTiles<T, DP, W> st;
   st.init(a, h, kr);
   if (kr.b < kr.e) st.load(kr.b, tiles0);
   // this lane's queries: column r of the wave's QT tiles of 16
@@ -201,13 +200,12 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
 }
 
-// dk and dv of a tile of 64 KT states: a wave has KT times 16 of them as columns, and
+// dk and dv of a tile of 16 KT W states: a wave has KT times 16 of them as columns, and
 // their rows of k and v in registers; the queries come through LDS.
-template <typename T, int DP, int KT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && KT * DP <= 128 || DP <= 64 && sizeof(T) == 4 ? 2 : 1)
-k_ask_dkv(AskArgs a) {
-  using Gm = AskGeo<T, DP>;
-  constexpr int TK = 64 * KT, SHIFT = KT == 1 ? 6 : 7;
+template <typename T, int DP, int KT, int W>
+__global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dkv(AskArgs a) {
+  using Gm = AskGeo<T, DP, W>;
+  constexpr int TK = 16 * KT * W, SHIFT = TK == 64 ? 6 : TK == 128 ? 7 : 8;
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float stat0[2 * kTile], stat1[2 * kTile];  // lse (base 2), delta
   const int G = a.Hq / a.Hkv;
@@ -223,7 +221,7 @@ k_ask_dkv(AskArgs a) {
   const int n = (int)vr.e;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  QueryTiles<T, DP> st;
+  QueryTiles<T, DP, W> st;
   st.init(a, h, qr.b, n);
   const int first = (int)vr.b;
   if (first < n) st.load(first, tiles0);
@@ -357,34 +355,37 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskAr
   store4<T>(to, sum);
 }
 
-template <typename T, int DP, int QT> hipError_t launch_dq(const AskArgs& a, hipStream_t st) {
-  const int64_t slots = (a.Nq * (a.Hq / a.Hkv) >> (QT == 1 ? 6 : 7)) + a.R;
-  hipLaunchKernelGGL((k_ask_dq<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256),
+template <typename T, int DP, int QT, int W> hipError_t launch_dq(const AskArgs& a, hipStream_t st) {
+  const int64_t slots = a.Nq * (a.Hq / a.Hkv) / (16 * QT * W) + a.R;
+  hipLaunchKernelGGL((k_ask_dq<T, DP, QT, W>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(64 * W), 0,
+                     st, a);
+  return hipGetLastError();
+}
+template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
+  const int64_t slots = a.Nk / (16 * KT * W) + a.R;
+  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W>), dim3((uint32_t)(slots * a.Hkv), a.SQ), dim3(64 * W),
                      0, st, a);
   return hipGetLastError();
 }
-template <typename T, int DP, int KT> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
-  const int64_t slots = (a.Nk >> (KT == 1 ? 6 : 7)) + a.R;
-  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT>), dim3((uint32_t)(slots * a.Hkv), a.SQ), dim3(256),
-                     0, st, a);
-  return hipGetLastError();
-}
-// Tiles of 16 queries per wave in dq's pass, as ask_tiles, and of states in dk and dv's.
-int query_tiles(const AskArgs& a, int dtype) { return a.D <= 64 ? ask_tiles(a, dtype) : 1; }
-int state_tiles(const AskArgs& a, int dtype) {
-  return dtype == 1 && a.D <= 64 && a.Nk / a.R >= 128 && a.Nq * (a.Hq / a.Hkv) / a.R >= 128 ? 2 : 1;
+// Blocks of eight waves in dq's pass, as ask_large, and of as many states in dk and dv's;
+// with two tiles of 16 a wave up to 64 wide (wider ones have no registers for two).
+int rows_dq(const AskArgs& a, int dtype) { return !ask_large(a, dtype) ? 64 : a.D <= 64 ? 256 : 128; }
+int rows_dkv(const AskArgs& a, int dtype) {
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
+  const bool large = dtype == 1 && a.Nk / a.R >= 256 && rows / a.R >= 256;
+  return !large ? 64 : a.D <= 64 ? 256 : 128;
 }
 
 hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (a.Nq) {
-    const bool two = query_tiles(a, dtype) == 2;
+    const bool large = rows_dq(a, dtype) > 64;
     e = by_width(a.D, dtype, [&](auto type, auto dp) {
       using T = decltype(type);
       constexpr int DP = decltype(dp)::value;
       if constexpr (sizeof(T) == 2)
-        if (two) return launch_dq<T, DP, 2>(a, st);
-      return launch_dq<T, DP, 1>(a, st);
+        if (large) return launch_dq<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
+      return launch_dq<T, DP, 1, 4>(a, st);
     });
     if (e != hipSuccess) return e;
     if (a.S > 1) {
@@ -396,13 +397,13 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     }
   }
   if (!a.dk || !a.Nk) return hipSuccess;
-  const bool two = state_tiles(a, dtype) == 2;
+  const bool large = rows_dkv(a, dtype) > 64;
   e = by_width(a.D, dtype, [&](auto type, auto dp) {
     using T = decltype(type);
     constexpr int DP = decltype(dp)::value;
     if constexpr (sizeof(T) == 2)
-      if (two) return launch_dkv<T, DP, 2>(a, st);
-    return launch_dkv<T, DP, 1>(a, st);
+      if (large) return launch_dkv<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
+    return launch_dkv<T, DP, 1, 4>(a, st);
   });
   if (e != hipSuccess || a.SQ == 1) return e;
   const int64_t threads = a.Nk * a.Hkv * a.D / 4;
@@ -417,15 +418,14 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
 // Pieces of the states in dq's pass, and of the queries in dk and dv's: with fewer blocks
 // of all of them than the chip holds.
 int ask_pieces_dq(const AskArgs& a, int dtype) {
-  const int q = query_tiles(a, dtype);
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  return ask_pieces_of((rows / (64 * q) + a.R) * a.Hkv,
-                       std::min(q == 2 ? 2 : 4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
+  const int rows = rows_dq(a, dtype);
+  return ask_pieces_of((a.Nq * (a.Hq / a.Hkv) / rows + a.R) * a.Hkv,
+                       rows > 64 ? 1 : std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {
-  const int k = state_tiles(a, dtype);
-  return ask_pieces_of((a.Nk / (64 * k) + a.R) * a.Hkv,
-                       std::min(k == 2 ? 2 : 4, ask_lds_blocks(a, dtype)),
+  const int rows = rows_dkv(a, dtype);
+  return ask_pieces_of((a.Nk / rows + a.R) * a.Hkv,
+                       rows > 64 ? 1 : std::min(4, ask_lds_blocks(a, dtype)),
                        a.Nq * (a.Hq / a.Hkv) / a.R);
 }
 

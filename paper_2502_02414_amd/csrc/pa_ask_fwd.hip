@@ -13,10 +13,11 @@ namespace pa {
 namespace {
 using namespace ask;
 
-template <typename T, int DP, int QT>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 4 : DP * sizeof(T) <= 256 ? 2 : 1) k_ask(AskArgs a) {
-  using Gm = AskGeo<T, DP>;
-  constexpr int TQ = 64 * QT, SHIFT = QT == 1 ? 6 : 7;
+template <typename T, int DP, int QT, int W>
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 4 : DP * sizeof(T) <= 256 ? 2 : 1)
+k_ask(AskArgs a) {
+  using Gm = AskGeo<T, DP, W>;
+  constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;
   // (arrays of their own: the compiler waits for the loads into the one that it reads)
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
@@ -35,7 +36,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && DP <= 64 ? 4 : DP * siz
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
-  StateTiles<T, DP> st;
+  StateTiles<T, DP, W> st;
   st.init(a, h, kr);
   if (kr.b < kr.e) st.load(kr.b, tiles0);
   // this lane's queries: column r of the wave's QT tiles of 16
@@ -192,30 +193,31 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs 
     a.lse[(int64_t)hq * a.Nq + row] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
 }
 
-template <typename T, int DP, int QT> hipError_t launch(const AskArgs& a, hipStream_t st) {
-  const int64_t G = a.Hq / a.Hkv, slots = (a.Nq * G >> (QT == 1 ? 6 : 7)) + a.R;
-  hipLaunchKernelGGL((k_ask<T, DP, QT>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(256), 0, st,
+template <typename T, int DP, int QT, int W> hipError_t launch(const AskArgs& a, hipStream_t st) {
+  const int64_t G = a.Hq / a.Hkv, slots = a.Nq * G / (16 * QT * W) + a.R;
+  hipLaunchKernelGGL((k_ask<T, DP, QT, W>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(64 * W), 0, st,
                      a);
   return hipGetLastError();
 }
 hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
-  const bool two = dtype == 1 && ask_tiles(a, dtype) == 2;
+  const bool large = ask_large(a, dtype);
   return by_width(a.D, dtype, [&](auto type, auto dp) {
     using T = decltype(type);
     constexpr int DP = decltype(dp)::value;
     if constexpr (sizeof(T) == 2)
-      if (two) return launch<T, DP, 2>(a, st);
-    return launch<T, DP, 1>(a, st);
+      if (large) return launch<T, DP, 2, 8>(a, st);
+    return launch<T, DP, 1, 4>(a, st);
   });
 }
 
 }  // namespace
 
-// Tiles of 16 queries per wave: two (bf16), which halves what is read from LDS for a
-// product, where requests are long enough to fill them and the chip.
-int ask_tiles(const AskArgs& a, int dtype) {
+// Blocks of eight waves with two tiles of 16 queries each (bf16) in place of four with one:
+// a tile of states is read by them a quarter as often, from LDS half as often, where
+// requests are long enough to fill them and the chip.
+bool ask_large(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  return dtype == 1 && rows / a.R >= 128 && rows / 128 * a.Hkv >= 256 ? 2 : 1;
+  return dtype == 1 && rows / a.R >= 256 && rows / 256 * a.Hkv >= 128 && a.Nk / a.R >= 128;
 }
 // Blocks of whole requests, and of how many of them a CU has room for, to the pieces that
 // fill the chip: at least two tiles each.
@@ -233,8 +235,9 @@ int ask_lds_blocks(const AskArgs& a, int dtype) {
 // Pieces of the states: with fewer blocks of whole ones than the chip holds.
 int ask_pieces(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  return ask_pieces_of((rows / (64 * ask_tiles(a, dtype)) + a.R) * a.Hkv,
-                       std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
+  const bool large = ask_large(a, dtype);
+  return ask_pieces_of((rows / (large ? 256 : 64) + a.R) * a.Hkv,
+                       large ? (a.D <= 64 ? 2 : 1) : std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
 }
 
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {

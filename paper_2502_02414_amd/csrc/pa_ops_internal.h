@@ -134,7 +134,7 @@ struct AskArgs {
   int SQ = 1;               // pieces of the queries
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
-int ask_tiles(const AskArgs& a, int dtype);  // of 16 queries, per wave
+bool ask_large(const AskArgs& a, int dtype);  // blocks of many queries
 int ask_pieces_of(int64_t blocks, int resident, int64_t rows);
 int ask_lds_blocks(const AskArgs& a, int dtype);
 int ask_pieces(const AskArgs& a, int dtype);     // S, forward
