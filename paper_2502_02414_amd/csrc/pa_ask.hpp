@@ -326,10 +326,27 @@ __device__ __forceinline__ void row_frags(WideF<T>* f, const T* row, int D, bool
     set_wide(f[k], on && c < D ? x : zero16());
   }
 }
+// Operands that are read together, ahead of their products (pipelined()): as the compiler
+// orders them, it reads, waits and multiplies.
+template <typename T> struct WidePair {
+  WideF<T> a, b;
+};
+template <typename T> struct ColumnPair {
+  K16<T> a, b;
+};
+
 // The larger one, NaN where either is (one instruction of three operands; the score of
 // a NaN makes its row NaN in any case).
 __device__ __forceinline__ float largest(float a, float b) {
   return __builtin_elementwise_maximum(a, b);
+}
+// Of the four lane groups.
+__device__ __forceinline__ float groups_largest(float v) {
+  float a = v, b = v;
+  lane_swap16(a, b);
+  float c = largest(a, b), d = c;
+  lane_swap32(c, d);
+  return largest(c, d);
 }
 // Of an accumulator's four.
 __device__ __forceinline__ float largest(float a, const f32x4& x) {

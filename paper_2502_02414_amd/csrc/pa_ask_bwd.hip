@@ -88,21 +88,20 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
     // half's products while the other's are)
     f32x4 x[4][QT], dp[4][QT];
     __builtin_amdgcn_s_setprio(1);
+    pipelined<4 * Gm::NK, 3, WidePair<T>>(
+        [&](int i, WidePair<T>& f) {
+          at.rows(f.a, kt, i / Gm::NK, i % Gm::NK);
+          at.rows(f.b, vt, i / Gm::NK, i % Gm::NK);
+        },
+        [&](int i, const WidePair<T>& f) {
+          const int t = i / Gm::NK, k = i % Gm::NK;
+          const f32x4 from = k ? zero4() : *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
-#pragma unroll
-      for (int k = 0; k < Gm::NK; ++k) {
-        WideF<T> kf, vf;
-        at.rows(kf, kt, t, k);
-        at.rows(vf, vt, t, k);
-#pragma unroll
-        for (int c = 0; c < QT; ++c) {
-          x[t][c] = mma(kf, qf[c][k], k ? x[t][c] : from);
-          dp[t][c] = mma(vf, of[c][k], k ? dp[t][c] : zero4());
-        }
-      }
-    }
+          for (int c = 0; c < QT; ++c) {
+            x[t][c] = mma(f.a, qf[c][k], k ? x[t][c] : from);
+            dp[t][c] = mma(f.b, of[c][k], k ? dp[t][c] : zero4());
+          }
+        });
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
@@ -122,17 +121,18 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
           set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       __builtin_amdgcn_s_setprio(1);
+      pipelined<Gm::ND, 4, ColumnPair<T>>(
+          [&](int d, ColumnPair<T>& f) {
+            at.columns(f.a, kt, t0, d);
+            at.columns(f.b, kt, t0 + 1, d);
+          },
+          [&](int d, const ColumnPair<T>& f) {
 #pragma unroll
-      for (int d = 0; d < Gm::ND; ++d) {
-        K16<T> k0, k1;
-        at.columns(k0, kt, t0, d);
-        at.columns(k1, kt, t0 + 1, d);
-#pragma unroll
-        for (int c = 0; c < QT; ++c) {
-          A[c][d] = mma16x2(k0, sf[c][0], k1, sf[c][1], A[c][d]);
-          if constexpr (FIX) Bk[c][d] = mma16x2(k0, pf[c][0], k1, pf[c][1], Bk[c][d]);
-        }
-      }
+            for (int c = 0; c < QT; ++c) {
+              A[c][d] = mma16x2(f.a, sf[c][0], f.b, sf[c][1], A[c][d]);
+              if constexpr (FIX) Bk[c][d] = mma16x2(f.a, pf[c][0], f.b, pf[c][1], Bk[c][d]);
+            }
+          });
       __builtin_amdgcn_s_setprio(0);
     }
   };
@@ -249,19 +249,19 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
     const char* dt = qt + Gm::TB;
     f32x4 x[4][KT], dp[4][KT];
     __builtin_amdgcn_s_setprio(1);
+    pipelined<4 * Gm::NK, 3, WidePair<T>>(
+        [&](int i, WidePair<T>& f) {
+          at.rows(f.a, qt, i / Gm::NK, i % Gm::NK);
+          at.rows(f.b, dt, i / Gm::NK, i % Gm::NK);
+        },
+        [&](int i, const WidePair<T>& f) {
+          const int t = i / Gm::NK, k = i % Gm::NK;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int k = 0; k < Gm::NK; ++k) {
-        WideF<T> qf, of;
-        at.rows(qf, qt, t, k);
-        at.rows(of, dt, t, k);
-#pragma unroll
-        for (int c = 0; c < KT; ++c) {
-          x[t][c] = mma(qf, kf[c][k], k ? x[t][c] : zero4());
-          dp[t][c] = mma(of, vf[c][k], k ? dp[t][c] : zero4());
-        }
-      }
+          for (int c = 0; c < KT; ++c) {
+            x[t][c] = mma(f.a, kf[c][k], k ? x[t][c] : zero4());
+            dp[t][c] = mma(f.b, vf[c][k], k ? dp[t][c] : zero4());
+          }
+        });
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
@@ -284,18 +284,20 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
         }
       }
       __builtin_amdgcn_s_setprio(1);
+      // (step 2 d: do's columns for dv, 2 d + 1: q's for dk)
+      pipelined<2 * Gm::ND, 4, ColumnPair<T>>(
+          [&](int i, ColumnPair<T>& f) {
+            at.columns(f.a, i & 1 ? qt : dt, t0, i / 2);
+            at.columns(f.b, i & 1 ? qt : dt, t0 + 1, i / 2);
+          },
+          [&](int i, const ColumnPair<T>& f) {
+            const int d = i / 2;
 #pragma unroll
-      for (int d = 0; d < Gm::ND; ++d) {
-        K16<T> a0, a1;
-        at.columns(a0, dt, t0, d);
-        at.columns(a1, dt, t0 + 1, d);
-#pragma unroll
-        for (int c = 0; c < KT; ++c) dv[c][d] = mma16x2(a0, pf[c][0], a1, pf[c][1], dv[c][d]);
-        at.columns(a0, qt, t0, d);
-        at.columns(a1, qt, t0 + 1, d);
-#pragma unroll
-        for (int c = 0; c < KT; ++c) dk[c][d] = mma16x2(a0, sf[c][0], a1, sf[c][1], dk[c][d]);
-      }
+            for (int c = 0; c < KT; ++c) {
+              if (i & 1) dk[c][d] = mma16x2(f.a, sf[c][0], f.b, sf[c][1], dk[c][d]);
+              else dv[c][d] = mma16x2(f.a, pf[c][0], f.b, pf[c][1], dv[c][d]);
+            }
+          });
       __builtin_amdgcn_s_setprio(0);
     }
   };

@@ -84,19 +84,31 @@ template <int DP, int NT> constexpr int few_bwd_bytes() {
              : 64 * (2 * DP + 32) + 32 * (32 * NT + 32);
 }
 
-// A virtual row of a request.
-struct Place {
-  int v, n;         // of n rows
-  uint32_t i, g;    // its query and head of the group (of row n - 1 past the end)
-  __device__ __forceinline__ void at(int v_, int n_, int G) {
-    v = v_;
-    n = n_;
-    const uint32_t c = v < n ? v : n - 1;
-    i = G == 1 ? c : c / (uint32_t)G;
-    g = c - i * G;
+// 16 bytes of virtual row `v` of a tile (32 of them from one that begins `rem` heads into a
+// query's group), from column c on, in bytes from the tile's first query; kNowhere past D.
+__device__ __forceinline__ int place(int v, int rem, int G, int64_t ld, int D, int c) {
+  const uint32_t u = v + rem, i = G == 1 ? u : u / (uint32_t)G, g = u - i * G;
+  return c < D ? (int)(i * (uint32_t)ld + g * D + c) * 2 : kNowhere;
+}
+// A tensor's rows of a head of a request from query i on, as many as a tile has and not
+// behind query `last`.
+__device__ __forceinline__ Buffer rows_from(const bf16* p, int64_t ld, int i, int last, int width) {
+  return buffer_of(p + i * ld, ((last - i < 32 ? last - i : 32) * ld + width) * 2);
+}
+// (stored past the caches, as what is streamed once)
+__device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, const f32x4& y, float f) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  bf16x8 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o[i] = (bf16)(x[i] * f);
+    o[i + 4] = (bf16)(y[i] * f);
   }
-  __device__ __forceinline__ bool in() const { return v < n; }
-};
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), b, at, 0, 0);
+}
+__device__ __forceinline__ uint4 load16_once(Buffer b, int at) {
+  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
+}
 
 // Which of the block's waves works on what: `heads` of them a head each, the others on
 // other tiles of the same heads.
@@ -104,7 +116,8 @@ struct Role {
   int h, sub, subs;
 };
 __device__ __forceinline__ Role role_of(int Hkv) {
-  const int w = threadIdx.x >> 6, W = blockDim.x >> 6, heads = Hkv < W ? Hkv : W;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int W = blockDim.x >> 6, heads = Hkv < W ? Hkv : W;
   return {(int)blockIdx.y * heads + w % heads, w / heads, W / heads};
 }
 
@@ -117,9 +130,8 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
   const Role me = role_of(a.Hkv);
   const int rq = blockIdx.x / P;
   const Range qr = range_of(a.q_off, rq, a.Nq), kr = range_of(a.k_off, rq, a.Nk);
-  const Range vr = piece(Range{0, (qr.e - qr.b) * G}, blockIdx.x % P, P);
-  if (me.h >= a.Hkv || me.sub >= me.subs || vr.b >= vr.e) return;
-  const int n = (int)vr.e;
+  const int n = (int)(qr.e - qr.b) * G, pc = blockIdx.x % P;
+  if (me.h >= a.Hkv || me.sub >= me.subs || 32 * (pc * me.subs + me.sub) >= n) return;
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + (int64_t)me.h * G * a.D + qr.b * a.ldq;
   const bf16* K = reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D;
@@ -140,38 +152,53 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
     S_::columns(vf, vr_, smem + (threadIdx.x >> 6) * S_::kBytes);
   }
 
-  struct Tile {
-    Place at[C];
-    K32<bf16> q[C][NK];
-  };
-  const int step = 16 * C * me.subs;
-  auto load = [&](int v, Tile& t) __attribute__((always_inline)) {
+  // this lane's parts of a tile of 32 rows: 16 bytes for each step of the width
+  const bool even = 32 % G == 0;  // (tiles begin at a query)
+  const int last = (int)(qr.e - qr.b) - 1;
+  int qo[C][NK], oo[C][NK];
+  auto places = [&](int rem) __attribute__((always_inline)) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      t.at[c].at(v + 16 * c + r, n, G);
-      const bf16* row = Q + t.at[c].i * a.ldq + t.at[c].g * a.D;
+    for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
-        const int col = 32 * k + 8 * g;
-        const uint4 x = ld_global16<true>(row + (col < a.D ? col : 0));
-        t.q[c][k].v = __builtin_bit_cast(bf16x8, col < a.D ? x : zero16());
+        qo[c][k] = place(16 * c + r, rem, G, a.ldq, a.D, 32 * k + 8 * g);
+        oo[c][k] = place(16 * c + r, rem, G, a.ldo, a.D, 32 * k + 8 * g);
       }
-    }
   };
-  auto work = [&](const Tile& q) __attribute__((always_inline)) {
+  places(0);
+  struct Tile {
+    uint4 q[C][NK];
+  };
+  const int step = 16 * C * me.subs * P;  // (blocks go over the rows together)
+  auto load = [&](int v, Tile& t) __attribute__((always_inline)) {
+    if (v >= n) return;
+    const int i0 = G == 1 ? v : v / G;
+    if (!even) places(v - i0 * G);
+    const Buffer b = rows_from(Q, a.ldq, i0, last, G * a.D);
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int k = 0; k < NK; ++k) t.q[c][k] = load16_once(b, qo[c][k]);
+  };
+  auto work = [&](int v, const Tile& q) __attribute__((always_inline)) {
+    const int i0 = G == 1 ? v : v / G;
+    if (!even) places(v - i0 * G);
+    const Buffer b = rows_from(O, a.ldo, i0, last, G * a.D);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       f32x4 x[NT], o[ND];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        x[t] = none[t];
+      for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int k = 0; k < NK; ++k) x[t] = mma32(kf[t][k], q.q[c][k], x[t]);
-      }
+        for (int k = 0; k < NK; ++k) {
+          K32<bf16> qf;
+          set_wide(qf, q.q[c][k]);
+          x[t] = mma32(kf[t][k], qf, k ? x[t] : none[t]);
+        }
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < NT; ++t) mx = largest(mx, x[t]);
-      mx = groups_max(mx) * sc;
+      mx = groups_largest(mx) * sc;
       const float base = mx == -INFINITY ? 0.f : mx;
       float sum = 0.f;
       K16<bf16> pf[NT];
@@ -186,40 +213,32 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
         set_k16(pf[t], p[0], p[1], p[2], p[3]);
       }
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        o[d] = zero4();
+      for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int t = 0; t < NT; t += 2) o[d] = mma16x2(vf[d][t], pf[t], vf[d][t + 1], pf[t + 1], o[d]);
-      }
+        for (int t = 0; t < NT; t += 2)
+          o[d] = mma16x2(vf[d][t], pf[t], vf[d][t + 1], pf[t + 1], t ? o[d] : zero4());
       sum = groups_sum(sum);
-      const float inv = sum > 0.f ? fast_rcp(sum) : sum == 0.f ? 0.f : sum;
-      const float lse2 = sum == 0.f ? -INFINITY : base + __builtin_amdgcn_logf(sum);
-      if (!q.at[c].in()) continue;
-      bf16* to = O + q.at[c].i * a.ldo + q.at[c].g * a.D + 8 * g;
+      // (1 / 0: of weights that are all 0)
+      const float inv = sum == 0.f ? 0.f : fast_rcp(sum);
+      const bool in = v + 16 * c + r < n;
 #pragma unroll
-      for (int d = 0; d < ND; d += 2) {
-        bf16x8 y;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[i] = (bf16)(o[d][i] * inv);
-          y[i + 4] = (bf16)(o[d + 1][i] * inv);
-        }
-        if (16 * d + 8 * g < a.D) st_global16(to + 16 * d, __builtin_bit_cast(uint4, y));
+      for (int k = 0; k < NK; ++k) store_lane(b, in ? oo[c][k] : kNowhere, o[2 * k], o[2 * k + 1], inv);
+      if (a.lse && g == 0 && in) {
+        const uint32_t u = v + 16 * c + r, i = G == 1 ? u : u / (uint32_t)G;
+        const float l = base + __builtin_amdgcn_logf(sum);
+        a.lse[(int64_t)(me.h * G + (int)(u - i * G)) * a.Nq + qr.b + i] = l * kLn2;
       }
-      if (a.lse && g == 0)
-        a.lse[(int64_t)(me.h * G + q.at[c].g) * a.Nq + qr.b + q.at[c].i] = lse2 * kLn2;
     }
   };
-  int v = (int)vr.b + 16 * C * me.sub;
-  if (v >= n) return;
+  int v = 16 * C * (pc * me.subs + me.sub);
   Tile t0, t1;
   load(v, t0);
   for (;;) {  // the next tiles on their way while these are worked on
     load(v + step, t1);
-    work(t0);
+    work(v, t0);
     if ((v += step) >= n) break;
     load(v + step, t0);
-    work(t1);
+    work(v, t1);
     if ((v += step) >= n) break;
   }
 }
@@ -236,10 +255,9 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   const Role me = role_of(a.Hkv);
   const int rq = blockIdx.x / P;
   const Range qr = range_of(a.q_off, rq, a.Nq), kr = range_of(a.k_off, rq, a.Nk);
-  const Range vr = piece(Range{0, (qr.e - qr.b) * G}, blockIdx.x % P, P);
+  const int n = (int)(qr.e - qr.b) * G, pc = blockIdx.x % P;
   // (requests that are longer are the other kernels')
   if (me.h >= a.Hkv || me.sub >= me.subs || kr.e - kr.b > 16 * NT) return;
-  const int n = (int)vr.e;
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const int64_t head = (int64_t)me.h * G * a.D;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head + qr.b * a.ldq;
@@ -262,36 +280,49 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
     for (int d = 0; d < ND; ++d) dk[t][d] = dv[t][d] = zero4();
 
+  // this lane's parts of a tile of 32 rows: chunks of q and do, and of dq's rows
+  const bool even = 32 % G == 0;  // (tiles begin at a query)
+  const int last = (int)(qr.e - qr.b) - 1;
+  int qo[NCH], od[NCH], dqo[2][NK];
+  auto places = [&](int rem) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NCH; ++j) {
+      const int c = lane + 64 * j;
+      qo[j] = place(c / CPR, rem, G, a.ldq, a.D, c % CPR * 8);
+      od[j] = place(c / CPR, rem, G, a.lddo, a.D, c % CPR * 8);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int k = 0; k < NK; ++k) dqo[c][k] = place(16 * c + r, rem, G, a.lddq, a.D, 32 * k + 8 * g);
+  };
+  places(0);
   struct Tile {
     uint4 q[NCH], d[NCH];
-    Place at[2];
     float lse[2];
   } tl;
   auto load = [&](int v) __attribute__((always_inline)) {
+    const int i0 = G == 1 ? v : v / G;
+    if (!even) places(v - i0 * G);
+    const Buffer bq = rows_from(Q, a.ldq, i0, last, G * a.D), bd = rows_from(DO, a.lddo, i0, last, G * a.D);
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-      const int c = lane + 64 * j, col = (c % CPR) * 8;
-      Place at;
-      at.at(v + c / CPR, n, G);
-      const int64_t in = at.g * a.D + (col < a.D ? col : 0);
-      const uint4 x = ld_global16<true>(Q + at.i * a.ldq + in);
-      const uint4 y = ld_global16<true>(DO + at.i * a.lddo + in);
-      const bool ok = at.in() && col < a.D;
-      tl.q[j] = ok ? x : zero16();
-      tl.d[j] = ok ? y : zero16();
+      const bool in = v + (lane + 64 * j) / CPR < n;
+      tl.q[j] = load16_once(bq, in ? qo[j] : kNowhere);
+      tl.d[j] = load16_once(bd, in ? od[j] : kNowhere);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-      Place& at = tl.at[c];
-      at.at(v + 16 * c + r, n, G);
-      const float l = a.lse[(int64_t)(me.h * G + at.g) * a.Nq + qr.b + at.i] * kLog2e;
-      tl.lse[c] = !at.in() || l == -INFINITY ? INFINITY : l;  // (weights of 0)
+      const bool in = v + 16 * c + r < n;
+      const uint32_t u = in ? v + 16 * c + r : n - 1, i = G == 1 ? u : u / (uint32_t)G;
+      const float l = a.lse[(int64_t)(me.h * G + (int)(u - i * G)) * a.Nq + qr.b + i];
+      tl.lse[c] = !in || l == -INFINITY ? INFINITY : l * kLog2e;  // (weights of 0)
     }
   };
   const RowBase<bf16> rb = row_base<bf16>(r, RB);
   const int tr = tr_base<bf16>(RB), tp = tr_base<bf16>(PB), sp = r * PB + 8 * g;
-  const int step = 32 * me.subs;
-  int v = (int)vr.b + 32 * me.sub;
+  const int step = 32 * me.subs * P;  // (blocks go over the rows together)
+  int v = 32 * (pc * me.subs + me.sub);
   if (v < n) load(v);
   for (; v < n; v += step) {
 #pragma unroll
@@ -300,10 +331,12 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       *reinterpret_cast<uint4*>(qt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.q[j];
       *reinterpret_cast<uint4*>(dt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.d[j];
     }
-    const Place at[2] = {tl.at[0], tl.at[1]};
     const float lse[2] = {tl.lse[0], tl.lse[1]};
     wave_sync();
+    const int i0 = G == 1 ? v : v / G;
+    const Buffer b = rows_from(DQ, a.lddq, i0, last, G * a.D);
     if (v + step < n) load(v + step);
+    if (!even) places(v - i0 * G);
     K16<bf16> sf[2][NT];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -317,12 +350,10 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       float delta = 0.f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        x[t] = none[t];
-        dp[t] = zero4();
 #pragma unroll
         for (int k = 0; k < NK; ++k) {
-          x[t] = mma32(kf[t][k], qf[k], x[t]);
-          dp[t] = mma32(vf[t][k], of[k], dp[t]);
+          x[t] = mma32(kf[t][k], qf[k], k ? x[t] : none[t]);
+          dp[t] = mma32(vf[t][k], of[k], k ? dp[t] : zero4());
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -343,25 +374,14 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       }
       f32x4 dq[ND];
 #pragma unroll
-      for (int d = 0; d < ND; ++d) {
-        dq[d] = zero4();
+      for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int t = 0; t < NT; t += 2)
-          dq[d] = mma16x2(kc[d][t], sf[c][t], kc[d][t + 1], sf[c][t + 1], dq[d]);
-      }
-      if (at[c].in()) {
-        bf16* to = DQ + at[c].i * a.lddq + at[c].g * a.D + 8 * g;
+          dq[d] = mma16x2(kc[d][t], sf[c][t], kc[d][t + 1], sf[c][t + 1], t ? dq[d] : zero4());
+      const bool in = v + 16 * c + r < n;
 #pragma unroll
-        for (int d = 0; d < ND; d += 2) {
-          bf16x8 y;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            y[i] = (bf16)(dq[d][i] * a.scale);
-            y[i + 4] = (bf16)(dq[d + 1][i] * a.scale);
-          }
-          if (16 * d + 8 * g < a.D) st_global16(to + 16 * d, __builtin_bit_cast(uint4, y));
-        }
-      }
+      for (int k = 0; k < NK; ++k)
+        store_lane(b, in ? dqo[c][k] : kNowhere, dq[2 * k], dq[2 * k + 1], a.scale);
     }
     // acc += (p or ds, in LDS)^T (rows, in LDS)
     auto add = [&](const char* rows, f32x4(&acc)[NT][ND]) __attribute__((always_inline)) {
@@ -440,9 +460,9 @@ Split split_of(const AskArgs& a, bool bwd) {
   const int heads = a.Hkv < s.waves ? a.Hkv : s.waves;
   s.groups = (a.Hkv + heads - 1) / heads;
   s.subs = s.waves / heads;
-  // some 2048 blocks forward, one per CU backward; at least two tiles a wave
+  // some 4096 blocks forward, one per CU backward; at least two tiles a wave
   const int64_t n = a.Nq * (a.Hq / a.Hkv) / a.R, least = 64 * s.subs;
-  int64_t P = (bwd ? 256 : 2048) / ((int64_t)a.R * s.groups);
+  int64_t P = (bwd ? 256 : 4096) / ((int64_t)a.R * s.groups);
   if (P > n / least) P = n / least;
   s.P = P < 1 ? 1 : (int)P;
   return s;

@@ -70,18 +70,15 @@ k_ask(AskArgs a) {
     const char* vt = kt + Gm::TB;
     f32x4 x[QT][4];
     __builtin_amdgcn_s_setprio(1);
+    // (states that are left out begin at -infinity; their rows are zeros)
+    pipelined<4 * Gm::NK, 3, WideF<T>>(
+        [&](int i, WideF<T>& kf) { at.rows(kf, kt, i / Gm::NK, i % Gm::NK); },
+        [&](int i, const WideF<T>& kf) {
+          const int t = i / Gm::NK, k = i % Gm::NK;
+          const f32x4 from = k ? zero4() : *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      // (states that are left out begin at -infinity; their rows are zeros)
-      const f32x4 from = *reinterpret_cast<const f32x4*>(&live[16 * t + 4 * g]);
-#pragma unroll
-      for (int k = 0; k < Gm::NK; ++k) {
-        WideF<T> kf;
-        at.rows(kf, kt, t, k);
-#pragma unroll
-        for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], k ? x[c][t] : from);
-      }
-    }
+          for (int c = 0; c < QT; ++c) x[c][t] = mma(kf, qf[c][k], k ? x[c][t] : from);
+        });
     __builtin_amdgcn_s_setprio(0);
     float base[QT];
 #pragma unroll
@@ -89,11 +86,11 @@ k_ask(AskArgs a) {
       float mx = -INFINITY;
 #pragma unroll
       for (int t = 0; t < 4; ++t) mx = largest(mx, x[c][t]);
-      mx = groups_max(mx) * sc;
+      mx = groups_largest(mx) * sc;
       // The maximum moves only where a score is 2^8 above it: weights up to 2^8 are as
       // exact, and most tiles leave o and l as they are.
       if (__any(mx > m[c] + 8.f)) {
-        const float to = fmaxf(m[c], mx), down = fast_exp2(m[c] - (to == -INFINITY ? 0.f : to));
+        const float to = largest(m[c], mx), down = fast_exp2(m[c] - (to == -INFINITY ? 0.f : to));
         m[c] = to;
         l[c] *= down;
 #pragma unroll
@@ -119,14 +116,15 @@ k_ask(AskArgs a) {
           set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
         }
       __builtin_amdgcn_s_setprio(1);
+      pipelined<Gm::ND, 4, ColumnPair<T>>(
+          [&](int d, ColumnPair<T>& v) {
+            at.columns(v.a, vt, t0, d);
+            at.columns(v.b, vt, t0 + 1, d);
+          },
+          [&](int d, const ColumnPair<T>& v) {
 #pragma unroll
-      for (int d = 0; d < Gm::ND; ++d) {
-        K16<T> v0f, v1f;
-        at.columns(v0f, vt, t0, d);
-        at.columns(v1f, vt, t0 + 1, d);
-#pragma unroll
-        for (int c = 0; c < QT; ++c) o[c][d] = mma16x2(v0f, pf[c][0], v1f, pf[c][1], o[c][d]);
-      }
+            for (int c = 0; c < QT; ++c) o[c][d] = mma16x2(v.a, pf[c][0], v.b, pf[c][1], o[c][d]);
+          });
       __builtin_amdgcn_s_setprio(0);
     }
   };
