@@ -27,6 +27,8 @@ LN2(x1) (bf16; fp32 storage keeps u).
 MLP's products in 8-bit integers (ops.pa_linear_i8).  ``SandwichStack`` has a
 norm after each half of a block as well, and learned residual scales.  A
 training step is ``forward``, ``backward`` and a step of ``adamw``'s optimizer.
+``QueryDecoder`` answers at points of its own from the states (or points) that an
+encoder left, for many requests at once.
 
 Parameters per layer (dict of device tensors): fp32 ln1_g, ln1_b, Wp [C,C],
 bp [C], A [C,M], b [M], a [C], Wq, bq, Wk, bk, Wv, bv (optional Wo, bo),
@@ -438,4 +440,186 @@ class SandwichStack(BlockStack):
             last = l + 1 == len(self.params)
             x = self._e(N, C)
             ops.pa_residual_norm(x1, z, self._joint(l, 2), x, None if last else h)
+        return x
+
+
+class QueryDecoder(BlockStack):
+    """Blocks that answer at query points from an encoder's states (a block stack's
+    points or slices' states, of any number and width), for one request or many:
+
+        x1 = x + drop(Ask(LN1(x), s) Wo + bo),    x2 = x1 + drop(MLP(LN2(x1)))
+
+    where Ask is ops.pa_cross_attention of q = h Wq + bq over k, v = s Wkv + bkv (side
+    by side in the rows of one product) and drop is ops.pa_dropout with the residual
+    add.  N query points of C channels in all, H query heads, Hkv heads of k and v
+    (default: H), each C / H wide; drop: the probability that training drops an element
+    with, seed: of its numbers.
+
+    Parameters per layer: ln1_g, ln1_b, bq [C], bkv [2 Hkv C / H], bo, ln2_g, ln2_b, b1
+    [4C], b2 fp32; Wq [C,C], Wkv [Cs, 2 Hkv C / H], Wo [C,C], W1 [C,4C], W2 [4C,C] in the
+    storage dtype (Cs: the states' width)."""
+
+    def __init__(self, N, C, H, params, dtype, Hkv=None, drop=0.0, seed=0, ln_eps=1e-5,
+                 device="cuda"):
+        import torch
+        self.torch = torch
+        Hkv = H if Hkv is None else Hkv
+        if C % H or H % Hkv:
+            raise ValueError("H must divide C, and Hkv H")
+        self.N, self.C, self.H, self.Hkv, self.D = N, C, H, Hkv, C // H
+        self.params, self.dt, self.ln_eps, self.dev = params, dtype, ln_eps, device
+        self.pdt = B.PA_BF16 if dtype == torch.bfloat16 else B.PA_F32
+        self.drop, self.seed = drop, seed
+        self.ws_rows = torch.empty(1024 * 4 * C, dtype=torch.float32, device=device)
+        self.ws_gemm = torch.empty(256 << 20, dtype=torch.uint8, device=device)
+        self.tuned = set()
+        self.fused_mlp = self.pdt == B.PA_BF16 and C in (64, 128, 256)
+        self.ws_int8 = self.int8 = self.int8_of = None
+        self.steps = 0
+        self.one = ops.make_cross_attention(H, Hkv, self.D)
+
+    def requests(self, q_off, k_off, mask=None, max_k=0):
+        """Which query points ask which states (ops.make_cross_attention)."""
+        return ops.make_cross_attention(self.H, self.Hkv, self.D, q_off=q_off, k_off=k_off,
+                                        mask=mask, max_k=max_k)
+
+    def _kv(self, p, s):
+        kv = self._e(s.shape[0], 2, self.Hkv, self.D)
+        if s.shape[0]:
+            self._gemm(s, p["Wkv"], kv.view(s.shape[0], -1), bias=p["bkv"])
+        return kv
+
+    def _ask(self, p, c, h, kv, par, lse=False):
+        """Ask(h) Wo + bo; c receives what the backward needs."""
+        N, H, D = self.N, self.H, self.D
+        q, o = self._e(N, self.C), self._e(N, H, D)
+        self._gemm(h, p["Wq"], q, bias=p["bq"])
+        l = self._f(H, N) if lse else None
+        ws = ops.cross_attention_workspace(par, N, kv.shape[0], self.dt, device=self.dev)
+        if par.tensors["q_off"] is not None:
+            o.zero_()  # (a point of no request asks nothing)
+            if lse:
+                l.zero_()
+        ops.pa_cross_attention(q.view(N, H, D), kv[:, 0], kv[:, 1], par, o, l, ws)
+        y = self._e(N, self.C)
+        self._gemm(o.view(N, -1), p["Wo"], y, bias=p["bo"])
+        c.update({"q": q, "kv": kv, "o": o, "lse": l})
+        return y
+
+    def _ask_backward(self, p, c, g, s, par, dy, ds, first):
+        """The gradient of h from that of Ask(h) Wo + bo; the states' goes into ds (added,
+        but for the first)."""
+        N, C, H, D = self.N, self.C, self.H, self.D
+        do, dq = self._e(N, C), self._e(N, C)
+        o, kv = c["o"], c["kv"]
+        Ns, F = kv.shape[0], 2 * self.Hkv * D
+        g["dWo"], g["dbo"] = self._f(C, C), self._f(C)
+        self._gemm(o.view(N, C), dy, g["dWo"], transA=True)
+        B.pa_colsum(dy, g["dbo"], self.ws_rows)
+        self._gemm(dy, p["Wo"], do, transB=True)
+        dkv = self._e(Ns, 2, self.Hkv, D)
+        if par.tensors["q_off"] is not None:
+            dq.zero_()
+            dkv.zero_()
+        ws = ops.cross_attention_workspace(par, N, Ns, self.dt, True, self.dev)
+        v3 = lambda t: t.view(N, H, D)
+        ops.pa_cross_attention_backward(v3(c["q"]), kv[:, 0], kv[:, 1], o, c["lse"], par, v3(do),
+                                        v3(dq), dkv[:, 0], dkv[:, 1], ws)
+        g["dWq"], g["dbq"] = self._f(C, C), self._f(C)
+        self._gemm(c["h"], dq, g["dWq"], transA=True)
+        B.pa_colsum(dq, g["dbq"], self.ws_rows)
+        dh = do
+        self._gemm(dq, p["Wq"], dh, transB=True)
+        g["dWkv"], g["dbkv"] = self._f(s.shape[1], F), self._f(F)
+        if Ns:
+            dkv = dkv.view(Ns, F)
+            self._gemm(s, dkv, g["dWkv"], transA=True)
+            B.pa_colsum(dkv, g["dbkv"], self.ws_rows)
+            self._gemm(dkv, p["Wkv"], ds, transB=True, beta=0.0 if first else 1.0)
+        else:
+            g["dWkv"].zero_()
+            g["dbkv"].zero_()
+        return dh
+
+    def _add(self, y, x, l, k):
+        """x + drop(y), the k-th of layer l."""
+        out, (at, dev) = self._e(self.N, self.C), self.at
+        ops.pa_dropout(y, out, self.drop, self.seed, at + 2 * l + k, r=x, offset_dev=dev)
+        return out
+
+    def _drop_grad(self, dy, l, k):
+        if not self.drop:
+            return dy
+        out, (at, dev) = self._e(self.N, self.C), self.at
+        ops.pa_dropout(dy, out, self.drop, self.seed, at + 2 * l + k, offset_dev=dev)
+        return out
+
+    def forward(self, x, s, par=None, step=0, offset_dev=None):
+        """x [N,C], s [Ns,Cs]: the answers [N,C]; par: which points ask which states
+        (``requests``; None: all of them all).  step: of the training, names the dropped
+        elements.  Those of a captured graph, whose step stands still, are named by
+        offset_dev, a device int64 [1] that counts 2 x layers a step (its own numbers follow
+        step's: 0 there).  Keeps what the backward needs."""
+        N, C = self.N, self.C
+        par = self.one if par is None else par
+        self.caches, self.states, self.par = [], s, par
+        self.at = (2 * len(self.params) * step, offset_dev)
+        for l, p in enumerate(self.params):
+            h, m1, r1 = self._e(N, C), self._f(N), self._f(N)
+            c = {"x": x, "h": h, "m1": m1, "r1": r1}
+            B.pa_layernorm(x, h, m1, r1, g=p["ln1_g"], b=p["ln1_b"], eps=self.ln_eps)
+            y = self._ask(p, c, h, self._kv(p, s), par, lse=True)
+            h2, m2, r2 = self._e(N, C), self._f(N), self._f(N)
+            if self.drop:
+                x1 = self._add(y, x, l, 0)
+                B.pa_layernorm(x1, h2, m2, r2, g=p["ln2_g"], b=p["ln2_b"], eps=self.ln_eps)
+                x = self._add(self._mlp(p, c, h2), x1, l, 1)
+            else:
+                x1 = self._e(N, C)
+                B.pa_layernorm(x, h2, m2, r2, g=p["ln2_g"], b=p["ln2_b"], r=y, xs=x1,
+                               eps=self.ln_eps)
+                x = self._mlp(p, c, h2, x1)
+            c.update({"x1": x1, "m2": m2, "r2": r2})
+            self.caches.append(c)
+        return x
+
+    def backward(self, dy):
+        """From the gradient of the answers: (dx, the states' gradient, [gradients per
+        layer])."""
+        N, C = self.N, self.C
+        s, par, L = self.states, self.par, len(self.params)
+        grads, ds = [None] * L, self._e(*s.shape)
+        for l in reversed(range(L)):
+            p, c, g = self.params[l], self.caches[l], {}
+            dh2 = self._mlp_backward(p, c, g, self._drop_grad(dy, l, 1))
+            dx1 = self._e(N, C)
+            g["dln2_g"], g["dln2_b"] = self._f(C), self._f(C)
+            B.pa_layernorm_backward(c["x1"], c["m2"], c["r2"], dh2, dx1, g=p["ln2_g"], dres=dy,
+                                    dg=g["dln2_g"], db=g["dln2_b"], ws=self.ws_rows)
+            dh = self._ask_backward(p, c, g, s, par, self._drop_grad(dx1, l, 0), ds, l == L - 1)
+            dx = self._e(N, C)
+            g["dln1_g"], g["dln1_b"] = self._f(C), self._f(C)
+            B.pa_layernorm_backward(c["x"], c["m1"], c["r1"], dh, dx, g=p["ln1_g"], dres=dx1,
+                                    dg=g["dln1_g"], db=g["dln1_b"], ws=self.ws_rows)
+            grads[l], dy = g, dx
+        return dy, ds, grads
+
+    def keep(self, s):
+        """k and v of every layer for states that many calls of ``infer`` ask."""
+        return [self._kv(p, s) for p in self.params]
+
+    def infer(self, x, s=None, par=None, kept=None):
+        """``forward`` without dropout, nothing kept for a backward; of the states s, or of
+        what ``keep`` made of them; after ``quantize`` with the MLP in 8-bit integers."""
+        self._ready()
+        N, C = self.N, self.C
+        par = self.one if par is None else par
+        m, r = self._f(N), self._f(N)
+        for l, p in enumerate(self.params):
+            h = self._e(N, C)
+            B.pa_layernorm(x, h, m, r, g=p["ln1_g"], b=p["ln1_b"], eps=self.ln_eps)
+            y = self._ask(p, {}, h, self._kv(p, s) if kept is None else kept[l], par)
+            x1, h2 = self._e(N, C), h
+            B.pa_layernorm(x, h2, m, r, g=p["ln2_g"], b=p["ln2_b"], r=y, xs=x1, eps=self.ln_eps)
+            x = self._mlp_infer(l, h2, x1)
         return x
