@@ -708,41 +708,37 @@ def make_cross_attention(Hq, Hkv, D, scale=None, q_off=None, k_off=None, mask=No
     return CrossAttention(st, {"q_off": q_off, "k_off": k_off, "mask": mask})
 
 
-def _rows(t, N, H, D, dtype, name, cur):
-    """(pointer, elements between rows) of a tensor of N rows of H heads of D, [N, H, D]
+def _rows(t, want, dtype, name, cur):
+    """(pointer, elements between rows) of a tensor of rows of heads, [N, H, D] as wanted
     or [N, H D], whose rows may be further apart than they are long."""
+    st = t.stride()
+    if t.shape == want and st[1] == want[2] and st[2] == 1 and t.dtype is dtype \
+            and t.get_device() == cur:
+        return t.data_ptr(), st[0]
+    N, H, D = want  # (the same once more, for what to say, and rows of one head or row)
     if t.get_device() != cur:
         B._ptr(t)
         raise ValueError(f"{name}: on {t.device}, not on the current device")
     if t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, the call needs {dtype}")
-    shape = t.shape
-    if len(shape) == 3:
-        ok = shape[0] == N and shape[1] == H and shape[2] == D
-        s0, s1, s2 = t.stride()
-        whole = (s2 == 1 or D == 1) and (s1 == D or H == 1)
-    elif len(shape) == 2:
-        ok = shape[0] == N and shape[1] == H * D
-        s0, s2 = t.stride()
-        whole = s2 == 1
-    else:
-        ok = False
-    if not ok:
-        raise ValueError(f"{name}: {list(shape)}, the call needs {[N, H, D]}")
-    if N and not whole:
+    if tuple(t.shape) not in ((N, H, D), (N, H * D)):
+        raise ValueError(f"{name}: {list(t.shape)}, the call needs {[N, H, D]}")
+    if N and (st[-1] != 1 or len(st) == 3 and st[1] != D and H > 1):
         raise ValueError(f"{name}: the elements of a row have to lie one behind the other")
-    return t.data_ptr(), s0
+    return t.data_ptr(), st[0]
 
 
 def _asked(q, k, par, cur):
-    """The sizes of a call."""
-    _here(par.device, "the parameters", cur)
-    if q.dim() not in (2, 3) or k.dim() not in (2, 3):
+    """What a call's tensors have to be: the query side's, the states', and their type."""
+    if par.device is not None:
+        _here(par.device, "the parameters", cur)
+    qs, ks = q.shape, k.shape
+    if len(qs) not in (2, 3) or len(ks) not in (2, 3):
         raise ValueError("q must be [Nq, Hq, D] and k [Nk, Hkv, D]")
-    Nq, Nk = q.shape[0], k.shape[0]
-    if par.mask is not None and par.mask.numel() != Nk:
-        raise ValueError(f"mask: {par.mask.numel()} elements, the call needs {Nk}")
-    return Nq, Nk, q.dtype, _code(q.dtype, "q")
+    if par.mask is not None and par.mask.numel() != ks[0]:
+        raise ValueError(f"mask: {par.mask.numel()} elements, the call needs {ks[0]}")
+    dt = q.dtype
+    return (qs[0], par.Hq, par.D), (ks[0], par.Hkv, par.D), dt, _code(dt, "q")
 
 
 def cross_attention_workspace(par, Nq, Nk, dtype, backward=False, device="cuda"):
@@ -757,14 +753,17 @@ def pa_cross_attention(q, k, v, par, o, lse=None, ws=None, stream=None):
     """o [Nq, Hq, D] (and lse [Hq, Nq] fp32): every row of q over the rows of k and v of
     its request (make_cross_attention); ws as cross_attention_workspace gives it."""
     cur = _current_device()
-    Nq, Nk, dt, code = _asked(q, k, par, cur)
-    Hq, Hkv, D = par.Hq, par.Hkv, par.D
+    qs, ks, dt, code = _asked(q, k, par, cur)
     _check(load().pa_cross_attention(
-        Nq, Nk, code, par.ref, *_rows(q, Nq, Hq, D, dt, "q", cur),
-        *_rows(k, Nk, Hkv, D, dt, "k", cur), *_rows(v, Nk, Hkv, D, dt, "v", cur),
-        *_rows(o, Nq, Hq, D, dt, "o", cur),
-        _in(lse, Nq * Hq, _torch().float32, "lse", False, cur),
-        None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))
+        qs[0], ks[0], code, par.ref, *_rows(q, qs, dt, "q", cur), *_rows(k, ks, dt, "k", cur),
+        *_rows(v, ks, dt, "v", cur), *_rows(o, qs, dt, "o", cur),
+        None if lse is None else _in(lse, qs[0] * qs[1], _torch().float32, "lse", False, cur),
+        *_room(ws, cur), B._stream(stream)))
+
+
+def _room(ws, cur):
+    """(pointer, bytes) of a workspace."""
+    return (None, 0) if ws is None else (_dev(ws, "ws", cur), ws.nbytes)
 
 
 def pa_cross_attention_backward(q, k, v, o, lse, par, d_o, dq, dk=None, dv=None, ws=None,
@@ -772,19 +771,17 @@ def pa_cross_attention_backward(q, k, v, o, lse, par, d_o, dq, dk=None, dv=None,
     """dq and, where given, dk and dv from the forward's o and lse and the gradient d_o
     of o; ws as cross_attention_workspace(..., backward=True) gives it."""
     cur = _current_device()
-    Nq, Nk, dt, code = _asked(q, k, par, cur)
-    Hq, Hkv, D = par.Hq, par.Hkv, par.D
+    qs, ks, dt, code = _asked(q, k, par, cur)
     if (dk is None) != (dv is None):
         raise ValueError("dk and dv go together")
-    none = (None, 0)
     _check(load().pa_cross_attention_backward(
-        Nq, Nk, code, par.ref, *_rows(q, Nq, Hq, D, dt, "q", cur),
-        *_rows(k, Nk, Hkv, D, dt, "k", cur), *_rows(v, Nk, Hkv, D, dt, "v", cur),
-        *_rows(o, Nq, Hq, D, dt, "o", cur), _in(lse, Nq * Hq, _torch().float32, "lse", True, cur),
-        *_rows(d_o, Nq, Hq, D, dt, "d_o", cur), *_rows(dq, Nq, Hq, D, dt, "dq", cur),
-        *(none if dk is None else _rows(dk, Nk, Hkv, D, dt, "dk", cur)),
-        *(none if dv is None else _rows(dv, Nk, Hkv, D, dt, "dv", cur)),
-        None if ws is None else _dev(ws, "ws", cur), B._nbytes(ws), B._stream(stream)))
+        qs[0], ks[0], code, par.ref, *_rows(q, qs, dt, "q", cur), *_rows(k, ks, dt, "k", cur),
+        *_rows(v, ks, dt, "v", cur), *_rows(o, qs, dt, "o", cur),
+        _in(lse, qs[0] * qs[1], _torch().float32, "lse", True, cur),
+        *_rows(d_o, qs, dt, "d_o", cur), *_rows(dq, qs, dt, "dq", cur),
+        *((None, 0) if dk is None else _rows(dk, ks, dt, "dk", cur)),
+        *((None, 0) if dv is None else _rows(dv, ks, dt, "dv", cur)),
+        *_room(ws, cur), B._stream(stream)))
 
 
 # ---- dropout ----
