@@ -364,6 +364,19 @@ template <typename T> __device__ __forceinline__ void store4(T* p, const f32x4& 
   }
 }
 
+// Sums over pieces by a block of 256: U groups of threads take every U-th piece and are
+// added in a tree (so in the same order every time).  v: this thread's; the first group's
+// threads, of P each, get the totals.
+template <typename V> __device__ __forceinline__ V add_groups(V v, V* lds, int u, int U, int at, int P) {
+  for (int half = U >> 1; half > 0; half >>= 1) {
+    __syncthreads();
+    if (u >= half && u < 2 * half) lds[(u - half) * P + at] = v;
+    __syncthreads();
+    if (u < half) v += lds[u * P + at];
+  }
+  return v;
+}
+
 // f(type, std::integral_constant of the width rounded up): fp32 is padded to multiples
 // of 16, bf16, whose steps are 32 wide, too (the tiles of its results are 16 wide).
 template <typename F> hipError_t by_width(int D, int dtype, F f) {

@@ -177,24 +177,33 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   }
 }
 
-// dq's pieces joined: a thread has four elements of a head of a row.
-template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a) {
+// dq's pieces joined, as k_ask_join.
+template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a, int rows_, int U) {
   constexpr bool FIX = sizeof(T) == 2;
-  const int per = a.D / 4;
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.Nq * a.Hq;
-  const int64_t at = t / per;
-  const int c = (int)(t - at * per) * 4;
-  if (at >= rows) return;
-  const int64_t row = at / a.Hq;
-  const int hq = (int)(at - row * a.Hq);
-  if (a.q_off && (row < a.q_off[0] || row >= a.q_off[a.R])) return;
+  __shared__ f32x4 lds[256];
+  __shared__ float ldse[256];
+  const int per = a.D / 4, item = threadIdx.x / (per * U), in = threadIdx.x % (per * U);
+  const int u = item < rows_ ? in / per : U, c = (in % per) * 4;  // (U: a thread too many)
+  const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * rows_ + item;
+  const bool on = item < rows_ && at < rows;
+  const int64_t row = on ? at / a.Hq : 0, first = a.q_off ? a.q_off[0] : 0;
+  const int64_t behind = a.q_off ? a.q_off[a.R] : a.Nq;
+  const bool write = on && row >= first && row < behind;
   float e = 0.f;
   f32x4 A = zero4(), B = zero4();
-  for (int s = 0; s < a.S; ++s) {
-    e += a.part_lse[s * rows + at];
-    A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
-    if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+  if (write)
+    for (int s = u; s < a.S; s += U) {
+      e += a.part_lse[s * rows + at];
+      A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
+      if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+    }
+  if (U > 1) {
+    A = add_groups(A, lds, u, U, in % per, per);
+    if constexpr (FIX) B = add_groups(B, lds, u, U, in % per, per);
+    e = add_groups(e, ldse, u, U, in % per, per);
   }
+  if (!write || u) return;
+  const int hq = (int)(at - row * a.Hq);
   if constexpr (FIX) A -= B * e;
   store4<T>(reinterpret_cast<T*>(a.dq) + row * a.lddq + (int64_t)hq * a.D + c, A * a.scale);
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
@@ -342,17 +351,21 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   }
 }
 
-// The records of the queries' pieces added in order.
-template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskArgs a) {
+// The records of the queries' pieces added, by U groups of 256 / U threads.
+template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskArgs a, int U) {
+  __shared__ f32x4 lds[256];
+  const int P = 256 / U, u = threadIdx.x / P, x = threadIdx.x % P;
   const int64_t width = (int64_t)a.Hkv * a.D, all = a.Nk * width;
-  const int64_t t = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (t >= all) return;
+  const int64_t t = ((int64_t)blockIdx.x * P + x) * 4;
+  const float* part = blockIdx.y ? a.part_v : a.part_k;
+  f32x4 sum = zero4();
+  if (t < all)
+    for (int s = u; s < a.SQ; s += U) sum += *reinterpret_cast<const f32x4*>(part + s * all + t);
+  if (U > 1) sum = add_groups(sum, lds, u, U, x, P);
+  if (u || t >= all) return;
   const int64_t row = t / width;
   const int c = (int)(t - row * width);
   if (a.k_off && (row < a.k_off[0] || row >= a.k_off[a.R])) return;
-  const float* part = blockIdx.y ? a.part_v : a.part_k;
-  f32x4 sum = zero4();
-  for (int s = 0; s < a.SQ; ++s) sum += *reinterpret_cast<const f32x4*>(part + s * all + t);
   T* to = reinterpret_cast<T*>(blockIdx.y ? a.dv : a.dk) + row * (blockIdx.y ? a.lddv : a.lddk) + c;
   store4<T>(to, sum);
 }
@@ -391,10 +404,10 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     });
     if (e != hipSuccess) return e;
     if (a.S > 1) {
-      const int64_t threads = a.Nq * a.Hq * (a.D / 4);
-      const dim3 grid((uint32_t)((threads + 255) / 256));
-      if (dtype == 1) hipLaunchKernelGGL(k_ask_dq_join<bf16>, grid, dim3(256), 0, st, a);
-      else hipLaunchKernelGGL(k_ask_dq_join<float>, grid, dim3(256), 0, st, a);
+      const AskJoin j = ask_join(a);
+      const dim3 grid((uint32_t)((a.Nq * a.Hq + j.rows - 1) / j.rows));
+      if (dtype == 1) hipLaunchKernelGGL(k_ask_dq_join<bf16>, grid, dim3(256), 0, st, a, j.rows, j.U);
+      else hipLaunchKernelGGL(k_ask_dq_join<float>, grid, dim3(256), 0, st, a, j.rows, j.U);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -408,10 +421,11 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     return launch_dkv<T, DP, 1, 4>(a, st);
   });
   if (e != hipSuccess || a.SQ == 1) return e;
-  const int64_t threads = a.Nk * a.Hkv * a.D / 4;
-  const dim3 grid((uint32_t)((threads + 255) / 256), 2);
-  if (dtype == 1) hipLaunchKernelGGL(k_ask_dkv_sum<bf16>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(k_ask_dkv_sum<float>, grid, dim3(256), 0, st, a);
+  const int U = a.SQ <= 8 ? 1 : a.SQ <= 64 ? 8 : 32;
+  const int64_t quads = a.Nk * a.Hkv * a.D / 4;
+  const dim3 grid((uint32_t)((quads + 256 / U - 1) / (256 / U)), 2);
+  if (dtype == 1) hipLaunchKernelGGL(k_ask_dkv_sum<bf16>, grid, dim3(256), 0, st, a, U);
+  else hipLaunchKernelGGL(k_ask_dkv_sum<float>, grid, dim3(256), 0, st, a, U);
   return hipGetLastError();
 }
 
