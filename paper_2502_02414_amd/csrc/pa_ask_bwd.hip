@@ -387,7 +387,9 @@ template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs
 int rows_dq(const AskArgs& a, int dtype) { return !ask_large(a, dtype) ? 64 : a.D <= 64 ? 256 : 128; }
 int rows_dkv(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  const bool large = dtype == 1 && a.Nk / a.R >= 256 && rows / a.R >= 256;
+  const int64_t each = a.Nk / a.R;
+  const bool large = dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && rows / a.R >= 128 &&
+                     (a.Nk + 255) / 256 * a.Hkv * (rows / a.R / kTile) >= (a.D <= 64 ? 4096 : 2048);
   return !large ? 64 : a.D <= 64 ? 256 : 128;
 }
 
@@ -431,18 +433,22 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
 
 }  // namespace
 
-// Pieces of the states in dq's pass, and of the queries in dk and dv's: with fewer blocks
-// of all of them than the chip holds.
+// Pieces of the states in dq's pass (four products, three in fp32), and of the queries in
+// dk and dv's (four).
 int ask_pieces_dq(const AskArgs& a, int dtype) {
-  const int rows = rows_dq(a, dtype);
-  return ask_pieces_of((a.Nq * (a.Hq / a.Hkv) / rows + a.R) * a.Hkv,
-                       rows > 64 ? 1 : std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
+  const int rows = rows_dq(a, dtype), tiles_of = rows == 256 ? 2 : 1;
+  const double cycles = 600 + (dtype == 1 ? 2.0 * 4 : 32.0 * 3) * a.D;
+  return ask_pieces_of((a.Nq * (a.Hq / a.Hkv) / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
+                       ask_resident(a, dtype, rows > 64), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
+                       (dtype == 1 ? 8.0 : 4.0) * a.Nq * a.Hq * (a.D + 1));
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {
-  const int rows = rows_dkv(a, dtype);
-  return ask_pieces_of((a.Nk / rows + a.R) * a.Hkv,
-                       rows > 64 ? 1 : std::min(4, ask_lds_blocks(a, dtype)),
-                       a.Nq * (a.Hq / a.Hkv) / a.R);
+  const int rows = rows_dkv(a, dtype), tiles_of = rows == 256 ? 2 : 1;
+  const double cycles = 600 + (dtype == 1 ? 2.0 : 32.0) * 4 * a.D;
+  return ask_pieces_of((a.Nk / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
+                       ask_resident(a, dtype, rows > 64), tiles_of * cycles,
+                       (a.Nq * (a.Hq / a.Hkv) / a.R + kTile - 1) / kTile,
+                       8.0 * a.Nk * a.Hkv * a.D);
 }
 
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st) {

@@ -231,30 +231,45 @@ hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
 
 // Blocks of eight waves with two tiles of 16 queries each (bf16) in place of four with one:
 // a tile of states is read by them a quarter as often, from LDS half as often, where
-// requests are long enough to fill them and the chip.
+// requests fill most of them and there is work for the chip (in pieces).
 bool ask_large(const AskArgs& a, int dtype) {
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  return dtype == 1 && rows / a.R >= 256 && rows / 256 * a.Hkv >= 128 && a.Nk / a.R >= 128;
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = rows / a.R, tiles = a.Nk / a.R / kTile;
+  return dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && tiles >= 2 &&
+         (rows + 255) / 256 * a.Hkv * tiles >= (a.D <= 64 ? 4096 : 2048);
 }
-// Blocks of whole requests, and of how many of them a CU has room for, to the pieces that
-// fill the chip: at least two tiles each.
-int ask_pieces_of(int64_t blocks, int resident, int64_t rows) {
-  const int64_t tiles = (rows + kTile - 1) / kTile;
-  int64_t S = (256 * resident + blocks / 2) / blocks;
-  if (S > tiles / 2) S = tiles / 2;
-  return (int)(S < 1 ? 1 : S > 256 ? 256 : S);
+
+// The number of pieces whose time comes out shortest: blocks of `waves` that take `cycles`
+// for each of `tiles` tiles.  n waves of a SIMD share it, up to `resident`, in n + 1 times
+// one's cycles (none is faster than 2000); a block's start is 6000; several pieces are joined,
+// `bytes` each at 1.5 KB a cycle, by a launch of 6000.
+int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
+                  double bytes) {
+  int best = 1;
+  double least = 0;
+  for (int S = 1; S <= 256 && S <= (tiles > 1 ? tiles : 1); S *= 2) {
+    const double n = (double)blocks * S * waves / 1024, rounds = std::max(1.0, n / resident);
+    const double tile = std::max(2000.0, cycles * (std::min(n, (double)resident) + 1));
+    const double t = rounds * (6000 + (double)((tiles + S - 1) / S) * tile) +
+                     (S > 1 ? 6000 + S * bytes / 1500 : 0);
+    if (S == 1 || t < least) {
+      best = S;
+      least = t;
+    }
+  }
+  return best;
 }
-// Blocks of the kernels that LDS has room for in a CU: two tiles of two tensors each.
-int ask_lds_blocks(const AskArgs& a, int dtype) {
-  const int bytes = a.D * (dtype == 1 ? 2 : 4);
-  return bytes <= 64 ? 9 : bytes <= 128 ? 4 : bytes <= 256 ? 2 : 1;
+// Waves of a SIMD that the kernels' registers and LDS leave room for.
+int ask_resident(const AskArgs& a, int dtype, bool large_backward) {
+  if (dtype == 0) return a.D <= 32 ? 4 : a.D <= 64 ? 2 : 1;
+  return a.D <= 64 && !large_backward ? 4 : 2;
 }
-// Pieces of the states: with fewer blocks of whole ones than the chip holds.
 int ask_pieces(const AskArgs& a, int dtype) {
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), tiles = (a.Nk / a.R + kTile - 1) / kTile;
   const bool large = ask_large(a, dtype);
-  return ask_pieces_of((rows / (large ? 256 : 64) + a.R) * a.Hkv,
-                       large ? (a.D <= 64 ? 2 : 1) : std::min(4, ask_lds_blocks(a, dtype)), a.Nk / a.R);
+  const double cycles = 450 + (dtype == 1 ? 2.0 : 32.0) * 2 * a.D;  // softmax, two products
+  return ask_pieces_of((rows / (large ? 256 : 64) + a.R) * a.Hkv, large ? 8 : 4,
+                       ask_resident(a, dtype, false), large ? 2 * cycles : cycles, tiles,
+                       4.0 * a.Nq * a.Hq * (a.D + 1));
 }
 
 // Eight pieces or fewer one after the other, many rows to a block; more by groups of

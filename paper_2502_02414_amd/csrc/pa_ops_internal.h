@@ -135,8 +135,9 @@ struct AskArgs {
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
 bool ask_large(const AskArgs& a, int dtype);  // blocks of many queries
-int ask_pieces_of(int64_t blocks, int resident, int64_t rows);
-int ask_lds_blocks(const AskArgs& a, int dtype);
+int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
+                  double bytes);
+int ask_resident(const AskArgs& a, int dtype, bool large_backward);
 int ask_pieces(const AskArgs& a, int dtype);     // S, forward
 int ask_pieces_dq(const AskArgs& a, int dtype);  // S, backward
 int ask_pieces_q(const AskArgs& a, int dtype);   // SQ
