@@ -382,15 +382,19 @@ template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs
                      0, st, a);
   return hipGetLastError();
 }
-// Blocks of eight waves in dq's pass, as ask_large, and of as many states in dk and dv's;
-// with two tiles of 16 a wave up to 64 wide (wider ones have no registers for two).
-int rows_dq(const AskArgs& a, int dtype) { return !ask_large(a, dtype) ? 64 : a.D <= 64 ? 256 : 128; }
+// Rows of a block.  Blocks of eight waves in dq's pass, as ask_large, and of as many states
+// in dk and dv's, with two tiles of 16 a wave up to 64 wide (wider ones have no registers
+// for two); up to 32 wide small blocks, of which more are resident, are as fast or faster
+// (us, small and large: 2,080 queries of 8 heads over 17,906 states 259 and 331 to 385,
+// 8,192 over 8,192 480 and 451; 64 wide and 4 heads 387 and 327).
+int rows_dq(const AskArgs& a, int dtype) {
+  return a.D <= 32 || !ask_large(a, dtype) ? 64 : a.D <= 64 ? 256 : 128;
+}
 int rows_dkv(const AskArgs& a, int dtype) {
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv);
-  const int64_t each = a.Nk / a.R;
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = a.Nk / a.R;
   const bool large = dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && rows / a.R >= 128 &&
                      (a.Nk + 255) / 256 * a.Hkv * (rows / a.R / kTile) >= (a.D <= 64 ? 4096 : 2048);
-  return !large ? 64 : a.D <= 64 ? 256 : 128;
+  return a.D <= 32 || !large ? 64 : a.D <= 64 ? 256 : 128;
 }
 
 hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
@@ -400,7 +404,7 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     e = by_width(a.D, dtype, [&](auto type, auto dp) {
       using T = decltype(type);
       constexpr int DP = decltype(dp)::value;
-      if constexpr (sizeof(T) == 2)
+      if constexpr (sizeof(T) == 2 && DP > 32)
         if (large) return launch_dq<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
       return launch_dq<T, DP, 1, 4>(a, st);
     });
@@ -418,7 +422,7 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
   e = by_width(a.D, dtype, [&](auto type, auto dp) {
     using T = decltype(type);
     constexpr int DP = decltype(dp)::value;
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2 && DP > 32)
       if (large) return launch_dkv<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
     return launch_dkv<T, DP, 1, 4>(a, st);
   });
