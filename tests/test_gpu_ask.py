@@ -392,3 +392,48 @@ def test_in_a_graph(case):
         torch.cuda.synchronize()
         assert torch.equal(o, eo) and torch.equal(lse, el), rep
         assert all(torch.equal(a, b) for a, b in zip(g, eg)), rep
+
+
+HEADS = [
+    # heads that do not fill a block's waves, more of them than it has, groups that do not
+    # divide a tile's rows; few states (a wave's registers) and more
+    ((50, 7), (30, 11), 3, 3, 32), ((70,), (20,), 10, 10, 64), ((41,), (60,), 20, 5, 16),
+    ((33, 90), (64, 5), 12, 12, 32), ((45,), (33,), 48, 1, 32), ((9,), (64,), 70, 1, 64),
+    ((20,), (17,), 12, 4, 48), ((40,), (200,), 48, 1, 64), ((13, 5), (100, 90), 66, 2, 40),
+    ((300,), (130,), 9, 3, 96), ((257,), (48,), 5, 5, 8),
+]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ql,kl,Hq,Hkv,D", HEADS)
+def test_heads(dt, ql, kl, Hq, Hkv, D):
+    say(f"cross attention heads {dt} {ql} {kl} {Hq}/{Hkv} {D}")
+    c = Case(ql, kl, Hq, Hkv, D, DT[dt], "some")
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("dt,ql,kl,Hq,Hkv,D,mask", [
+    ("bf16", (2050,), (8192,), 4, 4, 64, "some"),        # large blocks, two tiles a wave
+    ("bf16", (4090,), (2110,), 4, 2, 128, None),         # large blocks of wide heads
+    ("bf16", (1030, 2000, 1), (4100, 3000, 700), 4, 4, 48, "some"),
+    ("bf16", (3000,), (4097,), 4, 4, 32, None),
+    ("bf16", (5000,), (300,), 8, 4, 96, "some"),
+    ("f32", (1500,), (1700,), 2, 1, 64, "some"),
+    ("bf16", (20000, 3), (50, 64), 2, 2, 32, "some"),    # few states, many blocks
+    ("bf16", (70, 9000), (10, 30), 4, 1, 64, None),
+])
+def test_larger_ones(dt, ql, kl, Hq, Hkv, D, mask):
+    say(f"cross attention {dt} {ql} {kl} {Hq}/{Hkv} {D}")
+    c = Case(ql, kl, Hq, Hkv, D, DT[dt], mask, "fused")
+    c.check_forward()
+    c.check_backward()
+
+
+def test_one_request_has_most_of_the_rows():
+    """Lengths from nothing to thousands: what a mean of them would choose is not right."""
+    ql, kl = (0, 4000, 1, 3, 0, 2), (2, 1, 3000, 64, 5, 0)
+    for dt in (F32, BF16):
+        c = Case(ql, kl, 2, 2, 64, dt)
+        c.check_forward()
+        c.check_backward()
