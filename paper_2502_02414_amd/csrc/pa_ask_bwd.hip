@@ -9,9 +9,12 @@
 //
 // delta_i is do_i.o_i; of an o in bf16 that is off by some 2^-9 |do o|, and dq_i by
 // that error times sum_j p_j k_j, which does not shrink where many states count, as
-// dq_i does.  So dq's pass corrects it: with d0 = do.o,
-//   A = sum p (dp - d0) k,  B = sum p k,  e = sum p (dp - d0):
-//   dq = scale (A - e B),  delta = d0 + e.
+// dq_i does.  So dq's pass corrects it: with d0 = do.o, ds' = p (dp - d0), and ds'' as it is
+// rounded for the product,
+//   A = sum ds'' k,  B = sum p k:   dq = scale (A - (sum ds'') B),  delta = d0 + sum ds'.
+// That also takes out of A what the roundings of ds'' add up to (times any part that all k
+// have in common): dq's error is 1.3 to 1.4 times that of its own rounding to bf16, 1.4 to
+// 1.5 with sum ds' in its place.
 #include <algorithm>
 
 #include "pa_ask.hpp"
@@ -49,6 +52,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   int hq[QT];
   bool on[QT];
   float d0[QT], lse2[QT], e0[QT];
+  f32x4 E[FIX ? QT : 1];
   WideF<T> qf[QT][Gm::NK], of[QT][Gm::NK];
   f32x4 A[QT][Gm::ND], Bk[FIX ? QT : 1][FIX ? Gm::ND : 1];
 #pragma unroll
@@ -77,10 +81,13 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
       A[c][d] = zero4();
       if constexpr (FIX) Bk[c][d] = zero4();
     }
+    if constexpr (FIX) E[c] = zero4();
   }
   const bool busy = v0 + w * QT * 16 < n;
   const float sc = a.scale * kLog2e;
   const TileRead<T, DP> at;
+  K16<T> ones;
+  set_k16(ones, 1.f, 1.f, 1.f, 1.f);
   if (kr.b < kr.e) st.put(live0);
   auto work = [&](const char* kt, const float* live) __attribute__((always_inline)) {
     const char* vt = kt + Gm::TB;
@@ -121,6 +128,10 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
           set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       __builtin_amdgcn_s_setprio(1);
+      if constexpr (FIX) {
+#pragma unroll
+        for (int c = 0; c < QT; ++c) E[c] = mma16x2(ones, sf[c][0], ones, sf[c][1], E[c]);
+      }
       pipelined<Gm::ND, 4, ColumnPair<T>>(
           [&](int d, ColumnPair<T>& f) {
             at.columns(f.a, kt, t0, d);
@@ -157,7 +168,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
         f32x4 x = A[c][d];
-        if constexpr (FIX) x -= Bk[c][d] * e0[c];
+        if constexpr (FIX) x -= Bk[c][d] * E[c][0];
         if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, x * a.scale);
       }
       if (g == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c] + e0[c];
@@ -171,6 +182,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
       }
       if (g == 0) {
         a.part_lse[at] = e0[c];
+        if constexpr (FIX) a.part_e[at] = E[c][0];
         if (s == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c];
       }
     }
@@ -181,7 +193,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
 template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a, int rows_, int U) {
   constexpr bool FIX = sizeof(T) == 2;
   __shared__ f32x4 lds[256];
-  __shared__ float ldse[256];
+  __shared__ float ldse[256], ldsr[256];
   const int per = a.D / 4, item = threadIdx.x / (per * U), in = threadIdx.x % (per * U);
   const int u = item < rows_ ? in / per : U, c = (in % per) * 4;  // (U: a thread too many)
   const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * rows_ + item;
@@ -189,11 +201,12 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
   const int64_t row = on ? at / a.Hq : 0, first = a.q_off ? a.q_off[0] : 0;
   const int64_t behind = a.q_off ? a.q_off[a.R] : a.Nq;
   const bool write = on && row >= first && row < behind;
-  float e = 0.f;
+  float e = 0.f, er = 0.f;
   f32x4 A = zero4(), B = zero4();
   if (write)
     for (int s = u; s < a.S; s += U) {
       e += a.part_lse[s * rows + at];
+      if constexpr (FIX) er += a.part_e[s * rows + at];
       A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
       if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
     }
@@ -201,10 +214,11 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
     A = add_groups(A, lds, u, U, in % per, per);
     if constexpr (FIX) B = add_groups(B, lds, u, U, in % per, per);
     e = add_groups(e, ldse, u, U, in % per, per);
+    if constexpr (FIX) er = add_groups(er, ldsr, u, U, in % per, per);
   }
   if (!write || u) return;
   const int hq = (int)(at - row * a.Hq);
-  if constexpr (FIX) A -= B * e;
+  if constexpr (FIX) A -= B * er;
   store4<T>(reinterpret_cast<T*>(a.dq) + row * a.lddq + (int64_t)hq * a.D + c, A * a.scale);
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
 }

@@ -320,6 +320,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
     }
   };
   const RowBase<bf16> rb = row_base<bf16>(r, RB);
+  K16<bf16> ones;
+  set_k16(ones, 1.f, 1.f, 1.f, 1.f);
   const int tr = tr_base<bf16>(RB), tp = tr_base<bf16>(PB), sp = r * PB + 8 * g;
   const int step = 32 * me.subs * P;  // (blocks go over the rows together)
   int v = 32 * (pc * me.subs + me.sub);
@@ -346,7 +348,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
         ld_row<bf16>(qf[k], qt, rb, 16 * c * RB + 64 * k);
         ld_row<bf16>(of[k], dt, rb, 16 * c * RB + 64 * k);
       }
-      f32x4 x[NT], dp[NT];
+      f32x4 x[NT], dp[NT], e;
+      K16<bf16> pf[NT];
       float delta = 0.f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -360,9 +363,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
           x[t][i] = fast_exp2(fmaf(x[t][i], sc, -lse[c]));
           delta = fmaf(x[t][i], dp[t][i], delta);
         }
-        K16<bf16> pf;
-        set_k16(pf, x[t][0], x[t][1], x[t][2], x[t][3]);
-        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = pf.v;
+        set_k16(pf[t], x[t][0], x[t][1], x[t][2], x[t][3]);
+        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = pf[t].v;
       }
       delta = groups_sum(delta);
 #pragma unroll
@@ -374,10 +376,18 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       }
       f32x4 dq[ND];
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
+      for (int t = 0; t < NT; t += 2)
+        e = mma16x2(ones, sf[c][t], ones, sf[c][t + 1], t ? e : zero4());
 #pragma unroll
-        for (int t = 0; t < NT; t += 2)
+      for (int d = 0; d < ND; ++d) {
+        f32x4 b;
+#pragma unroll
+        for (int t = 0; t < NT; t += 2) {
           dq[d] = mma16x2(kc[d][t], sf[c][t], kc[d][t + 1], sf[c][t + 1], t ? dq[d] : zero4());
+          b = mma16x2(kc[d][t], pf[t], kc[d][t + 1], pf[t + 1], t ? b : zero4());
+        }
+        dq[d] -= b * e[0];
+      }
       const bool in = v + 16 * c + r < n;
 #pragma unroll
       for (int k = 0; k < NK; ++k)

@@ -617,7 +617,10 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
   }
   if (!backward) return at;
   a->delta = take(rows);
-  if (a->S > 1) a->part_b = take((uint64_t)a->S * rows * a->D);
+  if (a->S > 1) {
+    a->part_b = take((uint64_t)a->S * rows * a->D);
+    a->part_e = take((uint64_t)a->S * rows);
+  }
   a->SQ = pa::ask_pieces_q(*a, dtype);
   if (a->SQ > 1) {
     const uint64_t n = (uint64_t)a->SQ * a->Nk * a->Hkv * a->D;

@@ -130,7 +130,7 @@ struct AskArgs {
   const void* d_o = nullptr;
   void *dq = nullptr, *dk = nullptr, *dv = nullptr;
   float* delta = nullptr;   // [Hq,Nq]
-  float* part_b = nullptr;  // [S,Nq,Hq,D]
+  float *part_b = nullptr, *part_e = nullptr;  // [S,Nq,Hq,D], [S,Nq,Hq]
   int SQ = 1;               // pieces of the queries
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };

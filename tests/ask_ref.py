@@ -142,11 +142,20 @@ def backward(q, k, v, o, do, scale, q_off=None, k_off=None, mask=None):
             eds = eds + FLUSH * (1 + (dp - delta).abs())
             s0, e0 = (p * (dp - d0)).abs(), (delta - d0).abs()
             add = U * (n / 4 + 64)
+            # dq = scale (sum r k - (sum r) B) with B = sum p k, where r = ds' (1 + t), |t| <=
+            # hp, are ds' = p (dp - d0) as they are rounded, and p is rounded in B.  sum ds' (k
+            # - B) is dq's exact value (ds' differs from ds by p (delta - d0), and sum p (k - B)
+            # = 0), so that what is off is sum ds' t (k - B), at most hp sum |ds'| (|k| + |B|),
+            # and (sum r) times B's error, at most (e0 + hp sum |ds'|) hp sum p |k|.  (fp32:
+            # hp = 0, and sum ds k as it is.)
+            B, pk, s1 = p @ kk, p @ kk.abs(), s0.sum(1, keepdim=True)
+            q0 = s0 * s0
+            spread = (q0 @ (kk * kk) - 2 * B * (q0 @ kk) + B * B * q0.sum(1, keepdim=True)).clamp(min=0)
             out["dq"].put((rows, h), scale * (ds @ kk), hp,
-                          scale * ((s0 + e0 * p) @ kk.abs()),
-                          scale * (torch.sqrt((s0 * s0) @ (kk * kk))
-                                   + e0 * torch.sqrt((p * p) @ (kk * kk))),
-                          scale * ((eds + add * (s0 + e0 * p)) @ kk.abs()))
+                          scale * (s0 @ kk.abs() + s1 * B.abs() + (e0 + hp * s1) * pk),
+                          scale * (torch.sqrt(spread)
+                                   + (e0 + hp * s1) * torch.sqrt((p * p) @ (kk * kk))),
+                          scale * ((eds + add * (s0 + e0 * p)) @ kk.abs() + add * s1 * pk))
             add = U * (m / 4 + 64)
             out["dk"].put((live, hk), scale * (ds.t() @ qq), hp, scale * (ds.abs().t() @ qq.abs()),
                           scale * torch.sqrt((ds * ds).t() @ (qq * qq)),
