@@ -107,6 +107,15 @@ __device__ __forceinline__ int request_of(const int64_t* off, int R, int64_t N, 
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// A grid of any number of blocks (HIP takes 2^32 threads of a dimension), and a block's number
+// in it: there may be more blocks than were asked for.
+constexpr int kGridX = 22;
+inline dim3 grid_of(int64_t blocks, int pieces) {
+  const int64_t x = (int64_t)1 << kGridX;
+  return dim3((uint32_t)(blocks < x ? blocks : x), pieces, (uint32_t)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ uint32_t block_of() { return (blockIdx.z << kGridX) + blockIdx.x; }
+
 // A piece of [b, e): the s-th of S, in whole tiles.
 __device__ __forceinline__ Range piece(Range k, int s, int S) {
   if (S == 1) return k;
@@ -217,6 +226,11 @@ template <typename T, int DP, int W> struct StateTiles {
   }
   __device__ __forceinline__ void put(float* live) {
     if (threadIdx.x < kTile) live[threadIdx.x] = alive;
+  }
+  // One of a tile's states counts (a tile of none is no work; nor does a query that is NaN
+  // make its row NaN where nothing counts).
+  __device__ __forceinline__ bool some(const float* live) const {
+    return !mask || __any(live[threadIdx.x & 63] == 0.f);
   }
 };
 

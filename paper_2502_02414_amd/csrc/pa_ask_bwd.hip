@@ -31,8 +31,8 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
   const int G = a.Hq / a.Hkv;
-  const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
-  const int64_t slot = blockIdx.x / a.Hkv;
+  const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
+  const int64_t slot = block_of() / (uint32_t)a.Hkv;
   const int rq = request_of(a.q_off, a.R, a.Nq, G, SHIFT, slot);
   if (rq < 0) return;
   const Range qr = range_of(a.q_off, rq, a.Nq);
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
     tiles_ready();
     const bool more = p0 + kTile < kr.e;
     if (more) st.load(p0 + kTile, next);
-    if (busy) work(now, live);
+    if (busy && st.some(live)) work(now, live);
     if (more) st.put(live_next);
   };
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
@@ -232,8 +232,8 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float stat0[2 * kTile], stat1[2 * kTile];  // lse (base 2), delta
   const int G = a.Hq / a.Hkv;
-  const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
-  const int64_t slot = blockIdx.x / a.Hkv;
+  const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
+  const int64_t slot = block_of() / (uint32_t)a.Hkv;
   const int rq = request_of(a.k_off, a.R, a.Nk, 1, SHIFT, slot);
   if (rq < 0) return;
   const Range kr = range_of(a.k_off, rq, a.Nk);
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   const int first = (int)vr.b;
   if (first < n) st.load(first, tiles0);
   const int64_t p0 = kr.b + tile * TK + w * KT * 16 + r;
-  const bool busy = kr.b + tile * TK + w * KT * 16 < kr.e;
+  bool busy = false;  // (a state of the wave's counts)
   bool in[KT];
   bool counts[KT];
   WideF<T> kf[KT][Gm::NK], vf[KT][Gm::NK];
@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
     const int64_t p = in[c] ? p0 + 16 * c : kr.e - 1;
     const bool on = in[c] && (!a.mask || a.mask[p]);
     counts[c] = on;
+    busy = busy || __any(on);
     row_frags<T, DP>(kf[c], reinterpret_cast<const T*>(a.k) + p * a.ldk + (int64_t)h * a.D, a.D, on);
     row_frags<T, DP>(vf[c], reinterpret_cast<const T*>(a.v) + p * a.ldv + (int64_t)h * a.D, a.D, on);
 #pragma unroll
@@ -386,13 +387,13 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskAr
 
 template <typename T, int DP, int QT, int W> hipError_t launch_dq(const AskArgs& a, hipStream_t st) {
   const int64_t slots = a.Nq * (a.Hq / a.Hkv) / (16 * QT * W) + a.R;
-  hipLaunchKernelGGL((k_ask_dq<T, DP, QT, W>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(64 * W), 0,
+  hipLaunchKernelGGL((k_ask_dq<T, DP, QT, W>), grid_of(slots * a.Hkv, a.S), dim3(64 * W), 0,
                      st, a);
   return hipGetLastError();
 }
 template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
   const int64_t slots = a.Nk / (16 * KT * W) + a.R;
-  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W>), dim3((uint32_t)(slots * a.Hkv), a.SQ), dim3(64 * W),
+  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W>), grid_of(slots * a.Hkv, a.SQ), dim3(64 * W),
                      0, st, a);
   return hipGetLastError();
 }

@@ -62,9 +62,10 @@ template <int DP, int NT> struct States {
         ld_tr<bf16>(f[d][t], mine, at, 16 * t * RB + 64 * (d >> 1) + 8 * (d & 1), RB);
     wave_sync();
   }
-  // 0, or -infinity where a state is left out
-  static __device__ __forceinline__ void alive(f32x4 (&f)[NT], Range k, const uint8_t* mask) {
+  // 0, or -infinity where a state is left out; whether one is not
+  static __device__ __forceinline__ bool alive(f32x4 (&f)[NT], Range k, const uint8_t* mask) {
     const int g = lane_id() >> 4;
+    bool some = false;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -73,7 +74,9 @@ template <int DP, int NT> struct States {
         bool counts = p < k.e;
         if (mask && k.b < k.e) counts = counts && mask[counts ? p : k.e - 1];
         f[t][i] = counts ? 0.f : -INFINITY;
+        some = some || counts;
       }
+    return __any(some);
   }
 };
 
@@ -95,7 +98,7 @@ __device__ __forceinline__ int place(int v, int rem, int G, int64_t ld, int D, i
 __device__ __forceinline__ Buffer rows_from(const bf16* p, int64_t ld, int i, int last, int width) {
   return buffer_of(p + i * ld, ((last - i < 32 ? last - i : 32) * ld + width) * 2);
 }
-// (stored past the caches, as what is streamed once)
+// 16 bytes of a row from two tiles, times f.
 __device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, const f32x4& y, float f) {
   typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
   bf16x8 o;
@@ -105,9 +108,6 @@ __device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, con
     o[i + 4] = (bf16)(y[i] * f);
   }
   __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), b, at, 0, 0);
-}
-__device__ __forceinline__ uint4 load16_once(Buffer b, int at) {
-  return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0));
 }
 
 // Which of the block's waves works on what: `heads` of them a head each, the others on
@@ -144,11 +144,12 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
   K32<bf16> kf[NT][NK];
   K16<bf16> vf[ND][NT];
   f32x4 none[NT];
+  int D;  // of q (and of do): none is read where no state counts, so that no NaN is
   {
     K32<bf16> vr_[NT][NK];
     S_::rows(kf, K, a.ldk, kr, a.mask, a.D);
     S_::rows(vr_, V, a.ldv, kr, a.mask, a.D);
-    S_::alive(none, kr, a.mask);
+    D = S_::alive(none, kr, a.mask) ? a.D : 0;
     S_::columns(vf, vr_, smem + (threadIdx.x >> 6) * S_::kBytes);
   }
 
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
-        qo[c][k] = place(16 * c + r, rem, G, a.ldq, a.D, 32 * k + 8 * g);
+        qo[c][k] = place(16 * c + r, rem, G, a.ldq, D, 32 * k + 8 * g);
         oo[c][k] = place(16 * c + r, rem, G, a.ldo, a.D, 32 * k + 8 * g);
       }
   };
@@ -178,7 +179,7 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int k = 0; k < NK; ++k) t.q[c][k] = load16_once(b, qo[c][k]);
+      for (int k = 0; k < NK; ++k) t.q[c][k] = load16(b, qo[c][k]);
   };
   auto work = [&](int v, const Tile& q) __attribute__((always_inline)) {
     const int i0 = G == 1 ? v : v / G;
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   f32x4 none[NT], dk[NT][ND], dv[NT][ND];
   S_::rows(kf, reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D, a.ldk, kr, a.mask, a.D);
   S_::rows(vf, reinterpret_cast<const bf16*>(a.v) + (int64_t)me.h * a.D, a.ldv, kr, a.mask, a.D);
-  S_::alive(none, kr, a.mask);
+  const int D = S_::alive(none, kr, a.mask) ? a.D : 0;
   S_::columns(kc, kf, qt);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
@@ -288,8 +289,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
       const int c = lane + 64 * j;
-      qo[j] = place(c / CPR, rem, G, a.ldq, a.D, c % CPR * 8);
-      od[j] = place(c / CPR, rem, G, a.lddo, a.D, c % CPR * 8);
+      qo[j] = place(c / CPR, rem, G, a.ldq, D, c % CPR * 8);
+      od[j] = place(c / CPR, rem, G, a.lddo, D, c % CPR * 8);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
@@ -308,8 +309,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
       const bool in = v + (lane + 64 * j) / CPR < n;
-      tl.q[j] = load16_once(bq, in ? qo[j] : kNowhere);
-      tl.d[j] = load16_once(bd, in ? od[j] : kNowhere);
+      tl.q[j] = load16(bq, in ? qo[j] : kNowhere);
+      tl.d[j] = load16(bd, in ? od[j] : kNowhere);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -456,6 +457,7 @@ __global__ void __launch_bounds__(256) k_ask_few_sum(AskArgs a, int per, int64_t
 #pragma unroll
   for (int i = 1; i < 8; ++i) s += part[i][c];
   const int64_t row = e / width, col = e - row * width;
+  if (a.mask && !a.mask[kr.b + row]) s = zero4();  // (weights of 0, of a do that is NaN, too)
   bf16* to = reinterpret_cast<bf16*>(blockIdx.y ? a.dv : a.dk);
   store4<bf16>(to + (kr.b + row) * (blockIdx.y ? a.lddv : a.lddk) + col, s);
 }

@@ -22,8 +22,8 @@ k_ask(AskArgs a) {
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
   const int G = a.Hq / a.Hkv;
-  const int h = blockIdx.x % a.Hkv, s = blockIdx.y;
-  const int64_t slot = blockIdx.x / a.Hkv;
+  const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
+  const int64_t slot = block_of() / (uint32_t)a.Hkv;
   const int rq = request_of(a.q_off, a.R, a.Nq, G, SHIFT, slot);
   if (rq < 0) return;
   const Range qr = range_of(a.q_off, rq, a.Nq);
@@ -134,7 +134,7 @@ k_ask(AskArgs a) {
     tiles_ready();
     const bool more = p0 + kTile < kr.e;
     if (more) st.load(p0 + kTile, next);
-    if (busy) work(now, live);
+    if (busy && st.some(live)) work(now, live);
     if (more) st.put(live_next);
   };
   for (int64_t p0 = kr.b; p0 < kr.e; p0 += 2 * kTile) {
@@ -212,7 +212,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs 
 
 template <typename T, int DP, int QT, int W> hipError_t launch(const AskArgs& a, hipStream_t st) {
   const int64_t G = a.Hq / a.Hkv, slots = a.Nq * G / (16 * QT * W) + a.R;
-  hipLaunchKernelGGL((k_ask<T, DP, QT, W>), dim3((uint32_t)(slots * a.Hkv), a.S), dim3(64 * W), 0, st,
+  hipLaunchKernelGGL((k_ask<T, DP, QT, W>), grid_of(slots * a.Hkv, a.S), dim3(64 * W), 0, st,
                      a);
   return hipGetLastError();
 }

@@ -437,3 +437,53 @@ def test_one_request_has_most_of_the_rows():
         c = Case(ql, kl, 2, 2, 64, dt)
         c.check_forward()
         c.check_backward()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ql,kl,D", [((6, 5, 700), (40, 30, 20), 32), ((6, 5, 70), (64, 0, 50), 64),
+                                     ((6, 5, 70), (40, 0, 200), 48), ((2, 1, 3), (3000, 0, 2000), 128),
+                                     ((300, 40, 2000), (2000, 1, 2050), 64)])
+def test_queries_of_no_states_may_hold_anything(dt, ql, kl, D):
+    """Queries and gradients that are NaN where no state counts (a padded batch's) are read
+    by nothing: answers and gradients of 0, and none of another row's is NaN."""
+    c = Case(ql, kl, 2, 2, D, DT[dt], "rows")
+    rows = ql[0] + (ql[1] if not kl[1] else 0)
+    c.mask[c.k_off[1]] = c.mask[c.k_off[2]] = True
+    c.k[[c.k_off[1], c.k_off[2]]] = c.v[[c.k_off[1], c.k_off[2]]] = 0.5
+    c.par = ops.make_cross_attention(2, 2, D, q_off=torch.tensor(c.q_off).cuda(),
+                                     k_off=torch.tensor(c.k_off).cuda(), mask=c.mask.cuda(),
+                                     max_k=max(kl))
+    c.gk, c.gv = c.k.cuda(), c.v.cuda()
+    c.gq[:rows], c.gdo[:rows] = NAN, NAN
+    o, lse = c.forward()
+    assert (o[:rows] == 0).all() and (lse[:, :rows] == -INF).all()
+    dq, dk, dv = c.backward(o, lse)
+    n = c.k_off[1]
+    assert (dq[:rows] == 0).all() and (dk[:n] == 0).all() and (dv[:n] == 0).all()
+    for t in (o[rows:], lse[:, rows:], dq[rows:], dk[n:], dv[n:]):
+        assert torch.isfinite(t).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ql,kl", [((600,), (40,)), ((90,), (64,)), ((90,), (300,)), ((3,), (5000,)),
+                                   ((4000,), (130,))])
+def test_a_nan_gradient_reaches_no_state_that_is_left_out(dt, ql, kl):
+    c = Case(ql, kl, 4, 2, 40, DT[dt], "some")
+    o, lse = c.forward()
+    c.gdo[1] = NAN
+    dq, dk, dv = c.backward(o, lse)
+    off = ~c.mask.cuda()
+    assert (dk[off] == 0).all() and (dv[off] == 0).all() and torch.isnan(dv[~off]).all()
+    assert torch.isnan(dq[1]).all() and torch.isfinite(dq[2:]).all() and torch.isfinite(dq[0]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_requests_by_the_million(dt):
+    """More blocks than one dimension of a grid takes: 2^25, for 2^21 requests of nothing
+    around three of some rows."""
+    c = Case((3, 70, 1), (5, 130, 64), 16, 16, 8, DT[dt], "some", packed=True)
+    far = lambda off: torch.tensor([0] * (1 << 20) + off + [off[-1]] * (1 << 20)).cuda()
+    c.par = ops.make_cross_attention(16, 16, 8, q_off=far(c.q_off), k_off=far(c.k_off),
+                                     mask=c.mask.cuda(), max_k=130)
+    c.check_forward()
+    c.check_backward()
