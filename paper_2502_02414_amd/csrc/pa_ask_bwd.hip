@@ -403,7 +403,7 @@ template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs
 // (us, small and large: 2,080 queries of 8 heads over 17,906 states 259 and 331 to 385,
 // 8,192 over 8,192 480 and 451; 64 wide and 4 heads 387 and 327).
 int rows_dq(const AskArgs& a, int dtype) {
-  return a.D <= 32 || !ask_large(a, dtype) ? 64 : a.D <= 64 ? 256 : 128;
+  return a.D <= 32 || !ask_large(a, dtype, true) ? 64 : a.D <= 64 ? 256 : 128;
 }
 int rows_dkv(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = a.Nk / a.R;

@@ -11,6 +11,8 @@
 // ds^T.  The sums over the queries, dv += p^T do and dk += ds^T q, need p and ds with
 // queries along the product: they go through the wave's part of LDS, as do q and do.
 // A block's dk and dv are a record in the workspace, added in order.
+#include <algorithm>
+
 #include "pa_ask.hpp"
 
 namespace pa {
@@ -141,17 +143,9 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
 
   // (longer ones are the other kernel's, none has no states to read)
   if (kr.e - kr.b > 16 * NT) return;
-  K32<bf16> kf[NT][NK];
-  K16<bf16> vf[ND][NT];
   f32x4 none[NT];
-  int D;  // of q (and of do): none is read where no state counts, so that no NaN is
-  {
-    K32<bf16> vr_[NT][NK];
-    S_::rows(kf, K, a.ldk, kr, a.mask, a.D);
-    S_::rows(vr_, V, a.ldv, kr, a.mask, a.D);
-    D = S_::alive(none, kr, a.mask) ? a.D : 0;
-    S_::columns(vf, vr_, smem + (threadIdx.x >> 6) * S_::kBytes);
-  }
+  // of q: none is read where no state counts, so that no NaN is
+  const int D = S_::alive(none, kr, a.mask) ? a.D : 0;
 
   // this lane's parts of a tile of 32 rows: 16 bytes for each step of the width
   const bool even = 32 % G == 0;  // (tiles begin at a query)
@@ -181,6 +175,8 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
 #pragma unroll
       for (int k = 0; k < NK; ++k) t.q[c][k] = load16(b, qo[c][k]);
   };
+  K32<bf16> kf[NT][NK];
+  K16<bf16> vf[ND][NT];
   auto work = [&](int v, const Tile& q) __attribute__((always_inline)) {
     const int i0 = G == 1 ? v : v / G;
     if (!even) places(v - i0 * G);
@@ -233,7 +229,13 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
   };
   int v = 16 * C * (pc * me.subs + me.sub);
   Tile t0, t1;
-  load(v, t0);
+  load(v, t0);  // (on its way while the states come)
+  {
+    K32<bf16> vr_[NT][NK];
+    S_::rows(kf, K, a.ldk, kr, a.mask, a.D);
+    S_::rows(vr_, V, a.ldv, kr, a.mask, a.D);
+    S_::columns(vf, vr_, smem + (threadIdx.x >> 6) * S_::kBytes);
+  }
   for (;;) {  // the next tiles on their way while these are worked on
     load(v + step, t1);
     work(v, t0);
@@ -272,10 +274,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   K32<bf16> kf[NT][NK], vf[NT][NK];
   K16<bf16> kc[ND][NT];
   f32x4 none[NT], dk[NT][ND], dv[NT][ND];
-  S_::rows(kf, reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D, a.ldk, kr, a.mask, a.D);
-  S_::rows(vf, reinterpret_cast<const bf16*>(a.v) + (int64_t)me.h * a.D, a.ldv, kr, a.mask, a.D);
-  const int D = S_::alive(none, kr, a.mask) ? a.D : 0;
-  S_::columns(kc, kf, qt);
+  const int D = S_::alive(none, kr, a.mask) ? a.D : 0;  // (of q and do, as forward)
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -326,7 +325,10 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   const int tr = tr_base<bf16>(RB), tp = tr_base<bf16>(PB), sp = r * PB + 8 * g;
   const int step = 32 * me.subs * P;  // (blocks go over the rows together)
   int v = 32 * (pc * me.subs + me.sub);
-  if (v < n) load(v);
+  if (v < n) load(v);  // (on its way while the states come)
+  S_::rows(kf, reinterpret_cast<const bf16*>(a.k) + (int64_t)me.h * a.D, a.ldk, kr, a.mask, a.D);
+  S_::rows(vf, reinterpret_cast<const bf16*>(a.v) + (int64_t)me.h * a.D, a.ldv, kr, a.mask, a.D);
+  S_::columns(kc, kf, qt);
   for (; v < n; v += step) {
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
@@ -462,7 +464,11 @@ __global__ void __launch_bounds__(256) k_ask_few_sum(AskArgs a, int per, int64_t
   store4<bf16>(to + (kr.b + row) * (blockIdx.y ? a.lddv : a.lddk) + col, s);
 }
 
-// Blocks of a request, and how many waves of a block share a head.
+// Blocks of a request, and how many waves of a block share a head.  Forward: whole rounds of
+// the blocks that are resident, each wave with some 16 tiles (us, of 64 states of 8 heads of
+// 32: 100,000 queries 27 where blocks of two tiles took 40, a million 240 and, in 1953
+// blocks, 252; 300,000 of 4 heads of 64 67 and 108).  Backward: a block per CU, since each
+// leaves a record of all states' gradients.
 struct Split {
   int P, groups, subs, waves;
 };
@@ -472,9 +478,14 @@ Split split_of(const AskArgs& a, bool bwd) {
   const int heads = a.Hkv < s.waves ? a.Hkv : s.waves;
   s.groups = (a.Hkv + heads - 1) / heads;
   s.subs = s.waves / heads;
-  // some 4096 blocks forward, one per CU backward; at least two tiles a wave
-  const int64_t n = a.Nq * (a.Hq / a.Hkv) / a.R, least = 64 * s.subs;
-  int64_t P = (bwd ? 256 : 4096) / ((int64_t)a.R * s.groups);
+  const int64_t n = a.Nq * (a.Hq / a.Hkv) / a.R, each = (int64_t)a.R * s.groups;
+  int64_t P = 256 / each, least = 64 * s.subs;
+  if (!bwd) {
+    const int64_t resident = a.D > 32 && a.max_k > 32 ? 256 : 512, rows = n * each / s.subs;
+    const int64_t rounds = (rows / 256 / resident + 1) / 2;
+    P = (rounds ? rounds * resident : std::min(resident, std::max<int64_t>(256, rows / 128))) / each;
+    least = 32 * s.subs;
+  }
   if (P > n / least) P = n / least;
   s.P = P < 1 ? 1 : (int)P;
   return s;

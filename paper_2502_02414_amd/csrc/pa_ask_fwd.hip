@@ -5,6 +5,16 @@
 // sums are fp32, and exp(s - m) is rounded to the operands' type for the product with
 // v (bf16: 2^-9 of each weight, below the rounding of o, since the errors of several
 // weights do not line up; l adds up the unrounded ones).
+//
+// What bounds it: with few queries to a request the read of k and v (64 queries in 64
+// requests over a million states of 2 heads of 64, bf16: 100 us, 5.1 TB/s), with many the
+// products and the weights' arithmetic on the same SIMDs (16,384 queries over 16,384 states,
+// 4 heads of 64, bf16: 315 us, 870 TFLOP/s; the vector instructions take 70% of its cycles,
+// the matrix cores 35%; fp32, whose products run at 1/16 of that rate, is bound by them).
+// So: tiles come into LDS by loads that pass no register, one tile ahead of the products;
+// whole tiles of 64 states go without a bound's check (a state that is not there or left out
+// begins at -infinity in the accumulator); the maximum moves seldom; scores are scaled in
+// the exponential's fused multiply-add.
 #include <algorithm>
 
 #include "pa_ask.hpp"
@@ -13,6 +23,10 @@ namespace pa {
 namespace {
 using namespace ask;
 
+// A block has a tile of 16 QT W virtual rows and a head: a wave's QT tiles of 16 queries are
+// columns of its products, and every wave reads all of a tile of states.  Two blocks of
+// eight waves on a CU (128 VGPRs) with two tiles each took 315 us for 16,384 squared where
+// four of four waves took 340 and, at 256 VGPRs, two of four 382.
 template <typename T, int DP, int QT, int W>
 __global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 4 : DP * sizeof(T) <= 256 ? 2 : 1)
 k_ask(AskArgs a) {
@@ -217,7 +231,7 @@ template <typename T, int DP, int QT, int W> hipError_t launch(const AskArgs& a,
   return hipGetLastError();
 }
 hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
-  const bool large = ask_large(a, dtype);
+  const bool large = ask_large(a, dtype, false);
   return by_width(a.D, dtype, [&](auto type, auto dp) {
     using T = decltype(type);
     constexpr int DP = decltype(dp)::value;
@@ -231,11 +245,14 @@ hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
 
 // Blocks of eight waves with two tiles of 16 queries each (bf16) in place of four with one:
 // a tile of states is read by them a quarter as often, from LDS half as often, where
-// requests fill most of them and there is work for the chip (in pieces).
-bool ask_large(const AskArgs& a, int dtype) {
+// requests fill most of them and there is work for the chip (in pieces).  us, small and
+// large, of 4 heads: 16,384 squared of 64 wide 407 and 345, 8,192 squared 112 and 97, 4,096
+// squared 45 and 58, of 128 wide 59 and 53, 2,048 squared 28 and 35; dq's pass of 4,096
+// squared of 64 wide 5 more and less.
+bool ask_large(const AskArgs& a, int dtype, bool backward) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = rows / a.R, tiles = a.Nk / a.R / kTile;
   return dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && tiles >= 2 &&
-         (rows + 255) / 256 * a.Hkv * tiles >= (a.D <= 64 ? 4096 : 2048);
+         (rows + 255) / 256 * a.Hkv * tiles >= (a.D > 64 ? 2048 : backward ? 4096 : 8192);
 }
 
 // The number of pieces whose time comes out shortest: blocks of `waves` that take `cycles`
@@ -265,7 +282,7 @@ int ask_resident(const AskArgs& a, int dtype, bool large_backward) {
 }
 int ask_pieces(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), tiles = (a.Nk / a.R + kTile - 1) / kTile;
-  const bool large = ask_large(a, dtype);
+  const bool large = ask_large(a, dtype, false);
   const double cycles = 450 + (dtype == 1 ? 2.0 : 32.0) * 2 * a.D;  // softmax, two products
   return ask_pieces_of((rows / (large ? 256 : 64) + a.R) * a.Hkv, large ? 8 : 4,
                        ask_resident(a, dtype, false), large ? 2 * cycles : cycles, tiles,

@@ -134,7 +134,7 @@ struct AskArgs {
   int SQ = 1;               // pieces of the queries
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
-bool ask_large(const AskArgs& a, int dtype);  // blocks of many queries
+bool ask_large(const AskArgs& a, int dtype, bool backward);  // blocks of many queries
 int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
                   double bytes);
 int ask_resident(const AskArgs& a, int dtype, bool large_backward);

@@ -487,3 +487,15 @@ def test_requests_by_the_million(dt):
                                      mask=c.mask.cuda(), max_k=130)
     c.check_forward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("H,D,n", [(8, 32, 600_000), (4, 64, 300_000), (1, 8, 700_001)])
+def test_many_rounds_of_blocks_over_few_states(H, D, n):
+    """Queries that come back every 1000 rows have the answers of the first 1000 ones."""
+    c = Case((1000,), (50,), H, H, D, BF16, "some")
+    ro, rl = c.check_forward()
+    o, lse = c.forward()
+    at = torch.arange(n, device="cuda") % 1000
+    q, big, l = c.gq[at], torch.full((n, H, D), 7.0, dtype=BF16, device="cuda"), torch.empty(H, n, device="cuda")
+    ops.pa_cross_attention(q, c.gk, c.gv, c.par, big, l)
+    assert torch.equal(big, o[at]) and torch.equal(l, lse[:, at])
