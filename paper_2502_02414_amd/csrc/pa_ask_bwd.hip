@@ -15,6 +15,17 @@
 // That also takes out of A what the roundings of ds'' add up to (times any part that all k
 // have in common): dq's error is 1.3 to 1.4 times that of its own rounding to bf16, 1.4 to
 // 1.5 with sum ds' in its place.
+//
+// What bounds it: 8,192 queries of 4 heads over 8,192 states of one of 128, bf16, take
+// 520 to 550 us, dq's pass 48% of it: 625 to 660 TFLOP/s counting the five products of
+// the formulas, 880 to 920 with the two that are formed twice.  Two waves of a SIMD are all that
+// the registers leave (K, V or Q, dO rows, and two sums of the width, per wave), and a tile's
+// LDS reads, products and exponentials of one wait for each other more often than the other
+// wave fills.  One pass over the pairs would save two products, but adds one side's sums in
+// memory, by atomics (in an order that changes) or by records of it per block: 8,192 rows of 512
+// fp32 for each of the 128 tiles of states are 2.1 GB.
+// fp32: 6,001 queries of 4 heads over 3,333 states of 2 heads of 40, 9 requests, take 88 us, the
+// matrix cores busy for 38% of it: 1/16 of bf16's rate, with one to two waves to a SIMD.
 #include <algorithm>
 
 #include "pa_ask.hpp"
@@ -23,6 +34,8 @@ namespace pa {
 namespace {
 using namespace ask;
 
+// dq and delta of a tile of 16 QT W virtual rows, as k_ask: q and do in registers, the states
+// through LDS.
 template <typename T, int DP, int QT, int W>
 __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
@@ -33,14 +46,13 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   const int G = a.Hq / a.Hkv;
   const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
   const int64_t slot = block_of() / (uint32_t)a.Hkv;
-  const int rq = request_of(a.q_off, a.R, a.Nq, G, SHIFT, slot);
-  if (rq < 0) return;
-  const Range qr = range_of(a.q_off, rq, a.Nq);
+  Place pl;
+  if (!place_of(pl, a.q_off, a.Nq, a.k_off, a.Nk, a.R, G, SHIFT, slot)) return;
+  const Range qr = pl.mine, all = pl.theirs, kr = piece(all, s, a.S);
   const int n = (int)(qr.e - qr.b) * G;
-  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - rq;
+  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - pl.r;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  const Range all = range_of(a.k_off, rq, a.Nk), kr = piece(all, s, a.S);
   if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
@@ -234,12 +246,11 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   const int G = a.Hq / a.Hkv;
   const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
   const int64_t slot = block_of() / (uint32_t)a.Hkv;
-  const int rq = request_of(a.k_off, a.R, a.Nk, 1, SHIFT, slot);
-  if (rq < 0) return;
-  const Range kr = range_of(a.k_off, rq, a.Nk);
-  const int64_t tile = slot - (kr.b >> SHIFT) - rq;
+  Place pl;
+  if (!place_of(pl, a.k_off, a.Nk, a.q_off, a.Nq, a.R, 1, SHIFT, slot)) return;
+  const Range kr = pl.mine, qr = pl.theirs;
+  const int64_t tile = slot - (kr.b >> SHIFT) - pl.r;
   if (tile < 0 || tile * TK >= kr.e - kr.b || kr.e - kr.b <= a.few) return;
-  const Range qr = range_of(a.q_off, rq, a.Nq);
   const Range vr = piece(Range{0, (qr.e - qr.b) * G}, s, a.SQ);  // virtual rows
   const int n = (int)vr.e;
 
@@ -366,7 +377,9 @@ __global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_d
   }
 }
 
-// The records of the queries' pieces added, by U groups of 256 / U threads.
+// The records of the queries' pieces added, by U groups of 256 / U threads: few records by one
+// thread each, many in a tree (27,615 queries over 16 states, 128 wide, in many records: 108
+// us for the call with one thread, 38 so).
 template <typename T> __global__ void __launch_bounds__(256) k_ask_dkv_sum(AskArgs a, int U) {
   __shared__ f32x4 lds[256];
   const int P = 256 / U, u = threadIdx.x / P, x = threadIdx.x % P;

@@ -38,14 +38,13 @@ k_ask(AskArgs a) {
   const int G = a.Hq / a.Hkv;
   const int h = block_of() % (uint32_t)a.Hkv, s = blockIdx.y;
   const int64_t slot = block_of() / (uint32_t)a.Hkv;
-  const int rq = request_of(a.q_off, a.R, a.Nq, G, SHIFT, slot);
-  if (rq < 0) return;
-  const Range qr = range_of(a.q_off, rq, a.Nq);
+  Place pl;
+  if (!place_of(pl, a.q_off, a.Nq, a.k_off, a.Nk, a.R, G, SHIFT, slot)) return;
+  const Range qr = pl.mine, all = pl.theirs, kr = piece(all, s, a.S);
   const int n = (int)(qr.e - qr.b) * G;
-  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - rq;
+  const int64_t tile = slot - ((qr.b * G) >> SHIFT) - pl.r;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  const Range all = range_of(a.k_off, rq, a.Nk), kr = piece(all, s, a.S);
   if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
