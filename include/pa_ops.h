@@ -216,17 +216,19 @@ pa_status pa_linear_i8_workspace(int64_t N, int F, int K, size_t* bytes);
  *   o_i = sum_j exp(s_ij - lse_i) v_j,
  * o [Nq, Hq, D], lse [Hq, Nq] fp32.  A row without a state (or whose scores are
  * all -infinity) has o = 0 and lse = -infinity, and passes no gradient.  What k
- * and v hold where the mask is 0 is of no account, be it infinities or NaN.
+ * and v hold where the mask is 0 is of no account, be it infinities or NaN, nor
+ * what q and d_o hold in a request without a state; a state that is left out has
+ * gradients of 0.
  * Rows outside of the requests, in front of the first or behind the last, are
  * not read and their outputs left as they were.
  *
  * D a multiple of 8 in [8, 128]; Hkv divides Hq, Hq at most 4096; requests,
  * their rows and Nk from 0; Nq G and Nk below 2^31 - 2^21.  ld*: elements
  * between the rows of a tensor, a multiple of 16 bytes, less than 2^25 bytes and
- * at least its heads times D (with fewer than two rows: not looked at); k and v may lie side by side
- * in the rows of one product, and dk and dv so too.  Scores, softmax statistics and
- * sums are fp32; for bf16 the weights, and in the backward ds, are rounded to bf16
- * for the products over the states and over the queries.
+ * at least its heads times D (with fewer than two rows: not looked at); k and v
+ * may lie side by side in the rows of one product, and dk and dv so too.  Scores,
+ * softmax statistics and sums are fp32; for bf16 the weights, and in the backward
+ * ds, are rounded to bf16 for the products over the states and over the queries.
  * --------------------------------------------------------------------- */
 typedef struct {
   int32_t R;               /* requests, >= 1                                     */

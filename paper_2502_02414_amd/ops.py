@@ -13,8 +13,9 @@ same manner): the operators around the block stack.
                                residual add
 
 Tensors are contiguous GPU tensors on the current device (of pa_cross_attention's
-the rows may lie further apart); outputs are passed in.  Each wrapper checks device, dtype, size and contiguity against the call,
-and raises ValueError, or PAError with the library's message.
+the rows may lie further apart); outputs are passed in.  Each wrapper checks
+device, dtype, size and contiguity against the call, and raises ValueError, or
+PAError with the library's message.
 """
 from __future__ import annotations
 
