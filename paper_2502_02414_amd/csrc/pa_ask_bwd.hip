@@ -37,7 +37,7 @@ using namespace ask;
 // dq and delta of a tile of 16 QT W virtual rows, as k_ask: q and do in registers, the states
 // through LDS.
 template <typename T, int DP, int QT, int W>
-__global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dq(AskArgs a) {
+__global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
   constexpr bool FIX = sizeof(T) == 2;
   constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;
@@ -238,7 +238,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
 // dk and dv of a tile of 16 KT W states: a wave has KT times 16 of them as columns, and
 // their rows of k and v in registers; the queries come through LDS.
 template <typename T, int DP, int KT, int W>
-__global__ void __launch_bounds__(64 * W, DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dkv(AskArgs a) {
+__global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dkv(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
   constexpr int TK = 16 * KT * W, SHIFT = TK == 64 ? 6 : TK == 128 ? 7 : 8;
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
@@ -416,9 +416,11 @@ template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs
 // (us, small and large: 2,080 queries of 8 heads over 17,906 states 259 and 331 to 385,
 // 8,192 over 8,192 480 and 451; 64 wide and 4 heads 387 and 327).
 int rows_dq(const AskArgs& a, int dtype) {
+  if (ask_eight(a, dtype)) return 128;
   return a.D <= 32 || !ask_large(a, dtype, true) ? 64 : a.D <= 64 ? 256 : 128;
 }
 int rows_dkv(const AskArgs& a, int dtype) {
+  if (ask_eight(a, dtype)) return 128;
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = a.Nk / a.R;
   const bool large = dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && rows / a.R >= 128 &&
                      (a.Nk + 255) / 256 * a.Hkv * (rows / a.R / kTile) >= (a.D <= 64 ? 4096 : 2048);
@@ -434,6 +436,8 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
       constexpr int DP = decltype(dp)::value;
       if constexpr (sizeof(T) == 2 && DP > 32)
         if (large) return launch_dq<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
+      if constexpr (sizeof(T) == 4 && DP > 64)
+        if (large) return launch_dq<T, DP, 1, 8>(a, st);
       return launch_dq<T, DP, 1, 4>(a, st);
     });
     if (e != hipSuccess) return e;
@@ -452,6 +456,8 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     constexpr int DP = decltype(dp)::value;
     if constexpr (sizeof(T) == 2 && DP > 32)
       if (large) return launch_dkv<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
+    if constexpr (sizeof(T) == 4 && DP > 64)
+      if (large) return launch_dkv<T, DP, 1, 8>(a, st);
     return launch_dkv<T, DP, 1, 4>(a, st);
   });
   if (e != hipSuccess || a.SQ == 1) return e;
@@ -471,14 +477,14 @@ int ask_pieces_dq(const AskArgs& a, int dtype) {
   const int rows = rows_dq(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 * 4 : 32.0 * 3) * a.D;
   return ask_pieces_of((a.Nq * (a.Hq / a.Hkv) / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
-                       ask_resident(a, dtype, rows > 64), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
+                       ask_resident(a, dtype, rows > 64, true), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
                        (dtype == 1 ? 8.0 : 4.0) * a.Nq * a.Hq * (a.D + 1));
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {
   const int rows = rows_dkv(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 : 32.0) * 4 * a.D;
   return ask_pieces_of((a.Nk / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
-                       ask_resident(a, dtype, rows > 64), tiles_of * cycles,
+                       ask_resident(a, dtype, rows > 64, true), tiles_of * cycles,
                        (a.Nq * (a.Hq / a.Hkv) / a.R + kTile - 1) / kTile,
                        8.0 * a.Nk * a.Hkv * a.D);
 }

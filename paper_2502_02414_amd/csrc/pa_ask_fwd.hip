@@ -28,7 +28,7 @@ using namespace ask;
 // eight waves on a CU (128 VGPRs) with two tiles each took 315 us for 16,384 squared where
 // four of four waves took 340 and, at 256 VGPRs, two of four 382.
 template <typename T, int DP, int QT, int W>
-__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 4 : DP * sizeof(T) <= 256 ? 2 : 1)
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 4 : W == 8 || DP * sizeof(T) <= 256 ? 2 : 1)
 k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
   constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;
@@ -230,12 +230,14 @@ template <typename T, int DP, int QT, int W> hipError_t launch(const AskArgs& a,
   return hipGetLastError();
 }
 hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
-  const bool large = ask_large(a, dtype, false);
+  const bool large = ask_large(a, dtype, false), eight = ask_eight(a, dtype);
   return by_width(a.D, dtype, [&](auto type, auto dp) {
     using T = decltype(type);
     constexpr int DP = decltype(dp)::value;
     if constexpr (sizeof(T) == 2)
       if (large) return launch<T, DP, 2, 8>(a, st);
+    if constexpr (sizeof(T) == 4 && DP > 64)
+      if (eight) return launch<T, DP, 1, 8>(a, st);
     return launch<T, DP, 1, 4>(a, st);
   });
 }
@@ -252,6 +254,14 @@ bool ask_large(const AskArgs& a, int dtype, bool backward) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = rows / a.R, tiles = a.Nk / a.R / kTile;
   return dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && tiles >= 2 &&
          (rows + 255) / 256 * a.Hkv * tiles >= (a.D > 64 ? 2048 : backward ? 4096 : 8192);
+}
+
+// fp32 heads wider than 64, whose tiles leave room for one block on a CU: eight waves where
+// there is work for two on every SIMD (us, four and eight: 4,096 squared of 2 heads of 128 171
+// and 156, backward 506 and 470; 1,000 queries over 300 states of 8 heads 28 and 38).
+bool ask_eight(const AskArgs& a, int dtype) {
+  const int64_t rows = (a.Nq * (a.Hq / a.Hkv) + kTile - 1) / kTile;
+  return dtype == 0 && a.D > 64 && rows * a.Hkv * ((a.Nk / a.R + kTile - 1) / kTile) >= 1024;
 }
 
 // The number of pieces whose time comes out shortest: blocks of `waves` that take `cycles`
@@ -275,16 +285,17 @@ int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_
   return best;
 }
 // Waves of a SIMD that the kernels' registers and LDS leave room for.
-int ask_resident(const AskArgs& a, int dtype, bool large_backward) {
-  if (dtype == 0) return a.D <= 32 ? 4 : a.D <= 64 ? 2 : 1;
-  return a.D <= 64 && !large_backward ? 4 : 2;
+int ask_resident(const AskArgs& a, int dtype, bool eight, bool backward) {
+  if (dtype == 0) return a.D <= 32 ? 4 : a.D <= 64 || eight ? 2 : 1;
+  return a.D <= 64 && !(eight && backward) ? 4 : 2;
 }
 int ask_pieces(const AskArgs& a, int dtype) {
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), tiles = (a.Nk / a.R + kTile - 1) / kTile;
   const bool large = ask_large(a, dtype, false);
+  const int block = large ? 256 : ask_eight(a, dtype) ? 128 : 64;
   const double cycles = 450 + (dtype == 1 ? 2.0 : 32.0) * 2 * a.D;  // softmax, two products
-  return ask_pieces_of((rows / (large ? 256 : 64) + a.R) * a.Hkv, large ? 8 : 4,
-                       ask_resident(a, dtype, false), large ? 2 * cycles : cycles, tiles,
+  return ask_pieces_of((rows / block + a.R) * a.Hkv, block > 64 ? 8 : 4,
+                       ask_resident(a, dtype, block > 64, false), large ? 2 * cycles : cycles, tiles,
                        4.0 * a.Nq * a.Hq * (a.D + 1));
 }
 

@@ -137,7 +137,8 @@ struct AskArgs {
 bool ask_large(const AskArgs& a, int dtype, bool backward);  // blocks of many queries
 int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
                   double bytes);
-int ask_resident(const AskArgs& a, int dtype, bool large_backward);
+bool ask_eight(const AskArgs& a, int dtype);  // of eight waves, fp32
+int ask_resident(const AskArgs& a, int dtype, bool eight, bool backward);
 int ask_pieces(const AskArgs& a, int dtype);     // S, forward
 int ask_pieces_dq(const AskArgs& a, int dtype);  // S, backward
 int ask_pieces_q(const AskArgs& a, int dtype);   // SQ

@@ -499,3 +499,13 @@ def test_many_rounds_of_blocks_over_few_states(H, D, n):
     q, big, l = c.gq[at], torch.full((n, H, D), 7.0, dtype=BF16, device="cuda"), torch.empty(H, n, device="cuda")
     ops.pa_cross_attention(q, c.gk, c.gv, c.par, big, l)
     assert torch.equal(big, o[at]) and torch.equal(l, lse[:, at])
+
+
+@pytest.mark.parametrize("ql,kl,Hq,Hkv,D,mask", [((2100,), (2070,), 2, 2, 128, "some"),
+                                                 ((5000, 3, 700), (300, 100, 0), 4, 2, 80, None),
+                                                 ((1500, 1), (64, 2900), 4, 4, 96, "some")])
+def test_larger_ones_of_wide_heads_in_fp32(ql, kl, Hq, Hkv, D, mask):
+    say(f"cross attention f32 {ql} {kl} {Hq}/{Hkv} {D}")
+    c = Case(ql, kl, Hq, Hkv, D, F32, mask, "fused")
+    c.check_forward()
+    c.check_backward()
