@@ -58,12 +58,12 @@ __device__ __forceinline__ float wide_elem(const K16<float>& f, int e) { return 
 // neighbour) and, bf16, columns (ds_read_b64_tr_b16: in one cycle two chunks of rows 0-7
 // or of 8-15); with these keys both meet every bank once: 4.2 and 2.2 cycles for 1 KB and
 // 512 B, with keys that make the 16 rows' places differ 4.2 and 4.1, or 8.1 and 2.2.
-// W: waves of a block.
-template <typename T, int DP, int W = 4> struct AskGeo {
+// W: waves of a block; ROWS: of a tile.
+template <typename T, int DP, int W = 4, int ROWS = kTile> struct AskGeo {
   static constexpr int SZ = (int)sizeof(T), E = 16 / SZ;  // E: elements of 16 bytes
   static constexpr int NK = (DP + Wide<T>::W - 1) / Wide<T>::W, ND = DP / 16;  // steps; tiles
   static constexpr int CP = NK <= 1 ? 4 : NK <= 2 ? 8 : NK <= 4 ? 16 : 32;     // chunks of a row
-  static constexpr int RB = 16 * CP, TB = kTile * RB;     // bytes of a row, of a tile
+  static constexpr int RB = 16 * CP, TB = ROWS * RB;      // bytes of a row, of a tile
   static constexpr int NP = (TB + 1024 * W - 1) / (1024 * W);  // loads of a tile per wave
   static __device__ __forceinline__ int key(int row) {
     if constexpr (SZ == 4) return CP == 4 ? row >> 2 & 3 : CP == 8 ? row >> 1 & 7 : row & 15;
@@ -180,8 +180,8 @@ constexpr int kNowhere = 0x7fffff00;
 // Loads of a tile of up to 64 rows into LDS by W waves, 16 bytes a lane, without a
 // register between, zeros where rows or columns end.  Offsets within a tile stay below
 // 2^31: rows are at most 2^25 bytes apart.
-template <typename T, int DP, int W> struct TileLoad {
-  using Gm = AskGeo<T, DP, W>;
+template <typename T, int DP, int W, int ROWS = kTile> struct TileLoad {
+  using Gm = AskGeo<T, DP, W, ROWS>;
   int off[Gm::NP];
 
   // this lane's row and column in load j of its wave
@@ -269,11 +269,11 @@ template <typename T, int DP, int W> struct StateTiles {
   }
 };
 
-// Tiles of a request's virtual rows: q's, do's behind it, and their lse (base 2) and
+// Tiles of ROWS of a request's virtual rows: q's, do's behind it, and their lse (base 2) and
 // delta, [2][64] floats, with which rows past the end have weights of 0.
-template <typename T, int DP, int W> struct QueryTiles {
-  using Gm = AskGeo<T, DP, W>;
-  TileLoad<T, DP, W> q, d;
+template <typename T, int DP, int W, int ROWS> struct QueryTiles {
+  using Gm = AskGeo<T, DP, W, ROWS>;
+  TileLoad<T, DP, W, ROWS> q, d;
   const T *Q, *DO;
   const float *lse, *delta;
   int64_t ldq, lddo, Nq;
@@ -286,16 +286,16 @@ template <typename T, int DP, int W> struct QueryTiles {
     DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * D + b * lddo;
     lse = a.lse + (int64_t)h * G * Nq + b;
     delta = a.delta + (int64_t)h * G * Nq + b;
-    if (64 % G == 0) places(0);
+    if (ROWS % G == 0) places(0);
   }
   __device__ __forceinline__ void places(int rem) {
     q.queries(ldq, G, rem, D);
     d.queries(lddo, G, rem, D);
   }
   __device__ __forceinline__ void load(int v0, char* tiles) {
-    const int rows = n - v0 < kTile ? n - v0 : kTile;
+    const int rows = n - v0 < ROWS ? n - v0 : ROWS;
     const int i0 = G == 1 ? v0 : v0 / G, i1 = G == 1 ? v0 + rows - 1 : (v0 + rows - 1) / G;
-    if (64 % G) places(v0 - i0 * G);  // (tiles do not begin at a query)
+    if (ROWS % G) places(v0 - i0 * G);  // (tiles do not begin at a query)
     const Buffer bq = buffer_of(Q + i0 * ldq, ((i1 - i0) * ldq + G * D) * Gm::SZ);
     const Buffer bd = buffer_of(DO + i0 * lddo, ((i1 - i0) * lddo + G * D) * Gm::SZ);
 #pragma unroll
@@ -424,6 +424,46 @@ template <typename V> __device__ __forceinline__ V add_groups(V v, V* lds, int u
     if (u < half) v += lds[u * P + at];
   }
   return v;
+}
+
+// Of a block's 256 threads; lds: four floats of the call's own.
+__device__ __forceinline__ float block_largest(float v, float* lds) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) v = fmaxf(v, __shfl_xor(v, m));
+  if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+__device__ __forceinline__ float block_sum(float v, float* lds) {
+#pragma unroll
+  for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
+  if (lane_id() == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+// Is a row one of a request's?
+__device__ __forceinline__ bool asked_for(const AskArgs& a, int64_t row) {
+  return !a.q_off || (row >= a.q_off[0] && row < a.q_off[a.R]);
+}
+
+// How pieces are joined: up to 8 one behind the other by a thread, many rows to a block
+// (U = 0); more by a block for P fours of a row's elements, whose U groups of threads take
+// every U-th piece, all loads of a thread on their way together.  us, of calls with 256
+// pieces, with a thread for a row's four, a block for a row, and so: 62 queries of 4 heads over
+// 181,477 states 160, 41, 39; 4 queries over 60,000 states, 128 wide, fp32: -, 48, 33; one of 8
+// heads over 20,000 -, 19, 12.5.
+struct Join {
+  int P, U;
+  dim3 grid;
+};
+inline Join join_of(const AskArgs& a) {
+  const int per = a.D / 4;
+  const int64_t rows = a.Nq * a.Hq;
+  if (a.S <= 8) return {256 / per, 0, dim3((uint32_t)((rows + 256 / per - 1) / (256 / per)))};
+  const int blocks = (per + 7) / 8, P = (per + blocks - 1) / blocks;
+  int U = 1;
+  while (2 * U * P <= 256 && 2 * U <= a.S) U *= 2;
+  return {P, U, dim3((uint32_t)rows, blocks)};
 }
 
 // f(type, std::integral_constant of the width rounded up): fp32 is padded to multiples

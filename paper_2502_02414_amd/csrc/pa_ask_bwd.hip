@@ -201,46 +201,57 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   }
 }
 
-// dq's pieces joined, as k_ask_join.
-template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a, int rows_, int U) {
-  constexpr bool FIX = sizeof(T) == 2;
-  __shared__ f32x4 lds[256];
-  __shared__ float ldse[256], ldsr[256];
-  const int per = a.D / 4, item = threadIdx.x / (per * U), in = threadIdx.x % (per * U);
-  const int u = item < rows_ ? in / per : U, c = (in % per) * 4;  // (U: a thread too many)
-  const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * rows_ + item;
-  const bool on = item < rows_ && at < rows;
-  const int64_t row = on ? at / a.Hq : 0, first = a.q_off ? a.q_off[0] : 0;
-  const int64_t behind = a.q_off ? a.q_off[a.R] : a.Nq;
-  const bool write = on && row >= first && row < behind;
-  float e = 0.f, er = 0.f;
-  f32x4 A = zero4(), B = zero4();
-  if (write)
-    for (int s = u; s < a.S; s += U) {
-      e += a.part_lse[s * rows + at];
-      if constexpr (FIX) er += a.part_e[s * rows + at];
-      A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
-      if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
-    }
-  if (U > 1) {
-    A = add_groups(A, lds, u, U, in % per, per);
-    if constexpr (FIX) B = add_groups(B, lds, u, U, in % per, per);
-    e = add_groups(e, ldse, u, U, in % per, per);
-    if constexpr (FIX) er = add_groups(er, ldsr, u, U, in % per, per);
-  }
-  if (!write || u) return;
-  const int hq = (int)(at - row * a.Hq);
-  if constexpr (FIX) A -= B * er;
+// dq's pieces joined as the forward's are (join_of).
+template <typename T>
+__device__ __forceinline__ void put_joined(const AskArgs& a, int64_t row, int hq, int c, f32x4 A,
+                                           const f32x4& B, float e, float er) {
+  if constexpr (sizeof(T) == 2) A -= B * er;
   store4<T>(reinterpret_cast<T*>(a.dq) + row * a.lddq + (int64_t)hq * a.D + c, A * a.scale);
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
 }
+template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a, int each) {
+  constexpr bool FIX = sizeof(T) == 2;
+  const int per = a.D / 4, item = threadIdx.x / per, c = (threadIdx.x % per) * 4;
+  const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * each + item, row = at / a.Hq;
+  if (item >= each || at >= rows || !asked_for(a, row)) return;
+  float e = 0.f, er = 0.f;
+  f32x4 A = zero4(), B = zero4();
+  for (int s = 0; s < a.S; ++s) {
+    e += a.part_lse[s * rows + at];
+    if constexpr (FIX) er += a.part_e[s * rows + at];
+    A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
+    if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+  }
+  put_joined<T>(a, row, (int)(at - row * a.Hq), c, A, B, e, er);
+}
+template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join_many(AskArgs a, int P, int U) {
+  constexpr bool FIX = sizeof(T) == 2;
+  __shared__ float alle[4], allr[4];
+  __shared__ f32x4 lds[256];
+  const int64_t rows = a.Nq * a.Hq, at = blockIdx.x, row = at / a.Hq;
+  if (!asked_for(a, row)) return;
+  const int t = threadIdx.x, u = t / P, c = 4 * ((int)blockIdx.y * P + t % P);
+  f32x4 A = zero4(), B = zero4();
+  if (u < U && c < a.D) {
+#pragma unroll 8
+    for (int s = u; s < a.S; s += U) {
+      A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
+      if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+    }
+  }
+  const float e = block_sum(t < a.S ? a.part_lse[t * rows + at] : 0.f, alle);
+  const float er = FIX ? block_sum(t < a.S ? a.part_e[t * rows + at] : 0.f, allr) : 0.f;
+  A = add_groups(A, lds, u, U, t % P, P);
+  if constexpr (FIX) B = add_groups(B, lds, u, U, t % P, P);
+  if (u == 0 && c < a.D) put_joined<T>(a, row, (int)(at - row * a.Hq), c, A, B, e, er);
+}
 
 // dk and dv of a tile of 16 KT W states: a wave has KT times 16 of them as columns, and
-// their rows of k and v in registers; the queries come through LDS.
-template <typename T, int DP, int KT, int W>
+// their rows of k and v in registers; the queries come through LDS, 16 NR rows at a time.
+template <typename T, int DP, int KT, int W, int NR>
 __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dkv(AskArgs a) {
-  using Gm = AskGeo<T, DP, W>;
-  constexpr int TK = 16 * KT * W, SHIFT = TK == 64 ? 6 : TK == 128 ? 7 : 8;
+  constexpr int ROWS = 16 * NR, TK = 16 * KT * W, SHIFT = TK == 64 ? 6 : TK == 128 ? 7 : 8;
+  using Gm = AskGeo<T, DP, W, ROWS>;
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float stat0[2 * kTile], stat1[2 * kTile];  // lse (base 2), delta
   const int G = a.Hq / a.Hkv;
@@ -255,7 +266,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   const int n = (int)vr.e;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
-  QueryTiles<T, DP, W> st;
+  QueryTiles<T, DP, W, ROWS> st;
   st.init(a, h, qr.b, n);
   const int first = (int)vr.b;
   if (first < n) st.load(first, tiles0);
@@ -282,9 +293,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   if (first < n) st.put(stat0);
   auto work = [&](const char* qt, const float* stat) __attribute__((always_inline)) {
     const char* dt = qt + Gm::TB;
-    f32x4 x[4][KT], dp[4][KT];
+    f32x4 x[NR][KT], dp[NR][KT];
     __builtin_amdgcn_s_setprio(1);
-    pipelined<4 * Gm::NK, 3, WidePair<T>>(
+    pipelined<NR * Gm::NK, 3, WidePair<T>>(
         [&](int i, WidePair<T>& f) {
           at.rows(f.a, qt, i / Gm::NK, i % Gm::NK);
           at.rows(f.b, dt, i / Gm::NK, i % Gm::NK);
@@ -299,7 +310,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
         });
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-    for (int t0 = 0; t0 < 4; t0 += 2) {
+    for (int t0 = 0; t0 < NR; t0 += 2) {
       K16<T> pf[KT][2], sf[KT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
@@ -339,14 +350,14 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   auto turn = [&](int v0, const char* now, const float* stat, char* next, float* stat_next)
                   __attribute__((always_inline)) {
     tiles_ready();
-    const bool more = v0 + kTile < n;
-    if (more) st.load(v0 + kTile, next);
+    const bool more = v0 + ROWS < n;
+    if (more) st.load(v0 + ROWS, next);
     if (busy) work(now, stat);
     if (more) st.put(stat_next);
   };
-  for (int v0 = first; v0 < n; v0 += 2 * kTile) {
+  for (int v0 = first; v0 < n; v0 += 2 * ROWS) {
     turn(v0, tiles0, stat0, tiles1, stat1);
-    if (v0 + kTile < n) turn(v0 + kTile, tiles1, stat1, tiles0, stat0);
+    if (v0 + ROWS < n) turn(v0 + ROWS, tiles1, stat1, tiles0, stat0);
   }
 #pragma unroll
   for (int c = 0; c < KT; ++c) {
@@ -404,9 +415,9 @@ template <typename T, int DP, int QT, int W> hipError_t launch_dq(const AskArgs&
                      st, a);
   return hipGetLastError();
 }
-template <typename T, int DP, int KT, int W> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
+template <typename T, int DP, int KT, int W, int NR = 4> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
   const int64_t slots = a.Nk / (16 * KT * W) + a.R;
-  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W>), grid_of(slots * a.Hkv, a.SQ), dim3(64 * W),
+  hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W, NR>), grid_of(slots * a.Hkv, a.SQ), dim3(64 * W),
                      0, st, a);
   return hipGetLastError();
 }
@@ -419,7 +430,12 @@ int rows_dq(const AskArgs& a, int dtype) {
   if (ask_eight(a, dtype)) return 128;
   return a.D <= 32 || !ask_large(a, dtype, true) ? 64 : a.D <= 64 ? 256 : 128;
 }
+// Requests of 32 virtual rows or fewer (on average): dk and dv's pass in tiles of 32, not of 64
+// (4 queries of 16 heads over 262,808 states of 4 heads of 64, fp32, the call: 394 and 507 us;
+// 20 of 4 heads over 300,000, bf16: 231 and 244).
+bool few_rows(const AskArgs& a) { return a.Nq * (a.Hq / a.Hkv) <= 32 * (int64_t)a.R; }
 int rows_dkv(const AskArgs& a, int dtype) {
+  if (few_rows(a)) return 64;
   if (ask_eight(a, dtype)) return 128;
   const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = a.Nk / a.R;
   const bool large = dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && rows / a.R >= 128 &&
@@ -442,10 +458,13 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
     });
     if (e != hipSuccess) return e;
     if (a.S > 1) {
-      const AskJoin j = ask_join(a);
-      const dim3 grid((uint32_t)((a.Nq * a.Hq + j.rows - 1) / j.rows));
-      if (dtype == 1) hipLaunchKernelGGL(k_ask_dq_join<bf16>, grid, dim3(256), 0, st, a, j.rows, j.U);
-      else hipLaunchKernelGGL(k_ask_dq_join<float>, grid, dim3(256), 0, st, a, j.rows, j.U);
+      const Join j = join_of(a);
+      const auto go = [&](auto type) {
+        using T = decltype(type);
+        if (j.U) hipLaunchKernelGGL(k_ask_dq_join_many<T>, j.grid, dim3(256), 0, st, a, j.P, j.U);
+        else hipLaunchKernelGGL(k_ask_dq_join<T>, j.grid, dim3(256), 0, st, a, j.P);
+      };
+      dtype == 1 ? go(bf16{}) : go(float{});
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -458,7 +477,7 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
       if (large) return launch_dkv<T, DP, DP <= 64 ? 2 : 1, 8>(a, st);
     if constexpr (sizeof(T) == 4 && DP > 64)
       if (large) return launch_dkv<T, DP, 1, 8>(a, st);
-    return launch_dkv<T, DP, 1, 4>(a, st);
+    return few_rows(a) ? launch_dkv<T, DP, 1, 4, 2>(a, st) : launch_dkv<T, DP, 1, 4>(a, st);
   });
   if (e != hipSuccess || a.SQ == 1) return e;
   const int U = a.SQ <= 8 ? 1 : a.SQ <= 64 ? 8 : 32;

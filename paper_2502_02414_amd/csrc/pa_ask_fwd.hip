@@ -177,50 +177,53 @@ k_ask(AskArgs a) {
   }
 }
 
-// The pieces of the states joined: a block has a head of `rows_` rows, a thread four
-// elements of one, of every U-th piece.
-template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs a, int rows_, int U) {
-  __shared__ float top[256], weight[256];
-  __shared__ f32x4 lds[256];
-  const int per = a.D / 4, item = threadIdx.x / (per * U), in = threadIdx.x % (per * U);
-  const int u = item < rows_ ? in / per : U, c = (in % per) * 4;  // (U: a thread too many)
-  const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * rows_ + item;
-  const bool on = item < rows_ && at < rows;
-  const int64_t row = on ? at / a.Hq : 0, first = a.q_off ? a.q_off[0] : 0;
-  const int64_t behind = a.q_off ? a.q_off[a.R] : a.Nq;
-  const bool write = on && row >= first && row < behind;
-  float m = -INFINITY;
-  if (write)
-    for (int s = u; s < a.S; s += U) m = fmaxf(m, a.part_lse[s * rows + at]);
-  if (U > 1) {  // (one row to a block: the largest of all its pieces)
-    top[threadIdx.x] = m;
-    for (int half = 128; half > 0; half >>= 1) {
-      __syncthreads();
-      if ((int)threadIdx.x < half) top[threadIdx.x] = fmaxf(top[threadIdx.x], top[threadIdx.x + half]);
-    }
-    __syncthreads();
-    m = top[0];
-  }
-  const float base = m == -INFINITY ? 0.f : m;
-  float sum = 0.f;
-  f32x4 o = zero4();
-  if (write)
-    for (int s = u; s < a.S; s += U) {
-      const float w = fast_exp2(a.part_lse[s * rows + at] - base);
-      const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
-      sum += w;
-      o += x * w;
-    }
-  if (U > 1) {
-    o = add_groups(o, lds, u, U, in % per, per);
-    sum = add_groups(sum, weight, u, U, in % per, per);
-  }
-  if (!write || u) return;
-  const int hq = (int)(at - row * a.Hq);
+// A row's answer from the sum of its pieces' answers, weighted.
+template <typename T>
+__device__ __forceinline__ void put_joined(const AskArgs& a, int64_t row, int hq, int c, const f32x4& o,
+                                           float sum, float base) {
   const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
   store4<T>(reinterpret_cast<T*>(a.o) + row * a.ldo + (int64_t)hq * a.D + c, o * inv);
   if (a.lse && c == 0)
     a.lse[(int64_t)hq * a.Nq + row] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * kLn2;
+}
+// The pieces of the states joined (join_of): up to 8, a thread four elements of a row.
+template <typename T> __global__ void __launch_bounds__(256) k_ask_join(AskArgs a, int each) {
+  const int per = a.D / 4, item = threadIdx.x / per, c = (threadIdx.x % per) * 4;
+  const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * each + item, row = at / a.Hq;
+  if (item >= each || at >= rows || !asked_for(a, row)) return;
+  float m = -INFINITY;
+  for (int s = 0; s < a.S; ++s) m = fmaxf(m, a.part_lse[s * rows + at]);
+  const float base = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4 o = zero4();
+  for (int s = 0; s < a.S; ++s) {
+    const float w = fast_exp2(a.part_lse[s * rows + at] - base);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
+    sum += w;
+    o += x * w;
+  }
+  put_joined<T>(a, row, (int)(at - row * a.Hq), c, o, sum, base);
+}
+// More: a block four times P elements of a row.
+template <typename T> __global__ void __launch_bounds__(256) k_ask_join_many(AskArgs a, int P, int U) {
+  __shared__ float top[4], all[4], weight[256];
+  __shared__ f32x4 lds[256];
+  const int64_t rows = a.Nq * a.Hq, at = blockIdx.x, row = at / a.Hq;
+  if (!asked_for(a, row)) return;
+  const int t = threadIdx.x, u = t / P, c = 4 * ((int)blockIdx.y * P + t % P);
+  const float l = t < a.S ? a.part_lse[t * rows + at] : -INFINITY;
+  const float m = block_largest(l, top), base = m == -INFINITY ? 0.f : m;
+  const float w = t < a.S ? fast_exp2(l - base) : 0.f;
+  weight[t] = w;
+  const float sum = block_sum(w, all);  // (with a barrier: the weights are there)
+  f32x4 o = zero4();
+  if (u < U && c < a.D) {
+#pragma unroll 8
+    for (int s = u; s < a.S; s += U)
+      o += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c) * weight[s];
+  }
+  o = add_groups(o, lds, u, U, t % P, P);
+  if (u == 0 && c < a.D) put_joined<T>(a, row, (int)(at - row * a.Hq), c, o, sum, base);
 }
 
 template <typename T, int DP, int QT, int W> hipError_t launch(const AskArgs& a, hipStream_t st) {
@@ -299,17 +302,6 @@ int ask_pieces(const AskArgs& a, int dtype) {
                        4.0 * a.Nq * a.Hq * (a.D + 1));
 }
 
-// Eight pieces or fewer one after the other, many rows to a block; more by groups of
-// threads, a row to a block (62 queries of 4 heads over 181,477 states, in
-// 256 pieces: 160 us for the call where it takes 39 so).
-AskJoin ask_join(const AskArgs& a) {
-  const int per = a.D / 4;
-  if (a.S <= 8) return {256 / per, 1};
-  int U = 1;
-  while (2 * U * per <= 256 && 2 * U <= a.S) U *= 2;
-  return {1, U};
-}
-
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
   hipError_t e;
   if (ask_few_served(a, dtype)) {
@@ -323,10 +315,13 @@ hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
   }
   e = width(a, dtype, st);
   if (e != hipSuccess || a.S == 1) return e;
-  const AskJoin j = ask_join(a);
-  const dim3 grid((uint32_t)((a.Nq * a.Hq + j.rows - 1) / j.rows));
-  if (dtype == 1) hipLaunchKernelGGL(k_ask_join<bf16>, grid, dim3(256), 0, st, a, j.rows, j.U);
-  else hipLaunchKernelGGL(k_ask_join<float>, grid, dim3(256), 0, st, a, j.rows, j.U);
+  const Join j = join_of(a);
+  const auto go = [&](auto type) {
+    using T = decltype(type);
+    if (j.U) hipLaunchKernelGGL(k_ask_join_many<T>, j.grid, dim3(256), 0, st, a, j.P, j.U);
+    else hipLaunchKernelGGL(k_ask_join<T>, j.grid, dim3(256), 0, st, a, j.P);
+  };
+  dtype == 1 ? go(bf16{}) : go(float{});
   return hipGetLastError();
 }
 

@@ -142,10 +142,6 @@ int ask_resident(const AskArgs& a, int dtype, bool eight, bool backward);
 int ask_pieces(const AskArgs& a, int dtype);     // S, forward
 int ask_pieces_dq(const AskArgs& a, int dtype);  // S, backward
 int ask_pieces_q(const AskArgs& a, int dtype);   // SQ
-struct AskJoin {
-  int rows, U;  // rows of a head to a block, groups of threads to a row
-};
-AskJoin ask_join(const AskArgs& a);
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
 // Few states (pa_ask_few.hip): served, and faster.
 bool ask_few_served(const AskArgs& a, int dtype);
