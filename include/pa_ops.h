@@ -238,8 +238,9 @@ typedef struct {
   const int64_t* k_off;    /* outside of the tensor count as its ends); both, or */
                            /* both NULL with R = 1: all rows                     */
   const uint8_t* mask;     /* [Nk] on the device, nullable: 0 leaves a state out */
-  int64_t max_k;           /* states of the longest request, 0: not known.  It   */
-                           /* steers the choice of a kernel, not the result      */
+  int64_t max_k;           /* states of the longest request, 0: not known, which  */
+                           /* may be slower; a request of more than that may have */
+                           /* NaN for its answers and gradients                   */
 } pa_cross_attention_params;
 
 /* lse nullable.  Workspace: pa_cross_attention_workspace bytes (may be 0). */

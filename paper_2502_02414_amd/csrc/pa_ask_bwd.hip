@@ -48,12 +48,11 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   const int64_t slot = block_of() / (uint32_t)a.Hkv;
   Place pl;
   if (!place_of(pl, a.q_off, a.Nq, a.k_off, a.Nk, a.R, G, SHIFT, slot)) return;
-  const Range qr = pl.mine, all = pl.theirs, kr = piece(all, s, a.S);
+  const Range qr = pl.mine, kr = piece(pl.theirs, s, a.S);
   const int n = (int)(qr.e - qr.b) * G;
   const int64_t tile = slot - ((qr.b * G) >> SHIFT) - pl.r;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   StateTiles<T, DP, W> st;
@@ -261,7 +260,7 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   if (!place_of(pl, a.k_off, a.Nk, a.q_off, a.Nq, a.R, 1, SHIFT, slot)) return;
   const Range kr = pl.mine, qr = pl.theirs;
   const int64_t tile = slot - (kr.b >> SHIFT) - pl.r;
-  if (tile < 0 || tile * TK >= kr.e - kr.b || kr.e - kr.b <= a.few) return;
+  if (tile < 0 || tile * TK >= kr.e - kr.b) return;
   const Range vr = piece(Range{0, (qr.e - qr.b) * G}, s, a.SQ);  // virtual rows
   const int n = (int)vr.e;
 
@@ -437,7 +436,7 @@ bool few_rows(const AskArgs& a) { return a.Nq * (a.Hq / a.Hkv) <= 32 * (int64_t)
 int rows_dkv(const AskArgs& a, int dtype) {
   if (few_rows(a)) return 64;
   if (ask_eight(a, dtype)) return 128;
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = a.Nk / a.R;
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = (a.Nk + a.R - 1) / a.R;
   const bool large = dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && rows / a.R >= 128 &&
                      (a.Nk + 255) / 256 * a.Hkv * (rows / a.R / kTile) >= (a.D <= 64 ? 4096 : 2048);
   return a.D <= 32 || !large ? 64 : a.D <= 64 ? 256 : 128;
@@ -509,14 +508,7 @@ int ask_pieces_q(const AskArgs& a, int dtype) {
 }
 
 hipError_t launch_ask_backward(const AskArgs& a, int dtype, hipStream_t st) {
-  if (!ask_few_backward_served(a, dtype)) return passes(a, dtype, st);
-  const hipError_t e = launch_ask_few_backward(a, st);
-  if (e != hipSuccess || a.R == 1 || a.Nk <= ask_few_most(a)) return e;
-  // (a request that is longer than max_k says)
-  AskArgs rest = a;
-  rest.few = ask_few_most(a);
-  rest.S = rest.SQ = 1;
-  return passes(rest, dtype, st);
+  return ask_few_backward_served(a, dtype) ? launch_ask_few_backward(a, st) : passes(a, dtype, st);
 }
 
 }  // namespace pa

@@ -72,7 +72,8 @@ template <int DP, int NT> struct States {
         ld_tr<bf16>(f[d][t], mine, at, 16 * t * RB + 64 * (d >> 1) + 8 * (d & 1), RB);
     wave_sync();
   }
-  // 0, or -infinity where a state is left out; whether one is not
+  // 0, or -infinity where a state is left out; NaN in a request of more states than max_k
+  // says, so that its answers are; whether one counts
   static __device__ __forceinline__ bool alive(f32x4 (&f)[NT], Range k, const uint8_t* mask) {
     const int g = lane_id() >> 4;
     bool some = false;
@@ -83,7 +84,7 @@ template <int DP, int NT> struct States {
         const int64_t p = k.b + 16 * t + 4 * g + i;
         bool counts = p < k.e;
         if (mask && k.b < k.e) counts = counts && mask[counts ? p : k.e - 1];
-        f[t][i] = counts ? 0.f : -INFINITY;
+        f[t][i] = k.e - k.b > 16 * NT ? NAN : counts ? 0.f : -INFINITY;
         some = some || counts;
       }
     return __any(some);
@@ -149,8 +150,6 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
   bf16* O = reinterpret_cast<bf16*>(a.o) + (int64_t)me.h * G * a.D + qr.b * a.ldo;
   const float sc = a.scale * kLog2e;
 
-  // (longer ones are the other kernel's, none has no states to read)
-  if (kr.e - kr.b > 16 * NT) return;
   f32x4 none[NT];
   // of q: none is read where no state counts, so that no NaN is
   const int D = S_::alive(none, kr, a.mask) ? a.D : 0;
@@ -267,8 +266,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   const int rq = blockIdx.x / P;
   const Range qr = range_of(a.q_off, rq, a.Nq), kr = range_of(a.k_off, rq, a.Nk);
   const int n = (int)(qr.e - qr.b) * G, pc = blockIdx.x % P;
-  // (requests that are longer are the other kernels')
-  if (me.h >= a.Hkv || me.sub >= me.subs || kr.e - kr.b > 16 * NT) return;
+  if (me.h >= a.Hkv || me.sub >= me.subs) return;
   const int lane = lane_id(), r = lane & 15, g = lane >> 4;
   const int64_t head = (int64_t)me.h * G * a.D;
   const bf16* Q = reinterpret_cast<const bf16*>(a.q) + head + qr.b * a.ldq;
@@ -453,23 +451,26 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 __global__ void __launch_bounds__(256) k_ask_few_sum(AskArgs a, int per, int64_t rec, int blocks) {
   __shared__ f32x4 part[8][32];
   const int rq = blockIdx.x / blocks, u = threadIdx.x >> 5, c = threadIdx.x & 31;
-  const int64_t e = ((int64_t)(blockIdx.x % blocks) * 32 + c) * 4, width = (int64_t)a.Hkv * a.D;
+  const int64_t first = ((int64_t)(blockIdx.x % blocks) * 32 + c) * 4, width = (int64_t)a.Hkv * a.D;
   const Range kr = range_of(a.k_off, rq, a.Nk);
   const int64_t n = (kr.e - kr.b) * width;
-  if (n > rec) return;  // (not this kernel's)
   const float* p = (blockIdx.y ? a.part_v : a.part_k) + (int64_t)rq * per * rec;
   f32x4 s = zero4();
-  if (e < n)
-    for (int i = u; i < per; i += 8) s += *reinterpret_cast<const f32x4*>(p + i * rec + e);
+  if (first < n)
+    for (int i = u; i < per; i += 8) s += *reinterpret_cast<const f32x4*>(p + i * rec + first);
   part[u][c] = s;
   __syncthreads();
-  if (u || e >= n) return;
+  if (u) return;
 #pragma unroll
   for (int i = 1; i < 8; ++i) s += part[i][c];
-  const int64_t row = e / width, col = e - row * width;
-  if (a.mask && !a.mask[kr.b + row]) s = zero4();  // (weights of 0, of a do that is NaN, too)
   bf16* to = reinterpret_cast<bf16*>(blockIdx.y ? a.dv : a.dk);
-  store4<bf16>(to + (kr.b + row) * (blockIdx.y ? a.lddv : a.lddk) + col, s);
+  for (int64_t e = first; e < n; e += 128 * (int64_t)blocks) {
+    if (n > rec) s = f32x4{NAN, NAN, NAN, NAN};  // (more states than max_k says)
+    const int64_t row = e / width, col = e - row * width;
+    // (weights of 0, of a do that is NaN, too)
+    store4<bf16>(to + (kr.b + row) * (blockIdx.y ? a.lddv : a.lddk) + col,
+                 a.mask && !a.mask[kr.b + row] ? zero4() : s);
+  }
 }
 
 // Blocks of a request, and how many waves of a block share a head.  Forward: whole rounds of
@@ -520,7 +521,6 @@ hipError_t sizes(const AskArgs& a, bool bwd, hipStream_t st) {
 bool ask_few_served(const AskArgs& a, int dtype) {
   return dtype == 1 && a.D <= 64 && a.max_k <= 64 && a.R <= (1 << 20);
 }
-int ask_few_most(const AskArgs& a) { return 16 * tiles_of(a); }
 
 // Floats of the backward's records of dk, or of dv.
 int64_t ask_few_records(const AskArgs& a) {

@@ -40,12 +40,11 @@ k_ask(AskArgs a) {
   const int64_t slot = block_of() / (uint32_t)a.Hkv;
   Place pl;
   if (!place_of(pl, a.q_off, a.Nq, a.k_off, a.Nk, a.R, G, SHIFT, slot)) return;
-  const Range qr = pl.mine, all = pl.theirs, kr = piece(all, s, a.S);
+  const Range qr = pl.mine, kr = piece(pl.theirs, s, a.S);
   const int n = (int)(qr.e - qr.b) * G;
   const int64_t tile = slot - ((qr.b * G) >> SHIFT) - pl.r;
   if (tile < 0 || tile * TQ >= n) return;
   const int v0 = (int)tile * TQ;
-  if (all.e - all.b <= a.few) return;
 
   const int lane = lane_id(), r = lane & 15, g = lane >> 4, w = threadIdx.x >> 6;
   const T* Q = reinterpret_cast<const T*>(a.q) + (int64_t)h * G * a.D;
@@ -254,7 +253,8 @@ hipError_t width(const AskArgs& a, int dtype, hipStream_t st) {
 // squared 45 and 58, of 128 wide 59 and 53, 2,048 squared 28 and 35; dq's pass of 4,096
 // squared of 64 wide 5 more and less.
 bool ask_large(const AskArgs& a, int dtype, bool backward) {
-  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = rows / a.R, tiles = a.Nk / a.R / kTile;
+  const int64_t rows = a.Nq * (a.Hq / a.Hkv), each = (rows + a.R - 1) / a.R;
+  const int64_t tiles = a.Nk / a.R / kTile;
   return dtype == 1 && 5 * each >= 4 * ((each + 255) / 256 * 256) && tiles >= 2 &&
          (rows + 255) / 256 * a.Hkv * tiles >= (a.D > 64 ? 2048 : backward ? 4096 : 8192);
 }
@@ -303,17 +303,8 @@ int ask_pieces(const AskArgs& a, int dtype) {
 }
 
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st) {
-  hipError_t e;
-  if (ask_few_served(a, dtype)) {
-    e = launch_ask_few(a, st);
-    if (e != hipSuccess || a.R == 1 || a.Nk <= ask_few_most(a)) return e;
-    // (a request that is longer than max_k says)
-    AskArgs rest = a;
-    rest.few = ask_few_most(a);
-    rest.S = 1;
-    return width(rest, dtype, st);
-  }
-  e = width(a, dtype, st);
+  if (ask_few_served(a, dtype)) return launch_ask_few(a, st);
+  const hipError_t e = width(a, dtype, st);
   if (e != hipSuccess || a.S == 1) return e;
   const Join j = join_of(a);
   const auto go = [&](auto type) {

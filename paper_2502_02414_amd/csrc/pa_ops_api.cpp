@@ -572,7 +572,7 @@ static pa_status ask_params(const char* who, int64_t Nq, int64_t Nk, int dtype,
   PO_TRY(opt(who, p->k_off, "k_off", 8));
   a->Nq = Nq; a->Nk = Nk; a->R = p->R; a->Hq = p->Hq; a->Hkv = p->Hkv; a->D = p->D;
   a->scale = p->scale; a->q_off = p->q_off; a->k_off = p->k_off; a->mask = p->mask;
-  a->max_k = p->max_k && p->max_k < Nk ? p->max_k : Nk;
+  a->max_k = p->k_off && p->max_k && p->max_k < Nk ? p->max_k : Nk;
   return PA_OK;
 }
 // A tensor of N rows of H heads, given with the elements between its rows; without
@@ -607,7 +607,6 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
     const uint64_t n = (uint64_t)pa::ask_few_records(*a);
     a->part_k = take(n);
     a->part_v = take(n);
-    a->delta = take(rows);  // (for requests that are longer than max_k says)
     return at;
   }
   a->S = backward ? pa::ask_pieces_dq(*a, dtype) : pa::ask_pieces(*a, dtype);

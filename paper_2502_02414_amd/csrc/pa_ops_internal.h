@@ -116,7 +116,6 @@ struct AskArgs {
   const int64_t *q_off = nullptr, *k_off = nullptr;  // [R + 1], both or none (R = 1)
   const uint8_t* mask = nullptr;                     // [Nk]
   int64_t max_k = 0;  // states of the longest request, as the caller knows it
-  int few = -1;       // requests of at most so many states are another kernel's
   int64_t ldq = 0, ldk = 0, ldv = 0, ldo = 0;        // elements between rows
   const void *q = nullptr, *k = nullptr, *v = nullptr;
   void* o = nullptr;     // (read by the backward)
@@ -145,7 +144,6 @@ int ask_pieces_q(const AskArgs& a, int dtype);   // SQ
 hipError_t launch_ask(const AskArgs& a, int dtype, hipStream_t st);
 // Few states (pa_ask_few.hip): served, and faster.
 bool ask_few_served(const AskArgs& a, int dtype);
-int ask_few_most(const AskArgs& a);  // the most states of a request that it serves
 hipError_t launch_ask_few(const AskArgs& a, hipStream_t st);
 bool ask_few_backward_served(const AskArgs& a, int dtype);
 int64_t ask_few_records(const AskArgs& a);  // floats of its records in part_k, and in part_v

@@ -325,13 +325,36 @@ def test_a_padded_batch():
     assert (o[2 * L:3 * L] == 0).all()
 
 
-def test_max_k_steers_the_choice_alone():
-    """Too small a max_k, none and the right one: results within the bounds."""
-    for max_k in (0, 1, 64, 1000):
-        c = Case((300, 200), (64, 200), 8, 8, 32, BF16)
-        c.par.st.max_k = max_k
-        c.check_forward()
-        c.check_backward()
+@pytest.mark.parametrize("max_k", [0, 200, 1000])
+def test_max_k_steers_the_choice(max_k):
+    """None, the right one and a larger one: results within the bounds."""
+    c = Case((300, 200), (64, 200), 8, 8, 32, BF16)
+    c.par.st.max_k = max_k
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("max_k", [1, 32, 64])
+def test_a_request_of_more_states_than_max_k(max_k):
+    """Its answers and gradients are NaN, in all of its rows and in no other's."""
+    c = Case((300, 200, 50), (20, 200, 9), 8, 8, 32, BF16, "some", first=1, tail=2)
+    o, lse = c.forward()
+    right = (o, lse) + c.backward(o, lse)
+    c.par.st.max_k = max_k
+    o, lse = c.forward()
+    q, k = slice(301, 501), slice(21, 221)
+    assert torch.isnan(o[q]).all() and torch.isnan(lse[:, q]).all()
+    dq, dk, dv = c.backward(right[0], right[1])
+    assert torch.isnan(dq[q]).all()
+    on = c.mask.cuda()
+    for t in (dk, dv):
+        assert torch.isnan(t[k][on[k]]).all() and (t[k][~on[k]] == 0).all()
+    for got, want, rows in ((o, right[0], q), (lse.t(), right[1].t(), q), (dq, right[2], q),
+                            (dk, right[3], k), (dv, right[4], k)):
+        keep = torch.ones(got.shape[0], dtype=torch.bool, device="cuda")
+        keep[rows] = False
+        a, b = got[keep].float(), want[keep].float()
+        assert torch.isfinite(a).all() and ((a - b).abs() <= 0.05 * b.abs() + 0.05 * b.abs().max()).all()
 
 
 def test_offsets_outside_of_the_tensors():
