@@ -494,14 +494,14 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
 int ask_pieces_dq(const AskArgs& a, int dtype) {
   const int rows = rows_dq(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 * 4 : 32.0 * 3) * a.D;
-  return ask_pieces_of((a.Nq * (a.Hq / a.Hkv) / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
+  return ask_pieces_of(ask_blocks(a.Nq * (a.Hq / a.Hkv), a.R, rows) * a.Hkv, rows > 64 ? 8 : 4,
                        ask_resident(a, dtype, rows > 64, true), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
                        (dtype == 1 ? 8.0 : 4.0) * a.Nq * a.Hq * (a.D + 1));
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {
   const int rows = rows_dkv(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 : 32.0) * 4 * a.D;
-  return ask_pieces_of((a.Nk / rows + a.R) * a.Hkv, rows > 64 ? 8 : 4,
+  return ask_pieces_of(ask_blocks(a.Nk, a.R, rows) * a.Hkv, rows > 64 ? 8 : 4,
                        ask_resident(a, dtype, rows > 64, true), tiles_of * cycles,
                        (a.Nq * (a.Hq / a.Hkv) / a.R + kTile - 1) / kTile,
                        8.0 * a.Nk * a.Hkv * a.D);

@@ -267,19 +267,30 @@ bool ask_eight(const AskArgs& a, int dtype) {
   return dtype == 0 && a.D > 64 && rows * a.Hkv * ((a.Nk / a.R + kTile - 1) / kTile) >= 1024;
 }
 
+// Blocks of R requests of some N rows in all (none has more than it takes on average), of `rows` each.
+int64_t ask_blocks(int64_t N, int64_t R, int rows) {
+  return R * (((N + R - 1) / R + rows - 1) / rows);
+}
 // The number of pieces whose time comes out shortest: blocks of `waves` that take `cycles`
 // for each of `tiles` tiles.  n waves of a SIMD share it, up to `resident`, in n + 1 times
-// one's cycles (none is faster than 2000); a block's start is 6000; several pieces are joined,
-// `bytes` each at 1.5 KB a cycle, by a launch of 6000.
+// one's cycles (none is faster than 2000); a block's start is 6000; what does not fit comes in
+// rounds, of which the last one is one more where a CU has one block at a time, and a part
+// of one where it has several, whose ends differ; several pieces are joined, `bytes` each at 1.5 KB a
+// cycle, by a launch of 6000.  (us, the pieces that it chooses and others: 10,792 queries over
+// 17,721 states of 4 heads of 80, 4 pieces 364, 1 450, 2 461, 8 386; 643 over 14,654 of 8 of 32,
+// 16 42, 1 147, 4 53; 16,384 squared of 4 of 64, 2 333, 1 391, 4 325.)
 int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
                   double bytes) {
   int best = 1;
   double least = 0;
+  const int64_t once = 1024 * resident / waves;
   for (int S = 1; S <= 256 && S <= (tiles > 1 ? tiles : 1); S *= 2) {
-    const double n = (double)blocks * S * waves / 1024, rounds = std::max(1.0, n / resident);
-    const double tile = std::max(2000.0, cycles * (std::min(n, (double)resident) + 1));
-    const double t = rounds * (6000 + (double)((tiles + S - 1) / S) * tile) +
-                     (S > 1 ? 6000 + S * bytes / 1500 : 0);
+    const double each = (double)((tiles + S - 1) / S);
+    const auto round = [&](double n) { return 6000 + each * std::max(2000.0, cycles * (n + 1)); };
+    const int64_t rounds = blocks * S / once, last = blocks * S % once;
+    double t = rounds * round(resident) + (S > 1 ? 6000 + S * bytes / 1500 : 0);
+    if (rounds == 0 || (last && once == 256)) t += round((double)last * waves / 1024);
+    else t += round(resident) * last / once;
     if (S == 1 || t < least) {
       best = S;
       least = t;
@@ -297,7 +308,7 @@ int ask_pieces(const AskArgs& a, int dtype) {
   const bool large = ask_large(a, dtype, false);
   const int block = large ? 256 : ask_eight(a, dtype) ? 128 : 64;
   const double cycles = 450 + (dtype == 1 ? 2.0 : 32.0) * 2 * a.D;  // softmax, two products
-  return ask_pieces_of((rows / block + a.R) * a.Hkv, block > 64 ? 8 : 4,
+  return ask_pieces_of(ask_blocks(rows, a.R, block) * a.Hkv, block > 64 ? 8 : 4,
                        ask_resident(a, dtype, block > 64, false), large ? 2 * cycles : cycles, tiles,
                        4.0 * a.Nq * a.Hq * (a.D + 1));
 }

@@ -134,6 +134,7 @@ struct AskArgs {
   float *part_k = nullptr, *part_v = nullptr;  // [SQ,Nk,Hkv,D], or records
 };
 bool ask_large(const AskArgs& a, int dtype, bool backward);  // blocks of many queries
+int64_t ask_blocks(int64_t N, int64_t R, int rows);
 int ask_pieces_of(int64_t blocks, int waves, int resident, double cycles, int64_t tiles,
                   double bytes);
 bool ask_eight(const AskArgs& a, int dtype);  // of eight waves, fp32
