@@ -9,7 +9,7 @@
 // What bounds it: with few queries to a request the read of k and v (64 queries in 64
 // requests over a million states of 2 heads of 64, bf16: 100 us, 5.1 TB/s), with many the
 // products and the weights' arithmetic on the same SIMDs (16,384 queries over 16,384 states,
-// 4 heads of 64, bf16: 315 us, 870 TFLOP/s; the vector instructions take 70% of its cycles,
+// 4 heads of 64, bf16: 315 us, 870 TFLOP/s; the vector instructions take 66% of its cycles,
 // the matrix cores 35%; fp32, whose products run at 1/16 of that rate, is bound by them).
 // So: tiles come into LDS by loads that pass no register, one tile ahead of the products;
 // whole tiles of 64 states go without a bound's check (a state that is not there or left out
