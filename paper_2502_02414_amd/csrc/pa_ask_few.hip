@@ -91,11 +91,11 @@ template <int DP, int NT> struct States {
   }
 };
 
-// A wave's LDS in the backward: 32 rows of q and of do, 32 of p (or ds).
+// A wave's LDS in the backward: 32 rows of q and of do, and of p and ds (before them, its
+// states').
 template <int DP, int NT> constexpr int few_bwd_bytes() {
-  return States<DP, NT>::kBytes > 64 * (2 * DP + 32) + 32 * (32 * NT + 32)
-             ? States<DP, NT>::kBytes
-             : 64 * (2 * DP + 32) + 32 * (32 * NT + 32);
+  constexpr int rows = 64 * (2 * DP + 32) + 64 * (32 * NT + 32);
+  return States<DP, NT>::kBytes > rows ? States<DP, NT>::kBytes : rows;
 }
 
 // 16 bytes of virtual row `v` of a tile (32 of them from one that begins `rem` heads into a
@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   char* qt = smem + (threadIdx.x >> 6) * few_bwd_bytes<DP, NT>();
   char* dt = qt + 32 * RB;
   char* pt = qt + 64 * RB;
+  char* st = pt + 32 * PB;
 
   K32<bf16> kf[NT][NK], vf[NT][NK];
   K16<bf16> kc[ND][NT];
@@ -382,6 +383,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
         for (int i = 0; i < 4; ++i) ds[i] = x[t][i] * (dp[t][i] - delta);
         set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
+        *reinterpret_cast<bf16x4*>(st + sp + 16 * c * PB + 32 * t) = sf[c][t].v;
       }
       f32x4 dq[ND];
 #pragma unroll
@@ -403,8 +405,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
         store_lane(b, in ? dqo[c][k] : kNowhere, dq[2 * k], dq[2 * k + 1], a.scale);
     }
     // acc += (p or ds, in LDS)^T (rows, in LDS)
-    auto add = [&](const char* rows, f32x4(&acc)[NT][ND]) __attribute__((always_inline)) {
-      wave_sync();
+    auto add = [&](const char* weights, const char* rows, f32x4(&acc)[NT][ND]) __attribute__((always_inline)) {
       K16<bf16> b0[ND], b1[ND];
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
@@ -414,20 +415,16 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         K16<bf16> a0, a1;
-        ld_tr<bf16>(a0, pt, tp, 32 * t, PB);
-        ld_tr<bf16>(a1, pt, tp, 16 * PB + 32 * t, PB);
+        ld_tr<bf16>(a0, weights, tp, 32 * t, PB);
+        ld_tr<bf16>(a1, weights, tp, 16 * PB + 32 * t, PB);
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[t][d] = mma16x2(a0, b0[d], a1, b1[d], acc[t][d]);
       }
-      wave_sync();
     };
-    add(dt, dv);
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = sf[c][t].v;
-    add(qt, dk);
+    wave_sync();
+    add(pt, dt, dv);
+    add(st, qt, dk);
+    wave_sync();
   }
   if (!a.dk) return;
   const int64_t rec = (int64_t)16 * NT * a.Hkv * a.D;
