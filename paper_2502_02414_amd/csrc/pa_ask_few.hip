@@ -94,7 +94,7 @@ template <int DP, int NT> struct States {
 // A wave's LDS in the backward: 32 rows of q and of do, and of p and ds (before them, its
 // states').
 template <int DP, int NT> constexpr int few_bwd_bytes() {
-  constexpr int rows = 64 * (2 * DP + 32) + 64 * (32 * NT + 32);
+  constexpr int rows = 64 * 2 * DP + 64 * 32 * NT;
   return States<DP, NT>::kBytes > rows ? States<DP, NT>::kBytes : rows;
 }
 
@@ -257,7 +257,15 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
 template <int DP, int NT, int TH>
 __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) {
   constexpr int NK = DP / 32, ND = DP / 16;
-  constexpr int RB = 2 * DP + 32, PB = 32 * NT + 32;  // bytes of LDS rows: q and do; p and ds
+  // LDS rows of q and do in places as AskGeo's; of p and ds, which are written 8 bytes a
+  // lane for 16 rows at once, so that those meet every bank once too.  (With 32 bytes of
+  // padding between rows conflicts took 26% of the kernel's cycles: 300,000 queries over 20
+  // states of 8 heads of 32 121 us, and 106 so; over 64, where memory is the bound, no less.)
+  using Gm = AskGeo<bf16, DP>;
+  constexpr int RB = 2 * DP, PB = 32 * NT;
+  const auto key = [](int row) {
+    return NT == 4 ? 2 * (row >> 1 & 3) + (row >> 3 & 1) : 2 * (row >> 2 & 1) + (row >> 3 & 1);
+  };
   constexpr int CPR = DP / 8, NCH = CPR / 2;          // 16-byte chunks of a row; per lane of 32 rows
   using S_ = States<DP, NT>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -326,10 +334,15 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       tl.lse[c] = !in || l == -INFINITY ? INFINITY : l * kLog2e;  // (weights of 0)
     }
   };
-  const RowBase<bf16> rb = row_base<bf16>(r, RB);
   K16<bf16> ones;
   set_k16(ones, 1.f, 1.f, 1.f, 1.f);
-  const int tr = tr_base<bf16>(RB), tp = tr_base<bf16>(PB), sp = r * PB + 8 * g;
+  // (places of a tile's first 16 rows; those of step k, d or t differ by an exclusive or)
+  const int rt = 4 * g + (r >> 2), half = 8 * (r & 1), odd = r >> 1 & 1;
+  const int at_row = r * RB + (g ^ Gm::key(r)) * 16;
+  const int at_col = rt * RB + (odd ^ Gm::key(rt)) * 16 + half;
+  const int at_w = r * PB + ((g >> 1) ^ key(r)) * 16 + 8 * (g & 1);
+  const int at_wcol = rt * PB + (odd ^ key(rt)) * 16 + half;
+  const int at_in = lane / CPR * RB + ((lane % CPR) ^ Gm::key(lane / CPR)) * 16;
   const int step = 32 * me.subs * P;  // (blocks go over the rows together)
   int v = 32 * (pc * me.subs + me.sub);
   if (v < n) load(v);  // (on its way while the states come)
@@ -339,9 +352,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   for (; v < n; v += step) {
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-      const int c = lane + 64 * j;
-      *reinterpret_cast<uint4*>(qt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.q[j];
-      *reinterpret_cast<uint4*>(dt + lds_off(c / CPR, (c % CPR) * 16, RB)) = tl.d[j];
+      *reinterpret_cast<uint4*>(qt + at_in + 1024 * j) = tl.q[j];
+      *reinterpret_cast<uint4*>(dt + at_in + 1024 * j) = tl.d[j];
     }
     const float lse[2] = {tl.lse[0], tl.lse[1]};
     wave_sync();
@@ -355,8 +367,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       K32<bf16> qf[NK], of[NK];
 #pragma unroll
       for (int k = 0; k < NK; ++k) {
-        ld_row<bf16>(qf[k], qt, rb, 16 * c * RB + 64 * k);
-        ld_row<bf16>(of[k], dt, rb, 16 * c * RB + 64 * k);
+        set_wide(qf[k], *reinterpret_cast<const uint4*>(qt + (at_row ^ 64 * k) + 16 * c * RB));
+        set_wide(of[k], *reinterpret_cast<const uint4*>(dt + (at_row ^ 64 * k) + 16 * c * RB));
       }
       f32x4 x[NT], dp[NT], e;
       K16<bf16> pf[NT];
@@ -374,7 +386,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
           delta = fmaf(x[t][i], dp[t][i], delta);
         }
         set_k16(pf[t], x[t][0], x[t][1], x[t][2], x[t][3]);
-        *reinterpret_cast<bf16x4*>(pt + sp + 16 * c * PB + 32 * t) = pf[t].v;
+        *reinterpret_cast<bf16x4*>(pt + (at_w ^ 32 * t) + 16 * c * PB) = pf[t].v;
       }
       delta = groups_sum(delta);
 #pragma unroll
@@ -383,7 +395,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
 #pragma unroll
         for (int i = 0; i < 4; ++i) ds[i] = x[t][i] * (dp[t][i] - delta);
         set_k16(sf[c][t], ds[0], ds[1], ds[2], ds[3]);
-        *reinterpret_cast<bf16x4*>(st + sp + 16 * c * PB + 32 * t) = sf[c][t].v;
+        *reinterpret_cast<bf16x4*>(st + (at_w ^ 32 * t) + 16 * c * PB) = sf[c][t].v;
       }
       f32x4 dq[ND];
 #pragma unroll
@@ -409,14 +421,14 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       K16<bf16> b0[ND], b1[ND];
 #pragma unroll
       for (int d = 0; d < ND; ++d) {
-        ld_tr<bf16>(b0[d], rows, tr, 32 * d, RB);
-        ld_tr<bf16>(b1[d], rows, tr, 16 * RB + 32 * d, RB);
+        ld_tr<bf16>(b0[d], rows, at_col ^ 32 * d, 0, RB);
+        ld_tr<bf16>(b1[d], rows, at_col ^ 32 * d, 16 * RB, RB);
       }
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         K16<bf16> a0, a1;
-        ld_tr<bf16>(a0, weights, tp, 32 * t, PB);
-        ld_tr<bf16>(a1, weights, tp, 16 * PB + 32 * t, PB);
+        ld_tr<bf16>(a0, weights, at_wcol ^ 32 * t, 0, PB);
+        ld_tr<bf16>(a1, weights, at_wcol ^ 32 * t, 16 * PB, PB);
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[t][d] = mma16x2(a0, b0[d], a1, b1[d], acc[t][d]);
       }
