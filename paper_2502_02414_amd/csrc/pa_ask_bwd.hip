@@ -7,14 +7,15 @@
 // Sums over queries in one block go on in registers, over several they are records
 // that are added in order.
 //
-// delta_i is do_i.o_i; of an o in bf16 that is off by some 2^-9 |do o|, and dq_i by
-// that error times sum_j p_j k_j, which does not shrink where many states count, as
-// dq_i does.  So dq's pass corrects it: with d0 = do.o, ds' = p (dp - d0), and ds'' as it is
-// rounded for the product,
+// delta_i is do_i.o_i; of an o in bf16 that is off by some 2^-9 |do o|, of one in fp32 by what
+// its sum over the states lost, and dq_i by that error times sum_j p_j k_j, which does not
+// shrink where many states count, as dq_i does.  So dq's pass corrects it: with d0 = do.o,
+// ds' = p (dp - d0), and ds'' as it is rounded for the product,
 //   A = sum ds'' k,  B = sum p k:   dq = scale (A - (sum ds'') B),  delta = d0 + sum ds'.
-// That also takes out of A what the roundings of ds'' add up to (times any part that all k
-// have in common): dq's error is 1.3 to 1.4 times that of its own rounding to bf16, 1.4 to
-// 1.5 with sum ds' in its place.
+// In bf16 that also takes out of A what the roundings of ds'' add up to (times any part that
+// all k have in common): dq's error is 1.3 to 1.4 times that of its own rounding to bf16, 1.4
+// to 1.5 with sum ds' in its place.  In fp32 B, which is multiplied by an error, is a product
+// of p and k rounded to bf16, at 1/16 of A's time.
 //
 // What bounds it: 8,192 queries of 4 heads over 8,192 states of one of 128, bf16, take
 // 520 to 550 us, dq's pass 48% of it: 625 to 660 TFLOP/s counting the five products of
@@ -24,7 +25,7 @@
 // wave fills.  One pass over the pairs would save two products, but adds one side's sums in
 // memory, by atomics (in an order that changes) or by records of it per block: 8,192 rows of 512
 // fp32 for each of the 128 tiles of states are 2.1 GB.
-// fp32: 6,001 queries of 4 heads over 3,333 states of 2 heads of 40, 9 requests, take 88 us, the
+// fp32: 6,001 queries of 4 heads over 3,333 states of 2 heads of 40, 9 requests, take 90 us, the
 // matrix cores busy for 38% of it: 1/16 of bf16's rate, with one to two waves to a SIMD.
 #include <algorithm>
 
@@ -39,7 +40,7 @@ using namespace ask;
 template <typename T, int DP, int QT, int W>
 __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 1) k_ask_dq(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
-  constexpr bool FIX = sizeof(T) == 2;
+  constexpr bool HALF = sizeof(T) == 2;
   constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;
   __shared__ __attribute__((aligned(16))) char tiles0[2 * Gm::TB], tiles1[2 * Gm::TB];
   __shared__ __attribute__((aligned(16))) float live0[kTile], live1[kTile];
@@ -63,9 +64,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   int hq[QT];
   bool on[QT];
   float d0[QT], lse2[QT], e0[QT];
-  f32x4 E[FIX ? QT : 1];
+  f32x4 E[HALF ? QT : 1];
   WideF<T> qf[QT][Gm::NK], of[QT][Gm::NK];
-  f32x4 A[QT][Gm::ND], Bk[FIX ? QT : 1][FIX ? Gm::ND : 1];
+  f32x4 A[QT][Gm::ND], Bk[QT][Gm::ND];
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
     const int vq = v0 + (w * QT + c) * 16 + r;
@@ -89,10 +90,9 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
     if (lse2[c] == -INFINITY) lse2[c] = INFINITY;
 #pragma unroll
     for (int d = 0; d < Gm::ND; ++d) {
-      A[c][d] = zero4();
-      if constexpr (FIX) Bk[c][d] = zero4();
+      A[c][d] = Bk[c][d] = zero4();
     }
-    if constexpr (FIX) E[c] = zero4();
+    if constexpr (HALF) E[c] = zero4();
   }
   const bool busy = v0 + w * QT * 16 < n;
   const float sc = a.scale * kLog2e;
@@ -123,7 +123,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
     __builtin_amdgcn_s_setprio(0);
 #pragma unroll
     for (int t0 = 0; t0 < 4; t0 += 2) {
-      K16<T> pf[FIX ? QT : 1][2], sf[QT][2];
+      K16<bf16> pf[QT][2];
+      K16<T> sf[QT][2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -133,13 +134,13 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
           for (int i = 0; i < 4; ++i) {
             p[i] = fast_exp2(fmaf(x[t0 + u][c][i], sc, -lse2[c]));
             ds[i] = p[i] * (dp[t0 + u][c][i] - d0[c]);
-            if constexpr (FIX) e0[c] += ds[i];
+            e0[c] += ds[i];
           }
-          if constexpr (FIX) set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
+          set_k16(pf[c][u], p[0], p[1], p[2], p[3]);
           set_k16(sf[c][u], ds[0], ds[1], ds[2], ds[3]);
         }
       __builtin_amdgcn_s_setprio(1);
-      if constexpr (FIX) {
+      if constexpr (HALF) {
 #pragma unroll
         for (int c = 0; c < QT; ++c) E[c] = mma16x2(ones, sf[c][0], ones, sf[c][1], E[c]);
       }
@@ -149,10 +150,18 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
             at.columns(f.b, kt, t0 + 1, d);
           },
           [&](int d, const ColumnPair<T>& f) {
+            K16<bf16> ka, kb;
+            if constexpr (HALF) {
+              ka = f.a;
+              kb = f.b;
+            } else {
+              set_k16(ka, f.a.v[0], f.a.v[1], f.a.v[2], f.a.v[3]);
+              set_k16(kb, f.b.v[0], f.b.v[1], f.b.v[2], f.b.v[3]);
+            }
 #pragma unroll
             for (int c = 0; c < QT; ++c) {
               A[c][d] = mma16x2(f.a, sf[c][0], f.b, sf[c][1], A[c][d]);
-              if constexpr (FIX) Bk[c][d] = mma16x2(f.a, pf[c][0], f.b, pf[c][1], Bk[c][d]);
+              Bk[c][d] = mma16x2(ka, pf[c][0], kb, pf[c][1], Bk[c][d]);
             }
           });
       __builtin_amdgcn_s_setprio(0);
@@ -172,14 +181,14 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
   }
 #pragma unroll
   for (int c = 0; c < QT; ++c) {
-    if constexpr (FIX) e0[c] = groups_sum(e0[c]);
+    e0[c] = groups_sum(e0[c]);
+    const float rounded = HALF ? E[c][0] : e0[c];
     if (!on[c]) continue;
     if (a.S == 1) {
       T* DQ = reinterpret_cast<T*>(a.dq) + row[c] * a.lddq + (int64_t)hq[c] * a.D;
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
-        f32x4 x = A[c][d];
-        if constexpr (FIX) x -= Bk[c][d] * E[c][0];
+        const f32x4 x = A[c][d] - Bk[c][d] * rounded;
         if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, x * a.scale);
       }
       if (g == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c] + e0[c];
@@ -189,11 +198,11 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
       for (int d = 0; d < Gm::ND; ++d) {
         if (16 * d + 4 * g >= a.D) continue;
         store4<float>(a.part + at * a.D + 16 * d + 4 * g, A[c][d]);
-        if constexpr (FIX) store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, Bk[c][d]);
+        store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, Bk[c][d]);
       }
       if (g == 0) {
         a.part_lse[at] = e0[c];
-        if constexpr (FIX) a.part_e[at] = E[c][0];
+        if constexpr (HALF) a.part_e[at] = rounded;
         if (s == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c];
       }
     }
@@ -204,12 +213,12 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
 template <typename T>
 __device__ __forceinline__ void put_joined(const AskArgs& a, int64_t row, int hq, int c, f32x4 A,
                                            const f32x4& B, float e, float er) {
-  if constexpr (sizeof(T) == 2) A -= B * er;
+  A -= B * (sizeof(T) == 2 ? er : e);
   store4<T>(reinterpret_cast<T*>(a.dq) + row * a.lddq + (int64_t)hq * a.D + c, A * a.scale);
   if (c == 0) a.delta[(int64_t)hq * a.Nq + row] += e;
 }
 template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskArgs a, int each) {
-  constexpr bool FIX = sizeof(T) == 2;
+  constexpr bool HALF = sizeof(T) == 2;
   const int per = a.D / 4, item = threadIdx.x / per, c = (threadIdx.x % per) * 4;
   const int64_t rows = a.Nq * a.Hq, at = (int64_t)blockIdx.x * each + item, row = at / a.Hq;
   if (item >= each || at >= rows || !asked_for(a, row)) return;
@@ -217,14 +226,14 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join(AskAr
   f32x4 A = zero4(), B = zero4();
   for (int s = 0; s < a.S; ++s) {
     e += a.part_lse[s * rows + at];
-    if constexpr (FIX) er += a.part_e[s * rows + at];
+    if constexpr (HALF) er += a.part_e[s * rows + at];
     A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
-    if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+    B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
   }
   put_joined<T>(a, row, (int)(at - row * a.Hq), c, A, B, e, er);
 }
 template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join_many(AskArgs a, int P, int U) {
-  constexpr bool FIX = sizeof(T) == 2;
+  constexpr bool HALF = sizeof(T) == 2;
   __shared__ float alle[4], allr[4];
   __shared__ f32x4 lds[256];
   const int64_t rows = a.Nq * a.Hq, at = blockIdx.x, row = at / a.Hq;
@@ -235,13 +244,13 @@ template <typename T> __global__ void __launch_bounds__(256) k_ask_dq_join_many(
 #pragma unroll 8
     for (int s = u; s < a.S; s += U) {
       A += *reinterpret_cast<const f32x4*>(a.part + (s * rows + at) * a.D + c);
-      if constexpr (FIX) B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
+      B += *reinterpret_cast<const f32x4*>(a.part_b + (s * rows + at) * a.D + c);
     }
   }
   const float e = block_sum(t < a.S ? a.part_lse[t * rows + at] : 0.f, alle);
-  const float er = FIX ? block_sum(t < a.S ? a.part_e[t * rows + at] : 0.f, allr) : 0.f;
+  const float er = HALF ? block_sum(t < a.S ? a.part_e[t * rows + at] : 0.f, allr) : 0.f;
   A = add_groups(A, lds, u, U, t % P, P);
-  if constexpr (FIX) B = add_groups(B, lds, u, U, t % P, P);
+  B = add_groups(B, lds, u, U, t % P, P);
   if (u == 0 && c < a.D) put_joined<T>(a, row, (int)(at - row * a.Hq), c, A, B, e, er);
 }
 
@@ -489,14 +498,14 @@ hipError_t passes(const AskArgs& a, int dtype, hipStream_t st) {
 
 }  // namespace
 
-// Pieces of the states in dq's pass (four products, three in fp32), and of the queries in
+// Pieces of the states in dq's pass (four products, in fp32 three and one in bf16), and of the queries in
 // dk and dv's (four).
 int ask_pieces_dq(const AskArgs& a, int dtype) {
   const int rows = rows_dq(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 * 4 : 32.0 * 3) * a.D;
   return ask_pieces_of(ask_blocks(a.Nq * (a.Hq / a.Hkv), a.R, rows) * a.Hkv, rows > 64 ? 8 : 4,
                        ask_resident(a, dtype, rows > 64, true), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
-                       (dtype == 1 ? 8.0 : 4.0) * a.Nq * a.Hq * (a.D + 1));
+                       8.0 * a.Nq * a.Hq * (a.D + 1));
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {
   const int rows = rows_dkv(a, dtype), tiles_of = rows == 256 ? 2 : 1;

@@ -618,7 +618,7 @@ static size_t ask_layout(pa::AskArgs* a, int dtype, bool backward, void* ws) {
   a->delta = take(rows);
   if (a->S > 1) {
     a->part_b = take((uint64_t)a->S * rows * a->D);
-    a->part_e = take((uint64_t)a->S * rows);
+    if (dtype == PA_BF16) a->part_e = take((uint64_t)a->S * rows);
   }
   a->SQ = pa::ask_pieces_q(*a, dtype);
   if (a->SQ > 1) {

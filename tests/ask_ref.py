@@ -146,8 +146,11 @@ def backward(q, k, v, o, do, scale, q_off=None, k_off=None, mask=None):
             # hp, are ds' = p (dp - d0) as they are rounded, and p is rounded in B.  sum ds' (k
             # - B) is dq's exact value (ds' differs from ds by p (delta - d0), and sum p (k - B)
             # = 0), so that what is off is sum ds' t (k - B), at most hp sum |ds'| (|k| + |B|),
-            # and (sum r) times B's error, at most (e0 + hp sum |ds'|) hp sum p |k|.  (fp32:
-            # hp = 0, and sum ds k as it is.)
+            # and (sum r) times B's error, at most (e0 + hp sum |ds'|) hp sum p |k|.  fp32: hp =
+            # 0, and B is of p and k rounded to bf16, each by 2^-8 of it at most, its sum in 32
+            # bits: off by 2^-6.9 sum p |k|, times sum ds', e0 and what edl holds at most.  An
+            # error of a ds' in 32 bits, eds, is in sum r as well, so it meets |k| + |B|.
+            coarse = 2 ** -6.9 * (e0 + edl) if hp == 0 else 0.0
             B, pk, s1 = p @ kk, p @ kk.abs(), s0.sum(1, keepdim=True)
             q0 = s0 * s0
             spread = (q0 @ (kk * kk) - 2 * B * (q0 @ kk) + B * B * q0.sum(1, keepdim=True)).clamp(min=0)
@@ -155,7 +158,8 @@ def backward(q, k, v, o, do, scale, q_off=None, k_off=None, mask=None):
                           scale * (s0 @ kk.abs() + s1 * B.abs() + (e0 + hp * s1) * pk),
                           scale * (torch.sqrt(spread)
                                    + (e0 + hp * s1) * torch.sqrt((p * p) @ (kk * kk))),
-                          scale * ((eds + add * (s0 + e0 * p)) @ kk.abs() + add * s1 * pk))
+                          scale * ((eds + add * (s0 + e0 * p)) @ kk.abs()
+                                   + (add * s1 + eds.sum(1, keepdim=True) + coarse) * pk))
             add = U * (m / 4 + 64)
             out["dk"].put((live, hk), scale * (ds.t() @ qq), hp, scale * (ds.abs().t() @ qq.abs()),
                           scale * torch.sqrt((ds * ds).t() @ (qq * qq)),
