@@ -423,7 +423,8 @@ template <typename T, int DP, int QT, int W> hipError_t launch_dq(const AskArgs&
                      st, a);
   return hipGetLastError();
 }
-template <typename T, int DP, int KT, int W, int NR = 4> hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
+template <typename T, int DP, int KT, int W, int NR = 4>
+hipError_t launch_dkv(const AskArgs& a, hipStream_t st) {
   const int64_t slots = a.Nk / (16 * KT * W) + a.R;
   hipLaunchKernelGGL((k_ask_dkv<T, DP, KT, W, NR>), grid_of(slots * a.Hkv, a.SQ), dim3(64 * W),
                      0, st, a);
@@ -504,7 +505,8 @@ int ask_pieces_dq(const AskArgs& a, int dtype) {
   const int rows = rows_dq(a, dtype), tiles_of = rows == 256 ? 2 : 1;
   const double cycles = 600 + (dtype == 1 ? 2.0 * 4 : 32.0 * 3) * a.D;
   return ask_pieces_of(ask_blocks(a.Nq * (a.Hq / a.Hkv), a.R, rows) * a.Hkv, rows > 64 ? 8 : 4,
-                       ask_resident(a, dtype, rows > 64, true), tiles_of * cycles, (a.Nk / a.R + kTile - 1) / kTile,
+                       ask_resident(a, dtype, rows > 64, true), tiles_of * cycles,
+                       (a.Nk / a.R + kTile - 1) / kTile,
                        8.0 * a.Nq * a.Hq * (a.D + 1));
 }
 int ask_pieces_q(const AskArgs& a, int dtype) {

@@ -8,7 +8,8 @@
 // consecutive elements of its query's row of o.
 // Backward: the same for p and dp = v do^T; delta = sum_j p dp is formed here (all
 // states are at hand), so that o is not read and a lone state's ds is 0; dq^T = k^T
-// ds^T.  The sums over the queries, dv += p^T do and dk += ds^T q, need p and ds with
+// ds^T, less (sum_j ds) (sum_j p k) of ds as it is rounded, which would be 0 but for the
+// roundings.  The sums over the queries, dv += p^T do and dk += ds^T q, need p and ds with
 // queries along the product: they go through the wave's part of LDS, as do q and do.
 // A block's dk and dv are a record in the workspace, added in order.
 //
@@ -417,7 +418,8 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
         store_lane(b, in ? dqo[c][k] : kNowhere, dq[2 * k], dq[2 * k + 1], a.scale);
     }
     // acc += (p or ds, in LDS)^T (rows, in LDS)
-    auto add = [&](const char* weights, const char* rows, f32x4(&acc)[NT][ND]) __attribute__((always_inline)) {
+    auto add = [&](const char* weights, const char* rows, f32x4(&acc)[NT][ND])
+                   __attribute__((always_inline)) {
       K16<bf16> b0[ND], b1[ND];
 #pragma unroll
       for (int d = 0; d < ND; ++d) {

@@ -28,7 +28,9 @@ using namespace ask;
 // eight waves on a CU (128 VGPRs) with two tiles each took 315 us for 16,384 squared where
 // four of four waves took 340 and, at 256 VGPRs, two of four 382.
 template <typename T, int DP, int QT, int W>
-__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64 ? 4 : W == 8 || DP * sizeof(T) <= 256 ? 2 : 1)
+__global__ void __launch_bounds__(64 * W, sizeof(T) == 2 && DP <= 64             ? 4
+                                          : W == 8 || DP * sizeof(T) <= 256 ? 2
+                                                                            : 1)
 k_ask(AskArgs a) {
   using Gm = AskGeo<T, DP, W>;
   constexpr int TQ = 16 * QT * W, SHIFT = TQ == 64 ? 6 : TQ == 128 ? 7 : 8;

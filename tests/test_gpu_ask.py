@@ -519,7 +519,8 @@ def test_many_rounds_of_blocks_over_few_states(H, D, n):
     ro, rl = c.check_forward()
     o, lse = c.forward()
     at = torch.arange(n, device="cuda") % 1000
-    q, big, l = c.gq[at], torch.full((n, H, D), 7.0, dtype=BF16, device="cuda"), torch.empty(H, n, device="cuda")
+    q, big = c.gq[at], torch.full((n, H, D), 7.0, dtype=BF16, device="cuda")
+    l = torch.empty(H, n, device="cuda")
     ops.pa_cross_attention(q, c.gk, c.gv, c.par, big, l)
     assert torch.equal(big, o[at]) and torch.equal(l, lse[:, at])
 
