@@ -20,9 +20,8 @@
 // 1070.  Two tiles of queries are on their way while a wave works on two, and the blocks go
 // over the rows together, so that what is read at one time lies in one region: with a
 // range of the rows for every block and loads and stores past the caches 283 and 457 us.
-#include <algorithm>
-
 #include "pa_ask.hpp"
+#include "pa_ask_split.hpp"
 
 namespace pa {
 namespace {
@@ -172,7 +171,8 @@ __global__ void __launch_bounds__(512, DP* NT <= 128 ? 4 : 2) k_ask_few(AskArgs 
   struct Tile {
     uint4 q[C][NK];
   };
-  const int step = 16 * C * me.subs * P;  // (blocks go over the rows together)
+  // (blocks go over the rows together; at most kRowsAhead, so that v + step is below 2^31)
+  const int step = 16 * C * me.subs * P;
   auto load = [&](int v, Tile& t) __attribute__((always_inline)) {
     if (v >= n) return;
     const int i0 = G == 1 ? v : v / G;
@@ -484,36 +484,13 @@ __global__ void __launch_bounds__(256) k_ask_few_sum(AskArgs a, int per, int64_t
   }
 }
 
-// Blocks of a request, and how many waves of a block share a head.  Forward: whole rounds of
-// the blocks that are resident, each wave with some 16 tiles (us, of 64 states of 8 heads of
-// 32: 100,000 queries 27 where blocks of two tiles took 40, a million 240 and, in 1953
-// blocks, 252; 300,000 of 4 heads of 64 67 and 108).  Backward: a block per CU, since each
-// leaves a record of all states' gradients.
-struct Split {
-  int P, groups, subs, waves;
-};
-Split split_of(const AskArgs& a, bool bwd) {
-  Split s;
-  s.waves = bwd && a.D > 32 && a.max_k > 32 ? 4 : 8;
-  const int heads = a.Hkv < s.waves ? a.Hkv : s.waves;
-  s.groups = (a.Hkv + heads - 1) / heads;
-  s.subs = s.waves / heads;
-  const int64_t n = a.Nq * (a.Hq / a.Hkv) / a.R, each = (int64_t)a.R * s.groups;
-  int64_t P = 256 / each, least = 64 * s.subs;
-  if (!bwd) {
-    const int64_t resident = a.D > 32 && a.max_k > 32 ? 256 : 512, rows = n * each / s.subs;
-    const int64_t rounds = (rows / 256 / resident + 1) / 2;
-    P = (rounds ? rounds * resident : std::min(resident, std::max<int64_t>(256, rows / 128))) / each;
-    least = 32 * s.subs;
-  }
-  if (P > n / least) P = n / least;
-  s.P = P < 1 ? 1 : (int)P;
-  return s;
+FewSplit split_of(const AskArgs& a, bool bwd) {
+  return few_split(a.Nq, a.R, a.Hq, a.Hkv, a.D, a.max_k, bwd);
 }
 int tiles_of(const AskArgs& a) { return a.max_k <= 32 ? 2 : 4; }
 
 template <int DP, int NT> hipError_t launch(const AskArgs& a, bool bwd, hipStream_t st) {
-  const Split s = split_of(a, bwd);
+  const FewSplit s = split_of(a, bwd);
   const dim3 grid((uint32_t)(a.R * s.P), s.groups), block(64 * s.waves);
   constexpr int TH = DP * NT > 128 ? 256 : 512, lds = States<DP, NT>::kBytes;
   constexpr int lds_bwd = few_bwd_bytes<DP, NT>();
@@ -535,7 +512,7 @@ bool ask_few_served(const AskArgs& a, int dtype) {
 
 // Floats of the backward's records of dk, or of dv.
 int64_t ask_few_records(const AskArgs& a) {
-  const Split s = split_of(a, true);
+  const FewSplit s = split_of(a, true);
   return (int64_t)a.R * s.P * s.subs * 16 * tiles_of(a) * a.Hkv * a.D;
 }
 // (records of up to 256 MB: for more requests than that the other kernels need none)
@@ -548,7 +525,7 @@ hipError_t launch_ask_few(const AskArgs& a, hipStream_t st) { return sizes(a, fa
 hipError_t launch_ask_few_backward(const AskArgs& a, hipStream_t st) {
   hipError_t e = sizes(a, true, st);
   if (e != hipSuccess || !a.dk) return e;
-  const Split s = split_of(a, true);
+  const FewSplit s = split_of(a, true);
   const int64_t rec = (int64_t)16 * tiles_of(a) * a.Hkv * a.D;
   const int blocks = (int)((rec / 4 + 31) / 32);
   hipLaunchKernelGGL(k_ask_few_sum, dim3((uint32_t)(a.R * blocks), 2), dim3(256), 0, st, a,

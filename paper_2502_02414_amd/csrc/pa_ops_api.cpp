@@ -9,6 +9,7 @@
 #include <new>
 #include <vector>
 
+#include "pa_ask_split.hpp"
 #include "pa_internal.h"
 #include "pa_ops_internal.h"
 
@@ -557,7 +558,7 @@ static pa_status ask_params(const char* who, int64_t Nq, int64_t Nk, int dtype,
     return err(PA_ERR_INVALID, "%s: Hkv must divide Hq", who);
   if (p->D < 8 || p->D % 8 || p->D > 128)
     return err(PA_ERR_UNSUPPORTED, "%s: D must be a multiple of 8 in [8, 128]", who);
-  const int64_t most = 0x7fffffff - (1 << 21);
+  const int64_t most = pa::kMostRows;
   if (p->Hq > 4096 || p->R > (1 << 24) || Nk > most || Nq > most / (p->Hq / p->Hkv))
     return err(PA_ERR_UNSUPPORTED, "%s: Hq at most 4096, R 2^24, Nk and Nq Hq / Hkv below 2^31 - 2^21",
                who);

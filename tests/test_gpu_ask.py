@@ -533,3 +533,25 @@ def test_larger_ones_of_wide_heads_in_fp32(ql, kl, Hq, Hkv, D, mask):
     c = Case(ql, kl, Hq, Hkv, D, F32, mask, "fused")
     c.check_forward()
     c.check_backward()
+
+
+@pytest.mark.parametrize("Ns", [50, 70])
+def test_as_many_queries_as_a_call_takes(Ns):
+    """2^31 - 2^21 - 65,472 queries (34 GB of them), which come back every 65,472 rows: the
+    answers of the first ones, and nothing written in front of the answers or behind."""
+    n, period, pad = 65472 * 32767, 65472, 1 << 20
+    assert n < (1 << 31) - (1 << 21) <= n + period
+    say(f"cross attention of {n} queries over {Ns}")
+    c = Case((period,), (Ns,), 1, 1, 8, BF16, "some")
+    o, lse = c.forward()
+    q = torch.empty(n, 1, 8, dtype=BF16, device="cuda")
+    q.view(-1, period * 8).copy_(c.gq.view(1, -1))
+    out = torch.full((n + 2 * pad, 1, 8), 7.0, dtype=BF16, device="cuda")
+    l = torch.full((n + 2 * pad,), 7.0, device="cuda")
+    ws = ops.cross_attention_workspace(c.par, n, Ns, BF16)
+    ops.pa_cross_attention(q, c.gk, c.gv, c.par, out[pad:pad + n], l[pad:pad + n], ws)
+    for t, want in ((out.view(-1, 8), o.view(1, -1)), (l.view(-1, 1), lse.view(1, -1))):
+        assert (t[:pad] == 7).all() and (t[pad + n:] == 7).all()
+        rows = t[pad:pad + n].reshape(-1, want.shape[1])
+        for at in range(0, rows.shape[0], 4096):
+            assert (rows[at:at + 4096] == want).all(), at
