@@ -214,11 +214,12 @@ pa_status pa_linear_i8_workspace(int64_t N, int F, int K, size_t* bytes);
  * whose mask is not 0,
  *   s_ij = scale q_i.k_j,  lse_i = log sum_j exp(s_ij),
  *   o_i = sum_j exp(s_ij - lse_i) v_j,
- * o [Nq, Hq, D], lse [Hq, Nq] fp32.  A row without a state (or whose scores are
- * all -infinity) has o = 0 and lse = -infinity, and passes no gradient.  What k
- * and v hold where the mask is 0 is of no account, be it infinities or NaN, nor
- * what q and d_o hold in a request without a state; a state that is left out has
- * gradients of 0.
+ * o [Nq, Hq, D], lse [Hq, Nq] fp32.  A row without a state has o = 0 and lse =
+ * -infinity, and passes no gradient; so has and does, where q, v and d_o are
+ * finite, a row whose scores are all -infinity, infinities of k among what makes
+ * them so.  What k and v hold where the mask is 0 is of no account, be it
+ * infinities or NaN, nor what q and d_o hold in a request without a state; a state
+ * that is left out has gradients of 0.
  * Rows outside of the requests, in front of the first or behind the last, are
  * not read and their outputs left as they were.
  *

@@ -195,11 +195,12 @@ template <typename T, int DP, int W, int ROWS = kTile> struct TileLoad {
     for (int j = 0; j < Gm::NP; ++j)
       off[j] = col(j) < D ? (row(j) * (int)ld + col(j)) * Gm::SZ : kNowhere;
   }
-  // virtual rows of a request from row `rem` of a query's group on
-  __device__ __forceinline__ void queries(int64_t ld, int G, int rem, int D) {
+  // `rows` virtual rows of a request from row `rem` of a query's group on, the last one again
+  // behind it
+  __device__ __forceinline__ void queries(int64_t ld, int G, int rem, int D, int rows) {
 #pragma unroll
     for (int j = 0; j < Gm::NP; ++j) {
-      const uint32_t v = rem + row(j), i = G == 1 ? v : v / (uint32_t)G, g = v - i * G;
+      const uint32_t v = rem + (row(j) < rows ? row(j) : rows - 1), i = G == 1 ? v : v / (uint32_t)G, g = v - i * G;
       off[j] = col(j) < D ? (int)(i * (uint32_t)ld + g * D + col(j)) * Gm::SZ : kNowhere;
     }
   }
@@ -270,7 +271,8 @@ template <typename T, int DP, int W> struct StateTiles {
 };
 
 // Tiles of ROWS of a request's virtual rows: q's, do's behind it, and their lse (base 2) and
-// delta, [2][64] floats, with which rows past the end have weights of 0.
+// delta, [2][64] floats, with which rows past the end have weights of 0: they are the last row
+// again, whose scores are none that are NaN, where zeros' would be with a state's infinity.
 template <typename T, int DP, int W, int ROWS> struct QueryTiles {
   using Gm = AskGeo<T, DP, W, ROWS>;
   TileLoad<T, DP, W, ROWS> q, d;
@@ -286,22 +288,23 @@ template <typename T, int DP, int W, int ROWS> struct QueryTiles {
     DO = reinterpret_cast<const T*>(a.d_o) + (int64_t)h * G * D + b * lddo;
     lse = a.lse + (int64_t)h * G * Nq + b;
     delta = a.delta + (int64_t)h * G * Nq + b;
-    if (ROWS % G == 0) places(0);
+    if (ROWS % G == 0) places(0, ROWS);
   }
-  __device__ __forceinline__ void places(int rem) {
-    q.queries(ldq, G, rem, D);
-    d.queries(lddo, G, rem, D);
+  __device__ __forceinline__ void places(int rem, int rows) {
+    q.queries(ldq, G, rem, D, rows);
+    d.queries(lddo, G, rem, D, rows);
   }
   __device__ __forceinline__ void load(int v0, char* tiles) {
     const int rows = n - v0 < ROWS ? n - v0 : ROWS;
     const int i0 = G == 1 ? v0 : v0 / G, i1 = G == 1 ? v0 + rows - 1 : (v0 + rows - 1) / G;
-    if (ROWS % G) places(v0 - i0 * G);  // (tiles do not begin at a query)
+    // (tiles do not begin at a query; the last one ends inside)
+    if (ROWS % G || rows < ROWS) places(v0 - i0 * G, rows);
     const Buffer bq = buffer_of(Q + i0 * ldq, ((i1 - i0) * ldq + G * D) * Gm::SZ);
     const Buffer bd = buffer_of(DO + i0 * lddo, ((i1 - i0) * lddo + G * D) * Gm::SZ);
 #pragma unroll
     for (int j = 0; j < Gm::NP; ++j) {
-      q.load(bq, j, q.row(j) < rows, tiles);
-      d.load(bd, j, q.row(j) < rows, tiles + Gm::TB);
+      q.load(bq, j, true, tiles);
+      d.load(bd, j, true, tiles + Gm::TB);
     }
     if (threadIdx.x < kTile) {
       const bool ok = (int)threadIdx.x < rows;

@@ -184,12 +184,15 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
     e0[c] = groups_sum(e0[c]);
     const float rounded = HALF ? E[c][0] : e0[c];
     if (!on[c]) continue;
+    // (a row without states, or whose states' infinities left it with lse = -inf: 0 times those
+    // is NaN)
+    const bool none = lse2[c] == INFINITY;
     if (a.S == 1) {
       T* DQ = reinterpret_cast<T*>(a.dq) + row[c] * a.lddq + (int64_t)hq[c] * a.D;
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
         const f32x4 x = A[c][d] - Bk[c][d] * rounded;
-        if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, x * a.scale);
+        if (16 * d + 4 * g < a.D) store4<T>(DQ + 16 * d + 4 * g, none ? zero4() : x * a.scale);
       }
       if (g == 0) a.delta[(int64_t)hq[c] * a.Nq + row[c]] = d0[c] + e0[c];
     } else {
@@ -197,8 +200,8 @@ __global__ void __launch_bounds__(64 * W, W == 8 || DP * sizeof(T) <= 256 ? 2 : 
 #pragma unroll
       for (int d = 0; d < Gm::ND; ++d) {
         if (16 * d + 4 * g >= a.D) continue;
-        store4<float>(a.part + at * a.D + 16 * d + 4 * g, A[c][d]);
-        store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, Bk[c][d]);
+        store4<float>(a.part + at * a.D + 16 * d + 4 * g, none ? zero4() : A[c][d]);
+        store4<float>(a.part_b + at * a.D + 16 * d + 4 * g, none ? zero4() : Bk[c][d]);
       }
       if (g == 0) {
         a.part_lse[at] = e0[c];

@@ -110,7 +110,8 @@ __device__ __forceinline__ Buffer rows_from(const bf16* p, int64_t ld, int i, in
   return buffer_of(p + i * ld, ((last - i < 32 ? last - i : 32) * ld + width) * 2);
 }
 // 16 bytes of a row from two tiles, times f.
-__device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, const f32x4& y, float f) {
+__device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, const f32x4& y, float f,
+                                           bool none = false) {
   typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
   bf16x8 o;
 #pragma unroll
@@ -118,7 +119,8 @@ __device__ __forceinline__ void store_lane(Buffer b, int at, const f32x4& x, con
     o[i] = (bf16)(x[i] * f);
     o[i + 4] = (bf16)(y[i] * f);
   }
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), b, at, 0, 0);
+  const u32x4 bits = __builtin_bit_cast(u32x4, o);
+  __builtin_amdgcn_raw_buffer_store_b128(none ? u32x4{0, 0, 0, 0} : bits, b, at, 0, 0);
 }
 
 // Which of the block's waves works on what: `heads` of them a head each, the others on
@@ -300,32 +302,34 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
   const bool even = 32 % G == 0;  // (tiles begin at a query)
   const int last = (int)(qr.e - qr.b) - 1;
   int qo[NCH], od[NCH], dqo[2][NK];
-  auto places = [&](int rem) __attribute__((always_inline)) {
+  // (rows of q and do past the end are the last one again: zeros' scores would be NaN with a
+  // state's infinity)
+  auto places = [&](int rem, int rows) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-      const int c = lane + 64 * j;
-      qo[j] = place(c / CPR, rem, G, a.ldq, D, c % CPR * 8);
-      od[j] = place(c / CPR, rem, G, a.lddo, D, c % CPR * 8);
+      const int c = lane + 64 * j, u = rows == 32 || c / CPR < rows ? c / CPR : rows - 1;
+      qo[j] = place(u, rem, G, a.ldq, D, c % CPR * 8);
+      od[j] = place(u, rem, G, a.lddo, D, c % CPR * 8);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
       for (int k = 0; k < NK; ++k) dqo[c][k] = place(16 * c + r, rem, G, a.lddq, a.D, 32 * k + 8 * g);
   };
-  places(0);
+  places(0, 32);
   struct Tile {
     uint4 q[NCH], d[NCH];
     float lse[2];
   } tl;
   auto load = [&](int v) __attribute__((always_inline)) {
     const int i0 = G == 1 ? v : v / G;
-    if (!even) places(v - i0 * G);
+    if (n - v < 32) places(v - i0 * G, n - v);
+    else if (!even) places(v - i0 * G, 32);
     const Buffer bq = rows_from(Q, a.ldq, i0, last, G * a.D), bd = rows_from(DO, a.lddo, i0, last, G * a.D);
 #pragma unroll
     for (int j = 0; j < NCH; ++j) {
-      const bool in = v + (lane + 64 * j) / CPR < n;
-      tl.q[j] = load16(bq, in ? qo[j] : kNowhere);
-      tl.d[j] = load16(bd, in ? od[j] : kNowhere);
+      tl.q[j] = load16(bq, qo[j]);
+      tl.d[j] = load16(bd, od[j]);
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
     const int i0 = G == 1 ? v : v / G;
     const Buffer b = rows_from(DQ, a.lddq, i0, last, G * a.D);
     if (v + step < n) load(v + step);
-    if (!even) places(v - i0 * G);
+    if (!even) places(v - i0 * G, 32);
     K16<bf16> sf[2][NT];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -415,7 +419,9 @@ __global__ void __launch_bounds__(TH, TH / 256) k_ask_few_bwd(AskArgs a, int P) 
       const bool in = v + 16 * c + r < n;
 #pragma unroll
       for (int k = 0; k < NK; ++k)
-        store_lane(b, in ? dqo[c][k] : kNowhere, dq[2 * k], dq[2 * k + 1], a.scale);
+        // (a row without states: 0 times their infinities is NaN)
+        store_lane(b, in ? dqo[c][k] : kNowhere, dq[2 * k], dq[2 * k + 1], a.scale,
+                   lse[c] == INFINITY);
     }
     // acc += (p or ds, in LDS)^T (rows, in LDS)
     auto add = [&](const char* weights, const char* rows, f32x4(&acc)[NT][ND])

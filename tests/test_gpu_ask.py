@@ -555,3 +555,55 @@ def test_as_many_queries_as_a_call_takes(Ns):
         rows = t[pad:pad + n].reshape(-1, want.shape[1])
         for at in range(0, rows.shape[0], 4096):
             assert (rows[at:at + 4096] == want).all(), at
+
+
+INFINITE = [
+    # few states; more; heads that share them; pieces of states and of queries; large blocks
+    ((70, 37), (40, 20), 2, 2, 32), ((45, 9), (64, 31), 3, 1, 64), ((5, 1), (20, 1), 6, 2, 8),
+    ((70, 37), (130, 90), 2, 2, 32), ((45, 9), (100, 70), 3, 1, 72), ((3, 2), (3000, 2000), 4, 2, 64),
+    ((700, 41), (90, 65), 2, 2, 128), ((2070, 2010), (2100, 2050), 4, 4, 64),
+    ((1290, 1030), (1100, 900), 2, 2, 96)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ql,kl,Hq,Hkv,D", INFINITE)
+def test_rows_whose_scores_are_all_minus_infinity(dt, ql, kl, Hq, Hkv, D):
+    """Infinities in all states of the first request: its rows have answers and gradients of
+    0, its states gradients of 0, and the other request's are the same bits as without."""
+    say(f"scores of -infinity {dt} {ql} {kl} {Hq}/{Hkv} {D}")
+    c = Case(ql, kl, Hq, Hkv, D, DT[dt], "some")
+    c.gq[..., 0] = c.gq[..., 0].abs() + 0.5
+    o, lse = c.forward()
+    want = (o, lse.t(), *c.backward(o, lse))
+    n, m = ql[0], kl[0]
+    c.gk[:m, :, 0] = -INF
+    o, lse = c.forward()
+    assert (o[:n] == 0).all() and (lse[:, :n] == -INF).all()
+    got = (o, lse.t(), *c.backward(o, lse))
+    for t, name in zip(got[2:], ("dq", "dk", "dv")):
+        assert (t[:n if name == "dq" else m] == 0).all(), name
+    for a, b, at in zip(got, want, (n, n, n, m, m)):
+        assert torch.equal(a[at:], b[at:]) and torch.isfinite(b[at:]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("ql,kl,Hq,Hkv,D", INFINITE)
+def test_states_whose_scores_are_minus_infinity(dt, ql, kl, Hq, Hkv, D):
+    """Infinities in some states: weights of 0, so that answers and the states' gradients are
+    those of a call that leaves them out (dq is 0 times infinity where they are infinite)."""
+    c = Case(ql, kl, Hq, Hkv, D, DT[dt])
+    c.gq[..., 0] = c.gq[..., 0].abs() + 0.5
+    some = torch.arange(c.Nk, device="cuda") % 5 == 2
+    par = ops.make_cross_attention(Hq, Hkv, D, q_off=torch.tensor(c.q_off).cuda(),
+                                   k_off=torch.tensor(c.k_off).cuda(), mask=~some, max_k=max(kl))
+    par, c.par = c.par, par
+    o, lse = c.forward()
+    want = (o, lse, *c.backward(o, lse))
+    c.par = par
+    c.gk[some, :, 0] = -INF
+    o, lse = c.forward()
+    got = (o, lse, *c.backward(o, lse))
+    for i in (0, 1, 3, 4):
+        assert torch.isfinite(want[i]).all() and torch.equal(got[i], want[i]), i
+    assert (got[3][some] == 0).all() and (got[4][some] == 0).all()
+    assert torch.equal(got[2][..., 1:], want[2][..., 1:])
