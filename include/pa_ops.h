@@ -234,7 +234,7 @@ pa_status pa_linear_i8_workspace(int64_t N, int F, int K, size_t* bytes);
 typedef struct {
   int32_t R;               /* requests, >= 1                                     */
   int32_t Hq, Hkv, D;
-  float scale;             /* > 0, finite                                        */
+  float scale;             /* > 0, at most 2^127                                 */
   const int64_t* q_off;    /* [R + 1] on the device, not decreasing (values      */
   const int64_t* k_off;    /* outside of the tensor count as its ends); both, or */
                            /* both NULL with R = 1: all rows                     */

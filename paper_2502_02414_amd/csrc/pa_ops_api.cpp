@@ -564,8 +564,9 @@ static pa_status ask_params(const char* who, int64_t Nq, int64_t Nk, int dtype,
                who);
   if (((Nq * (p->Hq / p->Hkv) >> 6) + p->R) * p->Hkv > most || ((Nk >> 6) + p->R) * p->Hkv > most)
     return err(PA_ERR_UNSUPPORTED, "%s: too many rows times heads for one launch", who);
-  if (!(p->scale > 0.f) || !std::isfinite(p->scale))
-    return err(PA_ERR_INVALID, "%s: scale must be > 0 and finite", who);
+  // (scores are scaled for a power of 2: scale log2 e has to be finite too)
+  if (!(p->scale > 0.f) || !(p->scale <= 0x1p127f))
+    return err(PA_ERR_INVALID, "%s: scale must be > 0 and at most 2^127", who);
   if (!p->q_off != !p->k_off) return err(PA_ERR_INVALID, "%s: q_off and k_off go together", who);
   if (!p->q_off && p->R != 1) return err(PA_ERR_INVALID, "%s: R > 1 needs q_off and k_off", who);
   if (p->max_k < 0) return err(PA_ERR_INVALID, "%s: max_k must be >= 0", who);

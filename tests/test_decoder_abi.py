@@ -320,3 +320,13 @@ def test_elements_of_one_seed_differ_between_offsets():
         assert abs(x.double().mean().item() - 0.75) < 5 * (0.1875 / 4096) ** 0.5
     for x in (b, c):
         assert abs((a == x).double().mean().item() - 0.625) < 5 * (0.234375 / 4096) ** 0.5
+
+
+@fake_addresses
+@pytest.mark.parametrize("call", [forward, backward])
+def test_a_scale_that_the_kernels_cannot_hold(lib, call):
+    """They work with scale log2 e, which is infinite from 2.36e38 on (and would make a
+    score of 0 NaN): refused above 2^127, and nothing else is wrong with 2^127."""
+    for scale in (2.0 ** 127 * (1 + 2.0 ** -23), 2.36e38, 3.4e38):
+        refused(lib, call(lib, params(scale=scale)), INV, "scale")
+    refused(lib, call(lib, params(scale=2.0 ** 127), q=None), INV, "q is NULL")
