@@ -452,7 +452,7 @@ class QueryDecoder(BlockStack):
     where Ask is ops.pa_cross_attention of q = h Wq + bq over k, v = s Wkv + bkv (side
     by side in the rows of one product) and drop is ops.pa_dropout with the residual
     add.  N query points of C channels in all, H query heads, Hkv heads of k and v
-    (default: H), each C / H wide; drop: the probability that training drops an element
+    (default: H), each C / H wide (a multiple of 8, up to 128); drop: the probability that training drops an element
     with, seed: of its numbers.
 
     Parameters per layer: ln1_g, ln1_b, bq [C], bkv [2 Hkv C / H], bo, ln2_g, ln2_b, b1
@@ -464,8 +464,10 @@ class QueryDecoder(BlockStack):
         import torch
         self.torch = torch
         Hkv = H if Hkv is None else Hkv
-        if C % H or H % Hkv:
+        if H < 1 or Hkv < 1 or C % H or H % Hkv:
             raise ValueError("H must divide C, and Hkv H")
+        if C // H % 8 or not 8 <= C // H <= 128:
+            raise ValueError("C / H must be a multiple of 8, up to 128")
         self.N, self.C, self.H, self.Hkv, self.D = N, C, H, Hkv, C // H
         self.params, self.dt, self.ln_eps, self.dev = params, dtype, ln_eps, device
         self.pdt = B.PA_BF16 if dtype == torch.bfloat16 else B.PA_F32

@@ -330,3 +330,13 @@ def test_a_scale_that_the_kernels_cannot_hold(lib, call):
     for scale in (2.0 ** 127 * (1 + 2.0 ** -23), 2.36e38, 3.4e38):
         refused(lib, call(lib, params(scale=scale)), INV, "scale")
     refused(lib, call(lib, params(scale=2.0 ** 127), q=None), INV, "q is NULL")
+
+
+@pytest.mark.parametrize("C,H,Hkv,word", [
+    (100, 5, None, "multiple of 8"), (60, 2, None, "multiple of 8"), (512, 2, None, "128"),
+    (64, 3, None, "divide"), (64, 4, 3, "divide"), (64, 0, None, "divide"), (64, 4, 0, "divide")])
+def test_a_decoder_of_heads_that_its_attention_does_not_take(C, H, Hkv, word):
+    """Refused when it is made, before it allocates anything."""
+    from paper_2502_02414_amd.stack import QueryDecoder
+    with pytest.raises(ValueError, match=word):
+        QueryDecoder(10, C, H, [], BF, Hkv=Hkv, device="nowhere")
