@@ -1,5 +1,5 @@
-// Attention of many query points over few states, as a block stack's 16 to 64 are
-// (gfx950, bf16): a wave keeps its head's rows of k and v in registers and streams the
+// Attention of many query points over few states, as an encoder of 16 to 64 of them leaves
+// them (gfx950, bf16): a wave keeps its head's rows of k and v in registers and streams the
 // queries past them, forward and backward in one pass each.
 //
 // Forward: scores as k q^T (states are rows, queries columns), left out states as

@@ -27,8 +27,8 @@ LN2(x1) (bf16; fp32 storage keeps u).
 MLP's products in 8-bit integers (ops.pa_linear_i8).  ``SandwichStack`` has a
 norm after each half of a block as well, and learned residual scales.  A
 training step is ``forward``, ``backward`` and a step of ``adamw``'s optimizer.
-``QueryDecoder`` answers at points of its own from the states (or points) that an
-encoder left, for many requests at once.
+``QueryDecoder`` answers at points of its own from the states that an encoder left (a
+stack's points, say), for many requests at once.
 
 Parameters per layer (dict of device tensors): fp32 ln1_g, ln1_b, Wp [C,C],
 bp [C], A [C,M], b [M], a [C], Wq, bq, Wk, bk, Wv, bv (optional Wo, bo),
@@ -444,16 +444,19 @@ class SandwichStack(BlockStack):
 
 
 class QueryDecoder(BlockStack):
-    """Blocks that answer at query points from an encoder's states (a block stack's
-    points or slices' states, of any number and width), for one request or many:
+    """Blocks that answer at query points from an encoder's states, s [Ns,Cs] in the
+    storage dtype, for one request or many.  A block stack's states are the points that
+    its ``forward`` or ``infer`` answers (their gradient, of ``backward`` here, goes into
+    the stack's ``backward``; the states of its slices stay inside of it); a caller's own
+    encoder may leave any number of any width:
 
         x1 = x + drop(Ask(LN1(x), s) Wo + bo),    x2 = x1 + drop(MLP(LN2(x1)))
 
     where Ask is ops.pa_cross_attention of q = h Wq + bq over k, v = s Wkv + bkv (side
     by side in the rows of one product) and drop is ops.pa_dropout with the residual
     add.  N query points of C channels in all, H query heads, Hkv heads of k and v
-    (default: H), each C / H wide (a multiple of 8, up to 128); drop: the probability that training drops an element
-    with, seed: of its numbers.
+    (default: H), each C / H wide (a multiple of 8, up to 128); drop: the probability
+    that training drops an element with, seed: of its numbers.
 
     Parameters per layer: ln1_g, ln1_b, bq [C], bkv [2 Hkv C / H], bo, ln2_g, ln2_b, b1
     [4C], b2 fp32; Wq [C,C], Wkv [Cs, 2 Hkv C / H], Wo [C,C], W1 [C,4C], W2 [4C,C] in the

@@ -5,9 +5,11 @@ import pytest
 import torch
 
 import ask_ref as R
+import oracle
+from paper_2502_02414_amd import inputs as I
 from paper_2502_02414_amd import ops
-from paper_2502_02414_amd.stack import QueryDecoder
-from pa_cases import say
+from paper_2502_02414_amd.stack import BlockStack, QueryDecoder
+from pa_cases import dev, host, rel_l2, say
 
 pytestmark = pytest.mark.gpu
 
@@ -185,3 +187,33 @@ def test_a_frozen_encoder_and_integers():
     q = dec.infer(x, s)
     assert not torch.equal(plain, q)
     assert rel(q, plain.cpu().double()) <= 5e-2
+
+
+def test_an_encoder_that_trains_with_its_decoder():
+    """A block stack's points as the states, the decoder's gradient of them into the stack's
+    backward: against both in 64 bits.  The bar is that of four passes (stack and decoder,
+    forward and backward), 1e-5 each."""
+    n, C, H, M = 700, 64, 4, 16
+    w = I.small("stack", n, C, H, M, "f32", geometry="normal")
+    x, G = I.make_x(w, n), I.make_layer_gumbel(w, 0, n)
+    p = I.make_block_params(w, 0)
+    put = lambda k, v: float(v) if k == "b_t" else dev(v, "f32")
+    enc = BlockStack(n, C, H, M, [{k: put(k, v) for k, v in p.items()}], F32, w.tau0, w.tau_min, w.eps)
+    dec, xq, _, dy = make(300, C, H, H, C, 1, 2, F32)
+    s = enc.forward(dev(x, "f32"), [dev(G, "f32")])
+    out = dec.forward(xq, s)
+    dxq, ds, grads = dec.backward(dy.clone())
+    dx, egrads = enc.backward(ds)
+    s64, caches = oracle.stack_forward(x, [G], [p], w.tau0, w.tau_min, w.eps, H)
+    P = [{k: v.cpu().double().requires_grad_() for k, v in q.items()} for q in dec.params]
+    leaf, q64 = torch.tensor(s64).double().requires_grad_(), xq.cpu().double().requires_grad_()
+    ref = blocks(dec, P, q64, leaf, None, None, None, None)
+    (ref * dy.cpu().double()).sum().backward()
+    rdx, rgr = oracle.stack_backward(leaf.grad.numpy(), [G], [p], w.tau0, w.tau_min, w.eps, H, caches)
+    assert rel(out, ref.detach()) <= 4e-5 and rel(dxq, q64.grad) <= 4e-5
+    assert rel(ds, leaf.grad) <= 4e-5 and rel_l2(host(dx), rdx) <= 4e-5
+    for l, g in enumerate(grads):
+        for k in ("dWq", "dWo", "dW1", "dW2", "dln1_g", "dbo"):
+            assert rel(g[k], P[l][k[1:]].grad) <= 4e-5, (l, k)
+    for k in ("dW1", "dW2", "dWp", "dln1_g"):
+        assert rel_l2(host(egrads[0][k]), rgr[0][k]) <= 4e-5, k
