@@ -340,3 +340,18 @@ def test_a_decoder_of_heads_that_its_attention_does_not_take(C, H, Hkv, word):
     from paper_2502_02414_amd.stack import QueryDecoder
     with pytest.raises(ValueError, match=word):
         QueryDecoder(10, C, H, [], BF, Hkv=Hkv, device="nowhere")
+
+
+@fake_addresses
+def test_where_the_records_of_few_states_end(lib):
+    """The backward of few states keeps a record of 64 states for a block, up to 2^25 floats:
+    2,048 requests of 8 heads of 32, and not one more."""
+    n, sizes = ctypes.c_size_t(0), []
+    for requests in (2048, 2049):
+        p = params(R=requests, Hq=8, Hkv=8, D=32, max_k=64, q_off=FAKE, k_off=FAKE)
+        assert lib.pa_cross_attention_workspace(3 * requests, 64 * requests, 1, ctypes.byref(p), 1,
+                                                ctypes.byref(n)) == B.PA_OK
+        sizes.append(n.value)
+    assert sizes[0] == 2 * 4 * (1 << 25)
+    # delta alone (and no pieces): a float for each row and head
+    assert sizes[1] < 3 * 2049 * 8 * 4 + 256

@@ -607,3 +607,62 @@ def test_states_whose_scores_are_minus_infinity(dt, ql, kl, Hq, Hkv, D):
         assert torch.isfinite(want[i]).all() and torch.equal(got[i], want[i]), i
     assert (got[3][some] == 0).all() and (got[4][some] == 0).all()
     assert torch.equal(got[2][..., 1:], want[2][..., 1:])
+
+
+def test_few_states_of_more_requests_than_records_are_kept_for():
+    """2,100 requests of up to 64 states: the forward of few states, the backward of any
+    number (the records of more than 2,048 requests would be too many)."""
+    R_ = 2100
+    ql, kl = [(3 * r) % 4 for r in range(R_)], [(7 * r) % 65 for r in range(R_)]
+    say(f"cross attention of {R_} requests of few states")
+    c = Case(tuple(ql), tuple(kl), 2, 1, 32, BF16, "some", first=2, tail=3)
+    few = ops.cross_attention_workspace(c.par, c.Nq, c.Nk, BF16, True).numel()
+    assert few < 2 * 2049 * 8 * 64 * 32 * 4  # (no records)
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("ql,kl,Hq,Hkv,D", [((2, 20000) + (1, 0, 3) * 20, (64, 40) + (7, 64, 33) * 20, 2, 2, 32),
+                                            ((6000,) + (1,) * 30, (3,) + (64,) * 30, 6, 2, 64)])
+def test_one_request_has_most_of_the_queries_of_few_states(ql, kl, Hq, Hkv, D):
+    say(f"cross attention of few states, {max(ql)} of {sum(ql)} queries in one request")
+    c = Case(ql, kl, Hq, Hkv, D, BF16, "some", tail=1)
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("more", [0, 1])
+def test_few_states_by_the_million(more):
+    """As many requests as the forward of few states takes, and one more."""
+    c = Case((3, 70, 1), (5, 60, 64), 16, 16, 8, BF16, "some", packed=True)
+    n = (1 << 19) - 3
+    far = lambda off: torch.tensor([0] * n + off + [off[-1]] * (n + 3 + more)).cuda()
+    c.par = ops.make_cross_attention(16, 16, 8, q_off=far(c.q_off), k_off=far(c.k_off),
+                                     mask=c.mask.cuda(), max_k=64)
+    assert c.par.st.R == (1 << 20) + more
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("kl", [(50, 64), (300, 200)])
+def test_queries_beyond_32_bits(kl):
+    """q, o, do and dq in rows so far apart that their elements lie beyond 2^32: the same as
+    close by (few states, and more)."""
+    c = Case((40, 1060), kl, 4, 2, 64, BF16, "some")
+    o, lse = c.forward()
+    want = c.backward(o, lse)
+    pitch = 1 << 22
+    wide = torch.empty(c.Nq, pitch, dtype=BF16, device="cuda")  # 9.2 GB
+    assert wide.numel() > 1 << 32
+    at = lambda i: wide[:, 1024 * i:1024 * i + 256].unflatten(1, (4, 64))
+    q, far_o, do, dq = (at(i) for i in range(4))
+    q.copy_(c.gq)
+    do.copy_(c.gdo)
+    far_o.fill_(7.0)
+    l2 = torch.empty_like(lse)
+    ops.pa_cross_attention(q, c.gk, c.gv, c.par, far_o, l2, c.ws())
+    assert torch.equal(far_o, o) and torch.equal(lse, l2)
+    dk, dv = c.out(c.k), c.out(c.v)
+    ops.pa_cross_attention_backward(q, c.gk, c.gv, far_o, l2, c.par, do, dq, dk, dv, c.ws(True))
+    for a, b in zip((dq, dk, dv), want):
+        assert torch.equal(a, b)
