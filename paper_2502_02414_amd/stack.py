@@ -594,6 +594,8 @@ class QueryDecoder(BlockStack):
         N, C = self.N, self.C
         s, par, L = self.states, self.par, len(self.params)
         grads, ds = [None] * L, self._e(*s.shape)
+        if not L:
+            ds.zero_()
         for l in reversed(range(L)):
             p, c, g = self.params[l], self.caches[l], {}
             dh2 = self._mlp_backward(p, c, g, self._drop_grad(dy, l, 1))

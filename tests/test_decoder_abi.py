@@ -355,3 +355,14 @@ def test_where_the_records_of_few_states_end(lib):
     assert sizes[0] == 2 * 4 * (1 << 25)
     # delta alone (and no pieces): a float for each row and head
     assert sizes[1] < 3 * 2049 * 8 * 4 + 256
+
+
+def test_a_decoder_of_no_layers_gives_its_states_no_gradient():
+    """(What was in memory was returned.)"""
+    from paper_2502_02414_amd.stack import QueryDecoder
+    dec = QueryDecoder(5, 16, 2, [], F32, device="cpu")
+    dec._e = lambda *s, dt=None: torch.full(s, float("nan"), dtype=dt or F32)
+    x, s, dy = torch.ones(5, 16), torch.ones(3, 24), torch.full((5, 16), 2.0)
+    assert torch.equal(dec.forward(x, s), x)
+    dx, ds, grads = dec.backward(dy)
+    assert torch.equal(dx, dy) and torch.equal(ds, torch.zeros(3, 24)) and grads == []
