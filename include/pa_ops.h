@@ -230,6 +230,8 @@ pa_status pa_linear_i8_workspace(int64_t N, int F, int K, size_t* bytes);
  * may lie side by side in the rows of one product, and dk and dv so too.  Scores,
  * softmax statistics and sums are fp32; for bf16 the weights, and in the backward
  * ds, are rounded to bf16 for the products over the states and over the queries.
+ * In the backward of fp32 the weights and k are so for one product, sum_j p_ij k_j,
+ * which only multiplies the error that d_o.o has as a row's sum of p d_o.v.
  * --------------------------------------------------------------------- */
 typedef struct {
   int32_t R;               /* requests, >= 1                                     */
@@ -240,8 +242,9 @@ typedef struct {
                            /* both NULL with R = 1: all rows                     */
   const uint8_t* mask;     /* [Nk] on the device, nullable: 0 leaves a state out */
   int64_t max_k;           /* states of the longest request, 0: not known, which  */
-                           /* may be slower; a request of more than that may have */
-                           /* NaN for its answers and gradients                   */
+                           /* may be slower; a promise, for every replay of a     */
+                           /* captured call too: a request of more than that may  */
+                           /* have NaN for its answers and gradients              */
 } pa_cross_attention_params;
 
 /* lse nullable.  Workspace: pa_cross_attention_workspace bytes (may be 0). */

@@ -17,16 +17,18 @@
 // to 1.5 with sum ds' in its place.  In fp32 B, which is multiplied by an error, is a product
 // of p and k rounded to bf16, at 1/16 of A's time.
 //
-// What bounds it: 8,192 queries of 4 heads over 8,192 states of one of 128, bf16, take
-// 520 to 550 us, dq's pass 48% of it: 625 to 660 TFLOP/s counting the five products of
-// the formulas, 880 to 920 with the two that are formed twice.  Two waves of a SIMD are all that
-// the registers leave (K, V or Q, dO rows, and two sums of the width, per wave), and a tile's
-// LDS reads, products and exponentials of one wait for each other more often than the other
-// wave fills.  One pass over the pairs would save two products, but adds one side's sums in
-// memory, by atomics (in an order that changes) or by records of it per block: 8,192 rows of 512
-// fp32 for each of the 128 tiles of states are 2.1 GB.
+// What bounds it: the products.  8,192 queries of 4 heads over 8,192 states of one of 128,
+// bf16, take 505 to 535 us, dq's pass half of it: 640 to 680 TFLOP/s counting the five products
+// of the formulas, 1030 to 1090 with the eight that are formed (scores and dp twice, and B),
+// 85 to 90% of what a large library product reaches on this card.  The matrix cores are busy
+// for 46 to 50% (dq) and 43% of the passes' cycles (a library product at 1205 TFLOP/s for 48%),
+// vector instructions take 38% and 29%, LDS 38% and 50%.  One pass over the pairs would save
+// two products, but adds one side's sums in memory, by atomics (in an order that changes) or
+// by records of it per block: 8,192 rows of 512 fp32 for each of the 128 tiles of states are
+// 2.1 GB.
 // fp32: 6,001 queries of 4 heads over 3,333 states of 2 heads of 40, 9 requests, take 90 us, the
-// matrix cores busy for 38% of it: 1/16 of bf16's rate, with one to two waves to a SIMD.
+// matrix cores busy for 30% (dq) and 35% of the passes' cycles: 1/16 of bf16's rate, on one wave
+// to a SIMD (0.8 and 1.0 on average).
 #include <algorithm>
 
 #include "pa_ask.hpp"

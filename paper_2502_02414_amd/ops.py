@@ -689,8 +689,9 @@ def make_cross_attention(Hq, Hkv, D, scale=None, q_off=None, k_off=None, mask=No
     """Hq query heads over Hkv heads of states, D wide; scale: 1 / sqrt(D) where none
     is given; q_off, k_off: int64 [requests + 1], where the rows of each request begin
     and end (None: one request of all rows); mask: bool or uint8 [Nk], false for the
-    states that are left out; max_k: the states of the longest request, if known (one of
-    more than that may be answered with NaN)."""
+    states that are left out; max_k: the states of the longest request, if known, which is a
+    promise: one of more than that, by what the offsets say when the call (or a captured
+    one's replay) runs, may be answered with NaN."""
     torch = _torch()
     Hq, Hkv, D, R, ptr = int(Hq), int(Hkv), int(D), 1, {}
     if (q_off is None) != (k_off is None):

@@ -564,7 +564,8 @@ class QueryDecoder(BlockStack):
         (``requests``; None: all of them all).  step: of the training, names the dropped
         elements.  Those of a captured graph, whose step stands still, are named by
         offset_dev, a device int64 [1] that counts 2 x layers a step (its own numbers follow
-        step's: 0 there).  Keeps what the backward needs."""
+        step's: 0 there) and that ``backward`` reads again, so that it moves on behind that.
+        Keeps what the backward needs."""
         N, C = self.N, self.C
         par = self.one if par is None else par
         self.caches, self.states, self.par = [], s, par
